@@ -465,15 +465,15 @@ def _own(s):
     case = s["case"]
     ctx, B, kind = _context(s), case["batch"], case["kind"]
     if kind in ("append8", "attend8", "attend8_rows"):
-        kv = P.make_kv8_view(s["k8"], s["v8"], s["k_scale"], s["v_scale"], s["k_tail"], s["v_tail"], s["lens"],
+        kv = P.make_bytekv_view(s["k8"], s["v8"], s["k_scale"], s["v_scale"], s["k_tail"], s["v_tail"], s["lens"],
                              page_table=s["table"], max_seq_len=s["max_len"])
         if kind == "append8":
-            ctx.kv8_append(s["new_k"], s["new_v"], s["new"], kv, B)
+            ctx.bytekv_append(s["new_k"], s["new_v"], s["new"], kv, B)
             return [s["k8"], s["k_scale"], s["v8"], s["v_scale"], s["k_tail"], s["v_tail"]]
         if kind == "attend8":
-            ctx.kv8_decode_attn(s["q"], kv, B, s["out"], s["lse"])
+            ctx.bytekv_decode_attn(s["q"], kv, B, s["out"], s["lse"])
         else:
-            ctx.kv8_sparse_decode_attn(s["q"], kv, s["idx"], s["count"], B, s["out"], s["lse"])
+            ctx.bytekv_sparse_decode_attn(s["q"], kv, s["idx"], s["count"], B, s["out"], s["lse"])
         return [s["out"], s["lse"]]
     kv = P.make_view(s["k"], s["v"] if kind == "block_step" else s["k"], s["lens"], page_table=s["table"],
                      max_seq_len=s["max_len"])
