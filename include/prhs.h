@@ -313,6 +313,118 @@ prhs_status prhs_delta(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, con
                        const int32_t* count, int32_t idx_stride, int32_t batch, float* out_delta,
                        void* stream);
 
+/* ------------------------------------------------------------------------ the 8-bit KV cache
+ * (No counterpart in the paper.)  Rows of 128 one-byte floating-point codes; sixteen consecutive positions of one
+ * KV head form a block with one fp32 scale for its keys and one for its values:
+ *     x ~ scale * code,  scale = 2^max(ceil(log2(amax / top)), -126),  code = x / scale rounded to nearest even,
+ * amax the block's largest magnitude, top = 448 (e4m3) or 57344 (e5m2).  Only whole blocks are quantised.  The
+ * open block (the last t_b mod 16 positions) stays bf16 in a tail of 16 rows per (sequence, KV head), position
+ * i at row i mod 16; so the cache's content does not depend on how the rows were split over calls.
+ *   contiguous: row i of (b, kvh) is at  k + b*stride_outer + kvh*stride_head + i*128           (bytes)
+ *               its block's scale at     k_scale + b*scale_stride_outer + kvh*scale_stride_head + i/16
+ *   paged:      page = page_table[b*page_table_stride + i/16]
+ *               row at    k + page*stride_outer + kvh*stride_head + (i%16)*128
+ *               scale at  k_scale + page*scale_stride_outer + kvh*scale_stride_head
+ * v and v_scale use the same strides.  Codes and tails are 16-byte aligned, code strides positive multiples of 128,
+ * scale strides positive; a contiguous cache holds whole blocks (max_seq_len rounded up to 16 positions); a
+ * page table row holds max_seq_len / 16 entries, rounded up.  Fewer than 2^32 rows and 2^32 scales between the
+ * bases and the last one addressed. */
+#define PRHS_BYTEKV_E4M3 0
+#define PRHS_BYTEKV_E5M2 1
+typedef struct {
+  void* k;                   /* device codes; written by prhs_bytekv_append only                        */
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  void* k_tail;              /* device bf16 [B][Hkv][16][128]                                        */
+  void* v_tail;
+  int64_t stride_outer, stride_head;
+  int64_t scale_stride_outer, scale_stride_head;
+  const int32_t* page_table; /* device [B][page_table_stride] or NULL                                */
+  const int32_t* seq_lens;   /* device [B]: t_b; after the rows that prhs_bytekv_append brings in       */
+  int32_t page_table_stride;
+  int32_t max_seq_len;       /* host-side upper bound of every t_b; 0 = max_context                  */
+  int32_t num_pages;
+  int32_t format;            /* PRHS_BYTEKV_*                                                           */
+} prhs_bytekv_view;
+
+/* Append rows to the 8-bit cache: positions [t_b - new_lens[b], t_b) of every sequence, a prompt, a chunk or a
+ * token.  Blocks that become whole are quantised (the rows they already had come from the tail), rows of the
+ * block that stays open go to the tail; nothing else is written.
+ *   new_k, new_v  device bf16; row j of (b, kvh) at  b*stride_seq + kvh*stride_head + j*stride_row  (elements),
+ *                 16-byte aligned, strides multiples of 8
+ *   new_lens      device int32 [batch], 0 <= new_lens[b] <= min(max_new, t_b); a sequence that breaks this, or whose
+ *                 t_b exceeds max_seq_len, is left as it was and recorded (PRHS_FLAG_BAD_LENGTH)
+ *   max_new       host-side upper bound of new_lens (sizes the launch)
+ * A block with an infinity or a NaN is recorded (PRHS_FLAG_NONFINITE): infinities are stored as the largest code,
+ * NaNs as NaN, and the block's scale follows the largest exponent. */
+prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const void* new_k, const void* new_v, int64_t stride_seq,
+                            int64_t stride_head, int64_t stride_row, const int32_t* new_lens, int32_t max_new, int32_t batch,
+                            void* stream);
+
+/* prhs_dense_decode_attn over the 8-bit cache: attention over all i < t_b.  t_b = 0 gives a zero output row and
+ * lse = -inf.  q and out 16-byte aligned. */
+prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
+                                 void* stream);
+
+/* prhs_sparse_decode_attn over the 8-bit cache: same lists, same outputs. */
+prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, const int32_t* idx,
+                                        const int32_t* count, int32_t idx_stride, int32_t batch, void* out, float* out_lse,
+                                        void* stream);
+
+/* ------------------------------------------------------------- attention over selected blocks
+ * (No counterpart in the paper, whose retrieval scores every key.)  A block is sixteen consecutive positions (a
+ * page of a paged cache).  Of its keys the caller's cache keeps, per KV head and coordinate, the minimum and the
+ * maximum as int8 codes with one scale:  code = rint(x / scale), scale = 2^max(ceil(log2(amax / 127)), -126).
+ * A query head's score of a block is the largest q . k inside those bounds with q coded the same way per head:
+ *     score = sum_d max(q8_d lo8_d, q8_d hi8_d) * scale_block * scale_q,
+ * an exact integer sum and two powers of two, so scores are the same on every machine and ties are real.
+ *   contiguous: block j of (b, kvh) has index b*stride_outer + kvh*stride_head + j
+ *   paged:      page*stride_outer + kvh*stride_head
+ *   codes + index*256: 128 minima, then 128 maxima;  scale + index */
+typedef struct {
+  int8_t* codes;             /* device, 16-byte aligned */
+  float* scale;              /* device */
+  int64_t stride_outer, stride_head; /* in blocks, positive */
+} prhs_block_bounds_view;
+
+typedef struct {
+  int32_t top_blocks;        /* blocks of highest score taken from the middle; equal scores: lower block first   */
+  int32_t sink_blocks;       /* the first blocks, always taken                                                   */
+  int32_t recent_blocks;     /* the last blocks (the open one included), always taken                            */
+  uint32_t flags;            /* 0 or PRHS_GROUP_SETS: one set per KV head, ranked by the group's largest score   */
+} prhs_block_schedule;
+
+/* Bounds of the blocks that hold positions [first[b], t_b); first = NULL: of all blocks.  Every other entry stays as it
+ * was.  max_new: host-side upper bound of t_b - first[b] (sizes the launch); 0 = max_seq_len.  A sequence with
+ * first[b] outside [0, t_b], more new positions than max_new or t_b above max_seq_len is skipped and recorded
+ * (PRHS_FLAG_BAD_LENGTH).  A page-table row holds max_seq_len / 16 entries, rounded up, in these calls. */
+prhs_status prhs_block_bounds(prhs_ctx* ctx, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds, const int32_t* first,
+                              int32_t max_new, int32_t batch, void* stream);
+
+/* Score and select.  With n_b = ceil(t_b / 16): blocks [0, min(sink, n_b)), the best top_blocks of the middle, and the last
+ * `recent` blocks, ascending and unique.
+ *   out_blocks device int32 [batch][units][blocks_stride], -1 past the count; units = Hq, or Hkv with
+ *              PRHS_GROUP_SETS; blocks_stride >= min(top + sink + recent, ceil(max_seq_len / 16))
+ *   out_count  device int32 [batch][units]
+ * Bounds of all middle blocks must be up to date. */
+prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
+                            const prhs_block_schedule* sched, int32_t batch, int32_t* out_blocks, int32_t blocks_stride,
+                            int32_t* out_count, void* stream);
+
+/* Softmax attention over the positions of the listed blocks (flags as above says how the lists are indexed).  Order is
+ * free, a block listed twice is attended twice; a block outside [0, n_b) is skipped and recorded
+ * (PRHS_FLAG_BAD_INDEX).  An empty list gives a zero output row and lse = -inf.
+ *   out device bf16 [batch][Hq][128], out_lse device fp32 [batch][Hq] or NULL; q and out 16-byte aligned */
+prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
+                                   int32_t blocks_stride, uint32_t flags, int32_t batch, void* out, float* out_lse, void* stream);
+
+/* One decode step: the bounds of every sequence's last block (the one that holds the current token) are brought up to
+ * date, then prhs_block_topk and prhs_block_decode_attn.  recent_blocks >= 1. */
+prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
+                                   const prhs_block_schedule* sched, int32_t batch, void* out, float* out_lse, int32_t* out_blocks,
+                                   int32_t blocks_stride, int32_t* out_count, void* stream);
+
 /* Largest index-list length any call can produce: S0 + k + 2*r*m + W from prhs_config. */
 int32_t prhs_index_capacity(const prhs_ctx* ctx);
 
@@ -350,6 +462,8 @@ int32_t prhs_scores_ld(const prhs_ctx* ctx);
 #define PRHS_FLAG_BAD_PAGE        2u /* a page id outside [0, num_pages) was skipped          */
 #define PRHS_FLAG_SELECT_FALLBACK 4u /* informational: selection took the multi-pass path     */
 #define PRHS_FLAG_TIMEOUT         8u /* a bounded wait on a TMA barrier ran out; results invalid */
+#define PRHS_FLAG_BAD_LENGTH     16u /* a sequence whose lengths contradict each other was skipped */
+#define PRHS_FLAG_NONFINITE      32u /* an infinity or a NaN went into the 8-bit cache            */
 prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags);
 
 /* Per-kernel device timing for benchmarks (no counterpart in the paper: measurement support).

@@ -22,6 +22,8 @@ PRHS_DILATE_ANCHOR = 1
 PRHS_WANT_DELTA = 2
 PRHS_GROUP_SETS = 4
 PRHS_FLAG_BAD_INDEX, PRHS_FLAG_BAD_PAGE, PRHS_FLAG_SELECT_FALLBACK, PRHS_FLAG_TIMEOUT = 1, 2, 4, 8
+PRHS_FLAG_BAD_LENGTH, PRHS_FLAG_NONFINITE = 16, 32
+PRHS_BYTEKV_E4M3, PRHS_BYTEKV_E5M2 = 0, 1
 PRHS_CFG_NO_TMA = 1
 PRHS_CFG_TMA_GATHER = 2
 PRHS_CFG_MMA_SYNC_SCORE = 4
@@ -34,7 +36,9 @@ EXPORTS = ["prhs_create", "prhs_destroy", "prhs_score_topk", "prhs_build_index_s
            "prhs_get_shared_set", "prhs_get_scores", "prhs_scores_ld", "prhs_check",
            "prhs_launch_count", "prhs_selftest_wait", "prhs_state_bytes", "prhs_state_export", "prhs_state_import", "prhs_validate_index_lists", "prhs_last_error", "prhs_version", "prhs_profile_begin",
            "prhs_profile_end", "prhs_kernel_kind_name", "prhs_sparse_decode_attn_noalloc", "prhs_get_gate",
-           "prhs_noalloc_check", "prhs_gather_probe"]
+           "prhs_noalloc_check", "prhs_gather_probe", "prhs_bytekv_append", "prhs_bytekv_decode_attn",
+           "prhs_bytekv_sparse_decode_attn", "prhs_block_bounds", "prhs_block_topk", "prhs_block_decode_attn",
+           "prhs_block_decode_step"]
 NOALLOC_MAX_UNITS = 1024
 KERNEL_KINDS = 6
 
@@ -67,6 +71,21 @@ class Schedule(C.Structure):
                 ("sim_threshold", C.c_float)]
 
 
+class ByteKvView(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail")] + \
+               [(n, C.c_int64) for n in ("stride_outer", "stride_head", "scale_stride_outer", "scale_stride_head")] + \
+               [("page_table", C.c_void_p), ("seq_lens", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("page_table_stride", "max_seq_len", "num_pages", "format")]
+
+
+class BlockBoundsView(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p), ("stride_outer", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class BlockSchedule(C.Structure):
+    _fields_ = [("top_blocks", C.c_int32), ("sink_blocks", C.c_int32), ("recent_blocks", C.c_int32), ("flags", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -94,6 +113,15 @@ def load() -> C.CDLL:
         "prhs_decode_step_host": (st, [vp, i32, i32, C.POINTER(Schedule), vp, vp, vp, vp, C.POINTER(KvView), i32, vp, vp]),
         "prhs_decode_step_host_async": (st, [vp, i32, i32, C.POINTER(Schedule), vp, vp, vp, vp, C.POINTER(KvView), i32,
                                               vp, vp]),
+        "prhs_bytekv_append": (st, [vp, C.POINTER(ByteKvView), vp, vp, C.c_int64, C.c_int64, C.c_int64, vp, i32, i32, vp]),
+        "prhs_bytekv_decode_attn": (st, [vp, vp, C.POINTER(ByteKvView), i32, vp, vp, vp]),
+        "prhs_bytekv_sparse_decode_attn": (st, [vp, vp, C.POINTER(ByteKvView), vp, vp, i32, i32, vp, vp, vp]),
+        "prhs_block_bounds": (st, [vp, C.POINTER(KvView), C.POINTER(BlockBoundsView), vp, i32, i32, vp]),
+        "prhs_block_topk": (st, [vp, vp, C.POINTER(KvView), C.POINTER(BlockBoundsView), C.POINTER(BlockSchedule), i32, vp,
+                                 i32, vp, vp]),
+        "prhs_block_decode_attn": (st, [vp, vp, C.POINTER(KvView), vp, vp, i32, C.c_uint32, i32, vp, vp, vp]),
+        "prhs_block_decode_step": (st, [vp, vp, C.POINTER(KvView), C.POINTER(BlockBoundsView), C.POINTER(BlockSchedule), i32,
+                                        vp, vp, vp, i32, vp, vp]),
         "prhs_delta": (st, [vp, vp, C.POINTER(KvView), vp, vp, i32, i32, vp, vp]),
         "prhs_index_capacity": (i32, [vp]),
         "prhs_get_index_set": (st, [vp, i32, vp, vp, vp]),
@@ -155,6 +183,57 @@ def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
                   seq_lens.data_ptr(), max_seq_len, k.shape[0] if page_table is not None else 0)
     view._keep = (k, v, seq_lens, page_table)
     return view
+
+
+def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table=None, max_seq_len=0) -> ByteKvView:
+    """View of an 8-bit cache.
+
+    Codes (torch.float8_e4m3fn or torch.float8_e5m2) contiguous [B][Hkv][cap][128], cap a multiple of 16, with
+    fp32 scales [B][Hkv][cap/16]; or paged [pool][Hkv][16][128] with scales [pool][Hkv].  Tails bf16
+    [B][Hkv][16][128].
+    """
+    fmt = {torch.float8_e4m3fn: PRHS_BYTEKV_E4M3, torch.float8_e5m2: PRHS_BYTEKV_E5M2}[k.dtype]
+    assert v.dtype == k.dtype and k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride()
+    assert k.shape[-1] == 128 and k.stride(-1) == 1 and k.stride(-2) == 128 and k.shape[2] % 16 == 0
+    paged = page_table is not None
+    assert k_scale.dtype == torch.float32 and v_scale.dtype == torch.float32 and k_scale.stride() == v_scale.stride()
+    want = (k.shape[0], k.shape[1]) if paged else (k.shape[0], k.shape[1], k.shape[2] // 16)
+    assert k_scale.shape == v_scale.shape == want and (paged or k_scale.stride(2) == 1)
+    assert k_tail.dtype == v_tail.dtype == torch.bfloat16 and k_tail.shape == v_tail.shape
+    assert k_tail.shape[1:] == (k.shape[1], 16, 128) and k_tail.shape[0] >= seq_lens.shape[0]
+    assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous()
+    if paged:
+        assert k.shape[2] == 16 and page_table.dtype == torch.int32 and page_table.stride(-1) == 1
+    else:
+        assert k.shape[0] >= seq_lens.shape[0] and max_seq_len <= k.shape[2]
+    tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens) + ((page_table,) if paged else ())
+    _same_device(*tensors)
+    view = ByteKvView(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(k_tail), _ptr(v_tail),
+                      k.stride(0), k.stride(1), k_scale.stride(0), k_scale.stride(1),
+                      page_table.data_ptr() if paged else None, seq_lens.data_ptr(),
+                      page_table.stride(0) if paged else 0, max_seq_len,
+                      k.shape[0] if paged else 0, fmt)
+    view._keep = tensors
+    return view
+
+
+def make_block_bounds(codes, scale) -> BlockBoundsView:
+    """Bounds int8 [B][Hkv][blocks][2][128] with scales fp32 [B][Hkv][blocks], or per page [pool][Hkv][2][128], [pool][Hkv]."""
+    assert codes.dtype == torch.int8 and scale.dtype == torch.float32 and codes.shape[-2:] == (2, 128)
+    assert codes.shape[:-2] == scale.shape and codes.is_contiguous() and scale.is_contiguous()
+    _same_device(codes, scale)
+    view = BlockBoundsView(codes.data_ptr(), scale.data_ptr(), scale.stride(0), scale.stride(1))
+    view._keep = (codes, scale)
+    return view
+
+
+def make_block_schedule(top_blocks, sink_blocks=1, recent_blocks=1, flags=0) -> BlockSchedule:
+    return BlockSchedule(top_blocks, sink_blocks, recent_blocks, flags)
+
+
+def _same_device(*tensors):
+    dev = tensors[0].device
+    assert dev.type == "cuda" and all(t.device == dev for t in tensors), "tensors of a call must be on one CUDA device"
 
 
 class Context:
@@ -240,6 +319,70 @@ class Context:
     def delta(self, q, view, idx, count, batch, out_delta, stream=None):
         self._ck(self.lib.prhs_delta(self.h, _ptr(q), C.byref(view), _ptr(idx), _ptr(count),
                                      idx.shape[-1], batch, _ptr(out_delta), _stream(stream)))
+
+    # -- the 8-bit cache
+    def bytekv_append(self, new_k, new_v, new_lens, view, batch, max_new=0, stream=None):
+        """Append new_k / new_v (bf16 [B][Hkv][rows][128], any strides over the first three axes)."""
+        assert new_k.dtype == new_v.dtype == torch.bfloat16 and new_k.shape == new_v.shape and new_k.stride() == new_v.stride()
+        assert new_k.shape[0] >= batch and new_k.shape[1] == self.cfg.num_kv_heads and new_k.shape[3] == 128
+        assert new_k.stride(3) == 1 and new_lens.dtype == torch.int32 and new_lens.shape[0] >= batch
+        _same_device(new_k, new_v, new_lens, view._keep[0])
+        rows = new_k.shape[2]
+        assert 0 <= max_new <= rows
+        s0, s1, s2 = (st if n > 1 else 0 for st, n in zip(new_k.stride()[:3], new_k.shape[:3]))
+        self._ck(self.lib.prhs_bytekv_append(self.h, C.byref(view), new_k.data_ptr(), new_v.data_ptr(), s0, s1, s2,
+                                             _ptr(new_lens), max_new or rows, batch, _stream(stream)))
+
+    def bytekv_decode_attn(self, q, view, batch, out, out_lse=None, stream=None):
+        self._check_io(q, batch, out, out_lse, view._keep[0])
+        self._ck(self.lib.prhs_bytekv_decode_attn(self.h, _ptr(q), C.byref(view), batch, _ptr(out), _ptr(out_lse),
+                                                  _stream(stream)))
+
+    def bytekv_sparse_decode_attn(self, q, view, idx, count, batch, out, out_lse=None, stream=None):
+        self._check_io(q, batch, out, out_lse, view._keep[0])
+        assert idx.dtype == count.dtype == torch.int32 and idx.shape[:-1] == (batch, self.cfg.num_q_heads)
+        assert count.shape == idx.shape[:-1]
+        _same_device(q, idx, count)
+        self._ck(self.lib.prhs_bytekv_sparse_decode_attn(self.h, _ptr(q), C.byref(view), _ptr(idx), _ptr(count),
+                                                         idx.shape[-1], batch, _ptr(out), _ptr(out_lse), _stream(stream)))
+
+    # -- attention over selected blocks
+    def block_bounds(self, view, bounds, batch, first=None, max_new=0, stream=None):
+        assert first is None or (first.dtype == torch.int32 and first.shape[0] >= batch)
+        _same_device(view._keep[0], bounds._keep[0], *(() if first is None else (first,)))
+        self._ck(self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), _ptr(first), max_new, batch,
+                                            _stream(stream)))
+
+    def block_topk(self, q, view, bounds, sched, batch, out_blocks, out_count, stream=None):
+        self._check_blocks(q, batch, out_blocks, out_count, sched.flags)
+        _same_device(q, view._keep[0], bounds._keep[0])
+        self._ck(self.lib.prhs_block_topk(self.h, _ptr(q), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                          _ptr(out_blocks), out_blocks.shape[-1], _ptr(out_count), _stream(stream)))
+
+    def block_decode_attn(self, q, view, blocks, count, batch, out, out_lse=None, flags=0, stream=None):
+        self._check_io(q, batch, out, out_lse, view._keep[0])
+        self._check_blocks(q, batch, blocks, count, flags)
+        self._ck(self.lib.prhs_block_decode_attn(self.h, _ptr(q), C.byref(view), _ptr(blocks), _ptr(count), blocks.shape[-1],
+                                                 flags, batch, _ptr(out), _ptr(out_lse), _stream(stream)))
+
+    def block_decode_step(self, q, view, bounds, sched, batch, out, out_lse, out_blocks, out_count, stream=None):
+        self._check_io(q, batch, out, out_lse, view._keep[0])
+        self._check_blocks(q, batch, out_blocks, out_count, sched.flags)
+        _same_device(q, bounds._keep[0])
+        self._ck(self.lib.prhs_block_decode_step(self.h, _ptr(q), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                                 _ptr(out), _ptr(out_lse), _ptr(out_blocks), out_blocks.shape[-1],
+                                                 _ptr(out_count), _stream(stream)))
+
+    def _check_io(self, q, batch, out, out_lse, cache):
+        rows = (batch, self.cfg.num_q_heads)
+        assert q.dtype == out.dtype == torch.bfloat16 and tuple(q.shape) == tuple(out.shape) == rows + (128,)
+        assert out_lse is None or (out_lse.dtype == torch.float32 and tuple(out_lse.shape) == rows)
+        _same_device(q, out, cache, *(() if out_lse is None else (out_lse,)))
+
+    def _check_blocks(self, q, batch, blocks, count, flags):
+        units = self.cfg.num_kv_heads if flags & PRHS_GROUP_SETS else self.cfg.num_q_heads
+        assert blocks.dtype == count.dtype == torch.int32 and tuple(blocks.shape[:-1]) == tuple(count.shape) == (batch, units)
+        _same_device(q, blocks, count)
 
     def get_index_set(self, batch, stream=None):
         hq, cap = self.cfg.num_q_heads, self.index_capacity

@@ -1,0 +1,209 @@
+// C entry points of the block-selected attention: checks and launches.  Included by prhs.cu after bytekv_host.cuh.
+#pragma once
+#include "block_sparse.cuh"
+
+namespace {
+
+constexpr int kMaxBlocks = kMaxContext / kBlockRows;
+
+prhs_status check_bounds(prhs_ctx* ctx, const prhs_block_bounds_view* bv, BoundsDev* out) {
+  if (!bv || !bv->codes || !bv->scale) return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: NULL pointer");
+  if ((uintptr_t)bv->codes % 16 || (uintptr_t)bv->scale % 4)
+    return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: codes must be 16-byte aligned, scales 4-byte aligned");
+  if (bv->stride_outer <= 0 || bv->stride_head <= 0) return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: strides must be positive");
+  out->codes = bv->codes;
+  out->scale = bv->scale;
+  out->stride_outer = bv->stride_outer;
+  out->stride_head = bv->stride_head;
+  return PRHS_OK;
+}
+
+// The view as for the other calls, and what these kernels need on top: page-table rows that cover max_seq_len.
+prhs_status check_block_view(prhs_ctx* ctx, const prhs_kv_view* kv, int batch, KvDev* dv, int* max_t) {
+  prhs_status rc = check_view(ctx, kv, batch, dv, max_t);
+  if (rc != PRHS_OK) return rc;
+  if (kv->page_table && (long long)kv->page_table_stride * kBlockRows < *max_t)
+    return fail(ctx, PRHS_ERR_INVALID_ARG, "kv view: the page table's rows are shorter than max_seq_len");
+  return check_device(ctx);
+}
+
+prhs_status check_block_sched(prhs_ctx* ctx, const prhs_block_schedule* s, int blocks_stride, int max_t) {
+  if (!s) return fail(ctx, PRHS_ERR_INVALID_ARG, "block schedule: NULL");
+  if (s->top_blocks < 0 || s->sink_blocks < 0 || s->recent_blocks < 0)
+    return fail(ctx, PRHS_ERR_INVALID_ARG, "block schedule: negative budget");
+  if (s->top_blocks > kMaxBlocks || s->sink_blocks > kMaxBlocks || s->recent_blocks > kMaxBlocks)
+    return fail(ctx, PRHS_ERR_CAPACITY, "block schedule: budget above the largest context");
+  if (s->flags & ~PRHS_GROUP_SETS) return fail(ctx, PRHS_ERR_INVALID_ARG, "block schedule: unknown flag");
+  const int most = std::min(s->top_blocks + s->sink_blocks + s->recent_blocks, (max_t + kBlockRows - 1) / kBlockRows);
+  if (blocks_stride < std::max(most, 1)) return fail(ctx, PRHS_ERR_CAPACITY, "blocks_stride below the budget's blocks");
+  return PRHS_OK;
+}
+
+bool block_shared(const prhs_ctx* c, uint32_t flags) { return (flags & PRHS_GROUP_SETS) && c->gq > 1; }
+
+prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const BoundsDev& bd, const prhs_block_schedule* s,
+                              int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, bool update_last,
+                              cudaStream_t st) {
+  const bool shared = block_shared(c, s->flags);
+  BlockScoreParams sp;
+  sp.q = static_cast<const __nv_bfloat16*>(q);
+  sp.kv = kv;
+  sp.bd = bd;
+  sp.scores = c->scores;
+  sp.ld = c->ld;
+  sp.num_q_heads = c->cfg.num_q_heads;
+  sp.group_size = c->gq;
+  sp.group_max = shared ? 1 : 0;
+  sp.update_last = update_last ? 1 : 0;
+  sp.max_len = max_t;
+  sp.flags = c->flags;
+  const int blocks = (max_t + kBlockRows - 1) / kBlockRows;
+  {
+    LaunchScope ls(c, PRHS_KIND_SCORE, st);
+    block_score_kernel<<<dim3((blocks + kScoreBlocks - 1) / kScoreBlocks, c->cfg.num_kv_heads, batch), kScoreWarps * 32, 0, st>>>(sp);
+  }
+  BlockSelectParams p;
+  p.scores = c->scores;
+  p.ld = c->ld;
+  p.num_q_heads = c->cfg.num_q_heads;
+  p.heads_per_unit = shared ? c->gq : 1;
+  p.units_per_seq = c->cfg.num_q_heads / p.heads_per_unit;
+  p.seq_lens = kv.seq_lens;
+  p.top = s->top_blocks;
+  p.sink = s->sink_blocks;
+  p.recent = s->recent_blocks;
+  p.out_blocks = out_blocks;
+  p.stride = stride;
+  p.out_count = out_count;
+  p.max_len = max_t;
+  {
+    LaunchScope ls(c, PRHS_KIND_SELECT, st);
+    block_select_kernel<<<batch * p.units_per_seq, kBSThreads, 0, st>>>(p);
+  }
+  PRHS_CUDA(c, cudaGetLastError());
+  return PRHS_OK;
+}
+
+prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
+                              uint32_t flags, int batch, void* out, float* out_lse, cudaStream_t st) {
+  const bool shared = block_shared(c, flags);
+  BlockAttnParams bp;
+  bp.units_per_seq = shared ? c->cfg.num_kv_heads : c->cfg.num_q_heads;
+  bp.blocks = blocks;
+  bp.count = count;
+  bp.stride = stride;
+  AttnParams& p = bp.a;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.kv = kv;
+  p.idx = nullptr;
+  p.count = nullptr;
+  p.idx_stride = 0;
+  p.set = SetRef{};
+  p.num_q_heads = c->cfg.num_q_heads;
+  p.group_size = c->gq;
+  p.splits = pick_splits(c, batch * bp.units_per_seq, stride * kBlockRows);
+  p.partials = c->partials;
+  p.tickets = c->tickets;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.out_lse = out_lse;
+  p.lse_full = nullptr;
+  p.out_delta = nullptr;
+  p.flags = c->flags;
+  p.need = nullptr;
+  p.need_mode = 0;
+  {
+    LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
+    block_attn_kernel<<<dim3(p.splits, bp.units_per_seq, batch), kTThreads, kTSmemBytes, st>>>(bp);
+  }
+  PRHS_CUDA(c, cudaGetLastError());
+  return PRHS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+prhs_status prhs_block_bounds(prhs_ctx* ctx, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds, const int32_t* first,
+                              int32_t max_new, int32_t batch, void* stream) {
+  if (!ctx) return PRHS_ERR_INVALID_ARG;
+  KvDev dv;
+  BoundsDev bd;
+  int max_t;
+  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
+  if (rc != PRHS_OK) return rc;
+  if (max_new < 0) return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: negative max_new");
+  const int most = (first && max_new > 0) ? std::min(max_new, max_t) : max_t;
+  cudaStream_t st = as_stream(stream);
+  BoundsParams p;
+  p.kv = dv;
+  p.bd = bd;
+  p.first = first;
+  p.batch = batch;
+  p.num_kv_heads = ctx->cfg.num_kv_heads;
+  p.blocks_max = most == 1 ? 1 : std::min((most + 2 * (kBlockRows - 1)) / kBlockRows, (max_t + kBlockRows - 1) / kBlockRows);
+  p.max_len = max_t;
+  p.flags = ctx->flags;
+  const long long items = (long long)batch * p.num_kv_heads * p.blocks_max;
+  const int warps = items >= 8ll * ctx->sm_count ? 8 : 1;
+  const long long ctas = (items + warps - 1) / warps;
+  if (ctas > 0x7fffffffll) return fail(ctx, PRHS_ERR_UNSUPPORTED, "block bounds: too many blocks");
+  {
+    LaunchScope ls(ctx, PRHS_KIND_MISC, st);
+    block_bounds_kernel<<<(unsigned)ctas, 32 * warps, 0, st>>>(p);
+  }
+  PRHS_CUDA(ctx, cudaGetLastError());
+  return PRHS_OK;
+}
+
+prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
+                            const prhs_block_schedule* sched, int32_t batch, int32_t* out_blocks, int32_t blocks_stride,
+                            int32_t* out_count, void* stream) {
+  if (!ctx) return PRHS_ERR_INVALID_ARG;
+  if (!q || !out_blocks || !out_count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
+  if ((uintptr_t)q % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q must be 16-byte aligned");
+  KvDev dv;
+  BoundsDev bd;
+  int max_t;
+  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
+  if (rc == PRHS_OK) rc = check_block_sched(ctx, sched, blocks_stride, max_t);
+  if (rc != PRHS_OK) return rc;
+  return launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, false, as_stream(stream));
+}
+
+prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
+                                   int32_t blocks_stride, uint32_t flags, int32_t batch, void* out, float* out_lse, void* stream) {
+  if (!ctx) return PRHS_ERR_INVALID_ARG;
+  if (!q || !blocks || !count || !out) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
+  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (blocks_stride < 1 || blocks_stride > 3 * kMaxBlocks) return fail(ctx, PRHS_ERR_INVALID_ARG, "blocks_stride out of range");
+  if (flags & ~PRHS_GROUP_SETS) return fail(ctx, PRHS_ERR_INVALID_ARG, "block attention: unknown flag");
+  KvDev dv;
+  int max_t;
+  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  if (rc != PRHS_OK) return rc;
+  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, batch, out, out_lse, as_stream(stream));
+}
+
+prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
+                                   const prhs_block_schedule* sched, int32_t batch, void* out, float* out_lse, int32_t* out_blocks,
+                                   int32_t blocks_stride, int32_t* out_count, void* stream) {
+  if (!ctx) return PRHS_ERR_INVALID_ARG;
+  if (!q || !out || !out_blocks || !out_count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
+  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  KvDev dv;
+  BoundsDev bd;
+  int max_t;
+  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
+  if (rc == PRHS_OK) rc = check_block_sched(ctx, sched, blocks_stride, max_t);
+  if (rc != PRHS_OK) return rc;
+  if (sched->recent_blocks < 1)
+    return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
+  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, true, as_stream(stream));
+  if (rc != PRHS_OK) return rc;
+  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, batch, out, out_lse, as_stream(stream));
+}
+
+}  // extern "C"

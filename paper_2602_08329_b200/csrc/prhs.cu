@@ -25,6 +25,8 @@
 #include "gather_probe.cuh"
 #include "attn_tma.cuh"
 #include "attn_group_umma.cuh"
+#include "bytekv.cuh"
+#include "block_sparse.cuh"
 
 using namespace prhs;
 
@@ -572,6 +574,9 @@ prhs_status check_layer(prhs_ctx* c, int layer, int step, const prhs_schedule* s
 }  // namespace
 
 // =============================================================================== C ABI
+#include "bytekv_host.cuh"
+#include "block_host.cuh"
+
 extern "C" {
 
 const char* prhs_version(void) { return "prhs-b200 0.1"; }
@@ -809,6 +814,9 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
     e = cudaFuncSetAttribute(gather_probe_kernel<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGPSmemBytes);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(dense_attn_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
+  if (e == cudaSuccess) e = bytekv_set_attributes();
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(block_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
   if (e == cudaSuccess) {
     int nb = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, gather_attn_mma_kernel, kTThreads, kTSmemBytes);
@@ -1518,7 +1526,7 @@ prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags) {
     PRHS_CUDA(ctx, cudaMemsetAsync(ctx->flags, 0, sizeof(uint32_t), st));
     PRHS_CUDA(ctx, cudaStreamSynchronize(st));
   }
-  if (f & (PRHS_FLAG_BAD_INDEX | PRHS_FLAG_BAD_PAGE | PRHS_FLAG_TIMEOUT)) {
+  if (f & ~PRHS_FLAG_SELECT_FALLBACK) {
     char buf[96];
     snprintf(buf, sizeof buf, "device flag word 0x%x", f);
     return fail(ctx, PRHS_ERR_DEVICE_FLAG, buf);

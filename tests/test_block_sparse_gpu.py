@@ -1,0 +1,389 @@
+"""Block bounds, block scores and selection, attention over blocks, and whole steps, against the 64-bit forms."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_08329_b200 import binding as P
+from tests import cache_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Cache:
+    """A bf16 cache, contiguous or paged, with its bounds.  What holds nothing is NaN (rows) or 99 (bounds)."""
+
+    def __init__(self, batch, kv_heads, cap, paged, dev, seed=0):
+        self.B, self.H, self.paged, self.dev = batch, kv_heads, paged, dev
+        self.nb = -(-cap // 16)
+        g = torch.Generator().manual_seed(seed)
+        if paged:
+            self.pool = batch * self.nb + 2
+            self.table_cpu = torch.randperm(self.pool, generator=g)[: batch * self.nb].view(batch, self.nb).to(torch.int32)
+            self.table = self.table_cpu.to(dev)
+            shape, bshape = (self.pool, kv_heads, 16, 128), (self.pool, kv_heads)
+        else:
+            self.table = None
+            shape, bshape = (batch, kv_heads, self.nb * 16, 128), (batch, kv_heads, self.nb)
+        self.k, self.v = (torch.full(shape, math.nan, dtype=torch.bfloat16, device=dev) for _ in range(2))
+        self.codes = torch.full(bshape + (2, 128), 99, dtype=torch.int8, device=dev)
+        self.scale = torch.full(bshape, 99.0, device=dev)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=dev)
+        self.rows = torch.zeros(2, batch, kv_heads, 0, 128, dtype=torch.bfloat16)
+
+    def view(self, **kw):
+        return P.make_view(self.k, self.v, self.lens, page_table=self.table, **kw)
+
+    def bounds(self):
+        return P.make_block_bounds(self.codes, self.scale)
+
+    def place(self, rows, lens):
+        """rows [2][B][H][n][128]: the first lens[b] positions of every sequence."""
+        self.rows = rows
+        self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        for w, x in enumerate((self.k, self.v)):
+            for b, t in enumerate(lens):
+                if not self.paged:
+                    x[b, :, :t] = rows[w, b, :, :t].to(self.dev)
+                else:
+                    for j in range(-(-t // 16)):
+                        part = rows[w, b, :, 16 * j: min(16 * j + 16, t)]
+                        x[int(self.table_cpu[b, j]), :, : part.shape[1]] = part.to(self.dev)
+
+    def bound_of(self, b, h, j):
+        o = (int(self.table_cpu[b, j]), h) if self.paged else (b, h, j)
+        return self.codes[o].cpu().numpy(), float(self.scale[o])
+
+    def ref_bounds(self, b, h, t):
+        x = self.rows[0, b, h, :t].double().numpy()
+        got = [R.block_bounds(x[16 * j: 16 * j + 16]) for j in range(-(-t // 16))]
+        return np.stack([c for c, _ in got]) if got else np.zeros((0, 2, 128), np.int8), np.array([s for _, s in got])
+
+
+def make_ctx(cache, group, cap=None):
+    return P.Context(num_layers=1, max_batch=cache.B, num_q_heads=cache.H * group, num_kv_heads=cache.H,
+                     max_context=cap or cache.nb * 16, max_k=16, max_window=16, max_sinks=4, page_size=16 if cache.paged else 0)
+
+
+def random_rows(B, H, n, seed, drift=True):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(2, B, H, n, 128, generator=g)
+    if drift:
+        x[0] += torch.randn(B, H, -(-n // 16), 1, 128, generator=g).expand(-1, -1, -1, 16, -1).reshape(B, H, -1, 128)[:, :, :n]
+    return x.to(torch.bfloat16)
+
+
+def ref_sets(cache, q, lens, group, top, sink, recent, shared):
+    """{(b, unit): blocks}, from the reference bounds."""
+    sets = {}
+    for b, t in enumerate(lens):
+        nb = -(-t // 16)
+        for h in range(cache.H):
+            codes, scales = cache.ref_bounds(b, h, t)
+            sc = [R.block_scores(q[b, h * group + j], codes, scales) for j in range(group)]
+            if shared and group > 1:
+                sets[(b, h)] = R.select_blocks(np.max(sc, 0), nb, top, sink, recent)
+            else:
+                for j in range(group):
+                    sets[(b, h * group + j)] = R.select_blocks(sc[j], nb, top, sink, recent)
+    return sets
+
+
+def check_attention(cache, q, lens, group, sets, shared, out, lse):
+    y_all, l_all = np64(out), np64(lse)
+    for b, t in enumerate(lens):
+        for u in range(cache.H * group):
+            blocks = sets[(b, u // group if shared and group > 1 else u)]
+            pos = np.array([i for j in blocks for i in range(16 * j, min(16 * j + 16, t))], np.int64)
+            k, v = (cache.rows[w, b, u // group].double().numpy()[pos] for w in range(2))
+            y, l, tol, ltol = R.attend(q[b, u], k, v, True)
+            assert np.all(np.abs(y_all[b, u] - y) <= tol), (b, u)
+            assert l_all[b, u] == l if math.isinf(l) else abs(l_all[b, u] - l) <= ltol, (b, u)
+
+
+# ---------------------------------------------------------------------------------- bounds
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("first", ["all", "some", "last"])
+def test_bounds_are_exact_and_touch_nothing_else(cuda_device, paged, first):
+    lens = [0, 1, 16, 17, 150, 333]
+    cache = Cache(len(lens), 2, 340, paged, cuda_device)
+    ctx = make_ctx(cache, 1)
+    rows = random_rows(len(lens), 2, 340, 1)
+    rows[0, 4, 0, 32:48] = 0.0                                           # a block of zeros
+    rows[0, 5, 1] *= torch.exp2(torch.arange(340).float() / 4 - 60)[:, None].to(torch.bfloat16)
+    rows[0, 5, 0, 48:64, 7] = 127.0                                      # amax / 127 is a power of two
+    cache.place(rows, lens)
+    frm = {"all": [0] * 6, "some": [0, 0, 15, 17, 100, 16], "last": [t - 1 if t else 0 for t in lens]}[first]
+    kw = {} if first == "all" else dict(first=torch.tensor(frm, dtype=torch.int32, device=cuda_device),
+                                        max_new=1 if first == "last" else 0)
+    ctx.block_bounds(cache.view(), cache.bounds(), len(lens), **kw)
+    assert ctx.check() == 0
+    touched = set()
+    for b, t in enumerate(lens):
+        for h in range(2):
+            codes, scales = cache.ref_bounds(b, h, t)
+            for j in range(frm[b] // 16, -(-t // 16) if frm[b] < t else 0):
+                c, s = cache.bound_of(b, h, j)
+                assert s == scales[j] and np.array_equal(c, codes[j]), (b, h, j)
+                touched.add((int(cache.table_cpu[b, j]), h) if paged else (b, h, j))
+    sc = cache.scale.cpu()
+    for o in np.ndindex(*sc.shape):
+        if o not in touched:
+            assert sc[o] == 99.0 and bool((cache.codes[o] == 99).all()), o
+    ctx.close()
+
+
+def test_bounds_refuse_contradictory_lengths(cuda_device):
+    cache = Cache(3, 1, 64, False, cuda_device)
+    ctx = make_ctx(cache, 1)
+    cache.place(random_rows(3, 1, 64, 1), [40, 40, 40])
+    ctx.block_bounds(cache.view(), cache.bounds(), 3, first=torch.tensor([-1, 41, 39], dtype=torch.int32, device=cuda_device))
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    assert bool((cache.scale[:2] == 99.0).all()) and cache.scale[2, 0].tolist()[:2] == [99.0, 99.0] and float(cache.scale[2, 0, 2]) != 99.0
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------- selection
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("heads,group,shared", [(2, 1, False), (2, 4, False), (2, 4, True), (1, 16, False), (1, 16, True), (1, 11, True)])
+@pytest.mark.parametrize("budget", [(5, 1, 2), (0, 0, 0), (1, 0, 0), (200, 3, 0), (7, 500, 1), (30, 0, 8)])
+def test_selection_is_exact(cuda_device, paged, heads, group, shared, budget):
+    top, sink, recent = budget
+    lens = [0, 1, 16, 33, 700, 2047]
+    cache = Cache(len(lens), heads, 2047, paged, cuda_device)
+    ctx = make_ctx(cache, group)
+    cache.place(random_rows(len(lens), heads, 2047, 3), lens)
+    ctx.block_bounds(cache.view(), cache.bounds(), len(lens))
+    q = torch.randn(len(lens), heads * group, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    q[:, 0] = 0.0                                                        # every score zero: ties everywhere
+    q = q.to(cuda_device)
+    units = heads if shared else heads * group
+    blocks = torch.full((len(lens), units, max(1, min(top + sink + recent, 128)) + 3), 7, dtype=torch.int32, device=cuda_device)
+    count = torch.full((len(lens), units), -5, dtype=torch.int32, device=cuda_device)
+    sched = P.make_block_schedule(top, sink, recent, P.PRHS_GROUP_SETS if shared else 0)
+    ctx.block_topk(q, cache.view(), cache.bounds(), sched, len(lens), blocks, count)
+    assert ctx.check() == 0
+    for (b, u), want in ref_sets(cache, np64(q), lens, group, top, sink, recent, shared).items():
+        got = blocks[b, u].tolist()
+        assert int(count[b, u]) == len(want) and got[: len(want)] == want and all(x == -1 for x in got[len(want):]), (b, u)
+    ctx.close()
+
+
+def test_ties_go_to_the_lower_block(cuda_device):
+    # keys repeat with a period of five blocks: every score occurs many times
+    cache = Cache(1, 2, 5000, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    rows = random_rows(1, 2, 80, 6)
+    rows = rows.repeat(1, 1, 1, 63, 1)[:, :, :, :5000].contiguous()
+    cache.place(rows, [5000])
+    ctx.block_bounds(cache.view(), cache.bounds(), 1)
+    q = torch.randn(1, 4, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    for top in (1, 62, 63, 64, 130, 300):
+        blocks, count = torch.empty(1, 4, top + 1, dtype=torch.int32, device=cuda_device), torch.empty(1, 4, dtype=torch.int32, device=cuda_device)
+        ctx.block_topk(q, cache.view(), cache.bounds(), P.make_block_schedule(top, 0, 1), 1, blocks, count)
+        for (b, u), want in ref_sets(cache, np64(q), [5000], 2, top, 0, 1, False).items():
+            assert blocks[b, u].tolist()[: int(count[b, u])] == want, (top, u)
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------- attention
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("heads,group,shared", [(2, 1, False), (2, 4, False), (2, 4, True), (1, 16, True), (1, 11, False)])
+def test_attention_over_blocks(cuda_device, paged, heads, group, shared):
+    lens = [0, 3, 16, 250, 1599]
+    cache = Cache(len(lens), heads, 1600, paged, cuda_device)
+    ctx = make_ctx(cache, group)
+    cache.place(random_rows(len(lens), heads, 1600, 8), lens)
+    units = heads if shared else heads * group
+    rng = np.random.default_rng(2)
+    sets, stride = {}, 131
+    blocks, count = np.full((len(lens), units, stride), 1 << 28, np.int32), np.zeros((len(lens), units), np.int32)
+    for b, t in enumerate(lens):
+        nb = -(-t // 16)
+        for u in range(units):
+            n = 0 if nb == 0 else [131, 0, 1, 2, 3, 17, 64][(u + b) % 7]
+            sets[(b, u)] = rng.integers(0, nb, n).tolist() if n else []      # any order, repeats
+            blocks[b, u, :n], count[b, u] = sets[(b, u)], n
+    bd, cd = torch.from_numpy(blocks).to(cuda_device), torch.from_numpy(count).to(cuda_device)
+    q = torch.randn(len(lens), heads * group, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    flags = P.PRHS_GROUP_SETS if shared else 0
+    ctx.block_decode_attn(q, cache.view(), bd, cd, len(lens), out, lse, flags)
+    assert ctx.check() == 0
+    check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    # a block outside the sequence is left out and recorded
+    b, u = next(k for k, s in sets.items() if len(s) >= 3 and k[0] >= 3)
+    bd[b, u, 1], bd[b, u, 2] = -(-lens[b] // 16), -3
+    sets[(b, u)] = sets[(b, u)][:1] + sets[(b, u)][3:]
+    ctx.block_decode_attn(q, cache.view(), bd, cd, len(lens), out, lse, flags)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    ctx.close()
+
+
+def test_bad_pages_are_skipped_and_recorded(cuda_device):
+    cache = Cache(1, 1, 160, True, cuda_device)
+    ctx = make_ctx(cache, 1)
+    cache.place(random_rows(1, 1, 160, 8), [160])
+    ctx.block_bounds(cache.view(), cache.bounds(), 1)
+    cache.table[0, 3], cache.table[0, 5] = -1, cache.pool
+    q = torch.randn(1, 1, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    blocks, count = torch.empty(1, 1, 10, dtype=torch.int32, device=cuda_device), torch.empty(1, 1, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(1, 1, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(9, 0, 1), 1, out, lse, blocks, count)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    assert blocks[0, 0].tolist() == list(range(10))
+    check_attention(cache, np64(q), [160], 1, {(0, 0): [0, 1, 2, 4, 6, 7, 8, 9]}, False, out, lse)
+    ctx.block_bounds(cache.view(), cache.bounds(), 1)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    assert ctx.check() == 0
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------ steps
+@pytest.mark.parametrize("paged,group,shared", [(False, 1, False), (True, 4, True), (True, 4, False), (False, 16, True)])
+def test_decode_run(cuda_device, paged, group, shared):
+    # a prompt's bounds, then tokens one by one through whole steps captured in a graph
+    lens, H, cap = [30, 239, 16], 2, 300
+    cache = Cache(3, H, cap, paged, cuda_device)
+    ctx = make_ctx(cache, group)
+    rows = random_rows(3, H, cap, 12)
+    cache.place(rows, lens)
+    ctx.block_bounds(cache.view(), cache.bounds(), 3)
+    units = H if shared else H * group
+    q = torch.zeros(3, H * group, 128, dtype=torch.bfloat16, device=cuda_device)
+    blocks, count = torch.empty(3, units, 8, dtype=torch.int32, device=cuda_device), torch.empty(3, units, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(3, H * group, device=cuda_device)
+    sched = P.make_block_schedule(4, 1, 2, P.PRHS_GROUP_SETS if shared else 0)
+    view, bounds = cache.view(), cache.bounds()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        ctx.block_decode_step(q, view, bounds, sched, 3, out, lse, blocks, count)
+    g = torch.Generator().manual_seed(13)
+    for step in range(20):
+        lens = [t + 1 for t in lens]
+        cache.place(rows, lens)
+        q.copy_(torch.randn(3, H * group, 128, generator=g).to(torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        sets = ref_sets(cache, np64(q), lens, group, 4, 1, 2, shared)
+        for (b, u), want in sets.items():
+            assert blocks[b, u].tolist()[: int(count[b, u])] == want, (step, b, u)
+        check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    for b, t in enumerate(lens):                                           # the bounds kept up with the tokens
+        for h in range(H):
+            codes, scales = cache.ref_bounds(b, h, t)
+            for j in range(-(-t // 16)):
+                c, s = cache.bound_of(b, h, j)
+                assert s == scales[j] and np.array_equal(c, codes[j])
+    assert ctx.check() == 0
+    ctx.close()
+
+
+def test_all_blocks_are_the_dense_attention(cuda_device):
+    cache = Cache(2, 2, 700, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    cache.place(random_rows(2, 2, 700, 8), [700, 77])
+    ctx.block_bounds(cache.view(), cache.bounds(), 2)
+    q = torch.randn(2, 4, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    blocks, count = torch.empty(2, 4, 44, dtype=torch.int32, device=cuda_device), torch.empty(2, 4, dtype=torch.int32, device=cuda_device)
+    out, lse, want, wl = torch.empty_like(q), torch.empty(2, 4, device=cuda_device), torch.empty_like(q), torch.empty(2, 4, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(1000, 1, 1), 2, out, lse, blocks, count)
+    ctx.dense_decode_attn(q, cache.view(), 2, want, wl)
+    assert count.tolist() == [[44] * 4, [5] * 4]
+    assert float((out.float() - want.float()).abs().max()) <= 2.0 ** -6 and float((lse - wl).abs().max()) <= 2.0 ** -16
+    ctx.close()
+
+
+def test_long_context_selection(cuda_device):
+    # 2^18 positions: 16384 blocks; the selection's counts and the score grid over many CTAs
+    t = 1 << 18
+    cache = Cache(1, 1, t, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    g = torch.Generator(device=cuda_device).manual_seed(3)
+    cache.k.copy_(torch.randn(cache.k.shape, generator=g, device=cuda_device))
+    cache.v.copy_(torch.randn(cache.v.shape, generator=g, device=cuda_device))
+    cache.lens.fill_(t)
+    ctx.block_bounds(cache.view(), cache.bounds(), 1)
+    q = torch.randn(1, 2, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    blocks, count = torch.empty(1, 2, 2000, dtype=torch.int32, device=cuda_device), torch.empty(1, 2, dtype=torch.int32, device=cuda_device)
+    ctx.block_topk(q, cache.view(), cache.bounds(), P.make_block_schedule(1900, 1, 1), 1, blocks, count)
+    assert ctx.check() == 0
+    codes, scale = cache.codes[0, 0].cpu().numpy(), np64(cache.scale[0, 0])
+    for u in range(2):
+        want = R.select_blocks(R.block_scores(np64(q[0, u]), codes, scale), t // 16, 1900, 1, 1)
+        assert blocks[0, u].tolist()[: int(count[0, u])] == want
+    ctx.close()
+
+
+# -------------------------------------------------------------------------------- refusals
+def test_refusals(cuda_device):
+    cache = Cache(2, 2, 64, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    cache.place(random_rows(2, 2, 64, 1), [64, 64])
+    lib, C = ctx.lib, P.C
+    q = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=cuda_device)
+    out = torch.full_like(q, 7.0)
+    blocks, count = torch.zeros(2, 4, 4, dtype=torch.int32, device=cuda_device), torch.zeros(2, 4, dtype=torch.int32, device=cuda_device)
+    st = torch.cuda.current_stream().cuda_stream
+    INVALID, CAPACITY = 1, 6
+
+    def bounds(bd=None, view=None, new=0, b=2):
+        bd, view = bd or cache.bounds(), view or cache.view()
+        return lib.prhs_block_bounds(ctx.h, C.byref(view), C.byref(bd), None, new, b, st)
+
+    def step(sched=None, bd=None, view=None, stride=4, o=None, cnt=None):
+        bd, view, sched = bd or cache.bounds(), view or cache.view(), sched or P.make_block_schedule(1, 1, 1)
+        return lib.prhs_block_decode_step(ctx.h, q.data_ptr(), C.byref(view), C.byref(bd), C.byref(sched), 2,
+                                          out.data_ptr() if o is None else o, None, blocks.data_ptr(), stride,
+                                          count.data_ptr() if cnt is None else cnt, st)
+
+    def attn(stride=4, flags=0):
+        view = cache.view()
+        return lib.prhs_block_decode_attn(ctx.h, q.data_ptr(), C.byref(view), blocks.data_ptr(), count.data_ptr(), stride, flags, 2,
+                                          out.data_ptr(), None, st)
+
+    assert bounds() == 0 and step() == 0 and attn() == 0
+    torch.cuda.synchronize()
+    out.fill_(7.0)
+    for field, value in [("codes", None), ("scale", None), ("codes", cache.codes.data_ptr() + 8), ("stride_outer", 0), ("stride_head", -1)]:
+        bd = cache.bounds()
+        setattr(bd, field, value)
+        assert bounds(bd) == INVALID and step(bd=bd) == INVALID, field
+    assert bounds(new=-1) == INVALID and bounds(b=3) == CAPACITY
+    for sched, status in [(P.make_block_schedule(-1, 1, 1), INVALID), (P.make_block_schedule(1, -1, 1), INVALID),
+                          (P.make_block_schedule(1, 1, 0), INVALID), (P.make_block_schedule(1, 1, 1, 1), INVALID),
+                          (P.make_block_schedule(1 << 20, 1, 1), CAPACITY), (P.make_block_schedule(9, 1, 1), None)]:
+        assert step(sched) == (0 if status is None else status)           # nine middle blocks: the context has four in all
+    torch.cuda.synchronize()
+    out.fill_(7.0)
+    assert step(P.make_block_schedule(9, 1, 1), stride=3) == CAPACITY
+    assert step(o=out.data_ptr() + 2) == INVALID
+    view = cache.view()
+    view.max_seq_len = 65
+    assert step(view=view) == CAPACITY and bounds(view=view) == CAPACITY
+    assert attn(stride=0) == INVALID and attn(flags=1) == INVALID
+    assert lib.prhs_block_topk(None, q.data_ptr(), C.byref(view), None, None, 2, blocks.data_ptr(), 4, count.data_ptr(), st) == INVALID
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    with pytest.raises(AssertionError):
+        ctx.block_decode_attn(q, cache.view(), blocks[:, :2].contiguous(), count[:, :2].contiguous(), 2, out)
+    with pytest.raises(AssertionError):
+        P.make_block_bounds(cache.codes.float(), cache.scale)
+    pc = Cache(1, 1, 64, True, cuda_device)
+    pctx = make_ctx(pc, 1)
+    pview, pb = pc.view(), pc.bounds()
+    pview.page_table_stride = 3
+    assert lib.prhs_block_bounds(pctx.h, C.byref(pview), C.byref(pb), None, 0, 1, st) == INVALID
+    pctx.close()
+    ctx.close()
