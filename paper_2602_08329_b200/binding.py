@@ -71,6 +71,10 @@ class Schedule(C.Structure):
                 ("sim_threshold", C.c_float)]
 
 
+_BYTEKV_FORMATS = {torch.float8_e4m3fn: PRHS_BYTEKV_E4M3, torch.float8_e5m2: PRHS_BYTEKV_E5M2}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+
+
 class ByteKvView(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_tail", "v_tail")] + \
                [(n, C.c_int64) for n in ("stride_outer", "stride_head", "scale_stride_outer", "scale_stride_head")] + \
@@ -160,7 +164,7 @@ def _ptr(t):
 
 def _stream(stream=None):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -182,6 +186,7 @@ def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
                   _ptr(page_table), page_table.stride(0) if page_table is not None else 0,
                   seq_lens.data_ptr(), max_seq_len, k.shape[0] if page_table is not None else 0)
     view._keep = (k, v, seq_lens, page_table)
+    view._batch, view._heads, view._cap = seq_lens.shape[0], k.shape[1], k.shape[2] if page_table is None else 0
     return view
 
 
@@ -192,37 +197,40 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
     fp32 scales [B][Hkv][cap/16]; or paged [pool][Hkv][16][128] with scales [pool][Hkv].  Tails bf16
     [B][Hkv][16][128].
     """
-    fmt = {torch.float8_e4m3fn: PRHS_BYTEKV_E4M3, torch.float8_e5m2: PRHS_BYTEKV_E5M2}[k.dtype]
-    assert v.dtype == k.dtype and k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride()
-    assert k.shape[-1] == 128 and k.stride(-1) == 1 and k.stride(-2) == 128 and k.shape[2] % 16 == 0
-    paged = page_table is not None
-    assert k_scale.dtype == torch.float32 and v_scale.dtype == torch.float32 and k_scale.stride() == v_scale.stride()
-    want = (k.shape[0], k.shape[1]) if paged else (k.shape[0], k.shape[1], k.shape[2] // 16)
-    assert k_scale.shape == v_scale.shape == want and (paged or k_scale.stride(2) == 1)
-    assert k_tail.dtype == v_tail.dtype == torch.bfloat16 and k_tail.shape == v_tail.shape
-    assert k_tail.shape[1:] == (k.shape[1], 16, 128) and k_tail.shape[0] >= seq_lens.shape[0]
-    assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous()
+    fmt = _BYTEKV_FORMATS[k.dtype]
+    shape, stride, sshape, sstride = k.shape, k.stride(), k_scale.shape, k_scale.stride()
+    B, paged = seq_lens.shape[0], page_table is not None
+    assert v.dtype is k.dtype and v.shape == shape and v.stride() == stride and len(shape) == 4
+    assert shape[3] == 128 and stride[2:] == (128, 1) and shape[2] % 16 == 0
+    assert k_scale.dtype is _F32 and v_scale.dtype is _F32 and v_scale.shape == sshape and v_scale.stride() == sstride
+    assert k_tail.dtype is _BF16 and v_tail.dtype is _BF16 and k_tail.shape == v_tail.shape
+    assert k_tail.shape[1:] == (shape[1], 16, 128) and k_tail.shape[0] >= B
+    assert k_tail.is_contiguous() and v_tail.is_contiguous() and seq_lens.dtype is _I32 and seq_lens.is_contiguous()
     if paged:
-        assert k.shape[2] == 16 and page_table.dtype == torch.int32 and page_table.stride(-1) == 1
+        assert shape[2] == 16 and sshape == shape[:2] and page_table.dtype is _I32
+        assert page_table.stride(1) == 1 and page_table.shape[0] >= B
+        tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table)
+        table, table_stride, pages = page_table.data_ptr(), page_table.stride(0), shape[0]
     else:
-        assert k.shape[0] >= seq_lens.shape[0] and max_seq_len <= k.shape[2]
-    tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens) + ((page_table,) if paged else ())
+        assert sshape == (shape[0], shape[1], shape[2] // 16) and sstride[2] == 1 and shape[0] >= B and max_seq_len <= shape[2]
+        tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens)
+        table, table_stride, pages = None, 0, 0
     _same_device(*tensors)
-    view = ByteKvView(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(k_tail), _ptr(v_tail),
-                      k.stride(0), k.stride(1), k_scale.stride(0), k_scale.stride(1),
-                      page_table.data_ptr() if paged else None, seq_lens.data_ptr(),
-                      page_table.stride(0) if paged else 0, max_seq_len,
-                      k.shape[0] if paged else 0, fmt)
+    view = ByteKvView(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(),
+                      stride[0], stride[1], sstride[0], sstride[1], table, seq_lens.data_ptr(), table_stride, max_seq_len,
+                      pages, fmt)
     view._keep = tensors
+    view._batch, view._heads, view._cap = B, shape[1], 0 if paged else shape[2]
     return view
 
 
 def make_block_bounds(codes, scale) -> BlockBoundsView:
     """Bounds int8 [B][Hkv][blocks][2][128] with scales fp32 [B][Hkv][blocks], or per page [pool][Hkv][2][128], [pool][Hkv]."""
-    assert codes.dtype == torch.int8 and scale.dtype == torch.float32 and codes.shape[-2:] == (2, 128)
-    assert codes.shape[:-2] == scale.shape and codes.is_contiguous() and scale.is_contiguous()
+    shape, stride = codes.shape, scale.stride()
+    assert codes.dtype is torch.int8 and scale.dtype is _F32 and shape[-2:] == (2, 128)
+    assert shape[:-2] == scale.shape and codes.is_contiguous() and scale.is_contiguous()
     _same_device(codes, scale)
-    view = BlockBoundsView(codes.data_ptr(), scale.data_ptr(), scale.stride(0), scale.stride(1))
+    view = BlockBoundsView(codes.data_ptr(), scale.data_ptr(), stride[0], stride[1])
     view._keep = (codes, scale)
     return view
 
@@ -232,8 +240,10 @@ def make_block_schedule(top_blocks, sink_blocks=1, recent_blocks=1, flags=0) -> 
 
 
 def _same_device(*tensors):
-    dev = tensors[0].device
-    assert dev.type == "cuda" and all(t.device == dev for t in tensors), "tensors of a call must be on one CUDA device"
+    dev = tensors[0].get_device()
+    assert dev >= 0, "tensors of a call must be on a CUDA device"
+    for t in tensors:
+        assert t.get_device() == dev, "tensors of a call must be on one CUDA device"
 
 
 class Context:
@@ -323,66 +333,100 @@ class Context:
     # -- the 8-bit cache
     def bytekv_append(self, new_k, new_v, new_lens, view, batch, max_new=0, stream=None):
         """Append new_k / new_v (bf16 [B][Hkv][rows][128], any strides over the first three axes)."""
-        assert new_k.dtype == new_v.dtype == torch.bfloat16 and new_k.shape == new_v.shape and new_k.stride() == new_v.stride()
-        assert new_k.shape[0] >= batch and new_k.shape[1] == self.cfg.num_kv_heads and new_k.shape[3] == 128
-        assert new_k.stride(3) == 1 and new_lens.dtype == torch.int32 and new_lens.shape[0] >= batch
+        shape, stride = new_k.shape, new_k.stride()
+        assert new_k.dtype is _BF16 and new_v.dtype is _BF16 and new_v.shape == shape and new_v.stride() == stride
+        assert len(shape) == 4 and shape[0] >= batch and shape[1] == self.cfg.num_kv_heads and shape[3] == 128 and stride[3] == 1
+        assert new_lens.dtype is _I32 and new_lens.shape[0] >= batch and new_lens.is_contiguous() and 0 <= max_new <= shape[2]
         _same_device(new_k, new_v, new_lens, view._keep[0])
-        rows = new_k.shape[2]
-        assert 0 <= max_new <= rows
-        s0, s1, s2 = (st if n > 1 else 0 for st, n in zip(new_k.stride()[:3], new_k.shape[:3]))
+        self._fit(view, batch)
+        s0, s1, s2 = (st if n > 1 else 0 for st, n in zip(stride, shape[:3]))
         self._ck(self.lib.prhs_bytekv_append(self.h, C.byref(view), new_k.data_ptr(), new_v.data_ptr(), s0, s1, s2,
-                                             _ptr(new_lens), max_new or rows, batch, _stream(stream)))
+                                             new_lens.data_ptr(), max_new or shape[2], batch, _stream(stream)))
 
     def bytekv_decode_attn(self, q, view, batch, out, out_lse=None, stream=None):
-        self._check_io(q, batch, out, out_lse, view._keep[0])
-        self._ck(self.lib.prhs_bytekv_decode_attn(self.h, _ptr(q), C.byref(view), batch, _ptr(out), _ptr(out_lse),
-                                                  _stream(stream)))
+        lse = self._check_io(q, batch, out, out_lse, view)
+        self._ck(self.lib.prhs_bytekv_decode_attn(self.h, q.data_ptr(), C.byref(view), batch, out.data_ptr(), lse, _stream(stream)))
 
     def bytekv_sparse_decode_attn(self, q, view, idx, count, batch, out, out_lse=None, stream=None):
-        self._check_io(q, batch, out, out_lse, view._keep[0])
-        assert idx.dtype == count.dtype == torch.int32 and idx.shape[:-1] == (batch, self.cfg.num_q_heads)
-        assert count.shape == idx.shape[:-1]
-        _same_device(q, idx, count)
-        self._ck(self.lib.prhs_bytekv_sparse_decode_attn(self.h, _ptr(q), C.byref(view), _ptr(idx), _ptr(count),
-                                                         idx.shape[-1], batch, _ptr(out), _ptr(out_lse), _stream(stream)))
+        lse = self._check_io(q, batch, out, out_lse, view)
+        stride = self._check_lists(q, idx, count, batch, self.cfg.num_q_heads)
+        self._ck(self.lib.prhs_bytekv_sparse_decode_attn(self.h, q.data_ptr(), C.byref(view), idx.data_ptr(), count.data_ptr(),
+                                                         stride, batch, out.data_ptr(), lse, _stream(stream)))
 
     # -- attention over selected blocks
     def block_bounds(self, view, bounds, batch, first=None, max_new=0, stream=None):
-        assert first is None or (first.dtype == torch.int32 and first.shape[0] >= batch)
-        _same_device(view._keep[0], bounds._keep[0], *(() if first is None else (first,)))
+        assert first is None or (first.dtype is _I32 and first.shape[0] >= batch)
+        self._fit_bounds(view, bounds, batch)
+        if first is not None:
+            _same_device(first, bounds._keep[0])
         self._ck(self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), _ptr(first), max_new, batch,
                                             _stream(stream)))
 
     def block_topk(self, q, view, bounds, sched, batch, out_blocks, out_count, stream=None):
-        self._check_blocks(q, batch, out_blocks, out_count, sched.flags)
-        _same_device(q, view._keep[0], bounds._keep[0])
-        self._ck(self.lib.prhs_block_topk(self.h, _ptr(q), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                          _ptr(out_blocks), out_blocks.shape[-1], _ptr(out_count), _stream(stream)))
+        shape = (batch, self.cfg.num_q_heads, 128)
+        assert q.dtype is _BF16 and q.shape == shape and q.is_contiguous()
+        stride = self._check_lists(q, out_blocks, out_count, batch, self._block_units(sched.flags))
+        _same_device(q, view._keep[0])
+        self._fit_bounds(view, bounds, batch)
+        self._ck(self.lib.prhs_block_topk(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                          out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream)))
 
     def block_decode_attn(self, q, view, blocks, count, batch, out, out_lse=None, flags=0, stream=None):
-        self._check_io(q, batch, out, out_lse, view._keep[0])
-        self._check_blocks(q, batch, blocks, count, flags)
-        self._ck(self.lib.prhs_block_decode_attn(self.h, _ptr(q), C.byref(view), _ptr(blocks), _ptr(count), blocks.shape[-1],
-                                                 flags, batch, _ptr(out), _ptr(out_lse), _stream(stream)))
+        lse = self._check_io(q, batch, out, out_lse, view)
+        stride = self._check_lists(q, blocks, count, batch, self._block_units(flags))
+        self._ck(self.lib.prhs_block_decode_attn(self.h, q.data_ptr(), C.byref(view), blocks.data_ptr(), count.data_ptr(), stride,
+                                                 flags, batch, out.data_ptr(), lse, _stream(stream)))
 
     def block_decode_step(self, q, view, bounds, sched, batch, out, out_lse, out_blocks, out_count, stream=None):
-        self._check_io(q, batch, out, out_lse, view._keep[0])
-        self._check_blocks(q, batch, out_blocks, out_count, sched.flags)
-        _same_device(q, bounds._keep[0])
-        self._ck(self.lib.prhs_block_decode_step(self.h, _ptr(q), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                                 _ptr(out), _ptr(out_lse), _ptr(out_blocks), out_blocks.shape[-1],
-                                                 _ptr(out_count), _stream(stream)))
+        lse = self._check_io(q, batch, out, out_lse, view)
+        stride = self._check_lists(q, out_blocks, out_count, batch, self._block_units(sched.flags))
+        self._fit_bounds(view, bounds, batch)
+        self._ck(self.lib.prhs_block_decode_step(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                                 out.data_ptr(), lse, out_blocks.data_ptr(), stride, out_count.data_ptr(),
+                                                 _stream(stream)))
 
-    def _check_io(self, q, batch, out, out_lse, cache):
-        rows = (batch, self.cfg.num_q_heads)
-        assert q.dtype == out.dtype == torch.bfloat16 and tuple(q.shape) == tuple(out.shape) == rows + (128,)
-        assert out_lse is None or (out_lse.dtype == torch.float32 and tuple(out_lse.shape) == rows)
-        _same_device(q, out, cache, *(() if out_lse is None else (out_lse,)))
+    def _fit(self, view, batch):
+        """The view against this context: heads, batch, and no length beyond a contiguous cache's capacity."""
+        assert view._heads == self.cfg.num_kv_heads and batch <= view._batch
+        cap = view._cap
+        if cap:
+            if view.max_seq_len == 0 and cap < self.cfg.max_context:
+                view.max_seq_len = cap
+            assert view.max_seq_len <= cap
 
-    def _check_blocks(self, q, batch, blocks, count, flags):
-        units = self.cfg.num_kv_heads if flags & PRHS_GROUP_SETS else self.cfg.num_q_heads
-        assert blocks.dtype == count.dtype == torch.int32 and tuple(blocks.shape[:-1]) == tuple(count.shape) == (batch, units)
-        _same_device(q, blocks, count)
+    def _fit_bounds(self, view, bounds, batch):
+        self._fit(view, batch)
+        codes = bounds._keep[0]
+        shape = codes.shape
+        assert shape[1] == view._heads
+        if view._cap:
+            assert len(shape) == 5 and shape[0] >= batch and shape[2] * 16 >= (view.max_seq_len or self.cfg.max_context)
+        else:
+            assert len(shape) == 4 and shape[0] >= view.num_pages
+        _same_device(view._keep[0], codes)
+
+    def _block_units(self, flags):
+        return self.cfg.num_kv_heads if flags & PRHS_GROUP_SETS else self.cfg.num_q_heads
+
+    def _check_io(self, q, batch, out, out_lse, view):
+        """Shapes, types and devices of a decode attention's tensors; the address of out_lse or None."""
+        self._fit(view, batch)
+        shape = q.shape
+        assert shape == (batch, self.cfg.num_q_heads, 128) and out.shape == shape and q.dtype is _BF16 and out.dtype is _BF16
+        assert q.is_contiguous() and out.is_contiguous()
+        if out_lse is None:
+            _same_device(q, out, view._keep[0])
+            return None
+        assert out_lse.dtype is _F32 and out_lse.shape == shape[:2] and out_lse.is_contiguous()
+        _same_device(q, out, view._keep[0], out_lse)
+        return out_lse.data_ptr()
+
+    def _check_lists(self, q, lists, count, batch, units):
+        shape = lists.shape
+        assert lists.dtype is _I32 and count.dtype is _I32 and shape[:-1] == (batch, units) and count.shape == (batch, units)
+        assert lists.is_contiguous() and count.is_contiguous()
+        _same_device(q, lists, count)
+        return shape[-1]
 
     def get_index_set(self, batch, stream=None):
         hq, cap = self.cfg.num_q_heads, self.index_capacity

@@ -41,6 +41,26 @@ prhs_status check_block_sched(prhs_ctx* ctx, const prhs_block_schedule* s, int b
 
 bool block_shared(const prhs_ctx* c, uint32_t flags) { return (flags & PRHS_GROUP_SETS) && c->gq > 1; }
 
+// Launch of a kernel that calls step_wait(): beside the end of the kernel before it in the stream (programmatic
+// dependent launch), or in plain stream order.
+template <typename P>
+cudaError_t launch_ordered(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p, int overlap) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = overlap;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+template <typename P>
+cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t st, const P& p) {
+  return launch_ordered(kernel, grid, threads, smem, st, p, 1);
+}
 prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const BoundsDev& bd, const prhs_block_schedule* s,
                               int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, bool update_last,
                               cudaStream_t st) {
@@ -57,11 +77,19 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   sp.update_last = update_last ? 1 : 0;
   sp.max_len = max_t;
   sp.flags = c->flags;
+  // about four waves of CTAs (four resident per SM), one to eight rounds per warp
   const int blocks = (max_t + kBlockRows - 1) / kBlockRows;
+  const int step = kScoreWarps * kScoreRound;
+  const long long chunks = (long long)batch * c->cfg.num_kv_heads * ((blocks + step - 1) / step);
+  sp.rounds = (int)std::min<long long>(8, std::max<long long>(1, chunks / (16ll * c->sm_count)));
+  const int per_cta = step * sp.rounds;
   {
     LaunchScope ls(c, PRHS_KIND_SCORE, st);
-    block_score_kernel<<<dim3((blocks + kScoreBlocks - 1) / kScoreBlocks, c->cfg.num_kv_heads, batch), kScoreWarps * 32, 0, st>>>(sp);
+    const dim3 grid((blocks + per_cta - 1) / per_cta, c->cfg.num_kv_heads, batch);
+    if (c->gq > 8) block_score_kernel<true><<<grid, kScoreWarps * 32, 0, st>>>(sp);
+    else block_score_kernel<false><<<grid, kScoreWarps * 32, 0, st>>>(sp);
   }
+  PRHS_CUDA(c, cudaGetLastError());
   BlockSelectParams p;
   p.scores = c->scores;
   p.ld = c->ld;
@@ -78,44 +106,45 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.max_len = max_t;
   {
     LaunchScope ls(c, PRHS_KIND_SELECT, st);
-    block_select_kernel<<<batch * p.units_per_seq, kBSThreads, 0, st>>>(p);
+    const dim3 grid(batch * p.units_per_seq);
+    cudaError_t e;
+    if (blocks <= 4 * kBSThreads) e = launch_after(block_select_kernel<4>, grid, kBSThreads, 0, st, p);
+    else if (blocks <= 8 * kBSThreads) e = launch_after(block_select_kernel<8>, grid, kBSThreads, 0, st, p);
+    else if (blocks <= 16 * kBSThreads) e = launch_after(block_select_kernel<16>, grid, kBSThreads, 0, st, p);
+    else if (blocks <= 32 * kBSThreads) e = launch_after(block_select_kernel<32>, grid, kBSThreads, 0, st, p);
+    else e = launch_after(block_select_kernel<0>, grid, kBSThreads, 0, st, p);
+    PRHS_CUDA(c, e);
   }
-  PRHS_CUDA(c, cudaGetLastError());
   return PRHS_OK;
 }
 
 prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
-                              uint32_t flags, int batch, void* out, float* out_lse, cudaStream_t st) {
+                              uint32_t flags, int batch, void* out, float* out_lse, bool after_select, cudaStream_t st) {
   const bool shared = block_shared(c, flags);
-  BlockAttnParams bp;
-  bp.units_per_seq = shared ? c->cfg.num_kv_heads : c->cfg.num_q_heads;
-  bp.blocks = blocks;
-  bp.count = count;
-  bp.stride = stride;
-  AttnParams& p = bp.a;
+  BlockAttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.kv = kv;
-  p.idx = nullptr;
-  p.count = nullptr;
-  p.idx_stride = 0;
-  p.set = SetRef{};
+  p.blocks = blocks;
+  p.count = count;
+  p.stride = stride;
+  p.heads_per_unit = shared ? c->gq : 1;
+  p.units_per_seq = c->cfg.num_q_heads / p.heads_per_unit;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  p.splits = pick_splits(c, batch * bp.units_per_seq, stride * kBlockRows);
+  p.splits = pick_splits(c, batch * p.units_per_seq, stride * kBlockRows);
   p.partials = c->partials;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
-  p.lse_full = nullptr;
-  p.out_delta = nullptr;
   p.flags = c->flags;
-  p.need = nullptr;
-  p.need_mode = 0;
   {
     LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
-    block_attn_kernel<<<dim3(p.splits, bp.units_per_seq, batch), kTThreads, kTSmemBytes, st>>>(bp);
+    // (a caller's own lists may come from any kernel: then the launch is an ordinary one)
+    const dim3 grid(p.splits, p.units_per_seq, batch);
+    const cudaError_t e = launch_ordered(p.heads_per_unit > 8 ? block_attn_kernel<true> : block_attn_kernel<false>, grid, kTThreads,
+                                         kTSmemBytes, st, p, after_select ? 1 : 0);
+    PRHS_CUDA(c, e);
   }
-  PRHS_CUDA(c, cudaGetLastError());
   return PRHS_OK;
 }
 
@@ -183,7 +212,7 @@ prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_v
   int max_t;
   prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, batch, out, out_lse, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, batch, out, out_lse, false, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
@@ -203,7 +232,7 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
   rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, true, as_stream(stream));
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, batch, out, out_lse, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, batch, out, out_lse, true, as_stream(stream));
 }
 
 }  // extern "C"

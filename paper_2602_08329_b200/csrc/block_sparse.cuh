@@ -126,6 +126,7 @@ struct BlockScoreParams {
   BoundsDev bd;
   float* scores;            // [B][Hq][ld]; group_max: the row of the group's first head
   int ld, num_q_heads, group_size, group_max;
+  int rounds;               // rounds per warp
   int update_last;          // 1: the bounds of the last block are recomputed here (its score is not used)
   int max_len;
   uint32_t* flags;
@@ -138,9 +139,9 @@ __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, ui
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The int8 codes of one head's query: this lane's words are dimensions 64h + 16tg + 4w .. + 3 (h, w in 0..1, 0..3).
-// Returns the scale (0 for an absent head).
-__device__ __forceinline__ float code_query(const __nv_bfloat16* q, bool has, uint32_t (&w)[2][4]) {
+// The int8 codes of one head's query, negative and positive part (minima meet the one, maxima the other): this lane's
+// words are dimensions 64h + 16tg + 4w .. + 3 (h, w in 0..1, 0..3).  Returns the scale (0 for an absent head).
+__device__ __forceinline__ float code_query(const __nv_bfloat16* q, bool has, uint32_t (&neg)[2][4], uint32_t (&pos)[2][4]) {
   const int tg = threadIdx.x & 3;
   uint4 x[2][2];
   uint32_t mx = 0u;
@@ -157,26 +158,43 @@ __device__ __forceinline__ float code_query(const __nv_bfloat16* q, bool has, ui
   amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
   const int e = scale_exponent<6, 126>(amax);
   const float inv = pow2i(-e);
-  auto code = [&](float v) { return (uint32_t)__float2int_rn(v * inv) & 0xffu; };
+  auto word = [&](uint32_t a, uint32_t z, uint32_t& n, uint32_t& q4) {       // four bf16 -> their codes' two parts
+    const int c[4] = {__float2int_rn(bf_lo(a) * inv), __float2int_rn(bf_hi(a) * inv), __float2int_rn(bf_lo(z) * inv), __float2int_rn(bf_hi(z) * inv)};
+    n = q4 = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      n |= ((uint32_t)min(c[i], 0) & 0xffu) << (8 * i);
+      q4 |= (uint32_t)max(c[i], 0) << (8 * i);
+    }
+  };
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      w[h][2 * i] = code(bf_lo(x[h][i].x)) | code(bf_hi(x[h][i].x)) << 8 | code(bf_lo(x[h][i].y)) << 16 | code(bf_hi(x[h][i].y)) << 24;
-      w[h][2 * i + 1] = code(bf_lo(x[h][i].z)) | code(bf_hi(x[h][i].z)) << 8 | code(bf_lo(x[h][i].w)) << 16 | code(bf_hi(x[h][i].w)) << 24;
+      word(x[h][i].x, x[h][i].y, neg[h][2 * i], pos[h][2 * i]);
+      word(x[h][i].z, x[h][i].w, neg[h][2 * i + 1], pos[h][2 * i + 1]);
     }
   return has ? pow2i(e) : 0.f;
 }
 
-// grid (chunks of kScoreBlocks blocks, Hkv, B).  A warp takes eight blocks at a time as the columns of
-// mma.sync m16n8k32 (int8 in, int32 accumulate) with the group's heads on the rows.  The B fragments come
-// straight from global memory: lane (g, tg) loads the four 16-byte pieces 4i + tg of block g's 256 bytes (64
-// contiguous bytes per block and instruction) and deals their words to the k-slots as they lie; the query's
-// fragments are dealt the same way.  No shared memory, eight MMAs per 2 KB.  Bound by the stream of bounds.
+// Programmatic dependent launch: a kernel of a step is launched while the one before it still runs, does what
+// does not depend on it, and waits here.  Every CTA waits, those without work too, so that a kernel that has
+// ended means that all before it have.
+__device__ __forceinline__ void step_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void step_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// grid (chunks, Hkv, B).  A warp takes eight blocks at a time as the columns of mma.sync m16n8k32 (int8 in, int32
+// accumulate) with the group's heads on the rows.  The B fragments come straight from global memory: lane
+// (g, tg) loads the four 16-byte pieces 4i + tg of block g's 256 bytes (64 contiguous bytes per block and
+// instruction) and deals their words to the k-slots as they lie; the query's fragments are dealt the same way.
+// No shared memory, eight MMAs per 2 KB.  Sixteen blocks (4 KB) per warp and round, the next round's loads in
+// flight under this one's arithmetic, page ids a round further ahead.  Bound by the stream of bounds.
 constexpr int kScoreWarps = 4;
-constexpr int kScoreTiles = 4;                                   // tiles of eight blocks per warp
-constexpr int kScoreBlocks = kScoreWarps * kScoreTiles * 8;      // 128 blocks, 32 KB of bounds per CTA
-__global__ void __launch_bounds__(kScoreWarps * 32) block_score_kernel(BlockScoreParams p) {
+constexpr int kScoreTiles = 2;                                   // tiles of eight blocks per round
+constexpr int kScoreRound = kScoreTiles * 8;
+template <bool kWide>
+__global__ void __launch_bounds__(kScoreWarps * 32, 4) block_score_kernel(BlockScoreParams p) {
+  step_release();
   const int kvh = blockIdx.y, b = blockIdx.z;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, tg = lane & 3;
@@ -194,62 +212,80 @@ __global__ void __launch_bounds__(kScoreWarps * 32) block_score_kernel(BlockScor
     else if (lane == 0)
       atomicOr(p.flags, kFlagBadPage);
   }
-  const int base = (blockIdx.x * kScoreWarps + warp) * (kScoreTiles * 8);
-  if (base >= nb) return;
-  // where the blocks of this warp lie: bounds index of block base + lane (32 = kScoreTiles * 8 blocks)
-  static_assert(kScoreTiles * 8 == 32, "one block per lane");
-  long long bi = -1;
-  if (base + lane < nb) {
-    long long row;
-    if (!locate_block(p.kv, p.bd, b, kvh, base + lane, row, bi)) {
+  // rounds of this warp: blocks [first + r * step, + kScoreRound), r < rounds
+  const int step = kScoreWarps * kScoreRound;
+  const int first = blockIdx.x * p.rounds * step + warp * kScoreRound;
+  if (first >= nb) return;
+  const int rounds = min(p.rounds, (nb - first + step - 1) / step);
+  auto locate = [&](int r) -> long long {              // bounds index of this lane's block (lanes 0..15)
+    const int blk = first + r * step + (lane & 15);
+    long long row, bi = -1;
+    if (r < rounds && blk < nb && !locate_block(p.kv, p.bd, b, kvh, blk, row, bi)) {
       atomicOr(p.flags, kFlagBadPage);
       bi = -1;
     }
-  }
-  const float my_scale = bi >= 0 ? p.bd.scale[bi] : 0.f;
-  uint4 x[kScoreTiles][4];
+    return bi;
+  };
+  auto fetch = [&](long long bi, uint4 (&x)[kScoreTiles][4], float& scale) {
+    scale = bi >= 0 ? __ldcg(p.bd.scale + bi) : 0.f;
 #pragma unroll
-  for (int n = 0; n < kScoreTiles; ++n) {
-    const long long at = __shfl_sync(0xffffffffu, bi, 8 * n + g);
+    for (int n = 0; n < kScoreTiles; ++n) {
+      const long long at = __shfl_sync(0xffffffffu, bi, 8 * n + g);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      x[n][i] = at >= 0 ? *reinterpret_cast<const uint4*>(p.bd.codes + at * kBoundsBytes + (4 * i + tg) * 16) : make_uint4(0u, 0u, 0u, 0u);
-  }
+      for (int i = 0; i < 4; ++i)
+        x[n][i] = at >= 0 ? __ldcg(reinterpret_cast<const uint4*>(p.bd.codes + at * kBoundsBytes + (4 * i + tg) * 16)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  uint4 cur[kScoreTiles][4], next[kScoreTiles][4];
+  float s_cur, s_next = 0.f;
+  fetch(locate(0), cur, s_cur);
+  long long bi_next = locate(1);
+
   const __nv_bfloat16* q0 = p.q + ((long long)b * p.num_q_heads + head0 + g) * kHeadDim;
-  const bool has0 = g < gq, has1 = g + 8 < gq;
-  uint32_t w0[2][4], w1[2][4];
-  const float qs0 = code_query(q0, has0, w0);
-  const float qs1 = code_query(q0 + 8 * kHeadDim, has1, w1);
+  const bool has0 = g < gq, has1 = kWide && g + 8 < gq;
+  uint32_t n0[2][4], p0[2][4], n1[2][4], p1[2][4];      // heads g and g + 8
+  const float qs0 = code_query(q0, has0, n0, p0);
+  float qs1 = 0.f;
+  if (kWide) qs1 = code_query(q0 + 8 * kHeadDim, has1, n1, p1);
+  for (int r = 0; r < rounds; ++r) {
+    fetch(bi_next, next, s_next);
+    bi_next = locate(r + 2);
 #pragma unroll
-  for (int n = 0; n < kScoreTiles; ++n) {
-    if (base + 8 * n >= nb) break;
-    int d[4] = {0, 0, 0, 0};
+    for (int n = 0; n < kScoreTiles; ++n) {
+      const int blk = first + r * step + 8 * n + 2 * tg;
+      int d[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int h = i & 1;                       // pieces 0, 1: minima of dimensions 64h..; 2, 3: maxima
-      auto part = [&](uint32_t w) { return i < 2 ? __vmins4(w, 0u) : __vmaxs4(w, 0u); };
-      mma_s8(d, part(w0[h][0]), part(w1[h][0]), part(w0[h][1]), part(w1[h][1]), x[n][i].x, x[n][i].y);
-      mma_s8(d, part(w0[h][2]), part(w1[h][2]), part(w0[h][3]), part(w1[h][3]), x[n][i].z, x[n][i].w);
-    }
-    const int blk = base + 8 * n + 2 * tg;
-    const float s0 = __shfl_sync(0xffffffffu, my_scale, 8 * n + 2 * tg), s1 = __shfl_sync(0xffffffffu, my_scale, 8 * n + 2 * tg + 1);
-    float v[4] = {(float)d[0] * s0 * qs0, (float)d[1] * s1 * qs0, (float)d[2] * s0 * qs1, (float)d[3] * s1 * qs1};
-    if (p.group_max) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float m = fmaxf(has0 ? v[c] : -INFINITY, has1 ? v[2 + c] : -INFINITY);
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-        v[c] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+      for (int i = 0; i < 4; ++i) {
+        const int h = i & 1;                     // pieces 0, 1: minima of dimensions 64h..; 2, 3: maxima
+        auto w0 = [&](int k) { return i < 2 ? n0[h][k] : p0[h][k]; };
+        auto w1 = [&](int k) { return !kWide ? 0u : i < 2 ? n1[h][k] : p1[h][k]; };
+        mma_s8(d, w0(0), w1(0), w0(1), w1(1), cur[n][i].x, cur[n][i].y);
+        mma_s8(d, w0(2), w1(2), w0(3), w1(3), cur[n][i].z, cur[n][i].w);
       }
+      const float s0 = __shfl_sync(0xffffffffu, s_cur, 8 * n + 2 * tg), s1 = __shfl_sync(0xffffffffu, s_cur, 8 * n + 2 * tg + 1);
+      float v[4] = {(float)d[0] * s0 * qs0, (float)d[1] * s1 * qs0, (float)d[2] * s0 * qs1, (float)d[3] * s1 * qs1};
+      if (p.group_max) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float m = fmaxf(has0 ? v[c] : -INFINITY, has1 ? v[2 + c] : -INFINITY);
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+          v[c] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+        }
+      }
+      auto store = [&](int head, float a, float z) {
+        float* dst = p.scores + ((long long)b * p.num_q_heads + head0 + head) * p.ld + blk;
+        if (blk + 1 < nb) *reinterpret_cast<float2*>(dst) = make_float2(a, z);
+        else if (blk < nb) *dst = a;
+      };
+      if (p.group_max ? g == 0 : has0) store(g, v[0], v[1]);
+      if (!p.group_max && has1) store(g + 8, v[2], v[3]);
     }
-    auto store = [&](int head, float a, float z) {
-      float* dst = p.scores + ((long long)b * p.num_q_heads + head0 + head) * p.ld + blk;
-      if (blk + 1 < nb) *reinterpret_cast<float2*>(dst) = make_float2(a, z);
-      else if (blk < nb) *dst = a;
-    };
-    if (p.group_max ? g == 0 : has0) store(g, v[0], v[1]);
-    if (!p.group_max && has1) store(g + 8, v[2], v[3]);
+#pragma unroll
+    for (int n = 0; n < kScoreTiles; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cur[n][i] = next[n][i];
+    s_cur = s_next;
   }
 }
 
@@ -266,20 +302,24 @@ struct BlockSelectParams {
 };
 
 // One CTA per unit (a query head, or a KV head where the group shares a set).  The unit attends over blocks
-// [0, lo), the `top` best of [lo, hi), and [hi, nb).  The threshold is found by narrowing an interval of keys
-// (the scores' order-preserving 32-bit images): a histogram of 1024 equal bins over the interval says which
-// bin the top-th key lies in; that bin is the next interval, until it is one key wide.  Scores of one unit lie
-// close together, so bins over their own range spread them (bins over the leading bits would not, and the
-// shared-memory atomics would serialise).  Then one ordered pass writes the list.
+// [0, lo), the `top` best of [lo, hi), and [hi, nb).  The scores are read once into registers (kKeys per
+// thread, 512 threads; kKeys = 0 reads them again in every pass, for more than 16384 blocks).  The threshold
+// is found by narrowing an interval of keys (the scores' order-preserving 32-bit images): a histogram of 1024
+// equal bins over the interval says which bin the top-th key lies in, and that bin is the next interval.
+// Scores of one unit lie close together, so bins over their own range spread them (bins over the leading
+// bits would not, and the shared-memory atomics would serialise).  With at most 32 keys left in the bin, a warp
+// ranks them directly; that is usually after one histogram.  Then one ordered pass writes the list.
 constexpr int kBSThreads = 512;
-constexpr int kBSBins = 1024;
+constexpr int kBSWarps = kBSThreads / 32;
+constexpr int kBSBins = 2 * kBSThreads;
+template <int kKeys>
 __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectParams p) {
-  constexpr int kW = kBSThreads / 32;
   __shared__ int hist[kBSBins];
-  __shared__ uint32_t red_lo[kW], red_hi[kW];
-  __shared__ int warp_gt[kW], warp_eq[kW];
+  __shared__ uint32_t red_lo[kBSWarps], red_hi[kBSWarps], cand[32];
+  __shared__ int warp_a[kBSWarps], warp_b[kBSWarps];
   __shared__ uint32_t sh_base, sh_span;
-  __shared__ int sh_need;
+  __shared__ int sh_need, sh_count, sh_cands;
+  step_release();
   const int unit = blockIdx.x;
   const int b = unit / p.units_per_seq, u = unit % p.units_per_seq;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -295,184 +335,231 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
     else if (i >= total) out[i] = -1;
     else if (i >= lo + need0) out[i] = hi + (i - lo - need0);
   }
-  if (tid == 0) p.out_count[unit] = total;
+  hist[2 * tid] = 0;
+  hist[2 * tid + 1] = 0;
+  if (tid == 0) { p.out_count[unit] = total; sh_cands = 0; }
+  step_wait();
   if (need0 == 0) return;
-  // the threshold: keys above `thr` are taken, and the first `need` (by position) of those equal to it
-  uint32_t thr = 0u;
-  int need = need0;
-  if (need0 < hi - lo) {
-    uint32_t kmin = 0xffffffffu, kmax = 0u;
-    for (int i = lo + tid; i < hi; i += kBSThreads) {
-      const uint32_t k = float_to_key(__ldg(s + i));
-      kmin = min(kmin, k);
-      kmax = max(kmax, k);
-    }
-    kmin = __reduce_min_sync(0xffffffffu, kmin);
-    kmax = __reduce_max_sync(0xffffffffu, kmax);
-    if (lane == 0) { red_lo[warp] = kmin; red_hi[warp] = kmax; }
-    __syncthreads();
-    for (int w = 0; w < kW; ++w) { kmin = min(kmin, red_lo[w]); kmax = max(kmax, red_hi[w]); }
-    uint32_t base = kmin, span = kmax - kmin;        // the interval [base, base + span]
-    while (span > 0u) {
-      const int shift = max(0, 32 - __clz(span) - 10);   // (key - base) >> shift < 1024
-      for (int i = tid; i < kBSBins; i += kBSThreads) hist[i] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += kBSThreads) {
-        const uint32_t k = float_to_key(__ldg(s + i)) - base;
-        if (k <= span) atomicAdd(&hist[k >> shift], 1);
-      }
-      __syncthreads();
-      // warp 0 walks the bins from the top: lane l owns bins 1023 - 32 l .. 992 - 32 l
-      if (warp == 0) {
-        int sum = 0;
-        for (int i = 0; i < 32; ++i) sum += hist[kBSBins - 1 - (32 * lane + i)];
-        int incl = sum;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, incl, off);
-          if (lane >= off) incl += v;
-        }
-        int above = incl - sum;
-        if (above < need && incl >= need) {              // exactly one lane
-          int bin = kBSBins - 1 - 32 * lane;
-          while (above + hist[bin] < need) above += hist[bin--];
-          sh_base = base + ((uint32_t)bin << shift);
-          sh_span = min((1u << shift) - 1u, span - ((uint32_t)bin << shift));
-          sh_need = need - above;
-        }
-      }
-      __syncthreads();
-      base = sh_base;
-      span = sh_span;
-      need = sh_need;
-      __syncthreads();
-    }
-    thr = base;
+  if (need0 == hi - lo) {                          // every block of the middle
+    for (int i = tid; i < need0; i += kBSThreads) out[lo + i] = lo + i;
+    return;
   }
-  const bool all = need0 == hi - lo;
-  // ordered pass: every warp owns a run of positions; counts first, then places
-  const int run = ((hi - lo + kW - 1) / kW + 31) & ~31;
+  // every warp owns a run of positions, a lane every 32nd of it
+  const int run = (hi - lo + kBSThreads - 1) / kBSThreads * 32;
   const int from = lo + warp * run, to = min(from + run, hi);
-  int gt = 0, eq = 0;
-  for (int i = from; i < to; i += 32) {
-    const uint32_t k = i + lane < to ? float_to_key(__ldg(s + i + lane)) : 0u;
-    const bool in = i + lane < to;
-    gt += __popc(__ballot_sync(0xffffffffu, in && (all || k > thr)));
-    eq += __popc(__ballot_sync(0xffffffffu, in && !all && k == thr));
+  uint32_t keys[kKeys > 0 ? kKeys : 1];
+  auto fetch = [&](int r) -> uint32_t { return from + 32 * r + lane < to ? float_to_key(__ldcg(s + from + 32 * r + lane)) : 0u; };
+  // f(r, whether the position exists, its key) over this thread's positions
+  auto each = [&](auto f) {
+    if constexpr (kKeys > 0) {
+#pragma unroll
+      for (int r = 0; r < kKeys; ++r)
+        if (32 * r < run) f(r, from + 32 * r + lane < to, keys[r]);
+    } else {
+      for (int r = 0; 32 * r < run; ++r) f(r, from + 32 * r + lane < to, fetch(r));
+    }
+  };
+  if constexpr (kKeys > 0) {
+#pragma unroll
+    for (int r = 0; r < kKeys; ++r) keys[r] = fetch(r);
   }
-  if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
+  uint32_t kmin = 0xffffffffu, kmax = 0u;
+  each([&](int, bool in, uint32_t k) {
+    if (in) { kmin = min(kmin, k); kmax = max(kmax, k); }
+  });
+  kmin = __reduce_min_sync(0xffffffffu, kmin);
+  kmax = __reduce_max_sync(0xffffffffu, kmax);
+  if (lane == 0) { red_lo[warp] = kmin; red_hi[warp] = kmax; }
+  __syncthreads();
+  kmin = __reduce_min_sync(0xffffffffu, red_lo[lane & (kBSWarps - 1)]);
+  kmax = __reduce_max_sync(0xffffffffu, red_hi[lane & (kBSWarps - 1)]);
+  // the threshold: keys above `thr` are taken, and the first `need` (by position) of those equal to it
+  uint32_t base = kmin, span = kmax - kmin;          // the interval [base, base + span]
+  int need = need0;
+  while (span > 0u) {
+    const int shift = max(0, 32 - __clz(span) - 10);   // (key - base) >> shift < 1024
+    each([&](int, bool in, uint32_t k) {
+      if (in && k - base <= span) atomicAdd(&hist[(k - base) >> shift], 1);
+    });
+    __syncthreads();
+    // bins from the top: thread i owns the pair 1023 - 2i, 1022 - 2i
+    const int top_bin = kBSBins - 1 - 2 * tid;
+    const int c0 = hist[top_bin], c1 = hist[top_bin - 1];
+    hist[top_bin] = 0;
+    hist[top_bin - 1] = 0;
+    int incl = c0 + c1;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += v;
+    }
+    if (lane == 31) warp_a[warp] = incl;
+    __syncthreads();
+    incl += __reduce_add_sync(0xffffffffu, lane < warp ? warp_a[lane] : 0);
+    const int above = incl - c0 - c1;
+    if (above < need && incl >= need) {                // exactly one thread
+      const bool second = above + c0 < need;
+      const int bin = second ? top_bin - 1 : top_bin;
+      sh_base = base + ((uint32_t)bin << shift);
+      sh_span = min((1u << shift) - 1u, span - ((uint32_t)bin << shift));
+      sh_need = need - above - (second ? c0 : 0);
+      sh_count = second ? c1 : c0;
+    }
+    __syncthreads();
+    base = sh_base;
+    span = sh_span;
+    need = sh_need;
+    if (span > 0u && sh_count <= 32) {                 // few enough to rank directly
+      each([&](int, bool in, uint32_t k) {
+        if (in && k - base <= span) cand[atomicAdd(&sh_cands, 1)] = k;
+      });
+      __syncthreads();
+      const int n = sh_count;
+      const uint32_t k = lane < n ? cand[lane] : 0u;
+      int gt = 0, ge = 0;
+      for (int i = 0; i < n; ++i) {
+        const uint32_t other = __shfl_sync(0xffffffffu, k, i);
+        gt += other > k;
+        ge += other >= k;
+      }
+      const uint32_t who = __ballot_sync(0xffffffffu, lane < n && gt < need && ge >= need);
+      const int at = __ffs(who) - 1;                   // the threshold key (any of its equals)
+      base = __shfl_sync(0xffffffffu, k, at);
+      need -= __shfl_sync(0xffffffffu, gt, at);
+      break;
+    }
+  }
+  const uint32_t thr = base;
+  int gt = 0, eq = 0;
+  each([&](int, bool in, uint32_t k) {
+    gt += __popc(__ballot_sync(0xffffffffu, in && k > thr));
+    eq += __popc(__ballot_sync(0xffffffffu, in && k == thr));
+  });
+  __syncthreads();                                     // warp_a is read above
+  if (lane == 0) { warp_a[warp] = gt; warp_b[warp] = eq; }
   __syncthreads();
   int eq_before = 0, place = lo;
   for (int w = 0; w < warp; ++w) {
-    place += warp_gt[w] + max(0, min(warp_eq[w], need - eq_before));
-    eq_before += warp_eq[w];
+    place += warp_a[w] + max(0, min(warp_b[w], need - eq_before));
+    eq_before += warp_b[w];
   }
-  for (int i = from; i < to; i += 32) {
-    const bool in = i + lane < to;
-    const uint32_t k = in ? float_to_key(__ldg(s + i + lane)) : 0u;
+  each([&](int r, bool in, uint32_t k) {
     const uint32_t below = (1u << lane) - 1u;
-    const uint32_t eqm = __ballot_sync(0xffffffffu, in && !all && k == thr);
-    const bool take = in && (all || k > thr || (k == thr && eq_before + __popc(eqm & below) < need));
+    const uint32_t eqm = __ballot_sync(0xffffffffu, in && k == thr);
+    const bool take = in && (k > thr || (k == thr && eq_before + __popc(eqm & below) < need));
     const uint32_t tm = __ballot_sync(0xffffffffu, take);
-    if (take) out[place + __popc(tm & below)] = i + lane;
+    if (take) out[place + __popc(tm & below)] = from + 32 * r + lane;
     place += __popc(tm);
     eq_before += __popc(eqm);
-  }
+  });
 }
 
 // ------------------------------------------------------------------------------- attention
-// Attention over listed blocks of a bf16 cache.  kGroup: one list per KV head, its heads on the rows of the MMA
-// tile (the arithmetic of the dense kernel); else one list per query head.  grid (splits, units per
-// sequence, B).  A stage of the warp-private ring is one block, whose rows are contiguous; rows past the
-// end of the sequence are masked.  Partials, tickets and merge as in the dense kernel.
+// Attention over listed blocks of a bf16 cache: one list per query head, or one per KV head for its whole group.
+// grid (splits, units per sequence, B).  A stage of the warp-private ring is one block, whose rows are
+// contiguous; rows past the end of the sequence are masked.  The arithmetic is bf16_stage: 16 MMAs per block
+// for up to eight heads (kWide: 32 for up to sixteen).
 struct BlockAttnParams {
-  AttnParams a;             // q, kv, splits, partials, tickets, out, out_lse, flags; set and idx unused
+  const __nv_bfloat16* q;
+  KvDev kv;
   const int* blocks;        // [B][units][stride]
   const int* count;
   int stride, units_per_seq;
+  int num_q_heads, group_size, heads_per_unit, splits;
+  float* partials;          // [B][Hq][splits][kPartStride]
+  unsigned int* tickets;
+  __nv_bfloat16* out;
+  float* out_lse;
+  uint32_t* flags;
 };
 
-__global__ void __launch_bounds__(kTThreads) block_attn_kernel(BlockAttnParams bp) {
+template <bool kWide>
+__global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParams p) {
+  constexpr int kTiles = kWide ? 2 : 1;
   extern __shared__ __align__(128) unsigned char g_smem[];
-  const AttnParams& p = bp.a;
+  __shared__ float sm_m[kTWarps][16], sm_l[kTWarps][16], sm_lt[kTWarps][16];
+  __shared__ bool is_last;
   const int split = blockIdx.x, u = blockIdx.y, b = blockIdx.z;
-  const bool shared = bp.units_per_seq * p.group_size == p.num_q_heads && p.group_size > 1;
-  const int gq = shared ? p.group_size : 1;
-  const int head0 = u * gq, kvh = shared ? u : u / p.group_size;
+  const int gq = p.heads_per_unit;
+  const int head0 = u * gq, kvh = head0 / p.group_size;
+  const int unit0 = b * p.num_q_heads + head0;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int g = lane >> 2, tg = lane & 3;
+  const int g = lane >> 2;
   const int t = __ldg(p.kv.seq_lens + b);
   const int nb = (t + kBlockRows - 1) / kBlockRows;
-  const long long unit = (long long)b * bp.units_per_seq + u;
-  const int* list = bp.blocks + unit * bp.stride;
-  const int cnt = min(max(__ldg(bp.count + unit), 0), bp.stride);
+  const long long unit = (long long)b * p.units_per_seq + u;
+  const int* list = p.blocks + unit * p.stride;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kTStages * kTStageBytes);
+
+  uint32_t qb[kTiles][8][2];
+  load_query_bf16<kTiles>(p.q + (long long)unit0 * kHeadDim, gq, qb);
+  float o[kTiles][8][4];
+  clear_tiles<kTiles>(o);
+  SoftBf st[kTiles][2];
+
+  step_wait();                             // the lists may come from the kernel before this one
+  const int cnt = min(max(__ldcg(p.count + unit), 0), p.stride);
   const int per = (cnt + p.splits * kTWarps - 1) / (p.splits * kTWarps);
   const int start = min((split * kTWarps + warp) * per, cnt);
   const int nstages = min(start + per, cnt) - start;
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kTStages * kTStageBytes);
-  const bool has0 = g < gq, has1 = g + 8 < gq;
 
-  uint32_t aq[8][4];
-  {
-    const uint32_t* q0 = reinterpret_cast<const uint32_t*>(p.q + ((long long)b * p.num_q_heads + head0 + g) * kHeadDim);
-    const uint32_t* q1 = q0 + 8 * (kHeadDim / 2);
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      aq[ks][0] = has0 ? __ldg(q0 + ks * 8 + tg) : 0u;
-      aq[ks][1] = has1 ? __ldg(q1 + ks * 8 + tg) : 0u;
-      aq[ks][2] = has0 ? __ldg(q0 + ks * 8 + 4 + tg) : 0u;
-      aq[ks][3] = has1 ? __ldg(q1 + ks * 8 + 4 + tg) : 0u;
-    }
-  }
-  float o[16][4];
-#pragma unroll
-  for (int nt = 0; nt < 16; ++nt) { o[nt][0] = 0.f; o[nt][1] = 0.f; o[nt][2] = 0.f; o[nt][3] = 0.f; }
-  float m0 = -INFINITY, l0 = 0.f, m1 = -INFINITY, l1 = 0.f, lt0 = 0.f, lt1 = 0.f;
-
-  // block numbers and page ids of 32 list entries, one per lane, a group ahead of their use
+  // where 32 listed blocks lie (element offset and real rows), one per lane, looked up a group ahead
+  const bool paged = p.kv.page_table != nullptr;
   auto entry = [&](int grp) -> int {
     const int j = grp * 32 + lane;
     if (j >= nstages) return -1;
-    const int blk = __ldg(list + start + j);
+    const int blk = __ldcg(list + start + j);
     if ((unsigned)blk >= (unsigned)nb) {
       atomicOr(p.flags, kFlagBadIndex);
       return -1;
     }
     return blk;
   };
-  const bool paged = p.kv.page_table != nullptr;
   auto page_of = [&](int blk) -> int {
     return (paged && blk >= 0) ? __ldg(p.kv.page_table + (long long)b * p.kv.page_table_stride + blk) : 0;
   };
-  int blk_cur = entry(0), pg_cur = page_of(blk_cur);
-  int blk_next = entry(1), pg_next = page_of(blk_next);
+  long long off_cur = 0;
+  int rows_cur = 0;
+  auto place_group = [&](int blk, int page) {
+    rows_cur = blk >= 0 ? min(kBlockRows, t - blk * kBlockRows) : 0;
+    if (paged && rows_cur > 0 && (unsigned)page >= (unsigned)p.kv.num_pages) {
+      atomicOr(p.flags, kFlagBadPage);
+      rows_cur = 0;
+    }
+    off_cur = (long long)(paged ? page : b) * p.kv.stride_outer + (long long)kvh * p.kv.stride_head +
+              (paged ? 0ll : (long long)blk * (kBlockRows * kHeadDim));
+    if (rows_cur == 0) off_cur = 0;
+  };
+  int blk_next = entry(0), pg_next = page_of(blk_next);
+  place_group(blk_next, pg_next);
+  blk_next = entry(1);
+  pg_next = page_of(blk_next);
 
-  const __nv_bfloat16* src_base = (lane < 16 ? p.kv.k : p.kv.v) + (lane & 15) * 8;
-  const uint32_t dst_tile = (lane < 16 ? 0u : (uint32_t)kTTileBytes);
-  const long long lin = (long long)b * p.kv.stride_outer + (long long)kvh * p.kv.stride_head;
+  // a lane copies one 16-byte chunk of every row: lanes 0-15 of K, 16-31 of V
+  const __nv_bfloat16* src_base = lane < 16 ? p.kv.k : p.kv.v;
+  const uint32_t dst_lane = ring + (lane < 16 ? 0u : (uint32_t)kTTileBytes) + ((lane & 15u) << 4);
+  uint32_t sx[8];                          // source chunk that the swizzle wants at this lane's place, by row mod 8
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sx[k] = (((uint32_t)lane & 15u) ^ (uint32_t)k) << 3;
   int rows_of[kTStages];                   // real rows per ring slot (slots are compile-time below)
   auto issue = [&](int j, auto slot_c) {
     constexpr int kSlot = decltype(slot_c)::value;
     if (j < nstages) {
       if (j > 0 && (j & 31) == 0) {
-        blk_cur = blk_next; pg_cur = pg_next;
+        place_group(blk_next, pg_next);
         blk_next = entry((j >> 5) + 1);
         pg_next = page_of(blk_next);
       }
-      const int blk = __shfl_sync(0xffffffffu, blk_cur, j & 31);
-      const int page = __shfl_sync(0xffffffffu, pg_cur, j & 31);
-      int rows = blk >= 0 ? min(kBlockRows, t - blk * kBlockRows) : 0;
-      if (paged && rows > 0 && (unsigned)page >= (unsigned)p.kv.num_pages) {
-        if (lane == 0) atomicOr(p.flags, kFlagBadPage);
-        rows = 0;
-      }
-      const long long off = rows == 0 ? 0ll : paged ? (long long)page * p.kv.stride_outer + (long long)kvh * p.kv.stride_head
-                                                    : lin + (long long)blk * (kBlockRows * kHeadDim);
-      const uint32_t slot = ring + (uint32_t)kSlot * kTStageBytes + dst_tile;
+      const __nv_bfloat16* src = src_base + __shfl_sync(0xffffffffu, off_cur, j & 31);
+      const int rows = __shfl_sync(0xffffffffu, rows_cur, j & 31);
+      const uint32_t dst = dst_lane + (uint32_t)kSlot * kTStageBytes;
+      if (rows == kBlockRows) {
 #pragma unroll
-      for (int r = 0; r < kTStageRows; ++r) {
-        const uint32_t dst = slot + r * kRowBytes + ((((uint32_t)lane & 15u) ^ (r & 7u)) << 4);
-        cp_async_16(dst, src_base + (r < rows ? off + (long long)r * kHeadDim : 0ll), r < rows ? 16 : 0);
+        for (int r = 0; r < kTStageRows; ++r) cp_async_16_full(dst + r * kRowBytes, src + r * kHeadDim + sx[r & 7]);
+      } else {
+#pragma unroll
+        for (int r = 0; r < kTStageRows; ++r)
+          cp_async_16(dst + r * kRowBytes, src + (r < rows ? r * kHeadDim + sx[r & 7] : 0), r < rows ? 16 : 0);
       }
       rows_of[kSlot] = rows;
     }
@@ -488,8 +575,7 @@ __global__ void __launch_bounds__(kTThreads) block_attn_kernel(BlockAttnParams b
     issue(i + kTStages - 1, SlotC<(kSlot + kTStages - 1) % kTStages>{});
     if (rows == 0) return;
     const uint32_t kt = ring + (uint32_t)kSlot * kTStageBytes;
-    group_stage(kt, kt + kTTileBytes, aq, 2 * tg < rows, 2 * tg + 1 < rows, 8 + 2 * tg < rows, 9 + 2 * tg < rows, o, m0, l0,
-                m1, l1, lt0, lt1);
+    bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, gq, g < rows, g + 8 < rows, o, st);
   };
   int i = 0;
   for (; i + 2 < nstages; i += 3) {
@@ -500,7 +586,13 @@ __global__ void __launch_bounds__(kTThreads) block_attn_kernel(BlockAttnParams b
   if (i < nstages) stage(i, SlotC<0>{});
   if (i + 1 < nstages) stage(i + 1, SlotC<1>{});
   cp_async_wait<0>();
-  group_epilogue(p, g_smem, b, head0, gq, split, o, m0, l0, m1, l1, lt0, lt1);
+  __syncthreads();                         // the ring is free: it takes the warps' partials
+  float* sm_o = reinterpret_cast<float*>(g_smem);
+  store_partial_bf16<kTiles>(o, st, gq, sm_o + warp * gq * kHeadDim, sm_m[warp], sm_l[warp], sm_lt[warp]);
+  __syncthreads();
+  auto part_row = [&](int head, int part) -> float* { return p.partials + ((long long)(unit0 + head) * p.splits + part) * kPartStride; };
+  finish_unit(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], kTWarps, gq, p.splits, split, part_row, p.tickets, p.out, p.out_lse, unit0,
+              &is_last);
 }
 
 }  // namespace prhs

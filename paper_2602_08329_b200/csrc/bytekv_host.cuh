@@ -13,11 +13,15 @@ prhs_status check_device(prhs_ctx* c) {
 }
 
 cudaError_t bytekv_set_attributes() {
-  const void* kernels[] = {(const void*)bytekv_attn_kernel<kE4M3, false, false>, (const void*)bytekv_attn_kernel<kE4M3, false, true>,
-                           (const void*)bytekv_attn_kernel<kE4M3, true, false>,  (const void*)bytekv_attn_kernel<kE5M2, false, false>,
-                           (const void*)bytekv_attn_kernel<kE5M2, false, true>,  (const void*)bytekv_attn_kernel<kE5M2, true, false>};
-  for (const void* k : kernels) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, k8SmemBytes);
+  const struct { const void* kernel; int bytes; } all[] = {
+      {(const void*)bytekv_attn_kernel<kE4M3, false, false>, Shape8<false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE4M3, false, true>, Shape8<true>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE4M3, true, false>, Shape8<false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, false, false>, Shape8<false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, false, true>, Shape8<true>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, true, false>, Shape8<false>::kSmemBytes}};
+  for (const auto& k : all) {
+    const cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -72,28 +76,31 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.idx = idx;
   p.count = count;
   p.idx_stride = idx_stride;
+  p.batch = batch;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  const int units = idx ? c->cfg.num_q_heads : c->cfg.num_kv_heads;
-  p.splits = pick_splits(c, batch * units, max_count);
-  p.partials = c->partials;
+  p.splits = idx ? pick_splits(c, batch * c->cfg.num_q_heads, max_count) : 1;
+  p.partials = idx ? c->partials : c->stream_part;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
   p.flags = c->flags;
-  const dim3 grid(p.splits, units, batch);
+  // dense: one CTA per resident slot at most, each with a run of at least k8MinRun blocks
+  const long long blocks = (long long)batch * c->cfg.num_kv_heads * std::max(1, (max_count + kBlockRows - 1) / kBlockRows);
+  const int ctas = (int)std::min<long long>((c->gq > 8 ? Shape8<true>::kCtasPerSm : Shape8<false>::kCtasPerSm) * c->sm_count, (blocks + k8MinRun - 1) / k8MinRun);
+  const dim3 grid = idx ? dim3(p.splits, c->cfg.num_q_heads, batch) : dim3(ctas, 1, 1);
   {
     LaunchScope ls(c, idx ? PRHS_KIND_ATTN_SPARSE : PRHS_KIND_ATTN_DENSE, st);
     const bool e4 = format == PRHS_BYTEKV_E4M3;
     if (idx) {
-      if (e4) bytekv_attn_kernel<kE4M3, true, false><<<grid, k8Threads, k8SmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, true, false><<<grid, k8Threads, k8SmemBytes, st>>>(p);
+      if (e4) bytekv_attn_kernel<kE4M3, true, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
+      else bytekv_attn_kernel<kE5M2, true, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
     } else if (c->gq > 8) {
-      if (e4) bytekv_attn_kernel<kE4M3, false, true><<<grid, k8Threads, k8SmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, false, true><<<grid, k8Threads, k8SmemBytes, st>>>(p);
+      if (e4) bytekv_attn_kernel<kE4M3, false, true><<<grid, k8Threads, Shape8<true>::kSmemBytes, st>>>(p);
+      else bytekv_attn_kernel<kE5M2, false, true><<<grid, k8Threads, Shape8<true>::kSmemBytes, st>>>(p);
     } else {
-      if (e4) bytekv_attn_kernel<kE4M3, false, false><<<grid, k8Threads, k8SmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, false, false><<<grid, k8Threads, k8SmemBytes, st>>>(p);
+      if (e4) bytekv_attn_kernel<kE4M3, false, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
+      else bytekv_attn_kernel<kE5M2, false, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
     }
   }
   PRHS_CUDA(c, cudaGetLastError());

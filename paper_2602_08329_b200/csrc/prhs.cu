@@ -64,6 +64,7 @@ struct prhs_ctx {
   float* lse_full = nullptr;
   float* lse_c = nullptr;
   float* partials = nullptr;
+  float* stream_part = nullptr;     // parts of units that two CTAs of the 8-bit dense attention share
   unsigned int* tickets = nullptr;
   int* idx = nullptr;
   int* count = nullptr;
@@ -816,7 +817,9 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
     e = cudaFuncSetAttribute(dense_attn_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
   if (e == cudaSuccess) e = bytekv_set_attributes();
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(block_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
+    e = cudaFuncSetAttribute(block_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(block_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
   if (e == cudaSuccess) {
     int nb = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, gather_attn_mma_kernel, kTThreads, kTSmemBytes);
@@ -832,6 +835,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = dev_alloc(&c->lse_full, U);
   if (e == cudaSuccess) e = dev_alloc(&c->lse_c, U);
   if (e == cudaSuccess) e = dev_alloc(&c->partials, U * kMaxSplits * kPartStride);
+  if (e == cudaSuccess) e = dev_alloc(&c->stream_part, (size_t)2 * k8MaxCtasPerSm * c->sm_count * c->gq * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->tickets, U);
   if (e == cudaSuccess) e = dev_alloc(&c->idx, U * c->idx_cap);
   if (e == cudaSuccess) e = dev_alloc(&c->count, U);
@@ -877,7 +881,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
 
 prhs_status prhs_destroy(prhs_ctx* c) {
   if (!c) return PRHS_OK;
-  void* ptrs[] = {c->scores, c->part_ml, c->lse_full, c->lse_c, c->partials, c->tickets, c->idx,
+  void* ptrs[] = {c->scores, c->part_ml, c->lse_full, c->lse_c, c->partials, c->stream_part, c->tickets, c->idx,
                   c->count, c->flags, c->scratch_out, c->sstar_desc, c->sstar_asc, c->shat_asc,
                   c->n_star, c->n_hat, c->anchor_t, c->qhist, c->set_of_pos, c->nsets, c->g_need,
                   c->g_slot, c->g_ref, c->st_q, c->st_out, c->st_k, c->st_v};
