@@ -189,14 +189,14 @@ constexpr int k8MetaBytes = 160;                                        // 16 K 
 // With more than eight heads the accumulators need twice the registers: three CTAs per SM, deeper rings.
 template <bool kWide>
 struct Shape8 {
-  static constexpr int kStages = kWide ? 4 : 3;
-  static constexpr int kCtasPerSm = kWide ? 3 : 4;
+  static constexpr int kStages = 4;
+  static constexpr int kCtasPerSm = 3;
   static constexpr int kRingBytes = k8Warps * kStages * k8StageBytes;
   static constexpr int kSmemBytes = kRingBytes + k8Warps * kStages * k8MetaBytes;
   static_assert((k8Warps + 1) * (kWide ? 16 : 8) * kHeadDim * 4 <= (k8Warps - 1) * kStages * k8StageBytes,
                 "the rings of all but the last warp take the partials");
 };
-constexpr int k8MaxCtasPerSm = 4;
+constexpr int k8MaxCtasPerSm = 3;
 
 struct ByteKvAttnParams {
   const __nv_bfloat16* q;   // [B][Hq][128]
@@ -206,6 +206,7 @@ struct ByteKvAttnParams {
   int idx_stride;
   int batch, num_q_heads, group_size;
   int splits;               // kList
+  int even;                 // dense: even parts of every unit instead of equal runs (see below)
   float* partials;          // kList: [B][Hq][splits][kPartStride]; dense: [CTA][2][group][kPartStride]
   unsigned int* tickets;    // [B][Hq], zero on entry and on exit
   __nv_bfloat16* out;
@@ -279,40 +280,45 @@ __device__ __forceinline__ float load_query_f16(const __nv_bfloat16* q, bool has
   return __uint_as_float((uint32_t)e << 23) * (kScale * kLog2e);
 }
 
-// Work of the dense kernel.  The blocks of all (sequence, KV head) units, laid end to end, are dealt to the CTAs in
-// equal runs, whatever the lengths: a run may cover the end of one unit and the beginning of the next.  A unit
-// counts as at least one block (its open block, or nothing, still has to be written).  A CTA holds at most two
-// parts of units that it shares with its neighbours; whole units are finished on the spot.  With the even
-// splits of a grid (units x splits) a ragged batch waited for its longest sequence (32 sequences of 2K to 16K:
-// 156 us).
-constexpr int k8MinRun = 16;        // blocks per CTA at least: four stages per warp, all of them in flight at once
+// Work of the dense kernel.  Where there are many units (sequence, KV head), the blocks of all of them, laid end to
+// end, are dealt to the CTAs in equal runs whatever the lengths: a run may cover the end of one unit and the
+// beginning of the next.  A CTA holds at most two parts of units that it shares with its neighbours; whole units
+// are finished on the spot.  (With an even split of every unit a ragged batch waited for its longest sequence:
+// 32 sequences of 2K to 16K, 156 us.)  Where units are few against the CTAs (at most an eighth), every unit is cut
+// into even parts instead, one part per CTA: a CTA that crosses into a second unit pays its start and end twice
+// (8 KV heads of 2047 positions: 20 us against 12 us), and what the rounding wastes is small.
+// A unit counts as at least one block (its open block, or nothing, still has to be written).
+constexpr int k8MinRun = 16;        // blocks per CTA at least: four stages per warp
 
 __device__ __forceinline__ int unit_blocks(int t) { return max(1, t / kBlockRows); }
 
-// Warp-collective: the total of unit_blocks over the batch, and the sequence that holds item x / heads-many blocks
-// (first_b) with the number of blocks per head before it (before).  x < 0: the total only.
-__device__ __forceinline__ long long scan_lengths(const int* seq_lens, int batch, int heads, long long x, int* first_b, long long* before) {
+// Warp-collective.  Items are laid out sequence after sequence, heads * f(blocks of the sequence) each.  x < 0: their
+// number.  Else -1 and the sequence that holds item x (*b) with the number of items before it, or their number
+// where x lies past the end.
+template <typename F>
+__device__ __forceinline__ int scan_lengths(const int* seq_lens, int batch, int heads, F f, int x, int* b, int* before) {
   const int lane = threadIdx.x & 31;
-  long long sum = 0;
-  bool found = x < 0;
+  int sum = 0;
   for (int b0 = 0; b0 < batch; b0 += 32) {
-    const int w = b0 + lane < batch ? unit_blocks(__ldg(seq_lens + b0 + lane)) : 0;
+    const int w = b0 + lane < batch ? heads * f(unit_blocks(__ldg(seq_lens + b0 + lane))) : 0;
     int incl = w;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, off);
       if (lane >= off) incl += v;
     }
-    const uint32_t past = __ballot_sync(0xffffffffu, (sum + incl) * heads > x);
-    if (!found && past) {
-      const int at = __ffs(past) - 1;
-      *first_b = b0 + at;
-      *before = sum + __shfl_sync(0xffffffffu, incl - w, at);
-      found = true;
+    if (x >= 0) {
+      const uint32_t past = __ballot_sync(0xffffffffu, sum + incl > x);
+      if (past) {
+        const int at = __ffs(past) - 1;
+        *b = b0 + at;
+        *before = sum + __shfl_sync(0xffffffffu, incl - w, at);
+        return -1;
+      }
     }
     sum += __shfl_sync(0xffffffffu, incl, 31);
   }
-  return sum * heads;
+  return sum;
 }
 
 // kWide: more than eight heads per KV head (two column tiles).
@@ -346,34 +352,60 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
   const int lm_mi = lane >> 3, lm_r = lane & 7;
   const int vrow = (lm_mi & 1) * 8 + lm_r;
 
-  // this CTA's run of blocks [at, run_end), and the unit it begins in
-  int b, kvh, seg_lo = 0;
-  long long at = 0, run_end = 1, share = 1, unit_at = 0;
+  // this CTA's work
+  const bool even = !kList && p.even != 0;
+  int b, kvh, seg_lo = 0, part = 0, parts = 1;
+  int at = 0, run_end = 1, share = 1, unit_at = 0;
   if (kList) {
     b = blockIdx.z;
     kvh = blockIdx.y / p.group_size;
+    part = blockIdx.x;
+    parts = p.splits;
   } else {
-    const long long total = scan_lengths(p.kv.seq_lens, p.batch, num_kv, -1, nullptr, nullptr);
-    share = max((total + gridDim.x - 1) / gridDim.x, (long long)k8MinRun);
-    at = blockIdx.x * share;
-    run_end = min(at + share, total);
-    if (at >= total) return;
-    long long before = 0;
-    scan_lengths(p.kv.seq_lens, p.batch, num_kv, at, &b, &before);
-    const int w = unit_blocks(__ldg(p.kv.seq_lens + b));
-    kvh = (int)((at - before * num_kv) / w);
-    unit_at = before * num_kv + (long long)kvh * w;
-    seg_lo = (int)(at - unit_at);
+    const int total = scan_lengths(p.kv.seq_lens, p.batch, num_kv, [](int w) { return w; }, -1, &b, &at);
+    const int units = p.batch * num_kv, cta = blockIdx.x;
+    // runs: no shorter than k8MinRun blocks or a unit; even parts: as many as fit with every unit rounded up
+    const int ctas = even ? (int)gridDim.x - units : (int)gridDim.x;
+    share = max((total + ctas - 1) / ctas, min(k8MinRun, (total + units - 1) / units));
+    if (even) {
+      const int most = share;
+      auto count = [most](int w) { return (w + most - 1) / most; };
+      int before = 0;
+      if (scan_lengths(p.kv.seq_lens, p.batch, num_kv, count, cta, &b, &before) >= 0) return;     // more CTAs than parts
+      parts = count(unit_blocks(__ldg(p.kv.seq_lens + b)));
+      kvh = (cta - before) / parts;
+      part = (cta - before) - kvh * parts;
+    } else {
+      if ((long long)cta * share >= total) return;
+      at = cta * share;
+      run_end = min(at + share, total);
+      int before = 0;
+      scan_lengths(p.kv.seq_lens, p.batch, num_kv, [](int w) { return w; }, at, &b, &before);
+      const int w = unit_blocks(__ldg(p.kv.seq_lens + b));
+      kvh = (at - before) / w;
+      unit_at = before + kvh * w;
+      seg_lo = at - unit_at;
+    }
   }
-  const long long run_at = at;
 
-  while (true) {                               // units of the run (kList: one pass)
+  while (true) {                               // units of the run (one pass where the CTA has one part)
     const int unit0 = kList ? b * p.num_q_heads + (int)blockIdx.y : b * p.num_q_heads + kvh * gq;
     const int t = __ldg(p.kv.seq_lens + b);
     const int whole = t & ~(kBlockRows - 1);   // positions below are in the 8-bit cache, the rest in the tail
     const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
     const int w = unit_blocks(t);              // dense
-    const int seg_hi = kList ? 0 : (int)min((long long)w, run_end - unit_at);
+    int first_cta = 0, seg_hi = w;
+    if (!kList && even) {
+      const int per = (w + parts - 1) / parts;             // parts * per >= w > (parts - 1) * per where parts = ceil(w / share)
+      seg_lo = min(part * per, w);
+      seg_hi = min(seg_lo + per, w);
+      first_cta = (int)blockIdx.x - part;
+    } else if (!kList) {
+      seg_hi = min(w, run_end - unit_at);
+      first_cta = unit_at / share;
+      part = (int)blockIdx.x - first_cta;
+      parts = (unit_at + w - 1) / share - first_cta + 1;
+    }
 
     // list entries (kList) or blocks (dense) of this warp
     const int cnt = kList ? min(max(__ldg(p.count + unit0), 0), p.idx_stride) : min(seg_hi, whole / kBlockRows);
@@ -385,10 +417,10 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
       end = min(start + per, cnt);
       nstages = (end - start + kBlockRows - 1) / kBlockRows;
     } else {
-      const int per = (cnt - seg_lo + k8Warps - 1) / k8Warps;
+      const int per = (max(cnt - seg_lo, 0) + k8Warps - 1) / k8Warps;
       start = min(seg_lo + warp * per, cnt);
       end = min(start + per, cnt);
-      nstages = end - start;
+      nstages = max(end - start, 0);
     }
 
     // ---- the open block: belongs to the end of the unit (dense) or wherever the list names it
@@ -701,15 +733,14 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
       store_partial_bf16<kTiles>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps], sm_lt[k8Warps]);
     }
     __syncthreads();
-    // the parts this unit is in
-    const int first_cta = kList ? 0 : (int)(unit_at / share), last_cta = kList ? p.splits - 1 : (int)((unit_at + w - 1) / share);
-    auto part_row = [&](int head, int part) -> float* {
-      if (kList) return p.partials + ((long long)(unit0 + head) * p.splits + part) * kPartStride;
-      return p.partials + ((long long)(2 * (first_cta + part) + (part == 0 ? 1 : 0)) * gq + head) * kPartStride;
+    // a part's place: by unit and split (lists), else two per CTA, the one it begins in the middle of and the other
+    auto part_row = [&](int head, int i) -> float* {
+      if (kList) return p.partials + ((long long)(unit0 + head) * p.splits + i) * kPartStride;
+      return p.partials + ((long long)(2 * (first_cta + i) + (i == 0 ? 1 : 0)) * gq + head) * kPartStride;
     };
-    finish_unit(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, last_cta - first_cta + 1,
-                (int)blockIdx.x - first_cta, part_row, p.tickets, p.out, p.out_lse, unit0, &is_last);
-    if (kList) return;
+    finish_unit(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
+                p.out, p.out_lse, unit0, &is_last);
+    if (kList || even) return;
     unit_at += w;
     if (unit_at >= run_end) return;
     seg_lo = 0;

@@ -85,9 +85,14 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
   p.flags = c->flags;
-  // dense: one CTA per resident slot at most, each with a run of at least k8MinRun blocks
-  const long long blocks = (long long)batch * c->cfg.num_kv_heads * std::max(1, (max_count + kBlockRows - 1) / kBlockRows);
-  const int ctas = (int)std::min<long long>((c->gq > 8 ? Shape8<true>::kCtasPerSm : Shape8<false>::kCtasPerSm) * c->sm_count, (blocks + k8MinRun - 1) / k8MinRun);
+  // dense: one CTA per resident slot, fewer where the runs (at least k8MinRun blocks or a unit each) would not fill them
+  const long long units = (long long)batch * c->cfg.num_kv_heads;
+  const long long unit_max = std::max(1, (max_count + kBlockRows - 1) / kBlockRows);
+  if (!idx && units * unit_max >= (1ll << 30))
+    return fail(c, PRHS_ERR_UNSUPPORTED, "batch * heads * max_seq_len above 2^34: pass a smaller max_seq_len");
+  const int slots = (c->gq > 8 ? Shape8<true>::kCtasPerSm : Shape8<false>::kCtasPerSm) * c->sm_count;
+  p.even = 8 * units <= slots ? 1 : 0;
+  const int ctas = (int)std::min<long long>(slots, units * ((unit_max + k8MinRun - 1) / k8MinRun) + (p.even ? units : 0));
   const dim3 grid = idx ? dim3(p.splits, c->cfg.num_q_heads, batch) : dim3(ctas, 1, 1);
   {
     LaunchScope ls(c, idx ? PRHS_KIND_ATTN_SPARSE : PRHS_KIND_ATTN_DENSE, st);

@@ -149,77 +149,60 @@ __device__ __forceinline__ void store_partial_bf16(const float (&o)[kTiles][8][4
     }
 }
 
-// Merge of a unit's partials by the last CTA to arrive: a warp per head, a float4 of the 128 columns per lane, the
-// splits' weights one per lane.  row(head, split) is the address of a partial: o[128], m, l, l~.  The loads of
-// all splits are independent of one another (a merge that walked them one by one cost 20 us at 32 splits of
-// four heads).
-template <typename Row>
-__device__ __forceinline__ void merge_partials(Row row, int splits, int heads, __nv_bfloat16* out, float* out_lse, int unit0) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  for (int h = warp; h < heads; h += warps) {
-    float M = -INFINITY;
-    for (int sp = lane; sp < splits; sp += 32) M = fmaxf(M, __ldcg(row(h, sp) + kHeadDim));
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f, Lt = 0.f;
-    if (M != -INFINITY) {
-      for (int s0 = 0; s0 < splits; s0 += 32) {
-        float f = 0.f;
-        if (s0 + lane < splits) {
-          const float* r = row(h, s0 + lane);
-          f = exp2f(__ldcg(r + kHeadDim) - M);
-          L = fmaf(__ldcg(r + kHeadDim + 1), f, L);
-          Lt = fmaf(__ldcg(r + kHeadDim + 2), f, Lt);
-        }
-        const int n = min(32, splits - s0);
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) {
-          const float4 x = __ldcg(reinterpret_cast<const float4*>(row(h, s0 + i)) + lane);
-          const float fi = __shfl_sync(0xffffffffu, f, i);
-          acc.x = fmaf(x.x, fi, acc.x); acc.y = fmaf(x.y, fi, acc.y); acc.z = fmaf(x.z, fi, acc.z); acc.w = fmaf(x.w, fi, acc.w);
-        }
-      }
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      L += __shfl_xor_sync(0xffffffffu, L, off);
-      Lt += __shfl_xor_sync(0xffffffffu, Lt, off);
-    }
-    const float inv = Lt > 0.f ? 1.f / Lt : 0.f;
-    const uint2 y = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-    *reinterpret_cast<uint2*>(out + (long long)(unit0 + h) * kHeadDim + lane * 4) = y;
-    if (lane == 0 && out_lse) out_lse[unit0 + h] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+// Running combination of partials (m, l, l~ and four of the 128 columns per lane).
+struct Merged {
+  float m = -INFINITY, l = 0.f, lt = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void rescale(float mn) {
+    const float f = mn > -INFINITY ? exp2f(m - mn) : 0.f;
+    l *= f; lt *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+    m = mn;
   }
-}
-
-// End of a unit's work in a CTA of 128 threads: the warps' partials in shared memory (o [slot][head][128], m, l, l~
-// [slot][16]) become the result (one part) or this CTA's part in global memory; the CTA whose part arrives
-// last merges them (a ticket, no waiting).
-template <typename Row>
-__device__ __forceinline__ void finish_unit(const float* sm_o, const float* sm_m, const float* sm_l, const float* sm_lt, int slots,
-                                            int heads, int parts, int part, Row row, unsigned int* tickets, __nv_bfloat16* out,
-                                            float* out_lse, int unit0, bool* is_last) {
-  const int tid = threadIdx.x;
-  for (int j = 0; j < heads; ++j) {
-    float M = -INFINITY;
-    for (int s = 0; s < slots; ++s) M = fmaxf(M, sm_m[s * 16 + j]);
-    float acc = 0.f, L = 0.f, Lt = 0.f;
-    if (M != -INFINITY) {
-      for (int s = 0; s < slots; ++s) {
-        const float f = exp2f(sm_m[s * 16 + j] - M);
-        if (f > 0.f) acc = fmaf(sm_o[(s * heads + j) * kHeadDim + tid], f, acc);
-        L = fmaf(sm_l[s * 16 + j], f, L);
-        Lt = fmaf(sm_lt[s * 16 + j], f, Lt);
-      }
+  __device__ __forceinline__ void add(float m2, float l2, float lt2, float4 x) {      // m2 <= m
+    const float f = m2 > -INFINITY ? exp2f(m2 - m) : 0.f;
+    if (f > 0.f) {
+      l = fmaf(l2, f, l); lt = fmaf(lt2, f, lt);
+      o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
     }
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* out, float* out_lse, long long unit) const {
+    const int lane = threadIdx.x & 31;
+    const float inv = lt > 0.f ? 1.f / lt : 0.f;
+    *reinterpret_cast<uint2*>(out + unit * kHeadDim + lane * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (lane == 0 && out_lse) out_lse[unit] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
+};
+
+// End of a unit's work in a CTA of four warps: the warps' partials in shared memory (o [slot][head][128], m, l, l~
+// [slot][16]; at most five slots) become the result (one part) or this CTA's part in global memory, row(head, part)
+// = o[128], m, l, l~; the CTA whose part arrives last merges them (a ticket, no waiting).  A warp per head, or
+// several warps per head where there are fewer than four; a lane has four columns, and the loads of sixteen parts
+// are in flight at once.  (Heads one after the other, a column per thread, cost 5000 cycles for four heads in the
+// first half and 20 us for a merge of 32 parts.)
+template <typename Row>
+__device__ __forceinline__ void finish_unit(float* sm_o, float* sm_m, float* sm_l, float* sm_lt, int slots, int heads, int parts, int part,
+                                            Row row, unsigned int* tickets, __nv_bfloat16* out, float* out_lse, int unit0, bool* is_last) {
+  constexpr int kWarps = 4, kMaxSlots = 5, kBatch = 16;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  for (int h = warp; h < heads; h += kWarps) {
+    Merged r;
+    float m[kMaxSlots];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < kMaxSlots; ++s) {
+      m[s] = s < slots ? sm_m[s * 16 + h] : -INFINITY;
+      mx = fmaxf(mx, m[s]);
+    }
+    r.m = mx;
+#pragma unroll
+    for (int s = 0; s < kMaxSlots; ++s)
+      if (m[s] > -INFINITY) r.add(m[s], sm_l[s * 16 + h], sm_lt[s * 16 + h], reinterpret_cast<const float4*>(sm_o + (s * heads + h) * kHeadDim)[lane]);
     if (parts == 1) {
-      out[(long long)(unit0 + j) * kHeadDim + tid] = __float2bfloat16_rn(Lt > 0.f ? acc / Lt : 0.f);
-      if (tid == 0 && out_lse) out_lse[unit0 + j] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+      r.store(out, out_lse, unit0 + h);
     } else {
-      float* r = row(j, part);
-      r[tid] = acc;
-      if (tid == 0) { r[kHeadDim] = M; r[kHeadDim + 1] = L; r[kHeadDim + 2] = Lt; }
+      float4* dst = reinterpret_cast<float4*>(row(h, part));
+      __stcg(dst + lane, r.o);
+      if (lane == 0) __stcg(dst + 32, make_float4(r.m, r.l, r.lt, 0.f));
     }
   }
   if (parts == 1) return;
@@ -231,9 +214,59 @@ __device__ __forceinline__ void finish_unit(const float* sm_o, const float* sm_m
     if (*is_last) tickets[unit0] = 0u;
   }
   __syncthreads();
-  if (*is_last) {
-    __threadfence();
-    merge_partials(row, parts, heads, out, out_lse, unit0);
+  if (!*is_last) return;
+  __threadfence();
+  const int slices = heads >= kWarps ? 1 : kWarps / heads;            // warps per head
+  for (int h = slices == 1 ? warp : warp / slices; h < heads; h += kWarps / slices) {
+    const int slice = slices == 1 ? 0 : warp % slices;
+    Merged r;
+    for (int p0 = slice; p0 < parts; p0 += slices * kBatch) {
+      // m, l, l~ of sixteen parts, one per lane; their columns
+      const int mine = p0 + lane * slices;
+      float4 st = make_float4(-INFINITY, 0.f, 0.f, 0.f), x[kBatch];
+      if (lane < kBatch && mine < parts) st = __ldcg(reinterpret_cast<const float4*>(row(h, mine)) + 32);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p0 + i * slices < parts) x[i] = __ldcg(reinterpret_cast<const float4*>(row(h, p0 + i * slices)) + lane);
+      }
+      float mn = st.x;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
+      r.rescale(fmaxf(mn, r.m));
+      const float f = st.x > -INFINITY ? exp2f(st.x - r.m) : 0.f;
+      r.l = fmaf(st.y, f, r.l);                // per lane until the end
+      r.lt = fmaf(st.z, f, r.lt);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float fi = __shfl_sync(0xffffffffu, f, i);
+        if (fi > 0.f) {
+          r.o.x = fmaf(x[i].x, fi, r.o.x); r.o.y = fmaf(x[i].y, fi, r.o.y);
+          r.o.z = fmaf(x[i].z, fi, r.o.z); r.o.w = fmaf(x[i].w, fi, r.o.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      r.l += __shfl_xor_sync(0xffffffffu, r.l, off);
+      r.lt += __shfl_xor_sync(0xffffffffu, r.lt, off);
+    }
+    if (slices == 1) {
+      r.store(out, out_lse, unit0 + h);
+    } else {
+      reinterpret_cast<float4*>(sm_o + warp * kHeadDim)[lane] = r.o;
+      if (lane == 0) { sm_m[warp] = r.m; sm_l[warp] = r.l; sm_lt[warp] = r.lt; }
+    }
+  }
+  if (slices == 1) return;
+  __syncthreads();
+  if (warp < heads) {
+    Merged r;
+    for (int s = 0; s < slices; ++s) r.m = fmaxf(r.m, sm_m[warp * slices + s]);
+    for (int s = 0; s < slices; ++s)
+      r.add(sm_m[warp * slices + s], sm_l[warp * slices + s], sm_lt[warp * slices + s],
+            reinterpret_cast<const float4*>(sm_o + (warp * slices + s) * kHeadDim)[lane]);
+    r.store(out, out_lse, unit0 + warp);
   }
 }
 
