@@ -6,6 +6,18 @@ namespace {
 
 constexpr int kMaxBlocks = kMaxContext / kBlockRows;
 
+cudaError_t block_set_attributes() {
+  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true>, kTSmemBytes},
+                                                           {(const void*)block_score_kernel<false>, kScoreSmemBytes},
+                                                           {(const void*)block_score_kernel<true>, kScoreSmemBytes}};
+  for (const auto& k : all) {
+    const cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 prhs_status check_bounds(prhs_ctx* ctx, const prhs_block_bounds_view* bv, BoundsDev* out) {
   if (!bv || !bv->codes || !bv->scale) return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: NULL pointer");
   if ((uintptr_t)bv->codes % 16 || (uintptr_t)bv->scale % 4)
@@ -77,17 +89,15 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   sp.update_last = update_last ? 1 : 0;
   sp.max_len = max_t;
   sp.flags = c->flags;
-  // about four waves of CTAs (four resident per SM), one to eight rounds per warp
+  // about one wave of CTAs, none with less than one round of its four warps
   const int blocks = (max_t + kBlockRows - 1) / kBlockRows;
-  const int step = kScoreWarps * kScoreRound;
-  const long long chunks = (long long)batch * c->cfg.num_kv_heads * ((blocks + step - 1) / step);
-  sp.rounds = (int)std::min<long long>(8, std::max<long long>(1, chunks / (16ll * c->sm_count)));
-  const int per_cta = step * sp.rounds;
+  const int units = batch * c->cfg.num_kv_heads, step = kScoreWarps * kScoreRound;
+  const int chunks = std::max(1, std::min(kScoreCtasPerSm * c->sm_count / units, (blocks + step - 1) / step));
   {
     LaunchScope ls(c, PRHS_KIND_SCORE, st);
-    const dim3 grid((blocks + per_cta - 1) / per_cta, c->cfg.num_kv_heads, batch);
-    if (c->gq > 8) block_score_kernel<true><<<grid, kScoreWarps * 32, 0, st>>>(sp);
-    else block_score_kernel<false><<<grid, kScoreWarps * 32, 0, st>>>(sp);
+    const dim3 grid(chunks, c->cfg.num_kv_heads, batch);
+    if (c->gq > 8) block_score_kernel<true><<<grid, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
+    else block_score_kernel<false><<<grid, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
   }
   PRHS_CUDA(c, cudaGetLastError());
   BlockSelectParams p;

@@ -126,7 +126,6 @@ struct BlockScoreParams {
   BoundsDev bd;
   float* scores;            // [B][Hq][ld]; group_max: the row of the group's first head
   int ld, num_q_heads, group_size, group_max;
-  int rounds;               // rounds per warp
   int update_last;          // 1: the bounds of the last block are recomputed here (its score is not used)
   int max_len;
   uint32_t* flags;
@@ -139,44 +138,6 @@ __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, ui
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The int8 codes of one head's query, negative and positive part (minima meet the one, maxima the other): this lane's
-// words are dimensions 64h + 16tg + 4w .. + 3 (h, w in 0..1, 0..3).  Returns the scale (0 for an absent head).
-__device__ __forceinline__ float code_query(const __nv_bfloat16* q, bool has, uint32_t (&neg)[2][4], uint32_t (&pos)[2][4]) {
-  const int tg = threadIdx.x & 3;
-  uint4 x[2][2];
-  uint32_t mx = 0u;
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      x[h][i] = has ? __ldg(reinterpret_cast<const uint4*>(q + 64 * h + 16 * tg + 8 * i)) : make_uint4(0u, 0u, 0u, 0u);
-      mx = __vmaxu2(__vmaxu2(mx, __vmaxu2(x[h][i].x & 0x7fff7fffu, x[h][i].y & 0x7fff7fffu)),
-                    __vmaxu2(x[h][i].z & 0x7fff7fffu, x[h][i].w & 0x7fff7fffu));
-    }
-  uint32_t amax = max(mx & 0xffffu, mx >> 16);
-  amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-  amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-  const int e = scale_exponent<6, 126>(amax);
-  const float inv = pow2i(-e);
-  auto word = [&](uint32_t a, uint32_t z, uint32_t& n, uint32_t& q4) {       // four bf16 -> their codes' two parts
-    const int c[4] = {__float2int_rn(bf_lo(a) * inv), __float2int_rn(bf_hi(a) * inv), __float2int_rn(bf_lo(z) * inv), __float2int_rn(bf_hi(z) * inv)};
-    n = q4 = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      n |= ((uint32_t)min(c[i], 0) & 0xffu) << (8 * i);
-      q4 |= (uint32_t)max(c[i], 0) << (8 * i);
-    }
-  };
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      word(x[h][i].x, x[h][i].y, neg[h][2 * i], pos[h][2 * i]);
-      word(x[h][i].z, x[h][i].w, neg[h][2 * i + 1], pos[h][2 * i + 1]);
-    }
-  return has ? pow2i(e) : 0.f;
-}
-
 // Programmatic dependent launch: a kernel of a step is launched while the one before it still runs, does what
 // does not depend on it, and waits here.  Every CTA waits, those without work too, so that a kernel that has
 // ended means that all before it have.
@@ -184,86 +145,132 @@ __device__ __forceinline__ void step_wait() { asm volatile("griddepcontrol.wait;
 __device__ __forceinline__ void step_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // grid (chunks, Hkv, B).  A warp takes eight blocks at a time as the columns of mma.sync m16n8k32 (int8 in, int32
-// accumulate) with the group's heads on the rows.  The B fragments come straight from global memory: lane
-// (g, tg) loads the four 16-byte pieces 4i + tg of block g's 256 bytes (64 contiguous bytes per block and
-// instruction) and deals their words to the k-slots as they lie; the query's fragments are dealt the same way.
-// No shared memory, eight MMAs per 2 KB.  Sixteen blocks (4 KB) per warp and round, the next round's loads in
-// flight under this one's arithmetic, page ids a round further ahead.  Bound by the stream of bounds.
+// accumulate) with the group's heads on the rows (kWide: more than eight).  The bounds come through a
+// warp-private cp.async ring of 16 blocks (4 KB) per stage; lane (g, tg) reads the four 16-byte pieces 4i + tg of
+// block g's 256 bytes and deals their words to the k-slots as they lie, and the query's fragments are dealt the
+// same way: sixteen MMAs and eight shared-memory loads per 4 KB.  The query is coded once per CTA.  A CTA
+// takes an equal share of its sequence's blocks, and the grid is about one wave, so that the ring is set up once
+// (register prefetch with a dozen short CTAs per unit: 35 us for 137 MB).  Bound by the stream of bounds.
 constexpr int kScoreWarps = 4;
-constexpr int kScoreTiles = 2;                                   // tiles of eight blocks per round
-constexpr int kScoreRound = kScoreTiles * 8;
+constexpr int kScoreRound = 16;                                  // blocks per stage
+constexpr int kScoreStages = 4;
+constexpr int kScoreStageBytes = kScoreRound * kBoundsBytes + kScoreRound * 4;
+constexpr int kScoreSmemBytes = kScoreWarps * kScoreStages * kScoreStageBytes;      // 65 KB: three CTAs per SM
+constexpr int kScoreCtasPerSm = 3;
 template <bool kWide>
-__global__ void __launch_bounds__(kScoreWarps * 32, 4) block_score_kernel(BlockScoreParams p) {
+__global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score_kernel(BlockScoreParams p) {
+  constexpr int kHeads = kWide ? 16 : 8;
+  extern __shared__ __align__(128) unsigned char g_smem[];
+  __shared__ __align__(16) uint8_t qcodes[kHeads][2][kHeadDim];   // negative part (meets the minima), positive part
+  __shared__ float qscale[kHeads];
   step_release();
   const int kvh = blockIdx.y, b = blockIdx.z;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, tg = lane & 3;
   const int gq = p.group_size, head0 = kvh * gq;
   const int t = __ldg(p.kv.seq_lens + b);
   if (t > p.max_len || t < 0) {
-    if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(p.flags, kFlagBadLength);
+    if (tid == 0 && blockIdx.x == 0) atomicOr(p.flags, kFlagBadLength);
     return;
   }
   const int nb = (t + kBlockRows - 1) / kBlockRows;
-  if (p.update_last && blockIdx.x == 0 && warp == kScoreWarps - 1 && nb > 0) {
-    long long row, bi;
-    if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
-      bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
-    else if (lane == 0)
-      atomicOr(p.flags, kFlagBadPage);
-  }
-  // rounds of this warp: blocks [first + r * step, + kScoreRound), r < rounds
-  const int step = kScoreWarps * kScoreRound;
-  const int first = blockIdx.x * p.rounds * step + warp * kScoreRound;
-  if (first >= nb) return;
-  const int rounds = min(p.rounds, (nb - first + step - 1) / step);
-  auto locate = [&](int r) -> long long {              // bounds index of this lane's block (lanes 0..15)
-    const int blk = first + r * step + (lane & 15);
-    long long row, bi = -1;
-    if (r < rounds && blk < nb && !locate_block(p.kv, p.bd, b, kvh, blk, row, bi)) {
-      atomicOr(p.flags, kFlagBadPage);
-      bi = -1;
-    }
-    return bi;
-  };
-  auto fetch = [&](long long bi, uint4 (&x)[kScoreTiles][4], float& scale) {
-    scale = bi >= 0 ? __ldcg(p.bd.scale + bi) : 0.f;
-#pragma unroll
-    for (int n = 0; n < kScoreTiles; ++n) {
-      const long long at = __shfl_sync(0xffffffffu, bi, 8 * n + g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[n][i] = at >= 0 ? __ldcg(reinterpret_cast<const uint4*>(p.bd.codes + at * kBoundsBytes + (4 * i + tg) * 16)) : make_uint4(0u, 0u, 0u, 0u);
-    }
-  };
-  uint4 cur[kScoreTiles][4], next[kScoreTiles][4];
-  float s_cur, s_next = 0.f;
-  fetch(locate(0), cur, s_cur);
-  long long bi_next = locate(1);
+  const int groups = (nb + kScoreRound - 1) / kScoreRound, per = (groups + (int)gridDim.x - 1) / (int)gridDim.x;
+  const int g_lo = blockIdx.x * per, g_hi = min(g_lo + per, groups);
+  const bool updates = p.update_last && nb > 0 && blockIdx.x == gridDim.x - 1;
+  if (g_lo >= g_hi && !updates) return;
+  const int rounds = max(0, (g_hi - g_lo - warp + kScoreWarps - 1) / kScoreWarps);     // groups g_lo + warp + 4r
 
-  const __nv_bfloat16* q0 = p.q + ((long long)b * p.num_q_heads + head0 + g) * kHeadDim;
-  const bool has0 = g < gq, has1 = kWide && g + 8 < gq;
-  uint32_t n0[2][4], p0[2][4], n1[2][4], p1[2][4];      // heads g and g + 8
-  const float qs0 = code_query(q0, has0, n0, p0);
-  float qs1 = 0.f;
-  if (kWide) qs1 = code_query(q0 + 8 * kHeadDim, has1, n1, p1);
-  for (int r = 0; r < rounds; ++r) {
-    fetch(bi_next, next, s_next);
-    bi_next = locate(r + 2);
+  const bool paged = p.kv.page_table != nullptr;
+  const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kScoreStages * kScoreStageBytes);
+  auto page_of = [&](int r) -> int {                   // lanes 0..15: the page of block lane of round r
+    const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + (lane & 15);
+    return (paged && r < rounds && blk < nb) ? __ldg(ptab + blk) : 0;
+  };
+  int pg_next = page_of(0);
+  auto issue = [&](int r) {
+    if (r < rounds) {
+      const int blk0 = (g_lo + warp + kScoreWarps * r) * kScoreRound;
+      int at = -1;                                     // bounds index of block lane & 15
+      if (blk0 + (lane & 15) < nb) {
+        if (!paged) {
+          at = (int)(b * p.bd.stride_outer + kvh * p.bd.stride_head) + blk0 + (lane & 15);
+        } else if ((unsigned)pg_next < (unsigned)p.kv.num_pages) {
+          at = (int)(pg_next * p.bd.stride_outer + kvh * p.bd.stride_head);
+        } else {
+          atomicOr(p.flags, kFlagBadPage);
+        }
+      }
+      pg_next = page_of(r + 1);
+      const uint32_t slot = ring + (uint32_t)(r % kScoreStages) * kScoreStageBytes;
+      const int c = lane & 15;
 #pragma unroll
-    for (int n = 0; n < kScoreTiles; ++n) {
-      const int blk = first + r * step + 8 * n + 2 * tg;
+      for (int i = 0; i < 8; ++i) {
+        const int row = 2 * i + (lane >> 4);
+        const int from = __shfl_sync(0xffffffffu, at, row);
+        cp_async_16(slot + row * kBoundsBytes + ((c ^ ((row & 1) << 2)) << 4), p.bd.codes + (long long)max(from, 0) * kBoundsBytes + c * 16,
+                    from >= 0 ? 16 : 0);
+      }
+      if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + max(at, 0), at >= 0 ? 4 : 0);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int r = 0; r < kScoreStages - 1; ++r) issue(r);
+
+  // ---- the group's query codes: sixteen threads per head, eight dimensions each
+#pragma unroll
+  for (int h0 = 0; h0 < kHeads; h0 += 8) {
+    const int h = h0 + (tid >> 4), d = (tid & 15) * 8;
+    const uint4 x = h < gq ? __ldg(reinterpret_cast<const uint4*>(p.q + ((long long)b * p.num_q_heads + head0 + h) * kHeadDim + d))
+                           : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t mx = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+    uint32_t amax = max(mx & 0xffffu, mx >> 16);
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+    const int e = scale_exponent<6, 126>(amax);
+    const float inv = pow2i(-e);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t neg[2] = {0u, 0u}, pos[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int code = __float2int_rn((j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1])) * inv);
+      neg[j >> 2] |= ((uint32_t)min(code, 0) & 0xffu) << (8 * (j & 3));
+      pos[j >> 2] |= (uint32_t)max(code, 0) << (8 * (j & 3));
+    }
+    *reinterpret_cast<uint2*>(&qcodes[h][0][d]) = make_uint2(neg[0], neg[1]);
+    *reinterpret_cast<uint2*>(&qcodes[h][1][d]) = make_uint2(pos[0], pos[1]);
+    if ((tid & 15) == 0) qscale[h] = h < gq ? pow2i(e) : 0.f;
+  }
+  __syncthreads();
+  const bool has0 = g < gq, has1 = kWide && g + 8 < gq;
+  uint4 q0[4], q1[4];                                  // heads g and g + 8: pieces 4i + tg
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    q0[i] = *reinterpret_cast<const uint4*>(&qcodes[g][i >> 1][64 * (i & 1) + 16 * tg]);
+    q1[i] = kWide ? *reinterpret_cast<const uint4*>(&qcodes[(g + 8) & (kHeads - 1)][i >> 1][64 * (i & 1) + 16 * tg]) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  const float qs0 = qscale[g], qs1 = kWide ? qscale[(g + 8) & (kHeads - 1)] : 0.f;
+  float* const row0 = p.scores + ((long long)b * p.num_q_heads + head0 + (p.group_max ? 0 : g)) * p.ld;
+
+  for (int r = 0; r < rounds; ++r) {
+    cp_async_wait<kScoreStages - 2>();
+    __syncwarp();
+    issue(r + kScoreStages - 1);
+    const unsigned char* slot = g_smem + (warp * kScoreStages + r % kScoreStages) * kScoreStageBytes;
+    const float* scales = reinterpret_cast<const float*>(slot + kScoreRound * kBoundsBytes);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
       int d[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int h = i & 1;                     // pieces 0, 1: minima of dimensions 64h..; 2, 3: maxima
-        auto w0 = [&](int k) { return i < 2 ? n0[h][k] : p0[h][k]; };
-        auto w1 = [&](int k) { return !kWide ? 0u : i < 2 ? n1[h][k] : p1[h][k]; };
-        mma_s8(d, w0(0), w1(0), w0(1), w1(1), cur[n][i].x, cur[n][i].y);
-        mma_s8(d, w0(2), w1(2), w0(3), w1(3), cur[n][i].z, cur[n][i].w);
+        const uint4 x = *reinterpret_cast<const uint4*>(slot + (8 * n + g) * kBoundsBytes + (((4 * i + tg) ^ ((g & 1) << 2)) << 4));
+        mma_s8(d, q0[i].x, q1[i].x, q0[i].y, q1[i].y, x.x, x.y);
+        mma_s8(d, q0[i].z, q1[i].z, q0[i].w, q1[i].w, x.z, x.w);
       }
-      const float s0 = __shfl_sync(0xffffffffu, s_cur, 8 * n + 2 * tg), s1 = __shfl_sync(0xffffffffu, s_cur, 8 * n + 2 * tg + 1);
-      float v[4] = {(float)d[0] * s0 * qs0, (float)d[1] * s1 * qs0, (float)d[2] * s0 * qs1, (float)d[3] * s1 * qs1};
+      const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + 8 * n + 2 * tg;
+      const float2 s = *reinterpret_cast<const float2*>(scales + 8 * n + 2 * tg);
+      float v[4] = {(float)d[0] * s.x * qs0, (float)d[1] * s.y * qs0, (float)d[2] * s.x * qs1, (float)d[3] * s.y * qs1};
       if (p.group_max) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -273,19 +280,21 @@ __global__ void __launch_bounds__(kScoreWarps * 32, 4) block_score_kernel(BlockS
           v[c] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
         }
       }
-      auto store = [&](int head, float a, float z) {
-        float* dst = p.scores + ((long long)b * p.num_q_heads + head0 + head) * p.ld + blk;
-        if (blk + 1 < nb) *reinterpret_cast<float2*>(dst) = make_float2(a, z);
-        else if (blk < nb) *dst = a;
+      auto store = [&](float* row, float a, float z) {
+        if (blk + 1 < nb) *reinterpret_cast<float2*>(row + blk) = make_float2(a, z);
+        else if (blk < nb) row[blk] = a;
       };
-      if (p.group_max ? g == 0 : has0) store(g, v[0], v[1]);
-      if (!p.group_max && has1) store(g + 8, v[2], v[3]);
+      if (p.group_max ? g == 0 : has0) store(row0, v[0], v[1]);
+      if (kWide && !p.group_max && has1) store(row0 + 8ll * p.ld, v[2], v[3]);
     }
-#pragma unroll
-    for (int n = 0; n < kScoreTiles; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) cur[n][i] = next[n][i];
-    s_cur = s_next;
+  }
+  cp_async_wait<0>();
+  if (updates && warp == kScoreWarps - 1) {            // the bounds of the last block (its score is not used)
+    long long row, bi;
+    if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
+      bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
+    else if (lane == 0)
+      atomicOr(p.flags, kFlagBadPage);
   }
 }
 
@@ -438,11 +447,8 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
   __syncthreads();                                     // warp_a is read above
   if (lane == 0) { warp_a[warp] = gt; warp_b[warp] = eq; }
   __syncthreads();
-  int eq_before = 0, place = lo;
-  for (int w = 0; w < warp; ++w) {
-    place += warp_a[w] + max(0, min(warp_b[w], need - eq_before));
-    eq_before += warp_b[w];
-  }
+  int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_b[lane & (kBSWarps - 1)] : 0);
+  int place = lo + __reduce_add_sync(0xffffffffu, lane < warp ? warp_a[lane & (kBSWarps - 1)] : 0) + min(eq_before, need);
   each([&](int r, bool in, uint32_t k) {
     const uint32_t below = (1u << lane) - 1u;
     const uint32_t eqm = __ballot_sync(0xffffffffu, in && k == thr);
