@@ -83,21 +83,22 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   sp.bd = bd;
   sp.scores = c->scores;
   sp.ld = c->ld;
+  sp.batch = batch;
   sp.num_q_heads = c->cfg.num_q_heads;
   sp.group_size = c->gq;
   sp.group_max = shared ? 1 : 0;
   sp.update_last = update_last ? 1 : 0;
   sp.max_len = max_t;
   sp.flags = c->flags;
-  // about one wave of CTAs, none with less than one round of its four warps
+  // one wave of CTAs, none with less than one round of its four warps
   const int blocks = (max_t + kBlockRows - 1) / kBlockRows;
-  const int units = batch * c->cfg.num_kv_heads, step = kScoreWarps * kScoreRound;
-  const int chunks = std::max(1, std::min(kScoreCtasPerSm * c->sm_count / units, (blocks + step - 1) / step));
+  const long long groups = (long long)batch * c->cfg.num_kv_heads * ((blocks + kScoreRound - 1) / kScoreRound);
+  if (groups >= (1ll << 30)) return fail(c, PRHS_ERR_UNSUPPORTED, "batch * heads * max_seq_len above 2^38: pass a smaller max_seq_len");
+  const int ctas = (int)std::min<long long>(kScoreCtasPerSm * c->sm_count, (groups + kScoreWarps - 1) / kScoreWarps);
   {
     LaunchScope ls(c, PRHS_KIND_SCORE, st);
-    const dim3 grid(chunks, c->cfg.num_kv_heads, batch);
-    if (c->gq > 8) block_score_kernel<true><<<grid, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
-    else block_score_kernel<false><<<grid, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
+    if (c->gq > 8) block_score_kernel<true><<<ctas, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
+    else block_score_kernel<false><<<ctas, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
   }
   PRHS_CUDA(c, cudaGetLastError());
   BlockSelectParams p;
@@ -128,6 +129,26 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   return PRHS_OK;
 }
 
+// Splits of a list of blocks, in cycles as measured: a warp works one block off in about 900 when CTAs are few and waits
+// for its share of the HBM stream (2760 when every slot is taken) when they are many; a CTA's start and end
+// cost about 3000, a merge of parts 4500 (one user, 19 blocks per head: 10.9 us a step with one split, 12.9 with
+// two; 8 x 32 heads of 73 blocks: 60 us with one, 72 with two).
+int block_splits(const prhs_ctx* c, int units, int blocks) {
+  const int slots = 2 * c->sm_count;
+  int best = 1;
+  double best_cost = 1e30;
+  for (int s = 1; s <= kMaxSplits; ++s) {
+    const int per_warp = (blocks + s * kTWarps - 1) / (s * kTWarps);
+    const long long ctas = (long long)units * s;
+    const double waves = (double)((ctas + slots - 1) / slots);
+    const double stage = std::max(900.0, 2760.0 * std::min<long long>(ctas, slots) / slots);
+    const double cost = waves * (3000.0 + per_warp * stage) + (s > 1 ? 4500.0 : 0.0);
+    if (cost < best_cost * 0.999) { best_cost = cost; best = s; }
+    if (per_warp == 1) break;
+  }
+  return best;
+}
+
 prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
                               uint32_t flags, int batch, void* out, float* out_lse, bool after_select, cudaStream_t st) {
   const bool shared = block_shared(c, flags);
@@ -141,7 +162,7 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.units_per_seq = c->cfg.num_q_heads / p.heads_per_unit;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  p.splits = pick_splits(c, batch * p.units_per_seq, stride * kBlockRows);
+  p.splits = block_splits(c, batch * p.units_per_seq, stride);
   p.partials = c->partials;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);

@@ -14,6 +14,7 @@
 #include "attn.cuh"
 #include "common.cuh"
 #include "bytekv.cuh"
+#include "head_tiles.cuh"
 
 namespace prhs {
 
@@ -125,7 +126,7 @@ struct BlockScoreParams {
   KvDev kv;
   BoundsDev bd;
   float* scores;            // [B][Hq][ld]; group_max: the row of the group's first head
-  int ld, num_q_heads, group_size, group_max;
+  int ld, batch, num_q_heads, group_size, group_max;
   int update_last;          // 1: the bounds of the last block are recomputed here (its score is not used)
   int max_len;
   uint32_t* flags;
@@ -144,13 +145,15 @@ __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, ui
 __device__ __forceinline__ void step_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void step_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// grid (chunks, Hkv, B).  A warp takes eight blocks at a time as the columns of mma.sync m16n8k32 (int8 in, int32
+// A warp takes eight blocks at a time as the columns of mma.sync m16n8k32 (int8 in, int32
 // accumulate) with the group's heads on the rows (kWide: more than eight).  The bounds come through a
 // warp-private cp.async ring of 16 blocks (4 KB) per stage; lane (g, tg) reads the four 16-byte pieces 4i + tg of
 // block g's 256 bytes and deals their words to the k-slots as they lie, and the query's fragments are dealt the
-// same way: sixteen MMAs and eight shared-memory loads per 4 KB.  The query is coded once per CTA.  A CTA
-// takes an equal share of its sequence's blocks, and the grid is about one wave, so that the ring is set up once
-// (register prefetch with a dozen short CTAs per unit: 35 us for 137 MB).  Bound by the stream of bounds.
+// same way: sixteen MMAs and eight shared-memory loads per 4 KB.  The groups of 16 blocks of all units, laid end to
+// end, are dealt to one wave of CTAs in equal runs (a run may cross into the next unit: then the query is coded
+// again).  One CTA column per unit instead waited for the longest of ragged sequences (16 of 8K to 64K: 27 us
+// for 75 MB); a dozen short CTAs per unit with register prefetch took 35 us for 137 MB against 27 us.  Bound by
+// the stream of bounds.
 constexpr int kScoreWarps = 4;
 constexpr int kScoreRound = 16;                                  // blocks per stage
 constexpr int kScoreStages = 4;
@@ -164,137 +167,160 @@ __global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score
   __shared__ __align__(16) uint8_t qcodes[kHeads][2][kHeadDim];   // negative part (meets the minima), positive part
   __shared__ float qscale[kHeads];
   step_release();
-  const int kvh = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, tg = lane & 3;
-  const int gq = p.group_size, head0 = kvh * gq;
-  const int t = __ldg(p.kv.seq_lens + b);
-  if (t > p.max_len || t < 0) {
-    if (tid == 0 && blockIdx.x == 0) atomicOr(p.flags, kFlagBadLength);
-    return;
-  }
-  const int nb = (t + kBlockRows - 1) / kBlockRows;
-  const int groups = (nb + kScoreRound - 1) / kScoreRound, per = (groups + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int g_lo = blockIdx.x * per, g_hi = min(g_lo + per, groups);
-  const bool updates = p.update_last && nb > 0 && blockIdx.x == gridDim.x - 1;
-  if (g_lo >= g_hi && !updates) return;
-  const int rounds = max(0, (g_hi - g_lo - warp + kScoreWarps - 1) / kScoreWarps);     // groups g_lo + warp + 4r
-
+  const int gq = p.group_size, num_kv = p.num_q_heads / gq;
   const bool paged = p.kv.page_table != nullptr;
-  const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kScoreStages * kScoreStageBytes);
-  auto page_of = [&](int r) -> int {                   // lanes 0..15: the page of block lane of round r
-    const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + (lane & 15);
-    return (paged && r < rounds && blk < nb) ? __ldg(ptab + blk) : 0;
-  };
-  int pg_next = page_of(0);
-  auto issue = [&](int r) {
-    if (r < rounds) {
-      const int blk0 = (g_lo + warp + kScoreWarps * r) * kScoreRound;
-      int at = -1;                                     // bounds index of block lane & 15
-      if (blk0 + (lane & 15) < nb) {
-        if (!paged) {
-          at = (int)(b * p.bd.stride_outer + kvh * p.bd.stride_head) + blk0 + (lane & 15);
-        } else if ((unsigned)pg_next < (unsigned)p.kv.num_pages) {
-          at = (int)(pg_next * p.bd.stride_outer + kvh * p.bd.stride_head);
-        } else {
-          atomicOr(p.flags, kFlagBadPage);
-        }
-      }
-      pg_next = page_of(r + 1);
-      const uint32_t slot = ring + (uint32_t)(r % kScoreStages) * kScoreStageBytes;
-      const int c = lane & 15;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 2 * i + (lane >> 4);
-        const int from = __shfl_sync(0xffffffffu, at, row);
-        cp_async_16(slot + row * kBoundsBytes + ((c ^ ((row & 1) << 2)) << 4), p.bd.codes + (long long)max(from, 0) * kBoundsBytes + c * 16,
-                    from >= 0 ? 16 : 0);
-      }
-      if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + max(at, 0), at >= 0 ? 4 : 0);
-    }
-    cp_async_commit();
-  };
-#pragma unroll
-  for (int r = 0; r < kScoreStages - 1; ++r) issue(r);
 
-  // ---- the group's query codes: sixteen threads per head, eight dimensions each
-#pragma unroll
-  for (int h0 = 0; h0 < kHeads; h0 += 8) {
-    const int h = h0 + (tid >> 4), d = (tid & 15) * 8;
-    const uint4 x = h < gq ? __ldg(reinterpret_cast<const uint4*>(p.q + ((long long)b * p.num_q_heads + head0 + h) * kHeadDim + d))
-                           : make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t mx = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-    uint32_t amax = max(mx & 0xffffu, mx >> 16);
-#pragma unroll
-    for (int off = 1; off < 16; off <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, off));
-    const int e = scale_exponent<6, 126>(amax);
-    const float inv = pow2i(-e);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t neg[2] = {0u, 0u}, pos[2] = {0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int code = __float2int_rn((j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1])) * inv);
-      neg[j >> 2] |= ((uint32_t)min(code, 0) & 0xffu) << (8 * (j & 3));
-      pos[j >> 2] |= (uint32_t)max(code, 0) << (8 * (j & 3));
-    }
-    *reinterpret_cast<uint2*>(&qcodes[h][0][d]) = make_uint2(neg[0], neg[1]);
-    *reinterpret_cast<uint2*>(&qcodes[h][1][d]) = make_uint2(pos[0], pos[1]);
-    if ((tid & 15) == 0) qscale[h] = h < gq ? pow2i(e) : 0.f;
-  }
-  __syncthreads();
-  const bool has0 = g < gq, has1 = kWide && g + 8 < gq;
-  uint4 q0[4], q1[4];                                  // heads g and g + 8: pieces 4i + tg
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    q0[i] = *reinterpret_cast<const uint4*>(&qcodes[g][i >> 1][64 * (i & 1) + 16 * tg]);
-    q1[i] = kWide ? *reinterpret_cast<const uint4*>(&qcodes[(g + 8) & (kHeads - 1)][i >> 1][64 * (i & 1) + 16 * tg]) : make_uint4(0u, 0u, 0u, 0u);
-  }
-  const float qs0 = qscale[g], qs1 = kWide ? qscale[(g + 8) & (kHeads - 1)] : 0.f;
-  float* const row0 = p.scores + ((long long)b * p.num_q_heads + head0 + (p.group_max ? 0 : g)) * p.ld;
+  // this CTA's run of groups and the unit it begins in; a sequence of impossible length has no groups
+  const int max_len = p.max_len;
+  auto groups_of = [max_len](int t) { return t > max_len || t < 0 ? 0 : (t + kScoreRound * kBlockRows - 1) / (kScoreRound * kBlockRows); };
+  int b = 0, at = 0;
+  const int total = count_items(p.kv.seq_lens, p.batch, num_kv, groups_of);
+  const int share = max((total + (int)gridDim.x - 1) / (int)gridDim.x, kScoreWarps);
+  if (blockIdx.x == 0)
+    for (int i = tid; i < p.batch; i += kScoreWarps * 32)
+      if (__ldg(p.kv.seq_lens + i) > max_len || __ldg(p.kv.seq_lens + i) < 0) atomicOr(p.flags, kFlagBadLength);
+  if ((long long)blockIdx.x * share >= total) return;
+  at = blockIdx.x * share;
+  const int run_end = min(at + share, total);
+  int before = 0;
+  find_item(p.kv.seq_lens, p.batch, num_kv, groups_of, at, &b, &before);
+  int groups = groups_of(__ldg(p.kv.seq_lens + b));
+  int kvh = (at - before) / groups;
+  int g_lo = at - before - kvh * groups;
 
-  for (int r = 0; r < rounds; ++r) {
-    cp_async_wait<kScoreStages - 2>();
-    __syncwarp();
-    issue(r + kScoreStages - 1);
-    const unsigned char* slot = g_smem + (warp * kScoreStages + r % kScoreStages) * kScoreStageBytes;
-    const float* scales = reinterpret_cast<const float*>(slot + kScoreRound * kBoundsBytes);
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      int d[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 x = *reinterpret_cast<const uint4*>(slot + (8 * n + g) * kBoundsBytes + (((4 * i + tg) ^ ((g & 1) << 2)) << 4));
-        mma_s8(d, q0[i].x, q1[i].x, q0[i].y, q1[i].y, x.x, x.y);
-        mma_s8(d, q0[i].z, q1[i].z, q0[i].w, q1[i].w, x.z, x.w);
-      }
-      const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + 8 * n + 2 * tg;
-      const float2 s = *reinterpret_cast<const float2*>(scales + 8 * n + 2 * tg);
-      float v[4] = {(float)d[0] * s.x * qs0, (float)d[1] * s.y * qs0, (float)d[2] * s.x * qs1, (float)d[3] * s.y * qs1};
-      if (p.group_max) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float m = fmaxf(has0 ? v[c] : -INFINITY, has1 ? v[2 + c] : -INFINITY);
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-          v[c] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+  while (true) {                                       // units of the run
+    const int t = __ldg(p.kv.seq_lens + b);
+    const int head0 = kvh * gq;
+    const int nb = (t + kBlockRows - 1) / kBlockRows;
+    const int g_hi = min(groups, g_lo + run_end - at);
+    const bool updates = p.update_last && g_hi == groups;
+    const int rounds = max(0, (g_hi - g_lo - warp + kScoreWarps - 1) / kScoreWarps);     // groups g_lo + warp + 4r
+    const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
+    auto page_of = [&](int r) -> int {                   // lanes 0..15: the page of block lane of round r
+      const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + (lane & 15);
+      return (paged && r < rounds && blk < nb) ? __ldg(ptab + blk) : 0;
+    };
+    int pg_next = page_of(0);
+    auto issue = [&](int r) {
+      if (r < rounds) {
+        const int blk0 = (g_lo + warp + kScoreWarps * r) * kScoreRound;
+        int at = -1;                                     // bounds index of block lane & 15
+        if (blk0 + (lane & 15) < nb) {
+          if (!paged) {
+            at = (int)(b * p.bd.stride_outer + kvh * p.bd.stride_head) + blk0 + (lane & 15);
+          } else if ((unsigned)pg_next < (unsigned)p.kv.num_pages) {
+            at = (int)(pg_next * p.bd.stride_outer + kvh * p.bd.stride_head);
+          } else {
+            atomicOr(p.flags, kFlagBadPage);
+          }
         }
+        pg_next = page_of(r + 1);
+        const uint32_t slot = ring + (uint32_t)(r % kScoreStages) * kScoreStageBytes;
+        const int c = lane & 15;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int row = 2 * i + (lane >> 4);
+          const int from = __shfl_sync(0xffffffffu, at, row);
+          cp_async_16(slot + row * kBoundsBytes + ((c ^ ((row & 1) << 2)) << 4), p.bd.codes + (long long)max(from, 0) * kBoundsBytes + c * 16,
+                      from >= 0 ? 16 : 0);
+        }
+        if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + max(at, 0), at >= 0 ? 4 : 0);
       }
-      auto store = [&](float* row, float a, float z) {
-        if (blk + 1 < nb) *reinterpret_cast<float2*>(row + blk) = make_float2(a, z);
-        else if (blk < nb) row[blk] = a;
-      };
-      if (p.group_max ? g == 0 : has0) store(row0, v[0], v[1]);
-      if (kWide && !p.group_max && has1) store(row0 + 8ll * p.ld, v[2], v[3]);
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int r = 0; r < kScoreStages - 1; ++r) issue(r);
+
+    // ---- the group's query codes: sixteen threads per head, eight dimensions each
+#pragma unroll
+    for (int h0 = 0; h0 < kHeads; h0 += 8) {
+      const int h = h0 + (tid >> 4), d = (tid & 15) * 8;
+      const uint4 x = h < gq ? __ldg(reinterpret_cast<const uint4*>(p.q + ((long long)b * p.num_q_heads + head0 + h) * kHeadDim + d))
+                             : make_uint4(0u, 0u, 0u, 0u);
+      const uint32_t mx = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+      uint32_t amax = max(mx & 0xffffu, mx >> 16);
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+      const int e = scale_exponent<6, 126>(amax);
+      const float inv = pow2i(-e);
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint32_t neg[2] = {0u, 0u}, pos[2] = {0u, 0u};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int code = __float2int_rn((j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1])) * inv);
+        neg[j >> 2] |= ((uint32_t)min(code, 0) & 0xffu) << (8 * (j & 3));
+        pos[j >> 2] |= (uint32_t)max(code, 0) << (8 * (j & 3));
+      }
+      *reinterpret_cast<uint2*>(&qcodes[h][0][d]) = make_uint2(neg[0], neg[1]);
+      *reinterpret_cast<uint2*>(&qcodes[h][1][d]) = make_uint2(pos[0], pos[1]);
+      if ((tid & 15) == 0) qscale[h] = h < gq ? pow2i(e) : 0.f;
     }
-  }
-  cp_async_wait<0>();
-  if (updates && warp == kScoreWarps - 1) {            // the bounds of the last block (its score is not used)
-    long long row, bi;
-    if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
-      bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
-    else if (lane == 0)
-      atomicOr(p.flags, kFlagBadPage);
+    __syncthreads();
+    const bool has0 = g < gq, has1 = kWide && g + 8 < gq;
+    uint4 q0[4], q1[4];                                  // heads g and g + 8: pieces 4i + tg
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q0[i] = *reinterpret_cast<const uint4*>(&qcodes[g][i >> 1][64 * (i & 1) + 16 * tg]);
+      q1[i] = kWide ? *reinterpret_cast<const uint4*>(&qcodes[(g + 8) & (kHeads - 1)][i >> 1][64 * (i & 1) + 16 * tg]) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    const float qs0 = qscale[g], qs1 = kWide ? qscale[(g + 8) & (kHeads - 1)] : 0.f;
+    float* const row0 = p.scores + ((long long)b * p.num_q_heads + head0 + (p.group_max ? 0 : g)) * p.ld;
+
+    for (int r = 0; r < rounds; ++r) {
+      cp_async_wait<kScoreStages - 2>();
+      __syncwarp();
+      issue(r + kScoreStages - 1);
+      const unsigned char* slot = g_smem + (warp * kScoreStages + r % kScoreStages) * kScoreStageBytes;
+      const float* scales = reinterpret_cast<const float*>(slot + kScoreRound * kBoundsBytes);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        int d[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4*>(slot + (8 * n + g) * kBoundsBytes + (((4 * i + tg) ^ ((g & 1) << 2)) << 4));
+          mma_s8(d, q0[i].x, q1[i].x, q0[i].y, q1[i].y, x.x, x.y);
+          mma_s8(d, q0[i].z, q1[i].z, q0[i].w, q1[i].w, x.z, x.w);
+        }
+        const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + 8 * n + 2 * tg;
+        const float2 s = *reinterpret_cast<const float2*>(scales + 8 * n + 2 * tg);
+        float v[4] = {(float)d[0] * s.x * qs0, (float)d[1] * s.y * qs0, (float)d[2] * s.x * qs1, (float)d[3] * s.y * qs1};
+        if (p.group_max) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float m = fmaxf(has0 ? v[c] : -INFINITY, has1 ? v[2 + c] : -INFINITY);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            v[c] = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+          }
+        }
+        auto store = [&](float* row, float a, float z) {
+          if (blk + 1 < nb) *reinterpret_cast<float2*>(row + blk) = make_float2(a, z);
+          else if (blk < nb) row[blk] = a;
+        };
+        if (p.group_max ? g == 0 : has0) store(row0, v[0], v[1]);
+        if (kWide && !p.group_max && has1) store(row0 + 8ll * p.ld, v[2], v[3]);
+      }
+    }
+    cp_async_wait<0>();
+    if (updates && warp == kScoreWarps - 1) {            // the bounds of the last block (its score is not used)
+      long long row, bi;
+      if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
+        bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
+      else if (lane == 0)
+        atomicOr(p.flags, kFlagBadPage);
+    }
+    at += g_hi - g_lo;
+    if (at >= run_end) return;
+    g_lo = 0;
+    if (++kvh == num_kv) {                               // the next sequence that has blocks
+      kvh = 0;
+      do groups = groups_of(__ldg(p.kv.seq_lens + ++b));
+      while (groups == 0);
+    }
+    __syncthreads();                                     // the query's codes are written again
   }
 }
 
@@ -597,7 +623,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   store_partial_bf16<kTiles>(o, st, gq, sm_o + warp * gq * kHeadDim, sm_m[warp], sm_l[warp], sm_lt[warp]);
   __syncthreads();
   auto part_row = [&](int head, int part) -> float* { return p.partials + ((long long)(unit0 + head) * p.splits + part) * kPartStride; };
-  finish_unit(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], kTWarps, gq, p.splits, split, part_row, p.tickets, p.out, p.out_lse, unit0,
+  finish_unit<kTWarps>(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], kTWarps, gq, p.splits, split, part_row, p.tickets, p.out, p.out_lse, unit0,
               &is_last);
 }
 

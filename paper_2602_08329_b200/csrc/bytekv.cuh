@@ -167,12 +167,15 @@ __global__ void __launch_bounds__(256) bytekv_append_kernel(ByteKvAppendParams p
 //   O^T += V^T P^T   ldmatrix.trans moves byte pairs: a lane receives dimensions 2g and 2g+1 of its two keys, so
 //                    tile row g is dimension 16c + 2g and row g + 8 is 16c + 2g + 1.  P^T is S^T's tile
 //                    transposed 8 x 8 in registers (movmatrix).
+// (The tensor cores would also take the keys' codes as they are, mma.sync m16n8k32 against the query in two e4m3
+// parts, exactly and without converting the keys; that measured slower, 358 us against 333 us for 2.1 GB.)
 // Sixteen MMAs per stage for up to eight heads; a lane's logits and its output columns belong to the same two
 // heads, 2tg and 2tg + 1, so a new reference exponent needs no shuffle to reach the accumulators.
 // (The first version had the heads on the rows: 24 MMAs, and four-lane shuffles of the factors.)
-// The warps run dependent chains (copy, convert, multiply, exponential, convert, multiply), so what the stream needs is
-// many of them: sixteen per SM with 12 KB rings.  (Eight with 24 KB rings issued 0.43 instructions per
-// cycle and scheduler, most of the stalls fixed latencies; a ragged paged batch of 32 took 151 us.)
+// The warps run dependent chains (copy, multiply, exponential, convert, multiply), so the stream needs many of them:
+// twelve per SM with 16 KB rings.  (Eight with 24 KB rings issued 0.43 instructions per cycle and scheduler, most
+// of the stalls fixed latencies: 147 us against 126 us for a ragged paged batch of 32; sixteen with 12 KB
+// rings have too few bytes in flight: 341 us against 329 us for 2.1 GB.)
 // Exponent bookkeeping.  The query is scaled by a power of two into [1, 2) (fp16 then keeps it to 2^-25 of its
 // largest element).  A key block's scale multiplies its logits.  A value block's scale 2^e multiplies the
 // weights: w = 2^(x - m) * 2^(e - R + 7), with m the running reference of the logits and R, an integer per
@@ -182,18 +185,19 @@ __global__ void __launch_bounds__(256) bytekv_append_kernel(ByteKvAppendParams p
 // The open block (bf16) enters the ring behind the last stage of the last warp and is one stage of the bf16 arithmetic
 // (bf16_stage) into a partial of its own, merged with the warps' partials.
 constexpr float k8Unscale = 0.0078125f;      // 2^-7: the weights enter the product times 2^7
-constexpr int k8Warps = 4;
-constexpr int k8Threads = k8Warps * 32;
 constexpr int k8StageBytes = 2 * kBlock8Bytes;                          // 16 K rows + 16 V rows = 4 KB
 constexpr int k8MetaBytes = 160;                                        // 16 K scales, 16 V scales, valid bits
-// With more than eight heads the accumulators need twice the registers: three CTAs per SM, deeper rings.
-template <bool kWide>
+// Lists have one CTA per unit where units are many: eight warps each, so that 256 of them keep the SMs busy.  (With four
+// warps and three CTAs per SM, 188 of 444 CTA slots stay empty: 29.3 us for 256 lists of 1838 entries.)
+template <bool kList, bool kWide>
 struct Shape8 {
-  static constexpr int kStages = 4;
-  static constexpr int kCtasPerSm = 3;
-  static constexpr int kRingBytes = k8Warps * kStages * k8StageBytes;
-  static constexpr int kSmemBytes = kRingBytes + k8Warps * kStages * k8MetaBytes;
-  static_assert((k8Warps + 1) * (kWide ? 16 : 8) * kHeadDim * 4 <= (k8Warps - 1) * kStages * k8StageBytes,
+  static constexpr int kWarps = kList ? 8 : 4;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kStages = kList ? 3 : 4;
+  static constexpr int kCtasPerSm = kList ? 2 : 3;
+  static constexpr int kRingBytes = kWarps * kStages * k8StageBytes;
+  static constexpr int kSmemBytes = kRingBytes + kWarps * kStages * k8MetaBytes;
+  static_assert((kWarps + 1) * (kList ? 1 : kWide ? 16 : 8) * kHeadDim * 4 <= (kWarps - 1) * kStages * k8StageBytes,
                 "the rings of all but the last warp take the partials");
 };
 constexpr int k8MaxCtasPerSm = 3;
@@ -205,9 +209,8 @@ struct ByteKvAttnParams {
   const int* count;         // [B][Hq]
   int idx_stride;
   int batch, num_q_heads, group_size;
-  int splits;               // kList
-  int even;                 // dense: even parts of every unit instead of equal runs (see below)
-  float* partials;          // kList: [B][Hq][splits][kPartStride]; dense: [CTA][2][group][kPartStride]
+  int deal;                 // kRuns, kParts, kWhole
+  float* partials;          // [CTA][2][heads per unit][kPartStride]
   unsigned int* tickets;    // [B][Hq], zero on entry and on exit
   __nv_bfloat16* out;
   float* out_lse;
@@ -280,51 +283,31 @@ __device__ __forceinline__ float load_query_f16(const __nv_bfloat16* q, bool has
   return __uint_as_float((uint32_t)e << 23) * (kScale * kLog2e);
 }
 
-// Work of the dense kernel.  Where there are many units (sequence, KV head), the blocks of all of them, laid end to
-// end, are dealt to the CTAs in equal runs whatever the lengths: a run may cover the end of one unit and the
-// beginning of the next.  A CTA holds at most two parts of units that it shares with its neighbours; whole units
-// are finished on the spot.  (With an even split of every unit a ragged batch waited for its longest sequence:
-// 32 sequences of 2K to 16K, 156 us.)  Where units are few against the CTAs (at most an eighth), every unit is cut
-// into even parts instead, one part per CTA: a CTA that crosses into a second unit pays its start and end twice
-// (8 KV heads of 2047 positions: 20 us against 12 us), and what the rounding wastes is small.
-// A unit counts as at least one block (its open block, or nothing, still has to be written).
-constexpr int k8MinRun = 16;        // blocks per CTA at least: four stages per warp
+// Work.  A unit is a (sequence, KV head), its items the whole blocks; or (lists) a (sequence, query head), its items
+// groups of sixteen entries, as many as a list can have (idx_stride: nobody has to look through all counts).
+// A unit counts as at least one item (its open block, or nothing, still has to be written).  Three ways to deal
+// units to CTAs:
+//   runs    the blocks of all units, laid end to end, in equal runs, whatever the lengths: a run may cover the end
+//           of one unit and the beginning of the next.  A CTA holds at most two parts of units that it shares with
+//           its neighbours; whole units are finished on the spot.  (With an even split of every unit a ragged
+//           batch waited for its longest sequence: 32 sequences of 2K to 16K, 156 us.)
+//   parts   where units are few against the CTAs (at most an eighth; lists, at most half): every unit in even parts,
+//           one part per CTA.  A CTA that crosses into a second unit pays its start and end twice (8 KV heads of
+//           2047 positions: 20 us against 12 us), and what the rounding wastes is small.
+//   whole   other lists: one CTA per unit (256 lists of 1838 entries: 29 us; in runs, 34 us)
+constexpr int kRuns = 0, kParts = 1, kWhole = 2;
+// items per CTA at least: below, a merge costs more than the shorter part saves
+template <bool kList>
+constexpr int k8MinRun = kList ? 32 : 16;
 
 __device__ __forceinline__ int unit_blocks(int t) { return max(1, t / kBlockRows); }
 
-// Warp-collective.  Items are laid out sequence after sequence, heads * f(blocks of the sequence) each.  x < 0: their
-// number.  Else -1 and the sequence that holds item x (*b) with the number of items before it, or their number
-// where x lies past the end.
-template <typename F>
-__device__ __forceinline__ int scan_lengths(const int* seq_lens, int batch, int heads, F f, int x, int* b, int* before) {
-  const int lane = threadIdx.x & 31;
-  int sum = 0;
-  for (int b0 = 0; b0 < batch; b0 += 32) {
-    const int w = b0 + lane < batch ? heads * f(unit_blocks(__ldg(seq_lens + b0 + lane))) : 0;
-    int incl = w;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += v;
-    }
-    if (x >= 0) {
-      const uint32_t past = __ballot_sync(0xffffffffu, sum + incl > x);
-      if (past) {
-        const int at = __ffs(past) - 1;
-        *b = b0 + at;
-        *before = sum + __shfl_sync(0xffffffffu, incl - w, at);
-        return -1;
-      }
-    }
-    sum += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  return sum;
-}
-
 // kWide: more than eight heads per KV head (two column tiles).
 template <int kFmt, bool kList, bool kWide>
-__global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_attn_kernel(ByteKvAttnParams p) {
-  constexpr int kStages = Shape8<kWide>::kStages;
+__global__ void __launch_bounds__(Shape8<kList, kWide>::kThreads, Shape8<kList, kWide>::kCtasPerSm)
+bytekv_attn_kernel(ByteKvAttnParams p) {
+  using Shape = Shape8<kList, kWide>;
+  constexpr int kStages = Shape::kStages, k8Warps = Shape::kWarps;
   constexpr int kTiles = kWide ? 2 : 1;        // column tiles of eight heads
   extern __shared__ __align__(128) unsigned char g_smem[];
   __shared__ int tail_count[kBlockRows];       // kList: how often each row of the open block is listed
@@ -338,7 +321,7 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
   const bool paged = p.kv.page_table != nullptr;
   const uint32_t smem0 = (uint32_t)__cvta_generic_to_shared(g_smem);
   const uint32_t ring = smem0 + warp * (kStages * k8StageBytes);
-  const uint32_t meta = smem0 + Shape8<kWide>::kRingBytes + warp * (kStages * k8MetaBytes);
+  const uint32_t meta = smem0 + Shape::kRingBytes + warp * (kStages * k8MetaBytes);
 
   // copies: a lane fills 16-byte position lane % 8 of row 2i + lane / 16 of the K (lane / 8 even) or V tile with
   // the source chunk that the swizzle wants there: the destination is the same in every stage and there are
@@ -352,79 +335,83 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
   const int lm_mi = lane >> 3, lm_r = lane & 7;
   const int vrow = (lm_mi & 1) * 8 + lm_r;
 
-  // this CTA's work
-  const bool even = !kList && p.even != 0;
-  int b, kvh, seg_lo = 0, part = 0, parts = 1;
-  int at = 0, run_end = 1, share = 1, unit_at = 0;
-  if (kList) {
-    b = blockIdx.z;
-    kvh = blockIdx.y / p.group_size;
-    part = blockIdx.x;
-    parts = p.splits;
-  } else {
-    const int total = scan_lengths(p.kv.seq_lens, p.batch, num_kv, [](int w) { return w; }, -1, &b, &at);
-    const int units = p.batch * num_kv, cta = blockIdx.x;
-    // runs: no shorter than k8MinRun blocks or a unit; even parts: as many as fit with every unit rounded up
-    const int ctas = even ? (int)gridDim.x - units : (int)gridDim.x;
-    share = max((total + ctas - 1) / ctas, min(k8MinRun, (total + units - 1) / units));
-    if (even) {
+  // this CTA's work: it begins in unit `sub` of sequence `seq` (lists: unit seq), at item seg_lo
+  const int cta = blockIdx.x, units = p.batch * (kList ? p.num_q_heads : num_kv);
+  const int list_items = kList ? max(1, (p.idx_stride + kBlockRows - 1) / kBlockRows) : 0;
+  int seq = cta, sub = 0, seg_lo = 0, part = 0, parts = 1;
+  int run_end = 1, share = 1, unit_at = 0;
+  if (p.deal != kWhole) {
+    int before = 0;
+    const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, unit_blocks);
+    // no shorter than k8MinRun items or a unit; parts: as many as fit with every unit rounded up
+    const int ctas = p.deal == kParts ? (int)gridDim.x - units : (int)gridDim.x;
+    share = max((total + ctas - 1) / ctas, min(k8MinRun<kList>, (total + units - 1) / units));
+    if (p.deal == kParts) {
       const int most = share;
-      auto count = [most](int w) { return (w + most - 1) / most; };
-      int before = 0;
-      if (scan_lengths(p.kv.seq_lens, p.batch, num_kv, count, cta, &b, &before) >= 0) return;     // more CTAs than parts
-      parts = count(unit_blocks(__ldg(p.kv.seq_lens + b)));
-      kvh = (cta - before) / parts;
-      part = (cta - before) - kvh * parts;
-    } else {
+      auto count = [most](int t) { return (unit_blocks(t) + most - 1) / most; };
+      if (kList) {
+        parts = (list_items + most - 1) / most;
+        if (cta >= units * parts) return;
+        seq = cta / parts;
+        part = cta - seq * parts;
+      } else {
+        if (!find_item(p.kv.seq_lens, p.batch, num_kv, count, cta, &seq, &before)) return;     // more CTAs than parts
+        parts = count(__ldg(p.kv.seq_lens + seq));
+        sub = (cta - before) / parts;
+        part = (cta - before) - sub * parts;
+      }
+    } else if (!kList) {
       if ((long long)cta * share >= total) return;
-      at = cta * share;
+      const int at = cta * share;
       run_end = min(at + share, total);
-      int before = 0;
-      scan_lengths(p.kv.seq_lens, p.batch, num_kv, [](int w) { return w; }, at, &b, &before);
-      const int w = unit_blocks(__ldg(p.kv.seq_lens + b));
-      kvh = (at - before) / w;
-      unit_at = before + kvh * w;
+      find_item(p.kv.seq_lens, p.batch, num_kv, unit_blocks, at, &seq, &before);
+      const int w = unit_blocks(__ldg(p.kv.seq_lens + seq));
+      sub = (at - before) / w;
+      unit_at = before + sub * w;
       seg_lo = at - unit_at;
     }
   }
 
   while (true) {                               // units of the run (one pass where the CTA has one part)
-    const int unit0 = kList ? b * p.num_q_heads + (int)blockIdx.y : b * p.num_q_heads + kvh * gq;
+    const int b = kList ? seq / p.num_q_heads : seq;
+    const int kvh = kList ? (seq - b * p.num_q_heads) / p.group_size : sub;
+    const int unit0 = kList ? seq : b * p.num_q_heads + kvh * gq;
     const int t = __ldg(p.kv.seq_lens + b);
     const int whole = t & ~(kBlockRows - 1);   // positions below are in the 8-bit cache, the rest in the tail
     const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
-    const int w = unit_blocks(t);              // dense
-    int first_cta = 0, seg_hi = w;
-    if (!kList && even) {
+    const int listed = kList ? min(max(__ldg(p.count + unit0), 0), p.idx_stride) : 0;
+    const int w = kList ? list_items : unit_blocks(t);
+    // items that have rows; parts and CTAs behind the last of them have nothing to do
+    const int live = kList ? (listed + kBlockRows - 1) / kBlockRows : whole / kBlockRows;
+    int first_cta = cta, seg_hi = w;
+    if (p.deal == kParts) {
       const int per = (w + parts - 1) / parts;             // parts * per >= w > (parts - 1) * per where parts = ceil(w / share)
       seg_lo = min(part * per, w);
       seg_hi = min(seg_lo + per, w);
-      first_cta = (int)blockIdx.x - part;
-    } else if (!kList) {
+      first_cta = cta - part;
+      if (kList) parts = max(1, (live + per - 1) / per);
+    } else if (!kList && p.deal == kRuns) {
       seg_hi = min(w, run_end - unit_at);
       first_cta = unit_at / share;
-      part = (int)blockIdx.x - first_cta;
+      part = cta - first_cta;
       parts = (unit_at + w - 1) / share - first_cta + 1;
     }
 
-    // list entries (kList) or blocks (dense) of this warp
-    const int cnt = kList ? min(max(__ldg(p.count + unit0), 0), p.idx_stride) : min(seg_hi, whole / kBlockRows);
-    int start, end, nstages;
+    if (kList && part >= parts) return;        // behind the list's last entry
+
+    // list entries (kList) or blocks (dense) of this warp: [start, end)
+    const int seg_end = min(seg_hi, live);
+    const int per_warp = (max(seg_end - seg_lo, 0) + k8Warps - 1) / k8Warps;
+    int start = min(seg_lo + warp * per_warp, max(seg_end, seg_lo));
+    int end = max(min(start + per_warp, seg_end), start);
+    const int nstages = end - start;
     if (kList) {
-      int per = (cnt + p.splits * k8Warps - 1) / (p.splits * k8Warps);
-      per = (per + kBlockRows - 1) & ~(kBlockRows - 1);
-      start = min(((int)blockIdx.x * k8Warps + warp) * per, cnt);
-      end = min(start + per, cnt);
-      nstages = (end - start + kBlockRows - 1) / kBlockRows;
-    } else {
-      const int per = (max(cnt - seg_lo, 0) + k8Warps - 1) / k8Warps;
-      start = min(seg_lo + warp * per, cnt);
-      end = min(start + per, cnt);
-      nstages = max(end - start, 0);
+      start = min(start * kBlockRows, listed);
+      end = min(end * kBlockRows, listed);
     }
 
     // ---- the open block: belongs to the end of the unit (dense) or wherever the list names it
-    const bool want_tail = t > whole && (kList || seg_hi == w);
+    const bool want_tail = t > whole && (kList ? listed > 0 : seg_hi == w);
     const int nissue = nstages + (want_tail && warp == k8Warps - 1 ? 2 : 0);      // its keys, its values
     if (kList) {
       if (tid < kBlockRows) tail_count[tid] = 0;
@@ -478,7 +465,7 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
     };
     if (kList) {
       ld.list = p.idx + (long long)unit0 * p.idx_stride;
-      ld.fused = 0; ld.s0 = 0; ld.nmid = 0; ld.lo = 0; ld.wlo = 0; ld.count = cnt;
+      ld.fused = 0; ld.s0 = 0; ld.nmid = 0; ld.lo = 0; ld.wlo = 0; ld.count = listed;
       pos1 = check_pos(list_entry(ld, start + lane, end), 0);
       resolve(pos1, page_of(pos1));
       pos1 = check_pos(list_entry(ld, start + 32 + lane, end), 1);
@@ -733,18 +720,16 @@ __global__ void __launch_bounds__(k8Threads, Shape8<kWide>::kCtasPerSm) bytekv_a
       store_partial_bf16<kTiles>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps], sm_lt[k8Warps]);
     }
     __syncthreads();
-    // a part's place: by unit and split (lists), else two per CTA, the one it begins in the middle of and the other
+    // a part's place: two per CTA, the one it begins in the middle of and the other
     auto part_row = [&](int head, int i) -> float* {
-      if (kList) return p.partials + ((long long)(unit0 + head) * p.splits + i) * kPartStride;
       return p.partials + ((long long)(2 * (first_cta + i) + (i == 0 ? 1 : 0)) * gq + head) * kPartStride;
     };
-    finish_unit(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
+    finish_unit<k8Warps>(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
                 p.out, p.out_lse, unit0, &is_last);
-    if (kList || even) return;
     unit_at += w;
-    if (unit_at >= run_end) return;
+    if (kList || p.deal != kRuns || unit_at >= run_end) return;
     seg_lo = 0;
-    if (++kvh == num_kv) { kvh = 0; ++b; }
+    if (++sub == num_kv) { sub = 0; ++seq; }
     __syncthreads();                           // the ring and the partials in it are used again
   }
 }

@@ -14,12 +14,12 @@ prhs_status check_device(prhs_ctx* c) {
 
 cudaError_t bytekv_set_attributes() {
   const struct { const void* kernel; int bytes; } all[] = {
-      {(const void*)bytekv_attn_kernel<kE4M3, false, false>, Shape8<false>::kSmemBytes},
-      {(const void*)bytekv_attn_kernel<kE4M3, false, true>, Shape8<true>::kSmemBytes},
-      {(const void*)bytekv_attn_kernel<kE4M3, true, false>, Shape8<false>::kSmemBytes},
-      {(const void*)bytekv_attn_kernel<kE5M2, false, false>, Shape8<false>::kSmemBytes},
-      {(const void*)bytekv_attn_kernel<kE5M2, false, true>, Shape8<true>::kSmemBytes},
-      {(const void*)bytekv_attn_kernel<kE5M2, true, false>, Shape8<false>::kSmemBytes}};
+      {(const void*)bytekv_attn_kernel<kE4M3, false, false>, Shape8<false, false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE4M3, false, true>, Shape8<false, true>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE4M3, true, false>, Shape8<true, false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, false, false>, Shape8<false, false>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, false, true>, Shape8<false, true>::kSmemBytes},
+      {(const void*)bytekv_attn_kernel<kE5M2, true, false>, Shape8<true, false>::kSmemBytes}};
   for (const auto& k : all) {
     const cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes);
     if (e != cudaSuccess) return e;
@@ -79,34 +79,33 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.batch = batch;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  p.splits = idx ? pick_splits(c, batch * c->cfg.num_q_heads, max_count) : 1;
-  p.partials = idx ? c->partials : c->stream_part;
+  p.partials = c->stream_part;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
   p.flags = c->flags;
-  // dense: one CTA per resident slot, fewer where the runs (at least k8MinRun blocks or a unit each) would not fill them
-  const long long units = (long long)batch * c->cfg.num_kv_heads;
+  // how the units are dealt (see bytekv.cuh), and to how many CTAs: one per resident slot, fewer where the items
+  // (k8MinRun per CTA) would not fill them.  max_count: positions of a sequence or entries of a list at most.
+  const int slots = (idx ? Shape8<true, false>::kCtasPerSm : Shape8<false, false>::kCtasPerSm) * c->sm_count;
+  const int min_run = idx ? k8MinRun<true> : k8MinRun<false>;
+  const long long units = (long long)batch * (idx ? c->cfg.num_q_heads : c->cfg.num_kv_heads);
   const long long unit_max = std::max(1, (max_count + kBlockRows - 1) / kBlockRows);
-  if (!idx && units * unit_max >= (1ll << 30))
-    return fail(c, PRHS_ERR_UNSUPPORTED, "batch * heads * max_seq_len above 2^34: pass a smaller max_seq_len");
-  const int slots = (c->gq > 8 ? Shape8<true>::kCtasPerSm : Shape8<false>::kCtasPerSm) * c->sm_count;
-  p.even = 8 * units <= slots ? 1 : 0;
-  const int ctas = (int)std::min<long long>(slots, units * ((unit_max + k8MinRun - 1) / k8MinRun) + (p.even ? units : 0));
-  const dim3 grid = idx ? dim3(p.splits, c->cfg.num_q_heads, batch) : dim3(ctas, 1, 1);
+  if (units * unit_max >= (1ll << 30))
+    return fail(c, PRHS_ERR_UNSUPPORTED, "units times their largest length above 2^34: pass a smaller max_seq_len or idx_stride");
+  p.deal = (idx ? 2 : 8) * units <= slots ? kParts : idx ? kWhole : kRuns;
+  const long long full = units * ((unit_max + min_run - 1) / min_run) + (p.deal == kParts ? units : 0);
+  const int ctas = (int)(p.deal == kWhole ? units : std::min<long long>(slots, full));
+  const dim3 grid(ctas);
   {
     LaunchScope ls(c, idx ? PRHS_KIND_ATTN_SPARSE : PRHS_KIND_ATTN_DENSE, st);
     const bool e4 = format == PRHS_BYTEKV_E4M3;
-    if (idx) {
-      if (e4) bytekv_attn_kernel<kE4M3, true, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, true, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
-    } else if (c->gq > 8) {
-      if (e4) bytekv_attn_kernel<kE4M3, false, true><<<grid, k8Threads, Shape8<true>::kSmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, false, true><<<grid, k8Threads, Shape8<true>::kSmemBytes, st>>>(p);
-    } else {
-      if (e4) bytekv_attn_kernel<kE4M3, false, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
-      else bytekv_attn_kernel<kE5M2, false, false><<<grid, k8Threads, Shape8<false>::kSmemBytes, st>>>(p);
-    }
+    auto launch = [&](auto kernel, int threads, int smem) { kernel<<<grid, threads, smem, st>>>(p); };
+    using List = Shape8<true, false>;
+    using Narrow = Shape8<false, false>;
+    using Wide = Shape8<false, true>;
+    if (idx) launch(e4 ? bytekv_attn_kernel<kE4M3, true, false> : bytekv_attn_kernel<kE5M2, true, false>, List::kThreads, List::kSmemBytes);
+    else if (c->gq > 8) launch(e4 ? bytekv_attn_kernel<kE4M3, false, true> : bytekv_attn_kernel<kE5M2, false, true>, Wide::kThreads, Wide::kSmemBytes);
+    else launch(e4 ? bytekv_attn_kernel<kE4M3, false, false> : bytekv_attn_kernel<kE5M2, false, false>, Narrow::kThreads, Narrow::kSmemBytes);
   }
   PRHS_CUDA(c, cudaGetLastError());
   return PRHS_OK;

@@ -12,6 +12,42 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return y;
 }
 
+// Items are laid out sequence after sequence, heads * f(length) each.  Warp-collective: their number.
+template <typename F>
+__device__ __forceinline__ int count_items(const int* seq_lens, int batch, int heads, F f) {
+  if (batch == 1) return heads * f(__ldg(seq_lens));
+  int sum = 0;
+#pragma unroll 4
+  for (int b = threadIdx.x & 31; b < batch; b += 32) sum += f(__ldg(seq_lens + b));
+  return heads * __reduce_add_sync(0xffffffffu, sum);
+}
+// Warp-collective: the sequence that holds item x (*b) and the number of items before it; false where x lies past the end.
+template <typename F>
+__device__ __forceinline__ bool find_item(const int* seq_lens, int batch, int heads, F f, int x, int* b, int* before) {
+  const int lane = threadIdx.x & 31;
+  *b = *before = 0;
+  if (batch == 1) return x < heads * f(__ldg(seq_lens));
+  int sum = 0;
+  for (int b0 = 0; b0 < batch; b0 += 32) {
+    const int w = b0 + lane < batch ? heads * f(__ldg(seq_lens + b0 + lane)) : 0;
+    int incl = w;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += v;
+    }
+    const uint32_t past = __ballot_sync(0xffffffffu, sum + incl > x);
+    if (past) {
+      const int at = __ffs(past) - 1;
+      *b = b0 + at;
+      *before = sum + __shfl_sync(0xffffffffu, incl - w, at);
+      return true;
+    }
+    sum += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return false;
+}
+
 // One head's softmax bookkeeping in a lane: l sums the fp32 weights (log-sum-exp), lt the weights as rounded to bf16,
 // which is what divides the output.
 struct SoftBf {
@@ -173,16 +209,16 @@ struct Merged {
   }
 };
 
-// End of a unit's work in a CTA of four warps: the warps' partials in shared memory (o [slot][head][128], m, l, l~
-// [slot][16]; at most five slots) become the result (one part) or this CTA's part in global memory, row(head, part)
+// End of a unit's work in a CTA of kWarps warps: the warps' partials in shared memory (o [slot][head][128], m, l, l~
+// [slot][16]; at most one slot more than warps) become the result (one part) or this CTA's part in global memory, row(head, part)
 // = o[128], m, l, l~; the CTA whose part arrives last merges them (a ticket, no waiting).  A warp per head, or
-// several warps per head where there are fewer than four; a lane has four columns, and the loads of sixteen parts
+// several warps per head where there are fewer than kWarps; a lane has four columns, and the loads of sixteen parts
 // are in flight at once.  (Heads one after the other, a column per thread, cost 5000 cycles for four heads in the
 // first half and 20 us for a merge of 32 parts.)
-template <typename Row>
+template <int kWarps, typename Row>
 __device__ __forceinline__ void finish_unit(float* sm_o, float* sm_m, float* sm_l, float* sm_lt, int slots, int heads, int parts, int part,
                                             Row row, unsigned int* tickets, __nv_bfloat16* out, float* out_lse, int unit0, bool* is_last) {
-  constexpr int kWarps = 4, kMaxSlots = 5, kBatch = 16;
+  constexpr int kMaxSlots = kWarps + 1, kBatch = 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   for (int h = warp; h < heads; h += kWarps) {
     Merged r;
@@ -217,8 +253,8 @@ __device__ __forceinline__ void finish_unit(float* sm_o, float* sm_m, float* sm_
   if (!*is_last) return;
   __threadfence();
   const int slices = heads >= kWarps ? 1 : kWarps / heads;            // warps per head
-  for (int h = slices == 1 ? warp : warp / slices; h < heads; h += kWarps / slices) {
-    const int slice = slices == 1 ? 0 : warp % slices;
+  const int slice = slices == 1 ? 0 : warp % slices;
+  for (int h = warp / slices; h < heads; h += kWarps / slices) {
     Merged r;
     for (int p0 = slice; p0 < parts; p0 += slices * kBatch) {
       // m, l, l~ of sixteen parts, one per lane; their columns
