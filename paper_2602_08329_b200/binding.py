@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -73,6 +74,9 @@ class Schedule(C.Structure):
 
 _BYTEKV_FORMATS = {torch.float8_e4m3fn: PRHS_BYTEKV_E4M3, torch.float8_e5m2: PRHS_BYTEKV_E5M2}
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+# the views' fields in C layout (a packed buffer builds a structure in half the time of its constructor)
+_KV_PACK = struct.Struct("@2P2qPi4xP2i").pack
+_BYTEKV_PACK = struct.Struct("@6P4q2P4i").pack
 
 
 class ByteKvView(C.Structure):
@@ -179,14 +183,18 @@ def make_schedule(top_k, window, sinks, refresh_interval=1, layer_group=1, dilat
 
 def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
     """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128]."""
-    assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.shape[-1] == 128
-    assert k.stride() == v.stride() and k.stride(-1) == 1 and k.stride(-2) == 128
-    assert seq_lens.dtype == torch.int32
-    view = KvView(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
-                  _ptr(page_table), page_table.stride(0) if page_table is not None else 0,
-                  seq_lens.data_ptr(), max_seq_len, k.shape[0] if page_table is not None else 0)
+    shape, stride = k.shape, k.stride()
+    assert k.dtype is _BF16 and v.dtype is _BF16 and shape[-1] == 128
+    assert stride == v.stride() and stride[-1] == 1 and stride[-2] == 128
+    assert seq_lens.dtype is _I32
+    if page_table is None:
+        table, table_stride, pages = 0, 0, 0
+    else:
+        table, table_stride, pages = _ptr(page_table), page_table.stride(0), shape[0]
+    view = KvView.from_buffer_copy(_KV_PACK(k.data_ptr(), v.data_ptr(), stride[0], stride[1], table, table_stride,
+                                            seq_lens.data_ptr(), max_seq_len, pages))
     view._keep = (k, v, seq_lens, page_table)
-    view._batch, view._heads, view._cap = seq_lens.shape[0], k.shape[1], k.shape[2] if page_table is None else 0
+    view._batch, view._heads, view._cap = seq_lens.shape[0], shape[1], 0 if pages else shape[2]
     return view
 
 
@@ -214,11 +222,11 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
     else:
         assert sshape == (shape[0], shape[1], shape[2] // 16) and sstride[2] == 1 and shape[0] >= B and max_seq_len <= shape[2]
         tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens)
-        table, table_stride, pages = None, 0, 0
+        table, table_stride, pages = 0, 0, 0
     _same_device(*tensors)
-    view = ByteKvView(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(),
-                      stride[0], stride[1], sstride[0], sstride[1], table, seq_lens.data_ptr(), table_stride, max_seq_len,
-                      pages, fmt)
+    view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(
+        k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(), stride[0],
+        stride[1], sstride[0], sstride[1], table, seq_lens.data_ptr(), table_stride, max_seq_len, pages, fmt))
     view._keep = tensors
     view._batch, view._heads, view._cap = B, shape[1], 0 if paged else shape[2]
     return view
