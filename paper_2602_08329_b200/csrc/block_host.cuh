@@ -150,7 +150,7 @@ int block_splits(const prhs_ctx* c, int units, int blocks) {
 }
 
 prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
-                              uint32_t flags, int batch, void* out, float* out_lse, bool after_select, cudaStream_t st) {
+                              uint32_t flags, int max_t, int batch, void* out, float* out_lse, const prhs_block_schedule* step, cudaStream_t st) {
   const bool shared = block_shared(c, flags);
   BlockAttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -163,6 +163,11 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
   p.splits = block_splits(c, batch * p.units_per_seq, stride);
+  p.max_len = max_t;
+  p.fixed = step ? 1 : 0;
+  p.sink = step ? step->sink_blocks : 0;
+  p.recent = step ? step->recent_blocks : 0;
+  p.top = step ? step->top_blocks : 0;
   p.partials = c->partials;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -170,10 +175,10 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.flags = c->flags;
   {
     LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
-    // (a caller's own lists may come from any kernel: then the launch is an ordinary one)
+    // `step`: the lists are this step's, from the kernel before; a caller's own may come from any kernel (ordinary launch)
     const dim3 grid(p.splits, p.units_per_seq, batch);
     const cudaError_t e = launch_ordered(p.heads_per_unit > 8 ? block_attn_kernel<true> : block_attn_kernel<false>, grid, kTThreads,
-                                         kTSmemBytes, st, p, after_select ? 1 : 0);
+                                         kTSmemBytes, st, p, step ? 1 : 0);
     PRHS_CUDA(c, e);
   }
   return PRHS_OK;
@@ -243,7 +248,7 @@ prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_v
   int max_t;
   prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, batch, out, out_lse, false, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse, nullptr, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
@@ -263,7 +268,7 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
   rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, true, as_stream(stream));
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, batch, out, out_lse, true, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, sched, as_stream(stream));
 }
 
 }  // extern "C"

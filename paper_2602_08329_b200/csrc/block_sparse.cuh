@@ -490,7 +490,8 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
 // Attention over listed blocks of a bf16 cache: one list per query head, or one per KV head for its whole group.
 // grid (splits, units per sequence, B).  A stage of the warp-private ring is one block, whose rows are
 // contiguous; rows past the end of the sequence are masked.  The arithmetic is bf16_stage: 16 MMAs per block
-// for up to eight heads (kWide: 32 for up to sixteen).
+// for up to eight heads (kWide: 32 for up to sixteen).  In a step, the first and the last blocks do not depend on
+// the selection: they are attended over while it runs, before step_wait().
 struct BlockAttnParams {
   const __nv_bfloat16* q;
   KvDev kv;
@@ -498,6 +499,10 @@ struct BlockAttnParams {
   const int* count;
   int stride, units_per_seq;
   int num_q_heads, group_size, heads_per_unit, splits;
+  int max_len;
+  // a step knows without the selection that blocks [0, sink) and the last `recent` are attended over (fixed = 1): it
+  // takes the lists' middle part only, `top` entries at most
+  int fixed, sink, recent, top;
   float* partials;          // [B][Hq][splits][kPartStride]
   unsigned int* tickets;
   __nv_bfloat16* out;
@@ -517,7 +522,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   const int unit0 = b * p.num_q_heads + head0;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2;
-  const int t = __ldg(p.kv.seq_lens + b);
+  const int t = min(max(__ldg(p.kv.seq_lens + b), 0), p.max_len);
   const int nb = (t + kBlockRows - 1) / kBlockRows;
   const long long unit = (long long)b * p.units_per_seq + u;
   const int* list = p.blocks + unit * p.stride;
@@ -529,95 +534,112 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   clear_tiles<kTiles>(o);
   SoftBf st[kTiles][2];
 
-  step_wait();                             // the lists may come from the kernel before this one
-  const int cnt = min(max(__ldcg(p.count + unit), 0), p.stride);
-  const int per = (cnt + p.splits * kTWarps - 1) / (p.splits * kTWarps);
-  const int start = min((split * kTWarps + warp) * per, cnt);
-  const int nstages = min(start + per, cnt) - start;
-
-  // where 32 listed blocks lie (element offset and real rows), one per lane, looked up a group ahead
-  const bool paged = p.kv.page_table != nullptr;
-  auto entry = [&](int grp) -> int {
-    const int j = grp * 32 + lane;
-    if (j >= nstages) return -1;
-    const int blk = __ldcg(list + start + j);
-    if ((unsigned)blk >= (unsigned)nb) {
-      atomicOr(p.flags, kFlagBadIndex);
-      return -1;
-    }
-    return blk;
-  };
-  auto page_of = [&](int blk) -> int {
-    return (paged && blk >= 0) ? __ldg(p.kv.page_table + (long long)b * p.kv.page_table_stride + blk) : 0;
-  };
-  long long off_cur = 0;
-  int rows_cur = 0;
-  auto place_group = [&](int blk, int page) {
-    rows_cur = blk >= 0 ? min(kBlockRows, t - blk * kBlockRows) : 0;
-    if (paged && rows_cur > 0 && (unsigned)page >= (unsigned)p.kv.num_pages) {
-      atomicOr(p.flags, kFlagBadPage);
-      rows_cur = 0;
-    }
-    off_cur = (long long)(paged ? page : b) * p.kv.stride_outer + (long long)kvh * p.kv.stride_head +
-              (paged ? 0ll : (long long)blk * (kBlockRows * kHeadDim));
-    if (rows_cur == 0) off_cur = 0;
-  };
-  int blk_next = entry(0), pg_next = page_of(blk_next);
-  place_group(blk_next, pg_next);
-  blk_next = entry(1);
-  pg_next = page_of(blk_next);
-
-  // a lane copies one 16-byte chunk of every row: lanes 0-15 of K, 16-31 of V
-  const __nv_bfloat16* src_base = lane < 16 ? p.kv.k : p.kv.v;
-  const uint32_t dst_lane = ring + (lane < 16 ? 0u : (uint32_t)kTTileBytes) + ((lane & 15u) << 4);
-  uint32_t sx[8];                          // source chunk that the swizzle wants at this lane's place, by row mod 8
-#pragma unroll
-  for (int k = 0; k < 8; ++k) sx[k] = (((uint32_t)lane & 15u) ^ (uint32_t)k) << 3;
-  int rows_of[kTStages];                   // real rows per ring slot (slots are compile-time below)
-  auto issue = [&](int j, auto slot_c) {
-    constexpr int kSlot = decltype(slot_c)::value;
-    if (j < nstages) {
-      if (j > 0 && (j & 31) == 0) {
-        place_group(blk_next, pg_next);
-        blk_next = entry((j >> 5) + 1);
-        pg_next = page_of(blk_next);
-      }
-      const __nv_bfloat16* src = src_base + __shfl_sync(0xffffffffu, off_cur, j & 31);
-      const int rows = __shfl_sync(0xffffffffu, rows_cur, j & 31);
-      const uint32_t dst = dst_lane + (uint32_t)kSlot * kTStageBytes;
-      if (rows == kBlockRows) {
-#pragma unroll
-        for (int r = 0; r < kTStageRows; ++r) cp_async_16_full(dst + r * kRowBytes, src + r * kHeadDim + sx[r & 7]);
+  // two passes over the ring: the blocks that are known (a step), then the listed ones
+  const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent);
+  const int worker = split * kTWarps + warp, workers = p.splits * kTWarps;
+  for (int pass = p.fixed ? 0 : 1; pass < 2; ++pass) {
+    int cnt;
+    if (pass == 0) {
+      cnt = lo + nb - hi;
+    } else {
+      step_wait();                           // the lists may come from the kernel before this one
+      if (p.fixed) {
+        cnt = min(p.top, hi - lo);
+        list += lo;
       } else {
-#pragma unroll
-        for (int r = 0; r < kTStageRows; ++r)
-          cp_async_16(dst + r * kRowBytes, src + (r < rows ? r * kHeadDim + sx[r & 7] : 0), r < rows ? 16 : 0);
+        cnt = min(max(__ldcg(p.count + unit), 0), p.stride);
       }
-      rows_of[kSlot] = rows;
     }
-    cp_async_commit();
-  };
-  issue(0, SlotC<0>{});
-  issue(1, SlotC<1>{});
-  auto stage = [&](int i, auto slot_c) {
-    constexpr int kSlot = decltype(slot_c)::value;
-    cp_async_wait<kTStages - 2>();
+    const int per = (cnt + workers - 1) / workers;
+    const int start = min(worker * per, cnt);
+    const int nstages = min(start + per, cnt) - start;
+
+    // where 32 listed blocks lie (element offset and real rows), one per lane, looked up a group ahead
+    const bool paged = p.kv.page_table != nullptr;
+    auto entry = [&](int grp) -> int {
+      const int j = grp * 32 + lane;
+      if (j >= nstages) return -1;
+      if (pass == 0) return start + j < lo ? start + j : hi + start + j - lo;
+      const int blk = __ldcg(list + start + j);
+      if ((unsigned)blk >= (unsigned)nb) {
+        atomicOr(p.flags, kFlagBadIndex);
+        return -1;
+      }
+      return blk;
+    };
+    auto page_of = [&](int blk) -> int {
+      return (paged && blk >= 0) ? __ldg(p.kv.page_table + (long long)b * p.kv.page_table_stride + blk) : 0;
+    };
+    long long off_cur = 0;
+    int rows_cur = 0;
+    auto place_group = [&](int blk, int page) {
+      rows_cur = blk >= 0 ? min(kBlockRows, t - blk * kBlockRows) : 0;
+      if (paged && rows_cur > 0 && (unsigned)page >= (unsigned)p.kv.num_pages) {
+        atomicOr(p.flags, kFlagBadPage);
+        rows_cur = 0;
+      }
+      off_cur = (long long)(paged ? page : b) * p.kv.stride_outer + (long long)kvh * p.kv.stride_head +
+                (paged ? 0ll : (long long)blk * (kBlockRows * kHeadDim));
+      if (rows_cur == 0) off_cur = 0;
+    };
+    int blk_next = entry(0), pg_next = page_of(blk_next);
+    place_group(blk_next, pg_next);
+    blk_next = entry(1);
+    pg_next = page_of(blk_next);
+
+    // a lane copies one 16-byte chunk of every row: lanes 0-15 of K, 16-31 of V
+    const __nv_bfloat16* src_base = lane < 16 ? p.kv.k : p.kv.v;
+    const uint32_t dst_lane = ring + (lane < 16 ? 0u : (uint32_t)kTTileBytes) + ((lane & 15u) << 4);
+    uint32_t sx[8];                          // source chunk that the swizzle wants at this lane's place, by row mod 8
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sx[k] = (((uint32_t)lane & 15u) ^ (uint32_t)k) << 3;
+    int rows_of[kTStages];                   // real rows per ring slot (slots are compile-time below)
+    auto issue = [&](int j, auto slot_c) {
+      constexpr int kSlot = decltype(slot_c)::value;
+      if (j < nstages) {
+        if (j > 0 && (j & 31) == 0) {
+          place_group(blk_next, pg_next);
+          blk_next = entry((j >> 5) + 1);
+          pg_next = page_of(blk_next);
+        }
+        const __nv_bfloat16* src = src_base + __shfl_sync(0xffffffffu, off_cur, j & 31);
+        const int rows = __shfl_sync(0xffffffffu, rows_cur, j & 31);
+        const uint32_t dst = dst_lane + (uint32_t)kSlot * kTStageBytes;
+        if (rows == kBlockRows) {
+#pragma unroll
+          for (int r = 0; r < kTStageRows; ++r) cp_async_16_full(dst + r * kRowBytes, src + r * kHeadDim + sx[r & 7]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < kTStageRows; ++r)
+            cp_async_16(dst + r * kRowBytes, src + (r < rows ? r * kHeadDim + sx[r & 7] : 0), r < rows ? 16 : 0);
+        }
+        rows_of[kSlot] = rows;
+      }
+      cp_async_commit();
+    };
+    issue(0, SlotC<0>{});
+    issue(1, SlotC<1>{});
+    auto stage = [&](int i, auto slot_c) {
+      constexpr int kSlot = decltype(slot_c)::value;
+      cp_async_wait<kTStages - 2>();
+      __syncwarp();
+      const int rows = rows_of[kSlot];
+      issue(i + kTStages - 1, SlotC<(kSlot + kTStages - 1) % kTStages>{});
+      if (rows == 0) return;
+      const uint32_t kt = ring + (uint32_t)kSlot * kTStageBytes;
+      bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, gq, g < rows, g + 8 < rows, o, st);
+    };
+    int i = 0;
+    for (; i + 2 < nstages; i += 3) {
+      stage(i, SlotC<0>{});
+      stage(i + 1, SlotC<1>{});
+      stage(i + 2, SlotC<2>{});
+    }
+    if (i < nstages) stage(i, SlotC<0>{});
+    if (i + 1 < nstages) stage(i + 1, SlotC<1>{});
+    cp_async_wait<0>();
     __syncwarp();
-    const int rows = rows_of[kSlot];
-    issue(i + kTStages - 1, SlotC<(kSlot + kTStages - 1) % kTStages>{});
-    if (rows == 0) return;
-    const uint32_t kt = ring + (uint32_t)kSlot * kTStageBytes;
-    bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, gq, g < rows, g + 8 < rows, o, st);
-  };
-  int i = 0;
-  for (; i + 2 < nstages; i += 3) {
-    stage(i, SlotC<0>{});
-    stage(i + 1, SlotC<1>{});
-    stage(i + 2, SlotC<2>{});
   }
-  if (i < nstages) stage(i, SlotC<0>{});
-  if (i + 1 < nstages) stage(i + 1, SlotC<1>{});
-  cp_async_wait<0>();
   __syncthreads();                         // the ring is free: it takes the warps' partials
   float* sm_o = reinterpret_cast<float*>(g_smem);
   store_partial_bf16<kTiles>(o, st, gq, sm_o + warp * gq * kHeadDim, sm_m[warp], sm_l[warp], sm_lt[warp]);
