@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
       issue(i + kTStages - 1, SlotC<(kSlot + kTStages - 1) % kTStages>{});
       if (rows == 0) return;
       const uint32_t kt = ring + (uint32_t)kSlot * kTStageBytes;
-      bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, gq, g < rows, g + 8 < rows, o, st);
+      bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, g < rows, g + 8 < rows, o, st);
     };
     int i = 0;
     for (; i + 2 < nstages; i += 3) {

@@ -224,6 +224,14 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same with a zero accumulator going in.
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                              uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, int src_bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
@@ -253,10 +261,9 @@ __device__ __forceinline__ void codes_to_f16_split(uint32_t w, uint32_t& even, u
   }
 }
 
-// One head's softmax bookkeeping in a lane.
+// One head's softmax bookkeeping in a lane.  R, an integer, is the reference exponent of the value scales.
 struct Soft8 {
-  float m = -INFINITY, l = 0.f;
-  int R = -1000;            // reference exponent of the value scales; any real exponent exceeds it
+  float m = kNoLogit, l = 0.f, R = 0.f;
 };
 
 // The query of one head (g of the lane) as B fragments: this lane's elements 16c + 4tg .. + 3, scaled into [1, 2).
@@ -544,14 +551,12 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
     // ---- query fragments (while the first copies are on their way) and logit factors
     uint32_t q0[kTiles][8], q1[kTiles][8];
     float qm[kTiles][2];
-    bool has[kTiles][2];
 #pragma unroll
     for (int hh = 0; hh < kTiles; ++hh) {
       const float f = load_query_f16(p.q + (long long)(unit0 + 8 * hh + g) * kHeadDim, 8 * hh + g < gq, q0[hh], q1[hh]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         qm[hh][e] = __shfl_sync(0xffffffffu, f, 8 * tg + 4 * e);
-        has[hh][e] = 8 * hh + 2 * tg + e < gq;
       }
     }
 
@@ -571,10 +576,6 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       // ---- S^T = K Q^T (two chains)
       float s[kTiles][2][4];
 #pragma unroll
-      for (int hh = 0; hh < kTiles; ++hh)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) { s[hh][c][0] = 0.f; s[hh][c][1] = 0.f; s[hh][c][2] = 0.f; s[hh][c][3] = 0.f; }
-#pragma unroll
       for (int pp = 0; pp < 2; ++pp) {
         uint32_t b0[4], b1[4];
         ldmatrix_x4(b0, kt + lm_r * kRow8Bytes + (((4 * pp + lm_mi) ^ lm_r) << 4));
@@ -585,32 +586,35 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
           codes_to_f16<kFmt>(b0[c], a0, a2);
           codes_to_f16<kFmt>(b1[c], a1, a3);
 #pragma unroll
-          for (int hh = 0; hh < kTiles; ++hh) mma_f16(s[hh][c & 1], a0, a1, a2, a3, q0[hh][4 * pp + c], q1[hh][4 * pp + c]);
+          for (int hh = 0; hh < kTiles; ++hh) {
+            if (pp == 0 && c < 2) mma_f16_first(s[hh][c], a0, a1, a2, a3, q0[hh][c], q1[hh][c]);
+            else mma_f16(s[hh][c & 1], a0, a1, a2, a3, q0[hh][4 * pp + c], q1[hh][4 * pp + c]);
+          }
         }
       }
-      // ---- logits of this lane's keys g and g + 8 for its heads; value scales as exponents
-      float ks[2];
-      int ve[2];
-      if (kList) {
-        ks[0] = ms[g]; ks[1] = ms[8 + g];
-        ve[0] = (int)(__float_as_uint(ms[16 + g]) >> 23) - 127;
-        ve[1] = (int)(__float_as_uint(ms[24 + g]) >> 23) - 127;
-      } else {
-        ks[0] = ms[0]; ks[1] = ks[0];
-        ve[0] = (int)(__float_as_uint(ms[16]) >> 23) - 127; ve[1] = ve[0];
+      // ---- logits of this lane's keys g and g + 8 for its heads; value scales as exponents.  (Heads that are not there
+      // have a zero query and columns that nobody reads.)
+      float ks[2], ve[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        ks[n] = ms[kList ? 8 * n + g : 0];
+        ve[n] = (float)((int)(__float_as_uint(ms[16 + (kList ? 8 * n + g : 0)]) >> 23) - 127);
       }
       float x[kTiles][2][2];                   // [tile][head][key]
       bool exceed = false;
 #pragma unroll
       for (int hh = 0; hh < kTiles; ++hh)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+          const Soft8& h = st[hh][e];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const bool ok = has[hh][e] && (!kList || ((vm >> (8 * n + g)) & 1u));
-            x[hh][e][n] = ok ? (s[hh][0][2 * n + e] + s[hh][1][2 * n + e]) * (qm[hh][e] * ks[n]) : -INFINITY;
-            exceed = exceed || x[hh][e][n] + (float)max(ve[n] - st[hh][e].R, 0) > st[hh][e].m + 8.f;
+            x[hh][e][n] = (s[hh][0][2 * n + e] + s[hh][1][2 * n + e]) * (qm[hh][e] * ks[n]);
+            if (kList && !((vm >> (8 * n + g)) & 1u)) x[hh][e][n] = -INFINITY;
           }
+          if (kList) exceed = exceed || fmaxf(x[hh][e][0] + fmaxf(ve[0] - h.R, 0.f), x[hh][e][1] + fmaxf(ve[1] - h.R, 0.f)) > h.m + 8.f;
+          else exceed = exceed || fmaxf(x[hh][e][0], x[hh][e][1]) + fmaxf(ve[0] - h.R, 0.f) > h.m + 8.f;
+        }
       if (__any_sync(0xffffffffu, exceed)) {
 #pragma unroll
         for (int hh = 0; hh < kTiles; ++hh) {
@@ -619,23 +623,19 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
           for (int e = 0; e < 2; ++e) {
             Soft8& h = st[hh][e];
             float mx = fmaxf(x[hh][e][0], x[hh][e][1]);
-            float my = fmaxf(x[hh][e][0] + (float)ve[0], x[hh][e][1] + (float)ve[1]);
+            float my = fmaxf(x[hh][e][0] + ve[0], x[hh][e][1] + ve[1]);
 #pragma unroll
             for (int off = 4; off <= 16; off <<= 1) {
               mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
               my = fmaxf(my, __shfl_xor_sync(0xffffffffu, my, off));
             }
-            fo[e] = 1.f;
-            if (mx > -INFINITY) {
-              const float mn = fmaxf(h.m, mx);
-              // m + R, the reference of the weighted values, moves up only
-              const float top = h.m > -INFINITY ? fmaxf(my, h.m + (float)h.R) : my;
-              const int Rn = (int)fmaxf(ceilf(top - mn), -400.f);
-              fo[e] = h.m > -INFINITY ? exp2f(h.m - mn + (float)(h.R - Rn)) : 0.f;
-              h.l *= h.m > -INFINITY ? exp2f(h.m - mn) : 0.f;
-              h.m = mn;
-              h.R = Rn;
-            }
+            const float mn = fmaxf(h.m, mx);
+            // m + R, the reference of the weighted values, moves up only
+            const float Rn = fmaxf(ceilf(fmaxf(my, h.m + h.R) - mn), -400.f);
+            fo[e] = exp2_fast(h.m - mn + h.R - Rn);
+            h.l *= exp2_fast(h.m - mn);
+            h.m = mn;
+            h.R = Rn;
           }
 #pragma unroll
           for (int c = 0; c < 8; ++c) { o[hh][c][0] *= fo[0]; o[hh][c][1] *= fo[1]; o[hh][c][2] *= fo[0]; o[hh][c][3] *= fo[1]; }
@@ -646,14 +646,18 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       for (int hh = 0; hh < kTiles; ++hh) {
         float wgt[2][2];                       // [key][head]
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+          Soft8& h = st[hh][e];
+          float vf[2];                         // 2^(value scale - R + 7)
+          vf[0] = exp2_fast(fminf(ve[0] - h.R + 7.f, 126.f));
+          vf[1] = kList ? exp2_fast(fminf(ve[1] - h.R + 7.f, 126.f)) : vf[0];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            Soft8& h = st[hh][e];
-            const float pv = x[hh][e][n] > -INFINITY ? exp2f(x[hh][e][n] - h.m) : 0.f;
+            const float pv = exp2_fast(x[hh][e][n] - h.m);
             h.l += pv;
-            wgt[n][e] = pv * __uint_as_float((uint32_t)min(max(ve[n] - h.R + 134, 0), 254) << 23);
+            wgt[n][e] = pv * vf[n];
           }
+        }
         pb[hh][0] = transpose_8x8(pack_f16x2(wgt[0][0], wgt[0][1]));
         pb[hh][1] = transpose_8x8(pack_f16x2(wgt[1][0], wgt[1][1]));
       }
@@ -687,8 +691,8 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
         const int head = 8 * hh + 2 * tg + e;
-        if (g == 0) { sm_m[warp][head] = st[hh][e].m; sm_l[warp][head] = l; sm_lt[warp][head] = l; }
-        f[e] = __uint_as_float((uint32_t)min(max(st[hh][e].R + 127, 0), 254) << 23);     // 2^R
+        if (g == 0) { sm_m[warp][head] = l > 0.f ? st[hh][e].m : -INFINITY; sm_l[warp][head] = l; sm_lt[warp][head] = l; }
+        f[e] = __uint_as_float((uint32_t)min(max((int)st[hh][e].R + 127, 0), 254) << 23);     // 2^R
         if (head < gq) {
 #pragma unroll
           for (int c = 0; c < 8; ++c)
@@ -716,7 +720,7 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       const uint32_t kt = ring + (uint32_t)slot_i * k8StageBytes;
       const uint32_t vt = ring + (uint32_t)(slot_i + 1 == kStages ? 0 : slot_i + 1) * k8StageBytes;
       for (int d = 0; d < passes; ++d)         // a row listed d times takes part in d passes (lists rarely repeat)
-        bf16_stage<kTiles>(kt, vt, tq, gq, times[0] > d, times[1] > d, to, ts);
+        bf16_stage<kTiles>(kt, vt, tq, times[0] > d, times[1] > d, to, ts);
       store_partial_bf16<kTiles>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps], sm_lt[k8Warps]);
     }
     __syncthreads();

@@ -48,10 +48,20 @@ __device__ __forceinline__ bool find_item(const int* seq_lens, int batch, int he
   return false;
 }
 
+// 2^x by the hardware's approximation, to 2^-22 relative; results below 2^-126 are zero.  (exp2f spends four more
+// instructions on denormal results, which as weights are nothing beside the largest one.)
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The reference exponent before the first logit: below every finite logit, and finite, so that no difference is NaN.
+constexpr float kNoLogit = -3.0e38f;
+
 // One head's softmax bookkeeping in a lane: l sums the fp32 weights (log-sum-exp), lt the weights as rounded to bf16,
 // which is what divides the output.
 struct SoftBf {
-  float m = -INFINITY, l = 0.f, lt = 0.f;
+  float m = kNoLogit, l = 0.f, lt = 0.f;
 };
 
 template <int kTiles>
@@ -80,23 +90,22 @@ __device__ __forceinline__ void load_query_bf16(const __nv_bfloat16* q, int head
 
 // One stage of 16 rows (K tile and V tile of [16][128] bf16, 16-byte chunk c of row r at chunk c ^ (r & 7)) by a warp:
 // S^T = K Q^T, online softmax, O^T += V^T P^T.  A lane owns keys g and g + 8 (real where v0, v1) for heads
-// 8hh + 2tg and + 1; o[hh][c] are dimensions 16c + g (0, 1) and 16c + g + 8 (2, 3) of the same two heads.
+// 8hh + 2tg and + 1 (heads that are not there have a zero query and columns that nobody reads); o[hh][c] are dimensions 16c + g (0, 1) and 16c + g + 8 (2, 3) of the same two heads.
 template <int kTiles>
-__device__ __forceinline__ void bf16_stage(uint32_t kt, uint32_t vt, const uint32_t (&qb)[kTiles][8][2], int heads, bool v0, bool v1,
+__device__ __forceinline__ void bf16_stage(uint32_t kt, uint32_t vt, const uint32_t (&qb)[kTiles][8][2], bool v0, bool v1,
                                            float (&o)[kTiles][8][4], SoftBf (&st)[kTiles][2]) {
-  const int lane = threadIdx.x & 31, tg = lane & 3;
+  const int lane = threadIdx.x & 31;
   const int row = (lane & 7) + 8 * ((lane >> 3) & 1), half = lane >> 4;     // ldmatrix: this lane's row, chunk of a pair
   float s[kTiles][2][4];
-#pragma unroll
-  for (int hh = 0; hh < kTiles; ++hh)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) { s[hh][c][0] = 0.f; s[hh][c][1] = 0.f; s[hh][c][2] = 0.f; s[hh][c][3] = 0.f; }
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
     uint32_t a[4];
     ldmatrix_x4(a, kt + row * kRowBytes + (((2 * ks + half) ^ (row & 7)) << 4));
 #pragma unroll
-    for (int hh = 0; hh < kTiles; ++hh) mma_bf16_full(s[hh][ks & 1], a[0], a[1], a[2], a[3], qb[hh][ks][0], qb[hh][ks][1]);
+    for (int hh = 0; hh < kTiles; ++hh) {
+      if (ks < 2) { s[hh][ks][0] = 0.f; s[hh][ks][1] = 0.f; s[hh][ks][2] = 0.f; s[hh][ks][3] = 0.f; }
+      mma_bf16_full(s[hh][ks & 1], a[0], a[1], a[2], a[3], qb[hh][ks][0], qb[hh][ks][1]);
+    }
   }
   const float sc = kScale * kLog2e;
   float x[kTiles][2][2];                     // [tile][head][key]
@@ -105,9 +114,8 @@ __device__ __forceinline__ void bf16_stage(uint32_t kt, uint32_t vt, const uint3
   for (int hh = 0; hh < kTiles; ++hh)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const bool has = 8 * hh + 2 * tg + e < heads;
-      x[hh][e][0] = has && v0 ? (s[hh][0][e] + s[hh][1][e]) * sc : -INFINITY;
-      x[hh][e][1] = has && v1 ? (s[hh][0][2 + e] + s[hh][1][2 + e]) * sc : -INFINITY;
+      x[hh][e][0] = v0 ? (s[hh][0][e] + s[hh][1][e]) * sc : -INFINITY;
+      x[hh][e][1] = v1 ? (s[hh][0][2 + e] + s[hh][1][2 + e]) * sc : -INFINITY;
       exceed = exceed || fmaxf(x[hh][e][0], x[hh][e][1]) > st[hh][e].m + 8.f;
     }
   // the reference exponent moves only when a logit exceeds it by more than 8 (weights stay below 2^8)
@@ -121,7 +129,7 @@ __device__ __forceinline__ void bf16_stage(uint32_t kt, uint32_t vt, const uint3
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
         const float mn = fmaxf(st[hh][e].m, mx);
-        f[e] = mn > -INFINITY ? exp2f(st[hh][e].m - mn) : 1.f;
+        f[e] = exp2_fast(st[hh][e].m - mn);
         st[hh][e].m = mn;
         st[hh][e].l *= f[e];
         st[hh][e].lt *= f[e];
@@ -138,7 +146,7 @@ __device__ __forceinline__ void bf16_stage(uint32_t kt, uint32_t vt, const uint3
     for (int e = 0; e < 2; ++e)
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        w[n][e] = x[hh][e][n] > -INFINITY ? exp2f(x[hh][e][n] - st[hh][e].m) : 0.f;
+        w[n][e] = exp2_fast(x[hh][e][n] - st[hh][e].m);
         st[hh][e].l += w[n][e];
       }
 #pragma unroll
@@ -175,7 +183,7 @@ __device__ __forceinline__ void store_partial_bf16(const float (&o)[kTiles][8][4
       }
       const int head = 8 * hh + 2 * tg + e;
       if (head < heads) {
-        if (g == 0) { sm_m[head] = st[hh][e].m; sm_l[head] = l; sm_lt[head] = lt; }
+        if (g == 0) { sm_m[head] = l > 0.f ? st[hh][e].m : -INFINITY; sm_l[head] = l; sm_lt[head] = lt; }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           sm_o[head * kHeadDim + 16 * c + g] = o[hh][c][e];
