@@ -363,7 +363,8 @@ prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const 
                             void* stream);
 
 /* prhs_dense_decode_attn over the 8-bit cache: attention over all i < t_b.  t_b = 0 gives a zero output row and
- * lse = -inf.  q and out 16-byte aligned. */
+ * lse = -inf; a t_b outside [0, max_seq_len] is cut to it and recorded (PRHS_FLAG_BAD_LENGTH).  q and out are
+ * 16-byte aligned and do not overlap. */
 prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
                                  void* stream);
 
@@ -415,7 +416,7 @@ prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv
 /* Softmax attention over the positions of the listed blocks (flags as above says how the lists are indexed).  Order is
  * free, a block listed twice is attended twice; a block outside [0, n_b) is skipped and recorded
  * (PRHS_FLAG_BAD_INDEX).  An empty list gives a zero output row and lse = -inf.
- *   out device bf16 [batch][Hq][128], out_lse device fp32 [batch][Hq] or NULL; q and out 16-byte aligned */
+ *   out device bf16 [batch][Hq][128], out_lse device fp32 [batch][Hq] or NULL; q and out 16-byte aligned, apart */
 prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
                                    int32_t blocks_stride, uint32_t flags, int32_t batch, void* out, float* out_lse, void* stream);
 
@@ -462,7 +463,7 @@ int32_t prhs_scores_ld(const prhs_ctx* ctx);
 #define PRHS_FLAG_BAD_PAGE        2u /* a page id outside [0, num_pages) was skipped          */
 #define PRHS_FLAG_SELECT_FALLBACK 4u /* informational: selection took the multi-pass path     */
 #define PRHS_FLAG_TIMEOUT         8u /* a bounded wait on a TMA barrier ran out; results invalid */
-#define PRHS_FLAG_BAD_LENGTH     16u /* a sequence whose lengths contradict each other was skipped */
+#define PRHS_FLAG_BAD_LENGTH     16u /* lengths contradict each other: sequence skipped, or its length cut */
 #define PRHS_FLAG_NONFINITE      32u /* an infinity or a NaN went into the 8-bit cache            */
 prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags);
 

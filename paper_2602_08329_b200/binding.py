@@ -194,7 +194,7 @@ def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
     view = KvView.from_buffer_copy(_KV_PACK(k.data_ptr(), v.data_ptr(), stride[0], stride[1], table, table_stride,
                                             seq_lens.data_ptr(), max_seq_len, pages))
     view._keep = (k, v, seq_lens, page_table)
-    view._batch, view._heads, view._cap = seq_lens.shape[0], shape[1], 0 if pages else shape[2]
+    view._batch, view._heads, view._cap, view._dev = seq_lens.shape[0], shape[1], 0 if pages else shape[2], k.get_device()
     return view
 
 
@@ -223,12 +223,12 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
         assert sshape == (shape[0], shape[1], shape[2] // 16) and sstride[2] == 1 and shape[0] >= B and max_seq_len <= shape[2]
         tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens)
         table, table_stride, pages = 0, 0, 0
-    _same_device(*tensors)
+    dev = _same_device(*tensors)
     view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(
         k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(), stride[0],
         stride[1], sstride[0], sstride[1], table, seq_lens.data_ptr(), table_stride, max_seq_len, pages, fmt))
     view._keep = tensors
-    view._batch, view._heads, view._cap = B, shape[1], 0 if paged else shape[2]
+    view._batch, view._heads, view._cap, view._dev = B, shape[1], 0 if paged else shape[2], dev
     return view
 
 
@@ -237,9 +237,8 @@ def make_block_bounds(codes, scale) -> BlockBoundsView:
     shape, stride = codes.shape, scale.stride()
     assert codes.dtype is torch.int8 and scale.dtype is _F32 and shape[-2:] == (2, 128)
     assert shape[:-2] == scale.shape and codes.is_contiguous() and scale.is_contiguous()
-    _same_device(codes, scale)
     view = BlockBoundsView(codes.data_ptr(), scale.data_ptr(), stride[0], stride[1])
-    view._keep = (codes, scale)
+    view._keep, view._shape, view._dev = (codes, scale), shape, _same_device(codes, scale)
     return view
 
 
@@ -247,11 +246,12 @@ def make_block_schedule(top_blocks, sink_blocks=1, recent_blocks=1, flags=0) -> 
     return BlockSchedule(top_blocks, sink_blocks, recent_blocks, flags)
 
 
-def _same_device(*tensors):
+def _same_device(*tensors) -> int:
     dev = tensors[0].get_device()
     assert dev >= 0, "tensors of a call must be on a CUDA device"
     for t in tensors:
         assert t.get_device() == dev, "tensors of a call must be on one CUDA device"
+    return dev
 
 
 class Context:
@@ -269,6 +269,7 @@ class Context:
         if rc != PRHS_OK:
             raise PrhsError(rc, self.lib.prhs_last_error(None).decode())
         self.h = h
+        self._hq, self._hkv, self._max_context = num_q_heads, num_kv_heads, max_context
 
     def close(self):
         if getattr(self, "h", None):
@@ -341,100 +342,109 @@ class Context:
     # -- the 8-bit cache
     def bytekv_append(self, new_k, new_v, new_lens, view, batch, max_new=0, stream=None):
         """Append new_k / new_v (bf16 [B][Hkv][rows][128], any strides over the first three axes)."""
-        shape, stride = new_k.shape, new_k.stride()
-        assert new_k.dtype is _BF16 and new_v.dtype is _BF16 and new_v.shape == shape and new_v.stride() == stride
-        assert len(shape) == 4 and shape[0] >= batch and shape[1] == self.cfg.num_kv_heads and shape[3] == 128 and stride[3] == 1
-        assert new_lens.dtype is _I32 and new_lens.shape[0] >= batch and new_lens.is_contiguous() and 0 <= max_new <= shape[2]
-        _same_device(new_k, new_v, new_lens, view._keep[0])
+        shape, (s0, s1, s2, s3) = new_k.shape, new_k.stride()
+        n0, n1, rows, d = shape
+        assert new_k.dtype is _BF16 and new_v.dtype is _BF16 and new_v.shape == shape and new_v.stride() == (s0, s1, s2, s3)
+        assert n0 >= batch and n1 == self._hkv and d == 128 and s3 == 1 and 0 <= max_new <= rows
+        assert new_lens.dtype is _I32 and new_lens.shape[0] >= batch and new_lens.is_contiguous()
+        assert new_k.get_device() == new_v.get_device() == new_lens.get_device() == view._dev
         self._fit(view, batch)
-        s0, s1, s2 = (st if n > 1 else 0 for st, n in zip(stride, shape[:3]))
-        self._ck(self.lib.prhs_bytekv_append(self.h, C.byref(view), new_k.data_ptr(), new_v.data_ptr(), s0, s1, s2,
-                                             new_lens.data_ptr(), max_new or shape[2], batch, _stream(stream)))
+        # the stride of an axis of one element is arbitrary
+        rc = self.lib.prhs_bytekv_append(self.h, C.byref(view), new_k.data_ptr(), new_v.data_ptr(), s0 if n0 > 1 else 0,
+                                         s1 if n1 > 1 else 0, s2 if rows > 1 else 0, new_lens.data_ptr(), max_new or rows, batch,
+                                         _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def bytekv_decode_attn(self, q, view, batch, out, out_lse=None, stream=None):
         lse = self._check_io(q, batch, out, out_lse, view)
-        self._ck(self.lib.prhs_bytekv_decode_attn(self.h, q.data_ptr(), C.byref(view), batch, out.data_ptr(), lse, _stream(stream)))
+        rc = self.lib.prhs_bytekv_decode_attn(self.h, q.data_ptr(), C.byref(view), batch, out.data_ptr(), lse, _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def bytekv_sparse_decode_attn(self, q, view, idx, count, batch, out, out_lse=None, stream=None):
         lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(q, idx, count, batch, self.cfg.num_q_heads)
-        self._ck(self.lib.prhs_bytekv_sparse_decode_attn(self.h, q.data_ptr(), C.byref(view), idx.data_ptr(), count.data_ptr(),
-                                                         stride, batch, out.data_ptr(), lse, _stream(stream)))
+        stride = self._check_lists(view._dev, idx, count, batch, self._hq)
+        rc = self.lib.prhs_bytekv_sparse_decode_attn(self.h, q.data_ptr(), C.byref(view), idx.data_ptr(), count.data_ptr(), stride,
+                                                     batch, out.data_ptr(), lse, _stream(stream))
+        if rc:
+            self._ck(rc)
 
     # -- attention over selected blocks
     def block_bounds(self, view, bounds, batch, first=None, max_new=0, stream=None):
-        assert first is None or (first.dtype is _I32 and first.shape[0] >= batch)
         self._fit_bounds(view, bounds, batch)
+        at = None
         if first is not None:
-            _same_device(first, bounds._keep[0])
-        self._ck(self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), _ptr(first), max_new, batch,
-                                            _stream(stream)))
+            assert first.dtype is _I32 and first.shape[0] >= batch and first.is_contiguous() and first.get_device() == view._dev
+            at = first.data_ptr()
+        rc = self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), at, max_new, batch, _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def block_topk(self, q, view, bounds, sched, batch, out_blocks, out_count, stream=None):
-        shape = (batch, self.cfg.num_q_heads, 128)
-        assert q.dtype is _BF16 and q.shape == shape and q.is_contiguous()
-        stride = self._check_lists(q, out_blocks, out_count, batch, self._block_units(sched.flags))
-        _same_device(q, view._keep[0])
+        assert q.dtype is _BF16 and q.shape == (batch, self._hq, 128) and q.is_contiguous() and q.get_device() == view._dev
+        stride = self._check_lists(view._dev, out_blocks, out_count, batch, self._block_units(sched.flags))
         self._fit_bounds(view, bounds, batch)
-        self._ck(self.lib.prhs_block_topk(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                          out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream)))
+        rc = self.lib.prhs_block_topk(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                      out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def block_decode_attn(self, q, view, blocks, count, batch, out, out_lse=None, flags=0, stream=None):
         lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(q, blocks, count, batch, self._block_units(flags))
-        self._ck(self.lib.prhs_block_decode_attn(self.h, q.data_ptr(), C.byref(view), blocks.data_ptr(), count.data_ptr(), stride,
-                                                 flags, batch, out.data_ptr(), lse, _stream(stream)))
+        stride = self._check_lists(view._dev, blocks, count, batch, self._block_units(flags))
+        rc = self.lib.prhs_block_decode_attn(self.h, q.data_ptr(), C.byref(view), blocks.data_ptr(), count.data_ptr(), stride, flags,
+                                             batch, out.data_ptr(), lse, _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def block_decode_step(self, q, view, bounds, sched, batch, out, out_lse, out_blocks, out_count, stream=None):
         lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(q, out_blocks, out_count, batch, self._block_units(sched.flags))
+        stride = self._check_lists(view._dev, out_blocks, out_count, batch, self._block_units(sched.flags))
         self._fit_bounds(view, bounds, batch)
-        self._ck(self.lib.prhs_block_decode_step(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                                 out.data_ptr(), lse, out_blocks.data_ptr(), stride, out_count.data_ptr(),
-                                                 _stream(stream)))
+        rc = self.lib.prhs_block_decode_step(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
+                                             out.data_ptr(), lse, out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream))
+        if rc:
+            self._ck(rc)
 
     def _fit(self, view, batch):
         """The view against this context: heads, batch, and no length beyond a contiguous cache's capacity."""
-        assert view._heads == self.cfg.num_kv_heads and batch <= view._batch
+        assert view._heads == self._hkv and batch <= view._batch and view._dev >= 0
         cap = view._cap
         if cap:
-            if view.max_seq_len == 0 and cap < self.cfg.max_context:
-                view.max_seq_len = cap
-            assert view.max_seq_len <= cap
+            n = view.max_seq_len
+            if n == 0 and cap < self._max_context:
+                n = view.max_seq_len = cap
+            assert n <= cap
 
     def _fit_bounds(self, view, bounds, batch):
         self._fit(view, batch)
-        codes = bounds._keep[0]
-        shape = codes.shape
-        assert shape[1] == view._heads
+        shape = bounds._shape
+        assert shape[1] == view._heads and bounds._dev == view._dev
         if view._cap:
-            assert len(shape) == 5 and shape[0] >= batch and shape[2] * 16 >= (view.max_seq_len or self.cfg.max_context)
+            assert len(shape) == 5 and shape[0] >= batch and shape[2] * 16 >= (view.max_seq_len or self._max_context)
         else:
             assert len(shape) == 4 and shape[0] >= view.num_pages
-        _same_device(view._keep[0], codes)
 
     def _block_units(self, flags):
-        return self.cfg.num_kv_heads if flags & PRHS_GROUP_SETS else self.cfg.num_q_heads
+        return self._hkv if flags & PRHS_GROUP_SETS else self._hq
 
     def _check_io(self, q, batch, out, out_lse, view):
         """Shapes, types and devices of a decode attention's tensors; the address of out_lse or None."""
         self._fit(view, batch)
-        shape = q.shape
-        assert shape == (batch, self.cfg.num_q_heads, 128) and out.shape == shape and q.dtype is _BF16 and out.dtype is _BF16
-        assert q.is_contiguous() and out.is_contiguous()
+        shape, dev = q.shape, view._dev
+        assert shape == (batch, self._hq, 128) and out.shape == shape and q.dtype is _BF16 and out.dtype is _BF16
+        assert q.is_contiguous() and out.is_contiguous() and q.get_device() == dev and out.get_device() == dev
         if out_lse is None:
-            _same_device(q, out, view._keep[0])
             return None
-        assert out_lse.dtype is _F32 and out_lse.shape == shape[:2] and out_lse.is_contiguous()
-        _same_device(q, out, view._keep[0], out_lse)
+        assert out_lse.dtype is _F32 and out_lse.shape == shape[:2] and out_lse.is_contiguous() and out_lse.get_device() == dev
         return out_lse.data_ptr()
 
-    def _check_lists(self, q, lists, count, batch, units):
-        shape = lists.shape
-        assert lists.dtype is _I32 and count.dtype is _I32 and shape[:-1] == (batch, units) and count.shape == (batch, units)
-        assert lists.is_contiguous() and count.is_contiguous()
-        _same_device(q, lists, count)
-        return shape[-1]
+    def _check_lists(self, dev, lists, count, batch, units):
+        b, u, stride = lists.shape
+        assert b == batch and u == units and lists.dtype is _I32 and count.dtype is _I32 and count.shape == (batch, units)
+        assert lists.is_contiguous() and count.is_contiguous() and lists.get_device() == dev and count.get_device() == dev
+        return stride
 
     def get_index_set(self, batch, stream=None):
         hq, cap = self.cfg.num_q_heads, self.index_capacity

@@ -240,13 +240,13 @@ prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv
 prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
                                    int32_t blocks_stride, uint32_t flags, int32_t batch, void* out, float* out_lse, void* stream) {
   if (!ctx) return PRHS_ERR_INVALID_ARG;
-  if (!q || !blocks || !count || !out) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
-  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (!blocks || !count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
   if (blocks_stride < 1 || blocks_stride > 3 * kMaxBlocks) return fail(ctx, PRHS_ERR_INVALID_ARG, "blocks_stride out of range");
   if (flags & ~PRHS_GROUP_SETS) return fail(ctx, PRHS_ERR_INVALID_ARG, "block attention: unknown flag");
   KvDev dv;
   int max_t;
-  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  prhs_status rc = check_q_out(ctx, q, out, batch);
+  if (rc == PRHS_OK) rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
   return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse, nullptr, as_stream(stream));
 }
@@ -255,12 +255,12 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
                                    const prhs_block_schedule* sched, int32_t batch, void* out, float* out_lse, int32_t* out_blocks,
                                    int32_t blocks_stride, int32_t* out_count, void* stream) {
   if (!ctx) return PRHS_ERR_INVALID_ARG;
-  if (!q || !out || !out_blocks || !out_count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
-  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (!out_blocks || !out_count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
   KvDev dv;
   BoundsDev bd;
   int max_t;
-  prhs_status rc = check_block_view(ctx, kv, batch, &dv, &max_t);
+  prhs_status rc = check_q_out(ctx, q, out, batch);
+  if (rc == PRHS_OK) rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
   if (rc == PRHS_OK) rc = check_block_sched(ctx, sched, blocks_stride, max_t);
   if (rc != PRHS_OK) return rc;

@@ -522,7 +522,8 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   const int unit0 = b * p.num_q_heads + head0;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2;
-  const int t = min(max(__ldg(p.kv.seq_lens + b), 0), p.max_len);
+  const int given = __ldg(p.kv.seq_lens + b), t = min(max(given, 0), p.max_len);
+  if (t != given && tid == 0) atomicOr(p.flags, kFlagBadLength);
   const int nb = (t + kBlockRows - 1) / kBlockRows;
   const long long unit = (long long)b * p.units_per_seq + u;
   const int* list = p.blocks + unit * p.stride;

@@ -210,6 +210,7 @@ struct ByteKvAttnParams {
   int idx_stride;
   int batch, num_q_heads, group_size;
   int deal;                 // kRuns, kParts, kWhole
+  int max_len;              // lengths outside [0, max_len] are cut to it (and recorded)
   float* partials;          // [CTA][2][heads per unit][kPartStride]
   unsigned int* tickets;    // [B][Hq], zero on entry and on exit
   __nv_bfloat16* out;
@@ -307,8 +308,6 @@ constexpr int kRuns = 0, kParts = 1, kWhole = 2;
 template <bool kList>
 constexpr int k8MinRun = kList ? 32 : 16;
 
-__device__ __forceinline__ int unit_blocks(int t) { return max(1, t / kBlockRows); }
-
 // kWide: more than eight heads per KV head (two column tiles).
 template <int kFmt, bool kList, bool kWide>
 __global__ void __launch_bounds__(Shape8<kList, kWide>::kThreads, Shape8<kList, kWide>::kCtasPerSm)
@@ -343,19 +342,21 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
   const int vrow = (lm_mi & 1) * 8 + lm_r;
 
   // this CTA's work: it begins in unit `sub` of sequence `seq` (lists: unit seq), at item seg_lo
+  const int max_len = p.max_len;
+  auto blocks_of = [max_len](int t) { return max(1, min(t, max_len) / kBlockRows); };      // a unit's items, at least one
   const int cta = blockIdx.x, units = p.batch * (kList ? p.num_q_heads : num_kv);
   const int list_items = kList ? max(1, (p.idx_stride + kBlockRows - 1) / kBlockRows) : 0;
   int seq = cta, sub = 0, seg_lo = 0, part = 0, parts = 1;
   int run_end = 1, share = 1, unit_at = 0;
   if (p.deal != kWhole) {
     int before = 0;
-    const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, unit_blocks);
+    const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, blocks_of);
     // no shorter than k8MinRun items or a unit; parts: as many as fit with every unit rounded up
     const int ctas = p.deal == kParts ? (int)gridDim.x - units : (int)gridDim.x;
     share = max((total + ctas - 1) / ctas, min(k8MinRun<kList>, (total + units - 1) / units));
     if (p.deal == kParts) {
       const int most = share;
-      auto count = [most](int t) { return (unit_blocks(t) + most - 1) / most; };
+      auto count = [&](int t) { return (blocks_of(t) + most - 1) / most; };
       if (kList) {
         parts = (list_items + most - 1) / most;
         if (cta >= units * parts) return;
@@ -371,8 +372,8 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       if ((long long)cta * share >= total) return;
       const int at = cta * share;
       run_end = min(at + share, total);
-      find_item(p.kv.seq_lens, p.batch, num_kv, unit_blocks, at, &seq, &before);
-      const int w = unit_blocks(__ldg(p.kv.seq_lens + seq));
+      find_item(p.kv.seq_lens, p.batch, num_kv, blocks_of, at, &seq, &before);
+      const int w = blocks_of(__ldg(p.kv.seq_lens + seq));
       sub = (at - before) / w;
       unit_at = before + sub * w;
       seg_lo = at - unit_at;
@@ -383,11 +384,12 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
     const int b = kList ? seq / p.num_q_heads : seq;
     const int kvh = kList ? (seq - b * p.num_q_heads) / p.group_size : sub;
     const int unit0 = kList ? seq : b * p.num_q_heads + kvh * gq;
-    const int t = __ldg(p.kv.seq_lens + b);
+    const int given = __ldg(p.kv.seq_lens + b), t = min(max(given, 0), max_len);
+    if (t != given && tid == 0) atomicOr(p.flags, kFlagBadLength);
     const int whole = t & ~(kBlockRows - 1);   // positions below are in the 8-bit cache, the rest in the tail
     const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
     const int listed = kList ? min(max(__ldg(p.count + unit0), 0), p.idx_stride) : 0;
-    const int w = kList ? list_items : unit_blocks(t);
+    const int w = kList ? list_items : blocks_of(t);
     // items that have rows; parts and CTAs behind the last of them have nothing to do
     const int live = kList ? (listed + kBlockRows - 1) / kBlockRows : whole / kBlockRows;
     int first_cta = cta, seg_hi = w;

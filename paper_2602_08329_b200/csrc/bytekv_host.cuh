@@ -12,6 +12,17 @@ prhs_status check_device(prhs_ctx* c) {
   return PRHS_OK;
 }
 
+// q [batch][Hq][128] in, out of the same shape: 16-byte aligned and apart (a CTA writes its result while others still
+// read their queries).
+prhs_status check_q_out(prhs_ctx* c, const void* q, const void* out, int batch) {
+  if (!q || !out) return fail(c, PRHS_ERR_INVALID_ARG, "NULL pointer");
+  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(c, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  const uintptr_t bytes = (uintptr_t)std::max(batch, 0) * c->cfg.num_q_heads * kRowBytes;
+  if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes)
+    return fail(c, PRHS_ERR_INVALID_ARG, "q and out overlap");
+  return PRHS_OK;
+}
+
 cudaError_t bytekv_set_attributes() {
   const struct { const void* kernel; int bytes; } all[] = {
       {(const void*)bytekv_attn_kernel<kE4M3, false, false>, Shape8<false, false>::kSmemBytes},
@@ -69,7 +80,7 @@ prhs_status check_bytekv(prhs_ctx* ctx, const prhs_bytekv_view* kv, int batch, B
 }
 
 prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, int format, const int* idx, const int* count, int idx_stride,
-                            int max_count, int batch, void* out, float* out_lse, cudaStream_t st) {
+                            int max_count, int max_t, int batch, void* out, float* out_lse, cudaStream_t st) {
   ByteKvAttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.kv = kv;
@@ -80,6 +91,7 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
   p.partials = c->stream_part;
+  p.max_len = max_t;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
@@ -160,27 +172,26 @@ prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const 
 prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
                                  void* stream) {
   if (!ctx) return PRHS_ERR_INVALID_ARG;
-  if (!q || !out) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
-  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   ByteKvDev dv;
   int max_t;
-  prhs_status rc = check_bytekv(ctx, kv, batch, &dv, &max_t);
+  prhs_status rc = check_q_out(ctx, q, out, batch);
+  if (rc == PRHS_OK) rc = check_bytekv(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_bytekv_attn(ctx, q, dv, kv->format, nullptr, nullptr, 0, max_t, batch, out, out_lse, as_stream(stream));
+  return launch_bytekv_attn(ctx, q, dv, kv->format, nullptr, nullptr, 0, max_t, max_t, batch, out, out_lse, as_stream(stream));
 }
 
 prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, const int32_t* idx,
                                         const int32_t* count, int32_t idx_stride, int32_t batch, void* out, float* out_lse,
                                         void* stream) {
   if (!ctx) return PRHS_ERR_INVALID_ARG;
-  if (!q || !idx || !count || !out) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
+  if (!idx || !count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
   if (idx_stride < 1) return fail(ctx, PRHS_ERR_INVALID_ARG, "idx_stride must be >= 1");
-  if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(ctx, PRHS_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   ByteKvDev dv;
   int max_t;
-  prhs_status rc = check_bytekv(ctx, kv, batch, &dv, &max_t);
+  prhs_status rc = check_q_out(ctx, q, out, batch);
+  if (rc == PRHS_OK) rc = check_bytekv(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_bytekv_attn(ctx, q, dv, kv->format, idx, count, idx_stride, idx_stride, batch, out, out_lse, as_stream(stream));
+  return launch_bytekv_attn(ctx, q, dv, kv->format, idx, count, idx_stride, idx_stride, max_t, batch, out, out_lse, as_stream(stream));
 }
 
 }  // extern "C"

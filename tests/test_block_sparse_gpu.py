@@ -290,6 +290,60 @@ def test_decode_run(cuda_device, paged, group, shared):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group,shared,batch", [(2, 2, False, 70), (8, 8, True, 40), (1, 12, True, 65)])
+def test_steps_of_many_ragged_sequences(cuda_device, heads, group, shared, batch):
+    g = torch.Generator().manual_seed(3)
+    lens = torch.randint(0, 700, (batch,), generator=g).tolist()
+    for b in range(0, batch, 7):
+        lens[b] = [0, 1, 16, 690, 17][b // 7 % 5]
+    cache = Cache(batch, heads, 700, True, cuda_device)
+    ctx = make_ctx(cache, group)
+    cache.place(random_rows(batch, heads, 700, 5), [max(t - 1, 0) for t in lens])
+    ctx.block_bounds(cache.view(), cache.bounds(), batch)
+    cache.place(cache.rows, lens)
+    units = heads if shared else heads * group
+    q = torch.randn(batch, heads * group, 128, generator=g).to(torch.bfloat16).to(cuda_device)
+    blocks, count = torch.empty(batch, units, 12, dtype=torch.int32, device=cuda_device), torch.empty(batch, units, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    sched = P.make_block_schedule(8, 2, 2, P.PRHS_GROUP_SETS if shared else 0)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, batch, out, lse, blocks, count)
+    assert ctx.check() == 0
+    sets = ref_sets(cache, np64(q), lens, group, 8, 2, 2, shared)
+    for (b, u), want in sets.items():
+        assert blocks[b, u].tolist() == want + [-1] * (12 - len(want)), (b, u)
+    check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    for b, t in enumerate(lens):
+        for h in range(heads):
+            codes, scales = cache.ref_bounds(b, h, t)
+            for j in range(-(-t // 16)):
+                c, s = cache.bound_of(b, h, j)
+                assert s == scales[j] and np.array_equal(c, codes[j])
+    ctx.close()
+
+
+def test_empty_batch_and_lengths_out_of_range(cuda_device):
+    cache = Cache(3, 1, 64, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    cache.place(random_rows(3, 1, 64, 1), [64, 64, 64])
+    ctx.block_bounds(cache.view(), cache.bounds(), 3)
+    q = torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(3, 2, device=cuda_device)
+    blocks, count = torch.empty(3, 2, 4, dtype=torch.int32, device=cuda_device), torch.empty(3, 2, dtype=torch.int32, device=cuda_device)
+    step = lambda: ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(2, 1, 1), 3, out, lse, blocks, count)  # noqa: E731
+    cache.lens.zero_()
+    step()
+    assert ctx.check() == 0 and bool((out == 0).all()) and bool((lse == -math.inf).all())
+    assert bool((count == 0).all()) and bool((blocks == -1).all())
+    cache.lens.copy_(torch.tensor([64, -1, 65], dtype=torch.int32))
+    step()
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    sets = ref_sets(cache, np64(q)[:1], [64], 2, 2, 1, 1, False)
+    check_attention(cache, np64(q), [64], 2, sets, False, out, lse)
+    assert bool((out[1] == 0).all()) and count[1].tolist() == [0, 0]
+    ctx.close()
+
+
 def test_all_blocks_are_the_dense_attention(cuda_device):
     cache = Cache(2, 2, 700, False, cuda_device)
     ctx = make_ctx(cache, 2)
@@ -368,7 +422,7 @@ def test_refusals(cuda_device):
     torch.cuda.synchronize()
     out.fill_(7.0)
     assert step(P.make_block_schedule(9, 1, 1), stride=3) == CAPACITY
-    assert step(o=out.data_ptr() + 2) == INVALID
+    assert step(o=out.data_ptr() + 2) == INVALID and step(o=q.data_ptr() + 1024) == INVALID
     view = cache.view()
     view.max_seq_len = 65
     assert step(view=view) == CAPACITY and bounds(view=view) == CAPACITY

@@ -369,6 +369,69 @@ def test_decode_run_in_a_graph(cuda_device):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group,batch", [(2, 2, 70), (4, 8, 40), (8, 1, 100), (3, 16, 33)])
+def test_many_ragged_sequences(cuda_device, heads, group, batch):
+    # more units than parts: equal runs that cross units, sequences without whole blocks or without anything
+    g = torch.Generator().manual_seed(8)
+    lens = torch.randint(0, 420, (batch,), generator=g).tolist()
+    for b in range(0, batch, 9):
+        lens[b] = [0, 3, 16, 417, 15][b // 9 % 5]
+    cache = Cache("e4m3", batch, heads, 420, True, cuda_device)
+    ctx = make_ctx(cache, group)
+    fill(ctx, cache, lens)
+    q = torch.randn(batch, heads * group, 128, generator=g).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.bytekv_decode_attn(q, cache.view(), batch, out, lse)
+    assert ctx.check() == 0
+    check_dense(ctx, cache, lens, group, q, out, lse)
+    ctx.close()
+
+
+@pytest.mark.parametrize("heads,group,batch,stride", [(4, 4, 16, 70), (2, 1, 3, 1500), (4, 8, 2, 900)])
+def test_lists_in_one_cta_and_in_parts(cuda_device, heads, group, batch, stride):
+    # 256 units: one CTA each; few units: even parts, with counts from nothing to the whole stride
+    U = heads * group
+    lens = [600 + 37 * b for b in range(batch)]
+    cache = Cache("e4m3", batch, heads, max(lens), False, cuda_device)
+    ctx = make_ctx(cache, group)
+    fill(ctx, cache, lens)
+    rng = np.random.default_rng(6)
+    cnt = rng.integers(0, stride + 1, (batch, U)).astype(np.int32)
+    cnt[0, 0], cnt[-1, -1] = 0, stride
+    idx = np.stack([rng.integers(0, lens[b], (U, stride)) for b in range(batch)]).astype(np.int32)
+    q = torch.randn(batch, U, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.bytekv_sparse_decode_attn(q, cache.view(), torch.from_numpy(idx).to(cuda_device), torch.from_numpy(cnt).to(cuda_device), batch, out, lse)
+    assert ctx.check() == 0
+    y_all, l_all = np64(out), np64(lse)
+    for b in range(batch):
+        kv = {h: (cache.rows("k", b, h, lens[b]), cache.rows("v", b, h, lens[b])) for h in range(heads)}
+        for u in range(U):
+            c = idx[b, u, : cnt[b, u]]
+            y, l, tol, ltol = R.attend(np64(q[b, u]), kv[u // group][0][c], kv[u // group][1][c], True)
+            assert np.all(np.abs(y_all[b, u] - y) <= tol), (b, u)
+            assert l_all[b, u] == l if math.isinf(l) else abs(l_all[b, u] - l) <= ltol
+    ctx.close()
+
+
+def test_lengths_out_of_range_are_cut_and_recorded(cuda_device):
+    cache = Cache("e4m3", 3, 1, 64, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    fill(ctx, cache, [64, 64, 64])
+    cache.set_lens([-3, 1 << 30, 20])
+    q = torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(3, 2, device=cuda_device)
+    idx = torch.arange(64, dtype=torch.int32, device=cuda_device).expand(3, 2, 64).contiguous()
+    cnt = torch.full((3, 2), 20, dtype=torch.int32, device=cuda_device)
+    for call in (lambda: ctx.bytekv_decode_attn(q, cache.view(), 3, out, lse),
+                 lambda: ctx.bytekv_sparse_decode_attn(q, cache.view(), idx, cnt, 3, out, lse)):
+        call()
+        with pytest.raises(P.PrhsError):
+            ctx.check()
+        assert bool((out[0] == 0).all()) and bool((lse[0] == -math.inf).all())
+    ctx.close()
+
+
 def test_split_counts_agree(cuda_device):
     # one long sequence runs split over many CTAs, a batch of copies with fewer splits: both near the 64-bit value
     for batch in (1, 48):
@@ -428,6 +491,7 @@ def test_refusals(cuda_device):
     assert append(view, m=0) == INVALID and append(view, m=65) == CAPACITY and append(view, r=4) == INVALID
     assert append(view, k=None) == INVALID and append(view, n=None) == INVALID and append(view, v=new.data_ptr() + 2) == INVALID
     assert append(view, b=3) == CAPACITY and attn(view, b=0) == INVALID and attn(view, o=out.data_ptr() + 4) == INVALID
+    assert attn(view, o=q.data_ptr()) == INVALID and attn(view, o=q.data_ptr() + 256) == INVALID     # q and out overlap
     assert rows(view, stride=0) == INVALID
     assert lib.prhs_bytekv_decode_attn(None, q.data_ptr(), C.byref(view), 2, out.data_ptr(), None, st) == INVALID
     torch.cuda.synchronize()
