@@ -2,6 +2,8 @@
 
 Argument marshalling only: every step of the path runs in the CUDA library.  Tensors are
 passed as raw device (or host) pointers; torch is used for device memory and streams.
+The views and the calls of the 8-bit cache and of block selection read their tensors through a
+compiled helper (csrc/marshal.cpp): the small calls of a decode loop are bound by the host.
 Loading fails loudly if the library has not been built -- there is no fallback.
 """
 from __future__ import annotations
@@ -72,8 +74,6 @@ class Schedule(C.Structure):
                 ("sim_threshold", C.c_float)]
 
 
-_BYTEKV_FORMATS = {torch.float8_e4m3fn: PRHS_BYTEKV_E4M3, torch.float8_e5m2: PRHS_BYTEKV_E5M2}
-_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 # the views' fields in C layout (a packed buffer builds a structure in half the time of its constructor)
 _KV_PACK = struct.Struct("@2P2qPi4xP2i").pack
 _BYTEKV_PACK = struct.Struct("@6P4q2P4i").pack
@@ -95,6 +95,20 @@ class BlockSchedule(C.Structure):
 
 
 _lib = None
+_marshal = None
+
+
+def _load_marshal():
+    """The compiled part of the binding (built with the library); raise if it is missing."""
+    global _marshal
+    if _marshal is None:
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise ImportError("paper_2602_08329_b200/_marshal.so is missing or does not fit this torch: run "
+                              "`python -m paper_2602_08329_b200.build`") from e
+        _marshal = m
+    return _marshal
 
 
 def load() -> C.CDLL:
@@ -183,18 +197,11 @@ def make_schedule(top_k, window, sinks, refresh_interval=1, layer_group=1, dilat
 
 def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
     """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128]."""
-    shape, stride = k.shape, k.stride()
-    assert k.dtype is _BF16 and v.dtype is _BF16 and shape[-1] == 128
-    assert stride == v.stride() and stride[-1] == 1 and stride[-2] == 128
-    assert seq_lens.dtype is _I32
-    if page_table is None:
-        table, table_stride, pages = 0, 0, 0
-    else:
-        table, table_stride, pages = _ptr(page_table), page_table.stride(0), shape[0]
-    view = KvView.from_buffer_copy(_KV_PACK(k.data_ptr(), v.data_ptr(), stride[0], stride[1], table, table_stride,
-                                            seq_lens.data_ptr(), max_seq_len, pages))
+    kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, cap, dev = \
+        (_marshal or _load_marshal()).kv_view(k, v, seq_lens, page_table)
+    view = KvView.from_buffer_copy(_KV_PACK(kp, vp, so, sh, table, table_stride, lens, max_seq_len, pages))
     view._keep = (k, v, seq_lens, page_table)
-    view._batch, view._heads, view._cap, view._dev = seq_lens.shape[0], shape[1], 0 if pages else shape[2], k.get_device()
+    view._batch, view._heads, view._cap, view._dev = batch, heads, cap, dev
     return view
 
 
@@ -205,53 +212,25 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
     fp32 scales [B][Hkv][cap/16]; or paged [pool][Hkv][16][128] with scales [pool][Hkv].  Tails bf16
     [B][Hkv][16][128].
     """
-    fmt = _BYTEKV_FORMATS[k.dtype]
-    shape, stride, sshape, sstride = k.shape, k.stride(), k_scale.shape, k_scale.stride()
-    B, paged = seq_lens.shape[0], page_table is not None
-    assert v.dtype is k.dtype and v.shape == shape and v.stride() == stride and len(shape) == 4
-    assert shape[3] == 128 and stride[2:] == (128, 1) and shape[2] % 16 == 0
-    assert k_scale.dtype is _F32 and v_scale.dtype is _F32 and v_scale.shape == sshape and v_scale.stride() == sstride
-    assert k_tail.dtype is _BF16 and v_tail.dtype is _BF16 and k_tail.shape == v_tail.shape
-    assert k_tail.shape[1:] == (shape[1], 16, 128) and k_tail.shape[0] >= B
-    assert k_tail.is_contiguous() and v_tail.is_contiguous() and seq_lens.dtype is _I32 and seq_lens.is_contiguous()
-    if paged:
-        assert shape[2] == 16 and sshape == shape[:2] and page_table.dtype is _I32
-        assert page_table.stride(1) == 1 and page_table.shape[0] >= B
-        tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table)
-        table, table_stride, pages = page_table.data_ptr(), page_table.stride(0), shape[0]
-    else:
-        assert sshape == (shape[0], shape[1], shape[2] // 16) and sstride[2] == 1 and shape[0] >= B and max_seq_len <= shape[2]
-        tensors = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens)
-        table, table_stride, pages = 0, 0, 0
-    dev = _same_device(*tensors)
-    view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(
-        k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(), stride[0],
-        stride[1], sstride[0], sstride[1], table, seq_lens.data_ptr(), table_stride, max_seq_len, pages, fmt))
-    view._keep = tensors
-    view._batch, view._heads, view._cap, view._dev = B, shape[1], 0 if paged else shape[2], dev
+    (kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride, pages, fmt, batch, heads, cap, dev) = \
+        (_marshal or _load_marshal()).bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table, max_seq_len)
+    view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride,
+                                                    max_seq_len, pages, fmt))
+    view._keep = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table)
+    view._batch, view._heads, view._cap, view._dev = batch, heads, cap, dev
     return view
 
 
 def make_block_bounds(codes, scale) -> BlockBoundsView:
     """Bounds int8 [B][Hkv][blocks][2][128] with scales fp32 [B][Hkv][blocks], or per page [pool][Hkv][2][128], [pool][Hkv]."""
-    shape, stride = codes.shape, scale.stride()
-    assert codes.dtype is torch.int8 and scale.dtype is _F32 and shape[-2:] == (2, 128)
-    assert shape[:-2] == scale.shape and codes.is_contiguous() and scale.is_contiguous()
-    view = BlockBoundsView(codes.data_ptr(), scale.data_ptr(), stride[0], stride[1])
-    view._keep, view._shape, view._dev = (codes, scale), shape, _same_device(codes, scale)
+    cp, sp, so, sh, outer, heads, blocks, dev = (_marshal or _load_marshal()).bounds_view(codes, scale)
+    view = BlockBoundsView(cp, sp, so, sh)
+    view._keep, view._outer, view._heads, view._blocks, view._dev = (codes, scale), outer, heads, blocks, dev
     return view
 
 
 def make_block_schedule(top_blocks, sink_blocks=1, recent_blocks=1, flags=0) -> BlockSchedule:
     return BlockSchedule(top_blocks, sink_blocks, recent_blocks, flags)
-
-
-def _same_device(*tensors) -> int:
-    dev = tensors[0].get_device()
-    assert dev >= 0, "tensors of a call must be on a CUDA device"
-    for t in tensors:
-        assert t.get_device() == dev, "tensors of a call must be on one CUDA device"
-    return dev
 
 
 class Context:
@@ -261,6 +240,7 @@ class Context:
                  max_window, max_sinks, max_dilate_r=1, max_dilate_m=-1, page_size=0,
                  min_layer_group=1, head_dim=128, max_block_sets=1, flags=0):
         self.lib = load()
+        _load_marshal()
         self.cfg = Config(num_layers, max_batch, num_q_heads, num_kv_heads, head_dim, max_context,
                           page_size, max_k, max_window, max_sinks, max_dilate_r, max_dilate_m,
                           min_layer_group, max_block_sets, flags)
@@ -342,31 +322,24 @@ class Context:
     # -- the 8-bit cache
     def bytekv_append(self, new_k, new_v, new_lens, view, batch, max_new=0, stream=None):
         """Append new_k / new_v (bf16 [B][Hkv][rows][128], any strides over the first three axes)."""
-        shape, (s0, s1, s2, s3) = new_k.shape, new_k.stride()
-        n0, n1, rows, d = shape
-        assert new_k.dtype is _BF16 and new_v.dtype is _BF16 and new_v.shape == shape and new_v.stride() == (s0, s1, s2, s3)
-        assert n0 >= batch and n1 == self._hkv and d == 128 and s3 == 1 and 0 <= max_new <= rows
-        assert new_lens.dtype is _I32 and new_lens.shape[0] >= batch and new_lens.is_contiguous()
-        assert new_k.get_device() == new_v.get_device() == new_lens.get_device() == view._dev
         self._fit(view, batch)
-        # the stride of an axis of one element is arbitrary
-        rc = self.lib.prhs_bytekv_append(self.h, C.byref(view), new_k.data_ptr(), new_v.data_ptr(), s0 if n0 > 1 else 0,
-                                         s1 if n1 > 1 else 0, s2 if rows > 1 else 0, new_lens.data_ptr(), max_new or rows, batch,
-                                         _stream(stream))
+        k, v, lens, s0, s1, s2, rows = _marshal.rows(new_k, new_v, new_lens, batch, self._hkv, view._dev, max_new)
+        rc = self.lib.prhs_bytekv_append(self.h, C.byref(view), k, v, s0, s1, s2, lens, max_new or rows, batch, _stream(stream))
         if rc:
             self._ck(rc)
 
     def bytekv_decode_attn(self, q, view, batch, out, out_lse=None, stream=None):
-        lse = self._check_io(q, batch, out, out_lse, view)
-        rc = self.lib.prhs_bytekv_decode_attn(self.h, q.data_ptr(), C.byref(view), batch, out.data_ptr(), lse, _stream(stream))
+        self._fit(view, batch)
+        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
+        rc = self.lib.prhs_bytekv_decode_attn(self.h, q, C.byref(view), batch, out, lse, _stream(stream))
         if rc:
             self._ck(rc)
 
     def bytekv_sparse_decode_attn(self, q, view, idx, count, batch, out, out_lse=None, stream=None):
-        lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(view._dev, idx, count, batch, self._hq)
-        rc = self.lib.prhs_bytekv_sparse_decode_attn(self.h, q.data_ptr(), C.byref(view), idx.data_ptr(), count.data_ptr(), stride,
-                                                     batch, out.data_ptr(), lse, _stream(stream))
+        self._fit(view, batch)
+        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
+        idx, count, stride = _marshal.lists(idx, count, batch, self._hq, view._dev)
+        rc = self.lib.prhs_bytekv_sparse_decode_attn(self.h, q, C.byref(view), idx, count, stride, batch, out, lse, _stream(stream))
         if rc:
             self._ck(rc)
 
@@ -375,35 +348,35 @@ class Context:
         self._fit_bounds(view, bounds, batch)
         at = None
         if first is not None:
-            assert first.dtype is _I32 and first.shape[0] >= batch and first.is_contiguous() and first.get_device() == view._dev
+            assert first.dtype is torch.int32 and first.shape[0] >= batch and first.is_contiguous() and first.get_device() == view._dev
             at = first.data_ptr()
         rc = self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), at, max_new, batch, _stream(stream))
         if rc:
             self._ck(rc)
 
     def block_topk(self, q, view, bounds, sched, batch, out_blocks, out_count, stream=None):
-        assert q.dtype is _BF16 and q.shape == (batch, self._hq, 128) and q.is_contiguous() and q.get_device() == view._dev
-        stride = self._check_lists(view._dev, out_blocks, out_count, batch, self._block_units(sched.flags))
         self._fit_bounds(view, bounds, batch)
-        rc = self.lib.prhs_block_topk(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                      out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream))
+        q, _, _ = _marshal.io(q, None, None, batch, self._hq, view._dev)
+        blocks, count, stride = _marshal.lists(out_blocks, out_count, batch, self._block_units(sched.flags), view._dev)
+        rc = self.lib.prhs_block_topk(self.h, q, C.byref(view), C.byref(bounds), C.byref(sched), batch, blocks, stride, count,
+                                      _stream(stream))
         if rc:
             self._ck(rc)
 
     def block_decode_attn(self, q, view, blocks, count, batch, out, out_lse=None, flags=0, stream=None):
-        lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(view._dev, blocks, count, batch, self._block_units(flags))
-        rc = self.lib.prhs_block_decode_attn(self.h, q.data_ptr(), C.byref(view), blocks.data_ptr(), count.data_ptr(), stride, flags,
-                                             batch, out.data_ptr(), lse, _stream(stream))
+        self._fit(view, batch)
+        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
+        blocks, count, stride = _marshal.lists(blocks, count, batch, self._block_units(flags), view._dev)
+        rc = self.lib.prhs_block_decode_attn(self.h, q, C.byref(view), blocks, count, stride, flags, batch, out, lse, _stream(stream))
         if rc:
             self._ck(rc)
 
     def block_decode_step(self, q, view, bounds, sched, batch, out, out_lse, out_blocks, out_count, stream=None):
-        lse = self._check_io(q, batch, out, out_lse, view)
-        stride = self._check_lists(view._dev, out_blocks, out_count, batch, self._block_units(sched.flags))
         self._fit_bounds(view, bounds, batch)
-        rc = self.lib.prhs_block_decode_step(self.h, q.data_ptr(), C.byref(view), C.byref(bounds), C.byref(sched), batch,
-                                             out.data_ptr(), lse, out_blocks.data_ptr(), stride, out_count.data_ptr(), _stream(stream))
+        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
+        blocks, count, stride = _marshal.lists(out_blocks, out_count, batch, self._block_units(sched.flags), view._dev)
+        rc = self.lib.prhs_block_decode_step(self.h, q, C.byref(view), C.byref(bounds), C.byref(sched), batch, out, lse, blocks, stride,
+                                             count, _stream(stream))
         if rc:
             self._ck(rc)
 
@@ -419,32 +392,14 @@ class Context:
 
     def _fit_bounds(self, view, bounds, batch):
         self._fit(view, batch)
-        shape = bounds._shape
-        assert shape[1] == view._heads and bounds._dev == view._dev
+        assert bounds._heads == view._heads and bounds._dev == view._dev
         if view._cap:
-            assert len(shape) == 5 and shape[0] >= batch and shape[2] * 16 >= (view.max_seq_len or self._max_context)
+            assert bounds._blocks * 16 >= (view.max_seq_len or self._max_context) and bounds._outer >= batch
         else:
-            assert len(shape) == 4 and shape[0] >= view.num_pages
+            assert bounds._blocks == 0 and bounds._outer >= view.num_pages
 
     def _block_units(self, flags):
         return self._hkv if flags & PRHS_GROUP_SETS else self._hq
-
-    def _check_io(self, q, batch, out, out_lse, view):
-        """Shapes, types and devices of a decode attention's tensors; the address of out_lse or None."""
-        self._fit(view, batch)
-        shape, dev = q.shape, view._dev
-        assert shape == (batch, self._hq, 128) and out.shape == shape and q.dtype is _BF16 and out.dtype is _BF16
-        assert q.is_contiguous() and out.is_contiguous() and q.get_device() == dev and out.get_device() == dev
-        if out_lse is None:
-            return None
-        assert out_lse.dtype is _F32 and out_lse.shape == shape[:2] and out_lse.is_contiguous() and out_lse.get_device() == dev
-        return out_lse.data_ptr()
-
-    def _check_lists(self, dev, lists, count, batch, units):
-        b, u, stride = lists.shape
-        assert b == batch and u == units and lists.dtype is _I32 and count.dtype is _I32 and count.shape == (batch, units)
-        assert lists.is_contiguous() and count.is_contiguous() and lists.get_device() == dev and count.get_device() == dev
-        return stride
 
     def get_index_set(self, batch, stream=None):
         hq, cap = self.cfg.num_q_heads, self.index_capacity
