@@ -23,6 +23,8 @@ prhs_status check_bounds(prhs_ctx* ctx, const prhs_block_bounds_view* bv, Bounds
   if ((uintptr_t)bv->codes % 16 || (uintptr_t)bv->scale % 4)
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: codes must be 16-byte aligned, scales 4-byte aligned");
   if (bv->stride_outer <= 0 || bv->stride_head <= 0) return fail(ctx, PRHS_ERR_INVALID_ARG, "block bounds: strides must be positive");
+  if (bv->stride_outer > 0x7fffffffll || bv->stride_head > 0x7fffffffll)
+    return fail(ctx, PRHS_ERR_UNSUPPORTED, "block bounds: strides above 2^31 blocks");
   out->codes = bv->codes;
   out->scale = bv->scale;
   out->stride_outer = bv->stride_outer;
@@ -81,6 +83,8 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   sp.q = static_cast<const __nv_bfloat16*>(q);
   sp.kv = kv;
   sp.bd = bd;
+  sp.bounds_outer = (int)bd.stride_outer;
+  sp.bounds_head = (int)bd.stride_head;
   sp.scores = c->scores;
   sp.ld = c->ld;
   sp.batch = batch;

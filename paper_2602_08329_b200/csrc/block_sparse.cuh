@@ -125,6 +125,7 @@ struct BlockScoreParams {
   const __nv_bfloat16* q;   // [B][Hq][128]
   KvDev kv;
   BoundsDev bd;
+  int bounds_outer, bounds_head;   // bd's strides: a bounds index (256 bytes) fits 31 bits on any device
   float* scores;            // [B][Hq][ld]; group_max: the row of the group's first head
   int ld, batch, num_q_heads, group_size, group_max;
   int update_last;          // 1: the bounds of the last block are recomputed here (its score is not used)
@@ -133,8 +134,7 @@ struct BlockScoreParams {
 };
 
 __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -204,30 +204,43 @@ __global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score
       return (paged && r < rounds && blk < nb) ? __ldg(ptab + blk) : 0;
     };
     int pg_next = page_of(0);
+    const int outer = p.bounds_outer, unit_at = (paged ? 0 : b * outer) + kvh * p.bounds_head;       // bounds indexes
+    // a lane copies chunk lane % 16 of every other block of the group; the swizzle depends on the block's parity
+    const int c = lane & 15, half = lane >> 4;
+    const uint32_t dst_lane = half * kBoundsBytes + ((c ^ (half << 2)) << 4);
+    const int8_t* const src_lane = p.bd.codes + c * 16;
     auto issue = [&](int r) {
       if (r < rounds) {
         const int blk0 = (g_lo + warp + kScoreWarps * r) * kScoreRound;
-        int at = -1;                                     // bounds index of block lane & 15
-        if (blk0 + (lane & 15) < nb) {
-          if (!paged) {
-            at = (int)(b * p.bd.stride_outer + kvh * p.bd.stride_head) + blk0 + (lane & 15);
-          } else if ((unsigned)pg_next < (unsigned)p.kv.num_pages) {
-            at = (int)(pg_next * p.bd.stride_outer + kvh * p.bd.stride_head);
-          } else {
-            atomicOr(p.flags, kFlagBadPage);
-          }
-        }
-        pg_next = page_of(r + 1);
         const uint32_t slot = ring + (uint32_t)(r % kScoreStages) * kScoreStageBytes;
-        const int c = lane & 15;
+        if (!paged && blk0 + kScoreRound <= nb) {        // 4 KB in a row
+          const int8_t* src = src_lane + (long long)(unit_at + blk0 + half) * kBoundsBytes;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int row = 2 * i + (lane >> 4);
-          const int from = __shfl_sync(0xffffffffu, at, row);
-          cp_async_16(slot + row * kBoundsBytes + ((c ^ ((row & 1) << 2)) << 4), p.bd.codes + (long long)max(from, 0) * kBoundsBytes + c * 16,
-                      from >= 0 ? 16 : 0);
+          for (int i = 0; i < 8; ++i) cp_async_16_full(slot + dst_lane + i * (2 * kBoundsBytes), src + i * (2 * kBoundsBytes));
+          if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + unit_at + blk0 + lane, 4);
+        } else {
+          int at = -1;                                   // bounds index of block lane % 16
+          if (blk0 + c < nb) {
+            if (!paged) at = unit_at + blk0 + c;
+            else if ((unsigned)pg_next < (unsigned)p.kv.num_pages) at = pg_next * outer + unit_at;
+            else atomicOr(p.flags, kFlagBadPage);
+          }
+          pg_next = page_of(r + 1);
+          const bool all = __all_sync(0xffffffffu, at >= 0);
+          if (all) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              cp_async_16_full(slot + dst_lane + i * (2 * kBoundsBytes),
+                               src_lane + (long long)__shfl_sync(0xffffffffu, at, 2 * i + half) * kBoundsBytes);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int from = __shfl_sync(0xffffffffu, at, 2 * i + half);
+              cp_async_16(slot + dst_lane + i * (2 * kBoundsBytes), src_lane + (long long)max(from, 0) * kBoundsBytes, from >= 0 ? 16 : 0);
+            }
+          }
+          if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + max(at, 0), at >= 0 ? 4 : 0);
         }
-        if (lane < 16) cp_async_4(slot + kScoreRound * kBoundsBytes + lane * 4, p.bd.scale + max(at, 0), at >= 0 ? 4 : 0);
       }
       cp_async_commit();
     };
@@ -275,18 +288,25 @@ __global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score
       issue(r + kScoreStages - 1);
       const unsigned char* slot = g_smem + (warp * kScoreStages + r % kScoreStages) * kScoreStageBytes;
       const float* scales = reinterpret_cast<const float*>(slot + kScoreRound * kBoundsBytes);
+      // four chains of four MMAs: two tiles of eight blocks, minima and maxima apart
+      int d[2][2][4] = {};
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const int c = 2 * part + i;
+            const uint4 x = *reinterpret_cast<const uint4*>(slot + (8 * n + g) * kBoundsBytes + (((4 * c + tg) ^ ((g & 1) << 2)) << 4));
+            mma_s8(d[n][part], q0[c].x, q1[c].x, q0[c].y, q1[c].y, x.x, x.y);
+            mma_s8(d[n][part], q0[c].z, q1[c].z, q0[c].w, q1[c].w, x.z, x.w);
+          }
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
-        int d[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 x = *reinterpret_cast<const uint4*>(slot + (8 * n + g) * kBoundsBytes + (((4 * i + tg) ^ ((g & 1) << 2)) << 4));
-          mma_s8(d, q0[i].x, q1[i].x, q0[i].y, q1[i].y, x.x, x.y);
-          mma_s8(d, q0[i].z, q1[i].z, q0[i].w, q1[i].w, x.z, x.w);
-        }
         const int blk = (g_lo + warp + kScoreWarps * r) * kScoreRound + 8 * n + 2 * tg;
         const float2 s = *reinterpret_cast<const float2*>(scales + 8 * n + 2 * tg);
-        float v[4] = {(float)d[0] * s.x * qs0, (float)d[1] * s.y * qs0, (float)d[2] * s.x * qs1, (float)d[3] * s.y * qs1};
+        auto sum = [&](int j) { return (float)(d[n][0][j] + d[n][1][j]); };
+        float v[4] = {sum(0) * s.x * qs0, sum(1) * s.y * qs0, sum(2) * s.x * qs1, sum(3) * s.y * qs1};
         if (p.group_max) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
