@@ -1,0 +1,151 @@
+"""The calls of the 8-bit cache and of block selection without a GPU: layouts, refusals, and the 64-bit forms' own pins."""
+import ctypes as C
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_08329_b200 import binding as P
+from paper_2602_08329_b200 import build as B
+from tests import cache_ref as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    B.build()
+    return P.load()
+
+
+# ------------------------------------------------------------------------------- layouts
+def struct_fields(name):
+    """Field names of a struct of the header, in order."""
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "prhs.h")).read(), flags=re.S)
+    body = next(b for b, n in re.findall(r"typedef struct \{([^}]*)\}\s*(\w+);", text) if n == name)
+    names = []
+    for decl in body.split(";"):
+        names += [re.sub(r".*[\s*]", "", part.strip()) for part in decl.split(",") if part.strip()]
+    return names
+
+
+@pytest.mark.parametrize("name,mirror,size", [("prhs_bytekv_view", P.ByteKvView, 112), ("prhs_block_bounds_view", P.BlockBoundsView, 32),
+                                              ("prhs_block_schedule", P.BlockSchedule, 16)])
+def test_structs_mirror_the_header(name, mirror, size):
+    assert [f for f, _ in mirror._fields_] == struct_fields(name) and C.sizeof(mirror) == size
+
+
+def test_packed_views_have_the_struct_layout():
+    view = P.ByteKvView.from_buffer_copy(P._BYTEKV_PACK(*range(1, 17)))
+    assert [getattr(view, f) for f, _ in P.ByteKvView._fields_] == list(range(1, 17))
+    view = P.KvView.from_buffer_copy(P._KV_PACK(*range(1, 10)))
+    assert [getattr(view, f) for f, _ in P.KvView._fields_] == list(range(1, 10))
+
+
+def test_header_formats_match():
+    text = open(os.path.join(ROOT, "include", "prhs.h")).read()
+    for name in ("PRHS_BYTEKV_E4M3", "PRHS_BYTEKV_E5M2"):
+        assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(P, name)
+
+
+# ------------------------------------------------------------------------------- refusals
+def test_null_context_is_refused(lib):
+    kv, bounds, view = P.ByteKvView(), P.BlockBoundsView(), P.KvView()
+    sched = P.make_block_schedule(1)
+    assert lib.prhs_bytekv_append(None, C.byref(kv), None, None, 0, 0, 0, None, 1, 1, None) == 1
+    assert lib.prhs_bytekv_decode_attn(None, None, C.byref(kv), 1, None, None, None) == 1
+    assert lib.prhs_bytekv_sparse_decode_attn(None, None, C.byref(kv), None, None, 1, 1, None, None, None) == 1
+    assert lib.prhs_block_bounds(None, C.byref(view), C.byref(bounds), None, 0, 1, None) == 1
+    assert lib.prhs_block_topk(None, None, C.byref(view), C.byref(bounds), C.byref(sched), 1, None, 1, None, None) == 1
+    assert lib.prhs_block_decode_attn(None, None, C.byref(view), None, None, 1, 0, 1, None, None, None) == 1
+    assert lib.prhs_block_decode_step(None, None, C.byref(view), C.byref(bounds), C.byref(sched), 1, None, None, None, 1, None, None) == 1
+
+
+def test_host_tensors_and_wrong_types_are_refused(lib):
+    k = torch.zeros(2, 3, 32, 128, dtype=torch.float8_e4m3fn)
+    s = torch.zeros(2, 3, 2)
+    t = torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16)
+    lens = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(AssertionError, match="CUDA"):
+        P.make_bytekv_view(k, k, s, s, t, t, lens)
+    with pytest.raises(AssertionError, match="float8"):
+        P.make_bytekv_view(t, t, s, s, t, t, lens)
+    with pytest.raises(AssertionError):
+        P.make_bytekv_view(k, None, s, s, t, t, lens)
+    with pytest.raises(AssertionError, match="CUDA"):
+        P.make_block_bounds(torch.zeros(2, 3, 4, 2, 128, dtype=torch.int8), torch.zeros(2, 3, 4))
+    with pytest.raises(AssertionError):
+        P.make_view(t.float(), t.float(), lens)
+    m = P._load_marshal()
+    with pytest.raises(AssertionError):
+        m.io(t, None, None, 2, 3, 0)
+    with pytest.raises(AssertionError):
+        m.lists(lens, lens, 2, 3, 0)
+    with pytest.raises(AssertionError):
+        m.rows(t, t, lens, 2, 3, 0, 0)
+    N = None
+    for f, args in ((m.kv_view, (N, N, N, N)), (m.bytekv_view, (N,) * 8 + (0,)), (m.bounds_view, (N, N)), (m.rows, (N, N, N, 1, 1, 0, 0)),
+                    (m.io, (N, N, N, 1, 1, 0)), (m.lists, (N, N, 1, 1, 0))):
+        with pytest.raises(AssertionError):
+            f(*args)
+        with pytest.raises(TypeError):
+            f(*args[:-1])
+
+
+# --------------------------------------------------------------------- the 64-bit forms' pins
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)])
+def test_codes_are_torchs_rounding(fmt, dtype):
+    g = torch.Generator().manual_seed(1)
+    top = R.TOP[fmt][0]
+    x = (torch.rand(20000, generator=g) * 2 - 1) * top * torch.exp2(-torch.randint(0, 24, (20000,), generator=g).float())
+    x = torch.cat([x, torch.tensor([0.0, top, -top])])
+    assert np.array_equal(R.round_code(x.double().numpy(), fmt), x.to(dtype).double().numpy())
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_scales(fmt):
+    top = R.TOP[fmt][0]
+    assert float(R.scale_of(top, top)) == 1.0 and float(R.scale_of(np.nextafter(top, 1e9), top)) == 2.0
+    assert float(R.scale_of(top / 2, top)) == 0.5 and float(R.scale_of(0.0, top)) == 2.0 ** -126
+    assert float(R.scale_of(1e-40, top)) == 2.0 ** -126
+    rng = np.random.default_rng(0)
+    rows = rng.standard_normal((16, 128)) * np.exp2(rng.integers(-6, 6, (16, 1)))
+    codes, s = R.quantise(rows, fmt)
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(rows / s), 2.0 ** R.TOP[fmt][2]))) - R.TOP[fmt][1])
+    assert np.all(np.abs(codes * s - rows) <= s * step / 2) and np.abs(codes).max() <= top
+
+
+def test_scores_bound_every_key_inside_the_coded_box():
+    rng = np.random.default_rng(3)
+    for _ in range(20):
+        rows = rng.standard_normal((rng.integers(1, 17), 128)) * 2
+        codes, s = R.block_bounds(rows)
+        q = rng.standard_normal(128)
+        q8, qs = R.query_codes(q)
+        score = R.block_scores(q, codes[None], np.array([s]))[0]
+        inside = codes[0] + (codes[1].astype(int) - codes[0]) * rng.random((50, 128))
+        assert np.all(inside * s @ (q8 * qs) <= score * (1 + 1e-12) + 1e-9)
+        # a key is at most half a code outside its box, a query at most half a code off
+        off = 0.5 * s * np.abs(q8 * qs).sum() + 0.5 * qs * np.abs(rows).sum(-1).max()
+        assert (rows @ q).max() <= score + off
+
+
+def test_selection_takes_the_best_and_the_lowest_of_equals():
+    score = np.array([5.0, 1.0, 3.0, 3.0, 3.0, 9.0, 0.0, 3.0])
+    assert R.select_blocks(score, 8, 2, 1, 1) == [0, 2, 5, 7]
+    assert R.select_blocks(score, 8, 3, 0, 0) == [0, 2, 5]
+    assert R.select_blocks(score, 8, 100, 2, 2) == list(range(8))
+    assert R.select_blocks(score[:1], 1, 5, 3, 3) == [0] and R.select_blocks(score[:0], 0, 5, 3, 3) == []
+
+
+def test_attention_bounds_cover_a_bf16_emulation():
+    # weights rounded to bf16, result rounded to bf16: the error stays inside the stated bound
+    g = torch.Generator().manual_seed(2)
+    q, k, v = torch.randn(128, generator=g), torch.randn(300, 128, generator=g), torch.randn(300, 128, generator=g)
+    y, lse, tol, ltol = R.attend(q.numpy(), k.numpy(), v.numpy(), True)
+    a = (k @ q) * R.S
+    p = torch.exp(a - a.max()).to(torch.bfloat16).float()
+    got = ((p @ v) / p.sum()).to(torch.bfloat16).double().numpy()
+    assert np.all(np.abs(got - y) <= tol) and abs(float(torch.logsumexp(a, 0)) - lse) <= ltol
