@@ -350,7 +350,8 @@ typedef struct {
 
 /* Append rows to the 8-bit cache: positions [t_b - new_lens[b], t_b) of every sequence, a prompt, a chunk or a
  * token.  Blocks that become whole are quantised (the rows they already had come from the tail), rows of the
- * block that stays open go to the tail; nothing else is written.
+ * block that stays open go to the tail; nothing else is written.  A sequence may be cut back (a smaller t_b in
+ * the next call) to a multiple of 16 or within its open block; rows of a whole block are no longer in the tail.
  *   new_k, new_v  device bf16; row j of (b, kvh) at  b*stride_seq + kvh*stride_head + j*stride_row  (elements),
  *                 16-byte aligned, strides multiples of 8
  *   new_lens      device int32 [batch], 0 <= new_lens[b] <= min(max_new, t_b); a sequence that breaks this, or whose

@@ -210,6 +210,7 @@ prhs_status prhs_block_bounds(prhs_ctx* ctx, const prhs_kv_view* kv, const prhs_
   p.first = first;
   p.batch = batch;
   p.num_kv_heads = ctx->cfg.num_kv_heads;
+  p.max_new = most;
   p.blocks_max = most == 1 ? 1 : std::min((most + 2 * (kBlockRows - 1)) / kBlockRows, (max_t + kBlockRows - 1) / kBlockRows);
   p.max_len = max_t;
   p.flags = ctx->flags;

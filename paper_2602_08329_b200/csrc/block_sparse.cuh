@@ -93,7 +93,8 @@ struct BoundsParams {
   KvDev kv;
   BoundsDev bd;
   const int* first;         // [B] or nullptr (0): bounds of the blocks that hold positions [first, t)
-  int batch, num_kv_heads, blocks_max, max_len;     // blocks_max: blocks any sequence touches at most
+  int batch, num_kv_heads, max_len;
+  int max_new, blocks_max;  // positions [first, t) of any sequence at most, and the blocks they can touch
   uint32_t* flags;
 };
 
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(BoundsParams p) {
   const int kvh = (int)(bh % p.num_kv_heads), b = (int)(bh / p.num_kv_heads);
   const int t = __ldg(p.kv.seq_lens + b);
   const int f = p.first ? __ldg(p.first + b) : 0;
-  if (f < 0 || f > t || t > p.max_len || (t - f + kBlockRows - 1) / kBlockRows > p.blocks_max) {
+  if (f < 0 || f > t || t > p.max_len || t - f > p.max_new) {
     if ((threadIdx.x & 31) == 0) atomicOr(p.flags, kFlagBadLength);
     return;
   }

@@ -146,6 +146,11 @@ def test_bounds_refuse_contradictory_lengths(cuda_device):
     with pytest.raises(P.PrhsError):
         ctx.check()
     assert bool((cache.scale[:2] == 99.0).all()) and cache.scale[2, 0].tolist()[:2] == [99.0, 99.0] and float(cache.scale[2, 0, 2]) != 99.0
+    cache.scale.fill_(99.0)
+    ctx.block_bounds(cache.view(), cache.bounds(), 3, first=torch.tensor([8, 37, 38], dtype=torch.int32, device=cuda_device), max_new=2)
+    with pytest.raises(P.PrhsError):           # 32 and 3 new positions where two were announced
+        ctx.check()
+    assert bool((cache.scale[:2] == 99.0).all()) and float(cache.scale[2, 0, 2]) != 99.0
     ctx.close()
 
 
@@ -359,9 +364,9 @@ def test_all_blocks_are_the_dense_attention(cuda_device):
     ctx.close()
 
 
-def test_long_context_selection(cuda_device):
-    # 2^18 positions: 16384 blocks; the selection's counts and the score grid over many CTAs
-    t = 1 << 18
+@pytest.mark.parametrize("t,top", [(40000, 300), (100001, 1000), (1 << 18, 1900), ((1 << 18) + 4003, 1900)])
+def test_long_context_selection(cuda_device, t, top):
+    # 2500, 6251 and 16384 blocks are selected from registers, 16635 from memory
     cache = Cache(1, 1, t, False, cuda_device)
     ctx = make_ctx(cache, 2)
     g = torch.Generator(device=cuda_device).manual_seed(3)
@@ -369,14 +374,89 @@ def test_long_context_selection(cuda_device):
     cache.v.copy_(torch.randn(cache.v.shape, generator=g, device=cuda_device))
     cache.lens.fill_(t)
     ctx.block_bounds(cache.view(), cache.bounds(), 1)
-    q = torch.randn(1, 2, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    q = torch.randn(1, 2, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    q[0, 1] = 0.0                                                        # the whole middle ties
+    q = q.to(cuda_device)
     blocks, count = torch.empty(1, 2, 2000, dtype=torch.int32, device=cuda_device), torch.empty(1, 2, dtype=torch.int32, device=cuda_device)
-    ctx.block_topk(q, cache.view(), cache.bounds(), P.make_block_schedule(1900, 1, 1), 1, blocks, count)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(top, 1, 1), 1, out, lse, blocks, count)
     assert ctx.check() == 0
     codes, scale = cache.codes[0, 0].cpu().numpy(), np64(cache.scale[0, 0])
     for u in range(2):
-        want = R.select_blocks(R.block_scores(np64(q[0, u]), codes, scale), t // 16, 1900, 1, 1)
+        want = R.select_blocks(R.block_scores(np64(q[0, u]), codes, scale), -(-t // 16), top, 1, 1)
         assert blocks[0, u].tolist()[: int(count[0, u])] == want
+        pos = torch.tensor([i for j in want for i in range(16 * j, min(16 * j + 16, t))], device=cuda_device)
+        y, l, tol, ltol = R.attend(np64(q[0, u]), np64(cache.k[0, 0, pos]), np64(cache.v[0, 0, pos]), True)
+        assert np.all(np.abs(np64(out[0, u]) - y) <= tol) and abs(float(lse[0, u]) - l) <= ltol
+    ctx.close()
+
+
+def test_offsets_beyond_32_bits(cuda_device):
+    # pages whose rows lie more than 2^32 elements behind the base
+    H, pool = 8, (1 << 32) // (8 * 16 * 128) + 40
+    k, v = (torch.empty(pool, H, 16, 128, dtype=torch.bfloat16, device=cuda_device) for _ in range(2))
+    codes, scale = torch.empty(pool, H, 2, 128, dtype=torch.int8, device=cuda_device), torch.empty(pool, H, device=cuda_device)
+    table_cpu = (torch.arange(40, dtype=torch.int32) + (pool - 40)).flip(0).view(1, 40)
+    t = 633
+    rows = random_rows(1, H, t, 21)
+    for w, x in enumerate((k, v)):
+        for j in range(40):
+            part = rows[w, 0, :, 16 * j: min(16 * j + 16, t)]
+            x[int(table_cpu[0, j]), :, : part.shape[1]] = part.to(cuda_device)
+    lens = torch.tensor([t], dtype=torch.int32, device=cuda_device)
+    view = P.make_view(k, v, lens, page_table=table_cpu.to(cuda_device))
+    bounds = P.make_block_bounds(codes, scale)
+    ctx = P.Context(1, 1, H, H, 640, 16, 16, 4, page_size=16)
+    ctx.block_bounds(view, bounds, 1)
+    q = torch.randn(1, H, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(cuda_device)
+    blocks, count = torch.empty(1, H, 12, dtype=torch.int32, device=cuda_device), torch.empty(1, H, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(1, H, device=cuda_device)
+    ctx.block_decode_step(q, view, bounds, P.make_block_schedule(10, 1, 1), 1, out, lse, blocks, count)
+    assert ctx.check() == 0
+    for h in range(H):
+        x = rows[0, 0, h].double().numpy()
+        ref = [R.block_bounds(x[16 * j: 16 * j + 16]) for j in range(40)]
+        want = R.select_blocks(R.block_scores(np64(q[0, h]), np.stack([c for c, _ in ref]), np.array([s for _, s in ref])), 40, 10, 1, 1)
+        assert blocks[0, h].tolist() == want
+        pos = [i for j in want for i in range(16 * j, min(16 * j + 16, t))]
+        y, l, tol, ltol = R.attend(np64(q[0, h]), x[pos], rows[1, 0, h].double().numpy()[pos], True)
+        assert np.all(np.abs(np64(out[0, h]) - y) <= tol) and abs(float(lse[0, h]) - l) <= ltol
+    ctx.close()
+
+
+def test_steps_on_another_stream_and_two_graphs_of_one_context(cuda_device):
+    cache = Cache(2, 2, 500, True, cuda_device)
+    ctx = make_ctx(cache, 2)
+    cache.place(random_rows(2, 2, 500, 8), [500, 77])
+    ctx.block_bounds(cache.view(), cache.bounds(), 2)
+    sched = P.make_block_schedule(6, 1, 2)
+    qs = [torch.randn(2, 4, 128, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).to(cuda_device) for i in range(2)]
+    new = lambda: (torch.empty_like(qs[0]), torch.empty(2, 4, device=cuda_device), torch.empty(2, 4, 9, dtype=torch.int32, device=cuda_device),  # noqa: E731
+                   torch.empty(2, 4, dtype=torch.int32, device=cuda_device))
+    want = [new(), new()]
+    for q, w in zip(qs, want):
+        ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, 2, *w)
+    torch.cuda.synchronize()
+    side, got = torch.cuda.Stream(), [new(), new()]
+    with torch.cuda.stream(side):
+        for q, w in zip(qs, got):
+            ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, 2, *w)
+    side.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+    graphs, got = [], [new(), new()]
+    for q, w in zip(qs, got):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, 2, *w)
+    for _ in range(3):
+        for w in got:
+            for x in w:
+                x.fill_(9)
+        for g in graphs:                                                   # one after the other on one stream
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+    assert ctx.check() == 0
     ctx.close()
 
 
