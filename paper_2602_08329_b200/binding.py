@@ -96,6 +96,9 @@ class BlockSchedule(C.Structure):
 
 _lib = None
 _marshal = None
+# the calls the compiled helper makes, in the order it takes their addresses
+_MARSHAL_CALLS = ("bytekv_append", "bytekv_decode_attn", "bytekv_sparse_decode_attn", "block_bounds", "block_topk",
+                  "block_decode_attn", "block_decode_step")
 
 
 def _load_marshal():
@@ -107,6 +110,8 @@ def _load_marshal():
         except ImportError as e:
             raise ImportError("paper_2602_08329_b200/_marshal.so is missing or does not fit this torch: run "
                               "`python -m paper_2602_08329_b200.build`") from e
+        lib = load()
+        m.bind(*(C.cast(getattr(lib, "prhs_" + name), C.c_void_p).value for name in _MARSHAL_CALLS))
         _marshal = m
     return _marshal
 
@@ -249,12 +254,12 @@ class Context:
         if rc != PRHS_OK:
             raise PrhsError(rc, self.lib.prhs_last_error(None).decode())
         self.h = h
-        self._hq, self._hkv, self._max_context = num_q_heads, num_kv_heads, max_context
+        self._h, self._hq, self._hkv, self._max_context = h.value, num_q_heads, num_kv_heads, max_context
 
     def close(self):
         if getattr(self, "h", None):
             self.lib.prhs_destroy(self.h)
-            self.h = None
+            self.h, self._h = None, 0
 
     def __del__(self):
         try:
@@ -323,60 +328,49 @@ class Context:
     def bytekv_append(self, new_k, new_v, new_lens, view, batch, max_new=0, stream=None):
         """Append new_k / new_v (bf16 [B][Hkv][rows][128], any strides over the first three axes)."""
         self._fit(view, batch)
-        k, v, lens, s0, s1, s2, rows = _marshal.rows(new_k, new_v, new_lens, batch, self._hkv, view._dev, max_new)
-        rc = self.lib.prhs_bytekv_append(self.h, C.byref(view), k, v, s0, s1, s2, lens, max_new or rows, batch, _stream(stream))
+        rc = _marshal.bytekv_append(self._h, C.addressof(view), new_k, new_v, new_lens, batch, self._hkv, view._dev, max_new,
+                                    _stream(stream))
         if rc:
             self._ck(rc)
 
     def bytekv_decode_attn(self, q, view, batch, out, out_lse=None, stream=None):
         self._fit(view, batch)
-        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
-        rc = self.lib.prhs_bytekv_decode_attn(self.h, q, C.byref(view), batch, out, lse, _stream(stream))
+        rc = _marshal.bytekv_decode_attn(self._h, C.addressof(view), q, out, out_lse, batch, self._hq, view._dev, _stream(stream))
         if rc:
             self._ck(rc)
 
     def bytekv_sparse_decode_attn(self, q, view, idx, count, batch, out, out_lse=None, stream=None):
         self._fit(view, batch)
-        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
-        idx, count, stride = _marshal.lists(idx, count, batch, self._hq, view._dev)
-        rc = self.lib.prhs_bytekv_sparse_decode_attn(self.h, q, C.byref(view), idx, count, stride, batch, out, lse, _stream(stream))
+        rc = _marshal.bytekv_sparse_decode_attn(self._h, C.addressof(view), q, out, out_lse, batch, self._hq, view._dev,
+                                                _stream(stream), idx, count)
         if rc:
             self._ck(rc)
 
     # -- attention over selected blocks
     def block_bounds(self, view, bounds, batch, first=None, max_new=0, stream=None):
         self._fit_bounds(view, bounds, batch)
-        at = None
-        if first is not None:
-            assert first.dtype is torch.int32 and first.shape[0] >= batch and first.is_contiguous() and first.get_device() == view._dev
-            at = first.data_ptr()
-        rc = self.lib.prhs_block_bounds(self.h, C.byref(view), C.byref(bounds), at, max_new, batch, _stream(stream))
+        rc = _marshal.block_bounds(self._h, C.addressof(view), C.addressof(bounds), first, max_new, batch, view._dev, _stream(stream))
         if rc:
             self._ck(rc)
 
     def block_topk(self, q, view, bounds, sched, batch, out_blocks, out_count, stream=None):
         self._fit_bounds(view, bounds, batch)
-        q, _, _ = _marshal.io(q, None, None, batch, self._hq, view._dev)
-        blocks, count, stride = _marshal.lists(out_blocks, out_count, batch, self._block_units(sched.flags), view._dev)
-        rc = self.lib.prhs_block_topk(self.h, q, C.byref(view), C.byref(bounds), C.byref(sched), batch, blocks, stride, count,
-                                      _stream(stream))
+        rc = _marshal.block_topk(self._h, C.addressof(view), C.addressof(bounds), C.addressof(sched), q, batch, self._hq,
+                                 self._block_units(sched.flags), view._dev, _stream(stream), out_blocks, out_count)
         if rc:
             self._ck(rc)
 
     def block_decode_attn(self, q, view, blocks, count, batch, out, out_lse=None, flags=0, stream=None):
         self._fit(view, batch)
-        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
-        blocks, count, stride = _marshal.lists(blocks, count, batch, self._block_units(flags), view._dev)
-        rc = self.lib.prhs_block_decode_attn(self.h, q, C.byref(view), blocks, count, stride, flags, batch, out, lse, _stream(stream))
+        rc = _marshal.block_decode_attn(self._h, C.addressof(view), q, out, out_lse, batch, self._hq, self._block_units(flags),
+                                        view._dev, _stream(stream), blocks, count, flags)
         if rc:
             self._ck(rc)
 
     def block_decode_step(self, q, view, bounds, sched, batch, out, out_lse, out_blocks, out_count, stream=None):
         self._fit_bounds(view, bounds, batch)
-        q, out, lse = _marshal.io(q, out, out_lse, batch, self._hq, view._dev)
-        blocks, count, stride = _marshal.lists(out_blocks, out_count, batch, self._block_units(sched.flags), view._dev)
-        rc = self.lib.prhs_block_decode_step(self.h, q, C.byref(view), C.byref(bounds), C.byref(sched), batch, out, lse, blocks, stride,
-                                             count, _stream(stream))
+        rc = _marshal.block_decode_step(self._h, C.addressof(view), C.addressof(bounds), C.addressof(sched), q, out, out_lse, batch,
+                                        self._hq, self._block_units(sched.flags), view._dev, _stream(stream), out_blocks, out_count)
         if rc:
             self._ck(rc)
 

@@ -33,7 +33,11 @@ def _older(target: str, inputs) -> bool:
 
 
 def stale() -> bool:
-    return _older(LIB, sources()) or _older(MARSHAL, [os.path.join(CSRC, "marshal.cpp")])
+    return _older(LIB, sources()) or _older(MARSHAL, marshal_sources())
+
+
+def marshal_sources():
+    return [os.path.join(CSRC, "marshal.cpp"), os.path.join(os.path.dirname(HERE), "include", "prhs.h")]
 
 
 def _run(cmd, what: str) -> str:
@@ -46,7 +50,7 @@ def _run(cmd, what: str) -> str:
 def build_marshal(force: bool = False) -> str:
     """The extension links the torch libraries that the process has loaded anyway (no search path is recorded)."""
     src = os.path.join(CSRC, "marshal.cpp")
-    if force or _older(MARSHAL, [src]):
+    if force or _older(MARSHAL, marshal_sources()):
         import torch
         root = os.path.dirname(torch.__file__)
         inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),

@@ -1,13 +1,16 @@
 // Python extension of the binding: what the calls of the library need to know of their tensors (addresses, strides) and
-// the checks that go with it, read from the tensors directly.  A small decode call is bound by the host; asking a
-// tensor for its type, shape, strides, device and address through its Python attributes costs a tenth of a
-// microsecond each, five to ten microseconds a call.  Argument marshalling only: no CUDA here.
+// the checks that go with it, read from the tensors directly, and the calls themselves.  A small decode call is
+// bound by the host; asking a tensor for its type, shape, strides, device and address through its Python
+// attributes costs a tenth of a microsecond each, five to ten microseconds a call, and ctypes another one.
+// Argument marshalling only: no CUDA here, and the library's entry points are handed in by bind().
 #include <Python.h>
 
 #include <ATen/ATen.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+
+#include "../../include/prhs.h"
 
 namespace {
 
@@ -103,55 +106,210 @@ PyObject* bounds_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   return Py_BuildValue("LLLLLLLL", address(*c), address(*s), s->stride(0), s->stride(1), c->size(0), c->size(1), d == 5 ? c->size(2) : 0, dev);
 }
 
-// rows(new_k, new_v, new_lens, batch, heads, device, max_new): addresses of k, v and lens, strides (sequence, head, row), rows
-PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+// ------------------------------------------------------------------------------------ calls
+// The entry points, in the order that bind() receives them.
+struct Entries {
+  decltype(&prhs_bytekv_append) bytekv_append;
+  decltype(&prhs_bytekv_decode_attn) bytekv_decode_attn;
+  decltype(&prhs_bytekv_sparse_decode_attn) bytekv_sparse_decode_attn;
+  decltype(&prhs_block_bounds) block_bounds;
+  decltype(&prhs_block_topk) block_topk;
+  decltype(&prhs_block_decode_attn) block_decode_attn;
+  decltype(&prhs_block_decode_step) block_decode_step;
+} entry{};
+static_assert(sizeof(Entries) == 7 * sizeof(void*), "bind() fills the entries in order");
+
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (!count_is(nargs, 7)) return nullptr;
-  const at::Tensor *k = tensor(a[0]), *v = tensor(a[1]), *n = tensor(a[2]);
-  REQUIRE(k && v && n, "a tensor is missing");
-  const int64_t batch = PyLong_AsLongLong(a[3]), heads = PyLong_AsLongLong(a[4]), dev = PyLong_AsLongLong(a[5]), max_new = PyLong_AsLongLong(a[6]);
+  for (int i = 0; i < 7; ++i) {
+    void* p = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+    reinterpret_cast<void**>(&entry)[i] = p;
+  }
+  Py_RETURN_NONE;
+}
+
+// Integer and address arguments (PyErr_Occurred() once one is neither).
+struct Args {
+  PyObject* const* a;
+  int64_t integer(int i) const { return PyLong_AsLongLong(a[i]); }
+  template <typename T>
+  T* pointer(int i) const { return static_cast<T*>(PyLong_AsVoidPtr(a[i])); }
+};
+// The call with the interpreter released, as ctypes makes it; the status as a Python integer.
+template <typename F>
+PyObject* status(F call) {
+  prhs_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call();
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// A decode attention's q, out and out_lse (Python None: absent).
+struct Io {
+  const void* q;
+  void* out;
+  float* lse;
+  // nullptr: the error is set
+  PyObject* read(PyObject* oq, PyObject* oo, PyObject* ol, int64_t batch, int64_t heads, int64_t dev) {
+    const at::Tensor *tq = tensor(oq), *to = none(oo) ? nullptr : tensor(oo), *tl = none(ol) ? nullptr : tensor(ol);
+    REQUIRE(tq && (to || none(oo)) && (tl || none(ol)), "a tensor is missing");
+    for (const at::Tensor* t : {tq, to})
+      REQUIRE(!t || (is(t, at::kBFloat16, dev) && t->dim() == 3 && t->size(0) == batch && t->size(1) == heads && t->size(2) == 128 && t->is_contiguous()),
+              "q and out are contiguous bf16 [batch][Hq][128] on the cache's device");
+    REQUIRE(!tl || (is(tl, at::kFloat, dev) && tl->dim() == 2 && tl->size(0) == batch && tl->size(1) == heads && tl->is_contiguous()),
+            "out_lse is contiguous fp32 [batch][Hq] on the cache's device");
+    q = tq->data_ptr();
+    out = to ? to->data_ptr() : nullptr;
+    lse = tl ? static_cast<float*>(tl->data_ptr()) : nullptr;
+    return Py_None;
+  }
+};
+// Lists of entries or blocks, with their counts.
+struct Lists {
+  int32_t *lists, *count;
+  int32_t stride;
+  PyObject* read(PyObject* ol, PyObject* oc, int64_t batch, int64_t units, int64_t dev) {
+    const at::Tensor *l = tensor(ol), *c = tensor(oc);
+    REQUIRE(l && c, "a tensor is missing");
+    REQUIRE(is(l, at::kInt, dev) && l->dim() == 3 && l->size(0) == batch && l->size(1) == units && l->is_contiguous() && l->size(2) <= INT32_MAX,
+            "lists are contiguous int32 [batch][units][stride] on the cache's device");
+    REQUIRE(is(c, at::kInt, dev) && c->dim() == 2 && c->size(0) == batch && c->size(1) == units && c->is_contiguous(),
+            "counts are contiguous int32 [batch][units] on the cache's device");
+    lists = static_cast<int32_t*>(l->data_ptr());
+    count = static_cast<int32_t*>(c->data_ptr());
+    stride = (int32_t)l->size(2);
+    return Py_None;
+  }
+};
+
+// bytekv_append(ctx, view, new_k, new_v, new_lens, batch, heads, device, max_new, stream)
+PyObject* bytekv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 10)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_bytekv_view* kv = v.pointer<prhs_bytekv_view>(1);
+  const int64_t batch = v.integer(5), heads = v.integer(6), dev = v.integer(7), max_new = v.integer(8);
+  void* stream = v.pointer<void>(9);
   if (PyErr_Occurred()) return nullptr;
-  REQUIRE(is(k, at::kBFloat16, dev) && is(v, at::kBFloat16, dev) && same_layout(*k, *v), "new rows are bf16 on the cache's device, k and v alike");
+  const at::Tensor *k = tensor(a[2]), *vv = tensor(a[3]), *n = tensor(a[4]);
+  REQUIRE(k && vv && n, "a tensor is missing");
+  REQUIRE(is(k, at::kBFloat16, dev) && is(vv, at::kBFloat16, dev) && same_layout(*k, *vv), "new rows are bf16 on the cache's device, k and v alike");
   REQUIRE(k->dim() == 4 && k->size(0) >= batch && k->size(1) == heads && k->size(3) == 128 && k->stride(3) == 1, "new rows are [batch][Hkv][rows][128]");
-  REQUIRE(is(n, at::kInt, dev) && n->dim() == 1 && n->size(0) >= batch && n->is_contiguous(), "new_lens is int32 [batch]");
-  REQUIRE(0 <= max_new && max_new <= k->size(2), "max_new is at most the number of rows given");
+  REQUIRE(is(n, at::kInt, dev) && n->dim() == 1 && n->size(0) >= batch && n->is_contiguous(), "new_lens is int32 [batch] on the cache's device");
+  REQUIRE(0 <= max_new && max_new <= k->size(2) && k->size(2) <= INT32_MAX, "max_new is at most the number of rows given");
   auto stride = [&](int i) { return k->size(i) > 1 ? k->stride(i) : 0; };     // that of an axis of one element is arbitrary
-  return Py_BuildValue("LLLLLLL", address(*k), address(*v), address(*n), stride(0), stride(1), stride(2), k->size(2));
+  return status([&] {
+    return entry.bytekv_append(ctx, kv, k->data_ptr(), vv->data_ptr(), stride(0), stride(1), stride(2), static_cast<const int32_t*>(n->data_ptr()),
+                               (int32_t)(max_new ? max_new : k->size(2)), (int32_t)batch, stream);
+  });
 }
 
-// io(q, out, out_lse | None, batch, heads, device): their addresses
-PyObject* io(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  if (!count_is(nargs, 6)) return nullptr;
-  const at::Tensor *q = tensor(a[0]), *out = none(a[1]) ? nullptr : tensor(a[1]), *lse = none(a[2]) ? nullptr : tensor(a[2]);
-  REQUIRE(q && (out || none(a[1])) && (lse || none(a[2])), "a tensor is missing");
-  const int64_t batch = PyLong_AsLongLong(a[3]), heads = PyLong_AsLongLong(a[4]), dev = PyLong_AsLongLong(a[5]);
+// bytekv_decode_attn(ctx, view, q, out, out_lse, batch, heads, device, stream)
+PyObject* bytekv_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 9)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_bytekv_view* kv = v.pointer<prhs_bytekv_view>(1);
+  const int64_t batch = v.integer(5), heads = v.integer(6), dev = v.integer(7);
+  void* stream = v.pointer<void>(8);
   if (PyErr_Occurred()) return nullptr;
-  for (const at::Tensor* t : {q, out})
-    REQUIRE(!t || (is(t, at::kBFloat16, dev) && t->dim() == 3 && t->size(0) == batch && t->size(1) == heads && t->size(2) == 128 && t->is_contiguous()),
-            "q and out are contiguous bf16 [batch][Hq][128] on the cache's device");
-  REQUIRE(!lse || (is(lse, at::kFloat, dev) && lse->dim() == 2 && lse->size(0) == batch && lse->size(1) == heads && lse->is_contiguous()),
-          "out_lse is contiguous fp32 [batch][Hq] on the cache's device");
-  return Py_BuildValue("LLL", address(*q), out ? address(*out) : 0, lse ? address(*lse) : 0);
+  Io io;
+  if (!io.read(a[2], a[3], a[4], batch, heads, dev)) return nullptr;
+  return status([&] { return entry.bytekv_decode_attn(ctx, io.q, kv, (int32_t)batch, io.out, io.lse, stream); });
 }
 
-// lists(lists, count, batch, units, device): their addresses and the lists' stride
-PyObject* lists(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  if (!count_is(nargs, 5)) return nullptr;
-  const at::Tensor *l = tensor(a[0]), *c = tensor(a[1]);
-  REQUIRE(l && c, "a tensor is missing");
-  const int64_t batch = PyLong_AsLongLong(a[2]), units = PyLong_AsLongLong(a[3]), dev = PyLong_AsLongLong(a[4]);
+// bytekv_sparse_decode_attn(ctx, view, q, out, out_lse, batch, heads, device, stream, idx, count)
+PyObject* bytekv_sparse_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 11)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_bytekv_view* kv = v.pointer<prhs_bytekv_view>(1);
+  const int64_t batch = v.integer(5), heads = v.integer(6), dev = v.integer(7);
+  void* stream = v.pointer<void>(8);
   if (PyErr_Occurred()) return nullptr;
-  REQUIRE(is(l, at::kInt, dev) && l->dim() == 3 && l->size(0) == batch && l->size(1) == units && l->is_contiguous(), "lists are contiguous int32 [batch][units][stride]");
-  REQUIRE(is(c, at::kInt, dev) && c->dim() == 2 && c->size(0) == batch && c->size(1) == units && c->is_contiguous(), "counts are contiguous int32 [batch][units]");
-  return Py_BuildValue("LLL", address(*l), address(*c), l->size(2));
+  Io io;
+  Lists l;
+  if (!io.read(a[2], a[3], a[4], batch, heads, dev) || !l.read(a[9], a[10], batch, heads, dev)) return nullptr;
+  return status([&] { return entry.bytekv_sparse_decode_attn(ctx, io.q, kv, l.lists, l.count, l.stride, (int32_t)batch, io.out, io.lse, stream); });
 }
 
-PyMethodDef methods[] = {{"kv_view", (PyCFunction)(void*)kv_view, METH_FASTCALL, nullptr},
-                         {"bytekv_view", (PyCFunction)(void*)bytekv_view, METH_FASTCALL, nullptr},
-                         {"bounds_view", (PyCFunction)(void*)bounds_view, METH_FASTCALL, nullptr},
-                         {"rows", (PyCFunction)(void*)rows, METH_FASTCALL, nullptr},
-                         {"io", (PyCFunction)(void*)io, METH_FASTCALL, nullptr},
-                         {"lists", (PyCFunction)(void*)lists, METH_FASTCALL, nullptr},
-                         {nullptr, nullptr, 0, nullptr}};
+// block_bounds(ctx, view, bounds, first | None, max_new, batch, device, stream)
+PyObject* block_bounds(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 8)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_kv_view* kv = v.pointer<prhs_kv_view>(1);
+  const prhs_block_bounds_view* bounds = v.pointer<prhs_block_bounds_view>(2);
+  const int64_t max_new = v.integer(4), batch = v.integer(5), dev = v.integer(6);
+  void* stream = v.pointer<void>(7);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* first = none(a[3]) ? nullptr : tensor(a[3]);
+  REQUIRE(first || none(a[3]), "a tensor is missing");
+  REQUIRE(!first || (is(first, at::kInt, dev) && first->dim() == 1 && first->size(0) >= batch && first->is_contiguous()),
+          "first is int32 [batch] on the cache's device");
+  const int32_t* at = first ? static_cast<const int32_t*>(first->data_ptr()) : nullptr;
+  return status([&] { return entry.block_bounds(ctx, kv, bounds, at, (int32_t)max_new, (int32_t)batch, stream); });
+}
+
+// block_topk(ctx, view, bounds, sched, q, batch, heads, units, device, stream, blocks, count)
+PyObject* block_topk(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 12)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_kv_view* kv = v.pointer<prhs_kv_view>(1);
+  const prhs_block_bounds_view* bounds = v.pointer<prhs_block_bounds_view>(2);
+  const prhs_block_schedule* sched = v.pointer<prhs_block_schedule>(3);
+  const int64_t batch = v.integer(5), heads = v.integer(6), units = v.integer(7), dev = v.integer(8);
+  void* stream = v.pointer<void>(9);
+  if (PyErr_Occurred()) return nullptr;
+  Io io;
+  Lists l;
+  if (!io.read(a[4], Py_None, Py_None, batch, heads, dev) || !l.read(a[10], a[11], batch, units, dev)) return nullptr;
+  return status([&] { return entry.block_topk(ctx, io.q, kv, bounds, sched, (int32_t)batch, l.lists, l.stride, l.count, stream); });
+}
+
+// block_decode_attn(ctx, view, q, out, out_lse, batch, heads, units, device, stream, blocks, count, flags)
+PyObject* block_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 13)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_kv_view* kv = v.pointer<prhs_kv_view>(1);
+  const int64_t batch = v.integer(5), heads = v.integer(6), units = v.integer(7), dev = v.integer(8), flags = v.integer(12);
+  void* stream = v.pointer<void>(9);
+  if (PyErr_Occurred()) return nullptr;
+  Io io;
+  Lists l;
+  if (!io.read(a[2], a[3], a[4], batch, heads, dev) || !l.read(a[10], a[11], batch, units, dev)) return nullptr;
+  return status([&] {
+    return entry.block_decode_attn(ctx, io.q, kv, l.lists, l.count, l.stride, (uint32_t)flags, (int32_t)batch, io.out, io.lse, stream);
+  });
+}
+
+// block_decode_step(ctx, view, bounds, sched, q, out, out_lse, batch, heads, units, device, stream, blocks, count)
+PyObject* block_decode_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 14)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_kv_view* kv = v.pointer<prhs_kv_view>(1);
+  const prhs_block_bounds_view* bounds = v.pointer<prhs_block_bounds_view>(2);
+  const prhs_block_schedule* sched = v.pointer<prhs_block_schedule>(3);
+  const int64_t batch = v.integer(7), heads = v.integer(8), units = v.integer(9), dev = v.integer(10);
+  void* stream = v.pointer<void>(11);
+  if (PyErr_Occurred()) return nullptr;
+  Io io;
+  Lists l;
+  if (!io.read(a[4], a[5], a[6], batch, heads, dev) || !l.read(a[12], a[13], batch, units, dev)) return nullptr;
+  return status([&] {
+    return entry.block_decode_step(ctx, io.q, kv, bounds, sched, (int32_t)batch, io.out, io.lse, l.lists, l.stride, l.count, stream);
+  });
+}
+
+#define METHOD(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {METHOD(kv_view), METHOD(bytekv_view), METHOD(bounds_view), METHOD(bind), METHOD(bytekv_append), METHOD(bytekv_decode_attn),
+                         METHOD(bytekv_sparse_decode_attn), METHOD(block_bounds), METHOD(block_topk), METHOD(block_decode_attn),
+                         METHOD(block_decode_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -78,20 +78,22 @@ def test_host_tensors_and_wrong_types_are_refused(lib):
         P.make_block_bounds(torch.zeros(2, 3, 4, 2, 128, dtype=torch.int8), torch.zeros(2, 3, 4))
     with pytest.raises(AssertionError):
         P.make_view(t.float(), t.float(), lens)
-    m = P._load_marshal()
-    with pytest.raises(AssertionError):
-        m.io(t, None, None, 2, 3, 0)
-    with pytest.raises(AssertionError):
-        m.lists(lens, lens, 2, 3, 0)
-    with pytest.raises(AssertionError):
-        m.rows(t, t, lens, 2, 3, 0, 0)
-    N = None
-    for f, args in ((m.kv_view, (N, N, N, N)), (m.bytekv_view, (N,) * 8 + (0,)), (m.bounds_view, (N, N)), (m.rows, (N, N, N, 1, 1, 0, 0)),
-                    (m.io, (N, N, N, 1, 1, 0)), (m.lists, (N, N, 1, 1, 0))):
+    m, N = P._load_marshal(), None
+    calls = ((m.kv_view, (N, N, N, N)), (m.bytekv_view, (N,) * 8 + (0,)), (m.bounds_view, (N, N)),
+             (m.bytekv_append, (0, 0, t, t, lens, 2, 3, 0, 0, 0)), (m.bytekv_append, (0, 0, N, N, N, 2, 3, 0, 0, 0)),
+             (m.bytekv_decode_attn, (0, 0, t, t, N, 2, 3, 0, 0)), (m.bytekv_decode_attn, (0, 0, N, N, N, 2, 3, 0, 0)),
+             (m.bytekv_sparse_decode_attn, (0, 0, t, t, N, 2, 3, 0, 0, lens, lens)), (m.block_bounds, (0, 0, 0, lens, 0, 2, 0, 0)),
+             (m.block_topk, (0, 0, 0, 0, t, 2, 3, 3, 0, 0, lens, lens)), (m.block_decode_attn, (0, 0, t, t, N, 2, 3, 3, 0, 0, lens, lens, 0)),
+             (m.block_decode_step, (0, 0, 0, 0, t, t, N, 2, 3, 3, 0, 0, lens, lens)))
+    for f, args in calls:
         with pytest.raises(AssertionError):
-            f(*args)
+            f(*args)                            # nothing there, or host tensors where device 0 is asked for
         with pytest.raises(TypeError):
             f(*args[:-1])
+        with pytest.raises(TypeError):
+            f(*args, N)
+    with pytest.raises(TypeError):
+        m.bytekv_decode_attn("ctx", 0, t, t, N, 2, 3, 0, 0)
 
 
 # --------------------------------------------------------------------- the 64-bit forms' pins
