@@ -208,19 +208,16 @@ prhs_status prhs_block_bounds(prhs_ctx* ctx, const prhs_kv_view* kv, const prhs_
   p.kv = dv;
   p.bd = bd;
   p.first = first;
-  p.batch = batch;
-  p.num_kv_heads = ctx->cfg.num_kv_heads;
   p.max_new = most;
-  p.blocks_max = most == 1 ? 1 : std::min((most + 2 * (kBlockRows - 1)) / kBlockRows, (max_t + kBlockRows - 1) / kBlockRows);
   p.max_len = max_t;
   p.flags = ctx->flags;
-  const long long items = (long long)batch * p.num_kv_heads * p.blocks_max;
-  const int warps = items >= 8ll * ctx->sm_count ? 8 : 1;
-  const long long ctas = (items + warps - 1) / warps;
-  if (ctas > 0x7fffffffll) return fail(ctx, PRHS_ERR_UNSUPPORTED, "block bounds: too many blocks");
+  if (ctx->cfg.num_kv_heads > 65535 || batch > 65535) return fail(ctx, PRHS_ERR_UNSUPPORTED, "block bounds: more than 65535 heads or sequences");
+  // blocks a sequence can touch: its new positions may start anywhere in a block
+  const int blocks = most == 1 ? 1 : std::min((most + 2 * (kBlockRows - 1)) / kBlockRows, (max_t + kBlockRows - 1) / kBlockRows);
+  const int warps = std::min(blocks, 8);
   {
     LaunchScope ls(ctx, PRHS_KIND_MISC, st);
-    block_bounds_kernel<<<(unsigned)ctas, 32 * warps, 0, st>>>(p);
+    block_bounds_kernel<<<dim3((blocks + warps - 1) / warps, ctx->cfg.num_kv_heads, batch), 32 * warps, 0, st>>>(p);
   }
   PRHS_CUDA(ctx, cudaGetLastError());
   return PRHS_OK;

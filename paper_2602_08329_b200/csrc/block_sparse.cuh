@@ -93,18 +93,13 @@ struct BoundsParams {
   KvDev kv;
   BoundsDev bd;
   const int* first;         // [B] or nullptr (0): bounds of the blocks that hold positions [first, t)
-  int batch, num_kv_heads, max_len;
-  int max_new, blocks_max;  // positions [first, t) of any sequence at most, and the blocks they can touch
+  int max_len, max_new;     // t and t - first of any sequence at most
   uint32_t* flags;
 };
 
-// One warp per block.  Bound by HBM: 4 KB of keys in, 260 B out per block.
+// One warp per block, grid (blocks, Hkv, B).  Bound by HBM: 4 KB of keys in, 260 B out per block.
 __global__ void __launch_bounds__(256) block_bounds_kernel(BoundsParams p) {
-  const long long item = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int j = (int)(item % p.blocks_max);
-  const long long bh = item / p.blocks_max;
-  if (bh >= (long long)p.batch * p.num_kv_heads) return;
-  const int kvh = (int)(bh % p.num_kv_heads), b = (int)(bh / p.num_kv_heads);
+  const int j = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), kvh = blockIdx.y, b = blockIdx.z;
   const int t = __ldg(p.kv.seq_lens + b);
   const int f = p.first ? __ldg(p.first + b) : 0;
   if (f < 0 || f > t || t > p.max_len || t - f > p.max_new) {
