@@ -211,6 +211,7 @@ struct ByteKvAttnParams {
   int batch, num_q_heads, group_size;
   int deal;                 // kRuns, kParts, kWhole
   int max_len;              // lengths outside [0, max_len] are cut to it (and recorded)
+  int sm_count;             // runs may be short while every SM has one CTA at most
   float* partials;          // [CTA][2][heads per unit][kPartStride]
   unsigned int* tickets;    // [B][Hq], zero on entry and on exit
   __nv_bfloat16* out;
@@ -304,9 +305,13 @@ __device__ __forceinline__ float load_query_f16(const __nv_bfloat16* q, bool has
 //           2047 positions: 20 us against 12 us), and what the rounding wastes is small.
 //   whole   other lists: one CTA per unit (256 lists of 1838 entries: 29 us; in runs, 34 us)
 constexpr int kRuns = 0, kParts = 1, kWhole = 2;
-// items per CTA at least: below, a merge costs more than the shorter part saves
+// items per CTA at least: below, a merge costs more than the shorter part saves.  Where the items are so few that
+// runs of the short kind give no SM two CTAs, the short kind: nothing else would use the idle SMs
+// (8 KV heads of 2047 positions: 8.5 us against 9.3; of 500, 8.1 against 9.2.  With the short kind everywhere 8192
+// positions take 14.7 us, not 11.8: more than 16 parts are merged in two goes)
 template <bool kList>
 constexpr int k8MinRun = kList ? 32 : 16;
+constexpr int k8ShortRun = 8;
 
 // kWide: more than eight heads per KV head (two column tiles).
 template <int kFmt, bool kList, bool kWide>
@@ -351,9 +356,10 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
   if (p.deal != kWhole) {
     int before = 0;
     const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, blocks_of);
-    // no shorter than k8MinRun items or a unit; parts: as many as fit with every unit rounded up
+    // no shorter than the smallest run or a unit; parts: as many as fit with every unit rounded up
     const int ctas = p.deal == kParts ? (int)gridDim.x - units : (int)gridDim.x;
-    share = max((total + ctas - 1) / ctas, min(k8MinRun<kList>, (total + units - 1) / units));
+    const int min_run = total <= k8ShortRun * p.sm_count ? k8ShortRun : k8MinRun<kList>;
+    share = max((total + ctas - 1) / ctas, min(min_run, (total + units - 1) / units));
     if (p.deal == kParts) {
       const int most = share;
       auto count = [&](int t) { return (blocks_of(t) + most - 1) / most; };

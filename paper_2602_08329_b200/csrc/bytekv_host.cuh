@@ -97,7 +97,7 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.out_lse = out_lse;
   p.flags = c->flags;
   // how the units are dealt (see bytekv.cuh), and to how many CTAs: one per resident slot, fewer where the items
-  // (k8MinRun per CTA) would not fill them.  max_count: positions of a sequence or entries of a list at most.
+  // (k8MinRun per CTA, k8ShortRun where that still leaves one CTA per SM) would not fill them.  max_count: positions of a sequence or entries of a list at most.
   const int slots = (idx ? Shape8<true, false>::kCtasPerSm : Shape8<false, false>::kCtasPerSm) * c->sm_count;
   const int min_run = idx ? k8MinRun<true> : k8MinRun<false>;
   const long long units = (long long)batch * (idx ? c->cfg.num_q_heads : c->cfg.num_kv_heads);
@@ -105,7 +105,9 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   if (units * unit_max >= (1ll << 30))
     return fail(c, PRHS_ERR_UNSUPPORTED, "units times their largest length above 2^34: pass a smaller max_seq_len or idx_stride");
   p.deal = (idx ? 2 : 8) * units <= slots ? kParts : idx ? kWhole : kRuns;
-  const long long full = units * ((unit_max + min_run - 1) / min_run) + (p.deal == kParts ? units : 0);
+  p.sm_count = c->sm_count;
+  const long long few = std::min<long long>(c->sm_count, units * ((unit_max + k8ShortRun - 1) / k8ShortRun));
+  const long long full = std::max(few, units * ((unit_max + min_run - 1) / min_run)) + (p.deal == kParts ? units : 0);
   const int ctas = (int)(p.deal == kWhole ? units : std::min<long long>(slots, full));
   const dim3 grid(ctas);
   {
