@@ -76,8 +76,7 @@ cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem,
   return launch_ordered(kernel, grid, threads, smem, st, p, 1);
 }
 prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const BoundsDev& bd, const prhs_block_schedule* s,
-                              int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, bool update_last,
-                              cudaStream_t st) {
+                              int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, cudaStream_t st) {
   const bool shared = block_shared(c, s->flags);
   BlockScoreParams sp;
   sp.q = static_cast<const __nv_bfloat16*>(q);
@@ -91,7 +90,6 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   sp.num_q_heads = c->cfg.num_q_heads;
   sp.group_size = c->gq;
   sp.group_max = shared ? 1 : 0;
-  sp.update_last = update_last ? 1 : 0;
   sp.max_len = max_t;
   sp.flags = c->flags;
   // one wave of CTAs, none with less than one round of its four warps
@@ -154,7 +152,8 @@ int block_splits(const prhs_ctx* c, int units, int blocks) {
 }
 
 prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
-                              uint32_t flags, int max_t, int batch, void* out, float* out_lse, const prhs_block_schedule* step, cudaStream_t st) {
+                              uint32_t flags, int max_t, int batch, void* out, float* out_lse, const prhs_block_schedule* step, const BoundsDev* bd,
+                              cudaStream_t st) {
   const bool shared = block_shared(c, flags);
   BlockAttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -172,6 +171,7 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.sink = step ? step->sink_blocks : 0;
   p.recent = step ? step->recent_blocks : 0;
   p.top = step ? step->top_blocks : 0;
+  p.bd = bd ? *bd : BoundsDev{};
   p.partials = c->partials;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -236,7 +236,7 @@ prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv
   if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
   if (rc == PRHS_OK) rc = check_block_sched(ctx, sched, blocks_stride, max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, false, as_stream(stream));
+  return launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
@@ -250,7 +250,7 @@ prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_v
   prhs_status rc = check_q_out(ctx, q, out, batch);
   if (rc == PRHS_OK) rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse, nullptr, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse, nullptr, nullptr, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
@@ -268,9 +268,9 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
   if (rc != PRHS_OK) return rc;
   if (sched->recent_blocks < 1)
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
-  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, true, as_stream(stream));
+  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, as_stream(stream));
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, sched, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, sched, &bd, as_stream(stream));
 }
 
 }  // extern "C"

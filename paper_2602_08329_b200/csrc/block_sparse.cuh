@@ -124,7 +124,6 @@ struct BlockScoreParams {
   int bounds_outer, bounds_head;   // bd's strides: a bounds index (256 bytes) fits 31 bits on any device
   float* scores;            // [B][Hq][ld]; group_max: the row of the group's first head
   int ld, batch, num_q_heads, group_size, group_max;
-  int update_last;          // 1: the bounds of the last block are recomputed here (its score is not used)
   int max_len;
   uint32_t* flags;
 };
@@ -192,7 +191,6 @@ __global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score
     const int head0 = kvh * gq;
     const int nb = (t + kBlockRows - 1) / kBlockRows;
     const int g_hi = min(groups, g_lo + run_end - at);
-    const bool updates = p.update_last && g_hi == groups;
     const int rounds = max(0, (g_hi - g_lo - warp + kScoreWarps - 1) / kScoreWarps);     // groups g_lo + warp + 4r
     const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;
     auto page_of = [&](int r) -> int {                   // lanes 0..15: the page of block lane of round r
@@ -321,13 +319,6 @@ __global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtasPerSm) block_score
       }
     }
     cp_async_wait<0>();
-    if (updates && warp == kScoreWarps - 1) {            // the bounds of the last block (its score is not used)
-      long long row, bi;
-      if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
-        bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
-      else if (lane == 0)
-        atomicOr(p.flags, kFlagBadPage);
-    }
     at += g_hi - g_lo;
     if (at >= run_end) return;
     g_lo = 0;
@@ -519,6 +510,7 @@ struct BlockAttnParams {
   // a step knows without the selection that blocks [0, sink) and the last `recent` are attended over (fixed = 1): it
   // takes the lists' middle part only, `top` entries at most
   int fixed, sink, recent, top;
+  BoundsDev bd;             // and it recomputes the bounds of the last block
   float* partials;          // [B][Hq][splits][kPartStride]
   unsigned int* tickets;
   __nv_bfloat16* out;
@@ -550,6 +542,15 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   float o[kTiles][8][4];
   clear_tiles<kTiles>(o);
   SoftBf st[kTiles][2];
+
+  // a step writes the bounds of the last block, whose score nothing reads: here and now, while the selection runs
+  if (p.fixed && split == 0 && head0 % p.group_size == 0 && warp == kTWarps - 1 && nb > 0) {
+    long long row, bi;
+    if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
+      bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
+    else if (lane == 0)
+      atomicOr(p.flags, kFlagBadPage);
+  }
 
   // two passes over the ring: the blocks that are known (a step), then the listed ones
   const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent);
