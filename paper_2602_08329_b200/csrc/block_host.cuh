@@ -131,20 +131,25 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   return PRHS_OK;
 }
 
-// Splits of a list of blocks, in cycles as measured: a warp works one block off in about 900 when CTAs are few and waits
-// for its share of the HBM stream (2760 when every slot is taken) when they are many; a CTA's start and end
-// cost about 3000, a merge of parts 4500 (one user, 19 blocks per head: 10.9 us a step with one split, 12.9 with
-// two; 8 x 32 heads of 73 blocks: 60 us with one, 72 with two).
-int block_splits(const prhs_ctx* c, int units, int blocks) {
+// Splits of a list of blocks.  In cycles, as measured: a warp works one block off in about 900; 8 KB take 2.4 of the HBM
+// stream; of the smaller of the two a quarter stays visible; a CTA's start and end cost about 3000, a merge of parts
+// 4500, and 1500 for every further batch of parts (finish_unit).  us per step with 1, 2, 4, 8, 16 splits:
+//   32 lists of 19 blocks (one user)      9.7 11.8 12.0 12.4 15.3     128 sets of 137 for 4 heads  52.4 53.6
+//   32 lists of 73                       20.0 19.3 17.6 16.4 20.4     64 sets                      38.2 33.6 33.4 37.8
+//   64 lists of 73                       22.9 22.0 20.3 24.4 31.4     32 sets                      32.4 27.0 23.2 21.5 26.0
+//   256 lists of 73                      60 72                        8 sets                       28.7 23.6 19.5 17.8 17.0
+int block_splits(const prhs_ctx* c, int units, int blocks, int heads) {
   const int slots = 2 * c->sm_count;
+  const int merged = 16 * std::max(1, kTWarps / heads);          // parts of a head that are merged at a time
+  const double stream = 2.4 * units * blocks;
   int best = 1;
   double best_cost = 1e30;
   for (int s = 1; s <= kMaxSplits; ++s) {
     const int per_warp = (blocks + s * kTWarps - 1) / (s * kTWarps);
-    const long long ctas = (long long)units * s;
-    const double waves = (double)((ctas + slots - 1) / slots);
-    const double stage = std::max(900.0, 2760.0 * std::min<long long>(ctas, slots) / slots);
-    const double cost = waves * (3000.0 + per_warp * stage) + (s > 1 ? 4500.0 : 0.0);
+    const double waves = (double)(((long long)units * s + slots - 1) / slots);
+    const double work = waves * per_warp * 900.0;
+    const double cost = std::max(work, stream) + 0.25 * std::min(work, stream) + waves * 3000.0 +
+                        (s > 1 ? 4500.0 + 1500.0 * ((s + merged - 1) / merged - 1) : 0.0);
     if (cost < best_cost * 0.999) { best_cost = cost; best = s; }
     if (per_warp == 1) break;
   }
@@ -165,7 +170,9 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.units_per_seq = c->cfg.num_q_heads / p.heads_per_unit;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  p.splits = block_splits(c, batch * p.units_per_seq, stride);
+  // a unit's blocks at most; a step knows more than the width of the table
+  const int listed = step ? std::min(stride, step->sink_blocks + step->top_blocks + step->recent_blocks) : stride;
+  p.splits = block_splits(c, batch * p.units_per_seq, std::min(listed, std::max(1, (max_t + kBlockRows - 1) / kBlockRows)), p.heads_per_unit);
   p.max_len = max_t;
   p.fixed = step ? 1 : 0;
   p.sink = step ? step->sink_blocks : 0;
