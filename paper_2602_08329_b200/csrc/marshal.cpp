@@ -9,6 +9,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <exception>
 
 #include "../../include/prhs.h"
 
@@ -306,7 +307,20 @@ PyObject* block_decode_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
-#define METHOD(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
+// torch's C++ exceptions (a tensor without storage or strides) as Python's: none may leave a C function.
+template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t nargs) noexcept {
+  try {
+    return F(self, a, nargs);
+  } catch (const c10::Error& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+
+#define METHOD(name) {#name, (PyCFunction)(void*)guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(kv_view), METHOD(bytekv_view), METHOD(bounds_view), METHOD(bind), METHOD(bytekv_append), METHOD(bytekv_decode_attn),
                          METHOD(bytekv_sparse_decode_attn), METHOD(block_bounds), METHOD(block_topk), METHOD(block_decode_attn),
                          METHOD(block_decode_step), {nullptr, nullptr, 0, nullptr}};

@@ -96,6 +96,16 @@ def test_host_tensors_and_wrong_types_are_refused(lib):
         m.bytekv_decode_attn("ctx", 0, t, t, N, 2, 3, 0, 0)
 
 
+def test_tensors_without_storage_raise(lib):
+    """torch's C++ exception has to arrive as Python's; out of a C function it would end the process."""
+    sparse = torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16).to_sparse()
+    dense, lens = torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises((RuntimeError, AssertionError)):
+        P.make_view(sparse, sparse, lens)
+    with pytest.raises(RuntimeError, match="storage"):
+        P.make_view(dense, dense, lens.to_sparse())
+
+
 # --------------------------------------------------------------------- the 64-bit forms' pins
 @pytest.mark.parametrize("fmt,dtype", [("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)])
 def test_codes_are_torchs_rounding(fmt, dtype):
