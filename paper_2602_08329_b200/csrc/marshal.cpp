@@ -49,7 +49,8 @@ PyObject* kv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   REQUIRE(k->dim() >= 3 && k->size(-1) == 128 && k->strides() == v->strides() && k->stride(-1) == 1 && k->stride(-2) == 128,
           "rows of 128 contiguous elements, k and v alike");
   REQUIRE(lens->scalar_type() == at::kInt, "seq_lens is int32");
-  REQUIRE(!table || (table->scalar_type() == at::kInt && table->dim() == 2 && table->is_contiguous()), "the page table is contiguous int32 [batch][pages]");
+  REQUIRE(!table || (table->scalar_type() == at::kInt && table->dim() >= 1 && (table->dim() == 1 || table->stride(-1) == 1)),
+          "the page table is int32 [batch][pages], its rows contiguous");
   return Py_BuildValue("LLLLLLLLLLLL", address(*k), address(*v), k->stride(0), k->stride(1), table ? address(*table) : 0,
                        table ? table->stride(0) : 0, address(*lens), table ? k->size(0) : 0, lens->numel(), k->size(1),
                        table ? 0 : k->size(2), device(*k));

@@ -106,6 +106,17 @@ def test_tensors_without_storage_raise(lib):
         P.make_view(dense, dense, lens.to_sparse())
 
 
+def test_views_take_rows_of_a_wider_page_table(lib):
+    pool, lens = torch.zeros(9, 2, 16, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    table = torch.zeros(2, 8, dtype=torch.int32)
+    for t in (table, table[:, :4], table[:, 2:]):
+        view = P.make_view(pool, pool, lens, page_table=t)
+        assert (view.page_table_stride, view.page_table, view.num_pages) == (8, t.data_ptr(), 9)
+    for t in (table[:, ::2], table.long()):
+        with pytest.raises(AssertionError):
+            P.make_view(pool, pool, lens, page_table=t)
+
+
 # --------------------------------------------------------------------- the 64-bit forms' pins
 @pytest.mark.parametrize("fmt,dtype", [("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)])
 def test_codes_are_torchs_rounding(fmt, dtype):
