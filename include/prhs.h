@@ -380,7 +380,8 @@ prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const p
  * maximum as int8 codes with one scale:  code = rint(x / scale), scale = 2^max(ceil(log2(amax / 127)), -126).
  * A query head's score of a block is the largest q . k inside those bounds with q coded the same way per head:
  *     score = sum_d max(q8_d lo8_d, q8_d hi8_d) * scale_block * scale_q,
- * an exact integer sum and two powers of two, so scores are the same on every machine and ties are real.
+ * an exact integer sum and two powers of two, so scores are the same on every machine and ties are real (as far as
+ * the range of fp32 goes: a partial product beyond it is infinite or zero).
  *   contiguous: block j of (b, kvh) has index b*stride_outer + kvh*stride_head + j
  *   paged:      page*stride_outer + kvh*stride_head
  *   codes + index*256: 128 minima, then 128 maxima;  scale + index */
@@ -421,8 +422,9 @@ prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv
 prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
                                    int32_t blocks_stride, uint32_t flags, int32_t batch, void* out, float* out_lse, void* stream);
 
-/* One decode step: the bounds of every sequence's last block (the one that holds the current token) are brought up to
- * date, then prhs_block_topk and prhs_block_decode_attn.  recent_blocks >= 1. */
+/* One decode step: prhs_block_topk and prhs_block_decode_attn, and the bounds of every sequence's last block (the one that
+ * holds the current token) are brought up to date (not for a t_b outside [0, max_seq_len], which is cut and recorded).
+ * recent_blocks >= 1.  Sequences may share pages whose positions all of them have. */
 prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
                                    const prhs_block_schedule* sched, int32_t batch, void* out, float* out_lse, int32_t* out_blocks,
                                    int32_t blocks_stride, int32_t* out_count, void* stream);

@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   SoftBf st[kTiles][2];
 
   // a step writes the bounds of the last block, whose score nothing reads: here and now, while the selection runs
-  if (p.fixed && split == 0 && head0 % p.group_size == 0 && warp == kTWarps - 1 && nb > 0) {
+  if (p.fixed && split == 0 && head0 % p.group_size == 0 && warp == kTWarps - 1 && nb > 0 && t == given) {
     long long row, bi;
     if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
       bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);

@@ -97,7 +97,8 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   p.out_lse = out_lse;
   p.flags = c->flags;
   // how the units are dealt (see bytekv.cuh), and to how many CTAs: one per resident slot, fewer where the items
-  // (k8MinRun per CTA, k8ShortRun where that still leaves one CTA per SM) would not fill them.  max_count: positions of a sequence or entries of a list at most.
+  // (k8MinRun per CTA, k8ShortRun where that still leaves one CTA per SM) would not fill them.  max_count: positions
+  // of a sequence or entries of a list at most.
   const int slots = (idx ? Shape8<true, false>::kCtasPerSm : Shape8<false, false>::kCtasPerSm) * c->sm_count;
   const int min_run = idx ? k8MinRun<true> : k8MinRun<false>;
   const long long units = (long long)batch * (idx ? c->cfg.num_q_heads : c->cfg.num_kv_heads);

@@ -349,6 +349,30 @@ def test_empty_batch_and_lengths_out_of_range(cuda_device):
     ctx.close()
 
 
+def test_a_step_leaves_the_bounds_of_an_impossible_length(cuda_device):
+    """A step writes bounds of last blocks only, and none for a length that is cut."""
+    cache = Cache(3, 2, 64, True, cuda_device, seed=5)
+    ctx = make_ctx(cache, 1)
+    cache.place(random_rows(3, 2, 64, 5), [50, 64, 64])
+    ctx.block_bounds(cache.view(), cache.bounds(), 3)
+    before = cache.codes.clone(), cache.scale.clone()
+    for b, j in ((0, 3), (1, 3), (2, 3)):
+        page = int(cache.table_cpu[b, j])
+        cache.codes[page], cache.scale[page] = 77, 77.0
+    cache.lens.copy_(torch.tensor([50, 65, -3], dtype=torch.int32))
+    q = torch.randn(3, 2, 128, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(3, 2, device=cuda_device)
+    blocks, count = torch.empty(3, 2, 3, dtype=torch.int32, device=cuda_device), torch.empty(3, 2, dtype=torch.int32, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(1, 1, 1), 3, out, lse, blocks, count)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    for b in (1, 2):
+        page = int(cache.table_cpu[b, 3])
+        before[0][page], before[1][page] = 77, 77.0
+    assert torch.equal(cache.codes, before[0]) and torch.equal(cache.scale, before[1])
+    ctx.close()
+
+
 def test_all_blocks_are_the_dense_attention(cuda_device):
     cache = Cache(2, 2, 700, False, cuda_device)
     ctx = make_ctx(cache, 2)
