@@ -7,8 +7,10 @@ namespace {
 constexpr int kMaxBlocks = kMaxContext / kBlockRows;
 
 cudaError_t block_set_attributes() {
-  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true>, kTSmemBytes},
+  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<false, true>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true, true>, kTSmemBytes},
                                                            {(const void*)block_score_kernel<false>, kScoreSmemBytes},
                                                            {(const void*)block_score_kernel<true>, kScoreSmemBytes}};
   for (const auto& k : all) {
@@ -76,7 +78,7 @@ cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem,
   return launch_ordered(kernel, grid, threads, smem, st, p, 1);
 }
 prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const BoundsDev& bd, const prhs_block_schedule* s,
-                              int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, cudaStream_t st) {
+                              int max_t, int batch, int32_t* out_blocks, int stride, int32_t* out_count, bool select, cudaStream_t st) {
   const bool shared = block_shared(c, s->flags);
   BlockScoreParams sp;
   sp.q = static_cast<const __nv_bfloat16*>(q);
@@ -103,6 +105,7 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
     else block_score_kernel<false><<<ctas, kScoreWarps * 32, kScoreSmemBytes, st>>>(sp);
   }
   PRHS_CUDA(c, cudaGetLastError());
+  if (!select) return PRHS_OK;
   BlockSelectParams p;
   p.scores = c->scores;
   p.ld = c->ld;
@@ -129,6 +132,11 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
     PRHS_CUDA(c, e);
   }
   return PRHS_OK;
+}
+
+// Whether a step's attention kernel selects for itself (kSelect in block_sparse.cuh has both sides).
+bool step_selects_in_attn(const prhs_block_schedule* s, int max_t) {
+  return (max_t + kBlockRows - 1) / kBlockRows <= kSelectKeys * kTThreads && s->top_blocks <= kSelectTop;
 }
 
 // Splits of a list of blocks.  In cycles, as measured: a warp works one block off in about 900; 8 KB take 2.4 of the HBM
@@ -179,6 +187,11 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.recent = step ? step->recent_blocks : 0;
   p.top = step ? step->top_blocks : 0;
   p.bd = bd ? *bd : BoundsDev{};
+  const bool select = step && step_selects_in_attn(step, max_t);
+  p.scores = c->scores;
+  p.ld = c->ld;
+  p.out_blocks = const_cast<int32_t*>(blocks);
+  p.out_count = const_cast<int32_t*>(count);
   p.partials = c->partials;
   p.tickets = c->tickets;
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -188,8 +201,10 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
     LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
     // `step`: the lists are this step's, from the kernel before; a caller's own may come from any kernel (ordinary launch)
     const dim3 grid(p.splits, p.units_per_seq, batch);
-    const cudaError_t e = launch_ordered(p.heads_per_unit > 8 ? block_attn_kernel<true> : block_attn_kernel<false>, grid, kTThreads,
-                                         kTSmemBytes, st, p, step ? 1 : 0);
+    const bool wide = p.heads_per_unit > 8;
+    const cudaError_t e = launch_ordered(select ? (wide ? block_attn_kernel<true, true> : block_attn_kernel<false, true>)
+                                                : (wide ? block_attn_kernel<true, false> : block_attn_kernel<false, false>),
+                                         grid, kTThreads, kTSmemBytes, st, p, step ? 1 : 0);
     PRHS_CUDA(c, e);
   }
   return PRHS_OK;
@@ -243,7 +258,7 @@ prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv
   if (rc == PRHS_OK) rc = check_bounds(ctx, bounds, &bd);
   if (rc == PRHS_OK) rc = check_block_sched(ctx, sched, blocks_stride, max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, as_stream(stream));
+  return launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, true, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const int32_t* blocks, const int32_t* count,
@@ -275,7 +290,8 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
   if (rc != PRHS_OK) return rc;
   if (sched->recent_blocks < 1)
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
-  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, as_stream(stream));
+  const bool select = !step_selects_in_attn(sched, max_t);
+  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, select, as_stream(stream));
   if (rc != PRHS_OK) return rc;
   return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, sched, &bd, as_stream(stream));
 }

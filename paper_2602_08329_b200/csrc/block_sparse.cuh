@@ -348,51 +348,34 @@ struct BlockSelectParams {
   int max_len;
 };
 
-// One CTA per unit (a query head, or a KV head where the group shares a set).  The unit attends over blocks
-// [0, lo), the `top` best of [lo, hi), and [hi, nb).  The scores are read once into registers (kKeys per
-// thread, 512 threads; kKeys = 0 reads them again in every pass, for more than 16384 blocks).  The threshold
-// is found by narrowing an interval of keys (the scores' order-preserving 32-bit images): a histogram of 1024
-// equal bins over the interval says which bin the top-th key lies in, and that bin is the next interval.
-// Scores of one unit lie close together, so bins over their own range spread them (bins over the leading
-// bits would not, and the shared-memory atomics would serialise).  With at most 32 keys left in the bin, a warp
-// ranks them directly; that is usually after one histogram.  Then one ordered pass writes the list.
-constexpr int kBSThreads = 512;
-constexpr int kBSWarps = kBSThreads / 32;
-constexpr int kBSBins = 2 * kBSThreads;
-template <int kKeys>
-__global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectParams p) {
-  __shared__ int hist[kBSBins];
-  __shared__ uint32_t red_lo[kBSWarps], red_hi[kBSWarps], cand[32];
-  __shared__ int warp_a[kBSWarps], warp_b[kBSWarps];
-  __shared__ uint32_t sh_base, sh_span;
-  __shared__ int sh_need, sh_count, sh_cands;
-  step_release();
-  const int unit = blockIdx.x;
-  const int b = unit / p.units_per_seq, u = unit % p.units_per_seq;
+// The unit (a query head, or a KV head where the group shares a set) attends over blocks [0, lo), the `top` best of
+// [lo, hi), and [hi, nb).  Selection of the middle by one CTA of kThreads: the scores are read once into registers
+// (kKeys per thread; kKeys = 0 reads them again in every pass).  The threshold is found by narrowing an interval of
+// keys (the scores' order-preserving 32-bit images): a histogram of 2 kThreads equal bins over the interval says which
+// bin the top-th key lies in, and that bin is the next interval.  Scores of one unit lie close together, so bins over
+// their own range spread them (bins over the leading bits would not, and the shared-memory atomics would serialise).
+// With at most 32 keys left in the bin, a warp ranks them directly; that is usually after one histogram.  Then one
+// ordered pass hands out the list, put(place, block) in ascending order.
+template <int kThreads>
+struct SelectSmem {
+  int hist[2 * kThreads];                          // zero before and after
+  uint32_t red_lo[kThreads / 32], red_hi[kThreads / 32], cand[32];
+  int warp_a[kThreads / 32], warp_b[kThreads / 32];
+  uint32_t base, span;
+  int need, count, cands;                          // cands: zero before
+};
+template <int kThreads, int kKeys, typename Put>
+__device__ __forceinline__ void select_middle(const float* s, int lo, int hi, int need, SelectSmem<kThreads>& sm, Put put) {
+  constexpr int kWarps = kThreads / 32, kBins = 2 * kThreads, kBinBits = kThreads == 512 ? 10 : 8;
+  static_assert(kBins == 1 << kBinBits, "the bins are a power of two");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int t = min(max(__ldg(p.seq_lens + b), 0), p.max_len);
-  const int nb = (t + kBlockRows - 1) / kBlockRows;
-  const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent);
-  const int need0 = min(p.top, hi - lo);
-  const int total = lo + need0 + nb - hi;
-  const float* s = p.scores + ((long long)b * p.num_q_heads + u * p.heads_per_unit) * p.ld;
-  int* out = p.out_blocks + (long long)unit * p.stride;
-  for (int i = tid; i < p.stride; i += kBSThreads) {
-    if (i < lo) out[i] = i;
-    else if (i >= total) out[i] = -1;
-    else if (i >= lo + need0) out[i] = hi + (i - lo - need0);
-  }
-  hist[2 * tid] = 0;
-  hist[2 * tid + 1] = 0;
-  if (tid == 0) { p.out_count[unit] = total; sh_cands = 0; }
-  step_wait();
-  if (need0 == 0) return;
-  if (need0 == hi - lo) {                          // every block of the middle
-    for (int i = tid; i < need0; i += kBSThreads) out[lo + i] = lo + i;
+  if (need == 0) return;
+  if (need == hi - lo) {                           // every block of the middle
+    for (int i = tid; i < need; i += kThreads) put(i, lo + i);
     return;
   }
   // every warp owns a run of positions, a lane every 32nd of it
-  const int run = (hi - lo + kBSThreads - 1) / kBSThreads * 32;
+  const int run = (hi - lo + kThreads - 1) / kThreads * 32;
   const int from = lo + warp * run, to = min(from + run, hi);
   uint32_t keys[kKeys > 0 ? kKeys : 1];
   auto fetch = [&](int r) -> uint32_t { return from + 32 * r + lane < to ? float_to_key(__ldcg(s + from + 32 * r + lane)) : 0u; };
@@ -416,53 +399,52 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
   });
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   kmax = __reduce_max_sync(0xffffffffu, kmax);
-  if (lane == 0) { red_lo[warp] = kmin; red_hi[warp] = kmax; }
+  if (lane == 0) { sm.red_lo[warp] = kmin; sm.red_hi[warp] = kmax; }
   __syncthreads();
-  kmin = __reduce_min_sync(0xffffffffu, red_lo[lane & (kBSWarps - 1)]);
-  kmax = __reduce_max_sync(0xffffffffu, red_hi[lane & (kBSWarps - 1)]);
+  kmin = __reduce_min_sync(0xffffffffu, sm.red_lo[lane & (kWarps - 1)]);
+  kmax = __reduce_max_sync(0xffffffffu, sm.red_hi[lane & (kWarps - 1)]);
   // the threshold: keys above `thr` are taken, and the first `need` (by position) of those equal to it
   uint32_t base = kmin, span = kmax - kmin;          // the interval [base, base + span]
-  int need = need0;
   while (span > 0u) {
-    const int shift = max(0, 32 - __clz(span) - 10);   // (key - base) >> shift < 1024
+    const int shift = max(0, 32 - __clz(span) - kBinBits);   // (key - base) >> shift < kBins
     each([&](int, bool in, uint32_t k) {
-      if (in && k - base <= span) atomicAdd(&hist[(k - base) >> shift], 1);
+      if (in && k - base <= span) atomicAdd(&sm.hist[(k - base) >> shift], 1);
     });
     __syncthreads();
-    // bins from the top: thread i owns the pair 1023 - 2i, 1022 - 2i
-    const int top_bin = kBSBins - 1 - 2 * tid;
-    const int c0 = hist[top_bin], c1 = hist[top_bin - 1];
-    hist[top_bin] = 0;
-    hist[top_bin - 1] = 0;
+    // bins from the top: thread i owns the pair kBins - 1 - 2i, kBins - 2 - 2i
+    const int top_bin = kBins - 1 - 2 * tid;
+    const int c0 = sm.hist[top_bin], c1 = sm.hist[top_bin - 1];
+    sm.hist[top_bin] = 0;
+    sm.hist[top_bin - 1] = 0;
     int incl = c0 + c1;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, off);
       if (lane >= off) incl += v;
     }
-    if (lane == 31) warp_a[warp] = incl;
+    if (lane == 31) sm.warp_a[warp] = incl;
     __syncthreads();
-    incl += __reduce_add_sync(0xffffffffu, lane < warp ? warp_a[lane] : 0);
+    incl += __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_a[lane] : 0);
     const int above = incl - c0 - c1;
     if (above < need && incl >= need) {                // exactly one thread
       const bool second = above + c0 < need;
       const int bin = second ? top_bin - 1 : top_bin;
-      sh_base = base + ((uint32_t)bin << shift);
-      sh_span = min((1u << shift) - 1u, span - ((uint32_t)bin << shift));
-      sh_need = need - above - (second ? c0 : 0);
-      sh_count = second ? c1 : c0;
+      sm.base = base + ((uint32_t)bin << shift);
+      sm.span = min((1u << shift) - 1u, span - ((uint32_t)bin << shift));
+      sm.need = need - above - (second ? c0 : 0);
+      sm.count = second ? c1 : c0;
     }
     __syncthreads();
-    base = sh_base;
-    span = sh_span;
-    need = sh_need;
-    if (span > 0u && sh_count <= 32) {                 // few enough to rank directly
+    base = sm.base;
+    span = sm.span;
+    need = sm.need;
+    if (span > 0u && sm.count <= 32) {                 // few enough to rank directly
       each([&](int, bool in, uint32_t k) {
-        if (in && k - base <= span) cand[atomicAdd(&sh_cands, 1)] = k;
+        if (in && k - base <= span) sm.cand[atomicAdd(&sm.cands, 1)] = k;
       });
       __syncthreads();
-      const int n = sh_count;
-      const uint32_t k = lane < n ? cand[lane] : 0u;
+      const int n = sm.count;
+      const uint32_t k = lane < n ? sm.cand[lane] : 0u;
       int gt = 0, ge = 0;
       for (int i = 0; i < n; ++i) {
         const uint32_t other = __shfl_sync(0xffffffffu, k, i);
@@ -483,19 +465,52 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
     eq += __popc(__ballot_sync(0xffffffffu, in && k == thr));
   });
   __syncthreads();                                     // warp_a is read above
-  if (lane == 0) { warp_a[warp] = gt; warp_b[warp] = eq; }
+  if (lane == 0) { sm.warp_a[warp] = gt; sm.warp_b[warp] = eq; }
   __syncthreads();
-  int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_b[lane & (kBSWarps - 1)] : 0);
-  int place = lo + __reduce_add_sync(0xffffffffu, lane < warp ? warp_a[lane & (kBSWarps - 1)] : 0) + min(eq_before, need);
+  int eq_before = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_b[lane & (kWarps - 1)] : 0);
+  int place = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_a[lane & (kWarps - 1)] : 0) + min(eq_before, need);
   each([&](int r, bool in, uint32_t k) {
     const uint32_t below = (1u << lane) - 1u;
     const uint32_t eqm = __ballot_sync(0xffffffffu, in && k == thr);
     const bool take = in && (k > thr || (k == thr && eq_before + __popc(eqm & below) < need));
     const uint32_t tm = __ballot_sync(0xffffffffu, take);
-    if (take) out[place + __popc(tm & below)] = from + 32 * r + lane;
+    if (take) put(place + __popc(tm & below), from + 32 * r + lane);
     place += __popc(tm);
     eq_before += __popc(eqm);
   });
+}
+// What of a unit's list is known without scores: the first and the last blocks, -1 past the end, the count.
+template <int kThreads>
+__device__ __forceinline__ void write_known(int* out, int* count, int stride, int lo, int need, int hi, int nb) {
+  const int total = lo + need + nb - hi;
+  for (int i = threadIdx.x; i < stride; i += kThreads) {
+    if (i < lo) out[i] = i;
+    else if (i >= total) out[i] = -1;
+    else if (i >= lo + need) out[i] = hi + (i - lo - need);
+  }
+  if (threadIdx.x == 0) *count = total;
+}
+
+// One CTA per unit.
+constexpr int kBSThreads = 512;
+template <int kKeys>
+__global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectParams p) {
+  __shared__ SelectSmem<kBSThreads> sm;
+  step_release();
+  const int unit = blockIdx.x;
+  const int b = unit / p.units_per_seq, u = unit % p.units_per_seq;
+  const int tid = threadIdx.x;
+  const int t = min(max(__ldg(p.seq_lens + b), 0), p.max_len);
+  const int nb = (t + kBlockRows - 1) / kBlockRows;
+  const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent), need = min(p.top, hi - lo);
+  int* out = p.out_blocks + (long long)unit * p.stride;
+  write_known<kBSThreads>(out, p.out_count + unit, p.stride, lo, need, hi, nb);
+  sm.hist[2 * tid] = 0;
+  sm.hist[2 * tid + 1] = 0;
+  if (tid == 0) sm.cands = 0;
+  step_wait();
+  select_middle<kBSThreads, kKeys>(p.scores + ((long long)b * p.num_q_heads + u * p.heads_per_unit) * p.ld, lo, hi, need, sm,
+                                   [&](int place, int blk) { out[lo + place] = blk; });
 }
 
 // ------------------------------------------------------------------------------- attention
@@ -516,6 +531,11 @@ struct BlockAttnParams {
   // takes the lists' middle part only, `top` entries at most
   int fixed, sink, recent, top;
   BoundsDev bd;             // and it recomputes the bounds of the last block
+  // kSelect: the kernel before this one is the scores', and every CTA selects for itself
+  const float* scores;
+  int ld;
+  int* out_blocks;          // = blocks, written by the first CTA of a unit
+  int* out_count;
   float* partials;          // [B][Hq][splits][kPartStride]
   unsigned int* tickets;
   __nv_bfloat16* out;
@@ -523,9 +543,16 @@ struct BlockAttnParams {
   uint32_t* flags;
 };
 
-template <bool kWide>
+// kSelect (steps over at most kSelectKeys * kTThreads blocks, kSelectTop of them to select): every CTA selects for itself,
+// once the scores are there, and there is no kernel for it.  32 lists, us a step: 9.0 against 9.7 with 2047 positions, 9.6 against
+// 9.9 with 8191 (issued call by call: 10.3 against 12.0 and 11.3 against 12.1); 256 lists with 8191: 37.3 against 38.7.
+// With 16000 positions, eight keys a thread, four warps take longer than sixteen and a launch: 11.9 against 11.2.
+constexpr int kSelectKeys = 4, kSelectTop = 256;
+template <bool kWide, bool kSelect>
 __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParams p) {
   constexpr int kTiles = kWide ? 2 : 1;
+  __shared__ SelectSmem<kSelect ? kTThreads : 32> sm_select;
+  __shared__ int sm_list[kSelect ? kSelectTop : 1];
   extern __shared__ __align__(128) unsigned char g_smem[];
   __shared__ float sm_m[kTWarps][16], sm_l[kTWarps][16], sm_lt[kTWarps][16];
   __shared__ bool is_last;
@@ -560,6 +587,12 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   // two passes over the ring: the blocks that are known (a step), then the listed ones
   const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent);
   const int worker = split * kTWarps + warp, workers = p.splits * kTWarps;
+  if constexpr (kSelect) {
+    if (split == 0) write_known<kTThreads>(p.out_blocks + unit * p.stride, p.out_count + unit, p.stride, lo, min(p.top, hi - lo), hi, nb);
+    sm_select.hist[2 * tid] = 0;
+    sm_select.hist[2 * tid + 1] = 0;
+    if (tid == 0) sm_select.cands = 0;
+  }
   for (int pass = p.fixed ? 0 : 1; pass < 2; ++pass) {
     int cnt;
     if (pass == 0) {
@@ -569,6 +602,13 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
       if (p.fixed) {
         cnt = min(p.top, hi - lo);
         list += lo;
+        if constexpr (kSelect) {
+          select_middle<kTThreads, kSelectKeys>(p.scores + (long long)unit0 * p.ld, lo, hi, cnt, sm_select, [&](int place, int blk) {
+            sm_list[place] = blk;
+            if (split == 0) p.out_blocks[unit * p.stride + lo + place] = blk;
+          });
+          __syncthreads();
+        }
       } else {
         cnt = min(max(__ldcg(p.count + unit), 0), p.stride);
       }
@@ -583,7 +623,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
       const int j = grp * 32 + lane;
       if (j >= nstages) return -1;
       if (pass == 0) return start + j < lo ? start + j : hi + start + j - lo;
-      const int blk = __ldcg(list + start + j);
+      const int blk = kSelect ? sm_list[start + j] : __ldcg(list + start + j);
       if ((unsigned)blk >= (unsigned)nb) {
         atomicOr(p.flags, kFlagBadIndex);
         return -1;

@@ -349,6 +349,35 @@ def test_empty_batch_and_lengths_out_of_range(cuda_device):
     ctx.close()
 
 
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("cap,top", [(8192, 1), (8192, 255), (8192, 256), (8192, 257), (8192, 600), (8208, 16), (48, 2)])
+def test_a_step_selects_as_block_topk_does(cuda_device, cap, top, shared):
+    """On both sides of the sizes up to which the attention kernel selects for itself; a zero query ties all blocks."""
+    group, lens = 2, [cap, cap - 7, 33, 0]
+    cache = Cache(4, 2, cap, True, cuda_device, seed=cap + top)
+    ctx = make_ctx(cache, group)
+    cache.place(random_rows(4, 2, cap, cap + top), lens)
+    ctx.block_bounds(cache.view(), cache.bounds(), 4)
+    q = torch.randn(4, 4, 128, generator=torch.Generator().manual_seed(top)).to(torch.bfloat16)
+    q[1, 1], q[1, 2:] = 0, 0
+    q = q.to(cuda_device)
+    sched = P.make_block_schedule(top, 1, 2, P.PRHS_GROUP_SETS if shared else 0)
+    units = 2 if shared else 4
+    got, want = ((torch.full((4, units, top + 3), 7, dtype=torch.int32, device=cuda_device),
+                  torch.full((4, units), 7, dtype=torch.int32, device=cuda_device)) for _ in range(2))
+    out, lse = torch.empty_like(q), torch.empty(4, 4, device=cuda_device)
+    for _ in range(2):
+        ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, 4, out, lse, *got)
+    ctx.block_topk(q, cache.view(), cache.bounds(), sched, 4, *want)
+    assert ctx.check() == 0
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    sets = ref_sets(cache, np64(q), lens, group, top, 1, 2, shared)
+    for (b, u), blocks in sets.items():
+        assert got[0][b, u, : int(got[1][b, u])].tolist() == list(blocks)
+    check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    ctx.close()
+
+
 def test_a_step_leaves_the_bounds_of_an_impossible_length(cuda_device):
     """A step writes bounds of last blocks only, and none for a length that is cut."""
     cache = Cache(3, 2, 64, True, cuda_device, seed=5)
