@@ -209,7 +209,7 @@ struct ByteKvAttnParams {
   const int* count;         // [B][Hq]
   int idx_stride;
   int batch, num_q_heads, group_size;
-  int deal;                 // kRuns, kParts, kWhole
+  int deal;                 // kRuns (the kernel decides), kParts, kWhole
   int max_len;              // lengths outside [0, max_len] are cut to it (and recorded)
   int sm_count;             // runs may be short while every SM has one CTA at most
   float* partials;          // [CTA][2][heads per unit][kPartStride]
@@ -294,17 +294,22 @@ __device__ __forceinline__ float load_query_f16(const __nv_bfloat16* q, bool has
 
 // Work.  A unit is a (sequence, KV head), its items the whole blocks; or (lists) a (sequence, query head), its items
 // groups of sixteen entries, as many as a list can have (idx_stride: nobody has to look through all counts).
-// A unit counts as at least one item (its open block, or nothing, still has to be written).  Three ways to deal
+// A unit counts as at least one item (its open block, or nothing, still has to be written).  Four ways to deal
 // units to CTAs:
 //   runs    the blocks of all units, laid end to end, in equal runs, whatever the lengths: a run may cover the end
 //           of one unit and the beginning of the next.  A CTA holds at most two parts of units that it shares with
 //           its neighbours; whole units are finished on the spot.  (With an even split of every unit a ragged
 //           batch waited for its longest sequence: 32 sequences of 2K to 16K, 156 us.)
-//   parts   where units are few against the CTAs (at most an eighth; lists, at most half): every unit in even parts,
-//           one part per CTA.  A CTA that crosses into a second unit pays its start and end twice (8 KV heads of
-//           2047 positions: 20 us against 12 us), and what the rounding wastes is small.
-//   whole   other lists: one CTA per unit (256 lists of 1838 entries: 29 us; in runs, 34 us)
-constexpr int kRuns = 0, kParts = 1, kWhole = 2;
+//   parts   every unit in even parts, one part per CTA, where there are CTAs for that and the longest part is no
+//           longer than a run and k8Crossing: a CTA that crosses into a second unit pays its start and end twice.
+//           (8 KV heads of 2047 positions: 20 us in runs, 12 in parts.  32 x 8 heads of 500: 18.8 and 12.2; of 980:
+//           19.9 and 18.7; of 1809: 29.3 and, with k8Crossing = 48, 31.  10 x 8 of 140 for 16 heads: 39 and 10.3.)
+//   units   as runs, but a CTA takes whole units, those that begin in its run, where none is longer than k8Crossing
+//           (58 x 32 heads of 300 positions: 44.9 us in runs, 41.2)
+//   whole   lists, where two CTAs for each do not fit: one CTA per unit (256 lists of 1838 entries: 29 us; in runs, 34 us)
+// The host's choice is runs, parts or whole; for runs the kernel, which knows the lengths, decides between the first three.
+constexpr int kRuns = 0, kParts = 1, kWhole = 2, kUnits = 3;
+constexpr int k8Crossing = 32;               // blocks in the time that a second start and end take
 // items per CTA at least: below, a merge costs more than the shorter part saves.  Where the items are so few that
 // runs of the short kind give no SM two CTAs, the short kind: nothing else would use the idle SMs
 // (8 KV heads of 2047 positions: 8.5 us against 9.3; of 500, 8.1 against 9.2.  With the short kind everywhere 8192
@@ -353,14 +358,21 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
   const int list_items = kList ? max(1, (p.idx_stride + kBlockRows - 1) / kBlockRows) : 0;
   int seq = cta, sub = 0, seg_lo = 0, part = 0, parts = 1;
   int run_end = 1, share = 1, unit_at = 0;
-  if (p.deal != kWhole) {
-    int before = 0;
-    const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, blocks_of);
+  int deal = p.deal;
+  if (deal != kWhole) {
+    int before = 0, longest = list_items;
+    const int total = kList ? units * list_items : count_items(p.kv.seq_lens, p.batch, num_kv, blocks_of, &longest);
     // no shorter than the smallest run or a unit; parts: as many as fit with every unit rounded up
-    const int ctas = p.deal == kParts ? (int)gridDim.x - units : (int)gridDim.x;
-    const int min_run = total <= k8ShortRun * p.sm_count ? k8ShortRun : k8MinRun<kList>;
-    share = max((total + ctas - 1) / ctas, min(min_run, (total + units - 1) / units));
-    if (p.deal == kParts) {
+    const int min_run = total <= k8ShortRun * p.sm_count ? k8ShortRun : k8MinRun<kList>, ctas = (int)gridDim.x;
+    auto share_of = [&](int n) { return max((total + n - 1) / n, min(min_run, (total + units - 1) / units)); };
+    if (!kList) share = share_of(ctas);
+    if (units <= ctas) {
+      const int even = units < ctas ? share_of(ctas - units) : longest;
+      if (kList || min(even, longest) <= share + k8Crossing) { deal = kParts; share = even; }
+    } else if (longest <= k8Crossing) {
+      deal = kUnits;
+    }
+    if (deal == kParts) {
       const int most = share;
       auto count = [&](int t) { return (blocks_of(t) + most - 1) / most; };
       if (kList) {
@@ -368,6 +380,10 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
         if (cta >= units * parts) return;
         seq = cta / parts;
         part = cta - seq * parts;
+      } else if (longest <= share) {             // one part each
+        if (cta >= units) return;
+        seq = cta / num_kv;
+        sub = cta - seq * num_kv;
       } else {
         if (!find_item(p.kv.seq_lens, p.batch, num_kv, count, cta, &seq, &before)) return;     // more CTAs than parts
         parts = count(__ldg(p.kv.seq_lens + seq));
@@ -383,6 +399,12 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       sub = (at - before) / w;
       unit_at = before + sub * w;
       seg_lo = at - unit_at;
+      if (deal == kUnits && seg_lo > 0) {        // begun by the CTA before
+        unit_at += w;
+        if (unit_at >= run_end) return;
+        seg_lo = 0;
+        if (++sub == num_kv) { sub = 0; ++seq; }
+      }
     }
   }
 
@@ -399,13 +421,13 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
     // items that have rows; parts and CTAs behind the last of them have nothing to do
     const int live = kList ? (listed + kBlockRows - 1) / kBlockRows : whole / kBlockRows;
     int first_cta = cta, seg_hi = w;
-    if (p.deal == kParts) {
+    if (deal == kParts) {
       const int per = (w + parts - 1) / parts;             // parts * per >= w > (parts - 1) * per where parts = ceil(w / share)
       seg_lo = min(part * per, w);
       seg_hi = min(seg_lo + per, w);
       first_cta = cta - part;
       if (kList) parts = max(1, (live + per - 1) / per);
-    } else if (!kList && p.deal == kRuns) {
+    } else if (deal == kRuns) {
       seg_hi = min(w, run_end - unit_at);
       first_cta = unit_at / share;
       part = cta - first_cta;
@@ -739,7 +761,7 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
     finish_unit<k8Warps>(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
                 p.out, p.out_lse, unit0, &is_last);
     unit_at += w;
-    if (kList || p.deal != kRuns || unit_at >= run_end) return;
+    if (kList || deal == kParts || unit_at >= run_end) return;
     seg_lo = 0;
     if (++sub == num_kv) { sub = 0; ++seq; }
     __syncthreads();                           // the ring and the partials in it are used again

@@ -102,13 +102,14 @@ prhs_status launch_bytekv_attn(prhs_ctx* c, const void* q, const ByteKvDev& kv, 
   const int slots = (idx ? Shape8<true, false>::kCtasPerSm : Shape8<false, false>::kCtasPerSm) * c->sm_count;
   const int min_run = idx ? k8MinRun<true> : k8MinRun<false>;
   const long long units = (long long)batch * (idx ? c->cfg.num_q_heads : c->cfg.num_kv_heads);
-  const long long unit_max = std::max(1, (max_count + kBlockRows - 1) / kBlockRows);
+  const long long unit_max = std::max(1, (max_count + (idx ? kBlockRows - 1 : 0)) / kBlockRows);       // items of a unit
   if (units * unit_max >= (1ll << 30))
     return fail(c, PRHS_ERR_UNSUPPORTED, "units times their largest length above 2^34: pass a smaller max_seq_len or idx_stride");
-  p.deal = (idx ? 2 : 8) * units <= slots ? kParts : idx ? kWhole : kRuns;
+  p.deal = !idx ? kRuns : 2 * units <= slots ? kParts : kWhole;
   p.sm_count = c->sm_count;
   const long long few = std::min<long long>(c->sm_count, units * ((unit_max + k8ShortRun - 1) / k8ShortRun));
-  const long long full = std::max(few, units * ((unit_max + min_run - 1) / min_run)) + (p.deal == kParts ? units : 0);
+  const long long full = std::max(few, units * ((unit_max + min_run - 1) / min_run)) +
+                         (p.deal != kWhole && units < slots && unit_max > k8ShortRun ? units : 0);      // rounding of parts
   const int ctas = (int)(p.deal == kWhole ? units : std::min<long long>(slots, full));
   const dim3 grid(ctas);
   {

@@ -12,13 +12,22 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return y;
 }
 
-// Items are laid out sequence after sequence, heads * f(length) each.  Warp-collective: their number.
+// Items are laid out sequence after sequence, heads * f(length) each.  Warp-collective: their number, and the largest f.
 template <typename F>
-__device__ __forceinline__ int count_items(const int* seq_lens, int batch, int heads, F f) {
-  if (batch == 1) return heads * f(__ldg(seq_lens));
-  int sum = 0;
+__device__ __forceinline__ int count_items(const int* seq_lens, int batch, int heads, F f, int* longest = nullptr) {
+  if (batch == 1) {
+    const int w = f(__ldg(seq_lens));
+    if (longest) *longest = w;
+    return heads * w;
+  }
+  int sum = 0, most = 0;
 #pragma unroll 4
-  for (int b = threadIdx.x & 31; b < batch; b += 32) sum += f(__ldg(seq_lens + b));
+  for (int b = threadIdx.x & 31; b < batch; b += 32) {
+    const int w = f(__ldg(seq_lens + b));
+    sum += w;
+    most = max(most, w);
+  }
+  if (longest) *longest = __reduce_max_sync(0xffffffffu, most);
   return heads * __reduce_add_sync(0xffffffffu, sum);
 }
 // Warp-collective: the sequence that holds item x (*b) and the number of items before it; false where x lies past the end.

@@ -387,6 +387,25 @@ def test_many_ragged_sequences(cuda_device, heads, group, batch):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group,batch,paged", [(8, 2, 50, True), (8, 1, 60, False), (8, 16, 50, False), (4, 16, 10, True)])
+def test_short_sequences_beside_long_ones(cuda_device, heads, group, batch, paged):
+    # runs that cross units with the units below and above the number of CTAs; few short units, a CTA each
+    lens = torch.randint(0, 100, (batch,), generator=torch.Generator().manual_seed(4)).tolist()
+    cap = 100 if batch == 10 else 713
+    if cap > 100:
+        lens[3], lens[-1], lens[-2] = 713, 704, 0
+    cache = Cache("e5m2", batch, heads, cap, paged, cuda_device)
+    ctx = make_ctx(cache, group)
+    fill(ctx, cache, lens)
+    q = torch.randn(batch, heads * group, 128, generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    for _ in range(2):
+        ctx.bytekv_decode_attn(q, cache.view(), batch, out, lse)
+    assert ctx.check() == 0
+    check_dense(ctx, cache, lens, group, q, out, lse)
+    ctx.close()
+
+
 @pytest.mark.parametrize("heads,group,batch,stride", [(4, 4, 16, 70), (2, 1, 3, 1500), (4, 8, 2, 900)])
 def test_lists_in_one_cta_and_in_parts(cuda_device, heads, group, batch, stride):
     # 256 units: one CTA each; few units: even parts, with counts from nothing to the whole stride
