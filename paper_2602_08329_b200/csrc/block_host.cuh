@@ -7,10 +7,12 @@ namespace {
 constexpr int kMaxBlocks = kMaxContext / kBlockRows;
 
 cudaError_t block_set_attributes() {
-  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<false, true>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true, true>, kTSmemBytes},
+  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false, false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true, false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<false, true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true, true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<false, false, true>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<true, false, true>, kTSmemBytes},
                                                            {(const void*)block_score_kernel<false>, kScoreSmemBytes},
                                                            {(const void*)block_score_kernel<true>, kScoreSmemBytes}};
   for (const auto& k : all) {
@@ -134,11 +136,6 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
   return PRHS_OK;
 }
 
-// Whether a step's attention kernel selects for itself (kSelect in block_sparse.cuh has both sides).
-bool step_selects_in_attn(const prhs_block_schedule* s, int max_t) {
-  return (max_t + kBlockRows - 1) / kBlockRows <= kSelectKeys * kTThreads && s->top_blocks <= kSelectTop;
-}
-
 // Splits of a list of blocks.  In cycles, as measured: a warp works one block off in about 900; 8 KB take 2.4 of the HBM
 // stream; of the smaller of the two a quarter stays visible; a CTA's start and end cost about 3000, a merge of parts
 // 4500, and 1500 for every further batch of parts (finish_unit).  us per step with 1, 2, 4, 8, 16 splits:
@@ -146,27 +143,48 @@ bool step_selects_in_attn(const prhs_block_schedule* s, int max_t) {
 //   32 lists of 73                       20.0 19.3 17.6 16.4 20.4     64 sets                      38.2 33.6 33.4 37.8
 //   64 lists of 73                       22.9 22.0 20.3 24.4 31.4     32 sets                      32.4 27.0 23.2 21.5 26.0
 //   256 lists of 73                      60 72                        8 sets                       28.7 23.6 19.5 17.8 17.0
+// Or a warp per unit (0 splits): no start and end for every four warps, where units are many and lists short; at least one such
+// CTA per SM, and a tenth to gain, since the last of these longer CTAs leave the SMs unevenly used.  us, splits and warps:
+//   608 lists of 11 blocks  26.6 23.2    1856  70.8 65.1    512  20.3 22.1    1024 lists of 19  35.1 26.7    3840  117 101
+//   768 lists of 73         88.4 91.2    1856  195 206
 int block_splits(const prhs_ctx* c, int units, int blocks, int heads) {
   const int slots = 2 * c->sm_count;
   const int merged = 16 * std::max(1, kTWarps / heads);          // parts of a head that are merged at a time
   const double stream = 2.4 * units * blocks;
+  auto cost_of = [&](long long ctas, int per_warp) {
+    const double waves = (double)((ctas + slots - 1) / slots), work = waves * per_warp * 900.0;
+    return std::max(work, stream) + 0.25 * std::min(work, stream) + waves * 3000.0;
+  };
   int best = 1;
   double best_cost = 1e30;
   for (int s = 1; s <= kMaxSplits; ++s) {
     const int per_warp = (blocks + s * kTWarps - 1) / (s * kTWarps);
-    const double waves = (double)(((long long)units * s + slots - 1) / slots);
-    const double work = waves * per_warp * 900.0;
-    const double cost = std::max(work, stream) + 0.25 * std::min(work, stream) + waves * 3000.0 +
-                        (s > 1 ? 4500.0 + 1500.0 * ((s + merged - 1) / merged - 1) : 0.0);
+    const double cost = cost_of((long long)units * s, per_warp) + (s > 1 ? 4500.0 + 1500.0 * ((s + merged - 1) / merged - 1) : 0.0);
     if (cost < best_cost * 0.999) { best_cost = cost; best = s; }
     if (per_warp == 1) break;
   }
-  return best;
+  const int own = (units + kTWarps - 1) / kTWarps;
+  return own >= c->sm_count && cost_of(own, blocks) < 0.92 * best_cost ? 0 : best;
+}
+
+struct BlockPlan {
+  int splits;      // 0: a warp per unit
+  bool select;     // the attention kernel selects for itself (kSelect in block_sparse.cuh has both sides)
+};
+BlockPlan block_plan(const prhs_ctx* c, int batch, uint32_t flags, int stride, int max_t, const prhs_block_schedule* step) {
+  const int heads = block_shared(c, flags) ? c->gq : 1, units = batch * (c->cfg.num_q_heads / heads);
+  const int blocks = std::max(1, (max_t + kBlockRows - 1) / kBlockRows);
+  // a unit's blocks at most; a step knows more than the width of the table
+  const int listed = step ? std::min(stride, step->sink_blocks + step->top_blocks + step->recent_blocks) : stride;
+  BlockPlan plan;
+  plan.splits = block_splits(c, units, std::min(listed, blocks), heads);
+  plan.select = step && plan.splits > 0 && blocks <= kSelectKeys * kTThreads && step->top_blocks <= kSelectTop;
+  return plan;
 }
 
 prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const int32_t* blocks, const int32_t* count, int stride,
-                              uint32_t flags, int max_t, int batch, void* out, float* out_lse, const prhs_block_schedule* step, const BoundsDev* bd,
-                              cudaStream_t st) {
+                              uint32_t flags, int max_t, int batch, void* out, float* out_lse, const BlockPlan& plan, const prhs_block_schedule* step,
+                              const BoundsDev* bd, cudaStream_t st) {
   const bool shared = block_shared(c, flags);
   BlockAttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -178,16 +196,14 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   p.units_per_seq = c->cfg.num_q_heads / p.heads_per_unit;
   p.num_q_heads = c->cfg.num_q_heads;
   p.group_size = c->gq;
-  // a unit's blocks at most; a step knows more than the width of the table
-  const int listed = step ? std::min(stride, step->sink_blocks + step->top_blocks + step->recent_blocks) : stride;
-  p.splits = block_splits(c, batch * p.units_per_seq, std::min(listed, std::max(1, (max_t + kBlockRows - 1) / kBlockRows)), p.heads_per_unit);
+  p.splits = std::max(plan.splits, 1);
+  p.units = batch * p.units_per_seq;
   p.max_len = max_t;
   p.fixed = step ? 1 : 0;
   p.sink = step ? step->sink_blocks : 0;
   p.recent = step ? step->recent_blocks : 0;
   p.top = step ? step->top_blocks : 0;
   p.bd = bd ? *bd : BoundsDev{};
-  const bool select = step && step_selects_in_attn(step, max_t);
   p.scores = c->scores;
   p.ld = c->ld;
   p.out_blocks = const_cast<int32_t*>(blocks);
@@ -200,11 +216,12 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   {
     LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
     // `step`: the lists are this step's, from the kernel before; a caller's own may come from any kernel (ordinary launch)
-    const dim3 grid(p.splits, p.units_per_seq, batch);
-    const bool wide = p.heads_per_unit > 8;
-    const cudaError_t e = launch_ordered(select ? (wide ? block_attn_kernel<true, true> : block_attn_kernel<false, true>)
-                                                : (wide ? block_attn_kernel<true, false> : block_attn_kernel<false, false>),
-                                         grid, kTThreads, kTSmemBytes, st, p, step ? 1 : 0);
+    const bool own = plan.splits == 0, wide = p.heads_per_unit > 8;
+    const dim3 grid = own ? dim3((p.units + kTWarps - 1) / kTWarps) : dim3(p.splits, p.units_per_seq, batch);
+    const auto kernel = own ? (wide ? block_attn_kernel<true, false, true> : block_attn_kernel<false, false, true>)
+                        : plan.select ? (wide ? block_attn_kernel<true, true, false> : block_attn_kernel<false, true, false>)
+                                      : (wide ? block_attn_kernel<true, false, false> : block_attn_kernel<false, false, false>);
+    const cudaError_t e = launch_ordered(kernel, grid, kTThreads, kTSmemBytes, st, p, step ? 1 : 0);
     PRHS_CUDA(c, e);
   }
   return PRHS_OK;
@@ -272,7 +289,8 @@ prhs_status prhs_block_decode_attn(prhs_ctx* ctx, const void* q, const prhs_kv_v
   prhs_status rc = check_q_out(ctx, q, out, batch);
   if (rc == PRHS_OK) rc = check_block_view(ctx, kv, batch, &dv, &max_t);
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse, nullptr, nullptr, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, blocks, count, blocks_stride, flags, max_t, batch, out, out_lse,
+                           block_plan(ctx, batch, flags, blocks_stride, max_t, nullptr), nullptr, nullptr, as_stream(stream));
 }
 
 prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
@@ -290,10 +308,11 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
   if (rc != PRHS_OK) return rc;
   if (sched->recent_blocks < 1)
     return fail(ctx, PRHS_ERR_INVALID_ARG, "block step: recent_blocks must be >= 1 (the last block is attended over, not scored)");
-  const bool select = !step_selects_in_attn(sched, max_t);
-  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, select, as_stream(stream));
+  const BlockPlan plan = block_plan(ctx, batch, sched->flags, blocks_stride, max_t, sched);
+  rc = launch_block_topk(ctx, q, dv, bd, sched, max_t, batch, out_blocks, blocks_stride, out_count, !plan.select, as_stream(stream));
   if (rc != PRHS_OK) return rc;
-  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, sched, &bd, as_stream(stream));
+  return launch_block_attn(ctx, q, dv, out_blocks, out_count, blocks_stride, sched->flags, max_t, batch, out, out_lse, plan, sched, &bd,
+                           as_stream(stream));
 }
 
 }  // extern "C"

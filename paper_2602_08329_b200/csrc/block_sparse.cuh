@@ -525,7 +525,7 @@ struct BlockAttnParams {
   const int* blocks;        // [B][units][stride]
   const int* count;
   int stride, units_per_seq;
-  int num_q_heads, group_size, heads_per_unit, splits;
+  int num_q_heads, group_size, heads_per_unit, splits, units;
   int max_len;
   // a step knows without the selection that blocks [0, sink) and the last `recent` are attended over (fixed = 1): it
   // takes the lists' middle part only, `top` entries at most
@@ -548,22 +548,27 @@ struct BlockAttnParams {
 // 9.9 with 8191 (issued call by call: 10.3 against 12.0 and 11.3 against 12.1); 256 lists with 8191: 37.3 against 38.7.
 // With 16000 positions, eight keys a thread, four warps take longer than sixteen and a launch: 11.9 against 11.2.
 constexpr int kSelectKeys = 4, kSelectTop = 256;
-template <bool kWide, bool kSelect>
+// kOwn: a warp per unit, which it takes alone from start to end, four to a CTA; grid (units / 4).
+template <bool kWide, bool kSelect, bool kOwn>
 __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParams p) {
   constexpr int kTiles = kWide ? 2 : 1;
+  static_assert(!(kSelect && kOwn), "a selection takes a CTA");
   __shared__ SelectSmem<kSelect ? kTThreads : 32> sm_select;
   __shared__ int sm_list[kSelect ? kSelectTop : 1];
   extern __shared__ __align__(128) unsigned char g_smem[];
   __shared__ float sm_m[kTWarps][16], sm_l[kTWarps][16], sm_lt[kTWarps][16];
   __shared__ bool is_last;
-  const int split = blockIdx.x, u = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int own = blockIdx.x * kTWarps + warp;
+  if (kOwn && own >= p.units) return;
+  const int split = kOwn ? 0 : blockIdx.x, b = kOwn ? own / p.units_per_seq : blockIdx.z;
+  const int u = kOwn ? own - b * p.units_per_seq : blockIdx.y;
   const int gq = p.heads_per_unit;
   const int head0 = u * gq, kvh = head0 / p.group_size;
   const int unit0 = b * p.num_q_heads + head0;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2;
   const int given = __ldg(p.kv.seq_lens + b), t = min(max(given, 0), p.max_len);
-  if (t != given && tid == 0) atomicOr(p.flags, kFlagBadLength);
+  if (t != given && (kOwn ? lane : tid) == 0) atomicOr(p.flags, kFlagBadLength);
   const int nb = (t + kBlockRows - 1) / kBlockRows;
   const long long unit = (long long)b * p.units_per_seq + u;
   const int* list = p.blocks + unit * p.stride;
@@ -576,7 +581,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   SoftBf st[kTiles][2];
 
   // a step writes the bounds of the last block, whose score nothing reads: here and now, while the selection runs
-  if (p.fixed && split == 0 && head0 % p.group_size == 0 && warp == kTWarps - 1 && nb > 0 && t == given) {
+  if (p.fixed && split == 0 && head0 % p.group_size == 0 && (kOwn || warp == kTWarps - 1) && nb > 0 && t == given) {
     long long row, bi;
     if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
       bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
 
   // two passes over the ring: the blocks that are known (a step), then the listed ones
   const int lo = min(p.sink, nb), hi = max(lo, nb - p.recent);
-  const int worker = split * kTWarps + warp, workers = p.splits * kTWarps;
+  const int worker = kOwn ? 0 : split * kTWarps + warp, workers = kOwn ? 1 : p.splits * kTWarps;
   if constexpr (kSelect) {
     if (split == 0) write_known<kTThreads>(p.out_blocks + unit * p.stride, p.out_count + unit, p.stride, lo, min(p.top, hi - lo), hi, nb);
     sm_select.hist[2 * tid] = 0;
@@ -702,6 +707,18 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
     if (i + 1 < nstages) stage(i + 1, SlotC<1>{});
     cp_async_wait<0>();
     __syncwarp();
+  }
+  if constexpr (kOwn) {                      // the warp's ring is free: it takes the unit's sums, a head in a row
+    float* mine = reinterpret_cast<float*>(g_smem + warp * (kTStages * kTStageBytes));
+    store_partial_bf16<kTiles>(o, st, gq, mine, sm_m[warp], sm_l[warp], sm_lt[warp]);
+    __syncwarp();
+    for (int h = 0; h < gq; ++h) {
+      Merged r;
+      r.m = sm_m[warp][h];
+      r.add(r.m, sm_l[warp][h], sm_lt[warp][h], reinterpret_cast<const float4*>(mine + h * kHeadDim)[lane]);
+      r.store(p.out, p.out_lse, unit0 + h);
+    }
+    return;
   }
   __syncthreads();                         // the ring is free: it takes the warps' partials
   float* sm_o = reinterpret_cast<float*>(g_smem);

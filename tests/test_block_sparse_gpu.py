@@ -378,6 +378,34 @@ def test_a_step_selects_as_block_topk_does(cuda_device, cap, top, shared):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group,shared", [(8, 2, False), (16, 2, True), (10, 16, True)])
+def test_many_short_lists(cuda_device, heads, group, shared):
+    """So many units that a warp takes one alone; empty sequences and lists among them, the last CTA not full."""
+    batch = 61
+    lens = torch.randint(1, 150, (batch,), generator=torch.Generator().manual_seed(3)).tolist()
+    lens[0], lens[7], lens[60] = 0, 1, 150
+    cache = Cache(batch, heads, 150, True, cuda_device, seed=9)
+    ctx = make_ctx(cache, group)
+    cache.place(random_rows(batch, heads, 150, 9), lens)
+    ctx.block_bounds(cache.view(), cache.bounds(), batch)
+    q = torch.randn(batch, heads * group, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    flags, units = (P.PRHS_GROUP_SETS, heads) if shared else (0, heads * group)
+    blocks, count = (torch.empty(batch, units, 6, dtype=torch.int32, device=cuda_device), torch.empty(batch, units, dtype=torch.int32, device=cuda_device))
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(3, 1, 2, flags), batch, out, lse, blocks, count)
+    assert ctx.check() == 0
+    sets = ref_sets(cache, np64(q), lens, group, 3, 1, 2, shared)
+    check_attention(cache, np64(q), lens, group, sets, shared, out, lse)
+    again, lse2 = torch.full_like(q, math.nan), torch.full_like(lse, math.nan)
+    ctx.block_decode_attn(q, cache.view(), blocks, count, batch, again, lse2, flags)
+    check_attention(cache, np64(q), lens, group, sets, shared, again, lse2)
+    count[7], count[-1, -1] = 0, 0
+    ctx.block_decode_attn(q, cache.view(), blocks, count, batch, again, lse2, flags)
+    assert ctx.check() == 0 and bool((again[7] == 0).all()) and bool((lse2[7] == -math.inf).all())
+    assert bool((again[-1, -1] == 0).all())
+    ctx.close()
+
+
 def test_a_step_leaves_the_bounds_of_an_impossible_length(cuda_device):
     """A step writes bounds of last blocks only, and none for a length that is cut."""
     cache = Cache(3, 2, 64, True, cuda_device, seed=5)
