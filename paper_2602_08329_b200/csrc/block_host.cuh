@@ -138,7 +138,7 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
 
 // Splits of a list of blocks.  In cycles, as measured: a warp works one block off in about 900; 8 KB take 2.4 of the HBM
 // stream; of the smaller of the two a quarter stays visible; a CTA's start and end cost about 3000, a merge of parts
-// 4500, and 1500 for every further batch of parts (finish_unit).  us per step with 1, 2, 4, 8, 16 splits:
+// 3000, and 1500 for every batch of parts of every four heads (finish_unit).  us per step with 1, 2, 4, 8, 16 splits:
 //   32 lists of 19 blocks (one user)      9.7 11.8 12.0 12.4 15.3     128 sets of 137 for 4 heads  52.4 53.6
 //   32 lists of 73                       20.0 19.3 17.6 16.4 20.4     64 sets                      38.2 33.6 33.4 37.8
 //   64 lists of 73                       22.9 22.0 20.3 24.4 31.4     32 sets                      32.4 27.0 23.2 21.5 26.0
@@ -149,7 +149,7 @@ prhs_status launch_block_topk(prhs_ctx* c, const void* q, const KvDev& kv, const
 //   768 lists of 73         88.4 91.2    1856  195 206
 int block_splits(const prhs_ctx* c, int units, int blocks, int heads) {
   const int slots = 2 * c->sm_count;
-  const int merged = 16 * std::max(1, kTWarps / heads);          // parts of a head that are merged at a time
+  const int merged = 16 * std::max(1, kTWarps / heads), rounds = (heads + kTWarps - 1) / kTWarps;     // a merge: parts at a time, heads
   const double stream = 2.4 * units * blocks;
   auto cost_of = [&](long long ctas, int per_warp) {
     const double waves = (double)((ctas + slots - 1) / slots), work = waves * per_warp * 900.0;
@@ -159,7 +159,7 @@ int block_splits(const prhs_ctx* c, int units, int blocks, int heads) {
   double best_cost = 1e30;
   for (int s = 1; s <= kMaxSplits; ++s) {
     const int per_warp = (blocks + s * kTWarps - 1) / (s * kTWarps);
-    const double cost = cost_of((long long)units * s, per_warp) + (s > 1 ? 4500.0 + 1500.0 * ((s + merged - 1) / merged - 1) : 0.0);
+    const double cost = cost_of((long long)units * s, per_warp) + (s > 1 ? 3000.0 + 1500.0 * rounds * ((s + merged - 1) / merged) : 0.0);
     if (cost < best_cost * 0.999) { best_cost = cost; best = s; }
     if (per_warp == 1) break;
   }
