@@ -410,7 +410,8 @@ prhs_status prhs_block_bounds(prhs_ctx* ctx, const prhs_kv_view* kv, const prhs_
  *   out_blocks device int32 [batch][units][blocks_stride], -1 past the count; units = Hq, or Hkv with
  *              PRHS_GROUP_SETS; blocks_stride >= min(top + sink + recent, ceil(max_seq_len / 16))
  *   out_count  device int32 [batch][units]
- * Bounds of all middle blocks must be up to date. */
+ * Bounds of all middle blocks must be up to date.  A t_b outside [0, max_seq_len] is cut to it and recorded
+ * (PRHS_FLAG_BAD_LENGTH). */
 prhs_status prhs_block_topk(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, const prhs_block_bounds_view* bounds,
                             const prhs_block_schedule* sched, int32_t batch, int32_t* out_blocks, int32_t blocks_stride,
                             int32_t* out_count, void* stream);

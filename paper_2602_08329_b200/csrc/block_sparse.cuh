@@ -173,9 +173,10 @@ __global__ void __launch_bounds__(kScoreWarps * 32) __maxnreg__(kWide ? 168 : kS
   const bool paged = p.kv.page_table != nullptr;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kScoreStages * kScoreStageBytes);
 
-  // this CTA's run of groups and the unit it begins in; a sequence of impossible length has no groups
+  // this CTA's run of groups and the unit it begins in; an impossible length is cut, as the selection cuts it
   const int max_len = p.max_len;
-  auto groups_of = [max_len](int t) { return t > max_len || t < 0 ? 0 : (t + kScoreRound * kBlockRows - 1) / (kScoreRound * kBlockRows); };
+  auto length_of = [max_len](int t) { return min(max(t, 0), max_len); };
+  auto groups_of = [length_of](int t) { return (length_of(t) + kScoreRound * kBlockRows - 1) / (kScoreRound * kBlockRows); };
   int b = 0, at = 0;
   const int total = count_items(p.kv.seq_lens, p.batch, num_kv, groups_of);
   const int share = max((total + (int)gridDim.x - 1) / (int)gridDim.x, kScoreWarps);
@@ -192,9 +193,8 @@ __global__ void __launch_bounds__(kScoreWarps * 32) __maxnreg__(kWide ? 168 : kS
   int g_lo = at - before - kvh * groups;
 
   while (true) {                                       // units of the run
-    const int t = __ldg(p.kv.seq_lens + b);
     const int head0 = kvh * gq;
-    const int nb = (t + kBlockRows - 1) / kBlockRows;
+    const int nb = (length_of(__ldg(p.kv.seq_lens + b)) + kBlockRows - 1) / kBlockRows;
     const int g_hi = min(groups, g_lo + run_end - at);
     const int rounds = max(0, (g_hi - g_lo - warp + kScoreWarps - 1) / kScoreWarps);     // groups g_lo + warp + 4r
     const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride;

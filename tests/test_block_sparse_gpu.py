@@ -430,6 +430,35 @@ def test_a_step_leaves_the_bounds_of_an_impossible_length(cuda_device):
     ctx.close()
 
 
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("cap", [640, 8208])
+def test_a_length_beyond_the_maximum_selects_as_the_maximum(cuda_device, paged, cap):
+    """A length that is cut has scores like any other: nothing of an earlier call's is ranked.  (8208: a kernel of its own selects.)"""
+    cache = Cache(3, 2, cap, paged, cuda_device, seed=cap)
+    ctx = make_ctx(cache, 2)
+    cache.place(random_rows(3, 2, cap, 11), [cap] * 3)
+    ctx.block_bounds(cache.view(), cache.bounds(), 3)
+    new = lambda: (torch.full((3, 4, 9), 7, dtype=torch.int32, device=cuda_device), torch.full((3, 4), 7, dtype=torch.int32, device=cuda_device))  # noqa: E731
+    out, lse = torch.empty(3, 4, 128, dtype=torch.bfloat16, device=cuda_device), torch.empty(3, 4, device=cuda_device)
+    sched = P.make_block_schedule(6, 1, 2)
+    before, q = (torch.randn(3, 4, 128, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).to(cuda_device) for i in range(2))
+    calls = (lambda q, lists: ctx.block_topk(q, cache.view(), cache.bounds(), sched, 3, *lists),
+             lambda q, lists: ctx.block_decode_step(q, cache.view(), cache.bounds(), sched, 3, out, lse, *lists))
+    want = ref_sets(cache, np64(q), [cap] * 3, 2, 6, 1, 2, False)
+    for call in calls:
+        cache.lens.fill_(cap)
+        call(before, new())                                              # other scores in the workspace
+        cache.lens.copy_(torch.tensor([cap, cap + 1, 1 << 30], dtype=torch.int32))
+        blocks, count = new()
+        call(q, (blocks, count))
+        with pytest.raises(P.PrhsError):
+            ctx.check()
+        for (b, u), w in want.items():
+            assert blocks[b, u].tolist() == w and int(count[b, u]) == len(w), (b, u)
+    check_attention(cache, np64(q), [cap] * 3, 2, want, False, out, lse)
+    ctx.close()
+
+
 def test_all_blocks_are_the_dense_attention(cuda_device):
     cache = Cache(2, 2, 700, False, cuda_device)
     ctx = make_ctx(cache, 2)
