@@ -357,8 +357,8 @@ typedef struct {
  *   new_lens      device int32 [batch], 0 <= new_lens[b] <= min(max_new, t_b); a sequence that breaks this, or whose
  *                 t_b exceeds max_seq_len, is left as it was and recorded (PRHS_FLAG_BAD_LENGTH)
  *   max_new       host-side upper bound of new_lens (sizes the launch)
- * A block with an infinity or a NaN is recorded (PRHS_FLAG_NONFINITE): infinities are stored as the largest code,
- * NaNs as NaN, and the block's scale follows the largest exponent. */
+ * A block with an infinity or a NaN is recorded (PRHS_FLAG_NONFINITE): infinities are stored as the largest code and give
+ * the block the scale 2^120 (e4m3) or 2^113 (e5m2), NaNs are stored as NaN and do not count for the scale. */
 prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const void* new_k, const void* new_v, int64_t stride_seq,
                             int64_t stride_head, int64_t stride_row, const int32_t* new_lens, int32_t max_new, int32_t batch,
                             void* stream);

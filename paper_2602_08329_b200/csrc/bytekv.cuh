@@ -56,13 +56,18 @@ __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t
 template <int kFmt>
 __device__ __forceinline__ bool quantise_block(const uint4 (&x)[8], uint8_t* codes, float* scale) {
   const int lane = threadIdx.x & 31;
-  uint32_t mx = 0u;                                 // two bf16 magnitudes: their bits order like the values
+  // the largest magnitude (two bf16 at a time: their bits order like the values)
+  auto largest = [&](auto of) {
+    uint32_t mx = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    mx = __vmaxu2(__vmaxu2(mx, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
-                  __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
-  uint32_t amax = max(mx & 0xffffu, mx >> 16);
-  amax = __reduce_max_sync(0xffffffffu, amax);
+    for (int i = 0; i < 8; ++i)
+      mx = __vmaxu2(__vmaxu2(mx, __vmaxu2(of(x[i].x & 0x7fff7fffu), of(x[i].y & 0x7fff7fffu))),
+                    __vmaxu2(of(x[i].z & 0x7fff7fffu), of(x[i].w & 0x7fff7fffu)));
+    return __reduce_max_sync(0xffffffffu, max(mx & 0xffffu, mx >> 16));
+  };
+  uint32_t amax = largest([](uint32_t w) { return w; });
+  const bool finite = amax < 0x7f80u;
+  if (amax > 0x7f80u) amax = largest([](uint32_t w) { return w & ~__vcmpgtu2(w, 0x7f807f80u); });    // NaNs do not count
   const int e = kFmt == kE4M3 ? scale_exponent<8, 96>(amax) : scale_exponent<15, 96>(amax);
   const float inv = pow2i(-e);
   if (lane == 0) *scale = pow2i(e);
@@ -77,7 +82,7 @@ __device__ __forceinline__ bool quantise_block(const uint4 (&x)[8], uint8_t* cod
     uint2 out = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
     *reinterpret_cast<uint2*>(codes + (2 * i + (lane >> 4)) * kRow8Bytes + (lane & 15) * 8) = out;
   }
-  return amax < 0x7f80u;
+  return finite;
 }
 
 struct ByteKvAppendParams {

@@ -163,6 +163,34 @@ def test_append_refuses_contradictory_lengths_and_records_nonfinite(cuda_device)
     ctx.close()
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_a_nan_leaves_the_rest_of_its_block_as_it_is(cuda_device, fmt):
+    """The scale is that of the numbers; a block of NaNs has the smallest; infinities keep the one that their exponent gives."""
+    cache = Cache(fmt, 1, 2, 64, False, cuda_device)
+    ctx = make_ctx(cache, 1)
+    rows = torch.randn(2, 1, 2, 64, 128, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    rows[0, 0, 0, 3, 7], rows[1, 0, 1, 17] = math.nan, math.nan
+    rows[0, 0, 1, 32:48], rows[1, 0, 0, 50, 9], rows[1, 0, 0, 51, 10] = math.nan, -math.inf, math.nan
+    cache.set_lens([64])
+    ctx.bytekv_append(rows[0].to(cuda_device), rows[1].to(cuda_device), cache.lens.clone(), cache.view(), 1)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    for w, name in enumerate("kv"):
+        for h in range(2):
+            for j in range(4):
+                x = rows[w, 0, h, 16 * j: 16 * j + 16].double().numpy()
+                codes, s = cache.block(name, 0, h, j)
+                if np.isinf(x).any():
+                    top = R.TOP[fmt][0]
+                    assert s == (2.0 ** 120 if fmt == "e4m3" else 2.0 ** 113) and codes[2, 9] == -top
+                    assert np.all(codes[~np.isinf(x) & ~np.isnan(x)] == 0)
+                else:
+                    want, ws = R.quantise(np.where(np.isnan(x), 0.0, x), fmt)
+                    assert s == ws and np.array_equal(codes[~np.isnan(x)], want[~np.isnan(x)]), (name, h, j)
+                assert np.array_equal(np.isnan(codes), np.isnan(x))
+    ctx.close()
+
+
 def test_bad_pages_are_skipped_and_recorded(cuda_device):
     cache = Cache("e4m3", 2, 2, 64, True, cuda_device)
     ctx = make_ctx(cache, 2)
