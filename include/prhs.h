@@ -364,8 +364,9 @@ prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const 
                             void* stream);
 
 /* prhs_dense_decode_attn over the 8-bit cache: attention over all i < t_b.  t_b = 0 gives a zero output row and
- * lse = -inf; a t_b outside [0, max_seq_len] is cut to it and recorded (PRHS_FLAG_BAD_LENGTH).  q and out are
- * 16-byte aligned and do not overlap. */
+ * lse = -inf; a t_b outside [0, max_seq_len] is cut to it and recorded (PRHS_FLAG_BAD_LENGTH).  A logit that is NaN or +inf
+ * makes the row and its lse NaN, as the formula has it (also in the calls below).  q and out are 16-byte aligned and do not
+ * overlap. */
 prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
                                  void* stream);
 

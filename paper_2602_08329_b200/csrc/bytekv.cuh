@@ -737,7 +737,7 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
         const int head = 8 * hh + 2 * tg + e;
-        if (g == 0) { sm_m[warp][head] = l > 0.f ? st[hh][e].m : -INFINITY; sm_l[warp][head] = l; sm_lt[warp][head] = l; }
+        if (g == 0) { sm_m[warp][head] = l == 0.f ? -INFINITY : st[hh][e].m; sm_l[warp][head] = l; sm_lt[warp][head] = l; }
         f[e] = __uint_as_float((uint32_t)min(max((int)st[hh][e].R + 127, 0), 254) << 23);     // 2^R
         if (head < gq) {
 #pragma unroll

@@ -68,7 +68,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 constexpr float kNoLogit = -3.0e38f;
 
 // One head's softmax bookkeeping in a lane: l sums the fp32 weights (log-sum-exp), lt the weights as rounded to bf16,
-// which is what divides the output.
+// which is what divides the output.  A logit that is NaN or +inf makes l and lt NaN, and they stay NaN: the maximum passes
+// over a NaN, so it is by the sums that a row's result is known to be NaN, and by l = 0 alone that a row is empty.
 struct SoftBf {
   float m = kNoLogit, l = 0.f, lt = 0.f;
 };
@@ -192,7 +193,7 @@ __device__ __forceinline__ void store_partial_bf16(const float (&o)[kTiles][8][4
       }
       const int head = 8 * hh + 2 * tg + e;
       if (head < heads) {
-        if (g == 0) { sm_m[head] = l > 0.f ? st[hh][e].m : -INFINITY; sm_l[head] = l; sm_lt[head] = lt; }
+        if (g == 0) { sm_m[head] = l == 0.f ? -INFINITY : st[hh][e].m; sm_l[head] = l; sm_lt[head] = lt; }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           sm_o[head * kHeadDim + 16 * c + g] = o[hh][c][e];
@@ -213,16 +214,14 @@ struct Merged {
   }
   __device__ __forceinline__ void add(float m2, float l2, float lt2, float4 x) {      // m2 <= m
     const float f = m2 > -INFINITY ? exp2f(m2 - m) : 0.f;
-    if (f > 0.f) {
-      l = fmaf(l2, f, l); lt = fmaf(lt2, f, lt);
-      o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
-    }
+    l = fmaf(l2, f, l); lt = fmaf(lt2, f, lt);           // a NaN passes a factor of zero
+    o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
   }
   __device__ __forceinline__ void store(__nv_bfloat16* out, float* out_lse, long long unit) const {
     const int lane = threadIdx.x & 31;
-    const float inv = lt > 0.f ? 1.f / lt : 0.f;
+    const float inv = lt == 0.f ? 0.f : 1.f / lt;
     *reinterpret_cast<uint2*>(out + unit * kHeadDim + lane * 4) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    if (lane == 0 && out_lse) out_lse[unit] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    if (lane == 0 && out_lse) out_lse[unit] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
 };
 
@@ -293,10 +292,8 @@ __device__ __forceinline__ void finish_unit(float* sm_o, float* sm_m, float* sm_
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
         const float fi = __shfl_sync(0xffffffffu, f, i);
-        if (fi > 0.f) {
-          r.o.x = fmaf(x[i].x, fi, r.o.x); r.o.y = fmaf(x[i].y, fi, r.o.y);
-          r.o.z = fmaf(x[i].z, fi, r.o.z); r.o.w = fmaf(x[i].w, fi, r.o.w);
-        }
+        r.o.x = fmaf(x[i].x, fi, r.o.x); r.o.y = fmaf(x[i].y, fi, r.o.y);
+        r.o.z = fmaf(x[i].z, fi, r.o.z); r.o.w = fmaf(x[i].w, fi, r.o.w);
       }
     }
 #pragma unroll

@@ -570,6 +570,84 @@ def test_steps_on_another_stream_and_two_graphs_of_one_context(cuda_device):
     ctx.close()
 
 
+# ------------------------------------------------------------------------------ not finite
+def mild(rows):
+    """Keys small enough that no weight vanishes."""
+    rows[0] *= 0.25
+    return rows
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("heads,group,shared,batch", [(2, 2, False, 2), (1, 12, True, 2), (8, 4, True, 60), (16, 2, False, 60)])
+def test_a_key_that_is_not_finite_shows(cuda_device, bad, heads, group, shared, batch):
+    """The softmax over a NaN, or over an infinite logit, is NaN: for the heads that meet it and for no other, however the
+    list is dealt (parts, whole units, a warp per unit)."""
+    lens = [400 - 3 * b for b in range(batch)]
+    cache = Cache(batch, heads, 400, True, cuda_device, seed=2)
+    ctx = make_ctx(cache, group)
+    rows = mild(random_rows(batch, heads, 400, 31))
+    q = torch.randn(batch, heads * group, 128, generator=torch.Generator().manual_seed(1)).abs().to(torch.bfloat16)
+    hit = [(0, 0, 37), (1, heads - 1, lens[1] - 1)]                       # an ordinary block, the open one
+    for b, h, i in hit:
+        rows[0, b, h, i, 5] = bad                                        # q > 0: the logit is +inf or NaN
+    cache.place(rows, lens)
+    units = heads if shared else heads * group
+    nb = [-(-t // 16) for t in lens]
+    blocks = torch.zeros(batch, units, 25, dtype=torch.int32)
+    count = torch.zeros(batch, units, dtype=torch.int32)
+    for b in range(batch):
+        blocks[b, :, : nb[b]], count[b] = torch.arange(nb[b]), nb[b]
+    skip = units - 1                                                     # the last unit of sequence 0 leaves block 2 out
+    blocks[0, skip, : nb[0] - 1], count[0, skip] = torch.tensor([j for j in range(nb[0]) if j != 2]), nb[0] - 1
+    q = q.to(cuda_device)
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=cuda_device)
+    ctx.block_decode_attn(q, cache.view(), blocks.to(cuda_device), count.to(cuda_device), batch, out, lse, P.PRHS_GROUP_SETS if shared else 0)
+    y, l, per = np64(out), np64(lse), group if shared else 1
+    for b in range(batch):
+        for u in range(heads * group):
+            listed = blocks[b, u // per, : count[b, u // per]].tolist()
+            met = any((b, u // group) == x[:2] and x[2] // 16 in listed for x in hit)
+            if met:
+                assert np.isnan(y[b, u]).all() and np.isnan(l[b, u]), (b, u)
+            else:
+                pos = [i for j in listed for i in range(16 * j, min(16 * j + 16, lens[b]))]
+                k, v = (rows[w, b, u // group].double().numpy()[pos] for w in range(2))
+                want, wl, tol, ltol = R.attend(np64(q[b, u]), k, v, True)
+                assert np.all(np.abs(y[b, u] - want) <= tol) and abs(l[b, u] - wl) <= ltol, (b, u)
+    ctx.close()
+
+
+def test_values_and_queries_that_are_not_finite_show_in_a_step(cuda_device):
+    cache = Cache(3, 2, 700, False, cuda_device)
+    ctx = make_ctx(cache, 2)
+    rows, lens = mild(random_rows(3, 2, 700, 5)), [700, 650, 333]
+    rows[1, 0, 0, 3, 9], rows[1, 1, 1, 649, 11], rows[0, 2, 1, 332, 7] = math.nan, math.inf, -math.inf
+    cache.place(rows, lens)
+    ctx.block_bounds(cache.view(), cache.bounds(), 3)
+    try:                                                                 # the infinite key may be recorded
+        ctx.check()
+    except P.PrhsError:
+        pass
+    q = torch.randn(3, 4, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    q[0, 3, 77] = math.nan
+    q[2, 2:, 7] = 1.0                                                    # the key's logit is -inf: no weight, its value counts nothing
+    q = q.to(cuda_device)
+    blocks, count = torch.empty(3, 4, 44, dtype=torch.int32, device=cuda_device), torch.empty(3, 4, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.full_like(q, 7.0), torch.full((3, 4), 7.0, device=cuda_device)
+    ctx.block_decode_step(q, cache.view(), cache.bounds(), P.make_block_schedule(50, 1, 1), 3, out, lse, blocks, count)
+    y, l = np64(out), np64(lse)
+    assert np.isnan(y[0, 3]).all() and np.isnan(l[0, 3])
+    rows[1, 0, 0, 3, 9], rows[1, 1, 1, 649, 11] = 0, 0
+    for b, u, d in [(0, 0, 9), (0, 1, 9), (0, 2, None), (1, 0, None), (1, 1, None), (1, 2, 11), (1, 3, 11), (2, 0, None), (2, 2, None), (2, 3, None)]:
+        k, v = (rows[w, b, u // 2, : lens[b]].double().numpy() for w in range(2))
+        keep = np.arange(lens[b]) != (332 if (b, u // 2) == (2, 1) else -1)
+        want, wl, tol, ltol = R.attend(np64(q[b, u]), k[keep], v[keep], True)
+        rest = np.arange(128) != (-1 if d is None else d)
+        assert np.all(np.abs(y[b, u] - want)[rest] <= tol[rest]) and abs(l[b, u] - wl) <= ltol, (b, u)
+        assert d is None or not np.isfinite(y[b, u, d]), (b, u)
+    ctx.close()
+
+
 # -------------------------------------------------------------------------------- refusals
 def test_refusals(cuda_device):
     cache = Cache(2, 2, 64, False, cuda_device)

@@ -498,6 +498,55 @@ def test_split_counts_agree(cuda_device):
         ctx.close()
 
 
+# ------------------------------------------------------------------------------ not finite
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("heads,group,batch,t", [(2, 2, 3, 2055), (1, 12, 2, 535), (8, 2, 50, 90), (4, 4, 70, 400)])
+def test_numbers_that_are_not_finite_show(cuda_device, fmt, heads, group, batch, t):
+    """A NaN key, or an infinite one in the open block, makes the softmax NaN for the heads that read it and for no other; a NaN
+    value its coordinate.  Over all positions (runs, parts, whole units) and over lists."""
+    cache = Cache(fmt, batch, heads, t, False, cuda_device)
+    ctx = make_ctx(cache, group)
+    lens = [t - 2 * b % t for b in range(batch)]
+    g = torch.Generator().manual_seed(41)
+    rows = (torch.randn(2, batch, heads, t, 128, generator=g) * torch.tensor([0.25, 1.0])[:, None, None, None, None]).to(torch.bfloat16)
+    rows[0, 0, 0, 33, 5] = math.nan                                       # a key in the 8-bit cache
+    rows[0, 1, heads - 1, lens[1] - 1, 6] = math.inf                      # a key of the open block: +inf for every head (q > 0)
+    rows[1, 1, 0, 35, 8] = math.nan                                       # a value
+    if batch > 2:
+        rows[1, 2, 0, lens[2] - 1, 9] = math.inf                          # a value of the open block
+    cache.set_lens(lens)
+    ctx.bytekv_append(rows[0].to(cuda_device), rows[1].to(cuda_device), cache.lens.clone(), cache.view(), batch)
+    with pytest.raises(P.PrhsError):
+        ctx.check()
+    U = heads * group
+    q = torch.randn(batch, U, 128, generator=g).abs().to(torch.bfloat16)
+    if batch > 2:
+        q[2, U - 1, 3] = math.nan
+    q = q.to(cuda_device)
+    idx = torch.arange(t, dtype=torch.int32, device=cuda_device).expand(batch, U, t).contiguous()
+    cnt = torch.tensor(lens, dtype=torch.int32, device=cuda_device)[:, None].expand(batch, U).contiguous()
+    for call in (lambda o, s: ctx.bytekv_decode_attn(q, cache.view(), batch, o, s),
+                 lambda o, s: ctx.bytekv_sparse_decode_attn(q, cache.view(), idx, cnt, batch, o, s)):
+        out, lse = torch.full_like(q, 7.0), torch.full((batch, U), 7.0, device=cuda_device)
+        call(out, lse)
+        assert ctx.check() == 0
+        y_all, l_all = np64(out), np64(lse)
+        for b in [0, 1, 2, batch // 2, batch - 1]:
+            for u in range(U if b < batch else 0):
+                h = u // group
+                if (b, h) in ((0, 0), (1, heads - 1)) or (b == 2 and u == U - 1):
+                    assert np.isnan(y_all[b, u]).all() and np.isnan(l_all[b, u]), (b, u)
+                    continue
+                d = {(1, 0): 8, (2, 0): 9}.get((b, h), -1)
+                k, v = cache.rows("k", b, h, lens[b]), cache.rows("v", b, h, lens[b])
+                v = np.where(np.isfinite(v), v, 0.0)
+                y, l, tol, ltol = R.attend(np64(q[b, u]), k, v, True)
+                rest = np.arange(128) != d
+                assert np.all(np.abs(y_all[b, u] - y)[rest] <= tol[rest]) and abs(l_all[b, u] - l) <= ltol, (b, u)
+                assert d < 0 or not np.isfinite(y_all[b, u, d]), (b, u)
+    ctx.close()
+
+
 # -------------------------------------------------------------------------------- refusals
 def test_refusals(cuda_device):
     cache = Cache("e4m3", 2, 2, 64, False, cuda_device)
