@@ -765,8 +765,19 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       const int passes = kList ? __reduce_max_sync(0xffffffffu, max(times[0], times[1])) : 1;
       const uint32_t kt = ring + (uint32_t)slot_i * k8StageBytes;
       const uint32_t vt = ring + (uint32_t)(slot_i + 1 == kStages ? 0 : slot_i + 1) * k8StageBytes;
-      for (int d = 0; d < passes; ++d)         // a row listed d times takes part in d passes (lists rarely repeat)
+      for (int d = 0; d < passes; ++d) {       // a row listed d times takes part in d passes (lists rarely repeat)
+        if (kList) {                           // values of the others become zero: no weight times an infinity is NaN
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 2 * i + (lane >> 4);
+            if (tail_count[r] == d)
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vt + r * kRowBytes + ((lane & 15u) << 4)), "r"(0u) : "memory");
+          }
+          __syncwarp();
+        }
         bf16_stage<kTiles>(kt, vt, tq, times[0] > d, times[1] > d, to, ts);
+        __syncwarp();
+      }
       store_partial_bf16<kTiles>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps], sm_lt[k8Warps]);
     }
     __syncthreads();

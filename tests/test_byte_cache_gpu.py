@@ -547,6 +547,38 @@ def test_numbers_that_are_not_finite_show(cuda_device, fmt, heads, group, batch,
     ctx.close()
 
 
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("units,stride", [(2, 900), (80, 60)])
+def test_rows_of_the_open_block_that_a_list_leaves_out_do_not_matter(cuda_device, paged, units, stride):
+    """Infinities and NaNs in keys and values of open rows that no entry names; rows named once and several times beside them."""
+    t, batch = 1003, 3
+    cache = Cache("e4m3", batch, units, t, paged, cuda_device)
+    ctx = make_ctx(cache, 1)
+    new = fill(ctx, cache, [t] * batch)
+    assert ctx.check() == 0 and new is not None
+    for x, bad in ((cache.kt, math.nan), (cache.vt, math.inf)):          # open rows 992 .. 1002 are tail rows 0 .. 10
+        x[:, :, 1], x[:, :, 4], x[:, :, 10] = bad, -bad, math.nan
+    rng = np.random.default_rng(7)
+    idx = rng.integers(0, 992, (batch, units, stride)).astype(np.int32)
+    named = [992, 994, 994, 994, 999, 995, 999]
+    idx[:, :, 3:10] = named                                              # in one part of a list that is dealt in parts
+    idx[0, 0, -1] = 994                                                  # and in another
+    cnt = np.full((batch, units), stride, np.int32)
+    cnt[1, 1] = 12
+    idx[2, 0, 3:10] = 5                                                  # no open row at all
+    q = torch.randn(batch, units, 128, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.bytekv_sparse_decode_attn(q, cache.view(), torch.from_numpy(idx).to(cuda_device), torch.from_numpy(cnt).to(cuda_device), batch, out, lse)
+    assert ctx.check() == 0
+    y_all, l_all, qh = np64(out), np64(lse), np64(q)
+    for b in range(batch):
+        for u in sorted({0, 1, units // 2, units - 1}):
+            c = idx[b, u, : cnt[b, u]]
+            y, l, tol, ltol = R.attend(qh[b, u], cache.rows("k", b, u, t)[c], cache.rows("v", b, u, t)[c], True)
+            assert np.all(np.abs(y_all[b, u] - y) <= tol) and abs(l_all[b, u] - l) <= ltol, (b, u)
+    ctx.close()
+
+
 # -------------------------------------------------------------------------------- refusals
 def test_refusals(cuda_device):
     cache = Cache("e4m3", 2, 2, 64, False, cuda_device)
