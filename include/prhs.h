@@ -383,6 +383,9 @@ prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const p
  *     score = sum_d max(q8_d lo8_d, q8_d hi8_d) * scale_block * scale_q,
  * an exact integer sum and two powers of two, so scores are the same on every machine and ties are real (as far as
  * the range of fp32 goes: a partial product beyond it is infinite or zero).
+ * An infinity has the code 127 or -127 and gives its block, or its query, the scale 2^122 (so a block with an infinite
+ * bound that q meets with a code of its sign scores no less than any other); NaNs of a key are left out.  A block whose bounds meet either is recorded
+ * (PRHS_FLAG_NONFINITE), by prhs_block_bounds and by a step.
  *   contiguous: block j of (b, kvh) has index b*stride_outer + kvh*stride_head + j
  *   paged:      page*stride_outer + kvh*stride_head
  *   codes + index*256: 128 minima, then 128 maxima;  scale + index */
@@ -469,7 +472,7 @@ int32_t prhs_scores_ld(const prhs_ctx* ctx);
 #define PRHS_FLAG_SELECT_FALLBACK 4u /* informational: selection took the multi-pass path     */
 #define PRHS_FLAG_TIMEOUT         8u /* a bounded wait on a TMA barrier ran out; results invalid */
 #define PRHS_FLAG_BAD_LENGTH     16u /* lengths contradict each other: sequence skipped, or its length cut */
-#define PRHS_FLAG_NONFINITE      32u /* an infinity or a NaN went into the 8-bit cache            */
+#define PRHS_FLAG_NONFINITE      32u /* an infinity or a NaN went into the 8-bit cache or met a block's bounds */
 prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags);
 
 /* Per-kernel device timing for benchmarks (no counterpart in the paper: measurement support).

@@ -28,51 +28,69 @@ struct BoundsDev {
 };
 
 // ---------------------------------------------------------------------------------- bounds
+// The code of a number in units of its scale; infinities have the largest.
+__device__ __forceinline__ int code_of(float x, float inv) { return min(max(__float2int_rn(x * inv), -127), 127); }
+
 // One warp, one block: bounds of the block's rows below `rows` (1..16) into codes / scale.  src: the block's
-// first row.
-__device__ __forceinline__ void bounds_of_block(const __nv_bfloat16* src, int rows, int8_t* codes, float* scale) {
+// first row.  NaNs are left out (a coordinate of NaNs only counts as zero).  Returns whether every element was finite.
+__device__ __forceinline__ bool bounds_of_block(const __nv_bfloat16* src, int rows, int8_t* codes, float* scale) {
   const int lane = threadIdx.x & 31;
   const int r0 = lane >> 4, col = (lane & 15) * 8;
-  uint4 x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {               // rows past the end repeat row 0: no change to a minimum or maximum
-    const int r = 2 * i + r0;
-    x[i] = __ldg(reinterpret_cast<const uint4*>(src + (r < rows ? r : 0) * kHeadDim + col));
-  }
   uint32_t lo[4], hi[4];
+  // minima and maxima, and the largest magnitude of the block as bf16 bits; kNaN: one NaN makes its coordinate NaN
+  auto fold = [&](auto nan_c) -> uint32_t {
+    constexpr bool kNaN = decltype(nan_c)::value != 0;
+    auto low = [](uint32_t a, uint32_t b) {
+      const __nv_bfloat162 x = *reinterpret_cast<__nv_bfloat162*>(&a), y = *reinterpret_cast<__nv_bfloat162*>(&b);
+      const __nv_bfloat162 z = kNaN ? __hmin2_nan(x, y) : __hmin2(x, y);
+      return *reinterpret_cast<const uint32_t*>(&z);
+    };
+    auto high = [](uint32_t a, uint32_t b) {
+      const __nv_bfloat162 x = *reinterpret_cast<__nv_bfloat162*>(&a), y = *reinterpret_cast<__nv_bfloat162*>(&b);
+      const __nv_bfloat162 z = kNaN ? __hmax2_nan(x, y) : __hmax2(x, y);
+      return *reinterpret_cast<const uint32_t*>(&z);
+    };
+    uint4 x[8];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    auto word = [&](int i) { return j == 0 ? x[i].x : j == 1 ? x[i].y : j == 2 ? x[i].z : x[i].w; };
-    uint32_t a = word(0), z = word(0);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-      const uint32_t w = word(i);
-      const __nv_bfloat162 wb = *reinterpret_cast<const __nv_bfloat162*>(&w);
-      __nv_bfloat162 av = __hmin2(*reinterpret_cast<__nv_bfloat162*>(&a), wb), zv = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&z), wb);
-      a = *reinterpret_cast<uint32_t*>(&av);
-      z = *reinterpret_cast<uint32_t*>(&zv);
+    for (int i = 0; i < 8; ++i) {             // rows past the end repeat row 0: no change to a minimum or maximum
+      const int r = 2 * i + r0;
+      x[i] = __ldg(reinterpret_cast<const uint4*>(src + (r < rows ? r : 0) * kHeadDim + col));
     }
-    const uint32_t a2 = __shfl_xor_sync(0xffffffffu, a, 16), z2 = __shfl_xor_sync(0xffffffffu, z, 16);
-    const __nv_bfloat162 av = __hmin2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&a2));
-    const __nv_bfloat162 zv = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&z), *reinterpret_cast<const __nv_bfloat162*>(&z2));
-    lo[j] = *reinterpret_cast<const uint32_t*>(&av);
-    hi[j] = *reinterpret_cast<const uint32_t*>(&zv);
-  }
-  uint32_t mx = 0u;
+    uint32_t mx = 0u;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) mx = __vmaxu2(mx, __vmaxu2(lo[j] & 0x7fff7fffu, hi[j] & 0x7fff7fffu));
-  const uint32_t amax = __reduce_max_sync(0xffffffffu, max(mx & 0xffffu, mx >> 16));
+    for (int j = 0; j < 4; ++j) {
+      auto word = [&](int i) { return j == 0 ? x[i].x : j == 1 ? x[i].y : j == 2 ? x[i].z : x[i].w; };
+      uint32_t a = word(0), z = word(0);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) {
+        a = low(a, word(i));
+        z = high(z, word(i));
+      }
+      lo[j] = low(a, __shfl_xor_sync(0xffffffffu, a, 16));
+      hi[j] = high(z, __shfl_xor_sync(0xffffffffu, z, 16));
+      if (!kNaN) {
+        lo[j] &= ~__vcmpgtu2(lo[j] & 0x7fff7fffu, 0x7f807f80u);
+        hi[j] &= ~__vcmpgtu2(hi[j] & 0x7fff7fffu, 0x7f807f80u);
+      }
+      mx = __vmaxu2(mx, __vmaxu2(lo[j] & 0x7fff7fffu, hi[j] & 0x7fff7fffu));
+    }
+    return __reduce_max_sync(0xffffffffu, max(mx & 0xffffu, mx >> 16));
+  };
+  uint32_t amax = fold(SlotC<1>{});
+  const bool finite = amax < 0x7f80u;
+  if (amax > 0x7f80u) amax = fold(SlotC<0>{});      // (read again: that is rare)
   const int e = scale_exponent<6, 126>(amax);       // 127 = (1 + 126 / 128) 2^6
   const float inv = pow2i(-e);
   uint32_t c[2] = {0u, 0u};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t w = lane < 16 ? lo[j] : hi[j];
-    const uint32_t c0 = (uint32_t)__float2int_rn(bf_lo(w) * inv) & 0xffu, c1 = (uint32_t)__float2int_rn(bf_hi(w) * inv) & 0xffu;
+    const uint32_t c0 = (uint32_t)code_of(bf_lo(w), inv) & 0xffu, c1 = (uint32_t)code_of(bf_hi(w), inv) & 0xffu;
     c[j >> 1] |= (c0 | (c1 << 8)) << (16 * (j & 1));
   }
   *reinterpret_cast<uint2*>(codes + lane * 8) = make_uint2(c[0], c[1]);    // lanes 0-15 the minima, 16-31 the maxima
   if (lane == 0) *scale = pow2i(e);
+  return finite;
 }
 
 // Where block `blk` of (b, kvh) lies: rows and bounds.  false: a page id outside the pool.
@@ -113,7 +131,8 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(BoundsParams p) {
     if ((threadIdx.x & 31) == 0) atomicOr(p.flags, kFlagBadPage);
     return;
   }
-  bounds_of_block(p.kv.k + row, min(kBlockRows, t - blk * kBlockRows), p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
+  const bool finite = bounds_of_block(p.kv.k + row, min(kBlockRows, t - blk * kBlockRows), p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
+  if (!finite && (threadIdx.x & 31) == 0) atomicOr(p.flags, kFlagNonFinite);
 }
 
 // ----------------------------------------------------------------------------------- score
@@ -262,7 +281,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) __maxnreg__(kWide ? 168 : kS
       uint32_t neg[2] = {0u, 0u}, pos[2] = {0u, 0u};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int code = __float2int_rn((j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1])) * inv);
+        const int code = code_of(j & 1 ? bf_hi(w[j >> 1]) : bf_lo(w[j >> 1]), inv);
         neg[j >> 2] |= ((uint32_t)min(code, 0) & 0xffu) << (8 * (j & 3));
         pos[j >> 2] |= (uint32_t)max(code, 0) << (8 * (j & 3));
       }
@@ -583,10 +602,10 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   // a step writes the bounds of the last block, whose score nothing reads: here and now, while the selection runs
   if (p.fixed && split == 0 && head0 % p.group_size == 0 && (kOwn || warp == kTWarps - 1) && nb > 0 && t == given) {
     long long row, bi;
-    if (locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi))
-      bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi);
-    else if (lane == 0)
-      atomicOr(p.flags, kFlagBadPage);
+    uint32_t flag = 0u;
+    if (!locate_block(p.kv, p.bd, b, kvh, nb - 1, row, bi)) flag = kFlagBadPage;
+    else if (!bounds_of_block(p.kv.k + row, t - (nb - 1) * kBlockRows, p.bd.codes + bi * kBoundsBytes, p.bd.scale + bi)) flag = kFlagNonFinite;
+    if (flag && lane == 0) atomicOr(p.flags, flag);
   }
 
   // two passes over the ring: the blocks that are known (a step), then the listed ones

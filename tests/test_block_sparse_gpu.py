@@ -648,6 +648,52 @@ def test_values_and_queries_that_are_not_finite_show_in_a_step(cuda_device):
     ctx.close()
 
 
+def coded(x):
+    """int8 codes and scale of numbers among which are infinities (the largest code; the scale follows their exponent) and NaNs
+    (left out)."""
+    finite = np.where(np.isnan(x), 0.0, x)
+    s = 2.0 ** 122 if np.isinf(finite).any() else float(R.scale_of(np.abs(finite).max(), 127.0))
+    return np.clip(np.where(np.isinf(finite), np.sign(finite) * 127, np.rint(np.where(np.isinf(finite), 0, finite) / s)), -127, 127), s
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_bounds_and_scores_of_numbers_that_are_not_finite(cuda_device, paged):
+    cache = Cache(1, 2, 320, paged, cuda_device)
+    ctx = make_ctx(cache, 2)
+    rows = random_rows(1, 2, 320, 17)
+    rows[0, 0, 0, 20, 3], rows[0, 0, 0, 40, 4], rows[0, 0, 0, 41, 4] = math.inf, math.inf, -math.inf
+    rows[0, 0, 1, 50, 5], rows[0, 0, 1, 64:80, 6], rows[0, 0, 1, 81] = math.nan, math.nan, math.nan
+    rows[0, 0, 1, 100, 7], rows[0, 0, 1, 101, 7] = math.nan, -math.inf
+    cache.place(rows, [320])
+    ctx.block_bounds(cache.view(), cache.bounds(), 1)
+    with pytest.raises(P.PrhsError) as e:                                 # recorded
+        ctx.check()
+    assert e.value.status == 7
+    bounds = {}
+    for h in range(2):
+        for j in range(20):
+            x = rows[0, 0, h, 16 * j: 16 * j + 16].double().numpy()
+            lo, hi = np.where(np.isnan(x), math.inf, x).min(0), np.where(np.isnan(x), -math.inf, x).max(0)
+            empty = np.isnan(x).all(0)
+            want, s = coded(np.stack([np.where(empty, 0, lo), np.where(empty, 0, hi)]))
+            got, gs = cache.bound_of(0, h, j)
+            assert gs == s and np.array_equal(got, want), (h, j)
+            bounds[h, j] = want, s
+    q = torch.randn(1, 4, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    q[0, 0, 3], q[0, 1, 9], q[0, 3, 5] = 2.0, math.inf, -math.inf
+    q[0, 1, 8], q[0, 3, 4], q[0, 3, 6] = 1.0, -1.0, 1.0                   # neighbours of the infinite element keep their codes
+    blocks, count = torch.empty(1, 4, 5, dtype=torch.int32, device=cuda_device), torch.empty(1, 4, dtype=torch.int32, device=cuda_device)
+    ctx.block_topk(q.to(cuda_device), cache.view(), cache.bounds(), P.make_block_schedule(5, 0, 0), 1, blocks, count)
+    for u in range(4):
+        q8, qs = coded(np64(q[0, u]))
+        score = [np.maximum(q8 * bounds[u // 2, j][0][0], q8 * bounds[u // 2, j][0][1]).sum() * bounds[u // 2, j][1] * qs for j in range(20)]
+        with np.errstate(over="ignore"):
+            score = [float(np.float32(x)) for x in score]
+        assert blocks[0, u].tolist() == R.select_blocks(score, 20, 5, 0, 0), u
+    assert 1 in blocks[0, 0].tolist()                                     # q . k is +inf in block 1: it is attended over
+    ctx.close()
+
+
 # -------------------------------------------------------------------------------- refusals
 def test_refusals(cuda_device):
     cache = Cache(2, 2, 64, False, cuda_device)
