@@ -138,13 +138,25 @@ struct Args {
   template <typename T>
   T* pointer(int i) const { return static_cast<T*>(PyLong_AsVoidPtr(a[i])); }
 };
-// The call with the interpreter released, as ctypes makes it; the status as a Python integer.
+// The interpreter's lock, given up for as long as this lives, whichever way its scope is left.
+class Released {
+ public:
+  Released() : state_(PyEval_SaveThread()) {}
+  ~Released() { PyEval_RestoreThread(state_); }
+  Released(const Released&) = delete;
+  Released& operator=(const Released&) = delete;
+
+ private:
+  PyThreadState* state_;
+};
+// The call with the interpreter released, as ctypes makes it; the status as a Python integer.  Tensors are read before.
 template <typename F>
 PyObject* status(F call) {
   prhs_status rc;
-  Py_BEGIN_ALLOW_THREADS
-  rc = call();
-  Py_END_ALLOW_THREADS
+  {
+    const Released released;
+    rc = call();
+  }
   return PyLong_FromLong(rc);
 }
 
@@ -202,10 +214,11 @@ PyObject* bytekv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   REQUIRE(is(n, at::kInt, dev) && n->dim() == 1 && n->size(0) >= batch && n->is_contiguous(), "new_lens is int32 [batch] on the cache's device");
   REQUIRE(0 <= max_new && max_new <= k->size(2) && k->size(2) <= INT32_MAX, "max_new is at most the number of rows given");
   auto stride = [&](int i) { return k->size(i) > 1 ? k->stride(i) : 0; };     // that of an axis of one element is arbitrary
-  return status([&] {
-    return entry.bytekv_append(ctx, kv, k->data_ptr(), vv->data_ptr(), stride(0), stride(1), stride(2), static_cast<const int32_t*>(n->data_ptr()),
-                               (int32_t)(max_new ? max_new : k->size(2)), (int32_t)batch, stream);
-  });
+  const int64_t by_seq = stride(0), by_head = stride(1), by_row = stride(2);
+  const void *new_k = k->data_ptr(), *new_v = vv->data_ptr();
+  const int32_t* new_lens = static_cast<const int32_t*>(n->data_ptr());
+  const int32_t rows = (int32_t)(max_new ? max_new : k->size(2));
+  return status([&] { return entry.bytekv_append(ctx, kv, new_k, new_v, by_seq, by_head, by_row, new_lens, rows, (int32_t)batch, stream); });
 }
 
 // bytekv_decode_attn(ctx, view, q, out, out_lse, batch, heads, device, stream)

@@ -2,6 +2,8 @@
 import ctypes as C
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -104,6 +106,37 @@ def test_tensors_without_storage_raise(lib):
         P.make_view(sparse, sparse, lens)
     with pytest.raises(RuntimeError, match="storage"):
         P.make_view(dense, dense, lens.to_sparse())
+
+
+NO_DATA = """
+import torch
+from paper_2602_08329_b200 import binding as P
+m = P._load_marshal()
+t, lens, n = torch.zeros(5, 2, 3, 4, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), None
+lists = torch.zeros(2, 3, 4, dtype=torch.int32)
+calls = {
+    "append": lambda x: m.bytekv_append(0, 0, x, x, lens, 2, 3, -1, 0, 0),
+    "append, lengths": lambda x: m.bytekv_append(0, 0, t[0], t[0], x[:, 0, 0, 0].to(torch.int32), 2, 3, -1, 0, 0),
+    "attend": lambda x: m.bytekv_decode_attn(0, 0, x[:, :, 0].contiguous(), None, n, 2, 3, -1, 0),
+    "lists": lambda x: m.bytekv_sparse_decode_attn(0, 0, x[:, :, 0].contiguous(), None, n, 2, 3, -1, 0, lists, lists[:, :, 0].contiguous()),
+    "bounds": lambda x: m.block_bounds(0, 0, 0, x[:, 0, 0, 0].to(torch.int32), 0, 2, -1, 0),
+    "blocks": lambda x: m.block_decode_attn(0, 0, t[0, :, :, 0].contiguous(), None, n, 2, 3, 3, -1, 0, x[..., 0].to(torch.int32), lists[:, :, 0].contiguous(), 0),
+}
+for name, call in calls.items():
+    try:
+        torch.vmap(lambda x: call(x) and x)(t)
+    except RuntimeError as e:
+        assert "storage" in str(e) or "data" in str(e), (name, e)
+        print(name)
+"""
+
+
+def test_calls_with_tensors_that_have_no_data_raise(lib):
+    """A batched tensor has sizes, strides and a type, but no address.  (In a process of its own: without the interpreter's
+    lock an exception ends it.)"""
+    res = subprocess.run([sys.executable, "-X", "faulthandler", "-c", NO_DATA], cwd=ROOT, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-2000:]
+    assert res.stdout.split("\n")[:-1] == ["append", "append, lengths", "attend", "lists", "bounds", "blocks"]
 
 
 def test_views_take_rows_of_a_wider_page_table(lib):
