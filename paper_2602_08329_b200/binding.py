@@ -202,11 +202,11 @@ def make_schedule(top_k, window, sinks, refresh_interval=1, layer_group=1, dilat
 
 def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
     """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128]."""
-    kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, cap, dev = \
+    kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, cap, span, dev, why = \
         (_marshal or _load_marshal()).kv_view(k, v, seq_lens, page_table)
     view = KvView.from_buffer_copy(_KV_PACK(kp, vp, so, sh, table, table_stride, lens, max_seq_len, pages))
     view._keep = (k, v, seq_lens, page_table)
-    view._batch, view._heads, view._cap, view._dev = batch, heads, cap, dev
+    view._batch, view._heads, view._cap, view._span, view._dev, view._why, view._auto = batch, heads, cap, span, dev, why, None
     return view
 
 
@@ -217,12 +217,12 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
     fp32 scales [B][Hkv][cap/16]; or paged [pool][Hkv][16][128] with scales [pool][Hkv].  Tails bf16
     [B][Hkv][16][128].
     """
-    (kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride, pages, fmt, batch, heads, cap, dev) = \
+    (kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride, pages, fmt, batch, heads, cap, dev, span) = \
         (_marshal or _load_marshal()).bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table, max_seq_len)
     view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride,
                                                     max_seq_len, pages, fmt))
     view._keep = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table)
-    view._batch, view._heads, view._cap, view._dev = batch, heads, cap, dev
+    view._batch, view._heads, view._cap, view._span, view._dev, view._why, view._auto = batch, heads, cap, span, dev, None, None
     return view
 
 
@@ -255,6 +255,7 @@ class Context:
             raise PrhsError(rc, self.lib.prhs_last_error(None).decode())
         self.h = h
         self._h, self._hq, self._hkv, self._max_context = h.value, num_q_heads, num_kv_heads, max_context
+        self._dev = torch._C._cuda_getDevice()
 
     def close(self):
         if getattr(self, "h", None):
@@ -375,14 +376,15 @@ class Context:
             self._ck(rc)
 
     def _fit(self, view, batch):
-        """The view against this context: heads, batch, and no length beyond a contiguous cache's capacity."""
-        assert view._heads == self._hkv and batch <= view._batch and view._dev >= 0
-        cap = view._cap
-        if cap:
-            n = view.max_seq_len
-            if n == 0 and cap < self._max_context:
-                n = view.max_seq_len = cap
-            assert n <= cap
+        """The view against this context: heads, batch, device, and no length beyond what the cache, or a row of its page
+        table, holds (which is the bound where the view gives none)."""
+        assert view._heads == self._hkv and batch <= view._batch and view._dev == self._dev, \
+            view._why or "the view's heads, batch and device are those of the context and the call"
+        n = view.max_seq_len
+        if n == 0 or n == view._auto:
+            n = view._span if view._span < self._max_context else 0
+            view.max_seq_len = view._auto = n
+        assert n <= view._span, "max_seq_len is at most what the cache, or a row of its page table, holds"
 
     def _fit_bounds(self, view, bounds, batch):
         self._fit(view, batch)

@@ -8,6 +8,7 @@
 #include <ATen/ATen.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <exception>
 
@@ -40,7 +41,8 @@ bool count_is(Py_ssize_t nargs, Py_ssize_t n) {
 }
 
 // kv_view(k, v, seq_lens, page_table | None): k, v, stride_outer, stride_head, table, table_stride, seq_lens, pages, batch, heads,
-// cap, device (-1: host tensors, which no call takes)
+// cap (0: pages), span (positions that the cache, or a row of the page table, has), device (-1 where the block calls refuse the
+// view), why they do
 PyObject* kv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (!count_is(nargs, 4)) return nullptr;
   const at::Tensor *k = tensor(a[0]), *v = tensor(a[1]), *lens = tensor(a[2]), *table = none(a[3]) ? nullptr : tensor(a[3]);
@@ -51,9 +53,18 @@ PyObject* kv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   REQUIRE(lens->scalar_type() == at::kInt, "seq_lens is int32");
   REQUIRE(!table || (table->scalar_type() == at::kInt && table->dim() >= 1 && (table->dim() == 1 || table->stride(-1) == 1)),
           "the page table is int32 [batch][pages], its rows contiguous");
-  return Py_BuildValue("LLLLLLLLLLLL", address(*k), address(*v), k->stride(0), k->stride(1), table ? address(*table) : 0,
-                       table ? table->stride(0) : 0, address(*lens), table ? k->size(0) : 0, lens->numel(), k->size(1),
-                       table ? 0 : k->size(2), device(*k));
+  // what the block calls ask of a view beyond that; the other calls take it as it is
+  const bool paged = table != nullptr;
+  const int64_t dev = device(*k);
+  const char* why = nullptr;
+  if (k->dim() != 4 || v->sizes() != k->sizes()) why = "k and v are alike, with four axes";
+  else if (lens->dim() != 1 || !lens->is_contiguous()) why = "seq_lens is contiguous [batch]";
+  else if (paged && (table->dim() != 2 || k->size(2) != 16)) why = "the page table is [batch][pages], of pages of 16 positions";
+  else if (device(*v) != dev || device(*lens) != dev || (paged && device(*table) != dev) || dev < 0) why = "the tensors of a call are on one CUDA device";
+  const int64_t batch = std::min(lens->numel(), paged ? table->size(0) : k->size(0));
+  const int64_t cap = paged ? 0 : k->size(2), span = !paged ? cap : table->dim() == 2 ? 16 * table->size(1) : 0;
+  return Py_BuildValue("LLLLLLLLLLLLLz", address(*k), address(*v), k->stride(0), k->stride(1), paged ? address(*table) : 0,
+                       paged ? table->stride(0) : 0, address(*lens), paged ? k->size(0) : 0, batch, k->size(1), cap, span, why ? -1 : dev, why);
 }
 
 // bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table | None, max_seq_len): six addresses, stride_outer,
@@ -89,9 +100,10 @@ PyObject* bytekv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
             "scales are [batch][Hkv][cap / 16]");
     REQUIRE(k.size(0) >= batch && max_len <= k.size(2), "the cache holds the batch and max_seq_len positions");
   }
-  return Py_BuildValue("LLLLLLLLLLLLLLLLLLL", address(k), address(v), address(ks), address(vs), address(kt), address(vt), k.stride(0),
+  return Py_BuildValue("LLLLLLLLLLLLLLLLLLLL", address(k), address(v), address(ks), address(vs), address(kt), address(vt), k.stride(0),
                        k.stride(1), ks.stride(0), ks.stride(1), t[7] ? address(*t[7]) : 0, address(lens), t[7] ? t[7]->stride(0) : 0,
-                       t[7] ? k.size(0) : 0, type == at::kFloat8_e5m2 ? 1 : 0, batch, k.size(1), t[7] ? 0 : k.size(2), dev);
+                       t[7] ? k.size(0) : 0, type == at::kFloat8_e5m2 ? 1 : 0, batch, k.size(1), t[7] ? 0 : k.size(2), dev,
+                       t[7] ? 16 * t[7]->size(1) : k.size(2));
 }
 
 // bounds_view(codes, scale): codes, scale, stride_outer, stride_head, outer size, heads, blocks (0: per page), device

@@ -695,6 +695,60 @@ def test_bounds_and_scores_of_numbers_that_are_not_finite(cuda_device, paged):
 
 
 # -------------------------------------------------------------------------------- refusals
+def test_tensors_of_a_view_elsewhere_are_refused(cuda_device):
+    """Host lengths or page tables, fewer rows than the batch, values of another size: refused before any kernel."""
+    for paged in (False, True):
+        cache = Cache(2, 2, 64, paged, cuda_device)
+        ctx = make_ctx(cache, 2)
+        cache.place(random_rows(2, 2, 64, 1), [64, 64])
+        q = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=cuda_device)
+        out = torch.full_like(q, 7.0)
+        blocks, count = torch.zeros(2, 4, 4, dtype=torch.int32, device=cuda_device), torch.zeros(2, 4, dtype=torch.int32, device=cuda_device)
+        sched = P.make_block_schedule(1, 1, 1)
+        wrong = [dict(lens=cache.lens.cpu()), dict(v=cache.v.cpu()), dict(v=cache.v[:1]), dict(lens=cache.lens[None]),
+                 dict(lens=torch.zeros(3, dtype=torch.int32, device=cuda_device)[::2]), dict(lens=cache.lens[:1])]
+        wrong += [dict(table=cache.table.cpu()), dict(table=cache.table[:1]), dict(table=cache.table[0])] if paged else [dict(k=cache.k[:1], v=cache.v[:1])]
+        for w in wrong:
+            a = {**dict(k=cache.k, v=cache.v, lens=cache.lens, table=cache.table), **w}
+            view = P.make_view(a["k"], a["v"], a["lens"], page_table=a["table"])
+            for call in (lambda: ctx.block_bounds(view, cache.bounds(), 2),
+                         lambda: ctx.block_topk(q, view, cache.bounds(), sched, 2, blocks, count),
+                         lambda: ctx.block_decode_attn(q, view, blocks, count, 2, out),
+                         lambda: ctx.block_decode_step(q, view, cache.bounds(), sched, 2, out, None, blocks, count)):
+                with pytest.raises(AssertionError):
+                    call()
+        torch.cuda.synchronize()
+        assert bool((out == 7.0).all()) and bool((cache.scale == 99.0).all())
+        ctx.close()
+
+
+def test_a_slice_of_a_page_table_bounds_the_lengths(cuda_device):
+    """Columns beyond the slice are another's: a length that would need them is cut and recorded."""
+    cache = Cache(2, 2, 160, True, cuda_device)
+    ctx = make_ctx(cache, 2)
+    rows = random_rows(2, 2, 160, 3)
+    cache.place(rows, [160, 160])
+    ctx.block_bounds(cache.view(), cache.bounds(), 2)
+    assert ctx.check() == 0
+    view = P.make_view(cache.k, cache.v, cache.lens, page_table=cache.table[:, :5])
+    q = torch.randn(2, 4, 128, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.empty_like(q), torch.empty(2, 4, device=cuda_device)
+    blocks, count = torch.empty(2, 4, 5, dtype=torch.int32, device=cuda_device), torch.empty(2, 4, dtype=torch.int32, device=cuda_device)
+    for lens, cut in (([80, 33], 0), ([81, 160], 1)):
+        cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        ctx.block_decode_step(q, view, cache.bounds(), P.make_block_schedule(3, 1, 1), 2, out, lse, blocks, count)
+        if cut:
+            with pytest.raises(P.PrhsError):
+                ctx.check()
+        assert ctx.check() == 0
+        lens = [min(t, 80) for t in lens]
+        sets = {(b, u): list(range(-(-t // 16))) for b, t in enumerate(lens) for u in range(4)}
+        for (b, u), w in sets.items():
+            assert blocks[b, u].tolist()[: len(w)] == w
+        check_attention(cache, np64(q), lens, 2, sets, False, out, lse)
+    ctx.close()
+
+
 def test_refusals(cuda_device):
     cache = Cache(2, 2, 64, False, cuda_device)
     ctx = make_ctx(cache, 2)

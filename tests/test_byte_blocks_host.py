@@ -4,6 +4,7 @@ import os
 import re
 import subprocess
 import sys
+import types
 
 import numpy as np
 import pytest
@@ -148,6 +149,48 @@ def test_views_take_rows_of_a_wider_page_table(lib):
     for t in (table[:, ::2], table.long()):
         with pytest.raises(AssertionError):
             P.make_view(pool, pool, lens, page_table=t)
+
+
+def stand_in(**kw):
+    """What Context._fit reads of a context (none can be made without a GPU); its device is that of host tensors."""
+    return types.SimpleNamespace(**{**dict(_hkv=2, _max_context=64, _dev=-1), **kw})
+
+
+def test_the_block_calls_refuse_views_that_do_not_fit(lib):
+    k, lens = torch.zeros(3, 2, 64, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    pool, table = torch.zeros(9, 2, 16, 128, dtype=torch.bfloat16), torch.zeros(3, 4, dtype=torch.int32)
+    fit = lambda view, batch=3, **kw: P.Context._fit(stand_in(**kw), view, batch)  # noqa: E731
+    for view, why in ((P.make_view(k, k, lens), "one CUDA device"), (P.make_view(pool, pool, lens, page_table=table), "one CUDA device"),
+                      (P.make_view(k, k[:2], lens), "alike"), (P.make_view(k, k, torch.zeros(6, dtype=torch.int32)[::2]), "contiguous"),
+                      (P.make_view(k, k, lens[None]), "contiguous"), (P.make_view(k[:, 0], k[:, 0], lens), "four axes"),
+                      (P.make_view(pool, pool, lens[:1], page_table=table[0]), "pages of 16"),
+                      (P.make_view(k, k, lens, page_table=table), "pages of 16"),
+                      (P.make_view(k.to("meta"), k.to("meta"), lens), "one CUDA device")):
+        assert view._dev == -1
+        for dev in (0, 1):
+            with pytest.raises(AssertionError, match=why):
+                fit(view, 1, _dev=dev)
+    # a view of one device against a context of another, and batches beyond the cache's or the table's rows
+    for view in (P.make_view(k, k, lens), P.make_view(pool, pool, lens, page_table=table)):
+        view._why, view._dev = None, 1
+        fit(view, _dev=1)
+        for wrong in (dict(_dev=0), dict(_dev=1, _hkv=4), dict(_dev=1, batch=4)):
+            with pytest.raises(AssertionError, match="those of the context"):
+                fit(view, wrong.pop("batch", 3), **wrong)
+    assert P.make_view(k[:2], k[:2], lens)._batch == 2 and P.make_view(pool, pool, lens, page_table=table[:1])._batch == 1
+
+
+def test_lengths_end_with_the_cache_or_a_row_of_the_page_table(lib):
+    k, lens = torch.zeros(3, 2, 48, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    pool, table = torch.zeros(9, 2, 16, 128, dtype=torch.bfloat16), torch.zeros(3, 8, dtype=torch.int32)
+    for make in (lambda **kw: P.make_view(k, k, lens, **kw), lambda **kw: P.make_view(pool, pool, lens, page_table=table[:, 2:5], **kw)):
+        view = make()
+        for context, bound in ((640, 48), (48, 0), (32, 0), (64, 48)):      # 0: the context's maximum
+            P.Context._fit(stand_in(_max_context=context), view, 3)         # one view, several contexts
+            assert view.max_seq_len == bound
+        P.Context._fit(stand_in(), make(max_seq_len=48), 3)
+        with pytest.raises(AssertionError, match="at most"):
+            P.Context._fit(stand_in(), make(max_seq_len=49), 3)
 
 
 # --------------------------------------------------------------------- the 64-bit forms' pins
