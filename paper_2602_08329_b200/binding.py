@@ -64,6 +64,7 @@ class KvView(C.Structure):
                 ("stride_head", C.c_int64), ("page_table", C.c_void_p),
                 ("page_table_stride", C.c_int32), ("seq_lens", C.c_void_p),
                 ("max_seq_len", C.c_int32), ("num_pages", C.c_int32)]
+    _why = _auto = None        # why the block calls refuse the view; the bound of its lengths that Context._fit has set
 
 
 class Schedule(C.Structure):
@@ -84,6 +85,7 @@ class ByteKvView(C.Structure):
                [(n, C.c_int64) for n in ("stride_outer", "stride_head", "scale_stride_outer", "scale_stride_head")] + \
                [("page_table", C.c_void_p), ("seq_lens", C.c_void_p)] + \
                [(n, C.c_int32) for n in ("page_table_stride", "max_seq_len", "num_pages", "format")]
+    _why = _auto = None
 
 
 class BlockBoundsView(C.Structure):
@@ -202,11 +204,13 @@ def make_schedule(top_k, window, sinks, refresh_interval=1, layer_group=1, dilat
 
 def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
     """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128]."""
-    kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, cap, span, dev, why = \
+    kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, span, dev, why = \
         (_marshal or _load_marshal()).kv_view(k, v, seq_lens, page_table)
     view = KvView.from_buffer_copy(_KV_PACK(kp, vp, so, sh, table, table_stride, lens, max_seq_len, pages))
     view._keep = (k, v, seq_lens, page_table)
-    view._batch, view._heads, view._cap, view._span, view._dev, view._why, view._auto = batch, heads, cap, span, dev, why, None
+    view._batch, view._heads, view._span, view._dev = batch, heads, span, dev
+    if why is not None:
+        view._why = why
     return view
 
 
@@ -217,12 +221,12 @@ def make_bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_tabl
     fp32 scales [B][Hkv][cap/16]; or paged [pool][Hkv][16][128] with scales [pool][Hkv].  Tails bf16
     [B][Hkv][16][128].
     """
-    (kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride, pages, fmt, batch, heads, cap, dev, span) = \
+    (kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride, pages, fmt, batch, heads, span, dev) = \
         (_marshal or _load_marshal()).bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table, max_seq_len)
     view = ByteKvView.from_buffer_copy(_BYTEKV_PACK(kp, vp, ksp, vsp, ktp, vtp, so, sh, sso, ssh, table, lens, table_stride,
                                                     max_seq_len, pages, fmt))
     view._keep = (k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table)
-    view._batch, view._heads, view._cap, view._span, view._dev, view._why, view._auto = batch, heads, cap, span, dev, None, None
+    view._batch, view._heads, view._span, view._dev = batch, heads, span, dev
     return view
 
 
@@ -389,10 +393,11 @@ class Context:
     def _fit_bounds(self, view, bounds, batch):
         self._fit(view, batch)
         assert bounds._heads == view._heads and bounds._dev == view._dev
-        if view._cap:
-            assert bounds._blocks * 16 >= (view.max_seq_len or self._max_context) and bounds._outer >= batch
+        pages = view.num_pages
+        if pages:
+            assert bounds._blocks == 0 and bounds._outer >= pages
         else:
-            assert bounds._blocks == 0 and bounds._outer >= view.num_pages
+            assert bounds._blocks * 16 >= (view.max_seq_len or self._max_context) and bounds._outer >= batch
 
     def _block_units(self, flags):
         return self._hkv if flags & PRHS_GROUP_SETS else self._hq

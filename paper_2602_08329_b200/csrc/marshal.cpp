@@ -41,8 +41,7 @@ bool count_is(Py_ssize_t nargs, Py_ssize_t n) {
 }
 
 // kv_view(k, v, seq_lens, page_table | None): k, v, stride_outer, stride_head, table, table_stride, seq_lens, pages, batch, heads,
-// cap (0: pages), span (positions that the cache, or a row of the page table, has), device (-1 where the block calls refuse the
-// view), why they do
+// span (positions that the cache, or a row of the page table, has), device (-1 where the block calls refuse the view), why they do
 PyObject* kv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (!count_is(nargs, 4)) return nullptr;
   const at::Tensor *k = tensor(a[0]), *v = tensor(a[1]), *lens = tensor(a[2]), *table = none(a[3]) ? nullptr : tensor(a[3]);
@@ -62,9 +61,9 @@ PyObject* kv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   else if (paged && (table->dim() != 2 || k->size(2) != 16)) why = "the page table is [batch][pages], of pages of 16 positions";
   else if (device(*v) != dev || device(*lens) != dev || (paged && device(*table) != dev) || dev < 0) why = "the tensors of a call are on one CUDA device";
   const int64_t batch = std::min(lens->numel(), paged ? table->size(0) : k->size(0));
-  const int64_t cap = paged ? 0 : k->size(2), span = !paged ? cap : table->dim() == 2 ? 16 * table->size(1) : 0;
-  return Py_BuildValue("LLLLLLLLLLLLLz", address(*k), address(*v), k->stride(0), k->stride(1), paged ? address(*table) : 0,
-                       paged ? table->stride(0) : 0, address(*lens), paged ? k->size(0) : 0, batch, k->size(1), cap, span, why ? -1 : dev, why);
+  const int64_t span = !paged ? k->size(2) : table->dim() == 2 ? 16 * table->size(1) : 0;
+  return Py_BuildValue("LLLLLLLLLLLLz", address(*k), address(*v), k->stride(0), k->stride(1), paged ? address(*table) : 0,
+                       paged ? table->stride(0) : 0, address(*lens), paged ? k->size(0) : 0, batch, k->size(1), span, why ? -1 : dev, why);
 }
 
 // bytekv_view(k, v, k_scale, v_scale, k_tail, v_tail, seq_lens, page_table | None, max_seq_len): six addresses, stride_outer,
@@ -100,10 +99,9 @@ PyObject* bytekv_view(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
             "scales are [batch][Hkv][cap / 16]");
     REQUIRE(k.size(0) >= batch && max_len <= k.size(2), "the cache holds the batch and max_seq_len positions");
   }
-  return Py_BuildValue("LLLLLLLLLLLLLLLLLLLL", address(k), address(v), address(ks), address(vs), address(kt), address(vt), k.stride(0),
+  return Py_BuildValue("LLLLLLLLLLLLLLLLLLL", address(k), address(v), address(ks), address(vs), address(kt), address(vt), k.stride(0),
                        k.stride(1), ks.stride(0), ks.stride(1), t[7] ? address(*t[7]) : 0, address(lens), t[7] ? t[7]->stride(0) : 0,
-                       t[7] ? k.size(0) : 0, type == at::kFloat8_e5m2 ? 1 : 0, batch, k.size(1), t[7] ? 0 : k.size(2), dev,
-                       t[7] ? 16 * t[7]->size(1) : k.size(2));
+                       t[7] ? k.size(0) : 0, type == at::kFloat8_e5m2 ? 1 : 0, batch, k.size(1), t[7] ? 16 * t[7]->size(1) : k.size(2), dev);
 }
 
 // bounds_view(codes, scale): codes, scale, stride_outer, stride_head, outer size, heads, blocks (0: per page), device
