@@ -177,7 +177,9 @@ BlockPlan block_plan(const prhs_ctx* c, int batch, uint32_t flags, int stride, i
   // a unit's blocks at most; a step knows more than the width of the table
   const int listed = step ? std::min(stride, step->sink_blocks + step->top_blocks + step->recent_blocks) : stride;
   BlockPlan plan;
-  plan.splits = block_splits(c, units, std::min(listed, blocks), heads);
+  // (a grid has at most 65535 sequences, and as many units of one, on its own axes; a warp per unit needs neither)
+  const bool axes = batch <= 65535 && units / batch <= 65535;
+  plan.splits = axes ? block_splits(c, units, std::min(listed, blocks), heads) : 0;
   plan.select = step && plan.splits > 0 && blocks <= kSelectKeys * kTThreads && step->top_blocks <= kSelectTop;
   return plan;
 }

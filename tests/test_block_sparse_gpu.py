@@ -501,6 +501,30 @@ def test_long_context_selection(cuda_device, t, top):
     ctx.close()
 
 
+def test_more_sequences_than_a_grid_axis_holds(cuda_device):
+    """65600 sequences over the same pages, 73 blocks each: the result of sequence b is that of b mod 64."""
+    batch, t, nb = 65600, 1165, 73
+    g = torch.Generator().manual_seed(5)
+    rows = torch.randn(2, nb * 16, 128, generator=g).to(torch.bfloat16)
+    pool = rows.view(2, nb, 1, 16, 128).to(cuda_device)
+    lens = torch.full((batch,), t, dtype=torch.int32, device=cuda_device)
+    table = torch.arange(nb, dtype=torch.int32, device=cuda_device).expand(batch, nb).contiguous()
+    view = P.make_view(pool[0], pool[1], lens, page_table=table)
+    q64 = torch.randn(64, 1, 128, generator=g).to(torch.bfloat16)
+    q = q64.repeat(batch // 64, 1, 1).to(cuda_device)
+    blocks = torch.arange(nb, dtype=torch.int32, device=cuda_device).expand(batch, 1, nb).contiguous()
+    count = torch.full((batch, 1), nb, dtype=torch.int32, device=cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full((batch, 1), math.nan, device=cuda_device)
+    ctx = P.Context(1, batch, 1, 1, nb * 16, 16, 16, 4, page_size=16)
+    ctx.block_decode_attn(q, view, blocks, count, batch, out, lse)
+    assert ctx.check() == 0
+    assert torch.equal(out, out[:64].repeat(batch // 64, 1, 1)) and torch.equal(lse, lse[:64].repeat(batch // 64, 1))
+    for b in (0, 5, 63):
+        y, l, tol, ltol = R.attend(np64(q64[b, 0]), rows[0, :t].double().numpy(), rows[1, :t].double().numpy(), True)
+        assert np.all(np.abs(np64(out[b, 0]) - y) <= tol) and abs(float(lse[b, 0]) - l) <= ltol
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits(cuda_device):
     # pages whose rows lie more than 2^32 elements behind the base
     H, pool = 8, (1 << 32) // (8 * 16 * 128) + 40
