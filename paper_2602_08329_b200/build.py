@@ -6,6 +6,7 @@ binding, into _marshal.so.
 """
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import subprocess
 import sys
@@ -33,11 +34,29 @@ def _older(target: str, inputs) -> bool:
 
 
 def stale() -> bool:
-    return _older(LIB, sources()) or _older(MARSHAL, marshal_sources())
+    return _older(LIB, sources()) or _marshal_stale()
 
 
 def marshal_sources():
     return [os.path.join(CSRC, "marshal.cpp"), os.path.join(os.path.dirname(HERE), "include", "prhs.h")]
+
+
+def _built_for():
+    """What _marshal.so has to fit, as the text that it carries; None without torch (and so without a use for it)."""
+    try:
+        return f"for torch {importlib.metadata.version('torch')}, python {sys.version_info.major}.{sys.version_info.minor};"
+    except importlib.metadata.PackageNotFoundError:
+        return None
+
+
+def _marshal_stale() -> bool:
+    wanted = _built_for()
+    if wanted is None:
+        return False
+    if _older(MARSHAL, marshal_sources()):
+        return True
+    with open(MARSHAL, "rb") as f:
+        return wanted.encode() not in f.read()
 
 
 def _run(cmd, what: str) -> str:
@@ -48,15 +67,20 @@ def _run(cmd, what: str) -> str:
 
 
 def build_marshal(force: bool = False) -> str:
-    """The extension links the torch libraries that the process has loaded anyway (no search path is recorded)."""
+    """The extension links the torch libraries that the process has loaded anyway (no search path is recorded).
+
+    It is built again for another torch or python.  Where there is no torch there is no Python binding either, and the C
+    library is built alone.
+    """
     src = os.path.join(CSRC, "marshal.cpp")
-    if force or _older(MARSHAL, marshal_sources()):
+    wanted = _built_for()
+    if wanted is not None and (force or _marshal_stale()):
         import torch
         root = os.path.dirname(torch.__file__)
         inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"]]
         _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] + [f"-I{p}" for p in inc] +
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DPRHS_BUILT_FOR="{wanted}"'] + [f"-I{p}" for p in inc] +
              ["-o", MARSHAL, src, "-L" + os.path.join(root, "lib"), "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python"], "g++")
     return MARSHAL
 

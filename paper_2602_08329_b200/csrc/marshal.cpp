@@ -352,4 +352,12 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&module_def); }
+#ifndef PRHS_BUILT_FOR
+#define PRHS_BUILT_FOR ""
+#endif
+// built_for: the torch and the python that this was compiled for (build.py looks for the text in the file)
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* module = PyModule_Create(&module_def);
+  if (module && PyModule_AddStringConstant(module, "built_for", PRHS_BUILT_FOR) < 0) Py_CLEAR(module);
+  return module;
+}

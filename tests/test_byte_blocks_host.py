@@ -53,6 +53,27 @@ def test_header_formats_match():
         assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(P, name)
 
 
+# ------------------------------------------------------------------------------- build
+def test_the_compiled_binding_is_built_again_for_another_torch(lib, monkeypatch):
+    assert P._load_marshal().built_for == B._built_for() and not B.stale()
+    commands = []
+    monkeypatch.setattr(B, "_run", lambda cmd, what: commands.append((what, cmd)) or "")
+    B.build()
+    assert commands == []
+    for version, made in (("99.1.0", ["g++"]), (None, [])):
+        def lookup(name, version=version):
+            if version is None:
+                raise B.importlib.metadata.PackageNotFoundError(name)
+            return version
+        monkeypatch.setattr(B.importlib.metadata, "version", lookup)
+        commands.clear()
+        assert B.stale() == bool(made)
+        B.build()
+        assert [what for what, _ in commands] == made
+    B.build(force=True)                          # no torch: the C library alone
+    assert [what for what, _ in commands] == ["nvcc"]
+
+
 # ------------------------------------------------------------------------------- refusals
 def test_null_context_is_refused(lib):
     kv, bounds, view = P.ByteKvView(), P.BlockBoundsView(), P.KvView()
