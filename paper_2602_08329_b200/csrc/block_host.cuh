@@ -7,12 +7,15 @@ namespace {
 constexpr int kMaxBlocks = kMaxContext / kBlockRows;
 
 cudaError_t block_set_attributes() {
-  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<false, false, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true, false, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<false, true, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true, true, false>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<false, false, true>, kTSmemBytes},
-                                                           {(const void*)block_attn_kernel<true, false, true>, kTSmemBytes},
+  const struct { const void* kernel; int bytes; } all[] = {{(const void*)block_attn_kernel<4, false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<4, true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<4, false, true>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<8, false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<8, true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<8, false, true>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<16, false, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<16, true, false>, kTSmemBytes},
+                                                           {(const void*)block_attn_kernel<16, false, true>, kTSmemBytes},
                                                            {(const void*)block_score_kernel<false>, kScoreSmemBytes},
                                                            {(const void*)block_score_kernel<true>, kScoreSmemBytes}};
   for (const auto& k : all) {
@@ -218,11 +221,13 @@ prhs_status launch_block_attn(prhs_ctx* c, const void* q, const KvDev& kv, const
   {
     LaunchScope ls(c, PRHS_KIND_ATTN_SPARSE, st);
     // `step`: the lists are this step's, from the kernel before; a caller's own may come from any kernel (ordinary launch)
-    const bool own = plan.splits == 0, wide = p.heads_per_unit > 8;
+    const bool own = plan.splits == 0;
     const dim3 grid = own ? dim3((p.units + kTWarps - 1) / kTWarps) : dim3(p.splits, p.units_per_seq, batch);
-    const auto kernel = own ? (wide ? block_attn_kernel<true, false, true> : block_attn_kernel<false, false, true>)
-                        : plan.select ? (wide ? block_attn_kernel<true, true, false> : block_attn_kernel<false, true, false>)
-                                      : (wide ? block_attn_kernel<true, false, false> : block_attn_kernel<false, false, false>);
+    auto form = [&](auto heads) {
+      constexpr int kHeads = decltype(heads)::value;
+      return own ? block_attn_kernel<kHeads, false, true> : plan.select ? block_attn_kernel<kHeads, true, false> : block_attn_kernel<kHeads, false, false>;
+    };
+    const auto kernel = p.heads_per_unit > 8 ? form(SlotC<16>{}) : p.heads_per_unit > 4 ? form(SlotC<8>{}) : form(SlotC<4>{});
     const cudaError_t e = launch_ordered(kernel, grid, kTThreads, kTSmemBytes, st, p, step ? 1 : 0);
     PRHS_CUDA(c, e);
   }

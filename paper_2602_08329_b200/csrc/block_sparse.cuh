@@ -535,8 +535,8 @@ __global__ void __launch_bounds__(kBSThreads) block_select_kernel(BlockSelectPar
 // ------------------------------------------------------------------------------- attention
 // Attention over listed blocks of a bf16 cache: one list per query head, or one per KV head for its whole group.
 // grid (splits, units per sequence, B).  A stage of the warp-private ring is one block, whose rows are
-// contiguous; rows past the end of the sequence are masked.  The arithmetic is bf16_stage: 16 MMAs per block
-// for up to eight heads (kWide: 32 for up to sixteen).  In a step, the first and the last blocks do not depend on
+// contiguous; rows past the end of the sequence are masked.  The arithmetic is bf16_stage for kHeads heads at most: 16 MMAs
+// per block for four, 24 for eight, 48 for sixteen.  In a step, the first and the last blocks do not depend on
 // the selection: they are attended over while it runs, before step_wait().
 struct BlockAttnParams {
   const __nv_bfloat16* q;
@@ -568,14 +568,14 @@ struct BlockAttnParams {
 // With 16000 positions, eight keys a thread, four warps take longer than sixteen and a launch: 11.9 against 11.2.
 constexpr int kSelectKeys = 4, kSelectTop = 256;
 // kOwn: a warp per unit, which it takes alone from start to end, four to a CTA; grid (units / 4).
-template <bool kWide, bool kSelect, bool kOwn>
+template <int kHeads, bool kSelect, bool kOwn>
 __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParams p) {
-  constexpr int kTiles = kWide ? 2 : 1;
+  constexpr int kTiles = kHeadTiles<kHeads>;
   static_assert(!(kSelect && kOwn), "a selection takes a CTA");
   __shared__ SelectSmem<kSelect ? kTThreads : 32> sm_select;
   __shared__ int sm_list[kSelect ? kSelectTop : 1];
   extern __shared__ __align__(128) unsigned char g_smem[];
-  __shared__ float sm_m[kTWarps][16], sm_l[kTWarps][16], sm_lt[kTWarps][16];
+  __shared__ float sm_m[kTWarps][16], sm_l[kTWarps][16];
   __shared__ bool is_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int own = blockIdx.x * kTWarps + warp;
@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(g_smem) + warp * (kTStages * kTStageBytes);
 
   uint32_t qb[kTiles][8][2];
-  load_query_bf16<kTiles>(p.q + (long long)unit0 * kHeadDim, gq, qb);
+  load_query_bf16<kHeads>(p.q + (long long)unit0 * kHeadDim, gq, qb);
   float o[kTiles][8][4];
   clear_tiles<kTiles>(o);
   SoftBf st[kTiles][2];
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
       issue(i + kTStages - 1, SlotC<(kSlot + kTStages - 1) % kTStages>{});
       if (rows == 0) return;
       const uint32_t kt = ring + (uint32_t)kSlot * kTStageBytes;
-      bf16_stage<kTiles>(kt, kt + kTTileBytes, qb, g < rows, g + 8 < rows, o, st);
+      bf16_stage<kHeads>(kt, kt + kTTileBytes, qb, g < rows, g + 8 < rows, o, st);
     };
     int i = 0;
     for (; i + 2 < nstages; i += 3) {
@@ -729,22 +729,22 @@ __global__ void __launch_bounds__(kTThreads, 2) block_attn_kernel(BlockAttnParam
   }
   if constexpr (kOwn) {                      // the warp's ring is free: it takes the unit's sums, a head in a row
     float* mine = reinterpret_cast<float*>(g_smem + warp * (kTStages * kTStageBytes));
-    store_partial_bf16<kTiles>(o, st, gq, mine, sm_m[warp], sm_l[warp], sm_lt[warp]);
+    store_partial_bf16<kHeads>(o, st, gq, mine, sm_m[warp], sm_l[warp]);
     __syncwarp();
     for (int h = 0; h < gq; ++h) {
       Merged r;
       r.m = sm_m[warp][h];
-      r.add(r.m, sm_l[warp][h], sm_lt[warp][h], reinterpret_cast<const float4*>(mine + h * kHeadDim)[lane]);
+      r.add(r.m, sm_l[warp][h], reinterpret_cast<const float4*>(mine + h * kHeadDim)[lane]);
       r.store(p.out, p.out_lse, unit0 + h);
     }
     return;
   }
   __syncthreads();                         // the ring is free: it takes the warps' partials
   float* sm_o = reinterpret_cast<float*>(g_smem);
-  store_partial_bf16<kTiles>(o, st, gq, sm_o + warp * gq * kHeadDim, sm_m[warp], sm_l[warp], sm_lt[warp]);
+  store_partial_bf16<kHeads>(o, st, gq, sm_o + warp * gq * kHeadDim, sm_m[warp], sm_l[warp]);
   __syncthreads();
   auto part_row = [&](int head, int part) -> float* { return p.partials + ((long long)(unit0 + head) * p.splits + part) * kPartStride; };
-  finish_unit<kTWarps>(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], kTWarps, gq, p.splits, split, part_row, p.tickets, p.out, p.out_lse, unit0,
+  finish_unit<kTWarps>(sm_o, &sm_m[0][0], &sm_l[0][0], kTWarps, gq, p.splits, split, part_row, p.tickets, p.out, p.out_lse, unit0,
               &is_last);
 }
 

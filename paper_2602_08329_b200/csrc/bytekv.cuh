@@ -342,7 +342,7 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
   extern __shared__ __align__(128) unsigned char g_smem[];
   __shared__ int tail_count[kBlockRows];       // kList: how often each row of the open block is listed
   __shared__ bool is_last;
-  __shared__ float sm_m[k8Warps + 1][16], sm_l[k8Warps + 1][16], sm_lt[k8Warps + 1][16];
+  __shared__ float sm_m[k8Warps + 1][16], sm_l[k8Warps + 1][16];
   float* sm_o = reinterpret_cast<float*>(g_smem);
   const int gq = kList ? 1 : p.group_size;
   const int num_kv = p.num_q_heads / p.group_size;
@@ -737,7 +737,7 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
 #pragma unroll
         for (int off = 4; off <= 16; off <<= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
         const int head = 8 * hh + 2 * tg + e;
-        if (g == 0) { sm_m[warp][head] = l == 0.f ? -INFINITY : st[hh][e].m; sm_l[warp][head] = l; sm_lt[warp][head] = l; }
+        if (g == 0) { sm_m[warp][head] = l == 0.f ? -INFINITY : st[hh][e].m; sm_l[warp][head] = l; }
         f[e] = __uint_as_float((uint32_t)min(max((int)st[hh][e].R + 127, 0), 254) << 23);     // 2^R
         if (head < gq) {
 #pragma unroll
@@ -754,10 +754,11 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
       tail_live = any != 0;
     }
     if (tail_live && warp == k8Warps - 1) {    // its rows are still in this warp's ring: the partials end before it
+      constexpr int kTailHeads = kList ? 4 : kWide ? 16 : 8;
       uint32_t tq[kTiles][8][2];
       float to[kTiles][8][4];
       SoftBf ts[kTiles][2];
-      load_query_bf16<kTiles>(p.q + (long long)unit0 * kHeadDim, gq, tq);
+      load_query_bf16<kTailHeads>(p.q + (long long)unit0 * kHeadDim, gq, tq);
       clear_tiles<kTiles>(to);
       int times[2];                            // how often this lane's two keys are attended
 #pragma unroll
@@ -775,17 +776,17 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
           }
           __syncwarp();
         }
-        bf16_stage<kTiles>(kt, vt, tq, times[0] > d, times[1] > d, to, ts);
+        bf16_stage<kTailHeads>(kt, vt, tq, times[0] > d, times[1] > d, to, ts);
         __syncwarp();
       }
-      store_partial_bf16<kTiles>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps], sm_lt[k8Warps]);
+      store_partial_bf16<kTailHeads>(to, ts, gq, sm_o + k8Warps * gq * kHeadDim, sm_m[k8Warps], sm_l[k8Warps]);
     }
     __syncthreads();
     // a part's place: two per CTA, the one it begins in the middle of and the other
     auto part_row = [&](int head, int i) -> float* {
       return p.partials + ((long long)(2 * (first_cta + i) + (i == 0 ? 1 : 0)) * gq + head) * kPartStride;
     };
-    finish_unit<k8Warps>(sm_o, &sm_m[0][0], &sm_l[0][0], &sm_lt[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
+    finish_unit<k8Warps>(sm_o, &sm_m[0][0], &sm_l[0][0], tail_live ? k8Warps + 1 : k8Warps, gq, parts, part, part_row, p.tickets,
                 p.out, p.out_lse, unit0, &is_last);
     unit_at += w;
     if (kList || deal == kParts || unit_at >= run_end) return;

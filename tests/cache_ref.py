@@ -90,3 +90,18 @@ def attend(q, k, v, weights_bf16):
     tol = 2.0 ** -8 * np.abs(y) + (2 * e + 2.0 ** -20 + 2.0 ** -12 + w) * big + len(k) * 2.0 ** -31 * p.max() * np.abs(v).max() + 2.0 ** -134
     lse = m + math.log(total)
     return y, lse, tol, e + 2.0 ** -20 + 2.0 ** -12 * (len(k) > 4096) + 2.0 ** -22 * abs(lse)
+
+
+def attend_few(q, k, v, weight):
+    """(y, lse, bound, bound on the lse's error) as `attend` gives them, for at most a few hundred rows: the sums counted term by
+    term (n roundings of 2^-23, numerator and divisor, a matrix product's included), and weights that enter the product to `weight`
+    relative ([n] or one number) while the divisor sums them as they are in fp32."""
+    y, lse, _, _ = attend(q, k, v, True)
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    if len(k) == 0:
+        return y, lse, np.zeros(128), 0.0
+    p = np.exp(k @ q * S - lse)
+    e = float((S * (131 * 2.0 ** -24 * (np.abs(k) @ np.abs(q)) + 2.0 ** -25 * np.abs(q).max() * np.abs(k).sum(-1))).max())
+    big = p @ np.abs(v)
+    tol = 2.0 ** -8 * np.abs(y) + (2 * e + 2.0 ** -20 + len(k) * 2.0 ** -22) * big + (p * weight) @ np.abs(v) + 2.0 ** -134
+    return y, lse, tol, e + 2.0 ** -20 + len(k) * 2.0 ** -23 + 2.0 ** -22 * abs(lse)

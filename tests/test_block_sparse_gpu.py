@@ -233,6 +233,32 @@ def test_attention_over_blocks(cuda_device, paged, heads, group, shared):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group,shared", [(2, 1, False), (2, 4, True), (1, 4, False), (1, 5, True), (2, 8, True), (1, 9, True), (1, 16, True)])
+def test_weights_keep_their_low_bits(cuda_device, heads, group, shared):
+    """Values of one size and either sign nearly cancel: what is left shows the weights' own rounding, 2^-16 for two bf16."""
+    lens = list(range(1, 41, 3)) + [96, 200]
+    cache = Cache(len(lens), heads, 200, False, cuda_device)
+    ctx = make_ctx(cache, group)
+    rows = random_rows(len(lens), heads, 200, 19, drift=False)
+    rows[1] = torch.where(rows[1] > 0, 1.0, -1.0).to(torch.bfloat16)
+    cache.place(rows, lens)
+    units = heads if shared else heads * group
+    nb = [-(-t // 16) for t in lens]
+    blocks = torch.arange(13, dtype=torch.int32, device=cuda_device).expand(len(lens), units, 13).contiguous()
+    count = torch.tensor(nb, dtype=torch.int32, device=cuda_device)[:, None].expand(len(lens), units).contiguous()
+    q = torch.randn(len(lens), heads * group, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.block_decode_attn(q, cache.view(), blocks, count, len(lens), out, lse, P.PRHS_GROUP_SETS if shared else 0)
+    assert ctx.check() == 0
+    y_all, l_all, qh = np64(out), np64(lse), np64(q)
+    for b, t in enumerate(lens):
+        for u in range(heads * group):
+            y, l, tol, ltol = R.attend_few(qh[b, u], *(rows[w, b, u // group, :t].double().numpy() for w in range(2)), 2.0 ** -16)
+            assert np.all(np.abs(y_all[b, u] - y) <= tol), (b, u, np.max(np.abs(y_all[b, u] - y) / tol))
+            assert abs(l_all[b, u] - l) <= ltol, (b, u)
+    ctx.close()
+
+
 def test_bad_pages_are_skipped_and_recorded(cuda_device):
     cache = Cache(1, 1, 160, True, cuda_device)
     ctx = make_ctx(cache, 1)

@@ -323,6 +323,39 @@ def test_attention_over_lists(cuda_device, fmt, paged, heads, group):
     ctx.close()
 
 
+@pytest.mark.parametrize("heads,group", [(2, 1), (1, 4), (1, 5), (1, 8), (1, 9), (1, 16)])
+def test_weights_of_the_open_block_keep_their_low_bits(cuda_device, heads, group):
+    """Over fewer than sixteen positions everything is in the open block; over all of them and over lists with repeats."""
+    lens = list(range(1, 16))
+    cache = Cache("e4m3", 15, heads, 16, False, cuda_device)
+    ctx = make_ctx(cache, group)
+    new = torch.randn(2, 15, heads, 16, 128, generator=torch.Generator().manual_seed(23))
+    new[1] = torch.where(new[1] > 0, 1.0, -1.0)
+    new = new.to(torch.bfloat16)
+    cache.set_lens(lens)
+    ctx.bytekv_append(new[0].to(cuda_device), new[1].to(cuda_device), cache.lens.clone(), cache.view(), 15)
+    U = heads * group
+    q = torch.randn(15, U, 128, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(cuda_device)
+    lists = {b: np.arange(40) * 7 % t for b, t in enumerate(lens)}
+    idx = torch.from_numpy(np.stack([lists[b] for b in range(15)])).to(torch.int32)[:, None].expand(15, U, 40).contiguous().to(cuda_device)
+    cnt = torch.full((15, U), 40, dtype=torch.int32, device=cuda_device)
+    for listed in (False, True):
+        out, lse = torch.full_like(q, math.nan), torch.full((15, U), math.nan, device=cuda_device)
+        if listed:
+            ctx.bytekv_sparse_decode_attn(q, cache.view(), idx, cnt, 15, out, lse)
+        else:
+            ctx.bytekv_decode_attn(q, cache.view(), 15, out, lse)
+        assert ctx.check() == 0
+        y_all, l_all, qh = np64(out), np64(lse), np64(q)
+        for b, t in enumerate(lens):
+            at = lists[b] if listed else np.arange(t)
+            for u in range(U):
+                y, l, tol, ltol = R.attend_few(qh[b, u], *(new[w, b, u // group].double().numpy()[at] for w in range(2)), 2.0 ** -16)
+                assert np.all(np.abs(y_all[b, u] - y) <= tol), (b, u, np.max(np.abs(y_all[b, u] - y) / tol))
+                assert abs(l_all[b, u] - l) <= ltol, (b, u)
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits(cuda_device):
     # a pool whose last pages lie more than 2^32 bytes behind the base
     H, pool = 8, (1 << 32) // (8 * 16 * 128) + 40
