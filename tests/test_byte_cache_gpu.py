@@ -512,6 +512,113 @@ def test_lengths_out_of_range_are_cut_and_recorded(cuda_device):
     ctx.close()
 
 
+# What the tests above grant the weights, two bf16 roundings for every row, would hide a block of values that is left out or
+# counted twice.  Here each row can be seen on its own.
+def visible_values(t, seed, by_row):
+    """Values [t][128], a power of two per row: block j at coordinate 5 j mod 128, blocks 128 apart with opposite signs; by_row:
+    the block's rows eight coordinates apart.  Codes, weights and products are exact."""
+    i = torch.arange(t)
+    j = i // 16
+    v = torch.zeros(t, 128)
+    v[i, (5 * j + (8 * (i % 16) if by_row else 0)) % 128] = torch.exp2(((j + seed) % 3 - i % 4).float()) * (1.0 - 2.0 * (j // 128 % 2).float())
+    return v
+
+
+def check_visible(out, lse, v, at, where):
+    """q = 0: every row in `at` has the weight 1 / n; one block, or one listed row, is a good part of its coordinate's sum."""
+    n = len(at)
+    want = v[at].sum(0) / n
+    size = np.abs(v[at]).sum(0) / n
+    assert np.all(np.abs(out - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -12 * size), where
+    assert abs(lse - math.log(n)) <= 2.0 ** -18, where
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("heads,group,lens", [
+    (1, 2, [2050]), (2, 4, [9001, 37]), (1, 16, [4708]), (1, 1, [70000]),                                         # even parts
+    (8, 2, [500] * 12 + [17, 0, 16, 499]), (8, 4, [1500, 20, 800, 333, 2500, 1] * 6),                             # one part each; runs
+    (8, 9, [2047, 100, 1000, 3] * 8), (8, 4, [160 + 16 * (b % 19) for b in range(70)])])                          # wide; whole units
+def test_every_block_counts_once(cuda_device, fmt, heads, group, lens):
+    B = len(lens)
+    cache = Cache(fmt, B, heads, max(lens), B > 1, cuda_device)
+    ctx = make_ctx(cache, group)
+    v = torch.stack([torch.stack([visible_values(max(lens), 2 * b + h, False) for h in range(heads)]) for b in range(min(B, 6))])
+    cache.set_lens(lens)
+    new_v = v.to(torch.bfloat16).to(cuda_device)[torch.arange(B, device=cuda_device) % len(v)]
+    ctx.bytekv_append(torch.ones_like(new_v), new_v, cache.lens.clone(), cache.view(), B)
+    q = torch.zeros(B, heads * group, 128, dtype=torch.bfloat16, device=cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+    ctx.bytekv_decode_attn(q, cache.view(), B, out, lse)
+    assert ctx.check() == 0
+    y, l, v64 = np64(out), np64(lse), v.double().numpy()
+    for b, t in enumerate(lens):
+        for u in range(heads * group):
+            if t == 0:
+                assert not y[b, u].any() and l[b, u] == -math.inf
+            else:
+                check_visible(y[b, u], l[b, u], v64[b % len(v), u // group], np.arange(t), (b, u))
+    ctx.close()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("heads,group,B,t,stride", [(2, 1, 1, 2050, 1500), (1, 4, 3, 700, 300), (8, 4, 10, 1003, 130), (8, 2, 16, 400, 33)])
+def test_every_entry_counts_once(cuda_device, fmt, paged, heads, group, B, t, stride):
+    """Lists in parts and in whole: each entry as often as it is listed."""
+    U = heads * group
+    cache = Cache(fmt, B, heads, t, paged, cuda_device)
+    ctx = make_ctx(cache, group)
+    v = torch.stack([torch.stack([visible_values(t, 2 * b + h, True) for h in range(heads)]) for b in range(B)])
+    cache.set_lens([t] * B)
+    new_v = v.to(torch.bfloat16).to(cuda_device)
+    ctx.bytekv_append(torch.ones_like(new_v), new_v, cache.lens.clone(), cache.view(), B)
+    rng = np.random.default_rng(3)
+    idx = rng.integers(0, t, (B, U, stride)).astype(np.int32)
+    idx[:, :, ::3] = np.sort(idx[:, :, ::3], -1)
+    cnt = rng.integers(1, stride + 1, (B, U)).astype(np.int32)
+    cnt[0, 0] = stride
+    q = torch.zeros(B, U, 128, dtype=torch.bfloat16, device=cuda_device)
+    out, lse = torch.full_like(q, math.nan), torch.full((B, U), math.nan, device=cuda_device)
+    ctx.bytekv_sparse_decode_attn(q, cache.view(), torch.from_numpy(idx).to(cuda_device), torch.from_numpy(cnt).to(cuda_device), B, out, lse)
+    assert ctx.check() == 0
+    y, l, v64 = np64(out), np64(lse), v.double().numpy()
+    for b in range(B):
+        for u in range(U):
+            check_visible(y[b, u], l[b, u], v64[b, u // group], idx[b, u, : cnt[b, u]], (b, u))
+    ctx.close()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("heads,group,lens", [(2, 1, [2050, 16, 37]), (1, 4, [333, 640, 5]), (1, 12, [1000, 77, 2048])])
+def test_weights_of_whole_blocks_keep_the_bits_of_fp16(cuda_device, fmt, heads, group, lens):
+    """Rows of the 8-bit cache are granted 2^-11 a weight, those of the open block 2^-16."""
+    B, t_max = len(lens), max(lens)
+    cache = Cache(fmt, B, heads, t_max, True, cuda_device)
+    ctx = make_ctx(cache, group)
+    fill(ctx, cache, lens)
+    q = (torch.randn(B, heads * group, 128, generator=torch.Generator().manual_seed(3)) * 2).to(torch.bfloat16).to(cuda_device)
+    idx = torch.stack([torch.arange(t_max) * 11 % t for t in lens]).to(torch.int32)[:, None].expand(B, heads * group, t_max).contiguous().to(cuda_device)
+    cnt = torch.tensor(lens, dtype=torch.int32, device=cuda_device)[:, None].expand(B, heads * group).contiguous()
+    qh = np64(q)
+    for listed in (False, True):
+        out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device=cuda_device)
+        if listed:
+            ctx.bytekv_sparse_decode_attn(q, cache.view(), idx, cnt, B, out, lse)
+        else:
+            ctx.bytekv_decode_attn(q, cache.view(), B, out, lse)
+        assert ctx.check() == 0
+        y_all = np64(out)
+        for b, t in enumerate(lens):
+            at = np64(idx[b, 0, :t]).astype(int) if listed else np.arange(t)
+            for u in range(heads * group):
+                k, v = cache.rows("k", b, u // group, t)[at], cache.rows("v", b, u // group, t)[at]
+                y, _, tol, _ = R.attend_few(qh[b, u], k, v, np.where(at < t // 16 * 16, 2.0 ** -11, 2.0 ** -16))
+                p = np.exp(k @ qh[b, u] * R.S)
+                small = 2.0 ** -31 * (p / p.sum()).max() * np.abs(v).max() * t          # fp16's smallest step
+                assert np.all(np.abs(y_all[b, u] - y) <= tol + small), (b, u, np.max(np.abs(y_all[b, u] - y) / (tol + small)))
+    ctx.close()
+
+
 def test_split_counts_agree(cuda_device):
     # one long sequence runs split over many CTAs, a batch of copies with fewer splits: both near the 64-bit value
     for batch in (1, 48):
