@@ -326,7 +326,8 @@ prhs_status prhs_delta(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, con
  *               row at    k + page*stride_outer + kvh*stride_head + (i%16)*128
  *               scale at  k_scale + page*scale_stride_outer + kvh*scale_stride_head
  * v and v_scale use the same strides.  Codes and tails are 16-byte aligned, code strides positive multiples of 128,
- * scale strides positive; a contiguous cache holds whole blocks (max_seq_len rounded up to 16 positions); a
+ * scale strides positive; scales are powers of two, for whoever writes them (those of values are read by their exponent); a
+ * contiguous cache holds whole blocks (max_seq_len rounded up to 16 positions); a
  * page table row holds max_seq_len / 16 entries, rounded up.  Fewer than 2^32 rows and 2^32 scales between the
  * bases and the last one addressed. */
 #define PRHS_BYTEKV_E4M3 0
@@ -460,7 +461,8 @@ prhs_status prhs_get_gate(prhs_ctx* ctx, int32_t layer, int32_t batch, int32_t* 
                           int32_t* host_ref, void* stream);
 
 /* Copy the logits of the last retrieval pass to the host: fp32 [batch][Hq][ld] with
- * ld = prhs_scores_ld().  Synchronous; for tests. */
+ * ld = prhs_scores_ld().  (prhs_block_topk and prhs_block_decode_step put their scores into the same workspace.)
+ * Synchronous; for tests. */
 prhs_status prhs_get_scores(prhs_ctx* ctx, int32_t batch, float* host_scores, void* stream);
 int32_t prhs_scores_ld(const prhs_ctx* ctx);
 

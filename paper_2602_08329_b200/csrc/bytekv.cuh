@@ -157,8 +157,8 @@ __global__ void __launch_bounds__(256) bytekv_append_kernel(ByteKvAppendParams p
 }
 
 // ------------------------------------------------------------------------------- attention
-// Decode attention over the 8-bit cache: every position (kList = false; one CTA column per KV head, the
-// group's heads share the stream) or an explicit list per query head (kList = true).
+// Decode attention over the 8-bit cache: every position (kList = false; a unit is a KV head of a sequence, whose query heads
+// share the stream) or an explicit list per query head (kList = true).  How units are dealt to CTAs stands further down.
 //
 // The plumbing is that of the bf16 kernels (attn.cuh): warp-private cp.async rings of 16-row stages,
 // 16-byte chunk c of row r at chunk c ^ (r & 7), parts of a unit merged by the last CTA to arrive.  What
@@ -185,7 +185,8 @@ __global__ void __launch_bounds__(256) bytekv_append_kernel(ByteKvAppendParams p
 // largest element).  A key block's scale multiplies its logits.  A value block's scale 2^e multiplies the
 // weights: w = 2^(x - m) * 2^(e - R + 7), with m the running reference of the logits and R, an integer per
 // head, that of the value scales; both move only when a weight would exceed 2^15 (one vote a stage).
-// fp16 keeps w to 2^-12 relative down to 2^-29 of the largest weight.  The sum of the weights, m and the
+// The largest weight stands between 2^6 (where the reference has just moved) and 2^15, so fp16 keeps weights to 2^-11 relative
+// down to 2^-20 of the largest, and to 2^-31 of the largest below that.  The sum of the weights, m and the
 // accumulators are fp32.
 // The open block (bf16) enters the ring behind the last stage of the last warp and is one stage of the bf16 arithmetic
 // (bf16_stage) into a partial of its own, merged with the warps' partials.

@@ -4,8 +4,9 @@ Error bounds.  A rounding to a type is off by at most half a step, eps / 2 relat
 The attention kernels differ from the exact value by
   * logits: products are exact, 128 fp32 additions, the factor's two roundings, and the fp16 image of the query
     (exact to 2^-25 of its largest element):  e = s (131 * 2^-24 sum|q k| + 2^-25 max|q| sum|k|), s = 128^-1/2;
-  * weights: exp2 to 2^-21, one rounding to fp16 (2^-11; bf16: 2^-8 in the numerator and in the sum that
-    divides it), nothing smaller than 2^-31 of the largest weight kept by fp16;
+  * weights: exp2 to 2^-21, one rounding to fp16 (2^-11) for rows of whole blocks of the 8-bit cache, two to bf16 (2^-16
+    together) for bf16 rows (weights_bf16 grants one in the numerator and one in the sum that divides it, 2^-8 each;
+    `attend_few` what they have), nothing smaller than 2^-31 of the largest weight kept by fp16;
   * a sum of n fp32 terms in partial sums of at most 4096: 2^-12 relative is generous for n <= 2^17;
   * the result's rounding to bf16: 2^-8 |y|, and half a step of its subnormals, 2^-134.
 With A = sum_i p_i |v_i| (p normalised) the first two give (2 e + 2^-20 + w) A, w = 2^-11 or 2 * 2^-8.
