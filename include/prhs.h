@@ -371,7 +371,7 @@ prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const 
 prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
                                  void* stream);
 
-/* prhs_sparse_decode_attn over the 8-bit cache: same lists, same outputs. */
+/* prhs_sparse_decode_attn over the 8-bit cache: same lists, same outputs; idx_stride <= 2^30. */
 prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, const int32_t* idx,
                                         const int32_t* count, int32_t idx_stride, int32_t batch, void* out, float* out_lse,
                                         void* stream);

@@ -203,7 +203,11 @@ def make_schedule(top_k, window, sinks, refresh_interval=1, layer_group=1, dilat
 
 
 def make_view(k, v, seq_lens, page_table=None, max_seq_len=0) -> KvView:
-    """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128]."""
+    """View of a cache tensor: contiguous [B][Hkv][cap][128] or paged [pool][Hkv][16][128].
+
+    The block calls ask for v of k's size, contiguous lengths, rows of the cache or of the page table for the whole batch, all on the
+    context's device, and max_seq_len at most what the cache, or a row of the table, holds (0: that, or the context's maximum).
+    """
     kp, vp, so, sh, table, table_stride, lens, pages, batch, heads, span, dev, why = \
         (_marshal or _load_marshal()).kv_view(k, v, seq_lens, page_table)
     view = KvView.from_buffer_copy(_KV_PACK(kp, vp, so, sh, table, table_stride, lens, max_seq_len, pages))

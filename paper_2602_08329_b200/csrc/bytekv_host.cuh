@@ -190,6 +190,7 @@ prhs_status prhs_bytekv_sparse_decode_attn(prhs_ctx* ctx, const void* q, const p
   if (!ctx) return PRHS_ERR_INVALID_ARG;
   if (!idx || !count) return fail(ctx, PRHS_ERR_INVALID_ARG, "NULL pointer");
   if (idx_stride < 1) return fail(ctx, PRHS_ERR_INVALID_ARG, "idx_stride must be >= 1");
+  if (idx_stride > (1 << 30)) return fail(ctx, PRHS_ERR_UNSUPPORTED, "idx_stride above 2^30");
   ByteKvDev dv;
   int max_t;
   prhs_status rc = check_q_out(ctx, q, out, batch);

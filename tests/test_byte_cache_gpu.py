@@ -512,6 +512,27 @@ def test_lengths_out_of_range_are_cut_and_recorded(cuda_device):
     ctx.close()
 
 
+def test_a_list_stride_near_the_end_of_int32_is_refused(cuda_device):
+    """(Rounded up to sixteen it would leave int32.)  A stride is only a distance: with one unit the buffer need not be that long."""
+    cache = Cache("e4m3", 1, 1, 64, False, cuda_device)
+    ctx = make_ctx(cache, 1)
+    fill(ctx, cache, [64])
+    q = torch.zeros(1, 1, 128, dtype=torch.bfloat16, device=cuda_device)
+    out, lse = torch.full_like(q, 7.0), torch.full((1, 1), 7.0, device=cuda_device)
+    idx, cnt = torch.arange(64, dtype=torch.int32, device=cuda_device), torch.full((1,), 40, dtype=torch.int32, device=cuda_device)
+    view = cache.view()
+    for stride in ((1 << 30) + 1, (1 << 31) - 16, (1 << 31) - 1):
+        rc = ctx.lib.prhs_bytekv_sparse_decode_attn(ctx.h, q.data_ptr(), P.C.byref(view), idx.data_ptr(), cnt.data_ptr(), stride, 1, out.data_ptr(),
+                                                    lse.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        assert rc == 2, stride
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    rc = ctx.lib.prhs_bytekv_sparse_decode_attn(ctx.h, q.data_ptr(), P.C.byref(view), idx.data_ptr(), cnt.data_ptr(), 1 << 20, 1, out.data_ptr(),
+                                                lse.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and ctx.check() == 0 and abs(float(lse[0, 0]) - math.log(40)) <= 2.0 ** -18
+    ctx.close()
+
+
 # What the tests above grant the weights, two bf16 roundings for every row, would hide a block of values that is left out or
 # counted twice.  Here each row can be seen on its own.
 def visible_values(t, seed, by_row):
