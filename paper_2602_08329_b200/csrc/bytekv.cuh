@@ -659,8 +659,9 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
             x[hh][e][n] = (s[hh][0][2 * n + e] + s[hh][1][2 * n + e]) * (qm[hh][e] * ks[n]);
             if (kList && !((vm >> (8 * n + g)) & 1u)) x[hh][e][n] = -INFINITY;
           }
-          if (kList) exceed = exceed || fmaxf(x[hh][e][0] + fmaxf(ve[0] - h.R, 0.f), x[hh][e][1] + fmaxf(ve[1] - h.R, 0.f)) > h.m + 8.f;
-          else exceed = exceed || fmaxf(x[hh][e][0], x[hh][e][1]) + fmaxf(ve[0] - h.R, 0.f) > h.m + 8.f;
+          // (logits are compared by their differences: a large one has no room for an exponent beside it)
+          if (kList) exceed = exceed || x[hh][e][0] - h.m > 8.f - fmaxf(ve[0] - h.R, 0.f) || x[hh][e][1] - h.m > 8.f - fmaxf(ve[1] - h.R, 0.f);
+          else exceed = exceed || fmaxf(x[hh][e][0], x[hh][e][1]) - h.m > 8.f - fmaxf(ve[0] - h.R, 0.f);
         }
       if (__any_sync(0xffffffffu, exceed)) {
 #pragma unroll
@@ -670,15 +671,14 @@ bytekv_attn_kernel(ByteKvAttnParams p) {
           for (int e = 0; e < 2; ++e) {
             Soft8& h = st[hh][e];
             float mx = fmaxf(x[hh][e][0], x[hh][e][1]);
-            float my = fmaxf(x[hh][e][0] + ve[0], x[hh][e][1] + ve[1]);
 #pragma unroll
-            for (int off = 4; off <= 16; off <<= 1) {
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-              my = fmaxf(my, __shfl_xor_sync(0xffffffffu, my, off));
-            }
+            for (int off = 4; off <= 16; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
             const float mn = fmaxf(h.m, mx);
+            float my = fmaxf(x[hh][e][0] - mn + ve[0], x[hh][e][1] - mn + ve[1]);
+#pragma unroll
+            for (int off = 4; off <= 16; off <<= 1) my = fmaxf(my, __shfl_xor_sync(0xffffffffu, my, off));
             // m + R, the reference of the weighted values, moves up only
-            const float Rn = fmaxf(ceilf(fmaxf(my, h.m + h.R) - mn), -400.f);
+            const float Rn = fmaxf(ceilf(fmaxf(my, h.m - mn + h.R)), -400.f);
             fo[e] = exp2_fast(h.m - mn + h.R - Rn);
             h.l *= exp2_fast(h.m - mn);
             h.m = mn;

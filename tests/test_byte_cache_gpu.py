@@ -610,6 +610,36 @@ def test_every_entry_counts_once(cuda_device, fmt, paged, heads, group, B, t, st
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("size", [2.0 ** 4, 2.0 ** 9, 2.0 ** 12, 2.0 ** 20])
+@pytest.mark.parametrize("v_size", [2.0 ** -40, 1.0, 2.0 ** 20])
+def test_large_logits_leave_the_scales_of_the_values_alone(cuda_device, fmt, size, v_size):
+    """Equal keys, so every row has the same weight whatever the logits' size (up to 2^44, where a step of fp32 is 2^20)."""
+    lens, heads, group = [1610, 331, 96], 2, 3
+    cache = Cache(fmt, 3, heads, 1610, False, cuda_device)
+    ctx = make_ctx(cache, group)
+    v = torch.stack([torch.stack([visible_values(1610, 2 * b + h, False) for h in range(heads)]) for b in range(3)]) * v_size
+    k = torch.full((3, heads, 1610, 128), size, dtype=torch.bfloat16, device=cuda_device)
+    cache.set_lens(lens)
+    ctx.bytekv_append(k, v.to(torch.bfloat16).to(cuda_device), cache.lens.clone(), cache.view(), 3)
+    U = heads * group
+    q = torch.full((3, U, 128), size, dtype=torch.bfloat16, device=cuda_device)
+    idx = torch.arange(1610, dtype=torch.int32, device=cuda_device).expand(3, U, 1610).contiguous()
+    cnt = torch.tensor(lens, dtype=torch.int32, device=cuda_device)[:, None].expand(3, U).contiguous()
+    for listed in (False, True):
+        out = torch.full_like(q, math.nan)
+        if listed:
+            ctx.bytekv_sparse_decode_attn(q, cache.view(), idx, cnt, 3, out)
+        else:
+            ctx.bytekv_decode_attn(q, cache.view(), 3, out)
+        assert ctx.check() == 0
+        y, v64 = np64(out), v.double().numpy()
+        for b, t in enumerate(lens):
+            for u in range(U):
+                check_visible(y[b, u], math.log(t), v64[b, u // group], np.arange(t), (b, u, listed))
+    ctx.close()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("heads,group,lens", [(2, 1, [2050, 16, 37]), (1, 4, [333, 640, 5]), (1, 12, [1000, 77, 2048])])
 def test_weights_of_whole_blocks_keep_the_bits_of_fp16(cuda_device, fmt, heads, group, lens):
     """Rows of the 8-bit cache are granted 2^-11 a weight, those of the open block 2^-16."""
