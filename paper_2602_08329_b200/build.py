@@ -7,6 +7,7 @@ binding, into _marshal.so.
 from __future__ import annotations
 
 import importlib.metadata
+import importlib.util
 import os
 import subprocess
 import sys
@@ -43,10 +44,14 @@ def marshal_sources():
 
 def _built_for():
     """What _marshal.so has to fit, as the text that it carries; None without torch (and so without a use for it)."""
-    try:
-        return f"for torch {importlib.metadata.version('torch')}, python {sys.version_info.major}.{sys.version_info.minor};"
-    except importlib.metadata.PackageNotFoundError:
+    if importlib.util.find_spec("torch") is None:
         return None
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:       # a source tree on the path
+        import torch
+        version = torch.__version__
+    return f"for torch {version}, python {sys.version_info.major}.{sys.version_info.minor};"
 
 
 def _marshal_stale() -> bool:

@@ -61,17 +61,21 @@ def test_the_compiled_binding_is_built_again_for_another_torch(lib, monkeypatch)
     B.build()
     assert commands == []
     for version, made in (("99.1.0", ["g++"]), (None, [])):
-        def lookup(name, version=version):
-            if version is None:
-                raise B.importlib.metadata.PackageNotFoundError(name)
-            return version
-        monkeypatch.setattr(B.importlib.metadata, "version", lookup)
+        monkeypatch.setattr(B.importlib.metadata, "version", lambda name, version=version: version)
+        monkeypatch.setattr(B.importlib.util, "find_spec", lambda name, version=version: version)
         commands.clear()
         assert B.stale() == bool(made)
         B.build()
         assert [what for what, _ in commands] == made
     B.build(force=True)                          # no torch: the C library alone
     assert [what for what, _ in commands] == ["nvcc"]
+
+
+def test_a_torch_without_metadata_is_known_by_its_version(monkeypatch):
+    def unknown(name):
+        raise B.importlib.metadata.PackageNotFoundError(name)
+    monkeypatch.setattr(B.importlib.metadata, "version", unknown)
+    assert torch.__version__ in B._built_for()
 
 
 # ------------------------------------------------------------------------------- refusals
