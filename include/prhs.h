@@ -326,8 +326,8 @@ prhs_status prhs_delta(prhs_ctx* ctx, const void* q, const prhs_kv_view* kv, con
  *               row at    k + page*stride_outer + kvh*stride_head + (i%16)*128
  *               scale at  k_scale + page*scale_stride_outer + kvh*scale_stride_head
  * v and v_scale use the same strides.  Codes and tails are 16-byte aligned, code strides positive multiples of 128,
- * scale strides positive; scales are powers of two, for whoever writes them (those of values are read by their exponent); a
- * contiguous cache holds whole blocks (max_seq_len rounded up to 16 positions); a
+ * scale strides positive; scales are powers of two, for whoever writes them (those of values are read by their exponent).
+ * A contiguous cache holds whole blocks (max_seq_len rounded up to 16 positions); a
  * page table row holds max_seq_len / 16 entries, rounded up.  Fewer than 2^32 rows and 2^32 scales between the
  * bases and the last one addressed. */
 #define PRHS_BYTEKV_E4M3 0
@@ -366,8 +366,8 @@ prhs_status prhs_bytekv_append(prhs_ctx* ctx, const prhs_bytekv_view* kv, const 
 
 /* prhs_dense_decode_attn over the 8-bit cache: attention over all i < t_b.  t_b = 0 gives a zero output row and
  * lse = -inf; a t_b outside [0, max_seq_len] is cut to it and recorded (PRHS_FLAG_BAD_LENGTH).  A logit that is NaN or +inf
- * makes the row and its lse NaN, as the formula has it (also in the calls below).  q and out are 16-byte aligned and do not
- * overlap. */
+ * makes the row and its lse NaN, as the formula has it; a value that is infinite or NaN makes its coordinate infinite or NaN
+ * (also in the calls below).  q and out are 16-byte aligned and do not overlap. */
 prhs_status prhs_bytekv_decode_attn(prhs_ctx* ctx, const void* q, const prhs_bytekv_view* kv, int32_t batch, void* out, float* out_lse,
                                  void* stream);
 
