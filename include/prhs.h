@@ -435,6 +435,65 @@ prhs_status prhs_block_decode_step(prhs_ctx* ctx, const void* q, const prhs_kv_v
                                    const prhs_block_schedule* sched, int32_t batch, void* out, float* out_lse, int32_t* out_blocks,
                                    int32_t blocks_stride, int32_t* out_count, void* stream);
 
+/* -------------------------------------------------------------------------- new tokens
+ * (No counterpart in the paper, whose step starts from queries and a cache that are ready.)  The new tokens of several
+ * sequences come packed, one row each: sequence b has rows row_start[b] .. row_start[b + 1] - 1, and its n_b new
+ * tokens are the last n_b positions of its t_b (seq_lens counts them already), in order.  What rows of no sequence (padding)
+ * hold does not matter, and what they have in an output is left as it was.  A sequence with n_b outside [0, t_b], rows outside
+ * [0, num_rows) or t_b above max_seq_len is left out and recorded (PRHS_FLAG_BAD_LENGTH).  */
+typedef struct {
+  const void* q;              /* device bf16: head h of row r at  q + r*q_stride_row + h*q_stride_head  (elements) */
+  const void* k;              /* Hkv heads each, in the same way */
+  const void* v;
+  int64_t q_stride_row, q_stride_head, k_stride_row, k_stride_head, v_stride_row, v_stride_head; /* multiples of 8, >= 0 */
+  const int32_t* row_start;   /* device [batch + 1], ascending, or NULL: one row per sequence (num_rows = batch) */
+  const int32_t* positions;   /* device int32 [num_axes][positions_stride], a column per row; NULL: the token's position
+                                 in its sequence, on every axis                                                  */
+  int64_t positions_stride;   /* >= num_rows */
+  int32_t num_rows;
+} prhs_token_rows;
+
+/* How queries and keys are made from the projection's output, per head, in fp32 with one rounding to bf16 at the end:
+ *   norm (PRHS_PREP_NORM):  x <- x / sqrt(mean(x^2) + eps) * weight
+ *   rotation of the first rot_dim values: pair f (x_f and x_{f + rot_dim / 2}, or x_{2f} and x_{2f + 1} with
+ *   PRHS_PREP_ADJACENT) is turned by  positions[axis_of[f]] * inv_freq[f]  (the angle is formed in fp64) and multiplied by
+ *   rot_scale.  Several axes (time, height, width) are told apart by axis_of. */
+#define PRHS_PREP_NORM     1u
+#define PRHS_PREP_ADJACENT 2u
+#define PRHS_MAX_AXES 4
+typedef struct {
+  const float* q_weight;      /* device fp32 [128], or NULL: ones; only with PRHS_PREP_NORM */
+  const float* k_weight;
+  const float* inv_freq;      /* device fp32 [rot_dim / 2]; may be NULL with rot_dim = 0 */
+  float eps;                  /* >= 0 */
+  float rot_scale;            /* factor of cosines and sines; 1 for a plain rotation */
+  int32_t rot_dim;            /* even, 0 .. 128; 0 = no rotation */
+  int32_t num_axes;           /* 1 .. PRHS_MAX_AXES */
+  uint32_t flags;             /* PRHS_PREP_* */
+  uint8_t axis_of[64];        /* axis of each pair, < num_axes */
+} prhs_qk_prep;
+
+/* Queries and keys prepared, keys and values written to their positions of the bf16 cache (which the view's const does not
+ * keep from being written), queries to q_out, in one pass.
+ *   q_out  device bf16 [num_rows][Hq][128], 16-byte aligned, apart from the rows that come in
+ * A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE) and its rows are not written. */
+prhs_status prhs_qkv_append(prhs_ctx* ctx, const prhs_token_rows* rows, const prhs_qk_prep* prep, const prhs_kv_view* kv,
+                            int32_t batch, void* q_out, void* stream);
+
+/* The same into the 8-bit cache: keys are rounded to bf16 as above and then go where prhs_bytekv_append would put them, so that
+ * the cache holds the same whichever way rows came in.  (Infinities and NaNs as there.) */
+prhs_status prhs_bytekv_qkv_append(prhs_ctx* ctx, const prhs_token_rows* rows, const prhs_qk_prep* prep, const prhs_bytekv_view* kv,
+                                   int32_t batch, void* q_out, void* stream);
+
+/* Rows of the 8-bit cache read back: positions [first[b], t_b) (first = NULL: all) as bf16, scale * code rounded once (exact
+ * where bf16 has the range; the open block's rows are copied), into a bf16 cache of the same kind (contiguous or paged, with pages of its
+ * own; its seq_lens are not read, its max_seq_len is at least that of kv).  For whoever attends over the cache with
+ * prhs_chunk_attn or the calls for bf16 caches.  max_new: host-side upper bound of t_b - first[b]; 0 = max_seq_len.  A sequence with
+ * first[b] outside [0, t_b], more rows than max_new or t_b above max_seq_len is left out and recorded
+ * (PRHS_FLAG_BAD_LENGTH). */
+prhs_status prhs_bytekv_read(prhs_ctx* ctx, const prhs_bytekv_view* kv, const prhs_kv_view* out, const int32_t* first, int32_t max_new,
+                             int32_t batch, void* stream);
+
 /* Largest index-list length any call can produce: S0 + k + 2*r*m + W from prhs_config. */
 int32_t prhs_index_capacity(const prhs_ctx* ctx);
 

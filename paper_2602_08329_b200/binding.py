@@ -27,6 +27,7 @@ PRHS_GROUP_SETS = 4
 PRHS_FLAG_BAD_INDEX, PRHS_FLAG_BAD_PAGE, PRHS_FLAG_SELECT_FALLBACK, PRHS_FLAG_TIMEOUT = 1, 2, 4, 8
 PRHS_FLAG_BAD_LENGTH, PRHS_FLAG_NONFINITE = 16, 32
 PRHS_BYTEKV_E4M3, PRHS_BYTEKV_E5M2 = 0, 1
+PRHS_PREP_NORM, PRHS_PREP_ADJACENT, PRHS_MAX_AXES = 1, 2, 4
 PRHS_CFG_NO_TMA = 1
 PRHS_CFG_TMA_GATHER = 2
 PRHS_CFG_MMA_SYNC_SCORE = 4
@@ -41,7 +42,7 @@ EXPORTS = ["prhs_create", "prhs_destroy", "prhs_score_topk", "prhs_build_index_s
            "prhs_profile_end", "prhs_kernel_kind_name", "prhs_sparse_decode_attn_noalloc", "prhs_get_gate",
            "prhs_noalloc_check", "prhs_gather_probe", "prhs_bytekv_append", "prhs_bytekv_decode_attn",
            "prhs_bytekv_sparse_decode_attn", "prhs_block_bounds", "prhs_block_topk", "prhs_block_decode_attn",
-           "prhs_block_decode_step"]
+           "prhs_block_decode_step", "prhs_qkv_append", "prhs_bytekv_qkv_append", "prhs_bytekv_read"]
 NOALLOC_MAX_UNITS = 1024
 KERNEL_KINDS = 6
 
@@ -96,11 +97,25 @@ class BlockSchedule(C.Structure):
     _fields_ = [("top_blocks", C.c_int32), ("sink_blocks", C.c_int32), ("recent_blocks", C.c_int32), ("flags", C.c_uint32)]
 
 
+class TokenRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + \
+               [(n, C.c_int64) for n in ("q_stride_row", "q_stride_head", "k_stride_row", "k_stride_head", "v_stride_row",
+                                         "v_stride_head")] + \
+               [("row_start", C.c_void_p), ("positions", C.c_void_p), ("positions_stride", C.c_int64), ("num_rows", C.c_int32)]
+
+
+class QkPrep(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("eps", C.c_float),
+                ("rot_scale", C.c_float), ("rot_dim", C.c_int32), ("num_axes", C.c_int32), ("flags", C.c_uint32),
+                ("axis_of", C.c_uint8 * 64)]
+    _dev = None
+
+
 _lib = None
 _marshal = None
 # the calls the compiled helper makes, in the order it takes their addresses
 _MARSHAL_CALLS = ("bytekv_append", "bytekv_decode_attn", "bytekv_sparse_decode_attn", "block_bounds", "block_topk",
-                  "block_decode_attn", "block_decode_step")
+                  "block_decode_attn", "block_decode_step", "qkv_append", "bytekv_qkv_append", "bytekv_read")
 
 
 def _load_marshal():
@@ -151,6 +166,9 @@ def load() -> C.CDLL:
         "prhs_block_decode_attn": (st, [vp, vp, C.POINTER(KvView), vp, vp, i32, C.c_uint32, i32, vp, vp, vp]),
         "prhs_block_decode_step": (st, [vp, vp, C.POINTER(KvView), C.POINTER(BlockBoundsView), C.POINTER(BlockSchedule), i32,
                                         vp, vp, vp, i32, vp, vp]),
+        "prhs_qkv_append": (st, [vp, C.POINTER(TokenRows), C.POINTER(QkPrep), C.POINTER(KvView), i32, vp, vp]),
+        "prhs_bytekv_qkv_append": (st, [vp, C.POINTER(TokenRows), C.POINTER(QkPrep), C.POINTER(ByteKvView), i32, vp, vp]),
+        "prhs_bytekv_read": (st, [vp, C.POINTER(ByteKvView), C.POINTER(KvView), vp, i32, i32, vp]),
         "prhs_delta": (st, [vp, vp, C.POINTER(KvView), vp, vp, i32, i32, vp, vp]),
         "prhs_index_capacity": (i32, [vp]),
         "prhs_get_index_set": (st, [vp, i32, vp, vp, vp]),
@@ -244,6 +262,37 @@ def make_block_bounds(codes, scale) -> BlockBoundsView:
 
 def make_block_schedule(top_blocks, sink_blocks=1, recent_blocks=1, flags=0) -> BlockSchedule:
     return BlockSchedule(top_blocks, sink_blocks, recent_blocks, flags)
+
+
+def rotation_axes(sections, interleaved=False):
+    """Which axis each frequency takes its position from: sections[a] frequencies for axis a, one axis after the other, or (interleaved)
+    in turn for as long as an axis has any left."""
+    if not interleaved:
+        return [a for a, n in enumerate(sections) for _ in range(n)]
+    return [a for i in range(max(sections, default=0)) for a, n in enumerate(sections) if i < n]
+
+
+def make_qk_prep(q_weight=None, k_weight=None, eps=1e-6, norm=None, inv_freq=None, adjacent=False, axis_of=None,
+                 rot_scale=1.0) -> QkPrep:
+    """How new queries and keys are made: norm per head (weights fp32 [128]; norm=True without weights: ones), then the rotation of
+    the first 2 * len(inv_freq) values (fp32; halves, or adjacent pairs), axis_of[f] naming the axis of pair f (see rotation_axes)."""
+    norm = q_weight is not None or k_weight is not None if norm is None else norm
+    dev = None
+    for t, n in ((q_weight, 128), (k_weight, 128), (inv_freq, None)):
+        if t is None:
+            continue
+        assert t.dtype == torch.float32 and t.is_cuda and t.dim() == 1 and t.is_contiguous(), "weights and inv_freq are contiguous fp32 on a CUDA device"
+        assert n is None or t.shape[0] == n, "weights have 128 values"
+        assert dev in (None, t.get_device()), "weights and inv_freq are on one device"
+        dev = t.get_device()
+    pairs = 0 if inv_freq is None else inv_freq.shape[0]
+    assert pairs <= 64, "at most 128 values are rotated"
+    axes = [0] * pairs if axis_of is None else list(axis_of)
+    assert len(axes) == pairs and all(0 <= a < PRHS_MAX_AXES for a in axes), "axis_of names an axis for each of inv_freq"
+    p = QkPrep(_ptr(q_weight), _ptr(k_weight), _ptr(inv_freq) if pairs else None, eps, rot_scale, 2 * pairs, max(axes, default=0) + 1,
+               (PRHS_PREP_NORM if norm else 0) | (PRHS_PREP_ADJACENT if adjacent else 0), (C.c_uint8 * 64)(*axes))
+    p._keep, p._dev = (q_weight, k_weight, inv_freq), dev
+    return p
 
 
 class Context:
@@ -380,6 +429,34 @@ class Context:
         self._fit_bounds(view, bounds, batch)
         rc = _marshal.block_decode_step(self._h, C.addressof(view), C.addressof(bounds), C.addressof(sched), q, out, out_lse, batch,
                                         self._hq, self._block_units(sched.flags), view._dev, _stream(stream), out_blocks, out_count)
+        if rc:
+            self._ck(rc)
+
+    # -- new tokens
+    def qkv_append(self, q, k, v, view, prep, batch, q_out, row_start=None, positions=None, stream=None):
+        """New tokens into the bf16 cache: q, k, v bf16 [rows][heads][128] (any strides over the first two axes) packed sequence after
+        sequence, row_start int32 [batch + 1] (None: a row each); positions int32 [axes][rows] (None: those in the cache)."""
+        self._fit(view, batch)
+        assert prep._dev in (None, view._dev), "the weights are on the cache's device"
+        rc = _marshal.qkv_append(self._h, C.addressof(view), C.addressof(prep), q, k, v, q_out, row_start, positions, batch, self._hq,
+                                 self._hkv, prep.num_axes, view._dev, _stream(stream))
+        if rc:
+            self._ck(rc)
+
+    def bytekv_qkv_append(self, q, k, v, view, prep, batch, q_out, row_start=None, positions=None, stream=None):
+        """The same into the 8-bit cache."""
+        self._fit(view, batch)
+        assert prep._dev in (None, view._dev), "the weights are on the cache's device"
+        rc = _marshal.bytekv_qkv_append(self._h, C.addressof(view), C.addressof(prep), q, k, v, q_out, row_start, positions, batch,
+                                        self._hq, self._hkv, prep.num_axes, view._dev, _stream(stream))
+        if rc:
+            self._ck(rc)
+
+    def bytekv_read(self, view, out_view, batch, first=None, max_new=0, stream=None):
+        """Positions [first, seq_lens) of the 8-bit cache as bf16 into the cache of out_view."""
+        self._fit(view, batch)
+        self._fit(out_view, batch)
+        rc = _marshal.bytekv_read(self._h, C.addressof(view), C.addressof(out_view), first, max_new, batch, view._dev, _stream(stream))
         if rc:
             self._ck(rc)
 

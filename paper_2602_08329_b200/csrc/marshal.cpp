@@ -128,12 +128,16 @@ struct Entries {
   decltype(&prhs_block_topk) block_topk;
   decltype(&prhs_block_decode_attn) block_decode_attn;
   decltype(&prhs_block_decode_step) block_decode_step;
+  decltype(&prhs_qkv_append) qkv_append;
+  decltype(&prhs_bytekv_qkv_append) bytekv_qkv_append;
+  decltype(&prhs_bytekv_read) bytekv_read;
 } entry{};
-static_assert(sizeof(Entries) == 7 * sizeof(void*), "bind() fills the entries in order");
+constexpr int kEntries = 10;
+static_assert(sizeof(Entries) == kEntries * sizeof(void*), "bind() fills the entries in order");
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  if (!count_is(nargs, 7)) return nullptr;
-  for (int i = 0; i < 7; ++i) {
+  if (!count_is(nargs, kEntries)) return nullptr;
+  for (int i = 0; i < kEntries; ++i) {
     void* p = PyLong_AsVoidPtr(a[i]);
     if (PyErr_Occurred()) return nullptr;
     reinterpret_cast<void**>(&entry)[i] = p;
@@ -331,6 +335,98 @@ PyObject* block_decode_step(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   });
 }
 
+// row_start of packed rows (Python None: one row per sequence); nullptr with *ok false: the error is set
+const int32_t* row_starts(PyObject* o, int64_t batch, int64_t rows, int64_t dev, bool* ok) {
+  *ok = false;
+  const at::Tensor* t = none(o) ? nullptr : tensor(o);
+  REQUIRE(t || none(o), "a tensor is missing");
+  REQUIRE(!t || (is(t, at::kInt, dev) && t->dim() == 1 && t->size(0) >= batch + 1 && t->is_contiguous()), "row_start is int32 [batch + 1] on the cache's device");
+  REQUIRE(t || rows == batch, "without row_start every sequence has one row");
+  *ok = true;
+  return t ? static_cast<const int32_t*>(t->data_ptr()) : nullptr;
+}
+
+// New tokens: q, k, v [rows][heads][128] with any strides over the first two axes, q_out, row_start, positions.
+struct Tokens {
+  prhs_token_rows rows{};
+  void* out = nullptr;
+  PyObject* read(PyObject* const* a, int64_t batch, int64_t hq, int64_t hkv, int64_t axes, int64_t dev) {
+    const at::Tensor* t[4];
+    for (int i = 0; i < 4; ++i) {
+      t[i] = tensor(a[i]);
+      REQUIRE(t[i], "a tensor is missing");
+      REQUIRE(is(t[i], at::kBFloat16, dev) && t[i]->dim() == 3 && t[i]->size(0) == t[0]->size(0) && t[i]->size(1) == (i == 1 || i == 2 ? hkv : hq) &&
+                  t[i]->size(2) == 128 && t[i]->stride(2) == 1, "q, k, v and q_out are bf16 [rows][heads][128] on the cache's device");
+    }
+    const int64_t n = t[0]->size(0);
+    REQUIRE(n <= INT32_MAX, "more than 2^31 rows");
+    REQUIRE(t[3]->is_contiguous(), "q_out is contiguous");
+    bool ok;
+    rows.row_start = row_starts(a[4], batch, n, dev, &ok);
+    if (!ok) return nullptr;
+    const at::Tensor* pos = none(a[5]) ? nullptr : tensor(a[5]);
+    REQUIRE(pos || none(a[5]), "a tensor is missing");
+    if (pos) {
+      const int64_t d = pos->dim();
+      REQUIRE(is(pos, at::kInt, dev) && (d == 1 || d == 2) && pos->size(d - 1) >= n && (pos->size(d - 1) < 2 || pos->stride(d - 1) == 1) &&
+                  (d == 2 ? pos->size(0) : 1) >= axes, "positions are int32 [axes][rows] on the cache's device");
+      rows.positions = static_cast<const int32_t*>(pos->data_ptr());
+      rows.positions_stride = d == 2 && pos->size(0) > 1 ? pos->stride(0) : n;
+    }
+    auto stride = [&](int i, int axis) { return t[i]->size(axis) > 1 ? t[i]->stride(axis) : 0; };     // that of an axis of one element is arbitrary
+    rows.q = t[0]->data_ptr();
+    rows.k = t[1]->data_ptr();
+    rows.v = t[2]->data_ptr();
+    rows.q_stride_row = stride(0, 0);
+    rows.q_stride_head = stride(0, 1);
+    rows.k_stride_row = stride(1, 0);
+    rows.k_stride_head = stride(1, 1);
+    rows.v_stride_row = stride(2, 0);
+    rows.v_stride_head = stride(2, 1);
+    rows.num_rows = (int32_t)n;
+    out = t[3]->data_ptr();
+    return Py_None;
+  }
+};
+
+// qkv_append(ctx, view, prep, q, k, v, q_out, row_start | None, positions | None, batch, heads, kv_heads, axes, device, stream)
+template <typename View, typename F>
+PyObject* append_tokens(PyObject* const* a, Py_ssize_t nargs, F entry_point) {
+  if (!count_is(nargs, 15)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const View* kv = v.pointer<View>(1);
+  const prhs_qk_prep* prep = v.pointer<prhs_qk_prep>(2);
+  const int64_t batch = v.integer(9), hq = v.integer(10), hkv = v.integer(11), axes = v.integer(12), dev = v.integer(13);
+  void* stream = v.pointer<void>(14);
+  if (PyErr_Occurred()) return nullptr;
+  Tokens tokens;
+  if (!tokens.read(a + 3, batch, hq, hkv, axes, dev)) return nullptr;
+  return status([&] { return entry_point(ctx, &tokens.rows, prep, kv, (int32_t)batch, tokens.out, stream); });
+}
+PyObject* qkv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) { return append_tokens<prhs_kv_view>(a, nargs, entry.qkv_append); }
+PyObject* bytekv_qkv_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  return append_tokens<prhs_bytekv_view>(a, nargs, entry.bytekv_qkv_append);
+}
+
+// bytekv_read(ctx, view, out_view, first | None, max_new, batch, device, stream)
+PyObject* bytekv_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 8)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_bytekv_view* kv = v.pointer<prhs_bytekv_view>(1);
+  const prhs_kv_view* out = v.pointer<prhs_kv_view>(2);
+  const int64_t max_new = v.integer(4), batch = v.integer(5), dev = v.integer(6);
+  void* stream = v.pointer<void>(7);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* first = none(a[3]) ? nullptr : tensor(a[3]);
+  REQUIRE(first || none(a[3]), "a tensor is missing");
+  REQUIRE(!first || (is(first, at::kInt, dev) && first->dim() == 1 && first->size(0) >= batch && first->is_contiguous()),
+          "first is int32 [batch] on the cache's device");
+  const int32_t* at = first ? static_cast<const int32_t*>(first->data_ptr()) : nullptr;
+  return status([&] { return entry.bytekv_read(ctx, kv, out, at, (int32_t)max_new, (int32_t)batch, stream); });
+}
+
 // torch's C++ exceptions (a tensor without storage or strides) as Python's: none may leave a C function.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t nargs) noexcept {
@@ -347,7 +443,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t nargs) noexcept
 #define METHOD(name) {#name, (PyCFunction)(void*)guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(kv_view), METHOD(bytekv_view), METHOD(bounds_view), METHOD(bind), METHOD(bytekv_append), METHOD(bytekv_decode_attn),
                          METHOD(bytekv_sparse_decode_attn), METHOD(block_bounds), METHOD(block_topk), METHOD(block_decode_attn),
-                         METHOD(block_decode_step), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(block_decode_step), METHOD(qkv_append), METHOD(bytekv_qkv_append), METHOD(bytekv_read), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

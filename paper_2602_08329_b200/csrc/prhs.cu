@@ -27,6 +27,7 @@
 #include "attn_group_umma.cuh"
 #include "bytekv.cuh"
 #include "block_sparse.cuh"
+#include "tokens.cuh"
 
 using namespace prhs;
 
@@ -577,6 +578,7 @@ prhs_status check_layer(prhs_ctx* c, int layer, int step, const prhs_schedule* s
 // =============================================================================== C ABI
 #include "bytekv_host.cuh"
 #include "block_host.cuh"
+#include "tokens_host.cuh"
 
 extern "C" {
 
