@@ -494,6 +494,34 @@ prhs_status prhs_bytekv_qkv_append(prhs_ctx* ctx, const prhs_token_rows* rows, c
 prhs_status prhs_bytekv_read(prhs_ctx* ctx, const prhs_bytekv_view* kv, const prhs_kv_view* out, const int32_t* first, int32_t max_new,
                              int32_t batch, void* stream);
 
+/* What the new tokens of prhs_chunk_attn see: the token at position u - 1 attends over positions i < u with i < sinks or
+ * i >= max(u - window, P).  window = 0: no window.  P = floor((1 - phi^(alpha (l - l_s) / (N - l_s))) u) for l = layer + 1 >= l_s =
+ * psaw_layer_start, else 0: the sliding window by depth of prhs_schedule (Sec. 4.2, Eq. 11), which the paper's prefill uses as
+ * its decode steps do; psaw_layer_start = 0 switches it off.  N = prhs_config.num_layers. */
+typedef struct {
+  int32_t sinks;              /* >= 0 */
+  int32_t window;             /* >= 0 */
+  int32_t layer;              /* >= 0; read with psaw_layer_start > 0 only */
+  int32_t psaw_layer_start;
+  float psaw_phi;
+  float psaw_alpha;
+} prhs_chunk_mask;
+
+/* Causal attention of many new tokens per sequence (a prompt, a part of one, draft tokens) over everything in the bf16 cache,
+ * their own rows included.  Tokens are packed as in prhs_token_rows: sequence b's are rows row_start[b] .. row_start[b + 1] - 1
+ * and the last positions of its t_b; sequences that do not fit are left out and recorded (PRHS_FLAG_BAD_LENGTH), rows of no
+ * sequence are left as they were.
+ *   q, out     device bf16 [num_rows][Hq][128], 16-byte aligned, apart; num_rows = 0: nothing is done
+ *   out_lse    device fp32 [num_rows][Hq] or NULL: log of the sum of exponentials over what the token sees
+ *   row_start  device [batch + 1], ascending, or NULL: one row per sequence (num_rows = batch)
+ *   mask       NULL: every token sees all positions before it and its own
+ * A token that sees nothing (sinks = 0, P = u), or nothing but logits of -inf, has a zero row and lse = -inf.  A NaN or +inf logit makes the
+ * row and its lse NaN; a value that is infinite or NaN makes its coordinate infinite or NaN for the tokens that see it, and
+ * for no others.  A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE); its rows count as zeros.
+ * PRHS_ERR_UNSUPPORTED where the driver offers no tensor-map encoder. */
+prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_start, int32_t num_rows, const prhs_kv_view* kv,
+                            const prhs_chunk_mask* mask, int32_t batch, void* out, float* out_lse, void* stream);
+
 /* Largest index-list length any call can produce: S0 + k + 2*r*m + W from prhs_config. */
 int32_t prhs_index_capacity(const prhs_ctx* ctx);
 

@@ -42,7 +42,8 @@ EXPORTS = ["prhs_create", "prhs_destroy", "prhs_score_topk", "prhs_build_index_s
            "prhs_profile_end", "prhs_kernel_kind_name", "prhs_sparse_decode_attn_noalloc", "prhs_get_gate",
            "prhs_noalloc_check", "prhs_gather_probe", "prhs_bytekv_append", "prhs_bytekv_decode_attn",
            "prhs_bytekv_sparse_decode_attn", "prhs_block_bounds", "prhs_block_topk", "prhs_block_decode_attn",
-           "prhs_block_decode_step", "prhs_qkv_append", "prhs_bytekv_qkv_append", "prhs_bytekv_read"]
+           "prhs_block_decode_step", "prhs_qkv_append", "prhs_bytekv_qkv_append", "prhs_bytekv_read",
+           "prhs_chunk_attn"]
 NOALLOC_MAX_UNITS = 1024
 KERNEL_KINDS = 6
 
@@ -111,11 +112,16 @@ class QkPrep(C.Structure):
     _dev = None
 
 
+class ChunkMask(C.Structure):
+    _fields_ = [("sinks", C.c_int32), ("window", C.c_int32), ("layer", C.c_int32), ("psaw_layer_start", C.c_int32),
+                ("psaw_phi", C.c_float), ("psaw_alpha", C.c_float)]
+
+
 _lib = None
 _marshal = None
 # the calls the compiled helper makes, in the order it takes their addresses
 _MARSHAL_CALLS = ("bytekv_append", "bytekv_decode_attn", "bytekv_sparse_decode_attn", "block_bounds", "block_topk",
-                  "block_decode_attn", "block_decode_step", "qkv_append", "bytekv_qkv_append", "bytekv_read")
+                  "block_decode_attn", "block_decode_step", "qkv_append", "bytekv_qkv_append", "bytekv_read", "chunk_attn")
 
 
 def _load_marshal():
@@ -169,6 +175,7 @@ def load() -> C.CDLL:
         "prhs_qkv_append": (st, [vp, C.POINTER(TokenRows), C.POINTER(QkPrep), C.POINTER(KvView), i32, vp, vp]),
         "prhs_bytekv_qkv_append": (st, [vp, C.POINTER(TokenRows), C.POINTER(QkPrep), C.POINTER(ByteKvView), i32, vp, vp]),
         "prhs_bytekv_read": (st, [vp, C.POINTER(ByteKvView), C.POINTER(KvView), vp, i32, i32, vp]),
+        "prhs_chunk_attn": (st, [vp, vp, vp, i32, C.POINTER(KvView), C.POINTER(ChunkMask), i32, vp, vp, vp]),
         "prhs_delta": (st, [vp, vp, C.POINTER(KvView), vp, vp, i32, i32, vp, vp]),
         "prhs_index_capacity": (i32, [vp]),
         "prhs_get_index_set": (st, [vp, i32, vp, vp, vp]),
@@ -293,6 +300,12 @@ def make_qk_prep(q_weight=None, k_weight=None, eps=1e-6, norm=None, inv_freq=Non
                (PRHS_PREP_NORM if norm else 0) | (PRHS_PREP_ADJACENT if adjacent else 0), (C.c_uint8 * 64)(*axes))
     p._keep, p._dev = (q_weight, k_weight, inv_freq), dev
     return p
+
+
+def make_chunk_mask(sinks=0, window=0, layer=0, psaw_layer_start=0, psaw_phi=0.7, psaw_alpha=1.0) -> ChunkMask:
+    """Which earlier positions the tokens of chunk_attn see: the first `sinks`, and the last `window` (0: all) of those that layer
+    `layer`'s sliding window leaves (psaw_layer_start = 0: all)."""
+    return ChunkMask(sinks, window, layer, psaw_layer_start, psaw_phi, psaw_alpha)
 
 
 class Context:
@@ -457,6 +470,16 @@ class Context:
         self._fit(view, batch)
         self._fit(out_view, batch)
         rc = _marshal.bytekv_read(self._h, C.addressof(view), C.addressof(out_view), first, max_new, batch, view._dev, _stream(stream))
+        if rc:
+            self._ck(rc)
+
+    # -- attention of many new tokens
+    def chunk_attn(self, q, view, batch, out, out_lse=None, row_start=None, mask=None, stream=None):
+        """Causal attention of packed new tokens (q, out bf16 [rows][Hq][128], out_lse fp32 [rows][Hq]), sequence b's rows
+        row_start[b] .. row_start[b + 1] - 1 being its last positions, over all its positions in the cache (or those of `mask`)."""
+        self._fit(view, batch)
+        rc = _marshal.chunk_attn(self._h, C.addressof(view), 0 if mask is None else C.addressof(mask), q, out, out_lse, row_start, batch,
+                                 self._hq, view._dev, _stream(stream))
         if rc:
             self._ck(rc)
 

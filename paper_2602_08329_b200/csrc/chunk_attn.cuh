@@ -1,0 +1,856 @@
+// Attention of many new tokens per sequence (a prompt, a part of one, draft tokens) over everything cached, on the
+// fifth-generation tensor cores.
+//
+// A token at position u - 1 sees positions i < u that are among the first `sinks` or not before
+// P(u) = max(0, u - window, floor(c u)).  Its G heads of a KV head are G rows; T = 128 / G tokens (rounded down) fill the 128 rows of an
+// MMA.  A CTA works on an item, 2 T tokens of a sequence and one KV head, as two subtiles of T tokens with an
+// accumulator each, over tiles of 128 keys:
+//   producer warp   Q once per piece, then K and V tiles by TMA (128-byte swizzle) into a ring of five 32 KB slots
+//   MMA warp        one thread: S_s = Q_s K^T (128 x 128, fp32 in tensor memory), O_s += P_s V, P read from tensor memory
+//   8 softmax warps a thread owns a row: reads it (tcgen05.ld), weights 2^(x - m) in bf16 back over S (tcgen05.st), its sum in
+//                   fp32.  The two subtiles take turns: while the tensor core multiplies for one, the other's
+//                   weights are made
+//   2 mending warps tiles that some row sees in part only: V rows behind the sequence become zero, and so do values that are not
+//                   finite (noted, and added at the end for the rows that do see them): a weight of zero times an infinity in
+//                   a masked place would be NaN
+// The reference exponent m of a row moves only when a logit exceeds it by 2^8 (a vote per warp); O is then rescaled in tensor memory by
+// the softmax warps themselves: S of the next tile is issued behind the product of the previous one, so O is at rest.
+// An item of at most T tokens (drafts, short chunks) lets its two accumulators take the even and the odd tiles instead
+// (`halves`), and the stream of the cache is what bounds it.
+//
+// Work is dealt evenly whatever the lengths: the tiles of all items, laid end to end (sequence, KV head, tokens), are cut into as
+// many runs of equal length as there are CTAs (one per SM).  A piece of an item goes to a workspace as (m, l, O) in fp32; the
+// last CTA to arrive merges them (a ticket, no waiting).  A CTA has two pieces of that kind at most.
+//
+// Weights enter the product as bf16, one rounding of 2^-8: as two bf16 (what the decode kernels do, bound by the stream) they would cost
+// half as many MMAs again, which is what bounds this kernel.  Sums, references, O and what is merged are fp32.
+#pragma once
+#include <cuda.h>
+
+#include "attn_group_umma.cuh"
+#include "common.cuh"
+#include "score_umma.cuh"
+#include "tokens.cuh"
+
+namespace prhs {
+
+constexpr int kCATile = 128;                              // keys per tile, rows per subtile
+constexpr int kCAHalfBytes = kCATile * 128;               // [128 rows][64 columns] bf16
+constexpr int kCATileBytes = 2 * kCAHalfBytes;            // 32 KB
+constexpr int kCASlots = 5;
+constexpr int kCASmemBytes = (2 + kCASlots) * kCATileBytes + 1024;
+constexpr int kCAThreads = 12 * 32;
+constexpr int kCAMmaWarp = 8, kCALoadWarp = 9, kCAMendWarp = 10;
+constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // a piece in the workspace: O [2][32][128] float4, (m, l) [2][128]
+constexpr uint32_t kCAIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCATile >> 3) << 17) | ((uint32_t)(kCATile >> 4) << 24);
+constexpr uint32_t kCAIdescPV = kCAIdesc | (1u << 16);    // B = V tile read MN-major
+constexpr float kCAGap = 8.f;
+// An item's Q, merge and output cost about as much as two tiles; a run of fewer than kCAMinRun tiles is not worth its merge.
+constexpr int kCAItemCost = 2;
+constexpr int kCAMinRun = 4;
+constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
+
+struct ChunkParams {
+  KvDev kv;
+  const int* row_start;
+  __nv_bfloat16* out;
+  float* out_lse;
+  float* partials;               // [2 gridDim.x][kCASlotFloats]
+  unsigned int* tickets;         // [gridDim.x], zero between launches
+  uint32_t* flags;
+  double psaw_c;
+  int num_rows, batch, num_q_heads, num_kv_heads, group, tokens;     // tokens = T
+  int sinks, window, max_len;
+  unsigned int oob_row;          // a row outside the K and V tensors: zeros
+};
+
+// ---------------------------------------------------------------------------------------- the work
+__device__ __forceinline__ int first_visible(const ChunkParams& p, int u) {
+  int lo = p.psaw_c > 0.0 ? psaw_start(p.psaw_c, u) : 0;
+  if (p.window > 0) lo = max(lo, u - p.window);
+  return lo;
+}
+// A piece of an item: tiles k0 .. k1 - 1 of those its tokens see.
+struct Piece {
+  int b, kvh, row0, ntok, u0;    // u0: visible length of the first token
+  int k0, k1, st, lo;            // tile k is k for k < st, else lo + k - st
+  int first_cta, last_cta;       // CTAs that have pieces of the item
+  int t;
+  bool halves;
+  // per subtile: tokens [a, e), visible lengths of the first and last, where their windows begin
+  int a[2], e[2], uf[2], ul[2], pf[2], pl[2];
+  __device__ __forceinline__ int tile(int k) const { return k < st ? k : lo + k - st; }
+  __device__ __forceinline__ bool active(const ChunkParams& p, int s, int k) const {
+    if (halves) return ((k - k0) & 1) == s;
+    const int at = tile(k) * kCATile;
+    return e[s] > a[s] && at < ul[s] && (at < p.sinks || at + kCATile > pf[s]);
+  }
+  // some row of the subtile does not see all of the tile
+  __device__ __forceinline__ bool partly(const ChunkParams& p, int s, int k) const {
+    const int at = tile(k) * kCATile;
+    return !(at + kCATile <= uf[s] && (at + kCATile <= p.sinks || at >= pl[s]));
+  }
+  __device__ __forceinline__ bool mended(const ChunkParams& p, int k) const {
+    return (active(p, 0, k) && partly(p, 0, k)) || (active(p, 1, k) && partly(p, 1, k));
+  }
+};
+// Walks this CTA's run.  Every warp does so for itself; all lanes hold the same values.
+struct ChunkWalk {
+  const ChunkParams& p;
+  long long at = 0, end = 0, total = 0, item_at = 0;
+  int ctas = 0, b = 0, kvh = 0, i = 0, items = 0;
+  SeqRows s;
+
+  __device__ __forceinline__ explicit ChunkWalk(const ChunkParams& params) : p(params) {}
+  // tiles that item i's tokens see, as (st, lo, hi)
+  __device__ __forceinline__ void range(const SeqRows& q, int item, int* st, int* lo, int* hi) const {
+    const int a = item * 2 * p.tokens, e = min(q.n, a + 2 * p.tokens);
+    const int uf = q.t - q.n + a + 1, ul = q.t - q.n + e;
+    *hi = (ul + kCATile - 1) / kCATile;
+    *lo = first_visible(p, uf) / kCATile;
+    *st = min((min(p.sinks, ul) + kCATile - 1) / kCATile, *lo);
+  }
+  __device__ __forceinline__ int cost(const SeqRows& q, int item) const {
+    int st, lo, hi;
+    range(q, item, &st, &lo, &hi);
+    return st + hi - lo + kCAItemCost;
+  }
+  __device__ __forceinline__ int items_of(const SeqRows& q) const { return (q.n + 2 * p.tokens - 1) / (2 * p.tokens); }
+  __device__ __forceinline__ SeqRows seq(int at_b) const { return seq_rows(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, at_b); }
+  // Warp-collective: cost of all items of sequence b0 + lane (one KV head)
+  __device__ __forceinline__ long long costs(int b0) const {
+    const int lane = threadIdx.x & 31;
+    SeqRows q;
+    q.n = 0;
+    q.t = 0;
+    if (b0 + lane < p.batch) q = seq(b0 + lane);
+    const int m = items_of(q);
+    long long sum = 0;
+    if (m <= 2)
+      for (int x = 0; x < m; ++x) sum += cost(q, x);
+    uint32_t many = __ballot_sync(0xffffffffu, m > 2);
+    while (many) {
+      const int src = __ffs(many) - 1;
+      many &= many - 1;
+      SeqRows r;
+      r.n = __shfl_sync(0xffffffffu, q.n, src);
+      r.t = __shfl_sync(0xffffffffu, q.t, src);
+      const int mm = items_of(r);
+      long long part = 0;
+      for (int x = lane; x < mm; x += 32) part += cost(r, x);
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) part += __shfl_xor_sync(0xffffffffu, part, off);
+      if (lane == src) sum = part;
+    }
+    return sum;
+  }
+  // The CTA whose run holds place x.
+  __device__ __forceinline__ int cta_of(long long x) const { return (int)(((x + 1) * ctas - 1) / total); }
+
+  // false: nothing for this CTA
+  __device__ __forceinline__ bool begin() {
+    const int lane = threadIdx.x & 31;
+    long long mine0 = 0;          // of sequence `lane`
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+      long long w = costs(b0);
+      if (b0 == 0) mine0 = w;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) w += __shfl_xor_sync(0xffffffffu, w, off);
+      total += w;
+    }
+    total *= p.num_kv_heads;
+    ctas = (int)min((long long)gridDim.x, max(1ll, total / kCAMinRun));
+    if (total == 0 || (int)blockIdx.x >= ctas) return false;
+    at = total * blockIdx.x / ctas;
+    end = total * (blockIdx.x + 1) / ctas;
+    // the sequence
+    long long before = 0, one = 0;
+    for (int b0 = 0;; b0 += 32) {
+      const long long w = b0 == 0 ? mine0 : costs(b0);
+      long long incl = w * p.num_kv_heads;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += v;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, before + incl > at);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        b = b0 + l;
+        one = __shfl_sync(0xffffffffu, w, l);
+        before += __shfl_sync(0xffffffffu, incl, l) - one * p.num_kv_heads;
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    s = seq(b);
+    items = items_of(s);
+    kvh = (int)((at - before) / one);
+    before += one * kvh;
+    // the item
+    for (int x0 = 0;; x0 += 32) {
+      const int w = x0 + lane < items ? cost(s, x0 + lane) : 0;
+      int incl = w;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += v;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, before + incl > at);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        i = x0 + l;
+        item_at = before + __shfl_sync(0xffffffffu, incl - w, l);
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return true;
+  }
+  __device__ __forceinline__ bool next(Piece& x) {
+    if (at >= end) return false;
+    if (i == items) {
+      i = 0;
+      if (++kvh == p.num_kv_heads) {
+        kvh = 0;
+        do s = seq(++b);
+        while (s.n == 0);
+        items = items_of(s);
+      }
+    }
+    int hi;
+    range(s, i, &x.st, &x.lo, &hi);
+    const int w = x.st + hi - x.lo + kCAItemCost;
+    const long long to = min(item_at + w, end);
+    x.k0 = max((int)(at - item_at) - kCAItemCost, 0);
+    x.k1 = max((int)(to - item_at) - kCAItemCost, 0);
+    x.first_cta = cta_of(item_at);
+    x.last_cta = cta_of(item_at + w - 1);
+    x.b = b;
+    x.kvh = kvh;
+    x.row0 = s.r0 + i * 2 * p.tokens;
+    x.ntok = min(s.n - i * 2 * p.tokens, 2 * p.tokens);
+    x.u0 = s.t - s.n + i * 2 * p.tokens + 1;
+    x.t = s.t;
+    x.halves = x.ntok <= p.tokens;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      x.a[y] = x.halves ? 0 : y * p.tokens;
+      x.e[y] = x.halves ? x.ntok : min(x.ntok, (y + 1) * p.tokens);
+      x.uf[y] = x.u0 + x.a[y];
+      x.ul[y] = x.u0 + x.e[y] - 1;
+      x.pf[y] = first_visible(p, x.uf[y]);
+      x.pl[y] = first_visible(p, x.ul[y]);
+    }
+    at = to;
+    if (to == item_at + w) {
+      item_at = to;
+      ++i;
+    }
+    return true;
+  }
+};
+
+// ------------------------------------------------------------------------------------ instructions
+__device__ __forceinline__ void tma_load_2d_plain(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_plain(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
+// A operand in tensor memory
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr));
+}
+// the registers are operands of the wait so that no use of them can be scheduled before it
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+      "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// Ring position: slot and the parity of its fill.
+struct RingPos {
+  int slot = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void step() {
+    if (++slot == kCASlots) {
+      slot = 0;
+      parity ^= 1;
+    }
+  }
+};
+
+// The order in which K and V tiles go through the ring: V follows its K by one step (two where the accumulators take turns with the
+// tiles, so that both have a tile under way).
+#define PRHS_CHUNK_STEPS(x, k) for (int k = (x).k0, lag_ = (x).halves ? 2 : 1, stop_ = (x).k1 > (x).k0 ? (x).k1 + lag_ : (x).k0; k < stop_; ++k)
+
+// grid: one CTA per SM.  tm_q: q as [rows][Hq][128], box [T][G][64]; tm_k, tm_v: [rows][128], box [128][64], or [16][64] per page.
+template <bool kPaged>
+__global__ void __launch_bounds__(kCAThreads, 1)
+chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                  const __grid_constant__ ChunkParams p) {
+  extern __shared__ unsigned char ca_smem_raw[];
+  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_empty[2], drain
+  __shared__ __align__(8) unsigned long long bars[3 * kCASlots + 11];
+  __shared__ int mended_n[4], mended_tile[4][kCAMaxMended];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int sh_abort, sh_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x == 0) record_bad_sequences(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, p.batch, p.flags);
+  ChunkWalk walk(p);
+  if (!walk.begin()) return;
+  const uint32_t smem0 = ((uint32_t)__cvta_generic_to_shared(ca_smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = smem0 + 2 * kCATileBytes;
+  const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
+  const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
+  const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
+  const uint32_t bar_ofull = bar_qfull + 48, bar_oempty = bar_qfull + 64, bar_drain = bar_qfull + 80;
+  if (tid == 0) {
+    for (int i = 0; i < kCASlots; ++i) {
+      mbar_init(bar_full + 8 * i, 1);      // the producer's expect_tx arrive
+      mbar_init(bar_empty + 8 * i, 3);     // a commit of the MMA thread, the two mending warps (which follow the ring fill by fill)
+      mbar_init(bar_vready + 8 * i, 2);    // the mending warps
+    }
+    mbar_init(bar_qfull, 1);
+    mbar_init(bar_qempty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_sfull + 8 * i, 1);     // a commit of the MMA thread
+      mbar_init(bar_pfull + 8 * i, 4);     // the subtile's softmax warps
+      mbar_init(bar_ofull + 8 * i, 1);     // a commit of the MMA thread
+      mbar_init(bar_oempty + 8 * i, 4);    // the subtile's softmax warps
+    }
+    mbar_init(bar_drain, 1);
+    sh_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kCAMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem0 = *(volatile uint32_t*)&tmem_slot;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
+  Piece x;
+  auto gave_up = [&] {
+    atomicOr(p.flags, kFlagTimeout);
+    sh_abort = 1;
+  };
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    // -------------------------------------------------------------------------- softmax: a thread is a row
+    const int s = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t tm_s = tmem0 + s * kCATile + lanes, tm_o = tmem0 + (2 + s) * kCATile + lanes;
+    const int token = row / p.group, head = row - token * p.group;
+    const float c1 = kScale * kLog2e;
+    uint32_t s_par = 0, o_par = 0;
+    int buf = 0;                                     // of the mending warps' notes
+    bool aborted = false;                            // a warp that gave up goes on without touching anything: barriers stay balanced
+    while (walk.next(x)) {
+      const bool used = row < p.tokens * p.group && token < x.e[s] - x.a[s];
+      const bool warp_used = __any_sync(0xffffffffu, used);
+      const int u = used ? x.uf[s] + token : 0;
+      const int from = used ? first_visible(p, u) : 0;
+      float m = -INFINITY;
+      uint64_t l2 = 0ull;                            // two partial sums
+      bool any = false;                              // O holds something
+      for (int k = x.k0; k < x.k1; ++k) {
+        if (!x.active(p, s, k)) continue;
+        if (!aborted) {
+          aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh_abort));
+          if (aborted && lane == 0) gave_up();
+        }
+        s_par ^= 1;
+        if (aborted) continue;
+        if (warp_used) {
+          tc_fence_after();
+          uint32_t r[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(tm_s + 32 * c, r[c]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
+          if (x.partly(p, s, k)) {
+            const int at = x.tile(k) * kCATile, cu = u - at, cs = p.sinks - at, cf = from - at;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (!(c < cu && (c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
+          }
+          float mx0 = __uint_as_float(r[0][0]), mx1 = __uint_as_float(r[0][1]);
+#pragma unroll
+          for (int c = 2; c < 128; c += 4) {
+            mx0 = fmaxf(mx0, fmaxf(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[(c + 1) >> 5][(c + 1) & 31])));
+            if (c + 2 < 128) mx1 = fmaxf(mx1, fmaxf(__uint_as_float(r[(c + 2) >> 5][(c + 2) & 31]), __uint_as_float(r[(c + 3) >> 5][(c + 3) & 31])));
+          }
+          const float mx = fmaxf(mx0, mx1) * c1;
+          if (__any_sync(0xffffffffu, mx > m + kCAGap)) {
+            const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
+            l2 = fma_f32x2(l2, pack_f32x2(f, f), 0ull);
+            m = mn;
+            if (any) {
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                float o[16];
+                tmem_ld16(tm_o + 16 * c, o);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] *= f;
+                tmem_st16(tm_o + 16 * c, o);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          const uint64_t cc = pack_f32x2(c1, c1), mm = pack_f32x2(-ref, -ref);
+          uint64_t la = 0ull, lb = 0ull;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const int c = 64 * h + 2 * j;
+              float a, b;
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
+              else lb = add_f32x2(lb, pack_f32x2(a, b));
+              w[j] = pack_bf16x2(a, b);
+            }
+            tmem_st32(tm_s + 32 * h, w);
+          }
+          l2 = add_f32x2(l2, add_f32x2(la, lb));
+          tmem_wait_st();
+          tc_fence_before();
+        }
+        any = true;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_pfull + 8 * s);
+      }
+      float la, lb;
+      unpack_f32x2(l2, la, lb);
+      const float l = la + lb;
+      // ------------------------------------------------------------ the piece's result
+      if (any && !aborted) {
+        aborted = !__all_sync(0xffffffffu, mbar_wait(bar_ofull + 8 * s, o_par, &sh_abort));
+        if (aborted && lane == 0) gave_up();
+      }
+      if (any) o_par ^= 1;
+      const bool whole = x.first_cta == x.last_cta && !x.halves;
+      const int slot = 2 * blockIdx.x + (x.first_cta == (int)blockIdx.x ? 1 : 0);
+      float* const part = p.partials + (size_t)slot * kCASlotFloats;
+      const long long out_row = ((long long)(x.row0 + x.a[s] + token) * p.num_q_heads + x.kvh * p.group + head);
+      const int mended = any ? mended_n[buf & 3] : 0;
+      if (!aborted && warp_used) {
+        tc_fence_after();
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        // (a loop, not unrolled: it is outside the tiles)
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          uint32_t r[32];
+          if (any) {
+            tmem_ld32(tm_o + 32 * c, r);
+            tmem_wait_ld(r);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = 0u;
+          }
+          // values that are not finite and were kept out of the product: infinite or NaN whatever their weight
+          for (int y = 0; y < mended; ++y) {
+            const int at = mended_tile[buf & 3][y] * kCATile;
+            for (int i = at; i < min(at + kCATile, u); ++i) {
+              if (i >= p.sinks && i < from) continue;
+              long long off = (long long)x.b * p.kv.stride_outer + (long long)i * kHeadDim;
+              if (kPaged) {
+                const int page = __ldg(p.kv.page_table + (long long)x.b * p.kv.page_table_stride + (i >> kPageShift));
+                if ((unsigned)page >= (unsigned)p.kv.num_pages) continue;
+                off = (long long)page * p.kv.stride_outer + (i & 15) * kHeadDim;
+              }
+              const __nv_bfloat16* v = p.kv.v + off + (long long)x.kvh * p.kv.stride_head + 32 * c;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const float f = __bfloat162float(v[j]);
+                if (!isfinite(f)) r[j] = __float_as_uint(__uint_as_float(r[j]) + f);
+              }
+            }
+          }
+          if (!used) continue;
+          if (whole) {
+            uint4* to = reinterpret_cast<uint4*>(p.out + out_row * kHeadDim + 32 * c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              to[j] = make_uint4(pack_bf16x2(__uint_as_float(r[8 * j]) * inv, __uint_as_float(r[8 * j + 1]) * inv),
+                                 pack_bf16x2(__uint_as_float(r[8 * j + 2]) * inv, __uint_as_float(r[8 * j + 3]) * inv),
+                                 pack_bf16x2(__uint_as_float(r[8 * j + 4]) * inv, __uint_as_float(r[8 * j + 5]) * inv),
+                                 pack_bf16x2(__uint_as_float(r[8 * j + 6]) * inv, __uint_as_float(r[8 * j + 7]) * inv));
+          } else if (any) {
+            float4* to = reinterpret_cast<float4*>(part) + (s * 32 + 8 * c) * kCATile + row;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              __stcg(to + j * kCATile, make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]),
+                                                   __uint_as_float(r[4 * j + 3])));
+          }
+        }
+        if (used) {
+          if (whole) {
+            if (p.out_lse) p.out_lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+          } else {
+            __stcg(reinterpret_cast<float2*>(part + 2 * kCATile * kHeadDim) + s * kCATile + row, make_float2(m, l));
+          }
+        }
+        tc_fence_before();
+      }
+      if (any) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_oempty + 8 * s);
+      }
+      if (x.k1 > x.k0) ++buf;
+      if (!whole) {
+        // ---------------------------------------------------------- the last piece of an item to arrive merges them
+        __threadfence();
+        softmax_bar();
+        const int parts = x.last_cta - x.first_cta + 1;
+        if (tid == 0) {
+          bool last = true;
+          if (parts > 1) {
+            last = atomicAdd(p.tickets + x.first_cta, 1u) == (unsigned)parts - 1u;
+            if (last) p.tickets[x.first_cta] = 0u;
+          }
+          sh_last = last;
+        }
+        softmax_bar();
+        if (sh_last && !*(volatile int*)&sh_abort && used) {
+          __threadfence();
+          // this thread's row: its subtile's pieces, 128 columns; with `halves` those of both, and half of the columns
+          const int sub0 = x.halves ? 0 : s, sub1 = x.halves ? 1 : s, cols = x.halves ? 64 : 128;
+          auto base = [&](int c) { return p.partials + (size_t)(2 * c + (c == x.first_cta ? 1 : 0)) * kCASlotFloats; };
+          auto ml = [&](int c, int y) { return __ldcg(reinterpret_cast<const float2*>(base(c) + 2 * kCATile * kHeadDim) + y * kCATile + row); };
+          float M = -INFINITY, L = 0.f;
+          for (int c = x.first_cta; c <= x.last_cta; ++c)
+            for (int y = sub0; y <= sub1; ++y) M = fmaxf(M, ml(c, y).x);
+          for (int c = x.first_cta; c <= x.last_cta; ++c)
+            for (int y = sub0; y <= sub1; ++y) {
+              const float2 v = ml(c, y);
+              if (v.y != 0.f) L += v.y * exp2f(v.x - M);
+            }
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          const int c_begin = x.halves ? 64 * s : 0;
+#pragma unroll 1
+          for (int c0 = c_begin; c0 < c_begin + cols; c0 += 32) {
+            float acc[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[j] = 0.f;
+            for (int c = x.first_cta; c <= x.last_cta; ++c)
+              for (int y = sub0; y <= sub1; ++y) {
+                const float2 v = ml(c, y);
+                if (v.y == 0.f) continue;
+                const float f = exp2f(v.x - M);
+                const float4* o = reinterpret_cast<const float4*>(base(c)) + (y * 32 + c0 / 4) * kCATile + row;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const float4 w = __ldcg(o + j * kCATile);
+                  acc[4 * j] = fmaf(w.x, f, acc[4 * j]);
+                  acc[4 * j + 1] = fmaf(w.y, f, acc[4 * j + 1]);
+                  acc[4 * j + 2] = fmaf(w.z, f, acc[4 * j + 2]);
+                  acc[4 * j + 3] = fmaf(w.w, f, acc[4 * j + 3]);
+                }
+              }
+            uint4* to = reinterpret_cast<uint4*>(p.out + out_row * kHeadDim + c0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              to[j] = make_uint4(pack_bf16x2(acc[8 * j] * inv, acc[8 * j + 1] * inv), pack_bf16x2(acc[8 * j + 2] * inv, acc[8 * j + 3] * inv),
+                                 pack_bf16x2(acc[8 * j + 4] * inv, acc[8 * j + 5] * inv), pack_bf16x2(acc[8 * j + 6] * inv, acc[8 * j + 7] * inv));
+          }
+          if (p.out_lse && (!x.halves || s == 0)) p.out_lse[out_row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+        }
+        softmax_bar();                   // the slot may be written again
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == kCALoadWarp) {
+      // ------------------------------------------------------------------------ producer
+      const int outer_rows = (int)(p.kv.stride_outer >> 7), head_rows = (int)(p.kv.stride_head >> 7);
+      const uint32_t q_bytes = 2u * 128u * (uint32_t)(p.group * p.tokens);
+      RingPos pos;
+      uint32_t q_par = 0;
+      bool ring_full = false, q_full = false;        // whether slots (Q) have been filled before
+      int fills = 0;
+      bool ok = true;
+      while (ok && walk.next(x)) {
+        if (x.k0 == x.k1) continue;
+        if (lane == 0) {
+          if (q_full) {
+            ok = mbar_wait(bar_qempty, q_par, &sh_abort);
+            q_par ^= 1;
+          }
+          if (ok) {
+            mbar_expect_tx(bar_qfull, x.halves ? q_bytes : 2 * q_bytes);
+            for (int y = 0; y < (x.halves ? 1 : 2); ++y)
+              for (int h = 0; h < 2; ++h)
+                tma_load_3d_plain(smem0 + y * kCATileBytes + h * kCAHalfBytes, &tm_q, 64 * h, x.kvh * p.group, x.row0 + y * p.tokens, bar_qfull);
+          }
+        }
+        q_full = true;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        // pages: lanes 0 - 15 hold the row of page (lane / 2) mod 8 of the latest three tiles
+        const int page_at = (lane >> 1) & 7, half = lane & 1;
+        const int* table = kPaged ? p.kv.page_table + (long long)x.b * p.kv.page_table_stride : nullptr;
+        auto lookup = [&](int k) -> uint32_t {
+          if (!kPaged || k >= x.k1) return p.oob_row;
+          const int pg = x.tile(k) * (kCATile / kBlockRows) + page_at;
+          if (pg * kBlockRows >= x.t) return p.oob_row;
+          const int id = __ldg(table + pg);
+          if ((unsigned)id >= (unsigned)p.kv.num_pages) {
+            if (lane < 16) atomicOr(p.flags, kFlagBadPage);
+            return p.oob_row;
+          }
+          return (uint32_t)(id * outer_rows + x.kvh * head_rows);
+        };
+        uint32_t next_row = lookup(x.k0), rows[2] = {p.oob_row, p.oob_row};
+        auto fill = [&](const CUtensorMap* tm, int k, uint32_t page_row) {
+          if (lane == 0) {
+            if (ring_full) ok = mbar_wait(bar_empty + 8 * pos.slot, pos.parity ^ 1, &sh_abort);
+            if (ok) mbar_expect_tx(bar_full + 8 * pos.slot, kCATileBytes);
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) return;
+          const uint32_t dst = ring + pos.slot * kCATileBytes, bar = bar_full + 8 * pos.slot;
+          if (kPaged) {
+            if (lane < 16) tma_load_2d_plain(dst + half * kCAHalfBytes + page_at * 2048, tm, 64 * half, (int)page_row, bar);
+          } else if (lane == 0) {
+            const int r = x.b * outer_rows + x.kvh * head_rows + x.tile(k) * kCATile;
+            tma_load_2d_plain(dst, tm, 0, r, bar);
+            tma_load_2d_plain(dst + kCAHalfBytes, tm, 64, r, bar);
+          }
+          pos.step();
+          if (++fills == kCASlots) ring_full = true;
+        };
+        PRHS_CHUNK_STEPS(x, k) {
+          if (ok && k - lag_ >= x.k0) fill(&tm_v, k - lag_, rows[lag_ - 1]);
+          if (ok && k < x.k1) {
+            rows[1] = rows[0];
+            rows[0] = next_row;
+            next_row = lookup(k + 1);
+            fill(&tm_k, k, rows[0]);
+          } else {
+            rows[1] = rows[0];
+          }
+        }
+      }
+      if (!ok && lane == 0) gave_up();
+    } else if (warp == kCAMmaWarp) {
+      // ------------------------------------------------------------------------ MMA issue: one thread
+      if (lane == 0) {
+        RingPos pos;
+        uint32_t q_par = 0, vr_par = 0, p_par[2] = {0, 0}, oe_par[2] = {1, 1};
+        bool ok = true;
+        while (ok && walk.next(x)) {
+          if (x.k0 == x.k1) continue;
+          ok = mbar_wait(bar_qfull, q_par, &sh_abort);
+          q_par ^= 1;
+          bool started[2] = {false, false};
+          PRHS_CHUNK_STEPS(x, k) {
+            const int prev = k - lag_;
+            const bool pv = prev >= x.k0, qk = k < x.k1;
+            RingPos vpos = pos;
+            if (pv) {
+              pos.step();
+              if (ok) ok = mbar_wait(bar_full + 8 * vpos.slot, vpos.parity, &sh_abort);
+              if (ok && x.mended(p, prev)) {
+                ok = mbar_wait(bar_vready + 8 * vpos.slot, (vr_par >> vpos.slot) & 1u, &sh_abort);
+                vr_par ^= 1u << vpos.slot;
+              }
+            }
+            const RingPos kpos = pos;
+            if (qk) pos.step();
+            bool k_here = false;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              if (ok && pv && x.active(p, s, prev)) {
+                ok = mbar_wait(bar_pfull + 8 * s, p_par[s], &sh_abort);
+                p_par[s] ^= 1;
+                if (ok && !started[s]) {
+                  ok = mbar_wait(bar_oempty + 8 * s, oe_par[s], &sh_abort);
+                  oe_par[s] ^= 1;
+                }
+                if (ok) {
+                  tc_fence_after();
+                  const uint64_t vd = umma_desc_mn(ring + vpos.slot * kCATileBytes);
+#pragma unroll
+                  for (int ks = 0; ks < 8; ++ks)
+                    umma_bf16_ts(tmem0 + (2 + s) * kCATile, tmem0 + s * kCATile + 8 * ks, vd + (uint64_t)(ks * ((16 * 128) >> 4)), kCAIdescPV,
+                                 started[s] || ks > 0 ? 1u : 0u);
+                }
+                started[s] = true;
+              }
+              if (ok && pv && s == 1) umma_commit(bar_empty + 8 * vpos.slot);
+              if (ok && qk && x.active(p, s, k)) {
+                if (!k_here) ok = mbar_wait(bar_full + 8 * kpos.slot, kpos.parity, &sh_abort);
+                k_here = true;
+                if (ok) {
+                  tc_fence_after();
+                  const uint64_t qd = umma_desc(smem0 + (x.halves ? 0 : s) * kCATileBytes), kd = umma_desc(ring + kpos.slot * kCATileBytes);
+#pragma unroll
+                  for (int ks = 0; ks < 8; ++ks) {
+                    const uint64_t off = (uint64_t)((ks >> 2) * (kCAHalfBytes >> 4) + (ks & 3) * 2);
+                    umma_bf16(tmem0 + s * kCATile, qd + off, kd + off, kCAIdesc, ks > 0 ? 1u : 0u);
+                  }
+                  umma_commit(bar_sfull + 8 * s);
+                }
+              }
+            }
+            if (ok && qk) umma_commit(bar_empty + 8 * kpos.slot);
+            if (ok && k == x.k1 - 1) umma_commit(bar_qempty);
+            if (!ok) break;
+          }
+          if (ok) {
+            if (started[0]) umma_commit(bar_ofull);
+            if (started[1]) umma_commit(bar_ofull + 8);
+          }
+        }
+        if (!ok) gave_up();
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------------------ mending warps
+      const int t64 = tid - 32 * kCAMendWarp;
+      RingPos pos;
+      int buf = 0;
+      bool ok = true;
+      while (walk.next(x)) {         // (a warp that gave up goes on through the barriers of the other)
+        if (x.k0 == x.k1) continue;
+        if (t64 == 0) mended_n[buf & 3] = 0;
+        asm volatile("bar.sync 2, 64;" ::: "memory");
+        PRHS_CHUNK_STEPS(x, k) {
+          const int prev = k - lag_;
+          if (prev >= x.k0) {
+            const bool mend = x.mended(p, prev);
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh_abort));
+            if (mend) {
+              const int at = x.tile(prev) * kCATile;
+              bool odd = false;
+              if (ok) {
+                const uint32_t base = ring + pos.slot * kCATileBytes;
+                for (int i = t64; i < kCATile * 16; i += 64) {
+                  const int r = (i >> 3) & 127;
+                  const uint32_t addr = base + (uint32_t)i * 16u;
+                  uint32_t w[4];
+                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+                  const bool gone = at + r >= x.t;
+                  bool change = gone;
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                    const uint32_t bad = gone ? 0xffffffffu : __vcmpgeu2(w[j] & 0x7fff7fffu, 0x7f807f80u);
+                    change |= bad != 0u;
+                    odd |= !gone && bad != 0u;
+                    w[j] &= ~bad;
+                  }
+                  if (change)
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              }
+              uint32_t any_odd;
+              asm volatile("{ .reg .pred a, b; setp.ne.u32 a, %1, 0; barrier.cta.red.or.pred b, 2, 64, a; selp.u32 %0, 1, 0, b; }"
+                           : "=r"(any_odd) : "r"((uint32_t)odd) : "memory");
+              if (any_odd && t64 == 0) {
+                const int n = mended_n[buf & 3];
+                if (n < kCAMaxMended) {
+                  mended_tile[buf & 3][n] = x.tile(prev);
+                  mended_n[buf & 3] = n + 1;
+                }
+              }
+              __syncwarp();
+              if (ok && lane == 0) mbar_arrive(bar_vready + 8 * pos.slot);
+            }
+            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
+            pos.step();
+          }
+          if (k < x.k1) {
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh_abort));
+            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
+            pos.step();
+          }
+        }
+        ++buf;
+      }
+      if (!ok && lane == 0) gave_up();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (sh_abort) {
+    // copies and MMAs may still be in flight: bounded waits before shared and tensor memory go back
+    if (tid == kCALoadWarp * 32) {
+      for (int i = 0; i < kCASlots; ++i) {
+        const long long t0 = clock64();
+        while (!mbar_try_wait(bar_full + 8 * i, 0) && !mbar_try_wait(bar_full + 8 * i, 1))
+          if (clock64() - t0 > kWaitBudgetCycles / 8) break;
+      }
+    }
+    if (tid == kCAMmaWarp * 32) {
+      umma_commit(bar_drain);
+      const long long t0 = clock64();
+      while (!mbar_try_wait(bar_drain, 0))
+        if (clock64() - t0 > kWaitBudgetCycles / 8) break;
+    }
+    __syncthreads();
+  }
+  if (warp == kCAMmaWarp) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem0), "r"(512u) : "memory");
+  }
+}
+
+}  // namespace prhs

@@ -131,8 +131,9 @@ struct Entries {
   decltype(&prhs_qkv_append) qkv_append;
   decltype(&prhs_bytekv_qkv_append) bytekv_qkv_append;
   decltype(&prhs_bytekv_read) bytekv_read;
+  decltype(&prhs_chunk_attn) chunk_attn;
 } entry{};
-constexpr int kEntries = 10;
+constexpr int kEntries = 11;
 static_assert(sizeof(Entries) == kEntries * sizeof(void*), "bind() fills the entries in order");
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
@@ -427,6 +428,28 @@ PyObject* bytekv_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   return status([&] { return entry.bytekv_read(ctx, kv, out, at, (int32_t)max_new, (int32_t)batch, stream); });
 }
 
+// chunk_attn(ctx, view, mask (0: none), q, out, out_lse | None, row_start | None, batch, heads, device, stream)
+PyObject* chunk_attn(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  if (!count_is(nargs, 11)) return nullptr;
+  const Args v{a};
+  prhs_ctx* ctx = v.pointer<prhs_ctx>(0);
+  const prhs_kv_view* kv = v.pointer<prhs_kv_view>(1);
+  const prhs_chunk_mask* mask = v.pointer<prhs_chunk_mask>(2);
+  const int64_t batch = v.integer(7), heads = v.integer(8), dev = v.integer(9);
+  void* stream = v.pointer<void>(10);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* q = tensor(a[3]);
+  REQUIRE(q && q->dim() == 3 && q->size(0) <= INT32_MAX, "q is [rows][Hq][128]");
+  const int64_t rows = q->size(0);
+  REQUIRE(!none(a[4]), "a tensor is missing");
+  Io io;
+  if (!io.read(a[3], a[4], a[5], rows, heads, dev)) return nullptr;
+  bool ok;
+  const int32_t* starts = row_starts(a[6], batch, rows, dev, &ok);
+  if (!ok) return nullptr;
+  return status([&] { return entry.chunk_attn(ctx, io.q, starts, (int32_t)rows, kv, mask, (int32_t)batch, io.out, io.lse, stream); });
+}
+
 // torch's C++ exceptions (a tensor without storage or strides) as Python's: none may leave a C function.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t nargs) noexcept {
@@ -443,7 +466,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t nargs) noexcept
 #define METHOD(name) {#name, (PyCFunction)(void*)guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(kv_view), METHOD(bytekv_view), METHOD(bounds_view), METHOD(bind), METHOD(bytekv_append), METHOD(bytekv_decode_attn),
                          METHOD(bytekv_sparse_decode_attn), METHOD(block_bounds), METHOD(block_topk), METHOD(block_decode_attn),
-                         METHOD(block_decode_step), METHOD(qkv_append), METHOD(bytekv_qkv_append), METHOD(bytekv_read), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(block_decode_step), METHOD(qkv_append), METHOD(bytekv_qkv_append), METHOD(bytekv_read), METHOD(chunk_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -28,6 +28,7 @@
 #include "bytekv.cuh"
 #include "block_sparse.cuh"
 #include "tokens.cuh"
+#include "chunk_attn.cuh"
 
 using namespace prhs;
 
@@ -67,6 +68,9 @@ struct prhs_ctx {
   float* partials = nullptr;
   float* stream_part = nullptr;     // parts of units that two CTAs of the 8-bit dense attention share
   unsigned int* tickets = nullptr;
+  float* chunk_part = nullptr;      // pieces of items that CTAs of the chunk attention share, two per CTA
+  unsigned int* chunk_tickets = nullptr;
+  bool chunk_fits = false;
   int* idx = nullptr;
   int* count = nullptr;
   uint32_t* flags = nullptr;
@@ -579,6 +583,7 @@ prhs_status check_layer(prhs_ctx* c, int layer, int step, const prhs_schedule* s
 #include "bytekv_host.cuh"
 #include "block_host.cuh"
 #include "tokens_host.cuh"
+#include "chunk_host.cuh"
 
 extern "C" {
 
@@ -819,6 +824,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
     e = cudaFuncSetAttribute(dense_attn_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
   if (e == cudaSuccess) e = bytekv_set_attributes();
   if (e == cudaSuccess) e = block_set_attributes();
+  if (e == cudaSuccess) e = chunk_set_attributes(&c->chunk_fits);
   if (e == cudaSuccess) {
     int nb = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, gather_attn_mma_kernel, kTThreads, kTSmemBytes);
@@ -836,6 +842,9 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = dev_alloc(&c->partials, U * kMaxSplits * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->stream_part, (size_t)2 * k8MaxCtasPerSm * c->sm_count * c->gq * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->tickets, U);
+  if (e == cudaSuccess) e = dev_alloc(&c->chunk_part, (size_t)2 * c->sm_count * kCASlotFloats);
+  if (e == cudaSuccess) e = dev_alloc(&c->chunk_tickets, c->sm_count);
+  if (e == cudaSuccess) e = cudaMemset(c->chunk_tickets, 0, c->sm_count * sizeof(unsigned int));
   if (e == cudaSuccess) e = dev_alloc(&c->idx, U * c->idx_cap);
   if (e == cudaSuccess) e = dev_alloc(&c->count, U);
   if (e == cudaSuccess) e = dev_alloc(&c->flags, 1);
@@ -880,7 +889,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
 
 prhs_status prhs_destroy(prhs_ctx* c) {
   if (!c) return PRHS_OK;
-  void* ptrs[] = {c->scores, c->part_ml, c->lse_full, c->lse_c, c->partials, c->stream_part, c->tickets, c->idx,
+  void* ptrs[] = {c->scores, c->part_ml, c->lse_full, c->lse_c, c->partials, c->stream_part, c->tickets, c->chunk_part, c->chunk_tickets, c->idx,
                   c->count, c->flags, c->scratch_out, c->sstar_desc, c->sstar_asc, c->shat_asc,
                   c->n_star, c->n_hat, c->anchor_t, c->qhist, c->set_of_pos, c->nsets, c->g_need,
                   c->g_slot, c->g_ref, c->st_q, c->st_out, c->st_k, c->st_v};

@@ -15,7 +15,7 @@ bool apart(const void* a, uintptr_t a_bytes, const void* b, uintptr_t b_bytes) {
 
 prhs_status check_tokens(prhs_ctx* c, const prhs_token_rows* rows, const prhs_qk_prep* prep, int batch, const void* q_out, TokenRowsDev* in,
                          PrepDev* pd) {
-  if (!rows || !prep || !rows->q || !rows->k || !rows->v || !q_out) return fail(c, PRHS_ERR_INVALID_ARG, "new tokens: NULL pointer");
+  if (!rows || !prep || (rows->num_rows != 0 && (!rows->q || !rows->k || !rows->v || !q_out))) return fail(c, PRHS_ERR_INVALID_ARG, "new tokens: NULL pointer");
   const int hq = c->cfg.num_q_heads, hkv = c->cfg.num_kv_heads;
   const int64_t strides[] = {rows->q_stride_row, rows->q_stride_head, rows->k_stride_row, rows->k_stride_head, rows->v_stride_row, rows->v_stride_head};
   for (int64_t s : strides)

@@ -408,6 +408,8 @@ def test_refusals(cuda_device):
         p.axis_of[1] = 1
         with pytest.raises(P.PrhsError):
             call(t.q, t.k, t.v, view, p, 2, t.q_out, **ok)
+    for call, view in ((ctx.qkv_append, t.view()), (ctx.bytekv_qkv_append, cache.view())):       # no rows at all: nothing to do
+        call(t.q[:0], t.k[:0], t.v[:0], view, prep, 2, t.q_out[:0], row_start=torch.zeros(3, dtype=torch.int32, device=cuda_device))
     with pytest.raises(AssertionError):
         ctx.bytekv_read(cache.view(), t.view(), 2, first=t.lens_t.long())
     with pytest.raises(P.PrhsError):
