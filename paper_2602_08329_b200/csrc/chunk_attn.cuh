@@ -45,6 +45,7 @@ constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // 
 constexpr uint32_t kCAIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCATile >> 3) << 17) | ((uint32_t)(kCATile >> 4) << 24);
 constexpr uint32_t kCAIdescPV = kCAIdesc | (1u << 16);    // B = V tile read MN-major
 constexpr float kCAGap = 8.f;
+constexpr int kCAPoly = 3, kCAPolyOf = 8;                 // of eight pairs of exponentials, three on the FMA pipe
 // An item's Q, merge and output cost about as much as two tiles; a run of fewer than kCAMinRun tiles is not worth its merge.
 constexpr int kCAItemCost = 2;
 constexpr int kCAMinRun = 4;
@@ -71,30 +72,35 @@ __device__ __forceinline__ int first_visible(const ChunkParams& p, int u) {
   return lo;
 }
 // A piece of an item: tiles k0 .. k1 - 1 of those its tokens see.
+template <bool kMask>
 struct Piece {
   int b, kvh, row0, ntok, u0;    // u0: visible length of the first token
   int k0, k1, st, lo;            // tile k is k for k < st, else lo + k - st
   int first_cta, last_cta;       // CTAs that have pieces of the item
   int t;
   bool halves;
-  // per subtile: tokens [a, e), visible lengths of the first and last, where their windows begin
-  int a[2], e[2], uf[2], ul[2], pf[2], pl[2];
-  __device__ __forceinline__ int tile(int k) const { return k < st ? k : lo + k - st; }
+  __device__ __forceinline__ int tile(int k) const { return !kMask || k < st ? k : lo + k - st; }
+  // subtile s: tokens [a, e) of the item, visible lengths of its first and its last
+  __device__ __forceinline__ int a(const ChunkParams& p, int s) const { return halves || s == 0 ? 0 : p.tokens; }
+  __device__ __forceinline__ int e(const ChunkParams& p, int s) const { return halves || s == 1 ? ntok : min(ntok, p.tokens); }
+  __device__ __forceinline__ int uf(const ChunkParams& p, int s) const { return u0 + a(p, s); }
+  __device__ __forceinline__ int ul(const ChunkParams& p, int s) const { return u0 + e(p, s) - 1; }
   __device__ __forceinline__ bool active(const ChunkParams& p, int s, int k) const {
     if (halves) return ((k - k0) & 1) == s;
     const int at = tile(k) * kCATile;
-    return e[s] > a[s] && at < ul[s] && (at < p.sinks || at + kCATile > pf[s]);
+    return at < ul(p, s) && (!kMask || at < p.sinks || at + kCATile > first_visible(p, uf(p, s)));      // (both subtiles have tokens)
   }
   // some row of the subtile does not see all of the tile
   __device__ __forceinline__ bool partly(const ChunkParams& p, int s, int k) const {
     const int at = tile(k) * kCATile;
-    return !(at + kCATile <= uf[s] && (at + kCATile <= p.sinks || at >= pl[s]));
+    return !(at + kCATile <= uf(p, s) && (!kMask || at + kCATile <= p.sinks || at >= first_visible(p, ul(p, s))));
   }
   __device__ __forceinline__ bool mended(const ChunkParams& p, int k) const {
     return (active(p, 0, k) && partly(p, 0, k)) || (active(p, 1, k) && partly(p, 1, k));
   }
 };
 // Walks this CTA's run.  Every warp does so for itself; all lanes hold the same values.
+template <bool kMask>
 struct ChunkWalk {
   const ChunkParams& p;
   long long at = 0, end = 0, total = 0, item_at = 0;
@@ -107,8 +113,8 @@ struct ChunkWalk {
     const int a = item * 2 * p.tokens, e = min(q.n, a + 2 * p.tokens);
     const int uf = q.t - q.n + a + 1, ul = q.t - q.n + e;
     *hi = (ul + kCATile - 1) / kCATile;
-    *lo = first_visible(p, uf) / kCATile;
-    *st = min((min(p.sinks, ul) + kCATile - 1) / kCATile, *lo);
+    *lo = kMask ? first_visible(p, uf) / kCATile : 0;
+    *st = kMask ? min((min(p.sinks, ul) + kCATile - 1) / kCATile, *lo) : 0;
   }
   __device__ __forceinline__ int cost(const SeqRows& q, int item) const {
     int st, lo, hi;
@@ -207,7 +213,7 @@ struct ChunkWalk {
     }
     return true;
   }
-  __device__ __forceinline__ bool next(Piece& x) {
+  __device__ __forceinline__ bool next(Piece<kMask>& x) {
     if (at >= end) return false;
     if (i == items) {
       i = 0;
@@ -233,15 +239,6 @@ struct ChunkWalk {
     x.u0 = s.t - s.n + i * 2 * p.tokens + 1;
     x.t = s.t;
     x.halves = x.ntok <= p.tokens;
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      x.a[y] = x.halves ? 0 : y * p.tokens;
-      x.e[y] = x.halves ? x.ntok : min(x.ntok, (y + 1) * p.tokens);
-      x.uf[y] = x.u0 + x.a[y];
-      x.ul[y] = x.u0 + x.e[y] - 1;
-      x.pf[y] = first_visible(p, x.uf[y]);
-      x.pl[y] = first_visible(p, x.ul[y]);
-    }
     at = to;
     if (to == item_at + w) {
       item_at = to;
@@ -260,11 +257,42 @@ __device__ __forceinline__ void tma_load_3d_plain(uint32_t dst, const CUtensorMa
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
-// A operand in tensor memory
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+  return r != 0;
+}
+// lower words of the matrix descriptors (see umma_desc, umma_desc_mn); the upper one is kSUDescHi
+__device__ __forceinline__ uint32_t umma_desc_lo(uint32_t smem_addr) { return ((smem_addr >> 4) & 0x3fffu) | (1u << 16); }
+__device__ __forceinline__ uint32_t umma_desc_mn_lo(uint32_t smem_addr) {
+  return ((smem_addr >> 4) & 0x3fffu) | ((uint32_t)(kCAHalfBytes >> 4) << 16);
+}
+// S = Q K^T: eight steps of 16 columns, 32 bytes apart in a row; the second 64 columns are a box of their own, 16 KB further
+__device__ __forceinline__ void umma_qk(uint32_t d, uint32_t q_lo, uint32_t k_lo) {
   asm volatile(
-      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n .reg .b32 x, y;\n .reg .b64 a, b;\n .reg .pred f, t;\n"
+      " setp.ne.b32 f, 0, 0;\n setp.eq.b32 t, 0, 0;\n"
+      " mov.b64 a, {%1, %3};\n mov.b64 b, {%2, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, f;\n"
+      " add.u32 x, %1, 2;\n add.u32 y, %2, 2;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 4;\n add.u32 y, %2, 4;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 6;\n add.u32 y, %2, 6;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 1024;\n add.u32 y, %2, 1024;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 1026;\n add.u32 y, %2, 1026;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 1028;\n add.u32 y, %2, 1028;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n"
+      " add.u32 x, %1, 1030;\n add.u32 y, %2, 1030;\n mov.b64 a, {x, %3};\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, t;\n}"
+      ::"r"(d), "r"(q_lo), "r"(k_lo), "r"(kSUDescHi), "r"(kCAIdesc)
+      : "memory");
+}
+// O (+)= P V over 64 keys: four steps of 16 keys, 8 columns of P and 2 KB of V apart
+__device__ __forceinline__ void umma_pv4(uint32_t d, uint32_t a, uint32_t v_lo, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .b32 x, y;\n .reg .b64 b;\n .reg .pred f, t;\n"
+      " setp.ne.b32 f, %5, 0;\n setp.eq.b32 t, 0, 0;\n"
+      " mov.b64 b, {%2, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, f;\n"
+      " add.u32 x, %1, 8;\n add.u32 y, %2, 128;\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, t;\n"
+      " add.u32 x, %1, 16;\n add.u32 y, %2, 256;\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, t;\n"
+      " add.u32 x, %1, 24;\n add.u32 y, %2, 384;\n mov.b64 b, {y, %3};\n tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, t;\n}"
+      ::"r"(d), "r"(a), "r"(v_lo), "r"(kSUDescHi), "r"(kCAIdescPV), "r"(accumulate)
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
@@ -314,6 +342,35 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// the largest of three; NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t exp2_fast_x2(uint64_t t) {
+  float a, b;
+  unpack_f32x2(t, a, b);
+  return pack_f32x2(exp2_fast(a), exp2_fast(b));
+}
+// 2^t for two finite t <= 2^7 on the FMA pipe: t = n + f with n the nearest integer (found by adding 1.5 * 2^23) and 2^f, |f| <= 1/2, by the
+// polynomial of degree 4 of least relative error there (from a Remez exchange: 2.7e-6 at most, 4e-8 on average, where a weight
+// is rounded to 2^-8); n goes into the exponent.  Below 2^-125 the result stays there.
+__device__ __forceinline__ uint64_t exp2_poly_x2(uint64_t t) {
+  float a, b;
+  unpack_f32x2(t, a, b);
+  t = pack_f32x2(fmaxf(a, -125.f), fmaxf(b, -125.f));
+  const uint64_t y = add_f32x2(t, pack_f32x2(12582912.f, 12582912.f));
+  const uint64_t f = fma_f32x2(add_f32x2(y, pack_f32x2(-12582912.f, -12582912.f)), pack_f32x2(-1.f, -1.f), t);
+  uint64_t q = fma_f32x2(f, pack_f32x2(0.009570102207362652f, 0.009570102207362652f), pack_f32x2(0.05591785907745361f, 0.05591785907745361f));
+  q = fma_f32x2(q, f, pack_f32x2(0.240247443318367f, 0.240247443318367f));
+  q = fma_f32x2(q, f, pack_f32x2(0.6931217908859253f, 0.6931217908859253f));
+  q = fma_f32x2(q, f, pack_f32x2(0.9999992847442627f, 0.9999992847442627f));
+  float ya, yb;
+  unpack_f32x2(y, ya, yb);
+  unpack_f32x2(q, a, b);
+  return pack_f32x2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(ya) << 23)), __uint_as_float(__float_as_uint(b) + (__float_as_uint(yb) << 23)));
+}
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // Ring position: slot and the parity of its fill.
@@ -333,26 +390,26 @@ struct RingPos {
 #define PRHS_CHUNK_STEPS(x, k) for (int k = (x).k0, lag_ = (x).halves ? 2 : 1, stop_ = (x).k1 > (x).k0 ? (x).k1 + lag_ : (x).k0; k < stop_; ++k)
 
 // grid: one CTA per SM.  tm_q: q as [rows][Hq][128], box [T][G][64]; tm_k, tm_v: [rows][128], box [128][64], or [16][64] per page.
-template <bool kPaged>
+template <bool kPaged, bool kMask>
 __global__ void __launch_bounds__(kCAThreads, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ ChunkParams p) {
   extern __shared__ unsigned char ca_smem_raw[];
-  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_empty[2], drain
-  __shared__ __align__(8) unsigned long long bars[3 * kCASlots + 11];
+  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain
+  __shared__ __align__(8) unsigned long long bars[3 * kCASlots + 13];
   __shared__ int mended_n[4], mended_tile[4][kCAMaxMended];
   __shared__ uint32_t tmem_slot;
   __shared__ int sh_abort, sh_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0) record_bad_sequences(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, p.batch, p.flags);
-  ChunkWalk walk(p);
+  ChunkWalk<kMask> walk(p);
   if (!walk.begin()) return;
   const uint32_t smem0 = ((uint32_t)__cvta_generic_to_shared(ca_smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = smem0 + 2 * kCATileBytes;
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
   const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
   const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
-  const uint32_t bar_ofull = bar_qfull + 48, bar_oempty = bar_qfull + 64, bar_drain = bar_qfull + 80;
+  const uint32_t bar_ofull = bar_qfull + 64, bar_oempty = bar_qfull + 80, bar_drain = bar_qfull + 96;
   if (tid == 0) {
     for (int i = 0; i < kCASlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);      // the producer's expect_tx arrive
@@ -363,7 +420,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     mbar_init(bar_qempty, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_sfull + 8 * i, 1);     // a commit of the MMA thread
-      mbar_init(bar_pfull + 8 * i, 4);     // the subtile's softmax warps
+      mbar_init(bar_pfull + 16 * i, 4);    // the subtile's softmax warps
+      mbar_init(bar_pfull + 16 * i + 8, 4);
       mbar_init(bar_ofull + 8 * i, 1);     // a commit of the MMA thread
       mbar_init(bar_oempty + 8 * i, 4);    // the subtile's softmax warps
     }
@@ -380,7 +438,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem0 = *(volatile uint32_t*)&tmem_slot;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
-  Piece x;
+  Piece<kMask> x;
   auto gave_up = [&] {
     atomicOr(p.flags, kFlagTimeout);
     sh_abort = 1;
@@ -398,15 +456,44 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     int buf = 0;                                     // of the mending warps' notes
     bool aborted = false;                            // a warp that gave up goes on without touching anything: barriers stay balanced
     while (walk.next(x)) {
-      const bool used = row < p.tokens * p.group && token < x.e[s] - x.a[s];
+      const bool used = row < p.tokens * p.group && token < x.e(p, s) - x.a(p, s);
       const bool warp_used = __any_sync(0xffffffffu, used);
-      const int u = used ? x.uf[s] + token : 0;
-      const int from = used ? first_visible(p, u) : 0;
+      const int uf = x.uf(p, s), ul = x.ul(p, s), u = used ? uf + token : 0;
+      const int from = kMask && used ? first_visible(p, u) : 0, from0 = kMask ? first_visible(p, uf) : 0, from1 = kMask ? first_visible(p, ul) : 0;
       float m = -INFINITY;
       uint64_t l2 = 0ull;                            // two partial sums
       bool any = false;                              // O holds something
-      for (int k = x.k0; k < x.k1; ++k) {
-        if (!x.active(p, s, k)) continue;
+      // a tile that some row sees in part: masks, and logits that are not finite
+      auto careful = [&](uint32_t (&r)[4][32], bool partly, int at) {
+        const int cu = u - at, cs = p.sinks - at, cf = from - at;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 128; ++c) {
+          if (partly && !(c < cu && (!kMask || c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
+          mx = fmaxf(mx, __uint_as_float(r[c >> 5][c & 31]));            // (passes over NaNs)
+        }
+        return mx;
+      };
+      // the reference moves: what has been summed up so far is scaled down
+      auto raise = [&](float mx) {
+        const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
+        l2 = fma_f32x2(l2, pack_f32x2(f, f), 0ull);
+        m = mn;
+        if (any) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            float o[16];
+            tmem_ld16(tm_o + 16 * c, o);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[j] *= f;
+            tmem_st16(tm_o + 16 * c, o);
+          }
+        }
+      };
+      const int step = x.halves ? 2 : 1;
+      for (int k = x.halves ? x.k0 + s : x.k0; k < x.k1; k += step) {
+        const int at = x.tile(k) * kCATile;
+        if (!x.halves && !(at < ul && (!kMask || at < p.sinks || at + kCATile > from0))) continue;
         if (!aborted) {
           aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh_abort));
           if (aborted && lane == 0) gave_up();
@@ -420,60 +507,65 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           for (int c = 0; c < 4; ++c) tmem_ld32(tm_s + 32 * c, r[c]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
-          if (x.partly(p, s, k)) {
-            const int at = x.tile(k) * kCATile, cu = u - at, cs = p.sinks - at, cf = from - at;
+          const bool partly = !(at + kCATile <= uf && (!kMask || at + kCATile <= p.sinks || at >= from1));
+          float mx;
+          {
+            float y[4];
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (!(c < cu && (c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
-          }
-          float mx0 = __uint_as_float(r[0][0]), mx1 = __uint_as_float(r[0][1]);
+            for (int c = 0; c < 4; ++c) {
+              y[c] = __uint_as_float(r[c][0]);
 #pragma unroll
-          for (int c = 2; c < 128; c += 4) {
-            mx0 = fmaxf(mx0, fmaxf(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[(c + 1) >> 5][(c + 1) & 31])));
-            if (c + 2 < 128) mx1 = fmaxf(mx1, fmaxf(__uint_as_float(r[(c + 2) >> 5][(c + 2) & 31]), __uint_as_float(r[(c + 3) >> 5][(c + 3) & 31])));
-          }
-          const float mx = fmaxf(mx0, mx1) * c1;
-          if (__any_sync(0xffffffffu, mx > m + kCAGap)) {
-            const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
-            l2 = fma_f32x2(l2, pack_f32x2(f, f), 0ull);
-            m = mn;
-            if (any) {
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                float o[16];
-                tmem_ld16(tm_o + 16 * c, o);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] *= f;
-                tmem_st16(tm_o + 16 * c, o);
-              }
+              for (int j = 1; j < 31; j += 2) y[c] = max3_nan(y[c], __uint_as_float(r[c][j]), __uint_as_float(r[c][j + 1]));
+              y[c] = max3_nan(y[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
             }
+            mx = max3_nan(max3_nan(y[0], y[1], y[2]), y[3], y[3]);
           }
+          const bool plain = __all_sync(0xffffffffu, !partly && fabsf(mx) < INFINITY);
+          if (!plain) mx = careful(r, partly, at);
+          mx *= c1;
+          if (__any_sync(0xffffffffu, mx > m + kCAGap)) raise(mx);
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t cc = pack_f32x2(c1, c1), mm = pack_f32x2(-ref, -ref);
           uint64_t la = 0ull, lb = 0ull;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t w[32];
+            if (plain) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const int c = 64 * h + 2 * j;
-              float a, b;
-              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm), a, b);
-              a = exp2_fast(a);
-              b = exp2_fast(b);
-              if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
-              else lb = add_f32x2(lb, pack_f32x2(a, b));
-              w[j] = pack_bf16x2(a, b);
+              for (int j = 0; j < 32; ++j) {
+                const int c = 64 * h + 2 * j;
+                const uint64_t t = fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm);
+                const uint64_t e = j % kCAPolyOf < kCAPoly ? exp2_poly_x2(t) : exp2_fast_x2(t);
+                if (j & 1) la = add_f32x2(la, e);
+                else lb = add_f32x2(lb, e);
+                float a, b;
+                unpack_f32x2(e, a, b);
+                w[j] = pack_bf16x2(a, b);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const int c = 64 * h + 2 * j;
+                const uint64_t e = exp2_fast_x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm));
+                if (j & 1) la = add_f32x2(la, e);
+                else lb = add_f32x2(lb, e);
+                float a, b;
+                unpack_f32x2(e, a, b);
+                w[j] = pack_bf16x2(a, b);
+              }
             }
             tmem_st32(tm_s + 32 * h, w);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_pfull + 16 * s + 8 * h);
           }
           l2 = add_f32x2(l2, add_f32x2(la, lb));
-          tmem_wait_st();
-          tc_fence_before();
+        } else if (lane == 0) {
+          mbar_arrive(bar_pfull + 16 * s);
+          mbar_arrive(bar_pfull + 16 * s + 8);
         }
         any = true;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_pfull + 8 * s);
       }
       float la, lb;
       unpack_f32x2(l2, la, lb);
@@ -487,7 +579,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const bool whole = x.first_cta == x.last_cta && !x.halves;
       const int slot = 2 * blockIdx.x + (x.first_cta == (int)blockIdx.x ? 1 : 0);
       float* const part = p.partials + (size_t)slot * kCASlotFloats;
-      const long long out_row = ((long long)(x.row0 + x.a[s] + token) * p.num_q_heads + x.kvh * p.group + head);
+      const long long out_row = ((long long)(x.row0 + x.a(p, s) + token) * p.num_q_heads + x.kvh * p.group + head);
       const int mended = any ? mended_n[buf & 3] : 0;
       if (!aborted && warp_used) {
         tc_fence_after();
@@ -689,77 +781,94 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       }
       if (!ok && lane == 0) gave_up();
     } else if (warp == kCAMmaWarp) {
-      // ------------------------------------------------------------------------ MMA issue: one thread
-      if (lane == 0) {
-        RingPos pos;
-        uint32_t q_par = 0, vr_par = 0, p_par[2] = {0, 0}, oe_par[2] = {1, 1};
-        bool ok = true;
-        while (ok && walk.next(x)) {
-          if (x.k0 == x.k1) continue;
-          ok = mbar_wait(bar_qfull, q_par, &sh_abort);
-          q_par ^= 1;
-          bool started[2] = {false, false};
-          PRHS_CHUNK_STEPS(x, k) {
-            const int prev = k - lag_;
-            const bool pv = prev >= x.k0, qk = k < x.k1;
-            RingPos vpos = pos;
-            if (pv) {
-              pos.step();
-              if (ok) ok = mbar_wait(bar_full + 8 * vpos.slot, vpos.parity, &sh_abort);
-              if (ok && x.mended(p, prev)) {
-                ok = mbar_wait(bar_vready + 8 * vpos.slot, (vr_par >> vpos.slot) & 1u, &sh_abort);
-                vr_par ^= 1u << vpos.slot;
+      // ------------------------------------------------------------------------ MMA issue: one thread issues, the warp waits.
+      // (The control flow is the whole warp's: operands of an MMA are uniform registers, and in code that a single lane has branched
+      // into each one costs about a hundred cycles to issue.)
+      const bool leader = elect_one();
+      RingPos pos;
+      uint32_t q_par = 0, vr_par = 0, p_par[2] = {0, 0}, oe_par[2] = {1, 1};
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, &sh_abort));
+      };
+      while (ok && walk.next(x)) {
+        if (x.k0 == x.k1) continue;
+        wait(bar_qfull, q_par);
+        q_par ^= 1;
+        const int uf[2] = {x.uf(p, 0), x.uf(p, 1)}, ul[2] = {x.ul(p, 0), x.ul(p, 1)};
+        const int from0[2] = {kMask ? first_visible(p, uf[0]) : 0, kMask ? first_visible(p, uf[1]) : 0};
+        const int from1[2] = {kMask ? first_visible(p, ul[0]) : 0, kMask ? first_visible(p, ul[1]) : 0};
+        bool started[2] = {false, false};
+        // what tile k asks for: bits 0, 1: the subtiles that use it; bit 2: its values are mended first
+        auto asks = [&](int k) {
+          uint32_t r = 0;
+          const int at = x.tile(k) * kCATile;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const bool act = x.halves ? ((k - x.k0) & 1) == s : at < ul[s] && (!kMask || at < p.sinks || at + kCATile > from0[s]);
+            const bool all = at + kCATile <= uf[s] && (!kMask || at + kCATile <= p.sinks || at >= from1[s]);
+            if (act) r |= all ? 1u << s : 4u | 1u << s;
+          }
+          return r;
+        };
+        uint32_t before[2] = {0, 0};                 // of the latest two tiles
+        PRHS_CHUNK_STEPS(x, k) {
+          const bool pv = k - lag_ >= x.k0, qk = k < x.k1;
+          const uint32_t then = before[lag_ - 1], now = qk ? asks(k) : 0u;
+          before[1] = before[0];
+          before[0] = now;
+          const RingPos vpos = pos;
+          if (pv) {
+            pos.step();
+            wait(bar_full + 8 * vpos.slot, vpos.parity);
+            if (then & 4u) {
+              wait(bar_vready + 8 * vpos.slot, (vr_par >> vpos.slot) & 1u);
+              vr_par ^= 1u << vpos.slot;
+            }
+          }
+          const RingPos kpos = pos;
+          if (qk) pos.step();
+          bool k_here = false;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (pv && (then >> s) & 1u) {
+              const uint32_t d = tmem0 + (2 + s) * kCATile, a = tmem0 + s * kCATile, vd = umma_desc_mn_lo(ring + vpos.slot * kCATileBytes);
+              wait(bar_pfull + 16 * s, p_par[s]);
+              if (!started[s]) {
+                wait(bar_oempty + 8 * s, oe_par[s]);
+                oe_par[s] ^= 1;
+              }
+              tc_fence_after();
+              if (ok && leader) umma_pv4(d, a, vd, started[s] ? 1u : 0u);
+              wait(bar_pfull + 16 * s + 8, p_par[s]);
+              p_par[s] ^= 1;
+              tc_fence_after();
+              if (ok && leader) umma_pv4(d, a + 32, vd + 4 * ((16 * 128) >> 4), 1u);
+              started[s] = true;
+            }
+            if (s == 1 && pv && ok && leader) umma_commit(bar_empty + 8 * vpos.slot);
+            if ((now >> s) & 1u) {
+              if (!k_here) wait(bar_full + 8 * kpos.slot, kpos.parity);
+              k_here = true;
+              tc_fence_after();
+              if (ok && leader) {
+                umma_qk(tmem0 + s * kCATile, umma_desc_lo(smem0 + (x.halves ? 0 : s) * kCATileBytes), umma_desc_lo(ring + kpos.slot * kCATileBytes));
+                umma_commit(bar_sfull + 8 * s);
               }
             }
-            const RingPos kpos = pos;
-            if (qk) pos.step();
-            bool k_here = false;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              if (ok && pv && x.active(p, s, prev)) {
-                ok = mbar_wait(bar_pfull + 8 * s, p_par[s], &sh_abort);
-                p_par[s] ^= 1;
-                if (ok && !started[s]) {
-                  ok = mbar_wait(bar_oempty + 8 * s, oe_par[s], &sh_abort);
-                  oe_par[s] ^= 1;
-                }
-                if (ok) {
-                  tc_fence_after();
-                  const uint64_t vd = umma_desc_mn(ring + vpos.slot * kCATileBytes);
-#pragma unroll
-                  for (int ks = 0; ks < 8; ++ks)
-                    umma_bf16_ts(tmem0 + (2 + s) * kCATile, tmem0 + s * kCATile + 8 * ks, vd + (uint64_t)(ks * ((16 * 128) >> 4)), kCAIdescPV,
-                                 started[s] || ks > 0 ? 1u : 0u);
-                }
-                started[s] = true;
-              }
-              if (ok && pv && s == 1) umma_commit(bar_empty + 8 * vpos.slot);
-              if (ok && qk && x.active(p, s, k)) {
-                if (!k_here) ok = mbar_wait(bar_full + 8 * kpos.slot, kpos.parity, &sh_abort);
-                k_here = true;
-                if (ok) {
-                  tc_fence_after();
-                  const uint64_t qd = umma_desc(smem0 + (x.halves ? 0 : s) * kCATileBytes), kd = umma_desc(ring + kpos.slot * kCATileBytes);
-#pragma unroll
-                  for (int ks = 0; ks < 8; ++ks) {
-                    const uint64_t off = (uint64_t)((ks >> 2) * (kCAHalfBytes >> 4) + (ks & 3) * 2);
-                    umma_bf16(tmem0 + s * kCATile, qd + off, kd + off, kCAIdesc, ks > 0 ? 1u : 0u);
-                  }
-                  umma_commit(bar_sfull + 8 * s);
-                }
-              }
-            }
-            if (ok && qk) umma_commit(bar_empty + 8 * kpos.slot);
-            if (ok && k == x.k1 - 1) umma_commit(bar_qempty);
-            if (!ok) break;
           }
-          if (ok) {
-            if (started[0]) umma_commit(bar_ofull);
-            if (started[1]) umma_commit(bar_ofull + 8);
+          if (ok && leader) {
+            if (qk) umma_commit(bar_empty + 8 * kpos.slot);
+            if (k == x.k1 - 1) umma_commit(bar_qempty);
           }
+          if (!ok) break;
         }
-        if (!ok) gave_up();
+        if (ok && leader) {
+          if (started[0]) umma_commit(bar_ofull);
+          if (started[1]) umma_commit(bar_ofull + 8);
+        }
       }
+      if (!ok && lane == 0) gave_up();
       __syncwarp();
     } else {
       // ------------------------------------------------------------------------ mending warps

@@ -8,7 +8,8 @@ constexpr int kCARegsAtLaunch = 168;      // what the kernel's register split (2
 
 cudaError_t chunk_set_attributes(bool* fits) {
   *fits = true;
-  for (const void* k : {(const void*)chunk_attn_kernel<false>, (const void*)chunk_attn_kernel<true>}) {
+  for (const void* k : {(const void*)chunk_attn_kernel<false, false>, (const void*)chunk_attn_kernel<false, true>,
+                        (const void*)chunk_attn_kernel<true, false>, (const void*)chunk_attn_kernel<true, true>}) {
     cudaFuncAttributes a;
     cudaError_t e = cudaFuncGetAttributes(&a, k);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kCASmemBytes);
@@ -102,8 +103,9 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
   cudaStream_t st = as_stream(stream);
   {
     LaunchScope ls(ctx, PRHS_KIND_ATTN_DENSE, st);
-    if (paged) chunk_attn_kernel<true><<<ctx->sm_count, kCAThreads, kCASmemBytes, st>>>(tm_q, tm_k, tm_v, p);
-    else chunk_attn_kernel<false><<<ctx->sm_count, kCAThreads, kCASmemBytes, st>>>(tm_q, tm_k, tm_v, p);
+    auto launch = [&](auto kernel) { kernel<<<ctx->sm_count, kCAThreads, kCASmemBytes, st>>>(tm_q, tm_k, tm_v, p); };
+    if (p.window > 0 || p.psaw_c > 0.0) launch(paged ? chunk_attn_kernel<true, true> : chunk_attn_kernel<false, true>);
+    else launch(paged ? chunk_attn_kernel<true, false> : chunk_attn_kernel<false, false>);
   }
   PRHS_CUDA(ctx, cudaGetLastError());
   return PRHS_OK;
