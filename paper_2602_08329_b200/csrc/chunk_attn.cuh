@@ -79,25 +79,39 @@ struct Piece {
   int first_cta, last_cta;       // CTAs that have pieces of the item
   int t;
   bool halves;
+  // Subtile s uses tile k if k < sa or kb <= k < ke, and every one of its rows sees all of it if k < sf or kf <= k < kd.  (The first
+  // positions may reach beyond `lo`: all tiles are listed then, and st = lo.)
+  int sa, kb[2], ke[2], kf[2], kd[2], sf[2];
   __device__ __forceinline__ int tile(int k) const { return !kMask || k < st ? k : lo + k - st; }
   // subtile s: tokens [a, e) of the item, visible lengths of its first and its last
   __device__ __forceinline__ int a(const ChunkParams& p, int s) const { return halves || s == 0 ? 0 : p.tokens; }
   __device__ __forceinline__ int e(const ChunkParams& p, int s) const { return halves || s == 1 ? ntok : min(ntok, p.tokens); }
   __device__ __forceinline__ int uf(const ChunkParams& p, int s) const { return u0 + a(p, s); }
   __device__ __forceinline__ int ul(const ChunkParams& p, int s) const { return u0 + e(p, s) - 1; }
-  __device__ __forceinline__ bool active(const ChunkParams& p, int s, int k) const {
-    if (halves) return ((k - k0) & 1) == s;
-    const int at = tile(k) * kCATile;
-    return at < ul(p, s) && (!kMask || at < p.sinks || at + kCATile > first_visible(p, uf(p, s)));      // (both subtiles have tokens)
+  __device__ __forceinline__ void ranges(const ChunkParams& p) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int first = uf(p, s), last = ul(p, s);
+      ke[s] = (last + kCATile - 1) / kCATile;
+      kd[s] = first / kCATile;
+      kb[s] = kf[s] = sf[s] = 0;
+      if (kMask) {
+        const int shift = st - lo, all = min(p.sinks, ul(p, 1));
+        sa = shift ? st : (all + kCATile - 1) / kCATile;
+        kb[s] = first_visible(p, first) / kCATile + shift;
+        kf[s] = max((first_visible(p, last) + kCATile - 1) / kCATile + shift, st);
+        sf[s] = shift ? min(min(p.sinks, first) / kCATile, st) : min(p.sinks, first) / kCATile;
+        ke[s] += shift;
+        kd[s] += shift;
+      }
+    }
+  }
+  __device__ __forceinline__ bool active(int s, int k) const {
+    return halves ? ((k - k0) & 1) == s : k < ke[s] && (!kMask || k < sa || k >= kb[s]);
   }
   // some row of the subtile does not see all of the tile
-  __device__ __forceinline__ bool partly(const ChunkParams& p, int s, int k) const {
-    const int at = tile(k) * kCATile;
-    return !(at + kCATile <= uf(p, s) && (!kMask || at + kCATile <= p.sinks || at >= first_visible(p, ul(p, s))));
-  }
-  __device__ __forceinline__ bool mended(const ChunkParams& p, int k) const {
-    return (active(p, 0, k) && partly(p, 0, k)) || (active(p, 1, k) && partly(p, 1, k));
-  }
+  __device__ __forceinline__ bool partly(int s, int k) const { return !(kMask ? k < sf[s] || (k >= kf[s] && k < kd[s]) : k < kd[s]); }
+  __device__ __forceinline__ bool mended(int k) const { return (active(0, k) && partly(0, k)) || (active(1, k) && partly(1, k)); }
 };
 // Walks this CTA's run.  Every warp does so for itself; all lanes hold the same values.
 template <bool kMask>
@@ -239,6 +253,7 @@ struct ChunkWalk {
     x.u0 = s.t - s.n + i * 2 * p.tokens + 1;
     x.t = s.t;
     x.halves = x.ntok <= p.tokens;
+    x.ranges(p);
     at = to;
     if (to == item_at + w) {
       item_at = to;
@@ -458,8 +473,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     while (walk.next(x)) {
       const bool used = row < p.tokens * p.group && token < x.e(p, s) - x.a(p, s);
       const bool warp_used = __any_sync(0xffffffffu, used);
-      const int uf = x.uf(p, s), ul = x.ul(p, s), u = used ? uf + token : 0;
-      const int from = kMask && used ? first_visible(p, u) : 0, from0 = kMask ? first_visible(p, uf) : 0, from1 = kMask ? first_visible(p, ul) : 0;
+      const int u = used ? x.uf(p, s) + token : 0;
+      const int from = kMask && used ? first_visible(p, u) : 0;
+      const int kb = s ? x.kb[1] : x.kb[0], ke = x.halves ? x.k1 : min(x.k1, s ? x.ke[1] : x.ke[0]);
+      const int kf = s ? x.kf[1] : x.kf[0], kd = s ? x.kd[1] : x.kd[0], sf = s ? x.sf[1] : x.sf[0];
       float m = -INFINITY;
       uint64_t l2 = 0ull;                            // two partial sums
       bool any = false;                              // O holds something
@@ -491,9 +508,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
       };
       const int step = x.halves ? 2 : 1;
-      for (int k = x.halves ? x.k0 + s : x.k0; k < x.k1; k += step) {
-        const int at = x.tile(k) * kCATile;
-        if (!x.halves && !(at < ul && (!kMask || at < p.sinks || at + kCATile > from0))) continue;
+      for (int k = x.halves ? x.k0 + s : x.k0; k < ke; k += step) {
+        if (kMask && !x.halves && k >= x.sa && k < kb) continue;
         if (!aborted) {
           aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh_abort));
           if (aborted && lane == 0) gave_up();
@@ -507,7 +523,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           for (int c = 0; c < 4; ++c) tmem_ld32(tm_s + 32 * c, r[c]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
-          const bool partly = !(at + kCATile <= uf && (!kMask || at + kCATile <= p.sinks || at >= from1));
+          const bool partly = !(kMask ? k < sf || (k >= kf && k < kd) : k < kd);
           float mx;
           {
             float y[4];
@@ -521,7 +537,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             mx = max3_nan(max3_nan(y[0], y[1], y[2]), y[3], y[3]);
           }
           const bool plain = __all_sync(0xffffffffu, !partly && fabsf(mx) < INFINITY);
-          if (!plain) mx = careful(r, partly, at);
+          if (!plain) mx = careful(r, partly, x.tile(k) * kCATile);
           mx *= c1;
           if (__any_sync(0xffffffffu, mx > m + kCAGap)) raise(mx);
           const float ref = m == -INFINITY ? 0.f : m;
@@ -788,37 +804,67 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       RingPos pos;
       uint32_t q_par = 0, vr_par = 0, p_par[2] = {0, 0}, oe_par[2] = {1, 1};
       bool ok = true;
+      const uint32_t q_lo = umma_desc_lo(smem0), ring_k = umma_desc_lo(ring), ring_v = umma_desc_mn_lo(ring);
+      constexpr uint32_t kSlotLo = kCATileBytes >> 4;
+      // (a wait that runs out leaves the later ones to return at once)
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, &sh_abort));
+        if (!mbar_try_wait(bar, parity) && !mbar_wait(bar, parity, &sh_abort)) ok = false;
       };
       while (ok && walk.next(x)) {
         if (x.k0 == x.k1) continue;
         wait(bar_qfull, q_par);
         q_par ^= 1;
-        const int uf[2] = {x.uf(p, 0), x.uf(p, 1)}, ul[2] = {x.ul(p, 0), x.ul(p, 1)};
-        const int from0[2] = {kMask ? first_visible(p, uf[0]) : 0, kMask ? first_visible(p, uf[1]) : 0};
-        const int from1[2] = {kMask ? first_visible(p, ul[0]) : 0, kMask ? first_visible(p, ul[1]) : 0};
         bool started[2] = {false, false};
-        // what tile k asks for: bits 0, 1: the subtiles that use it; bit 2: its values are mended first
-        auto asks = [&](int k) {
-          uint32_t r = 0;
-          const int at = x.tile(k) * kCATile;
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const bool act = x.halves ? ((k - x.k0) & 1) == s : at < ul[s] && (!kMask || at < p.sinks || at + kCATile > from0[s]);
-            const bool all = at + kCATile <= uf[s] && (!kMask || at + kCATile <= p.sinks || at >= from1[s]);
-            if (act) r |= all ? 1u << s : 4u | 1u << s;
-          }
-          return r;
+        auto pv = [&](int s, int v_slot) {
+          const uint32_t d = tmem0 + (2 + s) * kCATile, a = tmem0 + s * kCATile, v = ring_v + v_slot * kSlotLo;
+          wait(bar_pfull + 16 * s, p_par[s]);
+          tc_fence_after();
+          if (leader && ok) umma_pv4(d, a, v, started[s] ? 1u : 0u);
+          wait(bar_pfull + 16 * s + 8, p_par[s]);
+          p_par[s] ^= 1;
+          tc_fence_after();
+          if (leader && ok) umma_pv4(d, a + 32, v + 4 * ((16 * 128) >> 4), 1u);
+          started[s] = true;
         };
-        uint32_t before[2] = {0, 0};                 // of the latest two tiles
+        auto qk = [&](int s, int k_slot) {
+          if (leader && ok) {
+            umma_qk(tmem0 + s * kCATile, x.halves ? q_lo : q_lo + s * kSlotLo, ring_k + k_slot * kSlotLo);
+            umma_commit(bar_sfull + 8 * s);
+          }
+        };
+        // tiles k - 1 that both subtiles see all of, with a tile k behind them that both use: nothing to ask
+        const int plain_from = max(x.k0, kMask ? max(max(x.kf[0], x.kf[1]), x.kb[1]) : 0) + 1;
+        const int plain_to = x.halves ? x.k0 : min(min(min(x.kd[0], x.kd[1]) + 1, x.k1), min(x.ke[0], x.ke[1]));
+        uint32_t before[2] = {0, 0};                 // what the latest two tiles ask for: bits 0, 1: the subtiles that use it; 2: mending
+        auto asks = [&](int k) -> uint32_t {
+          return (x.active(0, k) ? 1u : 0u) | (x.active(1, k) ? 2u : 0u) | (x.mended(k) ? 4u : 0u);
+        };
         PRHS_CHUNK_STEPS(x, k) {
-          const bool pv = k - lag_ >= x.k0, qk = k < x.k1;
-          const uint32_t then = before[lag_ - 1], now = qk ? asks(k) : 0u;
+          if (!ok) break;
+          const RingPos vpos = pos;
+          if (k >= plain_from && k < plain_to && started[0] && started[1]) {
+            pos.step();
+            const RingPos kpos = pos;
+            pos.step();
+            wait(bar_full + 8 * vpos.slot, vpos.parity);
+            pv(0, vpos.slot);
+            wait(bar_full + 8 * kpos.slot, kpos.parity);
+            qk(0, kpos.slot);
+            pv(1, vpos.slot);
+            if (leader && ok) umma_commit(bar_empty + 8 * vpos.slot);
+            qk(1, kpos.slot);
+            if (leader && ok) {
+              umma_commit(bar_empty + 8 * kpos.slot);
+              if (k == x.k1 - 1) umma_commit(bar_qempty);
+            }
+            before[0] = asks(k);
+            continue;
+          }
+          const bool do_pv = k - lag_ >= x.k0, do_qk = k < x.k1;
+          const uint32_t then = do_pv ? before[lag_ - 1] : 0u, now = do_qk ? asks(k) : 0u;
           before[1] = before[0];
           before[0] = now;
-          const RingPos vpos = pos;
-          if (pv) {
+          if (do_pv) {
             pos.step();
             wait(bar_full + 8 * vpos.slot, vpos.parity);
             if (then & 4u) {
@@ -827,48 +873,36 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
           }
           const RingPos kpos = pos;
-          if (qk) pos.step();
+          if (do_qk) pos.step();
           bool k_here = false;
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
-            if (pv && (then >> s) & 1u) {
-              const uint32_t d = tmem0 + (2 + s) * kCATile, a = tmem0 + s * kCATile, vd = umma_desc_mn_lo(ring + vpos.slot * kCATileBytes);
-              wait(bar_pfull + 16 * s, p_par[s]);
+            if ((then >> s) & 1u) {
               if (!started[s]) {
                 wait(bar_oempty + 8 * s, oe_par[s]);
                 oe_par[s] ^= 1;
               }
-              tc_fence_after();
-              if (ok && leader) umma_pv4(d, a, vd, started[s] ? 1u : 0u);
-              wait(bar_pfull + 16 * s + 8, p_par[s]);
-              p_par[s] ^= 1;
-              tc_fence_after();
-              if (ok && leader) umma_pv4(d, a + 32, vd + 4 * ((16 * 128) >> 4), 1u);
-              started[s] = true;
+              pv(s, vpos.slot);
             }
-            if (s == 1 && pv && ok && leader) umma_commit(bar_empty + 8 * vpos.slot);
+            if (s == 1 && do_pv && leader && ok) umma_commit(bar_empty + 8 * vpos.slot);
             if ((now >> s) & 1u) {
               if (!k_here) wait(bar_full + 8 * kpos.slot, kpos.parity);
               k_here = true;
               tc_fence_after();
-              if (ok && leader) {
-                umma_qk(tmem0 + s * kCATile, umma_desc_lo(smem0 + (x.halves ? 0 : s) * kCATileBytes), umma_desc_lo(ring + kpos.slot * kCATileBytes));
-                umma_commit(bar_sfull + 8 * s);
-              }
+              qk(s, kpos.slot);
             }
           }
-          if (ok && leader) {
-            if (qk) umma_commit(bar_empty + 8 * kpos.slot);
+          if (leader && ok) {
+            if (do_qk) umma_commit(bar_empty + 8 * kpos.slot);
             if (k == x.k1 - 1) umma_commit(bar_qempty);
           }
-          if (!ok) break;
         }
         if (ok && leader) {
           if (started[0]) umma_commit(bar_ofull);
           if (started[1]) umma_commit(bar_ofull + 8);
         }
       }
-      if (!ok && lane == 0) gave_up();
+      if (!ok) gave_up();
       __syncwarp();
     } else {
       // ------------------------------------------------------------------------ mending warps
@@ -883,7 +917,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         PRHS_CHUNK_STEPS(x, k) {
           const int prev = k - lag_;
           if (prev >= x.k0) {
-            const bool mend = x.mended(p, prev);
+            const bool mend = x.mended(prev);
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh_abort));
             if (mend) {
               const int at = x.tile(prev) * kCATile;
