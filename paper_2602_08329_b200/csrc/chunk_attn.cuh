@@ -6,21 +6,24 @@
 // MMA.  A CTA works on an item, 2 T tokens of a sequence and one KV head, as two subtiles of T tokens with an
 // accumulator each, over tiles of 128 keys:
 //   producer warp   Q once per piece, then K and V tiles by TMA (128-byte swizzle) into a ring of five 32 KB slots
-//   MMA warp        one thread: S_s = Q_s K^T (128 x 128, fp32 in tensor memory), O_s += P_s V, P read from tensor memory
-//   8 softmax warps a thread owns a row: reads it (tcgen05.ld), weights 2^(x - m) in bf16 back over S (tcgen05.st), its sum in
-//                   fp32.  The two subtiles take turns: while the tensor core multiplies for one, the other's
-//                   weights are made
+//   MMA warp        S = Q K^T (128 x 128, fp32 in tensor memory) and O += P V for the subtiles in turn, P read from tensor memory
+//   8 softmax warps a thread owns a row of a subtile: reads it (tcgen05.ld), weights 2^(x - m) in bf16 back over S (tcgen05.st), their
+//                   sum in fp32.  While the tensor core multiplies for one subtile, the other's weights are made
 //   2 mending warps tiles that some row sees in part only: V rows behind the sequence become zero, and so do values that are not
 //                   finite (noted, and added at the end for the rows that do see them): a weight of zero times an infinity in
 //                   a masked place would be NaN
-// The reference exponent m of a row moves only when a logit exceeds it by 2^8 (a vote per warp); O is then rescaled in tensor memory by
-// the softmax warps themselves: S of the next tile is issued behind the product of the previous one, so O is at rest.
+// The weights are taken against the reference exponent m as it stands, so that they need not wait for the tile's maximum; one vote
+// of the warp, before anything is stored, finds logits beyond 2^60 of it, NaNs, masks and rows without a reference,
+// which go a slower way.  m moves where a logit has exceeded it by 2^8, before the next tile; O is then rescaled in tensor memory by
+// the softmax warps themselves.
 // An item of at most T tokens (drafts, short chunks) lets its two accumulators take the even and the odd tiles instead
 // (`halves`), and the stream of the cache is what bounds it.
 //
-// Work is dealt evenly whatever the lengths: the tiles of all items, laid end to end (sequence, KV head, tokens), are cut into as
-// many runs of equal length as there are CTAs (one per SM).  A piece of an item goes to a workspace as (m, l, O) in fp32; the
-// last CTA to arrive merges them (a ticket, no waiting).  A CTA has two pieces of that kind at most.
+// Work is dealt evenly whatever the lengths: the tiles of all items, laid end to end (sequence, KV head, tokens), are cut into
+// runs of equal length, and every CTA (one per SM) takes as many of them, one in each round.  A piece of an item goes to a workspace as
+// (m, l, O) in fp32; the last CTA to arrive merges them (a ticket, no waiting).  A run has two pieces of that kind at most.
+// Several rounds keep what is looked at at a time small: 2048 tokens at 131072, all in one round, read 70 % of their
+// tiles from DRAM.
 //
 // Weights enter the product as bf16, one rounding of 2^-8: as two bf16 (what the decode kernels do, bound by the stream) they would cost
 // half as many MMAs again, which is what bounds this kernel.  Sums, references, O and what is merged are fp32.
@@ -38,29 +41,39 @@ constexpr int kCATile = 128;                              // keys per tile, rows
 constexpr int kCAHalfBytes = kCATile * 128;               // [128 rows][64 columns] bf16
 constexpr int kCATileBytes = 2 * kCAHalfBytes;            // 32 KB
 constexpr int kCASlots = 5;
-constexpr int kCASmemBytes = (2 + kCASlots) * kCATileBytes + 1024;
+constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
+// What is shared beside the tiles (they leave 3 KB).
+struct ChunkShared {
+  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain
+  unsigned long long bars[3 * kCASlots + 13];
+  int mended_n[4], mended_tile[4][kCAMaxMended];
+  uint32_t tmem;
+  int abort, last;
+};
+constexpr int kCASmemBytes = (2 + kCASlots) * kCATileBytes + (int)sizeof(ChunkShared);
 constexpr int kCAThreads = 12 * 32;
 constexpr int kCAMmaWarp = 8, kCALoadWarp = 9, kCAMendWarp = 10;
 constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // a piece in the workspace: O [2][32][128] float4, (m, l) [2][128]
 constexpr uint32_t kCAIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCATile >> 3) << 17) | ((uint32_t)(kCATile >> 4) << 24);
 constexpr uint32_t kCAIdescPV = kCAIdesc | (1u << 16);    // B = V tile read MN-major
-constexpr float kCAGap = 8.f;
-constexpr int kCAPoly = 3, kCAPolyOf = 8;                 // of eight pairs of exponentials, three on the FMA pipe
+constexpr float kCAGap = 8.f, kCAFar = 60.f;
 // An item's Q, merge and output cost about as much as two tiles; a run of fewer than kCAMinRun tiles is not worth its merge.
 constexpr int kCAItemCost = 2;
 constexpr int kCAMinRun = 4;
-constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
+// What the CTAs work on at a time should stay in L2: a round for every 1024 tiles that are looked at (64 MB), of runs of at least 192.
+constexpr int kCARoundTiles = 1024, kCARoundRun = 192, kCAMaxRounds = 8;
 
 struct ChunkParams {
   KvDev kv;
   const int* row_start;
   __nv_bfloat16* out;
   float* out_lse;
-  float* partials;               // [2 gridDim.x][kCASlotFloats]
-  unsigned int* tickets;         // [gridDim.x], zero between launches
+  float* partials;               // [2 gridDim.x max_rounds][kCASlotFloats]
+  unsigned int* tickets;         // [gridDim.x max_rounds], zero between launches
   uint32_t* flags;
   double psaw_c;
   int num_rows, batch, num_q_heads, num_kv_heads, group, tokens;     // tokens = T
+  int max_rounds;
   int sinks, window, max_len;
   unsigned int oob_row;          // a row outside the K and V tensors: zeros
 };
@@ -76,7 +89,7 @@ template <bool kMask>
 struct Piece {
   int b, kvh, row0, ntok, u0;    // u0: visible length of the first token
   int k0, k1, st, lo;            // tile k is k for k < st, else lo + k - st
-  int first_cta, last_cta;       // CTAs that have pieces of the item
+  int run, first_run, last_run;  // this one, and those that have pieces of the item
   int t;
   bool halves;
   // Subtile s uses tile k if k < sa or kb <= k < ke, and every one of its rows sees all of it if k < sf or kf <= k < kd.  (The first
@@ -118,7 +131,7 @@ template <bool kMask>
 struct ChunkWalk {
   const ChunkParams& p;
   long long at = 0, end = 0, total = 0, item_at = 0;
-  int ctas = 0, b = 0, kvh = 0, i = 0, items = 0;
+  int ctas = 0, runs = 0, run = 0, b = 0, kvh = 0, i = 0, items = 0;
   SeqRows s;
 
   __device__ __forceinline__ explicit ChunkWalk(const ChunkParams& params) : p(params) {}
@@ -164,29 +177,49 @@ struct ChunkWalk {
     }
     return sum;
   }
-  // The CTA whose run holds place x.
-  __device__ __forceinline__ int cta_of(long long x) const { return (int)(((x + 1) * ctas - 1) / total); }
+  // The run that holds place x.
+  __device__ __forceinline__ int run_of(long long x) const { return (int)(((x + 1) * runs - 1) / total); }
 
-  // false: nothing for this CTA
+  // Warp-collective.  false: nothing for this CTA
   __device__ __forceinline__ bool begin() {
-    const int lane = threadIdx.x & 31;
-    long long mine0 = 0;          // of sequence `lane`
+    long long seen = 0;           // tiles that are looked at, each once
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      long long w = costs(b0);
-      if (b0 == 0) mine0 = w;
+      long long w = costs(b0), v = 0;
+      if (b0 + (int)(threadIdx.x & 31) < p.batch) {
+        const SeqRows q = seq(b0 + (threadIdx.x & 31));
+        if (q.n > 0) {
+          int st, lo, hi;
+          range(q, 0, &st, &lo, &hi);
+          v = st + (q.t + kCATile - 1) / kCATile - lo;
+        }
+      }
 #pragma unroll
-      for (int off = 16; off > 0; off >>= 1) w += __shfl_xor_sync(0xffffffffu, w, off);
+      for (int off = 16; off > 0; off >>= 1) {
+        w += __shfl_xor_sync(0xffffffffu, w, off);
+        v += __shfl_xor_sync(0xffffffffu, v, off);
+      }
       total += w;
+      seen += v;
     }
     total *= p.num_kv_heads;
+    seen *= p.num_kv_heads;
+    if (total == 0) return false;
     ctas = (int)min((long long)gridDim.x, max(1ll, total / kCAMinRun));
-    if (total == 0 || (int)blockIdx.x >= ctas) return false;
-    at = total * blockIdx.x / ctas;
-    end = total * (blockIdx.x + 1) / ctas;
+    const long long rounds = min(min((seen + kCARoundTiles - 1) / kCARoundTiles, total / ((long long)ctas * kCARoundRun)), (long long)p.max_rounds);
+    runs = ctas * (int)max(rounds, 1ll);
+    run = (int)blockIdx.x;
+    return run < ctas && seek();
+  }
+  // Warp-collective: to the beginning of run `run`.
+  __device__ __forceinline__ bool seek() {
+    const int lane = threadIdx.x & 31;
+    if (run >= runs) return false;
+    at = total * run / runs;
+    end = total * (run + 1) / runs;
     // the sequence
     long long before = 0, one = 0;
     for (int b0 = 0;; b0 += 32) {
-      const long long w = b0 == 0 ? mine0 : costs(b0);
+      const long long w = costs(b0);
       long long incl = w * p.num_kv_heads;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -227,8 +260,13 @@ struct ChunkWalk {
     }
     return true;
   }
+  // Warp-collective.
   __device__ __forceinline__ bool next(Piece<kMask>& x) {
-    if (at >= end) return false;
+    if (at >= end) {
+      run += ctas;
+      if (!seek()) return false;
+    }
+    x.run = run;
     if (i == items) {
       i = 0;
       if (++kvh == p.num_kv_heads) {
@@ -244,8 +282,8 @@ struct ChunkWalk {
     const long long to = min(item_at + w, end);
     x.k0 = max((int)(at - item_at) - kCAItemCost, 0);
     x.k1 = max((int)(to - item_at) - kCAItemCost, 0);
-    x.first_cta = cta_of(item_at);
-    x.last_cta = cta_of(item_at + w - 1);
+    x.first_run = run_of(item_at);
+    x.last_run = run_of(item_at + w - 1);
     x.b = b;
     x.kvh = kvh;
     x.row0 = s.r0 + i * 2 * p.tokens;
@@ -363,29 +401,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ uint64_t exp2_fast_x2(uint64_t t) {
-  float a, b;
-  unpack_f32x2(t, a, b);
-  return pack_f32x2(exp2_fast(a), exp2_fast(b));
-}
-// 2^t for two finite t <= 2^7 on the FMA pipe: t = n + f with n the nearest integer (found by adding 1.5 * 2^23) and 2^f, |f| <= 1/2, by the
-// polynomial of degree 4 of least relative error there (from a Remez exchange: 2.7e-6 at most, 4e-8 on average, where a weight
-// is rounded to 2^-8); n goes into the exponent.  Below 2^-125 the result stays there.
-__device__ __forceinline__ uint64_t exp2_poly_x2(uint64_t t) {
-  float a, b;
-  unpack_f32x2(t, a, b);
-  t = pack_f32x2(fmaxf(a, -125.f), fmaxf(b, -125.f));
-  const uint64_t y = add_f32x2(t, pack_f32x2(12582912.f, 12582912.f));
-  const uint64_t f = fma_f32x2(add_f32x2(y, pack_f32x2(-12582912.f, -12582912.f)), pack_f32x2(-1.f, -1.f), t);
-  uint64_t q = fma_f32x2(f, pack_f32x2(0.009570102207362652f, 0.009570102207362652f), pack_f32x2(0.05591785907745361f, 0.05591785907745361f));
-  q = fma_f32x2(q, f, pack_f32x2(0.240247443318367f, 0.240247443318367f));
-  q = fma_f32x2(q, f, pack_f32x2(0.6931217908859253f, 0.6931217908859253f));
-  q = fma_f32x2(q, f, pack_f32x2(0.9999992847442627f, 0.9999992847442627f));
-  float ya, yb;
-  unpack_f32x2(y, ya, yb);
-  unpack_f32x2(q, a, b);
-  return pack_f32x2(__uint_as_float(__float_as_uint(a) + (__float_as_uint(ya) << 23)), __uint_as_float(__float_as_uint(b) + (__float_as_uint(yb) << 23)));
-}
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // Ring position: slot and the parity of its fill.
@@ -409,54 +424,54 @@ template <bool kPaged, bool kMask>
 __global__ void __launch_bounds__(kCAThreads, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ ChunkParams p) {
-  extern __shared__ unsigned char ca_smem_raw[];
-  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain
-  __shared__ __align__(8) unsigned long long bars[3 * kCASlots + 13];
-  __shared__ int mended_n[4], mended_tile[4][kCAMaxMended];
-  __shared__ uint32_t tmem_slot;
-  __shared__ int sh_abort, sh_last;
+  extern __shared__ __align__(1024) unsigned char ca_smem[];
+  ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ca_smem + (2 + kCASlots) * kCATileBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0) record_bad_sequences(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, p.batch, p.flags);
   ChunkWalk<kMask> walk(p);
   if (!walk.begin()) return;
-  const uint32_t smem0 = ((uint32_t)__cvta_generic_to_shared(ca_smem_raw) + 1023u) & ~1023u;
+  const uint32_t smem0 = (uint32_t)__cvta_generic_to_shared(ca_smem);
+  if (smem0 & 1023u) {                  // (the swizzle asks for it, and there is no room to round up)
+    if (threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
+    return;
+  }
   const uint32_t ring = smem0 + 2 * kCATileBytes;
-  const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(bars);
+  const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(sh.bars);
   const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
   const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
   const uint32_t bar_ofull = bar_qfull + 64, bar_oempty = bar_qfull + 80, bar_drain = bar_qfull + 96;
   if (tid == 0) {
     for (int i = 0; i < kCASlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);      // the producer's expect_tx arrive
-      mbar_init(bar_empty + 8 * i, 3);     // a commit of the MMA thread, the two mending warps (which follow the ring fill by fill)
+      mbar_init(bar_empty + 8 * i, 3);     // a commit, the mending warps
       mbar_init(bar_vready + 8 * i, 2);    // the mending warps
     }
     mbar_init(bar_qfull, 1);
-    mbar_init(bar_qempty, 1);
+    mbar_init(bar_qempty, 1);              // a commit
     for (int i = 0; i < 2; ++i) {
-      mbar_init(bar_sfull + 8 * i, 1);     // a commit of the MMA thread
-      mbar_init(bar_pfull + 16 * i, 4);    // the subtile's softmax warps
+      mbar_init(bar_sfull + 8 * i, 1);     // a commit
+      mbar_init(bar_pfull + 16 * i, 4);    // the subtile's softmax warps, for each half of the columns
       mbar_init(bar_pfull + 16 * i + 8, 4);
-      mbar_init(bar_ofull + 8 * i, 1);     // a commit of the MMA thread
+      mbar_init(bar_ofull + 8 * i, 1);     // a commit
       mbar_init(bar_oempty + 8 * i, 4);    // the subtile's softmax warps
     }
     mbar_init(bar_drain, 1);
-    sh_abort = 0;
+    sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kCAMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"((uint32_t)__cvta_generic_to_shared(&tmem_slot)), "r"(512u) : "memory");
+                 ::"r"((uint32_t)__cvta_generic_to_shared(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem0 = *(volatile uint32_t*)&tmem_slot;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
+  const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
   Piece<kMask> x;
   auto gave_up = [&] {
     atomicOr(p.flags, kFlagTimeout);
-    sh_abort = 1;
+    sh.abort = 1;
   };
 
   if (warp < 8) {
@@ -477,27 +492,18 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const int from = kMask && used ? first_visible(p, u) : 0;
       const int kb = s ? x.kb[1] : x.kb[0], ke = x.halves ? x.k1 : min(x.k1, s ? x.ke[1] : x.ke[0]);
       const int kf = s ? x.kf[1] : x.kf[0], kd = s ? x.kd[1] : x.kd[0], sf = s ? x.sf[1] : x.sf[0];
-      float m = -INFINITY;
+      float m = -INFINITY, next = -INFINITY;         // the reference, and the one to go on with
       uint64_t l2 = 0ull;                            // two partial sums
       bool any = false;                              // O holds something
-      // a tile that some row sees in part: masks, and logits that are not finite
-      auto careful = [&](uint32_t (&r)[4][32], bool partly, int at) {
-        const int cu = u - at, cs = p.sinks - at, cf = from - at;
-        float mx = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 128; ++c) {
-          if (partly && !(c < cu && (!kMask || c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
-          mx = fmaxf(mx, __uint_as_float(r[c >> 5][c & 31]));            // (passes over NaNs)
-        }
-        return mx;
-      };
-      // the reference moves: what has been summed up so far is scaled down
+      bool ready = false, late = false;              // every row has a reference; one has fallen behind
+      // The reference moves: what has been summed up so far is scaled down.  (S of the present tile was issued behind the
+      // products of those before it, so O is at rest.)
       auto raise = [&](float mx) {
         const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
         l2 = fma_f32x2(l2, pack_f32x2(f, f), 0ull);
         m = mn;
         if (any) {
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < 8; ++c) {
             float o[16];
             tmem_ld16(tm_o + 16 * c, o);
@@ -511,7 +517,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       for (int k = x.halves ? x.k0 + s : x.k0; k < ke; k += step) {
         if (kMask && !x.halves && k >= x.sa && k < kb) continue;
         if (!aborted) {
-          aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh_abort));
+          aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh.abort));
           if (aborted && lane == 0) gave_up();
         }
         s_par ^= 1;
@@ -521,6 +527,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           uint32_t r[4][32];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld32(tm_s + 32 * c, r[c]);
+          if (late) {
+            raise(next);
+            late = false;
+          }
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
           const bool partly = !(kMask ? k < sf || (k >= kf && k < kd) : k < kd);
@@ -534,41 +544,44 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               for (int j = 1; j < 31; j += 2) y[c] = max3_nan(y[c], __uint_as_float(r[c][j]), __uint_as_float(r[c][j + 1]));
               y[c] = max3_nan(y[c], __uint_as_float(r[c][31]), __uint_as_float(r[c][31]));
             }
-            mx = max3_nan(max3_nan(y[0], y[1], y[2]), y[3], y[3]);
+            mx = max3_nan(max3_nan(y[0], y[1], y[2]), y[3], y[3]) * c1;
           }
-          const bool plain = __all_sync(0xffffffffu, !partly && fabsf(mx) < INFINITY);
-          if (!plain) mx = careful(r, partly, x.tile(k) * kCATile);
-          mx *= c1;
-          if (__any_sync(0xffffffffu, mx > m + kCAGap)) raise(mx);
+          // The weights are taken against the reference as it stands, so that they need not wait for the maximum; up to 2^60 they
+          // are as good as any, and the reference moves before the next tile.
+          const bool plain = ready && !partly && !__any_sync(0xffffffffu, used && !(mx - m <= kCAFar));
+          if (plain) {
+            next = mx;
+            late = __any_sync(0xffffffffu, used && mx > m + kCAGap);
+          } else {
+            // a tile that some row sees in part, logits that are not finite, no reference yet
+            const int at = x.tile(k) * kCATile, cu = u - at, cs = p.sinks - at, cf = from - at;
+            mx = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 128; ++c) {
+              if (partly && !(c < cu && (!kMask || c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
+              mx = fmaxf(mx, __uint_as_float(r[c >> 5][c & 31]));            // (passes over NaNs)
+            }
+            mx *= c1;
+            if (__any_sync(0xffffffffu, used && mx > m + kCAGap)) raise(mx);
+            ready = __all_sync(0xffffffffu, !used || m > -INFINITY);
+          }
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t cc = pack_f32x2(c1, c1), mm = pack_f32x2(-ref, -ref);
           uint64_t la = 0ull, lb = 0ull;
+          // the weights, over S, and on to the tensor core in two halves
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t w[32];
-            if (plain) {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                const int c = 64 * h + 2 * j;
-                const uint64_t t = fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm);
-                const uint64_t e = j % kCAPolyOf < kCAPoly ? exp2_poly_x2(t) : exp2_fast_x2(t);
-                if (j & 1) la = add_f32x2(la, e);
-                else lb = add_f32x2(lb, e);
-                float a, b;
-                unpack_f32x2(e, a, b);
-                w[j] = pack_bf16x2(a, b);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) {
-                const int c = 64 * h + 2 * j;
-                const uint64_t e = exp2_fast_x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm));
-                if (j & 1) la = add_f32x2(la, e);
-                else lb = add_f32x2(lb, e);
-                float a, b;
-                unpack_f32x2(e, a, b);
-                w[j] = pack_bf16x2(a, b);
-              }
+            for (int j = 0; j < 32; ++j) {
+              const int c = 64 * h + 2 * j;
+              float a, b;
+              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
+              else lb = add_f32x2(lb, pack_f32x2(a, b));
+              w[j] = pack_bf16x2(a, b);
             }
             tmem_st32(tm_s + 32 * h, w);
             tmem_wait_st();
@@ -588,15 +601,15 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const float l = la + lb;
       // ------------------------------------------------------------ the piece's result
       if (any && !aborted) {
-        aborted = !__all_sync(0xffffffffu, mbar_wait(bar_ofull + 8 * s, o_par, &sh_abort));
+        aborted = !__all_sync(0xffffffffu, mbar_wait(bar_ofull + 8 * s, o_par, &sh.abort));
         if (aborted && lane == 0) gave_up();
       }
       if (any) o_par ^= 1;
-      const bool whole = x.first_cta == x.last_cta && !x.halves;
-      const int slot = 2 * blockIdx.x + (x.first_cta == (int)blockIdx.x ? 1 : 0);
+      const bool whole = x.first_run == x.last_run && !x.halves;
+      const int slot = 2 * x.run + (x.first_run == x.run ? 1 : 0);
       float* const part = p.partials + (size_t)slot * kCASlotFloats;
       const long long out_row = ((long long)(x.row0 + x.a(p, s) + token) * p.num_q_heads + x.kvh * p.group + head);
-      const int mended = any ? mended_n[buf & 3] : 0;
+      const int mended = any ? sh.mended_n[buf & 3] : 0;
       if (!aborted && warp_used) {
         tc_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -613,7 +626,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           }
           // values that are not finite and were kept out of the product: infinite or NaN whatever their weight
           for (int y = 0; y < mended; ++y) {
-            const int at = mended_tile[buf & 3][y] * kCATile;
+            const int at = sh.mended_tile[buf & 3][y] * kCATile;
             for (int i = at; i < min(at + kCATile, u); ++i) {
               if (i >= p.sinks && i < from) continue;
               long long off = (long long)x.b * p.kv.stride_outer + (long long)i * kHeadDim;
@@ -665,26 +678,26 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         // ---------------------------------------------------------- the last piece of an item to arrive merges them
         __threadfence();
         softmax_bar();
-        const int parts = x.last_cta - x.first_cta + 1;
+        const int parts = x.last_run - x.first_run + 1;
         if (tid == 0) {
           bool last = true;
           if (parts > 1) {
-            last = atomicAdd(p.tickets + x.first_cta, 1u) == (unsigned)parts - 1u;
-            if (last) p.tickets[x.first_cta] = 0u;
+            last = atomicAdd(p.tickets + x.first_run, 1u) == (unsigned)parts - 1u;
+            if (last) p.tickets[x.first_run] = 0u;
           }
-          sh_last = last;
+          sh.last = last;
         }
         softmax_bar();
-        if (sh_last && !*(volatile int*)&sh_abort && used) {
+        if (sh.last && !*(volatile int*)&sh.abort && used) {
           __threadfence();
           // this thread's row: its subtile's pieces, 128 columns; with `halves` those of both, and half of the columns
           const int sub0 = x.halves ? 0 : s, sub1 = x.halves ? 1 : s, cols = x.halves ? 64 : 128;
-          auto base = [&](int c) { return p.partials + (size_t)(2 * c + (c == x.first_cta ? 1 : 0)) * kCASlotFloats; };
+          auto base = [&](int c) { return p.partials + (size_t)(2 * c + (c == x.first_run ? 1 : 0)) * kCASlotFloats; };
           auto ml = [&](int c, int y) { return __ldcg(reinterpret_cast<const float2*>(base(c) + 2 * kCATile * kHeadDim) + y * kCATile + row); };
           float M = -INFINITY, L = 0.f;
-          for (int c = x.first_cta; c <= x.last_cta; ++c)
+          for (int c = x.first_run; c <= x.last_run; ++c)
             for (int y = sub0; y <= sub1; ++y) M = fmaxf(M, ml(c, y).x);
-          for (int c = x.first_cta; c <= x.last_cta; ++c)
+          for (int c = x.first_run; c <= x.last_run; ++c)
             for (int y = sub0; y <= sub1; ++y) {
               const float2 v = ml(c, y);
               if (v.y != 0.f) L += v.y * exp2f(v.x - M);
@@ -696,7 +709,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             float acc[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) acc[j] = 0.f;
-            for (int c = x.first_cta; c <= x.last_cta; ++c)
+            for (int c = x.first_run; c <= x.last_run; ++c)
               for (int y = sub0; y <= sub1; ++y) {
                 const float2 v = ml(c, y);
                 if (v.y == 0.f) continue;
@@ -737,7 +750,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (x.k0 == x.k1) continue;
         if (lane == 0) {
           if (q_full) {
-            ok = mbar_wait(bar_qempty, q_par, &sh_abort);
+            ok = mbar_wait(bar_qempty, q_par, &sh.abort);
             q_par ^= 1;
           }
           if (ok) {
@@ -767,7 +780,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         uint32_t next_row = lookup(x.k0), rows[2] = {p.oob_row, p.oob_row};
         auto fill = [&](const CUtensorMap* tm, int k, uint32_t page_row) {
           if (lane == 0) {
-            if (ring_full) ok = mbar_wait(bar_empty + 8 * pos.slot, pos.parity ^ 1, &sh_abort);
+            if (ring_full) ok = mbar_wait(bar_empty + 8 * pos.slot, pos.parity ^ 1, &sh.abort);
             if (ok) mbar_expect_tx(bar_full + 8 * pos.slot, kCATileBytes);
           }
           ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -796,6 +809,70 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
       }
       if (!ok && lane == 0) gave_up();
+    } else if (warp >= kCAMendWarp) {
+      // ------------------------------------------------------------------------ mending warps (they follow the ring fill by fill)
+      const int t64 = tid - 32 * kCAMendWarp;
+      RingPos pos;
+      int buf = 0;
+      bool ok = true;
+      while (walk.next(x)) {         // (a warp that gave up goes on through the barriers of the other)
+        if (x.k0 == x.k1) continue;
+        if (t64 == 0) sh.mended_n[buf & 3] = 0;
+        asm volatile("bar.sync 2, 64;" ::: "memory");
+        PRHS_CHUNK_STEPS(x, k) {
+          const int prev = k - lag_;
+          if (prev >= x.k0) {
+            const bool mend = x.mended(prev);
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh.abort));
+            if (mend) {
+              const int at = x.tile(prev) * kCATile;
+              bool odd = false;
+              if (ok) {
+                const uint32_t base = ring + pos.slot * kCATileBytes;
+                for (int i = t64; i < kCATile * 16; i += 64) {
+                  const int r = (i >> 3) & 127;
+                  const uint32_t addr = base + (uint32_t)i * 16u;
+                  uint32_t w[4];
+                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+                  const bool gone = at + r >= x.t;
+                  bool change = gone;
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                    const uint32_t bad = gone ? 0xffffffffu : __vcmpgeu2(w[j] & 0x7fff7fffu, 0x7f807f80u);
+                    change |= bad != 0u;
+                    odd |= !gone && bad != 0u;
+                    w[j] &= ~bad;
+                  }
+                  if (change)
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              }
+              uint32_t any_odd;
+              asm volatile("{ .reg .pred a, b; setp.ne.u32 a, %1, 0; barrier.cta.red.or.pred b, 2, 64, a; selp.u32 %0, 1, 0, b; }"
+                           : "=r"(any_odd) : "r"((uint32_t)odd) : "memory");
+              if (any_odd && t64 == 0) {
+                const int n = sh.mended_n[buf & 3];
+                if (n < kCAMaxMended) {
+                  sh.mended_tile[buf & 3][n] = x.tile(prev);
+                  sh.mended_n[buf & 3] = n + 1;
+                }
+              }
+              __syncwarp();
+              if (ok && lane == 0) mbar_arrive(bar_vready + 8 * pos.slot);
+            }
+            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
+            pos.step();
+          }
+          if (k < x.k1) {
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh.abort));
+            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
+            pos.step();
+          }
+        }
+        ++buf;
+      }
+      if (!ok && lane == 0) gave_up();
     } else if (warp == kCAMmaWarp) {
       // ------------------------------------------------------------------------ MMA issue: one thread issues, the warp waits.
       // (The control flow is the whole warp's: operands of an MMA are uniform registers, and in code that a single lane has branched
@@ -808,7 +885,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       constexpr uint32_t kSlotLo = kCATileBytes >> 4;
       // (a wait that runs out leaves the later ones to return at once)
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (!mbar_try_wait(bar, parity) && !mbar_wait(bar, parity, &sh_abort)) ok = false;
+        if (!mbar_try_wait(bar, parity) && !mbar_wait(bar, parity, &sh.abort)) ok = false;
       };
       while (ok && walk.next(x)) {
         if (x.k0 == x.k1) continue;
@@ -904,75 +981,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       }
       if (!ok) gave_up();
       __syncwarp();
-    } else {
-      // ------------------------------------------------------------------------ mending warps
-      const int t64 = tid - 32 * kCAMendWarp;
-      RingPos pos;
-      int buf = 0;
-      bool ok = true;
-      while (walk.next(x)) {         // (a warp that gave up goes on through the barriers of the other)
-        if (x.k0 == x.k1) continue;
-        if (t64 == 0) mended_n[buf & 3] = 0;
-        asm volatile("bar.sync 2, 64;" ::: "memory");
-        PRHS_CHUNK_STEPS(x, k) {
-          const int prev = k - lag_;
-          if (prev >= x.k0) {
-            const bool mend = x.mended(prev);
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh_abort));
-            if (mend) {
-              const int at = x.tile(prev) * kCATile;
-              bool odd = false;
-              if (ok) {
-                const uint32_t base = ring + pos.slot * kCATileBytes;
-                for (int i = t64; i < kCATile * 16; i += 64) {
-                  const int r = (i >> 3) & 127;
-                  const uint32_t addr = base + (uint32_t)i * 16u;
-                  uint32_t w[4];
-                  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
-                  const bool gone = at + r >= x.t;
-                  bool change = gone;
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) {
-                    const uint32_t bad = gone ? 0xffffffffu : __vcmpgeu2(w[j] & 0x7fff7fffu, 0x7f807f80u);
-                    change |= bad != 0u;
-                    odd |= !gone && bad != 0u;
-                    w[j] &= ~bad;
-                  }
-                  if (change)
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              }
-              uint32_t any_odd;
-              asm volatile("{ .reg .pred a, b; setp.ne.u32 a, %1, 0; barrier.cta.red.or.pred b, 2, 64, a; selp.u32 %0, 1, 0, b; }"
-                           : "=r"(any_odd) : "r"((uint32_t)odd) : "memory");
-              if (any_odd && t64 == 0) {
-                const int n = mended_n[buf & 3];
-                if (n < kCAMaxMended) {
-                  mended_tile[buf & 3][n] = x.tile(prev);
-                  mended_n[buf & 3] = n + 1;
-                }
-              }
-              __syncwarp();
-              if (ok && lane == 0) mbar_arrive(bar_vready + 8 * pos.slot);
-            }
-            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
-            pos.step();
-          }
-          if (k < x.k1) {
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * pos.slot, pos.parity, &sh_abort));
-            if (ok && lane == 0) mbar_arrive(bar_empty + 8 * pos.slot);
-            pos.step();
-          }
-        }
-        ++buf;
-      }
-      if (!ok && lane == 0) gave_up();
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (sh_abort) {
+  if (sh.abort) {
     // copies and MMAs may still be in flight: bounded waits before shared and tensor memory go back
     if (tid == kCALoadWarp * 32) {
       for (int i = 0; i < kCASlots; ++i) {

@@ -20,6 +20,12 @@ cudaError_t chunk_set_attributes(bool* fits) {
   return cudaSuccess;
 }
 
+// Rounds that a cache of the context's largest size can ask for (see chunk_attn.cuh): the workspace has room for their pieces.
+int chunk_rounds(const prhs_config& cfg) {
+  const long long tiles = (long long)cfg.max_batch * cfg.num_kv_heads * ((cfg.max_context + kCATile - 1) / kCATile);
+  return (int)std::min<long long>(kCAMaxRounds, (tiles + kCARoundTiles - 1) / kCARoundTiles);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
@@ -91,6 +97,7 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
   p.row_start = row_start;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.out_lse = out_lse;
+  p.max_rounds = ctx->chunk_rounds;
   p.partials = ctx->chunk_part;
   p.tickets = ctx->chunk_tickets;
   p.flags = ctx->flags;

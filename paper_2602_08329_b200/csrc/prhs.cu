@@ -68,9 +68,10 @@ struct prhs_ctx {
   float* partials = nullptr;
   float* stream_part = nullptr;     // parts of units that two CTAs of the 8-bit dense attention share
   unsigned int* tickets = nullptr;
-  float* chunk_part = nullptr;      // pieces of items that CTAs of the chunk attention share, two per CTA
+  float* chunk_part = nullptr;      // pieces of items that runs of the chunk attention share, two per run
   unsigned int* chunk_tickets = nullptr;
   bool chunk_fits = false;
+  int chunk_rounds = 1;
   int* idx = nullptr;
   int* count = nullptr;
   uint32_t* flags = nullptr;
@@ -835,6 +836,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = cudaEventCreateWithFlags(&c->ev_fork, cudaEventDisableTiming);
   if (e == cudaSuccess) e = cudaEventCreateWithFlags(&c->ev_join, cudaEventDisableTiming);
   const size_t U = units_max(c), G = c->num_groups;
+  c->chunk_rounds = chunk_rounds(*cfg);
   if (e == cudaSuccess) e = dev_alloc(&c->scores, U * c->ld);
   if (e == cudaSuccess) e = dev_alloc(&c->part_ml, U * std::max(c->max_chunks, kMaxSplits));
   if (e == cudaSuccess) e = dev_alloc(&c->lse_full, U);
@@ -842,9 +844,9 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = dev_alloc(&c->partials, U * kMaxSplits * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->stream_part, (size_t)2 * k8MaxCtasPerSm * c->sm_count * c->gq * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->tickets, U);
-  if (e == cudaSuccess) e = dev_alloc(&c->chunk_part, (size_t)2 * c->sm_count * kCASlotFloats);
-  if (e == cudaSuccess) e = dev_alloc(&c->chunk_tickets, c->sm_count);
-  if (e == cudaSuccess) e = cudaMemset(c->chunk_tickets, 0, c->sm_count * sizeof(unsigned int));
+  if (e == cudaSuccess) e = dev_alloc(&c->chunk_part, (size_t)2 * c->chunk_rounds * c->sm_count * kCASlotFloats);
+  if (e == cudaSuccess) e = dev_alloc(&c->chunk_tickets, (size_t)c->chunk_rounds * c->sm_count);
+  if (e == cudaSuccess) e = cudaMemset(c->chunk_tickets, 0, (size_t)c->chunk_rounds * c->sm_count * sizeof(unsigned int));
   if (e == cudaSuccess) e = dev_alloc(&c->idx, U * c->idx_cap);
   if (e == cudaSuccess) e = dev_alloc(&c->count, U);
   if (e == cudaSuccess) e = dev_alloc(&c->flags, 1);
