@@ -825,6 +825,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
     e = cudaFuncSetAttribute(dense_attn_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kTSmemBytes);
   if (e == cudaSuccess) e = bytekv_set_attributes();
   if (e == cudaSuccess) e = block_set_attributes();
+  if (e == cudaSuccess) e = tokens_set_attributes();
   if (e == cudaSuccess) e = chunk_set_attributes(&c->chunk_fits);
   if (e == cudaSuccess) {
     int nb = 0;

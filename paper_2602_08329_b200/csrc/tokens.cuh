@@ -80,86 +80,157 @@ __device__ __forceinline__ float2 rotation(int pos, float inv_freq, float scale)
   return make_float2((quarter == 1 || quarter == 2 ? -cc : cc) * scale, (quarter & 2 ? -ss : ss) * scale);
 }
 
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[16], int at) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[at + 2 * i] = bf_lo(u[i]);
-    x[at + 2 * i + 1] = bf_hi(u[i]);
-  }
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
-__device__ __forceinline__ uint4 pack8(const float (&x)[16], int at) {
-  return make_uint4(pack_bf16x2(x[at], x[at + 1]), pack_bf16x2(x[at + 2], x[at + 3]), pack_bf16x2(x[at + 4], x[at + 5]),
-                    pack_bf16x2(x[at + 6], x[at + 7]));
+__device__ __forceinline__ void unpack_f32x2(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
-// Eight lanes hold a head: lane l its 16-byte chunks l and l + 8, values 8l .. 8l + 7 and 64 + 8l .. 64 + 8l + 7.  Normalises
-// and rotates it, every operation written out so that the kernels agree to the bit.  cs: the row's 64 (cosine, sine); stage: 128 floats for this head (kRotPartial only).  Warp-collective.
+// What a row's heads are rotated with: the 64 cosines and sines, or, where all 128 values turn in halves, for queries and for keys the
+// products of them and the weights:  y_u = x_u (c w_u) + x_v (-s w_v),  y_v = x_v (c w_v) + x_u (s w_u).
 template <int kRot>
-__device__ __forceinline__ void prepare_head(uint4& a, uint4& b, const PrepDev& p, const float* weight, const float2* cs, float* stage) {
+struct RowTurns {
+  float c[64], s[64];
+  __device__ __forceinline__ void set(int f, float2 cs, const PrepDev&) {
+    c[f] = cs.x;
+    s[f] = cs.y;
+  }
+};
+template <>
+struct RowTurns<kRotHalves> {
+  // [queries, keys][c w_u, -s w_v, c w_v, s w_u]: 64 of each, in the order in which eight lanes read them (lane l needs 8l .. 8l + 7), so
+  // that a read of all lanes is one wavefront: these were what bounded the kernel
+  float t[2][4][2][8][4];
+  __device__ __forceinline__ void set(int f, float2 cs, const PrepDev& p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float* w = i ? p.k_weight : p.q_weight;
+      const float wu = w ? __ldg(w + f) : 1.f, wv = w ? __ldg(w + f + 64) : 1.f;
+      t[i][0][(f >> 2) & 1][f >> 3][f & 3] = __fmul_rn(cs.x, wu);
+      t[i][1][(f >> 2) & 1][f >> 3][f & 3] = -__fmul_rn(cs.y, wv);
+      t[i][2][(f >> 2) & 1][f >> 3][f & 3] = __fmul_rn(cs.x, wv);
+      t[i][3][(f >> 2) & 1][f >> 3][f & 3] = __fmul_rn(cs.y, wu);
+    }
+  }
+};
+
+// Eight lanes hold a head: lane l its 16-byte chunks l and l + 8, values 8l .. 8l + 7 and 64 + 8l .. 64 + 8l + 7, two to a register pair.
+// Normalises and rotates it (kind: 0 a query, else a key), every operation written out so that the kernels agree to the bit.  The
+// norm's factor comes last where the rotation does not wait for it.  stage: 128 floats for this head (kRotPartial
+// only).  Warp-collective.
+template <int kRot>
+__device__ __forceinline__ void prepare_head(uint4& a, uint4& b, const PrepDev& p, int kind, const RowTurns<kRot>& turns, float* stage) {
   const int l = threadIdx.x & 7;
-  float x[16];
-  unpack8(a, x, 0);
-  unpack8(b, x, 8);
+  uint64_t x[8];
+  {
+    const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = pack_f32x2(bf_lo(u[i]), bf_hi(u[i]));
+  }
+  uint64_t rr = 0ull;
   if (p.norm) {
-    float ss = 0.f;
+    uint64_t q = 0ull;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+    for (int i = 0; i < 8; ++i) q = fma_f32x2(x[i], x[i], q);
+    float ss, t;
+    unpack_f32x2(q, ss, t);
+    ss = __fadd_rn(ss, t);
 #pragma unroll
-    for (int off = 1; off < 8; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+    for (int off = 1; off < 8; off <<= 1) ss = __fadd_rn(ss, __shfl_xor_sync(0xffffffffu, ss, off));
     const float r = rsqrtf(fmaf(ss, 1.f / kHeadDim, p.eps));
+    rr = pack_f32x2(r, r);
+  }
+  if constexpr (kRot == kRotHalves) {
+    const auto& t = turns.t[kind != 0];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= r;
+    for (int i = 0; i < 4; i += 2) {
+      uint64_t f[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 v = *reinterpret_cast<const float4*>(t[j][i >> 1][l]);
+        f[j][0] = pack_f32x2(v.x, v.y);
+        f[j][1] = pack_f32x2(v.z, v.w);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint64_t u = x[i + j], w = x[4 + i + j];
+        x[i + j] = fma_f32x2(u, f[0][j], mul_f32x2(w, f[1][j]));
+        x[4 + i + j] = fma_f32x2(w, f[2][j], mul_f32x2(u, f[3][j]));
+      }
+    }
+    if (p.norm) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = mul_f32x2(x[i], rr);
+    }
+  } else if (p.norm) {
+    const float* weight = kind ? p.k_weight : p.q_weight;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = mul_f32x2(x[i], rr);
     if (weight) {
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const float4 w = __ldg(reinterpret_cast<const float4*>(weight + 8 * l + (i < 8 ? i : 56 + i)));
-        x[i] *= w.x;
-        x[i + 1] *= w.y;
-        x[i + 2] *= w.z;
-        x[i + 3] *= w.w;
+      for (int i = 0; i < 4; ++i) {
+        const float4 w = __ldg(reinterpret_cast<const float4*>(weight + 8 * l + 4 * (i & 1) + 64 * (i >> 1)));
+        x[2 * i] = mul_f32x2(x[2 * i], pack_f32x2(w.x, w.y));
+        x[2 * i + 1] = mul_f32x2(x[2 * i + 1], pack_f32x2(w.z, w.w));
       }
     }
   }
-  if (kRot == kRotHalves) {
+  if constexpr (kRot == kRotAdjacent) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float2 t = cs[8 * l + i];
-      const float u = x[i], w = x[8 + i];
-      x[i] = fmaf(u, t.x, -__fmul_rn(w, t.y));
-      x[8 + i] = fmaf(w, t.x, __fmul_rn(u, t.y));
-    }
-  } else if (kRot == kRotAdjacent) {
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const int f = 4 * l + (i < 8 ? i / 2 : 28 + i / 2);
+      const int f = 4 * l + (i < 4 ? i : 28 + i);
       if (2 * f < p.rot) {
-        const float2 t = cs[f];
-        const float u = x[i], w = x[i + 1];
-        x[i] = fmaf(u, t.x, -__fmul_rn(w, t.y));
-        x[i + 1] = fmaf(w, t.x, __fmul_rn(u, t.y));
+        float u, w;
+        unpack_f32x2(x[i], u, w);
+        const float c = turns.c[f], n = turns.s[f];
+        x[i] = pack_f32x2(fmaf(u, c, -__fmul_rn(w, n)), fmaf(w, c, __fmul_rn(u, n)));
       }
     }
-  } else {
+  } else if constexpr (kRot == kRotPartial) {
+    float y[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) stage[8 * l + (i < 8 ? i : 56 + i)] = x[i];
+    for (int i = 0; i < 8; ++i) {
+      unpack_f32x2(x[i], y[2 * i], y[2 * i + 1]);
+      *reinterpret_cast<float2*>(stage + 8 * l + 2 * (i & 3) + 64 * (i >> 2)) = make_float2(y[2 * i], y[2 * i + 1]);
+    }
     __syncwarp();
     const int half = p.rot >> 1;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int d = 8 * l + (i < 8 ? i : 56 + i);
-      if (d < half) {
-        const float2 t = cs[d];
-        x[i] = fmaf(x[i], t.x, -__fmul_rn(stage[d + half], t.y));
-      } else if (d < p.rot) {
-        const float2 t = cs[d - half];
-        x[i] = fmaf(x[i], t.x, __fmul_rn(stage[d - half], t.y));
-      }
+      const int d = 8 * l + (i & 7) + 64 * (i >> 3);
+      if (d < half) y[i] = fmaf(y[i], turns.c[d], -__fmul_rn(stage[d + half], turns.s[d]));
+      else if (d < p.rot) y[i] = fmaf(y[i], turns.c[d - half], __fmul_rn(stage[d - half], turns.s[d - half]));
     }
     __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = pack_f32x2(y[2 * i], y[2 * i + 1]);
   }
-  a = pack8(x, 0);
-  b = pack8(x, 8);
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float u, w;
+    unpack_f32x2(x[i], u, w);
+    o[i] = pack_bf16x2(u, w);
+  }
+  a = make_uint4(o[0], o[1], o[2], o[3]);
+  b = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
 // -------------------------------------------------------------------------------- into the bf16 cache
@@ -169,79 +240,129 @@ struct QkvAppendParams {
   KvDev kv;
   __nv_bfloat16* q_out;
   int max_len;
-  int chunks, chunk_heads;        // a row's heads (queries, keys, values in this order) in chunks of chunk_heads, a multiple of 8
+  int cta_rows;                   // rows per CTA, at most kQkvRows
   uint32_t* flags;
 };
-constexpr int kQkvWarps = 4;
+constexpr int kQkvWarps = 8, kQkvRows = 8, kQkvStages = 2;
+constexpr int kQkvMaxHeads = 512;                 // (the table of heads: 16 KB)
 
-// A warp takes a chunk of a row's heads, eight at a time (four per step of the lanes, two steps in flight).
+// Where a head (queries, keys, values in this order) is read and written: bytes to add are row * src_stride and the row's offset among
+// queries or in the cache.
+struct HeadPlace {
+  const char* src;
+  long long src_stride;
+  char* dst;
+  int kind;                       // 0 query, 1 key, 2 value
+};
+
+// A CTA takes cta_rows rows, and every gridDim.y-th of their groups of four heads: the places of heads and rows, and the rows' angles are
+// looked up and computed by all threads once, then the heads stream through, a group per warp and step, the next two on their way
+// (from before the look-ups).
 template <int kRot>
-__global__ void __launch_bounds__(32 * kQkvWarps) qkv_append_kernel(const __grid_constant__ QkvAppendParams p) {
-  __shared__ float2 sm_cs[kQkvWarps][64];
+__global__ void __launch_bounds__(32 * kQkvWarps, 3) qkv_append_kernel(const __grid_constant__ QkvAppendParams p) {
+  extern __shared__ uint4 qkv_smem[];
+  HeadPlace* const sm_heads = reinterpret_cast<HeadPlace*>(qkv_smem);
+  __shared__ __align__(16) RowTurns<kRot> sm_turns[kQkvRows];
   __shared__ float sm_stage[kRot == kRotPartial ? kQkvWarps : 1][kRot == kRotPartial ? 4 * kHeadDim : 1];
+  __shared__ long long sm_off[kQkvRows][2];       // bytes: of the row's queries in q_out, of the token in the cache; -1: not written
+  __shared__ int sm_pos[kQkvRows];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 7;
-  if (blockIdx.x == 0) record_bad_sequences(p.rows.row_start, p.rows.num_rows, p.kv.seq_lens, p.max_len, p.rows.batch, p.flags);
-  const long long unit = (long long)blockIdx.x * kQkvWarps + warp;
-  const int r = (int)(unit / p.chunks), h0 = (int)(unit % p.chunks) * p.chunk_heads;
-  if (r >= p.rows.num_rows) return;
-  const int nq = p.rows.num_q_heads, nkv = p.rows.num_kv_heads, heads = nq + 2 * nkv, h1 = min(h0 + p.chunk_heads, heads);
   const TokenRowsDev& in = p.rows;
-  // where head h of this row is read
-  auto source = [&](int h) {
-    if (h < nq) return in.q + (long long)r * in.q_row + (long long)h * in.q_head;
-    if (h < nq + nkv) return in.k + (long long)r * in.k_row + (long long)(h - nq) * in.k_head;
-    return in.v + (long long)r * in.v_row + (long long)(h - nq - nkv) * in.v_head;
-  };
-  uint4 a[2], b[2];
-  auto load = [&](int h) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const __nv_bfloat16* s = source(min(h + 4 * i + (lane >> 3), h1 - 1)) + 8 * l;
-      a[i] = *reinterpret_cast<const uint4*>(s);
-      b[i] = *reinterpret_cast<const uint4*>(s + 64);
+  const int nq = in.num_q_heads, nkv = in.num_kv_heads, heads = nq + 2 * nkv, groups = (heads + 3) >> 2;
+  const int r0 = blockIdx.x * p.cta_rows, rows = min(p.cta_rows, in.num_rows - r0);
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    record_bad_sequences(in.row_start, in.num_rows, p.kv.seq_lens, p.max_len, in.batch, p.flags);
+  for (int h = threadIdx.x; h < heads; h += 32 * kQkvWarps) {
+    HeadPlace x;
+    if (h < nq) x = {(const char*)(in.q + r0 * in.q_row + h * in.q_head), 2 * in.q_row, (char*)(p.q_out + (long long)h * kHeadDim), 0};
+    else if (h < nq + nkv)
+      x = {(const char*)(in.k + r0 * in.k_row + (h - nq) * in.k_head), 2 * in.k_row, (char*)(p.kv.k + (h - nq) * p.kv.stride_head), 1};
+    else x = {(const char*)(in.v + r0 * in.v_row + (h - nq - nkv) * in.v_head), 2 * in.v_row, (char*)(p.kv.v + (h - nq - nkv) * p.kv.stride_head), 2};
+    sm_heads[h] = x;
+  }
+  __syncthreads();
+  // this warp's steps: every `stride`-th of the rows' groups, as (row, group) without a division
+  const int stride = gridDim.y * kQkvWarps, first = blockIdx.y * kQkvWarps + warp;
+  const int by_row = stride / groups, by_group = stride - by_row * groups;
+  int lrow = first / groups, lgroup = first - lrow * groups;       // the next to be loaded
+  uint4 a[kQkvStages], b[kQkvStages];
+  auto load = [&](int i) {
+    if (lrow >= rows) return;
+    const HeadPlace& x = sm_heads[min(4 * lgroup + (lane >> 3), heads - 1)];
+    const char* from = x.src + lrow * x.src_stride + 16 * l;
+    a[i] = *reinterpret_cast<const uint4*>(from);
+    b[i] = *reinterpret_cast<const uint4*>(from + 128);
+    lrow += by_row;
+    lgroup += by_group;
+    if (lgroup >= groups) {
+      lgroup -= groups;
+      ++lrow;
     }
   };
-  load(h0);
-  const int seq = in.row_start ? last_start(in.row_start, in.batch, r) : r;
-  if (seq < 0) return;
-  const SeqRows s = seq_rows(in.row_start, in.num_rows, p.kv.seq_lens, p.max_len, seq);
-  if (!s.ok || r >= s.r0 + s.n) return;
-  const int pos = s.t - s.n + (r - s.r0);
-  for (int f = lane; 2 * f < p.prep.rot; f += 32) {
-    const int at = in.positions ? __ldg(in.positions + p.prep.axis_of[f] * in.positions_stride + r) : pos;
-    sm_cs[warp][f] = rotation(at, __ldg(p.prep.inv_freq + f), p.prep.rot_scale);
-  }
-  long long row = (long long)seq * p.kv.stride_outer + (long long)pos * kHeadDim;
-  bool page_ok = true;
-  if (p.kv.page_table) {
-    const int page = __ldg(p.kv.page_table + (long long)seq * p.kv.page_table_stride + (pos >> kPageShift));
-    page_ok = (unsigned)page < (unsigned)p.kv.num_pages;
-    if (!page_ok && lane == 0) atomicOr(p.flags, kFlagBadPage);
-    row = (long long)page * p.kv.stride_outer + (pos & 15) * kHeadDim;
-  }
-  __syncwarp();
-  for (int h = h0; h < h1; h += 8) {
-    uint4 ca[2] = {a[0], a[1]}, cb[2] = {b[0], b[1]};
-    if (h + 8 < h1) load(h + 8);
+  int row = lrow, group = lgroup;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int hh = h + 4 * i + (lane >> 3);
-      const bool is_v = hh >= nq + nkv;
-      if (!__all_sync(0xffffffffu, is_v || hh >= h1)) {
-        uint4 xa = ca[i], xb = cb[i];
-        prepare_head<kRot>(xa, xb, p.prep, hh < nq ? p.prep.q_weight : p.prep.k_weight, sm_cs[warp],
-                           sm_stage[kRot == kRotPartial ? warp : 0] + (kRot == kRotPartial ? (lane >> 3) * kHeadDim : 0));
-        if (!is_v) {
-          ca[i] = xa;
-          cb[i] = xb;
+  for (int i = 0; i < kQkvStages; ++i) load(i);
+  for (int i = warp; i < rows; i += kQkvWarps) {
+    const int r = r0 + i, seq = in.row_start ? last_start(in.row_start, in.batch, r) : r;
+    long long off_q = -1, off_kv = -1;
+    int pos = 0;
+    if (seq >= 0) {
+      const SeqRows s = seq_rows(in.row_start, in.num_rows, p.kv.seq_lens, p.max_len, seq);
+      if (s.ok && r < s.r0 + s.n) {
+        pos = s.t - s.n + (r - s.r0);
+        off_q = (long long)r * nq * kRowBytes;
+        off_kv = 2 * ((long long)seq * p.kv.stride_outer + (long long)pos * kHeadDim);
+        if (p.kv.page_table) {
+          const int page = __ldg(p.kv.page_table + (long long)seq * p.kv.page_table_stride + (pos >> kPageShift));
+          off_kv = 2 * ((long long)page * p.kv.stride_outer + (pos & 15) * kHeadDim);
+          if ((unsigned)page >= (unsigned)p.kv.num_pages) {
+            off_kv = -1;
+            if (lane == 0) atomicOr(p.flags, kFlagBadPage);
+          }
         }
       }
-      if (hh < h1 && (hh < nq || page_ok)) {
-        __nv_bfloat16* to = hh < nq ? p.q_out + ((long long)r * nq + hh) * kHeadDim
-                                    : const_cast<__nv_bfloat16*>(is_v ? p.kv.v : p.kv.k) + row +
-                                          (long long)(is_v ? hh - nq - nkv : hh - nq) * p.kv.stride_head;
-        *reinterpret_cast<uint4*>(to + 8 * l) = ca[i];
-        *reinterpret_cast<uint4*>(to + 64 + 8 * l) = cb[i];
+    }
+    if (lane == 0) {
+      sm_off[i][0] = off_q;
+      sm_off[i][1] = off_kv;
+    }
+#pragma unroll
+    for (int f = lane; f < 64; f += 32)
+      if (2 * f < p.prep.rot) {
+        const int at = in.positions ? __ldg(in.positions + p.prep.axis_of[f] * in.positions_stride + r) : pos;
+        sm_turns[i].set(f, rotation(at, __ldg(p.prep.inv_freq + f), p.prep.rot_scale), p.prep);
+      }
+  }
+  __syncthreads();
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < kQkvStages; ++i) {
+      if (row >= rows) return;
+      uint4 xa = a[i], xb = b[i];
+      load(i);
+      const int h = 4 * group + (lane >> 3);
+      const HeadPlace& x = sm_heads[min(h, heads - 1)];
+      const int kind = x.kind;
+      if (!__all_sync(0xffffffffu, kind == 2)) {
+        uint4 ya = xa, yb = xb;
+        prepare_head<kRot>(ya, yb, p.prep, kind, sm_turns[row],
+                           sm_stage[kRot == kRotPartial ? warp : 0] + (kRot == kRotPartial ? (lane >> 3) * kHeadDim : 0));
+        if (kind != 2) {
+          xa = ya;
+          xb = yb;
+        }
+      }
+      const long long off = sm_off[row][kind != 0];
+      if (h < heads && off >= 0) {
+        char* to = x.dst + off + 16 * l;
+        *reinterpret_cast<uint4*>(to) = xa;
+        *reinterpret_cast<uint4*>(to + 128) = xb;
+      }
+      row += by_row;
+      group += by_group;
+      if (group >= groups) {
+        group -= groups;
+        ++row;
       }
     }
   }
@@ -257,6 +378,8 @@ struct ByteKvQkvParams {
   uint32_t* flags;
 };
 constexpr int kQkv8Warps = 8;
+template <int kRot>
+constexpr int kQkv8SmemBytes = kQkv8Warps * kBlockRows * 16 * 16 + kBlockRows * (int)sizeof(RowTurns<kRot>);
 
 // Blocks of 16 positions that a sequence's new tokens touch.
 __device__ __forceinline__ int touched_blocks(const SeqRows& s) {
@@ -268,9 +391,11 @@ __device__ __forceinline__ int touched_blocks(const SeqRows& s) {
 // tail where a later block stays open: it alone reads the old tail, a warp does the same heads both times, and a thread reads
 // and writes the same 16-byte pieces, so program order keeps the two apart.
 template <int kFmt, int kRot>
-__global__ void __launch_bounds__(32 * kQkv8Warps) bytekv_qkv_append_kernel(const __grid_constant__ ByteKvQkvParams p) {
-  __shared__ float2 sm_cs[kBlockRows][64];
-  __shared__ uint4 sm_rows[kQkv8Warps][kBlockRows * 16];       // a block's prepared keys on their way to quantise_block's order
+__global__ void __launch_bounds__(32 * kQkv8Warps, 2) bytekv_qkv_append_kernel(const __grid_constant__ ByteKvQkvParams p) {
+  extern __shared__ uint4 sm_dyn[];
+  RowTurns<kRot>* const sm_turns = reinterpret_cast<RowTurns<kRot>*>(sm_dyn);
+  uint4 (*const sm_rows)[kBlockRows * 16] = reinterpret_cast<uint4 (*)[kBlockRows * 16]>(sm_dyn + kBlockRows * sizeof(RowTurns<kRot>) / 16);     // a block's prepared keys on their way to quantise_block's order
+  __shared__ float sm_stage[kRot == kRotPartial ? kQkv8Warps : 1][kRot == kRotPartial ? 4 * kHeadDim : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 7;
   const TokenRowsDev& in = p.rows;
   if (blockIdx.x == 0 && blockIdx.y == 0) record_bad_sequences(in.row_start, in.num_rows, p.kv.seq_lens, p.max_len, in.batch, p.flags);
@@ -303,10 +428,10 @@ __global__ void __launch_bounds__(32 * kQkv8Warps) bytekv_qkv_append_kernel(cons
       const int pos = which * kBlockRows + (i >> 6), f = i & 63;
       if (pos < start || pos >= s.t || 2 * f >= p.prep.rot) continue;
       const int at = in.positions ? __ldg(in.positions + p.prep.axis_of[f] * in.positions_stride + s.r0 + pos - start) : pos;
-      sm_cs[i >> 6][f] = rotation(at, __ldg(p.prep.inv_freq + f), p.prep.rot_scale);
+      sm_turns[i >> 6].set(f, rotation(at, __ldg(p.prep.inv_freq + f), p.prep.rot_scale), p.prep);
     }
   };
-  float* const stage = reinterpret_cast<float*>(sm_rows[warp]) + (lane >> 3) * kHeadDim;     // (before the rows are put there)
+  float* const stage = sm_stage[kRot == kRotPartial ? warp : 0] + (kRot == kRotPartial ? (lane >> 3) * kHeadDim : 0);
   // head h of keys (or values) of a block's new tokens, in quantise_block's order: lane holds 16-byte piece lane % 16 of rows 2i + lane / 16
   auto fetch = [&](int which, int h, bool is_v, uint4 (&x)[8]) {
     const __nv_bfloat16* src = is_v ? in.v + (long long)h * in.v_head : in.k + (long long)h * in.k_head;
@@ -319,23 +444,23 @@ __global__ void __launch_bounds__(32 * kQkv8Warps) bytekv_qkv_append_kernel(cons
       }
       return;
     }
-    uint4 a[4], b[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    // four rows at a time, the next four on their way
+    uint4 a, b;
+    auto load = [&](int i) {
       const int pos = which * kBlockRows + 4 * i + (lane >> 3);
       const __nv_bfloat16* from = src + (s.r0 + min(max(pos, start), s.t - 1) - start) * by + 8 * l;
-      a[i] = *reinterpret_cast<const uint4*>(from);
-      b[i] = *reinterpret_cast<const uint4*>(from + 64);
-    }
+      a = *reinterpret_cast<const uint4*>(from);
+      b = *reinterpret_cast<const uint4*>(from + 64);
+    };
+    load(0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int pos = which * kBlockRows + 4 * i + (lane >> 3);
-      prepare_head<kRot>(a[i], b[i], p.prep, p.prep.k_weight, sm_cs[min(max(pos, start), s.t - 1) & (kBlockRows - 1)], stage);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sm_rows[warp][(4 * i + (lane >> 3)) * 16 + l] = a[i];
-      sm_rows[warp][(4 * i + (lane >> 3)) * 16 + 8 + l] = b[i];
+      const int row = 4 * i + (lane >> 3), pos = which * kBlockRows + row;
+      uint4 ya = a, yb = b;
+      if (i < 3) load(i + 1);
+      prepare_head<kRot>(ya, yb, p.prep, 1, sm_turns[min(max(pos, start), s.t - 1) & (kBlockRows - 1)], stage);
+      sm_rows[warp][row * 16 + l] = ya;
+      sm_rows[warp][row * 16 + 8 + l] = yb;
     }
     __syncwarp();
 #pragma unroll
@@ -369,16 +494,32 @@ __global__ void __launch_bounds__(32 * kQkv8Warps) bytekv_qkv_append_kernel(cons
   // queries: four heads of a row at a time
   {
     const int first = max(start, blk * kBlockRows), n = min(s.t, (blk + 1) * kBlockRows) - first, quads = (nq + 3) / 4;
-    for (int task = blockIdx.y * kQkv8Warps + warp; task < n * quads; task += gridDim.y * kQkv8Warps) {
-      const int pos = first + task / quads, h = task % quads * 4 + (lane >> 3), hh = min(h, nq - 1);
-      const long long r = s.r0 + pos - start;
-      const __nv_bfloat16* from = in.q + r * in.q_row + (long long)hh * in.q_head + 8 * l;
-      uint4 a = *reinterpret_cast<const uint4*>(from), b = *reinterpret_cast<const uint4*>(from + 64);
-      prepare_head<kRot>(a, b, p.prep, p.prep.q_weight, sm_cs[pos & (kBlockRows - 1)], stage);
-      if (h < nq) {
-        __nv_bfloat16* to = p.q_out + (r * nq + h) * kHeadDim + 8 * l;
-        *reinterpret_cast<uint4*>(to) = a;
-        *reinterpret_cast<uint4*>(to + 64) = b;
+    const int by = gridDim.y * kQkv8Warps;
+    uint4 a[2], b[2];
+    auto load = [&](int task, int i) {
+      if (task >= n * quads) return;
+      const int row = task / quads, hh = min((task - row * quads) * 4 + (lane >> 3), nq - 1);
+      const __nv_bfloat16* from = in.q + (s.r0 + first + row - start) * in.q_row + (long long)hh * in.q_head + 8 * l;
+      a[i] = *reinterpret_cast<const uint4*>(from);
+      b[i] = *reinterpret_cast<const uint4*>(from + 64);
+    };
+    const int task0 = blockIdx.y * kQkv8Warps + warp;
+    load(task0, 0);
+    load(task0 + by, 1);
+    for (int task1 = task0; task1 < n * quads; task1 += 2 * by) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int task = task1 + i * by;
+        if (task >= n * quads) break;
+        uint4 xa = a[i], xb = b[i];
+        load(task + 2 * by, i);
+        const int row = task / quads, h = (task - row * quads) * 4 + (lane >> 3), pos = first + row;
+        prepare_head<kRot>(xa, xb, p.prep, 0, sm_turns[pos & (kBlockRows - 1)], stage);
+        if (h < nq) {
+          __nv_bfloat16* to = p.q_out + ((long long)(s.r0 + pos - start) * nq + h) * kHeadDim + 8 * l;
+          *reinterpret_cast<uint4*>(to) = xa;
+          *reinterpret_cast<uint4*>(to + 64) = xb;
+        }
       }
     }
   }
@@ -427,7 +568,7 @@ struct ByteKvReadParams {
   uint32_t* flags;
 };
 
-// A warp per block of 16 positions and keys or values (grid: pairs of warps along x, KV heads, sequences): eight lanes a row, 16 codes each.
+// A warp per block of 16 positions and keys or values (grid: pairs of warps along x, KV heads, sequences): half a warp a row.
 // Bound by HBM: 128 B in (and 8 B / 16) and 256 B out per row.
 template <int kFmt>
 __global__ void __launch_bounds__(256) bytekv_read_kernel(const __grid_constant__ ByteKvReadParams p) {
@@ -470,26 +611,22 @@ __global__ void __launch_bounds__(256) bytekv_read_kernel(const __grid_constant_
       scale += (long long)b * p.kv.scale_stride_outer + blk;
     }
     if (page_ok) {
-      uint4 c[4];
+      // half a warp a row, 8 codes (16 bytes of bf16) a lane: stores fill whole sectors
+      uint2 c[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = __ldg(reinterpret_cast<const uint4*>(codes + (4 * i + (lane >> 3)) * kRow8Bytes + 16 * (lane & 7)));
+      for (int i = 0; i < 8; ++i) c[i] = __ldg(reinterpret_cast<const uint2*>(codes + (2 * i + (lane >> 4)) * kRow8Bytes + 8 * (lane & 15)));
       const float z = __ldg(scale);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 4 * i + (lane >> 3), pos = blk * kBlockRows + row;
-        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-        uint32_t o[8];
+      for (int i = 0; i < 8; ++i) {
+        const int row = 2 * i + (lane >> 4), pos = blk * kBlockRows + row;
+        uint32_t o[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const __half2_raw raw = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[k >> 1] >> (16 * (k & 1))), kFmt == kE4M3 ? __NV_E4M3 : __NV_E5M2);
-          const float2 x = __half22float2(__half2(raw));
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t w = (k < 2 ? c[i].x : c[i].y) >> (16 * (k & 1));
+          const float2 x = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, kFmt == kE4M3 ? __NV_E4M3 : __NV_E5M2)));
           o[k] = pack_bf16x2(x.x * z, x.y * z);
         }
-        if (pos >= first && pos < t) {
-          __nv_bfloat16* at = to + row * kHeadDim + 16 * (lane & 7);
-          *reinterpret_cast<uint4*>(at) = make_uint4(o[0], o[1], o[2], o[3]);
-          *reinterpret_cast<uint4*>(at + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-        }
+        if (pos >= first && pos < t) *reinterpret_cast<uint4*>(to + row * kHeadDim + 8 * (lane & 15)) = make_uint4(o[0], o[1], o[2], o[3]);
       }
     }
   }

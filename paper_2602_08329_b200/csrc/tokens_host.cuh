@@ -68,6 +68,26 @@ prhs_status check_tokens(prhs_ctx* c, const prhs_token_rows* rows, const prhs_qk
   return PRHS_OK;
 }
 
+cudaError_t tokens_set_attributes() {
+  const struct { const void* kernel; int bytes; } all[] = {
+      {(const void*)bytekv_qkv_append_kernel<kE4M3, kRotHalves>, kQkv8SmemBytes<kRotHalves>},
+      {(const void*)bytekv_qkv_append_kernel<kE4M3, kRotAdjacent>, kQkv8SmemBytes<kRotAdjacent>},
+      {(const void*)bytekv_qkv_append_kernel<kE4M3, kRotPartial>, kQkv8SmemBytes<kRotPartial>},
+      {(const void*)bytekv_qkv_append_kernel<kE5M2, kRotHalves>, kQkv8SmemBytes<kRotHalves>},
+      {(const void*)bytekv_qkv_append_kernel<kE5M2, kRotAdjacent>, kQkv8SmemBytes<kRotAdjacent>},
+      {(const void*)bytekv_qkv_append_kernel<kE5M2, kRotPartial>, kQkv8SmemBytes<kRotPartial>}};
+  for (const auto& k : all) {
+    const cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes);
+    if (e != cudaSuccess) return e;
+  }
+  // more than the 48 KB that every kernel may use
+  for (const void* k : {(const void*)qkv_append_kernel<kRotHalves>, (const void*)qkv_append_kernel<kRotAdjacent>, (const void*)qkv_append_kernel<kRotPartial>}) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kQkvMaxHeads * (int)sizeof(HeadPlace));
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 int rot_kind(const prhs_qk_prep* prep) {
   if (prep->rot_dim == 0 || (prep->flags & PRHS_PREP_ADJACENT)) return kRotAdjacent;
   return prep->rot_dim == kHeadDim ? kRotHalves : kRotPartial;
@@ -98,17 +118,17 @@ prhs_status prhs_qkv_append(prhs_ctx* ctx, const prhs_token_rows* rows, const pr
   p.q_out = static_cast<__nv_bfloat16*>(q_out);
   p.max_len = max_t;
   p.flags = ctx->flags;
-  // whole rows per warp, so that angles are computed once, unless that leaves the GPU's warps without work
-  const int heads = ctx->cfg.num_q_heads + 2 * ctx->cfg.num_kv_heads;
-  const int fill = std::max(1, ctx->sm_count * 24 / std::max(1, rows->num_rows));
-  p.chunk_heads = (std::max(8, (heads + fill - 1) / fill) + 7) & ~7;
-  p.chunks = (heads + p.chunk_heads - 1) / p.chunk_heads;
-  const long long ctas = ((long long)rows->num_rows * p.chunks + kQkvWarps - 1) / kQkvWarps;
-  if (ctas > 0x7fffffffll) return fail(ctx, PRHS_ERR_UNSUPPORTED, "new tokens: too many rows in one call");
+  // eight rows to a CTA, so that what it looks up first is little beside what it moves; fewer, and their heads over several CTAs,
+  // where that leaves SMs without work
+  const int heads = ctx->cfg.num_q_heads + 2 * ctx->cfg.num_kv_heads, groups = (heads + 3) / 4, want = 3 * ctx->sm_count;
+  if (heads > kQkvMaxHeads) return fail(ctx, PRHS_ERR_UNSUPPORTED, "new tokens: more than 512 heads of queries, keys and values");
+  p.cta_rows = std::max(1, std::min(kQkvRows, rows->num_rows / want));
+  const int ctas = (rows->num_rows + p.cta_rows - 1) / p.cta_rows;
+  const dim3 grid(ctas, std::max(1, std::min({want / ctas, (p.cta_rows * groups + kQkvWarps - 1) / kQkvWarps, 65535})));
   cudaStream_t st = as_stream(stream);
   {
     LaunchScope ls(ctx, PRHS_KIND_MISC, st);
-    auto launch = [&](auto kernel) { kernel<<<(unsigned)ctas, 32 * kQkvWarps, 0, st>>>(p); };
+    auto launch = [&](auto kernel) { kernel<<<grid, 32 * kQkvWarps, heads * sizeof(HeadPlace), st>>>(p); };
     switch (rot_kind(prep)) {
       case kRotHalves: launch(qkv_append_kernel<kRotHalves>); break;
       case kRotAdjacent: launch(qkv_append_kernel<kRotAdjacent>); break;
@@ -140,16 +160,16 @@ prhs_status prhs_bytekv_qkv_append(prhs_ctx* ctx, const prhs_token_rows* rows, c
   {
     LaunchScope ls(ctx, PRHS_KIND_MISC, st);
     const dim3 grid((unsigned)blocks, (unsigned)by);
-    auto launch = [&](auto kernel) { kernel<<<grid, 32 * kQkv8Warps, 0, st>>>(p); };
+    auto launch = [&](auto kernel, int smem) { kernel<<<grid, 32 * kQkv8Warps, smem, st>>>(p); };
     const int rot = rot_kind(prep);
     if (kv->format == PRHS_BYTEKV_E4M3) {
-      if (rot == kRotHalves) launch(bytekv_qkv_append_kernel<kE4M3, kRotHalves>);
-      else if (rot == kRotAdjacent) launch(bytekv_qkv_append_kernel<kE4M3, kRotAdjacent>);
-      else launch(bytekv_qkv_append_kernel<kE4M3, kRotPartial>);
+      if (rot == kRotHalves) launch(bytekv_qkv_append_kernel<kE4M3, kRotHalves>, kQkv8SmemBytes<kRotHalves>);
+      else if (rot == kRotAdjacent) launch(bytekv_qkv_append_kernel<kE4M3, kRotAdjacent>, kQkv8SmemBytes<kRotAdjacent>);
+      else launch(bytekv_qkv_append_kernel<kE4M3, kRotPartial>, kQkv8SmemBytes<kRotPartial>);
     } else {
-      if (rot == kRotHalves) launch(bytekv_qkv_append_kernel<kE5M2, kRotHalves>);
-      else if (rot == kRotAdjacent) launch(bytekv_qkv_append_kernel<kE5M2, kRotAdjacent>);
-      else launch(bytekv_qkv_append_kernel<kE5M2, kRotPartial>);
+      if (rot == kRotHalves) launch(bytekv_qkv_append_kernel<kE5M2, kRotHalves>, kQkv8SmemBytes<kRotHalves>);
+      else if (rot == kRotAdjacent) launch(bytekv_qkv_append_kernel<kE5M2, kRotAdjacent>, kQkv8SmemBytes<kRotAdjacent>);
+      else launch(bytekv_qkv_append_kernel<kE5M2, kRotPartial>, kQkv8SmemBytes<kRotPartial>);
     }
   }
   PRHS_CUDA(ctx, cudaGetLastError());
