@@ -150,13 +150,16 @@ struct ChunkWalk {
   }
   __device__ __forceinline__ int items_of(const SeqRows& q) const { return (q.n + 2 * p.tokens - 1) / (2 * p.tokens); }
   __device__ __forceinline__ SeqRows seq(int at_b) const { return seq_rows(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, at_b); }
-  // Warp-collective: cost of all items of sequence b0 + lane (one KV head)
-  __device__ __forceinline__ long long costs(int b0) const {
+  // Sequence b0 + lane; none: no rows
+  __device__ __forceinline__ SeqRows lane_seq(int b0) const {
+    const int at_b = b0 + (int)(threadIdx.x & 31);
+    SeqRows q{0, 0, 0, true};
+    if (at_b < p.batch) q = seq(at_b);
+    return q;
+  }
+  // Warp-collective: cost of all items of the lane's sequence (one KV head)
+  __device__ __forceinline__ long long costs(const SeqRows& q) const {
     const int lane = threadIdx.x & 31;
-    SeqRows q;
-    q.n = 0;
-    q.t = 0;
-    if (b0 + lane < p.batch) q = seq(b0 + lane);
     const int m = items_of(q);
     long long sum = 0;
     if (m <= 2)
@@ -184,14 +187,12 @@ struct ChunkWalk {
   __device__ __forceinline__ bool begin() {
     long long seen = 0;           // tiles that are looked at, each once
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      long long w = costs(b0), v = 0;
-      if (b0 + (int)(threadIdx.x & 31) < p.batch) {
-        const SeqRows q = seq(b0 + (threadIdx.x & 31));
-        if (q.n > 0) {
-          int st, lo, hi;
-          range(q, 0, &st, &lo, &hi);
-          v = st + (q.t + kCATile - 1) / kCATile - lo;
-        }
+      const SeqRows q = lane_seq(b0);
+      long long w = costs(q), v = 0;
+      if (q.n > 0) {
+        int st, lo, hi;
+        range(q, 0, &st, &lo, &hi);
+        v = st + (q.t + kCATile - 1) / kCATile - lo;
       }
 #pragma unroll
       for (int off = 16; off > 0; off >>= 1) {
@@ -219,7 +220,8 @@ struct ChunkWalk {
     // the sequence
     long long before = 0, one = 0;
     for (int b0 = 0;; b0 += 32) {
-      const long long w = costs(b0);
+      const SeqRows q = lane_seq(b0);
+      const long long w = costs(q);
       long long incl = w * p.num_kv_heads;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -231,12 +233,14 @@ struct ChunkWalk {
         const int l = __ffs(past) - 1;
         b = b0 + l;
         one = __shfl_sync(0xffffffffu, w, l);
+        s.r0 = __shfl_sync(0xffffffffu, q.r0, l);
+        s.n = __shfl_sync(0xffffffffu, q.n, l);
+        s.t = __shfl_sync(0xffffffffu, q.t, l);
         before += __shfl_sync(0xffffffffu, incl, l) - one * p.num_kv_heads;
         break;
       }
       before += __shfl_sync(0xffffffffu, incl, 31);
     }
-    s = seq(b);
     items = items_of(s);
     kvh = (int)((at - before) / one);
     before += one * kvh;
@@ -378,6 +382,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// the lowest n bits, none for n <= 0, all for n >= 32
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 // the largest of three; NaN if one is
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
@@ -411,8 +417,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ca_smem + (2 + kCASlots) * kCATileBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0) record_bad_sequences(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, p.batch, p.flags);
-  ChunkWalk<kMask> walk(p);
-  if (!walk.begin()) return;
   const uint32_t smem0 = (uint32_t)__cvta_generic_to_shared(ca_smem);
   if (smem0 & 1023u) {                  // (the swizzle asks for it, and there is no room to round up)
     if (threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
@@ -442,6 +446,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  ChunkWalk<kMask> walk(p);
+  if (!walk.begin()) return;
   if (warp == kCAMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"((uint32_t)__cvta_generic_to_shared(&sh.tmem)), "r"(512u) : "memory");
@@ -537,12 +543,19 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             late = __any_sync(0xffffffffu, used && mx > m + kCAGap);
           } else {
             // a tile that some row sees in part, logits that are not finite, no reference yet
-            const int at = x.tile(k) * kCATile, cu = u - at, cs = p.sinks - at, cf = from - at;
             mx = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 128; ++c) {
-              if (partly && !(c < cu && (!kMask || c < cs || c >= cf))) r[c >> 5][c & 31] = 0xff800000u;
-              mx = fmaxf(mx, __uint_as_float(r[c >> 5][c & 31]));            // (passes over NaNs)
+            for (int c = 0; c < 4; ++c) {
+              if (partly) {
+                const int at = x.tile(k) * kCATile + 32 * c;
+                const uint32_t see = bits_below(u - at) & (kMask ? bits_below(p.sinks - at) | ~bits_below(from - at) : 0xffffffffu);
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                  if (!((see >> j) & 1u)) r[c][j] = 0xff800000u;
+              }
+#pragma unroll
+              for (int j = 0; j < 32; j += 2)                        // (passes over NaNs)
+                mx = fmaxf(mx, fmaxf(__uint_as_float(r[c][j]), __uint_as_float(r[c][j + 1])));
             }
             mx *= c1;
             if (__any_sync(0xffffffffu, used && mx > m + kCAGap)) raise(mx);
@@ -673,43 +686,40 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         softmax_bar();
         if (sh.last && !*(volatile int*)&sh.abort && used) {
           __threadfence();
-          // this thread's row: its subtile's pieces, 128 columns; with `halves` those of both, and half of the columns
-          const int sub0 = x.halves ? 0 : s, sub1 = x.halves ? 1 : s, cols = x.halves ? 64 : 128;
-          auto base = [&](int c) { return p.partials + (size_t)(2 * c + (c == x.first_run ? 1 : 0)) * kCASlotFloats; };
-          auto ml = [&](int c, int y) { return __ldcg(reinterpret_cast<const float2*>(base(c) + 2 * kCATile * kHeadDim) + y * kCATile + row); };
+          // this thread's row: its subtile's pieces, 128 columns in two goes; with `halves` those of both, and half of the columns
+          const int sub0 = x.halves ? 0 : s, subs = x.halves ? 2 : 1, n = parts * subs;
           float M = -INFINITY, L = 0.f;
-          for (int c = x.first_run; c <= x.last_run; ++c)
-            for (int y = sub0; y <= sub1; ++y) M = fmaxf(M, ml(c, y).x);
-          for (int c = x.first_run; c <= x.last_run; ++c)
-            for (int y = sub0; y <= sub1; ++y) {
-              const float2 v = ml(c, y);
-              if (v.y != 0.f) L += v.y * exp2f(v.x - M);
-            }
-          const float inv = L == 0.f ? 0.f : 1.f / L;
-          const int c_begin = x.halves ? 64 * s : 0;
 #pragma unroll 1
-          for (int c0 = c_begin; c0 < c_begin + cols; c0 += 32) {
-            float acc[32];
+          for (int c0 = x.halves ? 64 * s : 0; c0 < (x.halves ? 64 * s + 64 : 128); c0 += 64) {
+            float acc[64];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) acc[j] = 0.f;
-            for (int c = x.first_run; c <= x.last_run; ++c)
-              for (int y = sub0; y <= sub1; ++y) {
-                const float2 v = ml(c, y);
-                if (v.y == 0.f) continue;
-                const float f = exp2f(v.x - M);
-                const float4* o = reinterpret_cast<const float4*>(base(c)) + (y * 32 + c0 / 4) * kCATile + row;
+            for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+            M = -INFINITY;
+            L = 0.f;
+            for (int i = 0; i < n; ++i) {
+              const int c = x.first_run + i / subs, y = sub0 + i % subs;
+              const float* from = p.partials + (size_t)(2 * c + (c == x.first_run ? 1 : 0)) * kCASlotFloats;
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(from + 2 * kCATile * kHeadDim) + y * kCATile + row);
+              const float4* o = reinterpret_cast<const float4*>(from) + (y * 32 + c0 / 4) * kCATile + row;
+              if (v.y == 0.f) continue;                               // (nothing was seen, and O was not written)
+              float4 w[16];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const float4 w = __ldcg(o + j * kCATile);
-                  acc[4 * j] = fmaf(w.x, f, acc[4 * j]);
-                  acc[4 * j + 1] = fmaf(w.y, f, acc[4 * j + 1]);
-                  acc[4 * j + 2] = fmaf(w.z, f, acc[4 * j + 2]);
-                  acc[4 * j + 3] = fmaf(w.w, f, acc[4 * j + 3]);
-                }
+              for (int j = 0; j < 16; ++j) w[j] = __ldcg(o + j * kCATile);
+              const float mn = fmaxf(M, v.x), f = exp2f(M - mn), g = exp2f(v.x - mn);
+              M = mn;
+              L = fmaf(v.y, g, L * f);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                acc[4 * j] = fmaf(w[j].x, g, acc[4 * j] * f);
+                acc[4 * j + 1] = fmaf(w[j].y, g, acc[4 * j + 1] * f);
+                acc[4 * j + 2] = fmaf(w[j].z, g, acc[4 * j + 2] * f);
+                acc[4 * j + 3] = fmaf(w[j].w, g, acc[4 * j + 3] * f);
               }
+            }
+            const float inv = L == 0.f ? 0.f : 1.f / L;
             uint4* to = reinterpret_cast<uint4*>(p.out + out_row * kHeadDim + c0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 8; ++j)
               to[j] = make_uint4(pack_bf16x2(acc[8 * j] * inv, acc[8 * j + 1] * inv), pack_bf16x2(acc[8 * j + 2] * inv, acc[8 * j + 3] * inv),
                                  pack_bf16x2(acc[8 * j + 4] * inv, acc[8 * j + 5] * inv), pack_bf16x2(acc[8 * j + 6] * inv, acc[8 * j + 7] * inv));
           }
@@ -894,7 +904,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         };
         // tiles k - 1 that both subtiles see all of, with a tile k behind them that both use: nothing to ask
         const int plain_from = max(x.k0, kMask ? max(max(x.kf[0], x.kf[1]), x.kb[1]) : 0) + 1;
-        const int plain_to = x.halves ? x.k0 : min(min(min(x.kd[0], x.kd[1]) + 1, x.k1), min(x.ke[0], x.ke[1]));
+        const int plain_to = x.halves ? x.k0 : min(min(min(x.kd[0], x.kd[1]) + 1, x.k1), min(x.ke[0], x.ke[1]));       // (their last products come after)
+        // the last tile of each subtile (its O is complete behind it)
+        int last[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          last[s] = x.halves ? x.k1 - 2 : min(x.k1, x.ke[s]) - 1;
+          if (kMask && !x.halves && last[s] >= x.sa && last[s] < x.kb[s]) last[s] = x.sa - 1;      // (the piece ends among tiles that it skips)
+        }
         uint32_t before[2] = {0, 0};                 // what the latest two tiles ask for: bits 0, 1: the subtiles that use it; 2: mending
         auto asks = [&](int k) -> uint32_t {
           return (x.active(0, k) ? 1u : 0u) | (x.active(1, k) ? 2u : 0u) | (x.mended(k) ? 4u : 0u);
@@ -943,6 +960,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 oe_par[s] ^= 1;
               }
               pv(s, vpos.slot);
+              if (k - lag_ >= last[s] && leader && ok) umma_commit(bar_ofull + 8 * s);
             }
             if (s == 1 && do_pv && leader && ok) umma_commit(bar_empty + 8 * vpos.slot);
             if ((now >> s) & 1u) {
@@ -956,10 +974,6 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             if (do_qk) umma_commit(bar_empty + 8 * kpos.slot);
             if (k == x.k1 - 1) umma_commit(bar_qempty);
           }
-        }
-        if (ok && leader) {
-          if (started[0]) umma_commit(bar_ofull);
-          if (started[1]) umma_commit(bar_ofull + 8);
         }
       }
       if (!ok) gave_up();
