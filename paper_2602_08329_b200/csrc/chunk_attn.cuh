@@ -5,7 +5,8 @@
 // P(u) = max(0, u - window, floor(c u)).  Its G heads of a KV head are G rows; T = 128 / G tokens (rounded down) fill the 128 rows of an
 // MMA.  A CTA works on an item, 2 T tokens of a sequence and one KV head, as two subtiles of T tokens with an
 // accumulator each, over tiles of 128 keys:
-//   producer warp   Q once per piece, then K and V tiles by TMA (128-byte swizzle) into a ring of five 32 KB slots
+//   producer warp   finds this CTA's pieces of work and tells the others; Q once per piece, then K and V tiles by TMA (128-byte swizzle)
+//                   into a ring of five 32 KB slots
 //   MMA warp        S = Q K^T (128 x 128, fp32 in tensor memory) and O += P V for the subtiles in turn, P read from tensor memory
 //   8 softmax warps a thread owns a row of a subtile: reads it (tcgen05.ld), weights 2^(x - m) in bf16 back over S (tcgen05.st), their
 //                   sum in fp32.  While the tensor core multiplies for one subtile, the other's weights are made
@@ -42,10 +43,14 @@ constexpr int kCAHalfBytes = kCATile * 128;               // [128 rows][64 colum
 constexpr int kCATileBytes = 2 * kCAHalfBytes;            // 32 KB
 constexpr int kCASlots = 5;
 constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
+constexpr int kCAPieces = 4;                              // of a CTA that are known ahead
+constexpr int kCAPieceBytes = 128;
 // What is shared beside the tiles (they leave 3 KB).
 struct ChunkShared {
-  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain
-  unsigned long long bars[3 * kCASlots + 13];
+  unsigned char pieces[kCAPieces][kCAPieceBytes];
+  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
+  // piece_full[4], piece_empty[4]
+  unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces];
   int mended_n[4], mended_tile[4][kCAMaxMended];
   uint32_t tmem;
   int abort, last;
@@ -91,7 +96,7 @@ struct Piece {
   int k0, k1, st, lo;            // tile k is k for k < st, else lo + k - st
   int run, first_run, last_run;  // this one, and those that have pieces of the item
   int t;
-  bool halves;
+  int halves;
   // Subtile s uses tile k if k < sa or kb <= k < ke, and every one of its rows sees all of it if k < sf or kf <= k < kd.  (The first
   // positions may reach beyond `lo`: all tiles are listed then, and st = lo.)
   int sa, kb[2], ke[2], kf[2], kd[2], sf[2];
@@ -126,7 +131,7 @@ struct Piece {
   __device__ __forceinline__ bool partly(int s, int k) const { return !(kMask ? k < sf[s] || (k >= kf[s] && k < kd[s]) : k < kd[s]); }
   __device__ __forceinline__ bool mended(int k) const { return (active(0, k) && partly(0, k)) || (active(1, k) && partly(1, k)); }
 };
-// Walks this CTA's run.  Every warp does so for itself; all lanes hold the same values.
+// Walks this CTA's runs: one warp, all lanes hold the same values.
 template <bool kMask>
 struct ChunkWalk {
   const ChunkParams& p;
@@ -384,6 +389,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // the lowest n bits, none for n <= 0, all for n >= 32
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+// A bounded wait that does not end with another warp's.
+__device__ __forceinline__ bool mbar_wait_through(uint32_t bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity))
+    if (clock64() - t0 > 4 * kWaitBudgetCycles) return false;
+  return true;
+}
 // the largest of three; NaN if one is
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
@@ -426,7 +439,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(sh.bars);
   const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
   const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
-  const uint32_t bar_ofull = bar_qfull + 64, bar_oempty = bar_qfull + 80, bar_drain = bar_qfull + 96;
+  const uint32_t bar_ofull = bar_qfull + 64, bar_oempty = bar_qfull + 80, bar_drain = bar_qfull + 96, bar_piece = bar_qfull + 104;
   if (tid == 0) {
     for (int i = 0; i < kCASlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);      // the producer's expect_tx arrive
@@ -443,11 +456,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       mbar_init(bar_oempty + 8 * i, 4);    // the subtile's softmax warps
     }
     mbar_init(bar_drain, 1);
+    for (int i = 0; i < kCAPieces; ++i) {
+      mbar_init(bar_piece + 8 * i, 1);                     // the producer
+      mbar_init(bar_piece + 8 * (kCAPieces + i), 11);      // all other warps
+    }
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  ChunkWalk<kMask> walk(p);
-  if (!walk.begin()) return;
+  static_assert(sizeof(Piece<kMask>) <= kCAPieceBytes, "a piece has its place in shared memory");
   if (warp == kCAMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"((uint32_t)__cvta_generic_to_shared(&sh.tmem)), "r"(512u) : "memory");
@@ -458,6 +474,18 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   tc_fence_after();
   const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
   Piece<kMask> x;
+  // The next piece, by whatever warp but the producer; false: there is none.  (Waits whatever happened: the producer tells of all pieces and
+  // of the end even after an aborted wait, so that the warps of a barrier leave together.)
+  int piece_at = 0;
+  auto take = [&] {
+    const int i = piece_at % kCAPieces;
+    if (!__all_sync(0xffffffffu, mbar_wait_through(bar_piece + 8 * i, (piece_at / kCAPieces) & 1))) return false;
+    x = *reinterpret_cast<const Piece<kMask>*>(sh.pieces[i]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_piece + 8 * (kCAPieces + i));
+    ++piece_at;
+    return x.k1 >= 0;
+  };
   auto gave_up = [&] {
     atomicOr(p.flags, kFlagTimeout);
     sh.abort = 1;
@@ -474,7 +502,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     uint32_t s_par = 0, o_par = 0;
     int buf = 0;                                     // of the mending warps' notes
     bool aborted = false;                            // a warp that gave up goes on without touching anything: barriers stay balanced
-    while (walk.next(x)) {
+    while (take()) {
       const bool used = row < p.tokens * p.group && token < x.e(p, s) - x.a(p, s);
       const bool warp_used = __any_sync(0xffffffffu, used);
       const int u = used ? x.uf(p, s) + token : 0;
@@ -739,8 +767,23 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       bool ring_full = false, q_full = false;        // whether slots (Q) have been filled before
       int fills = 0;
       bool ok = true;
-      while (ok && walk.next(x)) {
-        if (x.k0 == x.k1) continue;
+      ChunkWalk<kMask> walk(p);
+      bool more = walk.begin();
+      while (more) {
+        more = walk.next(x);
+        const int at = piece_at % kCAPieces;
+        if (piece_at >= kCAPieces &&
+            !__all_sync(0xffffffffu, mbar_wait_through(bar_piece + 8 * (kCAPieces + at), (piece_at / kCAPieces - 1) & 1))) {
+          ok = false;
+          break;
+        }
+        if (!more) break;
+        if (lane == 0) {
+          *reinterpret_cast<Piece<kMask>*>(sh.pieces[at]) = x;
+          mbar_arrive(bar_piece + 8 * at);
+        }
+        ++piece_at;
+        if (!ok || x.k0 == x.k1) continue;
         if (lane == 0) {
           if (q_full) {
             ok = mbar_wait(bar_qempty, q_par, &sh.abort);
@@ -755,7 +798,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         q_full = true;
         ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
+        if (!ok) {
+          if (lane == 0) gave_up();
+          continue;
+        }
         // pages: lanes 0 - 15 hold the row of page (lane / 2) mod 8 of the latest three tiles
         const int page_at = (lane >> 1) & 7, half = lane & 1;
         const int* table = kPaged ? p.kv.page_table + (long long)x.b * p.kv.page_table_stride : nullptr;
@@ -800,15 +846,22 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             rows[1] = rows[0];
           }
         }
+        if (!ok && lane == 0) gave_up();
       }
-      if (!ok && lane == 0) gave_up();
+      if (lane == 0) {                   // the end
+        x.k0 = x.k1 = -1;
+        *reinterpret_cast<Piece<kMask>*>(sh.pieces[piece_at % kCAPieces]) = x;
+        mbar_arrive(bar_piece + 8 * (piece_at % kCAPieces));
+        if (!ok) gave_up();
+      }
+      __syncwarp();
     } else if (warp >= kCAMendWarp) {
       // ------------------------------------------------------------------------ mending warps (they follow the ring fill by fill)
       const int t64 = tid - 32 * kCAMendWarp;
       RingPos pos;
       int buf = 0;
       bool ok = true;
-      while (walk.next(x)) {         // (a warp that gave up goes on through the barriers of the other)
+      while (take()) {         // (a warp that gave up goes on through the barriers of the other)
         if (x.k0 == x.k1) continue;
         if (t64 == 0) sh.mended_n[buf & 3] = 0;
         asm volatile("bar.sync 2, 64;" ::: "memory");
@@ -880,8 +933,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       auto wait = [&](uint32_t bar, uint32_t parity) {
         if (!mbar_try_wait(bar, parity) && !mbar_wait(bar, parity, &sh.abort)) ok = false;
       };
-      while (ok && walk.next(x)) {
-        if (x.k0 == x.k1) continue;
+      while (take()) {
+        if (!ok || x.k0 == x.k1) continue;
         wait(bar_qfull, q_par);
         q_par ^= 1;
         bool started[2] = {false, false};
