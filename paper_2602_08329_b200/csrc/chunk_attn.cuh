@@ -45,13 +45,14 @@ constexpr int kCASlots = 5;
 constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
 constexpr int kCAPieces = 4;                              // of a CTA that are known ahead
 constexpr int kCAPieceBytes = 128;
+constexpr int kCANotes = 8;                               // pieces whose mended tiles are noted: the ring lets the mending warps run four ahead at most
 // What is shared beside the tiles (they leave 3 KB).
 struct ChunkShared {
   unsigned char pieces[kCAPieces][kCAPieceBytes];
   // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
   // piece_full[4], piece_empty[4]
   unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces];
-  int mended_n[4], mended_tile[4][kCAMaxMended];
+  int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];
   uint32_t tmem;
   int abort, last;
 };
@@ -61,12 +62,13 @@ constexpr int kCAMmaWarp = 8, kCALoadWarp = 9, kCAMendWarp = 10;
 constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // a piece in the workspace: O [2][32][128] float4, (m, l) [2][128]
 constexpr uint32_t kCAIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCATile >> 3) << 17) | ((uint32_t)(kCATile >> 4) << 24);
 constexpr uint32_t kCAIdescPV = kCAIdesc | (1u << 16);    // B = V tile read MN-major
+// A row's reference moves where a logit exceeds it by 2^kCAGap; up to 2^kCAFar the weights stand (bf16 and fp32 have the range).
 constexpr float kCAGap = 8.f, kCAFar = 60.f;
 // An item's Q, merge and output cost about as much as two tiles; a run of fewer than kCAMinRun tiles is not worth its merge.
 constexpr int kCAItemCost = 2;
 constexpr int kCAMinRun = 4;
 // What the CTAs work on at a time should stay in L2: a round for every 1024 tiles that are looked at (64 MB), of runs of at least 192.
-constexpr int kCARoundTiles = 1024, kCARoundRun = 192, kCAMaxRounds = 8;
+constexpr int kCARoundTiles = 1024, kCARoundRun = 192, kCAMaxRounds = 4;
 
 struct ChunkParams {
   KvDev kv;
@@ -280,8 +282,10 @@ struct ChunkWalk {
       i = 0;
       if (++kvh == p.num_kv_heads) {
         kvh = 0;
-        do s = seq(++b);
-        while (s.n == 0);
+        do {
+          if (++b >= p.batch) return false;          // (the lengths have changed since the work was counted)
+          s = seq(b);
+        } while (s.n == 0);
         items = items_of(s);
       }
     }
@@ -633,7 +637,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const int slot = 2 * x.run + (x.first_run == x.run ? 1 : 0);
       float* const part = p.partials + (size_t)slot * kCASlotFloats;
       const long long out_row = ((long long)(x.row0 + x.a(p, s) + token) * p.num_q_heads + x.kvh * p.group + head);
-      const int mended = any ? sh.mended_n[buf & 3] : 0;
+      const int mended = any ? sh.mended_n[buf % kCANotes] : 0;
       if (!aborted && warp_used) {
         tc_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -650,7 +654,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           }
           // values that are not finite and were kept out of the product: infinite or NaN whatever their weight
           for (int y = 0; y < mended; ++y) {
-            const int at = sh.mended_tile[buf & 3][y] * kCATile;
+            const int at = sh.mended_tile[buf % kCANotes][y] * kCATile;
             for (int i = at; i < min(at + kCATile, u); ++i) {
               if (i >= p.sinks && i < from) continue;
               long long off = (long long)x.b * p.kv.stride_outer + (long long)i * kHeadDim;
@@ -863,7 +867,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       bool ok = true;
       while (take()) {         // (a warp that gave up goes on through the barriers of the other)
         if (x.k0 == x.k1) continue;
-        if (t64 == 0) sh.mended_n[buf & 3] = 0;
+        if (t64 == 0) sh.mended_n[buf % kCANotes] = 0;
         asm volatile("bar.sync 2, 64;" ::: "memory");
         PRHS_CHUNK_STEPS(x, k) {
           const int prev = k - lag_;
@@ -898,10 +902,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               asm volatile("{ .reg .pred a, b; setp.ne.u32 a, %1, 0; barrier.cta.red.or.pred b, 2, 64, a; selp.u32 %0, 1, 0, b; }"
                            : "=r"(any_odd) : "r"((uint32_t)odd) : "memory");
               if (any_odd && t64 == 0) {
-                const int n = sh.mended_n[buf & 3];
+                const int n = sh.mended_n[buf % kCANotes];
                 if (n < kCAMaxMended) {
-                  sh.mended_tile[buf & 3][n] = x.tile(prev);
-                  sh.mended_n[buf & 3] = n + 1;
+                  sh.mended_tile[buf % kCANotes][n] = x.tile(prev);
+                  sh.mended_n[buf % kCANotes] = n + 1;
                 }
               }
               __syncwarp();
