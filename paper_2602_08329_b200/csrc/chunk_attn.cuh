@@ -6,7 +6,7 @@
 // MMA.  A CTA works on an item, 2 T tokens of a sequence and one KV head, as two subtiles of T tokens with an
 // accumulator each, over tiles of 128 keys:
 //   producer warp   finds this CTA's pieces of work and tells the others; Q once per piece, then K and V tiles by TMA (128-byte swizzle)
-//                   into a ring of five 32 KB slots
+//                   into a ring of 32 KB slots
 //   MMA warp        S = Q K^T (128 x 128, fp32 in tensor memory) and O += P V for the subtiles in turn, P read from tensor memory
 //   8 softmax warps a thread owns a row of a subtile: reads it (tcgen05.ld), weights 2^(x - m) in bf16 back over S (tcgen05.st), their
 //                   sum in fp32.  While the tensor core multiplies for one subtile, the other's weights are made
@@ -17,8 +17,9 @@
 // of the warp, before anything is stored, finds logits beyond 2^60 of it, NaNs, masks and rows without a reference,
 // which go a slower way.  m moves where a logit has exceeded it by 2^8, before the next tile; O is then rescaled in tensor memory by
 // the softmax warps themselves.
-// An item of at most T tokens (drafts, short chunks) lets its two accumulators take the even and the odd tiles instead
-// (`halves`), and the stream of the cache is what bounds it.
+// An item of at most T tokens lets its two accumulators take the even and the odd tiles instead (`halves`).  Calls of few tokens (kFew: T or
+// fewer per sequence on average; drafts, single tokens) cut all their items that way, with one tile of Q and six slots: the stream of the
+// cache is what bounds them.
 //
 // Work is dealt evenly whatever the lengths: the tiles of all items, laid end to end (sequence, KV head, tokens), are cut into
 // runs of equal length, and every CTA (one per SM) takes as many of them, one in each round.  A piece of an item goes to a workspace as
@@ -26,8 +27,9 @@
 // Several rounds keep what is looked at at a time small: 2048 tokens at 131072, all in one round, read 70 % of their
 // tiles from DRAM.
 //
-// Weights enter the product as bf16, one rounding of 2^-8: as two bf16 (what the decode kernels do, bound by the stream) they would cost
-// half as many MMAs again, which is what bounds this kernel.  Sums, references, O and what is merged are fp32.
+// Weights enter the product as bf16, one rounding of 2^-8, where the MMAs are what bounds the kernel: as two bf16 they would cost half as
+// many again.  Calls of few tokens, bound by the stream, take two bf16 (2^-16), as the decode kernels do.  Sums, references, O and what
+// is merged are fp32.
 #pragma once
 #include <cuda.h>
 
@@ -41,7 +43,8 @@ namespace prhs {
 constexpr int kCATile = 128;                              // keys per tile, rows per subtile
 constexpr int kCAHalfBytes = kCATile * 128;               // [128 rows][64 columns] bf16
 constexpr int kCATileBytes = 2 * kCAHalfBytes;            // 32 KB
-constexpr int kCASlots = 5;
+constexpr int kCATiles = 7;                               // of 32 KB: Q and the ring
+constexpr int kCASlots = 6;                               // of the ring at most
 constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
 constexpr int kCAPieces = 4;                              // of a CTA that are known ahead
 constexpr int kCAPieceBytes = 128;
@@ -49,14 +52,14 @@ constexpr int kCANotes = 8;                               // pieces whose mended
 // What is shared beside the tiles (they leave 3 KB).
 struct ChunkShared {
   unsigned char pieces[kCAPieces][kCAPieceBytes];
-  // kv_full[5], kv_empty[5], v_ready[5], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
+  // kv_full[6], kv_empty[6], v_ready[6], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
   // piece_full[4], piece_empty[4]
   unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces];
   int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];
   uint32_t tmem;
   int abort, last;
 };
-constexpr int kCASmemBytes = (2 + kCASlots) * kCATileBytes + (int)sizeof(ChunkShared);
+constexpr int kCASmemBytes = kCATiles * kCATileBytes + (int)sizeof(ChunkShared);
 constexpr int kCAThreads = 12 * 32;
 constexpr int kCAMmaWarp = 8, kCALoadWarp = 9, kCAMendWarp = 10;
 constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // a piece in the workspace: O [2][32][128] float4, (m, l) [2][128]
@@ -92,20 +95,21 @@ __device__ __forceinline__ int first_visible(const ChunkParams& p, int u) {
   return lo;
 }
 // A piece of an item: tiles k0 .. k1 - 1 of those its tokens see.
-template <bool kMask>
+template <bool kMask, bool kFew>
 struct Piece {
   int b, kvh, row0, ntok, u0;    // u0: visible length of the first token
   int k0, k1, st, lo;            // tile k is k for k < st, else lo + k - st
   int run, first_run, last_run;  // this one, and those that have pieces of the item
   int t;
-  int halves;
+  int short_item;
+  __device__ __forceinline__ bool halves() const { return kFew || short_item; }
   // Subtile s uses tile k if k < sa or kb <= k < ke, and every one of its rows sees all of it if k < sf or kf <= k < kd.  (The first
   // positions may reach beyond `lo`: all tiles are listed then, and st = lo.)
   int sa, kb[2], ke[2], kf[2], kd[2], sf[2];
   __device__ __forceinline__ int tile(int k) const { return !kMask || k < st ? k : lo + k - st; }
   // subtile s: tokens [a, e) of the item, visible lengths of its first and its last
-  __device__ __forceinline__ int a(const ChunkParams& p, int s) const { return halves || s == 0 ? 0 : p.tokens; }
-  __device__ __forceinline__ int e(const ChunkParams& p, int s) const { return halves || s == 1 ? ntok : min(ntok, p.tokens); }
+  __device__ __forceinline__ int a(const ChunkParams& p, int s) const { return halves() || s == 0 ? 0 : p.tokens; }
+  __device__ __forceinline__ int e(const ChunkParams& p, int s) const { return halves() || s == 1 ? ntok : min(ntok, p.tokens); }
   __device__ __forceinline__ int uf(const ChunkParams& p, int s) const { return u0 + a(p, s); }
   __device__ __forceinline__ int ul(const ChunkParams& p, int s) const { return u0 + e(p, s) - 1; }
   __device__ __forceinline__ void ranges(const ChunkParams& p) {
@@ -127,14 +131,14 @@ struct Piece {
     }
   }
   __device__ __forceinline__ bool active(int s, int k) const {
-    return halves ? ((k - k0) & 1) == s : k < ke[s] && (!kMask || k < sa || k >= kb[s]);
+    return halves() ? ((k - k0) & 1) == s : k < ke[s] && (!kMask || k < sa || k >= kb[s]);
   }
   // some row of the subtile does not see all of the tile
   __device__ __forceinline__ bool partly(int s, int k) const { return !(kMask ? k < sf[s] || (k >= kf[s] && k < kd[s]) : k < kd[s]); }
   __device__ __forceinline__ bool mended(int k) const { return (active(0, k) && partly(0, k)) || (active(1, k) && partly(1, k)); }
 };
 // Walks this CTA's runs: one warp, all lanes hold the same values.
-template <bool kMask>
+template <bool kMask, bool kFew>
 struct ChunkWalk {
   const ChunkParams& p;
   long long at = 0, end = 0, total = 0, item_at = 0;
@@ -144,7 +148,7 @@ struct ChunkWalk {
   __device__ __forceinline__ explicit ChunkWalk(const ChunkParams& params) : p(params) {}
   // tiles that item i's tokens see, as (st, lo, hi)
   __device__ __forceinline__ void range(const SeqRows& q, int item, int* st, int* lo, int* hi) const {
-    const int a = item * 2 * p.tokens, e = min(q.n, a + 2 * p.tokens);
+    const int a = item * per_item(), e = min(q.n, a + per_item());
     const int uf = q.t - q.n + a + 1, ul = q.t - q.n + e;
     *hi = (ul + kCATile - 1) / kCATile;
     *lo = kMask ? first_visible(p, uf) / kCATile : 0;
@@ -155,7 +159,8 @@ struct ChunkWalk {
     range(q, item, &st, &lo, &hi);
     return st + hi - lo + kCAItemCost;
   }
-  __device__ __forceinline__ int items_of(const SeqRows& q) const { return (q.n + 2 * p.tokens - 1) / (2 * p.tokens); }
+  __device__ __forceinline__ int per_item() const { return kFew ? p.tokens : 2 * p.tokens; }
+  __device__ __forceinline__ int items_of(const SeqRows& q) const { return (q.n + per_item() - 1) / per_item(); }
   __device__ __forceinline__ SeqRows seq(int at_b) const { return seq_rows(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, at_b); }
   // Sequence b0 + lane; none: no rows
   __device__ __forceinline__ SeqRows lane_seq(int b0) const {
@@ -272,7 +277,7 @@ struct ChunkWalk {
     return true;
   }
   // Warp-collective.
-  __device__ __forceinline__ bool next(Piece<kMask>& x) {
+  __device__ __forceinline__ bool next(Piece<kMask, kFew>& x) {
     if (at >= end) {
       run += ctas;
       if (!seek()) return false;
@@ -299,11 +304,11 @@ struct ChunkWalk {
     x.last_run = run_of(item_at + w - 1);
     x.b = b;
     x.kvh = kvh;
-    x.row0 = s.r0 + i * 2 * p.tokens;
-    x.ntok = min(s.n - i * 2 * p.tokens, 2 * p.tokens);
-    x.u0 = s.t - s.n + i * 2 * p.tokens + 1;
+    x.row0 = s.r0 + i * per_item();
+    x.ntok = min(s.n - i * per_item(), per_item());
+    x.u0 = s.t - s.n + i * per_item() + 1;
     x.t = s.t;
-    x.halves = x.ntok <= p.tokens;
+    x.short_item = x.ntok <= p.tokens;
     x.ranges(p);
     at = to;
     if (to == item_at + w) {
@@ -410,11 +415,12 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // Ring position: slot and the parity of its fill.
+template <int kSlots>
 struct RingPos {
   int slot = 0;
   uint32_t parity = 0;
   __device__ __forceinline__ void step() {
-    if (++slot == kCASlots) {
+    if (++slot == kSlots) {
       slot = 0;
       parity ^= 1;
     }
@@ -423,15 +429,16 @@ struct RingPos {
 
 // The order in which K and V tiles go through the ring: V follows its K by one step (two where the accumulators take turns with the
 // tiles, so that both have a tile under way).
-#define PRHS_CHUNK_STEPS(x, k) for (int k = (x).k0, lag_ = (x).halves ? 2 : 1, stop_ = (x).k1 > (x).k0 ? (x).k1 + lag_ : (x).k0; k < stop_; ++k)
+#define PRHS_CHUNK_STEPS(x, k) for (int k = (x).k0, lag_ = (x).halves() ? 2 : 1, stop_ = (x).k1 > (x).k0 ? (x).k1 + lag_ : (x).k0; k < stop_; ++k)
 
 // grid: one CTA per SM.  tm_q: q as [rows][Hq][128], box [T][G][64]; tm_k, tm_v: [rows][128], box [128][64], or [16][64] per page.
-template <bool kPaged, bool kMask>
+template <bool kPaged, bool kMask, bool kFew>
 __global__ void __launch_bounds__(kCAThreads, 1)
 chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ ChunkParams p) {
   extern __shared__ __align__(1024) unsigned char ca_smem[];
-  ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ca_smem + (2 + kCASlots) * kCATileBytes);
+  constexpr int kQTiles = kFew ? 1 : 2, kSlots = kCATiles - kQTiles;
+  ChunkShared& sh = *reinterpret_cast<ChunkShared*>(ca_smem + kCATiles * kCATileBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x == 0) record_bad_sequences(p.row_start, p.num_rows, p.kv.seq_lens, p.max_len, p.batch, p.flags);
   const uint32_t smem0 = (uint32_t)__cvta_generic_to_shared(ca_smem);
@@ -439,7 +446,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
     return;
   }
-  const uint32_t ring = smem0 + 2 * kCATileBytes;
+  const uint32_t ring = smem0 + kQTiles * kCATileBytes;
   const uint32_t bar0 = (uint32_t)__cvta_generic_to_shared(sh.bars);
   const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
   const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
@@ -467,7 +474,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  static_assert(sizeof(Piece<kMask>) <= kCAPieceBytes, "a piece has its place in shared memory");
+  static_assert(sizeof(Piece<kMask, kFew>) <= kCAPieceBytes, "a piece has its place in shared memory");
   if (warp == kCAMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"((uint32_t)__cvta_generic_to_shared(&sh.tmem)), "r"(512u) : "memory");
@@ -476,15 +483,15 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
-  Piece<kMask> x;
+  const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S (its low parts over the second)
+  Piece<kMask, kFew> x;
   // The next piece, by whatever warp but the producer; false: there is none.  (Waits whatever happened: the producer tells of all pieces and
   // of the end even after an aborted wait, so that the warps of a barrier leave together.)
   int piece_at = 0;
   auto take = [&] {
     const int i = piece_at % kCAPieces;
     if (!__all_sync(0xffffffffu, mbar_wait_through(bar_piece + 8 * i, (piece_at / kCAPieces) & 1))) return false;
-    x = *reinterpret_cast<const Piece<kMask>*>(sh.pieces[i]);
+    x = *reinterpret_cast<const Piece<kMask, kFew>*>(sh.pieces[i]);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_piece + 8 * (kCAPieces + i));
     ++piece_at;
@@ -511,7 +518,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const bool warp_used = __any_sync(0xffffffffu, used);
       const int u = used ? x.uf(p, s) + token : 0;
       const int from = kMask && used ? first_visible(p, u) : 0;
-      const int kb = s ? x.kb[1] : x.kb[0], ke = x.halves ? x.k1 : min(x.k1, s ? x.ke[1] : x.ke[0]);
+      const int kb = s ? x.kb[1] : x.kb[0], ke = x.halves() ? x.k1 : min(x.k1, s ? x.ke[1] : x.ke[0]);
       const int kf = s ? x.kf[1] : x.kf[0], kd = s ? x.kd[1] : x.kd[0], sf = s ? x.sf[1] : x.sf[0];
       float m = -INFINITY, next = -INFINITY;         // the reference, and the one to go on with
       uint64_t l2 = 0ull;                            // two partial sums
@@ -534,9 +541,9 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           }
         }
       };
-      const int step = x.halves ? 2 : 1;
-      for (int k = x.halves ? x.k0 + s : x.k0; k < ke; k += step) {
-        if (kMask && !x.halves && k >= x.sa && k < kb) continue;
+      const int step = x.halves() ? 2 : 1;
+      for (int k = x.halves() ? x.k0 + s : x.k0; k < ke; k += step) {
+        if (kMask && !x.halves() && k >= x.sa && k < kb) continue;
         if (!aborted) {
           aborted = !__all_sync(0xffffffffu, mbar_wait(bar_sfull + 8 * s, s_par, &sh.abort));
           if (aborted && lane == 0) gave_up();
@@ -596,27 +603,44 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t cc = pack_f32x2(c1, c1), mm = pack_f32x2(-ref, -ref);
           uint64_t la = 0ull, lb = 0ull;
-          // the weights, over S, and on to the tensor core in two halves
+          // the weights, over S, and on to the tensor core in two halves; of few tokens with what the rounding left of them, to 2^-16
+          auto weights = [&] {
+            constexpr bool kTwo = kFew;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t w[32];
+            for (int h = 0; h < 2; ++h) {
+              uint32_t w[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const int c = 64 * h + 2 * j;
-              float a, b;
-              unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm), a, b);
-              a = exp2_fast(a);
-              b = exp2_fast(b);
-              if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
-              else lb = add_f32x2(lb, pack_f32x2(a, b));
-              w[j] = pack_bf16x2(a, b);
+              for (int j = 0; j < 32; ++j) {
+                const int c = 64 * h + 2 * j;
+                uint32_t &ra = r[c >> 5][c & 31], &rb = r[c >> 5][(c & 31) + 1];
+                float a, b;
+                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(ra), __uint_as_float(rb)), cc, mm), a, b);
+                a = exp2_fast(a);
+                b = exp2_fast(b);
+                if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
+                else lb = add_f32x2(lb, pack_f32x2(a, b));
+                w[j] = pack_bf16x2(a, b);
+                if (kTwo) {
+                  ra = __float_as_uint(a);
+                  rb = __float_as_uint(b);
+                }
+              }
+              tmem_st32(tm_s + 32 * h, w);
+              if (kTwo) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                  const int c = 64 * h + 2 * j;
+                  w[j] = pack_bf16x2(__uint_as_float(r[c >> 5][c & 31]) - bf_lo(w[j]), __uint_as_float(r[c >> 5][(c & 31) + 1]) - bf_hi(w[j]));
+                }
+                tmem_st32(tm_s + 64 + 32 * h, w);
+              }
+              tmem_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_pfull + 16 * s + 8 * h);
             }
-            tmem_st32(tm_s + 32 * h, w);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_pfull + 16 * s + 8 * h);
-          }
+          };
+          weights();
           l2 = add_f32x2(l2, add_f32x2(la, lb));
         } else if (lane == 0) {
           mbar_arrive(bar_pfull + 16 * s);
@@ -633,7 +657,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (aborted && lane == 0) gave_up();
       }
       if (any) o_par ^= 1;
-      const bool whole = x.first_run == x.last_run && !x.halves;
+      const bool whole = x.first_run == x.last_run && !x.halves();
       const int slot = 2 * x.run + (x.first_run == x.run ? 1 : 0);
       float* const part = p.partials + (size_t)slot * kCASlotFloats;
       const long long out_row = ((long long)(x.row0 + x.a(p, s) + token) * p.num_q_heads + x.kvh * p.group + head);
@@ -719,10 +743,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (sh.last && !*(volatile int*)&sh.abort && used) {
           __threadfence();
           // this thread's row: its subtile's pieces, 128 columns in two goes; with `halves` those of both, and half of the columns
-          const int sub0 = x.halves ? 0 : s, subs = x.halves ? 2 : 1, n = parts * subs;
+          const int sub0 = x.halves() ? 0 : s, subs = x.halves() ? 2 : 1, n = parts * subs;
           float M = -INFINITY, L = 0.f;
 #pragma unroll 1
-          for (int c0 = x.halves ? 64 * s : 0; c0 < (x.halves ? 64 * s + 64 : 128); c0 += 64) {
+          for (int c0 = x.halves() ? 64 * s : 0; c0 < (x.halves() ? 64 * s + 64 : 128); c0 += 64) {
             float acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = 0.f;
@@ -755,7 +779,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               to[j] = make_uint4(pack_bf16x2(acc[8 * j] * inv, acc[8 * j + 1] * inv), pack_bf16x2(acc[8 * j + 2] * inv, acc[8 * j + 3] * inv),
                                  pack_bf16x2(acc[8 * j + 4] * inv, acc[8 * j + 5] * inv), pack_bf16x2(acc[8 * j + 6] * inv, acc[8 * j + 7] * inv));
           }
-          if (p.out_lse && (!x.halves || s == 0)) p.out_lse[out_row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+          if (p.out_lse && (!x.halves() || s == 0)) p.out_lse[out_row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
         }
         softmax_bar();                   // the slot may be written again
       }
@@ -766,12 +790,12 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       // ------------------------------------------------------------------------ producer
       const int outer_rows = (int)(p.kv.stride_outer >> 7), head_rows = (int)(p.kv.stride_head >> 7);
       const uint32_t q_bytes = 2u * 128u * (uint32_t)(p.group * p.tokens);
-      RingPos pos;
+      RingPos<kSlots> pos;
       uint32_t q_par = 0;
       bool ring_full = false, q_full = false;        // whether slots (Q) have been filled before
       int fills = 0;
       bool ok = true;
-      ChunkWalk<kMask> walk(p);
+      ChunkWalk<kMask, kFew> walk(p);
       bool more = walk.begin();
       while (more) {
         more = walk.next(x);
@@ -783,7 +807,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         if (!more) break;
         if (lane == 0) {
-          *reinterpret_cast<Piece<kMask>*>(sh.pieces[at]) = x;
+          *reinterpret_cast<Piece<kMask, kFew>*>(sh.pieces[at]) = x;
           mbar_arrive(bar_piece + 8 * at);
         }
         ++piece_at;
@@ -794,8 +818,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             q_par ^= 1;
           }
           if (ok) {
-            mbar_expect_tx(bar_qfull, x.halves ? q_bytes : 2 * q_bytes);
-            for (int y = 0; y < (x.halves ? 1 : 2); ++y)
+            mbar_expect_tx(bar_qfull, x.halves() ? q_bytes : 2 * q_bytes);
+            for (int y = 0; y < (x.halves() ? 1 : 2); ++y)
               for (int h = 0; h < 2; ++h)
                 tma_load_3d_plain(smem0 + y * kCATileBytes + h * kCAHalfBytes, &tm_q, 64 * h, x.kvh * p.group, x.row0 + y * p.tokens, bar_qfull);
           }
@@ -837,7 +861,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             tma_load_2d_plain(dst + kCAHalfBytes, tm, 64, r, bar);
           }
           pos.step();
-          if (++fills == kCASlots) ring_full = true;
+          if (++fills == kSlots) ring_full = true;
         };
         PRHS_CHUNK_STEPS(x, k) {
           if (ok && k - lag_ >= x.k0) fill(&tm_v, k - lag_, rows[lag_ - 1]);
@@ -854,7 +878,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       }
       if (lane == 0) {                   // the end
         x.k0 = x.k1 = -1;
-        *reinterpret_cast<Piece<kMask>*>(sh.pieces[piece_at % kCAPieces]) = x;
+        *reinterpret_cast<Piece<kMask, kFew>*>(sh.pieces[piece_at % kCAPieces]) = x;
         mbar_arrive(bar_piece + 8 * (piece_at % kCAPieces));
         if (!ok) gave_up();
       }
@@ -862,7 +886,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     } else if (warp >= kCAMendWarp) {
       // ------------------------------------------------------------------------ mending warps (they follow the ring fill by fill)
       const int t64 = tid - 32 * kCAMendWarp;
-      RingPos pos;
+      RingPos<kSlots> pos;
       int buf = 0;
       bool ok = true;
       while (take()) {         // (a warp that gave up goes on through the barriers of the other)
@@ -928,7 +952,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       // (The control flow is the whole warp's: operands of an MMA are uniform registers, and in code that a single lane has branched
       // into each one costs about a hundred cycles to issue.)
       const bool leader = elect_one();
-      RingPos pos;
+      RingPos<kSlots> pos;
       uint32_t q_par = 0, vr_par = 0, p_par[2] = {0, 0}, oe_par[2] = {1, 1};
       bool ok = true;
       const uint32_t q_lo = umma_desc_lo(smem0), ring_k = umma_desc_lo(ring), ring_v = umma_desc_mn_lo(ring);
@@ -947,27 +971,29 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           wait(bar_pfull + 16 * s, p_par[s]);
           tc_fence_after();
           if (leader && ok) umma_pv4(d, a, v, started[s] ? 1u : 0u);
+          if (kFew && leader && ok) umma_pv4(d, a + 64, v, 1u);
           wait(bar_pfull + 16 * s + 8, p_par[s]);
           p_par[s] ^= 1;
           tc_fence_after();
           if (leader && ok) umma_pv4(d, a + 32, v + 4 * ((16 * 128) >> 4), 1u);
+          if (kFew && leader && ok) umma_pv4(d, a + 96, v + 4 * ((16 * 128) >> 4), 1u);
           started[s] = true;
         };
         auto qk = [&](int s, int k_slot) {
           if (leader && ok) {
-            umma_qk(tmem0 + s * kCATile, x.halves ? q_lo : q_lo + s * kSlotLo, ring_k + k_slot * kSlotLo);
+            umma_qk(tmem0 + s * kCATile, x.halves() ? q_lo : q_lo + s * kSlotLo, ring_k + k_slot * kSlotLo);
             umma_commit(bar_sfull + 8 * s);
           }
         };
         // tiles k - 1 that both subtiles see all of, with a tile k behind them that both use: nothing to ask
         const int plain_from = max(x.k0, kMask ? max(max(x.kf[0], x.kf[1]), x.kb[1]) : 0) + 1;
-        const int plain_to = x.halves ? x.k0 : min(min(min(x.kd[0], x.kd[1]) + 1, x.k1), min(x.ke[0], x.ke[1]));       // (their last products come after)
+        const int plain_to = x.halves() ? x.k0 : min(min(min(x.kd[0], x.kd[1]) + 1, x.k1), min(x.ke[0], x.ke[1]));       // (their last products come after)
         // the last tile of each subtile (its O is complete behind it)
         int last[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          last[s] = x.halves ? x.k1 - 2 : min(x.k1, x.ke[s]) - 1;
-          if (kMask && !x.halves && last[s] >= x.sa && last[s] < x.kb[s]) last[s] = x.sa - 1;      // (the piece ends among tiles that it skips)
+          last[s] = x.halves() ? x.k1 - 2 : min(x.k1, x.ke[s]) - 1;
+          if (kMask && !x.halves() && last[s] >= x.sa && last[s] < x.kb[s]) last[s] = x.sa - 1;      // (the piece ends among tiles that it skips)
         }
         uint32_t before[2] = {0, 0};                 // what the latest two tiles ask for: bits 0, 1: the subtiles that use it; 2: mending
         auto asks = [&](int k) -> uint32_t {
@@ -975,10 +1001,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         };
         PRHS_CHUNK_STEPS(x, k) {
           if (!ok) break;
-          const RingPos vpos = pos;
+          const RingPos<kSlots> vpos = pos;
           if (k >= plain_from && k < plain_to && started[0] && started[1]) {
             pos.step();
-            const RingPos kpos = pos;
+            const RingPos<kSlots> kpos = pos;
             pos.step();
             wait(bar_full + 8 * vpos.slot, vpos.parity);
             pv(0, vpos.slot);
@@ -1006,7 +1032,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               vr_par ^= 1u << vpos.slot;
             }
           }
-          const RingPos kpos = pos;
+          const RingPos<kSlots> kpos = pos;
           if (do_qk) pos.step();
           bool k_here = false;
 #pragma unroll

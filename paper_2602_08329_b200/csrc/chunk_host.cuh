@@ -8,8 +8,10 @@ constexpr int kCARegsAtLaunch = 168;      // what the kernel's register split (2
 
 cudaError_t chunk_set_attributes(bool* fits) {
   *fits = true;
-  for (const void* k : {(const void*)chunk_attn_kernel<false, false>, (const void*)chunk_attn_kernel<false, true>,
-                        (const void*)chunk_attn_kernel<true, false>, (const void*)chunk_attn_kernel<true, true>}) {
+  for (const void* k : {(const void*)chunk_attn_kernel<false, false, false>, (const void*)chunk_attn_kernel<false, true, false>,
+                        (const void*)chunk_attn_kernel<true, false, false>, (const void*)chunk_attn_kernel<true, true, false>,
+                        (const void*)chunk_attn_kernel<false, false, true>, (const void*)chunk_attn_kernel<false, true, true>,
+                        (const void*)chunk_attn_kernel<true, false, true>, (const void*)chunk_attn_kernel<true, true, true>}) {
     cudaFuncAttributes a;
     cudaError_t e = cudaFuncGetAttributes(&a, k);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kCASmemBytes);
@@ -111,8 +113,11 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
   {
     LaunchScope ls(ctx, PRHS_KIND_ATTN_DENSE, st);
     auto launch = [&](auto kernel) { kernel<<<ctx->sm_count, kCAThreads, kCASmemBytes, st>>>(tm_q, tm_k, tm_v, p); };
-    if (p.window > 0 || p.psaw_c > 0.0) launch(paged ? chunk_attn_kernel<true, true> : chunk_attn_kernel<false, true>);
-    else launch(paged ? chunk_attn_kernel<true, false> : chunk_attn_kernel<false, false>);
+    const bool few = num_rows <= (long long)batch * p.tokens, masks = p.window > 0 || p.psaw_c > 0.0;
+    if (few && masks) launch(paged ? chunk_attn_kernel<true, true, true> : chunk_attn_kernel<false, true, true>);
+    else if (few) launch(paged ? chunk_attn_kernel<true, false, true> : chunk_attn_kernel<false, false, true>);
+    else if (masks) launch(paged ? chunk_attn_kernel<true, true, false> : chunk_attn_kernel<false, true, false>);
+    else launch(paged ? chunk_attn_kernel<true, false, false> : chunk_attn_kernel<false, false, false>);
   }
   PRHS_CUDA(ctx, cudaGetLastError());
   return PRHS_OK;
