@@ -17,9 +17,10 @@
 // of the warp, before anything is stored, finds logits beyond 2^60 of it, NaNs, masks and rows without a reference,
 // which go a slower way.  m moves where a logit has exceeded it by 2^8, before the next tile; O is then rescaled in tensor memory by
 // the softmax warps themselves.
-// An item of at most T tokens lets its two accumulators take the even and the odd tiles instead (`halves`).  Calls of few tokens (kFew: T or
-// fewer per sequence on average; drafts, single tokens) cut all their items that way, with one tile of Q and six slots: the stream of the
-// cache is what bounds them.
+// An item of at most T tokens lets its two accumulators take the even and the odd tiles instead (`halves`).
+// Calls of few tokens (kFew: 64 / G rows or fewer per sequence on average; drafts, single tokens), which the stream of the cache bounds, have
+// items of 64 rows cut that way, one tile of Q and six slots.  Q stands twice in its tile: rows 64 and on see the same logits, and
+// put what the rounding of the weights has left over S, so that O = (row) + (row + 64) has weights of two bf16 for no more time.
 //
 // Work is dealt evenly whatever the lengths: the tiles of all items, laid end to end (sequence, KV head, tokens), are cut into
 // runs of equal length, and every CTA (one per SM) takes as many of them, one in each round.  A piece of an item goes to a workspace as
@@ -28,7 +29,7 @@
 // tiles from DRAM.
 //
 // Weights enter the product as bf16, one rounding of 2^-8, where the MMAs are what bounds the kernel: as two bf16 they would cost half as
-// many again.  Calls of few tokens, bound by the stream, take two bf16 (2^-16), as the decode kernels do.  Sums, references, O and what
+// many again (2^-16 in calls of few tokens, as the decode kernels have it).  Sums, references, O and what
 // is merged are fp32.
 #pragma once
 #include <cuda.h>
@@ -483,7 +484,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S (its low parts over the second)
+  const uint32_t tmem0 = *(volatile uint32_t*)&sh.tmem;       // S0, S1, O0, O1: 128 columns each; P over the first half of S
   Piece<kMask, kFew> x;
   // The next piece, by whatever warp but the producer; false: there is none.  (Waits whatever happened: the producer tells of all pieces and
   // of the end even after an aborted wait, so that the warps of a barrier leave together.)
@@ -508,13 +509,14 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const int s = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t tm_s = tmem0 + s * kCATile + lanes, tm_o = tmem0 + (2 + s) * kCATile + lanes;
-    const int token = row / p.group, head = row - token * p.group;
+    const int mine = kFew ? row & 63 : row;          // (rows 64 and on repeat the others: see the top)
+    const int token = mine / p.group, head = mine - token * p.group;
     const float c1 = kScale * kLog2e;
     uint32_t s_par = 0, o_par = 0;
     int buf = 0;                                     // of the mending warps' notes
     bool aborted = false;                            // a warp that gave up goes on without touching anything: barriers stay balanced
     while (take()) {
-      const bool used = row < p.tokens * p.group && token < x.e(p, s) - x.a(p, s);
+      const bool used = mine < p.tokens * p.group && token < x.e(p, s) - x.a(p, s);
       const bool warp_used = __any_sync(0xffffffffu, used);
       const int u = used ? x.uf(p, s) + token : 0;
       const int from = kMask && used ? first_visible(p, u) : 0;
@@ -603,44 +605,32 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t cc = pack_f32x2(c1, c1), mm = pack_f32x2(-ref, -ref);
           uint64_t la = 0ull, lb = 0ull;
-          // the weights, over S, and on to the tensor core in two halves; of few tokens with what the rounding left of them, to 2^-16
-          auto weights = [&] {
-            constexpr bool kTwo = kFew;
+          // the weights (kLow: what their rounding leaves), over S, and on to the tensor core in two halves
+          auto weights = [&](auto low) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               uint32_t w[32];
 #pragma unroll
               for (int j = 0; j < 32; ++j) {
                 const int c = 64 * h + 2 * j;
-                uint32_t &ra = r[c >> 5][c & 31], &rb = r[c >> 5][(c & 31) + 1];
                 float a, b;
-                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(ra), __uint_as_float(rb)), cc, mm), a, b);
+                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(r[c >> 5][c & 31]), __uint_as_float(r[c >> 5][(c & 31) + 1])), cc, mm), a, b);
                 a = exp2_fast(a);
                 b = exp2_fast(b);
                 if (j & 1) la = add_f32x2(la, pack_f32x2(a, b));
                 else lb = add_f32x2(lb, pack_f32x2(a, b));
                 w[j] = pack_bf16x2(a, b);
-                if (kTwo) {
-                  ra = __float_as_uint(a);
-                  rb = __float_as_uint(b);
-                }
+                if (decltype(low)::value) w[j] = pack_bf16x2(a - bf_lo(w[j]), b - bf_hi(w[j]));
               }
               tmem_st32(tm_s + 32 * h, w);
-              if (kTwo) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                  const int c = 64 * h + 2 * j;
-                  w[j] = pack_bf16x2(__uint_as_float(r[c >> 5][c & 31]) - bf_lo(w[j]), __uint_as_float(r[c >> 5][(c & 31) + 1]) - bf_hi(w[j]));
-                }
-                tmem_st32(tm_s + 64 + 32 * h, w);
-              }
               tmem_wait_st();
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(bar_pfull + 16 * s + 8 * h);
             }
           };
-          weights();
+          if (kFew && row >= 64) weights(SlotC<1>());
+          else weights(SlotC<0>());
           l2 = add_f32x2(l2, add_f32x2(la, lb));
         } else if (lane == 0) {
           mbar_arrive(bar_pfull + 16 * s);
@@ -742,30 +732,38 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         softmax_bar();
         if (sh.last && !*(volatile int*)&sh.abort && used) {
           __threadfence();
-          // this thread's row: its subtile's pieces, 128 columns in two goes; with `halves` those of both, and half of the columns
+          // This thread's row: its subtile's pieces, 128 columns in four goes; with `halves` those of both, and half of the columns; of few
+          // tokens the rows of the weights' low parts too, and a quarter of the columns.
           const int sub0 = x.halves() ? 0 : s, subs = x.halves() ? 2 : 1, n = parts * subs;
+          const int c_begin = kFew ? 64 * s + 32 * (row >> 6) : x.halves() ? 64 * s : 0, c_end = c_begin + (kFew ? 32 : x.halves() ? 64 : 128);
           float M = -INFINITY, L = 0.f;
 #pragma unroll 1
-          for (int c0 = x.halves() ? 64 * s : 0; c0 < (x.halves() ? 64 * s + 64 : 128); c0 += 64) {
-            float acc[64];
+          for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+            float acc[32];
 #pragma unroll
-            for (int j = 0; j < 64; ++j) acc[j] = 0.f;
+            for (int j = 0; j < 32; ++j) acc[j] = 0.f;
             M = -INFINITY;
             L = 0.f;
+#pragma unroll 2
             for (int i = 0; i < n; ++i) {
               const int c = x.first_run + i / subs, y = sub0 + i % subs;
               const float* from = p.partials + (size_t)(2 * c + (c == x.first_run ? 1 : 0)) * kCASlotFloats;
-              const float2 v = __ldcg(reinterpret_cast<const float2*>(from + 2 * kCATile * kHeadDim) + y * kCATile + row);
-              const float4* o = reinterpret_cast<const float4*>(from) + (y * 32 + c0 / 4) * kCATile + row;
-              if (v.y == 0.f) continue;                               // (nothing was seen, and O was not written)
-              float4 w[16];
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(from + 2 * kCATile * kHeadDim) + y * kCATile + mine);
+              const float4* o = reinterpret_cast<const float4*>(from) + (y * 32 + c0 / 4) * kCATile + mine;
+              float4 w[8], low[8];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) w[j] = __ldcg(o + j * kCATile);
+              for (int j = 0; j < 8; ++j) w[j] = __ldcg(o + j * kCATile);
+              if (kFew) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) low[j] = __ldcg(o + j * kCATile + 64);
+              }
+              if (v.y == 0.f) continue;                               // (nothing was seen, and O was not written)
               const float mn = fmaxf(M, v.x), f = exp2f(M - mn), g = exp2f(v.x - mn);
               M = mn;
               L = fmaf(v.y, g, L * f);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
+              for (int j = 0; j < 8; ++j) {
+                if (kFew) w[j] = make_float4(w[j].x + low[j].x, w[j].y + low[j].y, w[j].z + low[j].z, w[j].w + low[j].w);
                 acc[4 * j] = fmaf(w[j].x, g, acc[4 * j] * f);
                 acc[4 * j + 1] = fmaf(w[j].y, g, acc[4 * j + 1] * f);
                 acc[4 * j + 2] = fmaf(w[j].z, g, acc[4 * j + 2] * f);
@@ -775,11 +773,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const float inv = L == 0.f ? 0.f : 1.f / L;
             uint4* to = reinterpret_cast<uint4*>(p.out + out_row * kHeadDim + c0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 4; ++j)
               to[j] = make_uint4(pack_bf16x2(acc[8 * j] * inv, acc[8 * j + 1] * inv), pack_bf16x2(acc[8 * j + 2] * inv, acc[8 * j + 3] * inv),
                                  pack_bf16x2(acc[8 * j + 4] * inv, acc[8 * j + 5] * inv), pack_bf16x2(acc[8 * j + 6] * inv, acc[8 * j + 7] * inv));
           }
-          if (p.out_lse && (!x.halves() || s == 0)) p.out_lse[out_row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+          if (p.out_lse && (kFew ? s == 0 && row < 64 : !x.halves() || s == 0)) p.out_lse[out_row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
         }
         softmax_bar();                   // the slot may be written again
       }
@@ -818,10 +816,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             q_par ^= 1;
           }
           if (ok) {
-            mbar_expect_tx(bar_qfull, x.halves() ? q_bytes : 2 * q_bytes);
-            for (int y = 0; y < (x.halves() ? 1 : 2); ++y)
+            mbar_expect_tx(bar_qfull, !kFew && x.halves() ? q_bytes : 2 * q_bytes);
+            for (int y = 0; y < (!kFew && x.halves() ? 1 : 2); ++y)
               for (int h = 0; h < 2; ++h)
-                tma_load_3d_plain(smem0 + y * kCATileBytes + h * kCAHalfBytes, &tm_q, 64 * h, x.kvh * p.group, x.row0 + y * p.tokens, bar_qfull);
+                tma_load_3d_plain(smem0 + y * (kFew ? kCAHalfBytes / 2 : kCATileBytes) + h * kCAHalfBytes, &tm_q, 64 * h, x.kvh * p.group,
+                                  x.row0 + (kFew ? 0 : y * p.tokens), bar_qfull);
           }
         }
         q_full = true;
@@ -971,12 +970,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           wait(bar_pfull + 16 * s, p_par[s]);
           tc_fence_after();
           if (leader && ok) umma_pv4(d, a, v, started[s] ? 1u : 0u);
-          if (kFew && leader && ok) umma_pv4(d, a + 64, v, 1u);
           wait(bar_pfull + 16 * s + 8, p_par[s]);
           p_par[s] ^= 1;
           tc_fence_after();
           if (leader && ok) umma_pv4(d, a + 32, v + 4 * ((16 * 128) >> 4), 1u);
-          if (kFew && leader && ok) umma_pv4(d, a + 96, v + 4 * ((16 * 128) >> 4), 1u);
           started[s] = true;
         };
         auto qk = [&](int s, int k_slot) {

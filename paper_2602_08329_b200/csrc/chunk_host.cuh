@@ -87,7 +87,8 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
                                   (unsigned long long)(paged ? kBlockRows : max_t);
   if (rows >= (1ull << 31) - kCATile) return fail(ctx, PRHS_ERR_UNSUPPORTED, "chunk attention: a cache of 2^31 rows or more");
   p.group = ctx->gq;
-  p.tokens = kCATile / ctx->gq;
+  const bool few = num_rows <= (long long)batch * (kCATile / 2 / ctx->gq);
+  p.tokens = (few ? kCATile / 2 : kCATile) / ctx->gq;
   alignas(64) CUtensorMap tm_q, tm_k, tm_v;
   const cuuint64_t qdim[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)hq, (cuuint64_t)num_rows}, qstr[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)hq * kRowBytes};
   const cuuint32_t qbox[3] = {64u, (cuuint32_t)p.group, (cuuint32_t)p.tokens};
@@ -113,7 +114,7 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
   {
     LaunchScope ls(ctx, PRHS_KIND_ATTN_DENSE, st);
     auto launch = [&](auto kernel) { kernel<<<ctx->sm_count, kCAThreads, kCASmemBytes, st>>>(tm_q, tm_k, tm_v, p); };
-    const bool few = num_rows <= (long long)batch * p.tokens, masks = p.window > 0 || p.psaw_c > 0.0;
+    const bool masks = p.window > 0 || p.psaw_c > 0.0;
     if (few && masks) launch(paged ? chunk_attn_kernel<true, true, true> : chunk_attn_kernel<false, true, true>);
     else if (few) launch(paged ? chunk_attn_kernel<true, false, true> : chunk_attn_kernel<false, false, true>);
     else if (masks) launch(paged ? chunk_attn_kernel<true, true, false> : chunk_attn_kernel<false, true, false>);
