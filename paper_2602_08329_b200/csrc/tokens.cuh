@@ -1,10 +1,10 @@
 // New tokens: queries and keys normalised per head and rotated by their positions, keys and values written to the cache
 // (bf16 rows, or 8-bit blocks), in one pass; and rows of the 8-bit cache read back as bf16.
 //
-// All of it is bound by HBM: a token's heads come in once and go out once (2 x 256 B per head and token; 256 + 128 B for the
-// keys and values of the 8-bit cache).  The arithmetic that could get in the way is the rotation's: 64 angles per
-// token, each a product of 24 + 31 bits reduced to a turn.  They are computed once per token and head chunk, in
-// fp64 (three operations and a conversion each), and kept in shared memory for all heads.
+// What they move: a token's heads come in once and go out once (2 x 256 B per head and token; 256 + 128 B for the keys and values of the
+// 8-bit cache).  The 64 angles of a token are computed once, in fp64, and kept in shared memory for all of its heads.  278 MB of ragged
+// image prompts take 61 to 64 us (4.4 TB/s, 0.67 of measured; 49 without the arithmetic: it is the chain of shuffles, table reads and
+// conversions of a head that is not hidden), 738 MB of two prompts into the 8-bit cache 158 us (0.71), 403 MB read back 65 us (0.94).
 #pragma once
 #include "bytekv.cuh"
 #include "common.cuh"
@@ -68,16 +68,22 @@ __device__ __forceinline__ int last_start(const int* row_start, int batch, int r
 }
 
 // ------------------------------------------------------------------------------------ heads
-// cosine and sine (times scale) of pos * inv_freq radians.  In fp64 the angle becomes quarter turns and the rest of one, which
-// is exact to 2^-52 of the angle; the rest, an eighth of a turn at most, is what fp32 has to hold.
+// cosine and sine (times scale) of pos * inv_freq radians, in fp64 until the end: the angle becomes quarter turns and the rest of one, an
+// eighth of a turn at most, whose Taylor series need eight terms for 2^-49.  (64 a row, for all of its heads: fp32 would save nothing
+// that shows, and its errors would move keys across the roundings of bf16 and of the 8-bit codes.)
 __device__ __forceinline__ float2 rotation(int pos, float inv_freq, float scale) {
   const double turns = (double)pos * ((double)inv_freq * 0.15915494309189533577);
-  const double q = rint(turns * 4.0);
-  float s, c;
-  sincospif(2.f * (float)(turns - 0.25 * q), &s, &c);
+  const double q = rint(turns * 4.0), x = (turns - 0.25 * q) * 6.283185307179586477, y = x * x;
+  double c = 1.0, s = 1.0;
+#pragma unroll
+  for (int n = 14; n >= 2; n -= 2) {
+    c = fma(c, y * (-1.0 / (n * (n - 1))), 1.0);
+    s = fma(s, y * (-1.0 / (n * (n + 1))), 1.0);
+  }
+  s *= x;
   const int quarter = (int)(long long)q & 3;
-  const float cc = quarter & 1 ? s : c, ss = quarter & 1 ? c : s;
-  return make_float2((quarter == 1 || quarter == 2 ? -cc : cc) * scale, (quarter & 2 ? -ss : ss) * scale);
+  const double cc = quarter & 1 ? s : c, ss = quarter & 1 ? c : s;
+  return make_float2((float)(quarter == 1 || quarter == 2 ? -cc : cc) * scale, (float)(quarter & 2 ? -ss : ss) * scale);
 }
 
 // two fp32 at a time
@@ -154,7 +160,10 @@ __device__ __forceinline__ void prepare_head(uint4& a, uint4& b, const PrepDev& 
     ss = __fadd_rn(ss, t);
 #pragma unroll
     for (int off = 1; off < 8; off <<= 1) ss = __fadd_rn(ss, __shfl_xor_sync(0xffffffffu, ss, off));
-    const float r = rsqrtf(fmaf(ss, 1.f / kHeadDim, p.eps));
+    // the reciprocal root, and one step of Newton's in fp64: its error would be that of all 128 values
+    const float v = fmaf(ss, 1.f / kHeadDim, p.eps), r0 = rsqrtf(v);
+    const float r1 = (float)fma(0.5 * r0, fma(-(double)v * r0, (double)r0, 1.0), (double)r0);
+    const float r = isfinite(r1) ? r1 : r0;
     rr = pack_f32x2(r, r);
   }
   if constexpr (kRot == kRotHalves) {
@@ -257,7 +266,9 @@ struct HeadPlace {
 
 // A CTA takes cta_rows rows, and every gridDim.y-th of their groups of four heads: the places of heads and rows, and the rows' angles are
 // looked up and computed by all threads once, then the heads stream through, a group per warp and step, the next two on their way
-// (from before the look-ups).
+// (from before the look-ups).  Eight rows: sixteen leave too few CTAs to even out (74 us for 278 MB against 67), four pay the look-ups
+// twice as often (66 against 61, later).  Copies through a ring in shared memory were no faster than registers (the ring's
+// wavefronts cost what its depth gains).
 template <int kRot>
 __global__ void __launch_bounds__(32 * kQkvWarps, 3) qkv_append_kernel(const __grid_constant__ QkvAppendParams p) {
   extern __shared__ uint4 qkv_smem[];
