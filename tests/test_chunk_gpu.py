@@ -383,3 +383,29 @@ def test_refusals(cuda_device):
         ctx.chunk_attn(t.qc, t.view(), 3, t.out, t.lse, **ok)
     ctx.chunk_attn(t.qc[:0], t.view(), 2, t.out[:0], t.lse[:0], row_start=torch.zeros(3, dtype=torch.int32, device=cuda_device))
     assert ctx.check() == 0 and torch.isnan(t.out).all()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_many_sequences_some_without_tokens(cuda_device, paged):
+    g = torch.Generator().manual_seed(8)
+    lens = torch.randint(0, 150, (300,), generator=g).tolist()
+    new = [min(n, int(m)) for n, m in zip(lens, torch.randint(0, 4, (300,), generator=g))]
+    new[37] = lens[37] = 140
+    t = fill(Batch(cuda_device, lens, new, 1, 2, paged))
+    call(t)
+    compare(t)
+
+
+def test_rows_of_no_sequence_alone(cuda_device):
+    """Padding only: nothing is computed, nothing written, and the next call is as ever."""
+    t = fill(Batch(cuda_device, [40, 200], [0, 0], 2, 4, False, pad_rows=300))
+    ctx = call(t)
+    assert torch.isnan(t.out).all() and torch.isnan(t.lse).all()
+    t.row_start[2] = 5
+    ctx.chunk_attn(t.qc, t.view(), 2, t.out, t.lse, row_start=t.row_start)
+    assert ctx.check() == 0 and int((~torch.isnan(t.lse[:, 0])).sum()) == 0      # (padding rows hold NaN queries: their rows are NaN)
+    prep = P.make_qk_prep()
+    t.row_start.zero_()
+    t.ck.fill_(math.nan)
+    ctx.qkv_append(t.q, t.k, t.v, t.view(), prep, 2, t.q_out, row_start=t.row_start)
+    assert ctx.check() == 0 and torch.isnan(t.ck).all() and torch.isnan(t.q_out).all()
