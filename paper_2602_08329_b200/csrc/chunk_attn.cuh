@@ -49,13 +49,13 @@ constexpr int kCASlots = 6;                               // of the ring at most
 constexpr int kCAMaxMended = 16;                          // tiles of a piece that a row sees in part: 3 + 3 + 1 at most
 constexpr int kCAPieces = 4;                              // of a CTA that are known ahead
 constexpr int kCAPieceBytes = 128;
-constexpr int kCANotes = 8;                               // pieces whose mended tiles are noted: the ring lets the mending warps run four ahead at most
+constexpr int kCANotes = 8;                               // pieces whose mended tiles are noted: the pieces known ahead let the mending warps run four ahead at most
 // What is shared beside the tiles (they leave 3 KB).
 struct ChunkShared {
   unsigned char pieces[kCAPieces][kCAPieceBytes];
   // kv_full[6], kv_empty[6], v_ready[6], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
-  // piece_full[4], piece_empty[4]
-  unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces];
+  // piece_full[4], piece_empty[4], noted[8]
+  unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces + kCANotes];
   int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];
   uint32_t tmem;
   int abort, last;
@@ -455,6 +455,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   const uint32_t bar_full = bar0, bar_empty = bar0 + 8 * kCASlots, bar_vready = bar0 + 16 * kCASlots;
   const uint32_t bar_qfull = bar0 + 24 * kCASlots, bar_qempty = bar_qfull + 8, bar_sfull = bar_qfull + 16, bar_pfull = bar_qfull + 32;
   const uint32_t bar_ofull = bar_qfull + 64, bar_oempty = bar_qfull + 80, bar_drain = bar_qfull + 96, bar_piece = bar_qfull + 104;
+  const uint32_t bar_noted = bar_piece + 16 * kCAPieces;
   if (tid == 0) {
     for (int i = 0; i < kCASlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);      // the producer's expect_tx arrive
@@ -474,6 +475,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     for (int i = 0; i < kCAPieces; ++i) {
       mbar_init(bar_piece + 8 * i, 1);                     // the producer
       mbar_init(bar_piece + 8 * (kCAPieces + i), 11);      // all other warps
+    }
+    for (int i = 0; i < kCANotes; ++i) {
+      mbar_init(bar_noted + 8 * i, 1);     // the mending warps' first thread, which writes the notes
+      sh.mended_n[i] = 0;
     }
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -645,8 +650,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       unpack_f32x2(l2, la, lb);
       const float l = la + lb;
       // ------------------------------------------------------------ the piece's result
+      // (O says nothing about the mending warps: of a piece that needs no mending the tensor core does not wait for them)
       if (any && !aborted) {
-        aborted = !__all_sync(0xffffffffu, mbar_wait(bar_ofull + 8 * s, o_par, &sh.abort));
+        aborted = !__all_sync(0xffffffffu, mbar_wait(bar_ofull + 8 * s, o_par, &sh.abort) &&
+                                               mbar_wait(bar_noted + 8 * (buf % kCANotes), (buf / kCANotes) & 1, &sh.abort));
         if (aborted && lane == 0) gave_up();
       }
       if (any) o_par ^= 1;
@@ -654,7 +661,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       const int slot = 2 * x.run + (x.first_run == x.run ? 1 : 0);
       float* const part = p.partials + (size_t)slot * kCASlotFloats;
       const long long out_row = ((long long)(x.row0 + x.a(p, s) + token) * p.num_q_heads + x.kvh * p.group + head);
-      const int mended = any ? sh.mended_n[buf % kCANotes] : 0;
+      const int mended = any && !aborted ? sh.mended_n[buf % kCANotes] : 0;
       if (!aborted && warp_used) {
         tc_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -946,6 +953,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             pos.step();
           }
         }
+        if (t64 == 0) mbar_arrive(bar_noted + 8 * (buf % kCANotes));       // (also after a wait that ran out)
         ++buf;
       }
       if (!ok && lane == 0) gave_up();

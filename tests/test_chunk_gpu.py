@@ -409,3 +409,23 @@ def test_rows_of_no_sequence_alone(cuda_device):
     t.ck.fill_(math.nan)
     ctx.qkv_append(t.q, t.k, t.v, t.view(), prep, 2, t.q_out, row_start=t.row_start)
     assert ctx.check() == 0 and torch.isnan(t.ck).all() and torch.isnan(t.q_out).all()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_short_pieces_without_mending_after_launches_with_notes(cuda_device, paged):
+    """Pieces of a few tiles that every row sees whole, on SMs whose shared memory still holds the notes of a launch that mended many: the first
+    tiles of a short cache are a piece of their own (four draft tokens over 2047 positions: two tiles), and nothing orders it but its notes' barrier."""
+    odd = fill(Batch(cuda_device, [500] * 16, [200] * 16, 2, 4, paged, pad_rows=0))
+    for b in range(16):
+        odd.full_v[b][:, 300::7, 3] = math.inf
+    store(odd)
+    ctx = P.Context(num_layers=1, max_batch=16, num_q_heads=8, num_kv_heads=2, max_context=2048, max_k=1, max_window=1, max_sinks=4,
+                    page_size=16 if paged else 0)
+    for lens, new in (([2047], [4]), ([2047, 300, 900], [4, 1, 2]), ([2047] * 12, [60] * 12)):
+        t = fill(Batch(cuda_device, lens, new, 2, 4, paged, pad_rows=0), seed=len(lens))
+        for _ in range(20):
+            ctx.chunk_attn(odd.qc, odd.view(), 16, odd.out, odd.lse, row_start=odd.row_start)
+            ctx.chunk_attn(t.qc, t.view(), t.B, t.out, t.lse, row_start=t.row_start)
+            t.out.clone()
+        assert ctx.check() == 0
+        compare(t)
