@@ -8,6 +8,7 @@
 #pragma once
 #include "bytekv.cuh"
 #include "common.cuh"
+#include "seq_rows.cuh"
 
 namespace prhs {
 
@@ -31,21 +32,6 @@ struct PrepDev {
 constexpr int kRotHalves = 0, kRotAdjacent = 1, kRotPartial = 2;
 
 // ------------------------------------------------------------------------------- sequences of rows
-// New tokens of sequence b: rows [r0, r1), positions [t - n, t).  ok: they fit together.
-struct SeqRows {
-  int r0, n, t;
-  bool ok;
-};
-__device__ __forceinline__ SeqRows seq_rows(const int* row_start, int num_rows, const int* seq_lens, int max_len, int b) {
-  SeqRows s;
-  int r1;
-  s.r0 = row_start ? __ldg(row_start + b) : b;
-  r1 = row_start ? __ldg(row_start + b + 1) : b + 1;
-  s.t = __ldg(seq_lens + b);
-  s.ok = s.r0 >= 0 && r1 >= s.r0 && r1 <= num_rows && r1 - s.r0 <= s.t && s.t <= max_len;
-  s.n = s.ok ? r1 - s.r0 : 0;
-  return s;
-}
 // One CTA of a launch: records sequences that do not fit.
 __device__ __forceinline__ void record_bad_sequences(const int* row_start, int num_rows, const int* seq_lens, int max_len, int batch,
                                                      uint32_t* flags) {
