@@ -1534,6 +1534,9 @@ prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags) {
   cudaStream_t st = as_stream(stream);
   uint32_t f = 0;
   PRHS_CUDA(ctx, cudaMemcpyAsync(&f, ctx->flags, sizeof(f), cudaMemcpyDeviceToHost, st));
+  // Tickets go back to zero with an item's last piece.  Pieces that were never published (a wait that ran out, lengths that changed while a
+  // call was under way, which not every change shows in a flag) would have the next call merge what has not arrived.
+  PRHS_CUDA(ctx, cudaMemsetAsync(ctx->chunk_tickets, 0, (size_t)ctx->chunk_rounds * ctx->sm_count * sizeof(unsigned int), st));
   PRHS_CUDA(ctx, cudaStreamSynchronize(st));
   PRHS_CUDA(ctx, cudaGetLastError());
   if (out_flags) *out_flags = f;

@@ -429,3 +429,30 @@ def test_short_pieces_without_mending_after_launches_with_notes(cuda_device, pag
             t.out.clone()
         assert ctx.check() == 0
         compare(t)
+
+
+def test_calls_are_sound_again_after_lengths_changed_under_way(cuda_device):
+    """Another stream sets lengths while calls of several rounds are under way; after a check the next call is as ever."""
+    lens, new = [30000, 25000], [900, 1500]
+    t = fill(Batch(cuda_device, lens, new, 8, 4, False, pad_rows=0))
+    ctx = t.ctx()
+    call(t, ctx)
+    want = t.out.clone(), t.lse.clone()
+    other = torch.cuda.Stream()
+    for i, wrong in enumerate(([3000, 2000], [30000, 30000], [900, 1500], [25000, 30000]) * 3):
+        n = torch.tensor(wrong, dtype=torch.int32, device=cuda_device)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            ctx.chunk_attn(t.qc, t.view(), 2, t.out, t.lse, row_start=t.row_start)
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(200000 + 150000 * i)
+            t.lens_t.copy_(n)
+        torch.cuda.synchronize()
+        try:
+            ctx.check()
+        except P.PrhsError as e:
+            assert e.status == 7
+        t.lens_t.copy_(torch.tensor(lens, dtype=torch.int32))
+        call(t, ctx)
+        for a, b in zip(want, (t.out, t.lse)):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
