@@ -163,7 +163,8 @@ gather_attn_tma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
   const float sc = kScale * kLog2e;
   const int lm_mi = lane >> 3, lm_r = lane & 7;
   const int vrow = (lm_mi & 1) * 8 + lm_r;
-  for (int i = 0; i < nstages; ++i) {
+  int i = 0;
+  for (; i < nstages; ++i) {
     const int slot_i = i % kATStages;
     if (!__all_sync(0xffffffffu, mbar_wait(bar0 + 8 * slot_i, (i / kATStages) & 1, &sh_abort))) {
       if (lane == 0) { atomicOr(p.flags, kFlagTimeout); sh_abort = 1; }
@@ -255,15 +256,9 @@ gather_attn_tma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
   }
   if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; sm_lt[warp] = lt; }
   __syncthreads();
-  // after an aborted wait copies may still be in flight towards this CTA's shared memory: one
-  // more bounded wait per barrier of the warp before anybody returns
-  if (sh_abort && lane == 0) {
-    for (int s = 0; s < kATStages; ++s) {
-      const long long t0 = clock64();
-      while (!mbar_try_wait(bar0 + 8 * s, 0) && !mbar_try_wait(bar0 + 8 * s, 1))
-        if (clock64() - t0 > kWaitBudgetCycles / 8) break;
-    }
-  }
+  // after an aborted wait copies may still be in flight towards this CTA's shared memory: a
+  // bounded wait for the latest fill of each of the warp's slots (it is kATStages - 1 stages ahead) before anybody returns
+  if (sh_abort && lane == 0) mbar_drain_ring(bar0, kATStages, min(nstages, i + kATStages - 1));
   if (sh_abort) __syncthreads();
   {
     float M = -INFINITY;

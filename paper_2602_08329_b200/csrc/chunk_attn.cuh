@@ -59,6 +59,7 @@ struct ChunkShared {
   int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];
   uint32_t tmem;
   int abort, last;
+  int fills, q_fills;              // of the ring; of Q, but for multiples of two (for the drain)
 };
 constexpr int kCASmemBytes = kCATiles * kCATileBytes + (int)sizeof(ChunkShared);
 constexpr int kCAThreads = 12 * 32;
@@ -568,7 +569,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (lane == 0) {
           if (q_full) {
             ok = mbar_wait(bar_qempty, q_par, &sh.abort);
-            q_par ^= 1;
+            if (ok) q_par ^= 1;
           }
           if (ok) {
             mbar_expect_tx(bar_qfull, !kFew && x.halves() ? q_bytes : 2 * q_bytes);
@@ -632,6 +633,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       }
       if (walk.changed() && lane == 0) atomicOr(p.flags, kFlagBadLength);
       if (lane == 0) {                   // the end
+        sh.fills = fills;
+        sh.q_fills = q_full ? (int)q_par + 1 : 0;
         x.k0 = x.k1 = -1;
         *reinterpret_cast<Piece<kMask, kFew>*>(sh.pieces[piece_at % kCAPieces]) = x;
         mbar_arrive(bar_piece + 8 * (piece_at % kCAPieces));
@@ -822,13 +825,10 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   if (sh.abort) {
     // copies and MMAs may still be in flight: bounded waits before shared and tensor memory go back
     if (tid == kCALoadWarp * 32) {
-      for (int i = 0; i < kCASlots; ++i) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(bar_full + 8 * i, 0) && !mbar_try_wait(bar_full + 8 * i, 1))
-          if (clock64() - t0 > kWaitBudgetCycles / 8) break;
-      }
+      mbar_drain_ring(bar_full, kSlots, sh.fills);
+      mbar_drain_ring(bar_qfull, 1, sh.q_fills);
     }
-    if (tid == kCAMmaWarp * 32) {
+    if (warp == kCAMmaWarp && elect_one()) {           // (a commit is of the MMAs of the thread that makes it)
       umma_commit(bar_drain);
       const long long t0 = clock64();
       while (!mbar_try_wait(bar_drain, 0))

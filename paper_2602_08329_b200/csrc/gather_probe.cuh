@@ -156,7 +156,8 @@ gather_probe_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
       }
     };
     for (int s = 0; s < kGPStages - 1; ++s) issue(s);
-    for (int i = 0; i < nstages; ++i) {
+    int i = 0;
+    for (; i < nstages; ++i) {
       const int slot_i = i % kGPStages;
       if (!__all_sync(0xffffffffu, mbar_wait(bar0 + 8 * slot_i, (i / kGPStages) & 1, &sh_abort))) {
         if (lane == 0) { atomicOr(p.flags, kFlagTimeout); sh_abort = 1; }
@@ -170,13 +171,7 @@ gather_probe_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     }
     // after an aborted wait copies may still be in flight towards this CTA's shared memory
     __syncthreads();
-    if (sh_abort && lane == 0) {
-      for (int s = 0; s < kGPStages; ++s) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(bar0 + 8 * s, 0) && !mbar_try_wait(bar0 + 8 * s, 1))
-          if (clock64() - t0 > kWaitBudgetCycles / 8) break;
-      }
-    }
+    if (sh_abort && lane == 0) mbar_drain_ring(bar0, kGPStages, min(nstages, i + kGPStages - 1));
   }
   if (acc == 0x9e3779b9u && cnt < 0) *p.sink = acc;      // never true: keeps the reads alive
 }

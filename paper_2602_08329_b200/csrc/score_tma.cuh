@@ -61,6 +61,9 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const v
     if (*abort || clock64() - t0 > budget) return false;
   return true;
 }
+}  // namespace prhs
+#include "mbar_drain.cuh"
+namespace prhs {
 // The key stream is read once and is far larger than L2: its lines are marked evict-first, and
 // the logits (a few tens of MB that the selection kernel reads next) evict-last, so that the
 // stream does not push the logits out to DRAM before they are used.
@@ -98,7 +101,7 @@ score_tma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
   extern __shared__ unsigned char st_smem_raw[];
   __shared__ __align__(8) unsigned long long bars[2 * kSTStages];     // full[0..NS), empty[NS..2NS)
   __shared__ float sm_m[kSTConsumers][16], sm_l[kSTConsumers][16];
-  __shared__ int sh_abort;
+  __shared__ int sh_abort, sh_fills;
   const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
   const int gq = p.group_size;
   const int head0 = kvh * gq;
@@ -147,7 +150,8 @@ score_tma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
     const uint64_t pol_k = l2_policy_evict_first();
     if (!kPaged) {
       if (lane == 0) {
-        for (int j = 0; j < nstages; ++j) {
+        int j = 0;
+        for (; j < nstages; ++j) {
           const int slot = j % kSTStages;
           if (j >= kSTStages && !mbar_wait(bar0 + 8 * (kSTStages + slot), ((j / kSTStages) - 1) & 1, &sh_abort)) {
             atomicOr(p.flags, kFlagTimeout);
@@ -161,13 +165,15 @@ score_tma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
           tma_load_2d(dst, &tm_k, 0, row_base + j * kSTStageRows, full, pol_k);
           tma_load_2d(dst + kSTHalfBytes, &tm_k, 64, row_base + j * kSTStageRows, full, pol_k);
         }
+        sh_fills = j;
       }
     } else {
       const int x = (lane >> 1) & 3, half = lane & 1;   // lanes 0-7: page x of the stage, 64-column half
       const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride + (start >> kPageShift) + x;
       bool have_next = lane < 8 && start + 16 * x < end;
       int pg_next = have_next ? __ldg(ptab) : 0;
-      for (int j = 0; j < nstages; ++j) {
+      int j = 0;
+      for (; j < nstages; ++j) {
         const int slot = j % kSTStages;
         const int pg = pg_next;
         const bool have = have_next;                // false: past the end, or lane >= 8
@@ -195,6 +201,7 @@ score_tma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
           tma_load_2d(dst, &tm_k, 64 * half, pg * outer_rows + row_base, full, pol_k);
         }
       }
+      if (lane == 0) sh_fills = j;
     }
   } else {
     // ---------------- consumers: 8 kSTNT keys of every stage per warp
@@ -293,14 +300,8 @@ score_tma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
     p.part_ml[((long long)b * p.num_q_heads + head0 + tid) * p.splits + split] = make_float2(mm, ll);
   }
   // After an aborted wait some copies may still be in flight towards this CTA's shared
-  // memory: give each full barrier one more bounded wait before the CTA returns.
-  if (sh_abort && tid == 0) {
-    for (int s = 0; s < kSTStages; ++s) {
-      const long long t0 = clock64();
-      while (!mbar_try_wait(bar0 + 8 * s, 0) && !mbar_try_wait(bar0 + 8 * s, 1))
-        if (clock64() - t0 > kWaitBudgetCycles / 8) break;
-    }
-  }
+  // memory: a bounded wait for each slot's latest fill before the CTA returns.
+  if (sh_abort && tid == 0) mbar_drain_ring(bar0, kSTStages, sh_fills);
 }
 
 // Self-test of the bounded wait: one thread waits on a barrier phase that nothing completes,

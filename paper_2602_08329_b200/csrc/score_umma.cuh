@@ -91,7 +91,7 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
   __shared__ __align__(8) unsigned long long bars[2 * kSUStages + 5];
   __shared__ float sm_m[4][kSUHeads], sm_l[4][kSUHeads];
   __shared__ uint32_t tmem_slot;
-  __shared__ int sh_abort;
+  __shared__ int sh_abort, sh_fills;
   const int split = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
   const int gq = p.group_size;
   const int head0 = kvh * gq;
@@ -162,7 +162,8 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
     const uint64_t pol_k = l2_policy_evict_first();
     if (!kPaged) {
       if (lane == 0) {
-        for (int j = 0; j < ntiles; ++j) {
+        int j = 0;
+        for (; j < ntiles; ++j) {
           const int slot = j % kSUStages;
           if (j >= kSUStages && !mbar_wait(bar_empty + 8 * slot, ((j / kSUStages) - 1) & 1, &sh_abort)) {
             atomicOr(p.flags, kFlagTimeout);
@@ -176,6 +177,7 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
           tma_load_2d(dst, &tm_k, 0, row_base + j * kSUTileRows, full, pol_k);
           tma_load_2d(dst + kSUHalfBytes, &tm_k, 64, row_base + j * kSUTileRows, full, pol_k);
         }
+        sh_fills = j;
       }
     } else {
       // lanes 0-15: page x of the tile's eight, 64-column half
@@ -183,7 +185,8 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
       const int* ptab = p.kv.page_table + (long long)b * p.kv.page_table_stride + (start >> kPageShift) + x;
       bool have_next = lane < 16 && start + 16 * x < end;
       int pg_next = have_next ? __ldg(ptab) : 0;
-      for (int j = 0; j < ntiles; ++j) {
+      int j = 0;
+      for (; j < ntiles; ++j) {
         const int slot = j % kSUStages;
         const int pg = pg_next;
         const bool have = have_next;
@@ -208,6 +211,7 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
           tma_load_2d(dst, &tm_k, 64 * half, pg * outer_rows + row_base, full, pol_k);
         }
       }
+      if (lane == 0) sh_fills = j;
     }
   } else if (warp == 1) {
     // ---------------- MMA issue: one thread
@@ -301,17 +305,11 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tm_k, ScoreParams p) {
     for (int w = 0; w < 4; ++w) ml_combine(mm, ll, sm_m[w][tid], sm_l[w][tid]);
     p.part_ml[((long long)b * p.num_q_heads + head0 + tid) * p.splits + split] = make_float2(mm, ll);
   }
-  // After an aborted wait copies and MMAs may still be in flight: give each full barrier one more
-  // bounded wait, and the tensor core a bounded wait on a last commit, before the tensor memory
+  // After an aborted wait copies and MMAs may still be in flight: a bounded wait for each slot's latest
+  // fill, and one on a last commit of the thread that issued the MMAs, before the tensor memory
   // is handed back.
   if (sh_abort) {
-    if (tid == 0) {
-      for (int s = 0; s < kSUStages; ++s) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(bar_full + 8 * s, 0) && !mbar_try_wait(bar_full + 8 * s, 1))
-          if (clock64() - t0 > kWaitBudgetCycles / 8) break;
-      }
-    }
+    if (tid == 0) mbar_drain_ring(bar_full, kSUStages, sh_fills);
     if (tid == 32) {
       umma_commit(bar_drain);
       const long long t0 = clock64();
