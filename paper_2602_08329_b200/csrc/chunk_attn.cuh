@@ -162,7 +162,11 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// (an aligned barrier, as the loads and stores of tensor memory are: all lanes of a warp at once)
+__device__ __forceinline__ void softmax_bar() {
+  __syncwarp();
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+}
 
 // Ring position: slot and the parity of its fill.
 template <int kSlots>
@@ -231,6 +235,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   }
   static_assert(sizeof(Piece<kMask, kFew>) <= kCAPieceBytes, "a piece has its place in shared memory");
   if (warp == kCAMmaWarp) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"((uint32_t)__cvta_generic_to_shared(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -249,6 +254,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     x = *reinterpret_cast<const Piece<kMask, kFew>*>(sh.pieces[i]);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_piece + 8 * (kCAPieces + i));
+    __syncwarp();
     ++piece_at;
     return x.k1 >= 0;
   };
@@ -381,6 +387,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(bar_pfull + 16 * s + 8 * h);
+              __syncwarp();
             }
           };
           if (kFew && row >= 64) weights(SlotC<1>());
@@ -415,6 +422,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t r[32];
+          __syncwarp();                  // (rows differ in what they add and whether they write)
           if (any) {
             tmem_ld32(tm_o + 32 * c, r);
             tmem_wait_ld(r);
@@ -650,6 +658,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       while (take()) {         // (a warp that gave up goes on through the barriers of the other)
         if (x.k0 == x.k1) continue;
         if (t64 == 0) sh.mended_n[buf % kCANotes] = 0;
+        __syncwarp();
         asm volatile("bar.sync 2, 64;" ::: "memory");
         PRHS_CHUNK_STEPS(x, k) {
           const int prev = k - lag_;

@@ -456,3 +456,25 @@ def test_calls_are_sound_again_after_lengths_changed_under_way(cuda_device):
         call(t, ctx)
         for a, b in zip(want, (t.out, t.lse)):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_lanes_of_a_warp_with_notes_of_their_own(cuda_device):
+    """Rows of a warp that differ in how many noted positions they see (loops of their own length between loads of tensor memory), in a group that
+    leaves rows of the warp unused."""
+    for group, paged in ((7, False), (3, True), (1, False)):
+        t = fill(Batch(cuda_device, [400, 65], [390, 65], 1, group, paged))
+        for b in range(2):
+            t.full_v[b][0, 1::2, 5] = math.nan
+            t.full_v[b][0, 64, 99] = math.inf
+        store(t)
+        call(t)
+        out, lse, tol, ltol = reference(t)
+        for b, (r0, n, T) in enumerate(((0, 390, 400), (390, 65, 65))):
+            u = torch.arange(T - n + 1, T + 1, device=t.dev)
+            got, want, near = (x[r0:r0 + n].double().clone() for x in (t.out, out, tol))
+            assert torch.isnan(got[u > 1][..., 5]).all() and torch.isfinite(got[u == 1]).all()
+            assert (got[u > 64][..., 99] == math.inf).all()
+            got[u > 1, :, 5] = want[u > 1, :, 5]
+            got[u > 64, :, 99] = want[u > 64, :, 99]
+            assert ((got - want).abs() <= near).all()
+            assert ((t.lse[r0:r0 + n].double() - lse[r0:r0 + n]).abs() <= ltol[r0:r0 + n]).all()
