@@ -516,8 +516,8 @@ typedef struct {
  *   row_start  device [batch + 1], ascending, or NULL: one row per sequence (num_rows = batch)
  *   mask       NULL: every token sees all positions before it and its own
  * A token that sees nothing (sinks = 0, P = u), or nothing but logits of -inf, has a zero row and lse = -inf.  A NaN or +inf logit makes the
- * row and its lse NaN; a value that is infinite or NaN makes its coordinate infinite or NaN for the tokens that see it, and
- * for no others.  A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE); its rows count as zeros.
+ * row and its lse NaN; a value that is infinite or NaN makes its coordinate infinite or NaN for the tokens that see it (also where its
+ * weight is zero), and for no others.  A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE); its rows count as zeros.
  * seq_lens and row_start are read more than once and must not change while the call is under way.  If they do, its results mean nothing, the change
  * is recorded (PRHS_FLAG_BAD_LENGTH) where it is noticed, and calls are sound again after a prhs_check.
  * PRHS_ERR_UNSUPPORTED where the driver offers no tensor-map encoder. */

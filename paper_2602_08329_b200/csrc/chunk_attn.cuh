@@ -56,7 +56,7 @@ struct ChunkShared {
   // kv_full[6], kv_empty[6], v_ready[6], q_full, q_empty, s_full[2], p_full[2][2] (halves of a tile's weights), o_full[2], o_empty[2], drain,
   // piece_full[4], piece_empty[4], noted[8]
   unsigned long long bars[3 * kCASlots + 13 + 2 * kCAPieces + kCANotes];
-  int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];
+  int mended_n[kCANotes], mended_tile[kCANotes][kCAMaxMended];      // 2 * tile + (its place in the piece, odd or even)
   uint32_t tmem;
   int abort, last;
   int fills, q_fills;              // of the ring; of Q, but for multiples of two (for the drain)
@@ -432,7 +432,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           }
           // values that are not finite and were kept out of the product: infinite or NaN whatever their weight
           for (int y = 0; y < mended; ++y) {
-            const int at = sh.mended_tile[buf % kCANotes][y] * kCATile;
+            const int note = sh.mended_tile[buf % kCANotes][y], at = (note >> 1) * kCATile;
+            if (x.halves() && (note & 1) != s) continue;               // (the other accumulator's tile)
             for (int i = at; i < min(at + kCATile, u); ++i) {
               if (i >= p.sinks && i < from) continue;
               long long off = (long long)x.b * p.kv.stride_outer + (long long)i * kHeadDim;
@@ -470,7 +471,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           if (whole) {
             if (p.out_lse) p.out_lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
           } else {
-            __stcg(reinterpret_cast<float2*>(part + 2 * kCATile * kHeadDim) + s * kCATile + row, make_float2(m, l));
+            __stcg(reinterpret_cast<float2*>(part + 2 * kCATile * kHeadDim) + s * kCATile + row, make_float2(m, any ? l : -1.f));
           }
         }
         tc_fence_before();
@@ -521,8 +522,11 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll
                 for (int j = 0; j < 8; ++j) low[j] = __ldcg(o + j * kCATile + 64);
               }
-              if (v.y == 0.f) continue;                               // (nothing was seen, and O was not written)
-              const float mn = fmaxf(M, v.x), f = exp2f(M - mn), g = exp2f(v.x - mn);
+              if (v.y < 0.f) continue;                                // (no tiles, and O was not written)
+              // A piece whose logits are all -inf has no weight, but still zero times its values that are not finite.
+              const float mn = fmaxf(M, v.x);
+              const bool none = mn == -INFINITY;
+              const float f = none ? 1.f : exp2f(M - mn), g = none ? 1.f : exp2f(v.x - mn);
               M = mn;
               L = fmaf(v.y, g, L * f);
 #pragma unroll
@@ -695,7 +699,7 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               if (any_odd && t64 == 0) {
                 const int n = sh.mended_n[buf % kCANotes];
                 if (n < kCAMaxMended) {
-                  sh.mended_tile[buf % kCANotes][n] = x.tile(prev);
+                  sh.mended_tile[buf % kCANotes][n] = 2 * x.tile(prev) + ((prev - x.k0) & 1);
                   sh.mended_n[buf % kCANotes] = n + 1;
                 }
               }

@@ -478,3 +478,31 @@ def test_lanes_of_a_warp_with_notes_of_their_own(cuda_device):
             got[u > 64, :, 99] = want[u > 64, :, 99]
             assert ((got - want).abs() <= near).all()
             assert ((t.lse[r0:r0 + n].double() - lse[r0:r0 + n]).abs() <= ltol[r0:r0 + n]).all()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("length,new,group", [(20000, 2, 4), (700, 3, 7), (300, 300, 2), (9000, 200, 4), (40, 40, 1)])
+def test_values_that_are_not_finite_where_all_logits_are_minus_infinity(cuda_device, length, new, group, paged):
+    """Zero times an infinity or a NaN is NaN, in whichever piece of the work it lies: the coordinate is not finite for all that see it, the others
+    are as without it.  A token that sees such logits alone has lse = -inf and zeros elsewhere."""
+    gone = length // 2
+    t = fill(Batch(cuda_device, [length], [new], 2, group, paged, pad_rows=0), k_amp=0.5)
+    t.qc[:, :, 0] = 1.0
+    t.full_k[0][:, :gone, 0] = -math.inf
+    odd = [(0, 0, 3, math.inf), (0, gone - 1, 70, math.nan), (1, gone // 2, 127, -math.inf), (1, gone - 1, 9, math.inf)]
+    for h, pos, d, x in odd:
+        t.full_v[0][h, pos, d] = x
+    store(t)
+    call(t)
+    out, lse, tol, ltol = reference(t)
+    got, gl = t.out.double(), t.lse.double()
+    u = torch.arange(length - new + 1, length + 1, device=t.dev)
+    where = torch.zeros_like(got, dtype=torch.bool)
+    for h, pos, d, x in odd:
+        where[u > pos, h * group:(h + 1) * group, d] = True
+    assert torch.isfinite(got[~where]).all() and not torch.isfinite(got[where]).any()
+    tol = torch.nan_to_num(tol, nan=math.inf)
+    empty = u <= gone
+    assert not got[empty][~where[empty]].any() and (gl[empty] == -math.inf).all()
+    assert ((got - out).abs()[~empty] <= tol[~empty])[~where[~empty]].all()
+    assert ((gl - lse).abs()[~empty] <= ltol[~empty]).all()
