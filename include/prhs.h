@@ -46,7 +46,7 @@ typedef enum {
   PRHS_OK = 0,
   PRHS_ERR_INVALID_ARG = 1, /* NULL pointer, bad shape, value out of the configured range */
   PRHS_ERR_UNSUPPORTED = 2, /* head_dim != 128, page_size not in {0,16}, group size > 16   */
-  PRHS_ERR_OOM = 3,         /* prhs_create could not allocate its workspaces               */
+  PRHS_ERR_OOM = 3,         /* prhs_create could not allocate its workspaces (or that of this call) */
   PRHS_ERR_CUDA = 4,        /* a CUDA runtime call failed; see prhs_last_error             */
   PRHS_ERR_STATE = 5,       /* no shared set for this block/group (leader not called yet)   */
   PRHS_ERR_CAPACITY = 6,    /* batch, k, window, ... exceed what prhs_create was given      */
@@ -107,6 +107,11 @@ typedef struct {
                               of 128-row tiles leave room for one deep or two shallow CTAs per SM,
                               where the mma.sync kernel pipelines 16-row stages per warp.  Kept for the
                               comparison. */
+
+#define PRHS_CFG_NO_CHUNK_ATTN 16u /* no workspace for prhs_chunk_attn (39 MB on 148 SMs, 79 to 158 MB for caches of more
+                              than 131072 positions over all sequences and KV heads), which then returns PRHS_ERR_UNSUPPORTED.  Without
+                              the flag a context that finds no memory for that workspace (or for less of it) is
+                              created all the same, and prhs_chunk_attn returns PRHS_ERR_OOM. */
 
 /* A view of one layer's KV cache (device memory, bf16, caller-owned).
  *   contiguous (page_table == NULL): row i of (b, kvh) is at
@@ -520,7 +525,8 @@ typedef struct {
  * weight is zero), and for no others.  A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE); its rows count as zeros.
  * seq_lens and row_start are read more than once and must not change while the call is under way.  If they do, its results mean nothing, the change
  * is recorded (PRHS_FLAG_BAD_LENGTH) where it is noticed, and calls are sound again after a prhs_check.
- * PRHS_ERR_UNSUPPORTED where the driver offers no tensor-map encoder. */
+ * PRHS_ERR_UNSUPPORTED where the driver offers no tensor-map encoder, or with PRHS_CFG_NO_CHUNK_ATTN; PRHS_ERR_OOM where prhs_create had no memory
+ * for the workspace. */
 prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_start, int32_t num_rows, const prhs_kv_view* kv,
                             const prhs_chunk_mask* mask, int32_t batch, void* out, float* out_lse, void* stream);
 

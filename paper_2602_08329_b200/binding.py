@@ -32,6 +32,7 @@ PRHS_CFG_NO_TMA = 1
 PRHS_CFG_TMA_GATHER = 2
 PRHS_CFG_MMA_SYNC_SCORE = 4
 PRHS_CFG_GROUP_TCGEN05 = 8
+PRHS_CFG_NO_CHUNK_ATTN = 16
 
 # every symbol include/prhs.h declares
 EXPORTS = ["prhs_create", "prhs_destroy", "prhs_score_topk", "prhs_build_index_set",

@@ -28,6 +28,27 @@ int chunk_rounds(const prhs_config& cfg) {
   return (int)std::min<long long>(kCAMaxRounds, (tiles + kCARoundTiles - 1) / kCARoundTiles);
 }
 
+// The workspace: for as many rounds as there is memory for (fewer read more of a long cache from DRAM).  Without any the
+// context serves all other calls.
+cudaError_t chunk_alloc(prhs_ctx* c) {
+  for (int rounds = chunk_rounds(c->cfg); rounds > 0; rounds /= 2) {
+    const size_t runs = (size_t)rounds * c->sm_count;
+    cudaError_t e = dev_alloc(&c->chunk_part, 2 * runs * kCASlotFloats);
+    if (e == cudaSuccess) {
+      e = dev_alloc(&c->chunk_tickets, runs);
+      if (e == cudaSuccess) {
+        c->chunk_rounds = rounds;
+        return cudaMemset(c->chunk_tickets, 0, runs * sizeof(unsigned int));
+      }
+      cudaFree(c->chunk_part);
+      c->chunk_part = nullptr;
+    }
+    if (e != cudaErrorMemoryAllocation) return e;
+    cudaGetLastError();
+  }
+  return cudaSuccess;
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
@@ -79,6 +100,8 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
     p.window = mask->window;
   }
   if (!ctx->encode_tiled) return fail(ctx, PRHS_ERR_UNSUPPORTED, "chunk attention: the driver offers no tensor-map encoder");
+  if (ctx->cfg.flags & PRHS_CFG_NO_CHUNK_ATTN) return fail(ctx, PRHS_ERR_UNSUPPORTED, "chunk attention: the context was created with PRHS_CFG_NO_CHUNK_ATTN");
+  if (!ctx->chunk_tickets) return fail(ctx, PRHS_ERR_OOM, "chunk attention: prhs_create had no memory for its workspace");
   if (!ctx->chunk_fits) return fail(ctx, PRHS_ERR_UNSUPPORTED, "chunk attention: built with fewer registers than its warps share out");
   if (num_rows == 0) return PRHS_OK;
   const bool paged = kv->page_table != nullptr;

@@ -71,7 +71,7 @@ struct prhs_ctx {
   float* chunk_part = nullptr;      // pieces of items that runs of the chunk attention share, two per run
   unsigned int* chunk_tickets = nullptr;
   bool chunk_fits = false;
-  int chunk_rounds = 1;
+  int chunk_rounds = 0;             // that the workspace has room for
   int* idx = nullptr;
   int* count = nullptr;
   uint32_t* flags = nullptr;
@@ -738,7 +738,7 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (cfg->num_q_heads / cfg->num_kv_heads > 16) return fail(nullptr, PRHS_ERR_UNSUPPORTED, "group size above 16");
   if (cfg->max_context > kMaxContext) return fail(nullptr, PRHS_ERR_UNSUPPORTED, "max_context above 2^20");
   if (cfg->max_k > 65536) return fail(nullptr, PRHS_ERR_UNSUPPORTED, "max_k above 65536");
-  if (cfg->flags & ~(PRHS_CFG_NO_TMA | PRHS_CFG_TMA_GATHER | PRHS_CFG_MMA_SYNC_SCORE | PRHS_CFG_GROUP_TCGEN05)) return fail(nullptr, PRHS_ERR_INVALID_ARG, "prhs_create: unknown configuration flag");
+  if (cfg->flags & ~(PRHS_CFG_NO_TMA | PRHS_CFG_TMA_GATHER | PRHS_CFG_MMA_SYNC_SCORE | PRHS_CFG_GROUP_TCGEN05 | PRHS_CFG_NO_CHUNK_ATTN)) return fail(nullptr, PRHS_ERR_INVALID_ARG, "prhs_create: unknown configuration flag");
 
   prhs_ctx* c = new (std::nothrow) prhs_ctx();
   if (!c) return fail(nullptr, PRHS_ERR_OOM, "host allocation failed");
@@ -837,7 +837,6 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = cudaEventCreateWithFlags(&c->ev_fork, cudaEventDisableTiming);
   if (e == cudaSuccess) e = cudaEventCreateWithFlags(&c->ev_join, cudaEventDisableTiming);
   const size_t U = units_max(c), G = c->num_groups;
-  c->chunk_rounds = chunk_rounds(*cfg);
   if (e == cudaSuccess) e = dev_alloc(&c->scores, U * c->ld);
   if (e == cudaSuccess) e = dev_alloc(&c->part_ml, U * std::max(c->max_chunks, kMaxSplits));
   if (e == cudaSuccess) e = dev_alloc(&c->lse_full, U);
@@ -845,9 +844,6 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = dev_alloc(&c->partials, U * kMaxSplits * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->stream_part, (size_t)2 * k8MaxCtasPerSm * c->sm_count * c->gq * kPartStride);
   if (e == cudaSuccess) e = dev_alloc(&c->tickets, U);
-  if (e == cudaSuccess) e = dev_alloc(&c->chunk_part, (size_t)2 * c->chunk_rounds * c->sm_count * kCASlotFloats);
-  if (e == cudaSuccess) e = dev_alloc(&c->chunk_tickets, (size_t)c->chunk_rounds * c->sm_count);
-  if (e == cudaSuccess) e = cudaMemset(c->chunk_tickets, 0, (size_t)c->chunk_rounds * c->sm_count * sizeof(unsigned int));
   if (e == cudaSuccess) e = dev_alloc(&c->idx, U * c->idx_cap);
   if (e == cudaSuccess) e = dev_alloc(&c->count, U);
   if (e == cudaSuccess) e = dev_alloc(&c->flags, 1);
@@ -879,6 +875,8 @@ prhs_status prhs_create(const prhs_config* cfg, prhs_ctx** out) {
   if (e == cudaSuccess) e = cudaMemset(c->g_slot, 0, G * U * sizeof(int));
   if (e == cudaSuccess) e = cudaMemset(c->g_ref, 0xff, G * U * sizeof(int));
   if (e == cudaSuccess) e = cudaMemset(c->count, 0, U * sizeof(int));
+  // last, and no reason to fail: what the other calls need is there
+  if (e == cudaSuccess && !(cfg->flags & PRHS_CFG_NO_CHUNK_ATTN)) e = chunk_alloc(c);
   if (e != cudaSuccess) {
     std::string msg = std::string("prhs_create: ") + cudaGetErrorString(e);
     const bool oom = (e == cudaErrorMemoryAllocation);
@@ -1536,7 +1534,8 @@ prhs_status prhs_check(prhs_ctx* ctx, void* stream, uint32_t* out_flags) {
   PRHS_CUDA(ctx, cudaMemcpyAsync(&f, ctx->flags, sizeof(f), cudaMemcpyDeviceToHost, st));
   // Tickets go back to zero with an item's last piece.  Pieces that were never published (a wait that ran out, lengths that changed while a
   // call was under way, which not every change shows in a flag) would have the next call merge what has not arrived.
-  PRHS_CUDA(ctx, cudaMemsetAsync(ctx->chunk_tickets, 0, (size_t)ctx->chunk_rounds * ctx->sm_count * sizeof(unsigned int), st));
+  if (ctx->chunk_tickets)
+    PRHS_CUDA(ctx, cudaMemsetAsync(ctx->chunk_tickets, 0, (size_t)ctx->chunk_rounds * ctx->sm_count * sizeof(unsigned int), st));
   PRHS_CUDA(ctx, cudaStreamSynchronize(st));
   PRHS_CUDA(ctx, cudaGetLastError());
   if (out_flags) *out_flags = f;

@@ -506,3 +506,67 @@ def test_values_that_are_not_finite_where_all_logits_are_minus_infinity(cuda_dev
     assert not got[empty][~where[empty]].any() and (gl[empty] == -math.inf).all()
     assert ((got - out).abs()[~empty] <= tol[~empty])[~where[~empty]].all()
     assert ((gl - lse).abs()[~empty] <= ltol[~empty]).all()
+
+
+def test_a_context_without_the_workspace(cuda_device):
+    """PRHS_CFG_NO_CHUNK_ATTN: attention of many tokens is refused, its memory is not taken, and everything else runs."""
+    t = fill(Batch(cuda_device, [300, 40], [1, 1], 2, 4, False, pad_rows=0))
+    make = lambda flags: P.Context(num_layers=1, max_batch=2, num_q_heads=8, num_kv_heads=2, max_context=304, max_k=1, max_window=1, max_sinks=4, flags=flags)  # noqa: E731
+    make(0).close()
+    taken = []
+    for flags in (0, P.PRHS_CFG_NO_CHUNK_ATTN):
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        ctx = make(flags)
+        taken.append(free - torch.cuda.mem_get_info()[0])
+        if not flags:
+            ctx.close()
+    assert taken[0] - taken[1] >= 32 << 20
+    with pytest.raises(P.PrhsError) as e:
+        ctx.chunk_attn(t.qc, t.view(), 2, t.out, t.lse)
+    assert e.value.status == 2
+    ctx.dense_decode_attn(t.qc, t.view(), 2, t.out, t.lse)
+    assert ctx.check() == 0
+    compare(t)
+
+
+def test_a_context_in_tight_memory(cuda_device):
+    """A context that finds no memory for the chunk attention's workspace, or for less of it than it would take, serves the rest."""
+    t = fill(Batch(cuda_device, [300, 40], [1, 1], 1, 4, False, pad_rows=0))
+    make = lambda: P.Context(num_layers=1, max_batch=2, num_q_heads=4, num_kv_heads=1, max_context=1 << 19, max_k=1, max_window=1, max_sinks=4)  # noqa: E731
+    ctx = make()                                    # 158 MB of workspace, and every kernel loaded
+    for f in (ctx.dense_decode_attn, ctx.chunk_attn):
+        f(t.qc, t.view(), 2, t.out, t.lse)
+    assert ctx.check() == 0
+    ctx.close()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held, MB = [], 1 << 20
+    try:
+        for left in (130 * MB, 36 * MB):            # room for two rounds or one; for none
+            while True:
+                free = torch.cuda.mem_get_info()[0] - left
+                if free < 2 * MB:
+                    break
+                try:
+                    held.append(torch.empty(min(free, 4096 * MB) // (2 * MB) * (2 * MB), dtype=torch.uint8, device=cuda_device))
+                except torch.cuda.OutOfMemoryError:
+                    break
+            ctx = make()
+            t.out.fill_(math.nan)
+            ctx.dense_decode_attn(t.qc, t.view(), 2, t.out, t.lse)
+            assert ctx.check() == 0
+            compare(t)
+            t.out.fill_(math.nan)
+            if left > 39 * MB:
+                ctx.chunk_attn(t.qc, t.view(), 2, t.out, t.lse)
+                assert ctx.check() == 0
+                compare(t)
+            else:
+                with pytest.raises(P.PrhsError) as e:
+                    ctx.chunk_attn(t.qc, t.view(), 2, t.out, t.lse)
+                assert e.value.status == 3 and ctx.check() == 0
+            ctx.close()
+    finally:
+        del held
+        torch.cuda.empty_cache()
