@@ -80,11 +80,6 @@ cudaError_t tokens_set_attributes() {
     const cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.bytes);
     if (e != cudaSuccess) return e;
   }
-  // more than the 48 KB that every kernel may use
-  for (const void* k : {(const void*)qkv_append_kernel<kRotHalves>, (const void*)qkv_append_kernel<kRotAdjacent>, (const void*)qkv_append_kernel<kRotPartial>}) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kQkvMaxHeads * (int)sizeof(HeadPlace));
-    if (e != cudaSuccess) return e;
-  }
   return cudaSuccess;
 }
 

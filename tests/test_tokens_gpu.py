@@ -419,3 +419,23 @@ def test_refusals(cuda_device):
     with pytest.raises(P.PrhsError):
         ctx.bytekv_read(cache.view(), t.view(), 2, max_new=-1)
     assert ctx.check() == 0
+
+
+@pytest.mark.parametrize("rot,adjacent", [(128, False), (128, True), (90, False), (0, False)])
+def test_as_many_heads_as_there_is_room_for(cuda_device, rot, adjacent):
+    """512 heads of queries, keys and values beside the rotation's tables; more are refused."""
+    t = Batch(cuda_device, [5, 40], [2, 1], 32, 14, False)
+    inv = freqs(rot)
+    prep = P.make_qk_prep(norm=True, eps=1e-5, inv_freq=inv.to(cuda_device) if rot else None, adjacent=adjacent)
+    ctx = t.ctx()
+    ctx.qkv_append(t.q, t.k, t.v, t.view(), prep, 2, t.q_out, row_start=t.row_start)
+    assert ctx.check() == 0
+    for b, r, pos in t.tokens():
+        angle = np.array([pos], np.longdouble) * inv.numpy().astype(np.longdouble)
+        check(t.q_out[r], *prepared(np64(t.q[r]), None, True, 1e-5, angle, adjacent))
+        check(t.ck[b, :, pos], *prepared(np64(t.k[r]), None, True, 1e-5, angle, adjacent))
+        assert torch.equal(t.cv[b, :, pos], t.v[r])
+    t = Batch(cuda_device, [5], [2], 33, 14, False)
+    with pytest.raises(P.PrhsError) as e:
+        t.ctx().qkv_append(t.q, t.k, t.v, t.view(), prep, 1, t.q_out, row_start=t.row_start)
+    assert e.value.status == 2
