@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2602_08329_b200 import binding as P
-from tests.test_tokens_gpu import BF, Batch, freqs
+from tests.test_tokens_gpu import BF, Batch, bits, freqs
 
 pytestmark = pytest.mark.gpu
 S = 128 ** -0.5
@@ -433,13 +433,13 @@ def test_short_pieces_without_mending_after_launches_with_notes(cuda_device, pag
 
 def test_calls_are_sound_again_after_lengths_changed_under_way(cuda_device):
     """Another stream sets lengths while calls of several rounds are under way; after a check the next call is as ever."""
-    lens, new = [30000, 25000], [900, 1500]
+    lens, new = [40000, 20000], [4096, 2500]             # four rounds
     t = fill(Batch(cuda_device, lens, new, 8, 4, False, pad_rows=0))
     ctx = t.ctx()
     call(t, ctx)
     want = t.out.clone(), t.lse.clone()
     other = torch.cuda.Stream()
-    for i, wrong in enumerate(([3000, 2000], [30000, 30000], [900, 1500], [25000, 30000]) * 3):
+    for i, wrong in enumerate(([5000, 3000], [40000, 40000], [4096, 2500], [20000, 40000]) * 3):
         n = torch.tensor(wrong, dtype=torch.int32, device=cuda_device)
         torch.cuda.synchronize()
         for _ in range(3):
@@ -570,3 +570,52 @@ def test_a_context_in_tight_memory(cuda_device):
     finally:
         del held
         torch.cuda.empty_cache()
+
+
+def rows_of(t, b, rows, heads, sinks=0, window=0):
+    """out, lse and their bounds (float64) for some new tokens of sequence b and some heads, as reference()."""
+    T, n, out = t.lens[b], t.new[b], []
+    u = torch.tensor([T - n + 1 + r for r in rows], device=t.dev)
+    lo = torch.tensor([first_visible(int(x), window, 0.0) for x in u], device=t.dev)
+    i = torch.arange(T, device=t.dev)
+    see = (i < u[:, None]) & ((i < sinks) | (i >= lo[:, None]))
+    for h in heads:
+        k, v, q = t.full_k[b][h // t.G].double(), t.full_v[b][h // t.G].double(), t.qc[[t.starts[b] + r for r in rows], h].double()
+        a = (q @ k.T * S).masked_fill(~see, -math.inf)
+        z = torch.logsumexp(a, -1)
+        p = torch.exp(a - z[:, None])
+        y = p @ v
+        e = (S * 131 * 2.0 ** -23 * (q.abs() @ k.abs().T)).masked_fill(~see, 0.0).amax(-1)
+        out.append((y, z, 2.0 ** -8 * y.abs() + (2 * e + 2.0 ** -20 + T * 2.0 ** -22 + 2.0 ** -8)[:, None] * (p @ v.abs()) + 2.0 ** -134,
+                    e + 2.0 ** -20 + T * 2.0 ** -23 + 2.0 ** -22 * z.abs()))
+    return [torch.stack(x, 1) for x in zip(*out)]
+
+
+@pytest.mark.parametrize("lens,new,kv_heads,group,sinks,window", [([40000, 3000], [2300, 1500], 8, 4, 0, 0), ([60000, 130], [4200, 130], 8, 4, 0, 0),
+                                                                  ([24000, 9000, 24001], [2048, 0, 1999], 32, 1, 130, 17000)])
+def test_several_rounds(cuda_device, lens, new, kv_heads, group, sinks, window):
+    """From 56832 units of work (148 SMs, runs of 192) over more than 1024 tiles: three rounds, four, and two under a window with ungrouped heads.  Paged and
+    contiguous give the same bits, as a second call does, and a sample is right."""
+    got = []
+    mask = P.make_chunk_mask(sinks=sinks, window=window) if window else None
+    for paged in (False, True):
+        t = fill(Batch(cuda_device, lens, new, kv_heads, group, paged), k_amp=0.7)
+        ctx = P.Context(num_layers=1, max_batch=len(lens), num_q_heads=kv_heads * group, num_kv_heads=kv_heads, max_context=t.cap, max_k=1, max_window=1,
+                        max_sinks=4, page_size=16 if paged else 0)
+        for _ in range(2):
+            t.out.fill_(math.nan)
+            call(t, ctx, mask)
+            got.append((t.out.clone(), t.lse.clone()))
+    for out, lse in got[1:]:
+        assert torch.equal(bits(out), bits(got[0][0])) and torch.equal(lse.view(torch.int32), got[0][1].view(torch.int32))
+    live = t.starts[-1]
+    assert torch.isnan(t.out[live:]).all() and torch.isfinite(t.out[:live]).all() and torch.isfinite(t.lse[:live]).all()
+    heads = sorted({0, 1, t.Hq // 2, t.Hq - 1})
+    for b, n in enumerate(new):
+        if not n:
+            continue
+        rows = sorted({0, n - 1, n // 2} | set(range(5, n, max(1, n // 60))))
+        out, lse, tol, ltol = rows_of(t, b, rows, heads, sinks, window)
+        at = [t.starts[b] + r for r in rows]
+        assert ((t.out[at][:, heads].double() - out).abs() <= tol).all()
+        assert ((t.lse[at][:, heads].double() - lse).abs() <= ltol).all()

@@ -439,3 +439,98 @@ def test_as_many_heads_as_there_is_room_for(cuda_device, rot, adjacent):
     with pytest.raises(P.PrhsError) as e:
         t.ctx().qkv_append(t.q, t.k, t.v, t.view(), prep, 1, t.q_out, row_start=t.row_start)
     assert e.value.status == 2
+
+
+def bits(t):
+    return t.view(torch.int16)
+
+
+@pytest.mark.parametrize("rows", [470, 900, 3605, 7100])
+@pytest.mark.parametrize("rot,adjacent,axes", [(128, False, 3), (128, True, 0), (90, False, 0), (64, False, 2)])
+@pytest.mark.parametrize("kv_heads,group,paged", [(1, 3, False), (3, 5, True)])
+def test_append_of_many_rows(cuda_device, rows, rot, adjacent, axes, kv_heads, group, paged):
+    """Several rows per CTA (from six rows an SM on, up to eight), a last CTA that is not full, heads that are no multiple of four: the same to the
+    bit as calls of few rows, in which a CTA has one, and a sample against the formula."""
+    new = [rows // 2 - 3, 0, 1, rows // 5, 40]
+    new.append(rows - sum(new))
+    lens = [n + 17 * (i % 3) for i, n in enumerate(new)]
+    t = Batch(cuda_device, lens, new, kv_heads, group, paged, seed=rows)
+    g = torch.Generator().manual_seed(6)
+    inv = freqs(rot)
+    axis_of = [int(a) for a in torch.randint(0, axes, (rot // 2,), generator=g)] if axes else None
+    positions = torch.randint(-50, 5000, (axes, t.rows), generator=g, dtype=torch.int32).to(cuda_device) if axes else None
+    weights = [(1 + 0.3 * torch.randn(128, generator=g)).to(cuda_device) for _ in range(2)]
+    prep = P.make_qk_prep(*weights, eps=1e-5, inv_freq=inv.to(cuda_device), adjacent=adjacent, axis_of=axis_of)
+    if axis_of and max(axis_of) + 1 < axes:
+        positions = positions[:max(axis_of) + 1].contiguous()
+    ctx = t.ctx()
+    ctx.qkv_append(t.q, t.k, t.v, t.view(), prep, t.B, t.q_out, row_start=t.row_start, positions=positions)
+    # the same in calls of at most 97 rows, sequences cut wherever that falls
+    q2, k2, v2 = torch.full_like(t.q_out, math.nan), torch.full_like(t.ck, math.nan), torch.full_like(t.cv, math.nan)
+    for a in range(0, t.starts[-1], 97):
+        b = min(a + 97, t.starts[-1])
+        cut = [min(max(s, a), b) for s in t.starts]
+        have = [min(max(n - (t.starts[i + 1] - cut[i + 1]), 0), n) for i, n in enumerate(lens)]
+        dev = lambda x: torch.tensor(x, dtype=torch.int32, device=cuda_device)  # noqa: E731
+        view = P.make_view(k2, v2, dev(have), page_table=t.table)
+        ctx.qkv_append(t.q[a:b], t.k[a:b], t.v[a:b], view, prep, t.B, q2[a:b], row_start=dev([c - a for c in cut]),
+                       positions=None if positions is None else positions[:, a:b])
+    assert ctx.check() == 0
+    for x, y in ((t.q_out, q2), (t.ck, k2), (t.cv, v2)):
+        assert torch.equal(bits(x), bits(y))
+    x, q_out, ck, cv = t.x.cpu(), t.q_out.cpu(), t.ck.cpu(), t.cv.cpu()
+    table = None if t.table is None else t.table.cpu()
+    pos_cpu = None if positions is None else positions.cpu().numpy()
+    w = [np64(v) for v in weights]
+    n = 0
+    for b, r, pos in t.tokens():
+        where = (int(table[b, pos // 16]), slice(None), pos % 16) if paged else (b, slice(None), pos)
+        assert torch.equal(cv[where], x[r, t.Hq + t.H:])
+        n += 1
+        if r % 23 and r < t.starts[-1] - 9:
+            continue
+        at = [int(pos_cpu[a, r]) if axes else pos for a in (axis_of or [0] * (rot // 2))]
+        angle = np.array(at, np.longdouble) * inv.numpy().astype(np.longdouble)
+        check(q_out[r], *prepared(np64(x[r, :t.Hq]), w[0], True, 1e-5, angle, adjacent))
+        check(ck[where], *prepared(np64(x[r, t.Hq:t.Hq + t.H]), w[1], True, 1e-5, angle, adjacent))
+    assert torch.isnan(q_out[t.starts[-1]:]).all() and int((~torch.isnan(cv[..., 0])).sum()) == n * t.H
+
+
+@pytest.mark.parametrize("fmt,paged", [("e4m3", False), ("e5m2", True)])
+@pytest.mark.parametrize("rot,adjacent,axes", [(128, False, 3), (40, False, 0), (128, True, 2)])
+@pytest.mark.parametrize("kv_heads,group", [(32, 1), (8, 7)])
+@pytest.mark.parametrize("chunks", [[1] * 18, [5, 37, 1, 10, 16, 3], [9, 4900, 30]])
+def test_8_bit_append_of_many_heads_and_blocks(cuda_device, fmt, paged, rot, adjacent, axes, kv_heads, group, chunks):
+    """A block's heads over several CTAs (few blocks) and several heads to a warp (many blocks), tails that are closed and opened again, several
+    axes of positions: the bf16 call's rows through bytekv_append, and the one call, the same to the bit."""
+    H, G, B = kv_heads, group, 2
+    total = sum(chunks)
+    share = lambda c, b: c if b == 0 else c // 3  # noqa: E731
+    g = torch.Generator().manual_seed(2)
+    one, two = (Cache(fmt, B, H, total + 16, paged, cuda_device, seed=4) for _ in range(2))
+    axis_of = [i % axes for i in range(rot // 2)] if axes else None
+    prep = P.make_qk_prep((1 + 0.2 * torch.randn(128, generator=g)).to(cuda_device), None, inv_freq=freqs(rot).to(cuda_device), adjacent=adjacent,
+                          axis_of=axis_of)
+    ctx = P.Context(num_layers=1, max_batch=B, num_q_heads=H * G, num_kv_heads=H, max_context=one.cap, max_k=16, max_window=16, max_sinks=4,
+                    page_size=16 if paged else 0)
+    have = [0] * B
+    for i, c in enumerate(chunks):
+        new = [share(c, b) for b in range(B)]
+        have = [h + n for h, n in zip(have, new)]
+        t = Batch(cuda_device, have, new, H, G, False, seed=10 + i)
+        positions = torch.randint(0, 9000, (axes, t.rows), generator=g, dtype=torch.int32).to(cuda_device) if axes else None
+        for cache in (one, two):
+            cache.set_lens(have)
+        t.ctx().qkv_append(t.q, t.k, t.v, t.view(), prep, B, t.q_out, row_start=t.row_start, positions=positions)
+        most = max(max(new), 1)
+        rows = torch.full((2, B, H, most, 128), math.nan, dtype=BF, device=cuda_device)
+        for b in range(B):
+            rows[0, b, :, :new[b]] = t.ck[b, :, have[b] - new[b]:have[b]]
+            rows[1, b, :, :new[b]] = t.cv[b, :, have[b] - new[b]:have[b]]
+        ctx.bytekv_append(rows[0], rows[1], torch.tensor(new, dtype=torch.int32, device=cuda_device), one.view(), B)
+        q_out = torch.full_like(t.q_out, math.nan)
+        ctx.bytekv_qkv_append(t.q, t.k, t.v, two.view(), prep, B, q_out, row_start=t.row_start, positions=positions)
+        assert ctx.check() == 0
+        assert torch.equal(bits(q_out), bits(t.q_out))
+        for a, b in zip(bytes_of(one), bytes_of(two)):
+            assert torch.equal(a, b)
