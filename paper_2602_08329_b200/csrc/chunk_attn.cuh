@@ -33,6 +33,7 @@
 // is merged are fp32.
 #pragma once
 #include <cuda.h>
+#include <float.h>
 
 #include "attn_group_umma.cuh"
 #include "chunk_walk.cuh"
@@ -67,7 +68,8 @@ constexpr int kCAMmaWarp = 8, kCALoadWarp = 9, kCAMendWarp = 10;
 constexpr int kCASlotFloats = 2 * kCATile * kHeadDim + 2 * kCATile * 2;      // a piece in the workspace: O [2][32][128] float4, (m, l) [2][128]
 constexpr uint32_t kCAIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kCATile >> 3) << 17) | ((uint32_t)(kCATile >> 4) << 24);
 constexpr uint32_t kCAIdescPV = kCAIdesc | (1u << 16);    // B = V tile read MN-major
-// A row's reference moves where a logit exceeds it by 2^kCAGap; up to 2^kCAFar the weights stand (bf16 and fp32 have the range).
+// A row's reference moves where a logit exceeds it by 2^kCAGap; up to 2^kCAFar the weights stand (bf16 and fp32 have the range:
+// 128 keys of values up to 2^50, in 592 pieces).
 constexpr float kCAGap = 8.f, kCAFar = 60.f;
 // ------------------------------------------------------------------------------------ instructions
 __device__ __forceinline__ void tma_load_2d_plain(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar) {
@@ -501,13 +503,13 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
           // tokens the rows of the weights' low parts too, and a quarter of the columns.
           const int sub0 = x.halves() ? 0 : s, subs = x.halves() ? 2 : 1, n = parts * subs;
           const int c_begin = kFew ? 64 * s + 32 * (row >> 6) : x.halves() ? 64 * s : 0, c_end = c_begin + (kFew ? 32 : x.halves() ? 64 : 128);
-          float M = -INFINITY, L = 0.f;
+          float M = 0.f, L = 0.f;
 #pragma unroll 1
           for (int c0 = c_begin; c0 < c_end; c0 += 32) {
             float acc[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) acc[j] = 0.f;
-            M = -INFINITY;
+            M = -FLT_MAX;                // (below or at every finite reference, so that no difference is of two infinities of one sign)
             L = 0.f;
 #pragma unroll 2
             for (int i = 0; i < n; ++i) {
@@ -523,10 +525,8 @@ chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 for (int j = 0; j < 8; ++j) low[j] = __ldcg(o + j * kCATile + 64);
               }
               if (v.y < 0.f) continue;                                // (no tiles, and O was not written)
-              // A piece whose logits are all -inf has no weight, but still zero times its values that are not finite.
-              const float mn = fmaxf(M, v.x);
-              const bool none = mn == -INFINITY;
-              const float f = none ? 1.f : exp2f(M - mn), g = none ? 1.f : exp2f(v.x - mn);
+              // (a piece whose logits are all -inf: v.x = -inf, g = 0, and zero times its values that are not finite)
+              const float mn = fmaxf(M, v.x), f = exp2f(M - mn), g = exp2f(v.x - mn);
               M = mn;
               L = fmaf(v.y, g, L * f);
 #pragma unroll

@@ -619,3 +619,20 @@ def test_several_rounds(cuda_device, lens, new, kv_heads, group, sinks, window):
         at = [t.starts[b] + r for r in rows]
         assert ((t.out[at][:, heads].double() - out).abs() <= tol).all()
         assert ((t.lse[at][:, heads].double() - lse).abs() <= ltol).all()
+
+
+@pytest.mark.parametrize("lens,new,group", [([20000], [2], 4), ([3000, 300], [700, 300], 4), ([9000], [200], 1)])
+def test_large_values_under_logits_that_jump(cuda_device, lens, new, group):
+    """Values of 2^50, and logits that rise by 58 binary orders from one stretch of tiles to the next: weights up to 2^58 against the reference that
+    stands, nothing overflows."""
+    t = fill(Batch(cuda_device, lens, new, 1, group, False, pad_rows=0))
+    t.qc.fill_(4.0)
+    high = 58 * math.log(2.0) / (4 * 128 * S)
+    for b, n in enumerate(lens):
+        stretch = torch.arange(n, device=cuda_device) // 128 % 5
+        t.full_k[b][:] = torch.where(stretch == 2, high, 0.0).to(BF)[None, :, None]
+        t.full_v[b] = (t.full_v[b].sign() * 2.0 ** 50).to(BF)
+        t.full_v[b][..., :64] = 2.0 ** 50
+    store(t)
+    call(t)
+    compare(t)
