@@ -523,6 +523,11 @@ typedef struct {
  * A token that sees nothing (sinks = 0, P = u), or nothing but logits of -inf, has a zero row and lse = -inf.  A NaN or +inf logit makes the
  * row and its lse NaN; a value that is infinite or NaN makes its coordinate infinite or NaN for the tokens that see it (also where its
  * weight is zero), and for no others.  A page id outside the pool is recorded (PRHS_FLAG_BAD_PAGE); its rows count as zeros.
+ * Logits, sums and results are held in fp32.  The weights of the softmax enter the product with V as one bf16 (off by at most 2^-8 of each; 0.0021 to
+ * 0.0024 of a result's norm instead of the 0.0017 that its own rounding is).  In calls of few tokens, num_rows <= batch * floor(64 / group), they
+ * enter as two (2^-16).  Finite values up to 2^50 in magnitude do not overflow on the way, whatever the logits.
+ * Such calls of few tokens have a kernel of their own, which a long part of a prompt among many single tokens would be slow in (up to 2.5 times):
+ * put the part into a call of its own.
  * seq_lens and row_start are read more than once and must not change while the call is under way.  If they do, its results mean nothing, the change
  * is recorded (PRHS_FLAG_BAD_LENGTH) where it is noticed, and calls are sound again after a prhs_check.
  * PRHS_ERR_UNSUPPORTED where the driver offers no tensor-map encoder, or with PRHS_CFG_NO_CHUNK_ATTN; PRHS_ERR_OOM where prhs_create had no memory

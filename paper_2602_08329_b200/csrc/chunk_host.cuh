@@ -110,6 +110,14 @@ prhs_status prhs_chunk_attn(prhs_ctx* ctx, const void* q, const int32_t* row_sta
                                   (unsigned long long)(paged ? kBlockRows : max_t);
   if (rows >= (1ull << 31) - kCATile) return fail(ctx, PRHS_ERR_UNSUPPORTED, "chunk attention: a cache of 2^31 rows or more");
   p.group = ctx->gq;
+  // Few tokens: at most 64 / G rows per sequence on average (padding counts), for then an item of 64 rows holds all new tokens of a sequence.
+  // Both kernels on both sides, us, 8 KV heads of 4, 16 sequences of n new tokens: at 4096 positions n = 1, 8, 16, 17, 32: few 71, 74, 86,
+  // 146, 158, general 76, 77, 81, 81, 81; at 16384 n = 1, 8, 16, 17: 222, 225, 254, 460 against 230, 232, 243, 245; one sequence of 2047,
+  // n = 1, 4, 16: 27, 27, 30 against 31, 31, 32.  From n = 12 on it is the weights' second part that is paid for.
+  // The average does not see a long part among single tokens, whose items are then 64 rows too: 63 single tokens and one part of 256 or 900 at
+  // 4096 positions take 360 and 520 us against 269 and 312 in the general kernel, at 16384 positions 1144 and 1695 against 1000 and
+  // 1233; with the part alone at 65536 positions 3365 against 1342.  The host does not know the rows of a sequence; a caller
+  // who does makes two calls.
   const bool few = num_rows <= (long long)batch * (kCATile / 2 / ctx->gq);
   p.tokens = (few ? kCATile / 2 : kCATile) / ctx->gq;
   alignas(64) CUtensorMap tm_q, tm_k, tm_v;
